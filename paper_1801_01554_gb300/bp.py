@@ -1,4 +1,4 @@
-"""ctypes binding of libbp.so (the C ABI declared in include/bp.h).
+"""ctypes binding of libbp.so (the C ABI declared in include/bp.h and include/bp_experts.h).
 
 Argument marshalling only: every step of the back-propagation path runs in the
 library's CUDA kernels.  Functions keep the C names; device buffers are passed
@@ -21,8 +21,10 @@ STATUS_NAMES = ["BP_OK", "BP_EINVAL", "BP_ENOMEM", "BP_ECUDA", "BP_ESHAPE", "BP_
 BP_F32, BP_BF16 = 0, 1
 BP_SIGMOID_LOGISTIC, BP_SIGMOID_TABLE = 0, 1
 BP_MAX_SIZES = 9
+BP_MAX_EXPERTS, BP_MAX_CHOICES, BP_MAX_RANK = 512, 16, 128
+BP_GATES_CHOSEN, BP_GATES_ALL = 0, 1
 
-# name -> (restype, argtypes); every symbol declared in include/bp.h
+# name -> (restype, argtypes); every symbol declared in include/bp.h and include/bp_experts.h
 _VP = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
@@ -54,6 +56,23 @@ SIGNATURES = {
                                     _VP, _VP, _VP]),
     "bp_debug_wait_test": (_I, [_VP, ctypes.c_ulonglong, _I]),
     "bp_last_error": (ctypes.c_char_p, []),
+    "bp_router_create": (_I, [_I, _I, _I, _I, _I, ctypes.POINTER(_VP)]),
+    "bp_router_destroy": (None, [_VP]),
+    "bp_route": (_I, [_VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "bp_route_backward": (_I, [_VP, _VP, _I, _VP, _VP, _VP, _VP, _VP]),
+    "bp_mix": (_I, [_VP, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP]),
+    "bp_mix_backward": (_I, [_VP, _VP, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP]),
+    "bp_experts_create": (_I, [_I, _I, _I, _I, _I, ctypes.POINTER(_VP)]),
+    "bp_experts_destroy": (None, [_VP]),
+    "bp_experts_forward": (_I, [_VP, _VP, _VP, _VP, _I, _VP, _VP, _I, _I, _VP, _VP]),
+    "bp_experts_backward": (_I, [_VP, _VP, _VP, _I, _VP, _VP, _I, _VP, _I, _VP, _VP, _VP, _I, _VP]),
+    "bp_experts_check": (_I, [_VP, _VP]),
+    "bp_adapters_create": (_I, [_I, _I, _I, _I, _I, _I, _I, ctypes.POINTER(_VP)]),
+    "bp_adapters_destroy": (None, [_VP]),
+    "bp_adapters_forward": (_I, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _I, _VP, _VP, _VP]),
+    "bp_adapters_backward": (_I, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _VP, _I, _VP, _VP,
+                                  _VP, _I, _VP]),
+    "bp_adapters_check": (_I, [_VP, _VP]),
 }
 
 
@@ -279,7 +298,243 @@ def bp_last_error() -> str:
     return load().bp_last_error().decode()
 
 
+# ------------------------------------------------- C names of include/bp_experts.h
+def _typed(x, dtype, what):
+    """Device address as _dptr, of a tensor whose element type is checked: the kernels read
+    raw memory, and an int64 index or a float64 gate would be read as something else."""
+    if x is None or isinstance(x, int):
+        return x
+    name = str(x.dtype)
+    if name != dtype:
+        raise ValueError(f"{what} must be {dtype} (got {name})")
+    return _dptr(x)
+
+
+def _room(**needed):
+    """Refuses tensors that are shorter than what the kernels read or write there."""
+    for what, (x, n) in needed.items():
+        if x is not None and not isinstance(x, int) and x.numel() < n:
+            raise ValueError(f"{what} holds {x.numel()} values; the call needs {n}")
+
+
+def _values(x, dtype, what):
+    return _typed(x, "torch.bfloat16" if dtype == BP_BF16 else "torch.float32", what)
+
+
+def _ints(x, what):
+    return _typed(x, "torch.int32", what)
+
+
+def _floats(x, what):
+    return _typed(x, "torch.float32", what)
+
+
+def bp_router_create(n_experts, k, dtype=BP_F32, max_patterns=1024, gates=BP_GATES_CHOSEN):
+    out = ctypes.c_void_p()
+    _check(load().bp_router_create(int(n_experts), int(k), int(dtype), int(max_patterns), int(gates),
+                                   ctypes.byref(out)))
+    return out.value
+
+
+def bp_router_destroy(h):
+    load().bp_router_destroy(h)
+
+
+def bp_route(h, logits, n, expert, gate, offsets, source, place, dtype=BP_F32, stream=None):
+    _check(load().bp_route(h, _values(logits, dtype, "logits"), int(n), _ints(expert, "expert"),
+                           _floats(gate, "gate"), _ints(offsets, "offsets"), _ints(source, "source"),
+                           _ints(place, "place"), _stream(stream)))
+
+
+def bp_route_backward(h, logits, n, expert, gate, dgate, dlogits, dtype=BP_F32, stream=None):
+    _check(load().bp_route_backward(h, _values(logits, dtype, "logits"), int(n), _ints(expert, "expert"),
+                                    _floats(gate, "gate"), _floats(dgate, "dgate"),
+                                    _values(dlogits, dtype, "dlogits"), _stream(stream)))
+
+
+def bp_mix(H, n_rows, place, gate, n, k, n_out, dtype, Y, stream=None):
+    _room(H=(H, n_rows * n_out), place=(place, n * k), gate=(gate, n * k), Y=(Y, n * n_out))
+    _check(load().bp_mix(_values(H, dtype, "H"), int(n_rows), _ints(place, "place"), _floats(gate, "gate"),
+                         int(n), int(k), int(n_out), int(dtype), _values(Y, dtype, "Y"), _stream(stream)))
+
+
+def bp_mix_backward(D, H, n_rows, place, gate, n, k, n_out, dtype, dH, dgate=None, stream=None):
+    _room(D=(D, n * n_out), H=(H, n_rows * n_out), place=(place, n * k), gate=(gate, n * k),
+          dH=(dH, n_rows * n_out), dgate=(dgate, n * k))
+    _check(load().bp_mix_backward(_values(D, dtype, "D"), _values(H, dtype, "H"), int(n_rows),
+                                  _ints(place, "place"), _floats(gate, "gate"), int(n), int(k), int(n_out),
+                                  int(dtype), _values(dH, dtype, "dH"), _floats(dgate, "dgate"),
+                                  _stream(stream)))
+
+
+def bp_experts_create(n_experts, n_in, n_out, dtype=BP_F32, max_rows=1024):
+    out = ctypes.c_void_p()
+    _check(load().bp_experts_create(int(n_experts), int(n_in), int(n_out), int(dtype), int(max_rows),
+                                    ctypes.byref(out)))
+    return out.value
+
+
+def bp_experts_destroy(h):
+    load().bp_experts_destroy(h)
+
+
+def bp_experts_forward(h, W, b, X, n_x, source, offsets, n_rows, Y, squash=False, dtype=BP_F32, stream=None):
+    _check(load().bp_experts_forward(h, _values(W, dtype, "W"), _floats(b, "b"), _values(X, dtype, "X"),
+                                     int(n_x), _ints(source, "source"), _ints(offsets, "offsets"),
+                                     int(n_rows), int(bool(squash)), _values(Y, dtype, "Y"), _stream(stream)))
+
+
+def bp_experts_backward(h, W, X, n_x, source, offsets, n_rows, D, dX=None, GW=None, Gb=None, squash=False,
+                        accumulate=False, dtype=BP_F32, stream=None):
+    _check(load().bp_experts_backward(h, _values(W, dtype, "W"), _values(X, dtype, "X"), int(n_x),
+                                      _ints(source, "source"), _ints(offsets, "offsets"), int(n_rows),
+                                      _values(D, dtype, "D"), int(bool(squash)), _values(dX, dtype, "dX"),
+                                      _floats(GW, "GW"), _floats(Gb, "Gb"), int(bool(accumulate)),
+                                      _stream(stream)))
+
+
+def bp_experts_check(h, stream=None):
+    _check(load().bp_experts_check(h, _stream(stream)))
+
+
+def bp_adapters_create(n_adapters, rank, n_in, n_out, dtype=BP_F32, max_rows=1024, max_requests=64):
+    out = ctypes.c_void_p()
+    _check(load().bp_adapters_create(int(n_adapters), int(rank), int(n_in), int(n_out), int(dtype),
+                                     int(max_rows), int(max_requests), ctypes.byref(out)))
+    return out.value
+
+
+def bp_adapters_destroy(h):
+    load().bp_adapters_destroy(h)
+
+
+def bp_adapters_forward(h, W, b, A, B, scale, X, offsets, adapter, n_requests, n_rows, U, Y, squash=False,
+                        dtype=BP_F32, stream=None):
+    _check(load().bp_adapters_forward(h, _values(W, dtype, "W"), _floats(b, "b"), _values(A, dtype, "A"),
+                                      _values(B, dtype, "B"), _floats(scale, "scale"), _values(X, dtype, "X"),
+                                      _ints(offsets, "offsets"), _ints(adapter, "adapter"), int(n_requests),
+                                      int(n_rows), int(bool(squash)), _floats(U, "U"), _values(Y, dtype, "Y"),
+                                      _stream(stream)))
+
+
+def bp_adapters_backward(h, W, A, B, scale, X, U, offsets, adapter, n_requests, n_rows, D, dX=None, GA=None,
+                         GB=None, squash=False, accumulate=False, dtype=BP_F32, stream=None):
+    _check(load().bp_adapters_backward(h, _values(W, dtype, "W"), _values(A, dtype, "A"),
+                                       _values(B, dtype, "B"), _floats(scale, "scale"),
+                                       _values(X, dtype, "X"), _floats(U, "U"), _ints(offsets, "offsets"),
+                                       _ints(adapter, "adapter"), int(n_requests), int(n_rows),
+                                       _values(D, dtype, "D"), int(bool(squash)), _values(dX, dtype, "dX"),
+                                       _floats(GA, "GA"), _floats(GB, "GB"), int(bool(accumulate)),
+                                       _stream(stream)))
+
+
+def bp_adapters_check(h, stream=None):
+    _check(load().bp_adapters_check(h, _stream(stream)))
+
+
 # ------------------------------------------------------------------ convenience
+class _Handle:
+    """A handle of the library, freed by close() or at the end of a with block."""
+
+    _free = None
+
+    def close(self):
+        if getattr(self, "h", None):
+            type(self)._free(self.h)
+            self.h = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Router(_Handle):
+    """Owns one bp_router handle; methods forward to bp_route and bp_route_backward."""
+
+    _free = staticmethod(bp_router_destroy)
+
+    def __init__(self, n_experts, k, dtype=BP_F32, max_patterns=1024, gates=BP_GATES_CHOSEN):
+        self.n_experts, self.k, self.dtype = int(n_experts), int(k), dtype
+        self.h = bp_router_create(n_experts, k, dtype, max_patterns, gates)
+
+    def forward(self, logits, n, expert, gate, offsets, source, place, stream=None):
+        _room(logits=(logits, n * self.n_experts), expert=(expert, n * self.k), gate=(gate, n * self.k),
+              offsets=(offsets, self.n_experts + 1), source=(source, n * self.k), place=(place, n * self.k))
+        bp_route(self.h, logits, n, expert, gate, offsets, source, place, self.dtype, stream)
+
+    def backward(self, logits, n, expert, gate, dgate, dlogits, stream=None):
+        _room(logits=(logits, n * self.n_experts), expert=(expert, n * self.k), gate=(gate, n * self.k),
+              dgate=(dgate, n * self.k), dlogits=(dlogits, n * self.n_experts))
+        bp_route_backward(self.h, logits, n, expert, gate, dgate, dlogits, self.dtype, stream)
+
+
+class Experts(_Handle):
+    """Owns one bp_experts handle; methods forward to the C names above."""
+
+    _free = staticmethod(bp_experts_destroy)
+
+    def __init__(self, n_experts, n_in, n_out, dtype=BP_F32, max_rows=1024):
+        self.n_experts, self.n_in, self.n_out, self.dtype = int(n_experts), int(n_in), int(n_out), dtype
+        self.h = bp_experts_create(n_experts, n_in, n_out, dtype, max_rows)
+
+    def forward(self, W, b, X, n_x, source, offsets, n_rows, Y, squash=False, stream=None):
+        E, i, o = self.n_experts, self.n_in, self.n_out
+        _room(W=(W, E * o * i), b=(b, E * o), X=(X, n_x * i), source=(source, n_rows), offsets=(offsets, E + 1),
+              Y=(Y, n_rows * o))
+        bp_experts_forward(self.h, W, b, X, n_x, source, offsets, n_rows, Y, squash, self.dtype, stream)
+
+    def backward(self, W, X, n_x, source, offsets, n_rows, D, dX=None, GW=None, Gb=None, squash=False,
+                 accumulate=False, stream=None):
+        E, i, o = self.n_experts, self.n_in, self.n_out
+        _room(W=(W, E * o * i), X=(X, n_x * i), source=(source, n_rows), offsets=(offsets, E + 1),
+              D=(D, n_rows * o), dX=(dX, n_rows * i), GW=(GW, E * o * i), Gb=(Gb, E * o))
+        bp_experts_backward(self.h, W, X, n_x, source, offsets, n_rows, D, dX, GW, Gb, squash, accumulate,
+                            self.dtype, stream)
+
+    def check(self, stream=None):
+        bp_experts_check(self.h, stream)
+
+
+class Adapters(_Handle):
+    """Owns one bp_adapters handle; methods forward to the C names above."""
+
+    _free = staticmethod(bp_adapters_destroy)
+
+    def __init__(self, n_adapters, rank, n_in, n_out, dtype=BP_F32, max_rows=1024, max_requests=64):
+        self.n_adapters, self.rank, self.dtype = int(n_adapters), int(rank), dtype
+        self.n_in, self.n_out = int(n_in), int(n_out)
+        self.h = bp_adapters_create(n_adapters, rank, n_in, n_out, dtype, max_rows, max_requests)
+
+    def forward(self, W, b, A, B, scale, X, offsets, adapter, n_requests, n_rows, U, Y, squash=False,
+                stream=None):
+        a, r, i, o = self.n_adapters, self.rank, self.n_in, self.n_out
+        _room(W=(W, o * i), b=(b, o), A=(A, a * r * i), B=(B, a * r * o), scale=(scale, a), X=(X, n_rows * i),
+              offsets=(offsets, n_requests + 1), adapter=(adapter, n_requests), U=(U, n_rows * r),
+              Y=(Y, n_rows * o))
+        bp_adapters_forward(self.h, W, b, A, B, scale, X, offsets, adapter, n_requests, n_rows, U, Y, squash,
+                            self.dtype, stream)
+
+    def backward(self, W, A, B, scale, X, U, offsets, adapter, n_requests, n_rows, D, dX=None, GA=None,
+                 GB=None, squash=False, accumulate=False, stream=None):
+        a, r, i, o = self.n_adapters, self.rank, self.n_in, self.n_out
+        _room(W=(W, o * i), A=(A, a * r * i), B=(B, a * r * o), scale=(scale, a), X=(X, n_rows * i),
+              U=(U, n_rows * r), offsets=(offsets, n_requests + 1), adapter=(adapter, n_requests),
+              D=(D, n_rows * o), dX=(dX, n_rows * i), GA=(GA, a * r * i), GB=(GB, a * r * o))
+        bp_adapters_backward(self.h, W, A, B, scale, X, U, offsets, adapter, n_requests, n_rows, D, dX, GA, GB,
+                             squash, accumulate, self.dtype, stream)
+
+    def check(self, stream=None):
+        bp_adapters_check(self.h, stream)
+
+
 class Net:
     """Owns one bp_net handle; methods forward to the C names above."""
 

@@ -1,0 +1,501 @@
+// C ABI of the router, the mix, and the expert and adapter layers (include/bp_experts.h):
+// argument checks, handles and the choice of kernels.
+#include <cuda_runtime.h>
+
+#include <climits>
+#include <cstdarg>
+#include <cstdio>
+#include <new>
+
+#include "bp_experts_internal.h"
+
+using namespace bp;
+
+struct bp_router {
+    int E = 0, k = 0, dtype = BP_F32, cap = 0, gates = BP_GATES_CHOSEN;
+    int* hist = nullptr;
+};
+
+struct bp_experts {
+    int E = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0;
+    int* flags = nullptr;
+};
+
+struct bp_adapters {
+    int n = 0, rank = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, max_requests = 0;
+    int* flags = nullptr;
+    float* low = nullptr;   // [cap, rank] v of the backward pass
+};
+
+namespace {
+
+constexpr int kMaxUnits = 1 << 20;
+constexpr int kMaxAdapters = 65535;   // a grid dimension
+
+bp_status fail(bp_status st, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    set_error_message(buf);
+    return st;
+}
+
+bp_status cuda_status(cudaError_t e, const char* what) {
+    if (e == cudaSuccess) return BP_OK;
+    return fail(e == cudaErrorMemoryAllocation ? BP_ENOMEM : BP_ECUDA, "%s: %s (%s)", what, cudaGetErrorName(e),
+                cudaGetErrorString(e));
+}
+
+// A buffer that a call reads or writes: present unless the call has no rows for it, and aligned.
+struct Buffer {
+    const void* p;
+    const char* name;
+    int align;
+    bool needed;
+};
+template <int N>
+bp_status check_buffers(const char* call, const Buffer (&b)[N]) {
+    for (const Buffer& x : b) {
+        if (x.p == nullptr && x.needed) return fail(BP_EINVAL, "%s: %s is NULL", call, x.name);
+        if (((uintptr_t)x.p & (uintptr_t)(x.align - 1)) != 0)
+            return fail(BP_EINVAL, "%s: %s must be %d-byte aligned", call, x.name, x.align);
+    }
+    return BP_OK;
+}
+
+bp_status check_dtype(const char* call, int dtype) {
+    if (dtype == BP_F32 || dtype == BP_BF16) return BP_OK;
+    return fail(BP_EINVAL, "%s: unknown dtype %d", call, dtype);
+}
+
+bp_status check_range(const char* call, const char* what, long long v, long long lo, long long hi) {
+    if (v >= lo && v <= hi) return BP_OK;
+    return fail(BP_EINVAL, "%s: %s must be in [%lld, %lld] (got %lld)", call, what, lo, hi, v);
+}
+
+bp_status check_units(const char* call, int n_in, int n_out, int dtype) {
+    bp_status st = check_range(call, "n_in", n_in, 1, kMaxUnits);
+    if (st == BP_OK) st = check_range(call, "n_out", n_out, 1, kMaxUnits);
+    if (st == BP_OK && dtype == BP_BF16 && (n_in % 8 != 0 || n_out % 8 != 0))
+        st = fail(BP_ESHAPE, "%s: bfloat16 layers need n_in and n_out to be multiples of 8 (got %d and %d)", call,
+                  n_in, n_out);
+    return st;
+}
+
+bp_status make_flags(int** flags, const char* call) {
+    cudaError_t e = cudaMalloc(flags, sizeof(int));
+    if (e == cudaSuccess) e = cudaMemset(*flags, 0, sizeof(int));
+    return cuda_status(e, call);
+}
+
+bp_status read_flags(int* flags, void* stream, const char* call) {
+    int f = 0;
+    cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
+    if (e == cudaSuccess) e = cudaMemcpy(&f, flags, sizeof f, cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess && f != 0) e = cudaMemset(flags, 0, sizeof f);
+    if (e != cudaSuccess) return cuda_status(e, call);
+    if (f & kFlagTimeout)
+        return fail(BP_ETIMEOUT, "a bounded device-side wait ran out; the launch stopped early");
+    if (f & kFlagBounds)
+        return fail(BP_ESTATE, "an offset, source row or adapter of a call was out of range");
+    return BP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+// ------------------------------------------------------------ router
+bp_status bp_router_create(int n_experts, int k, int dtype, int max_patterns, int gates, bp_router** out) {
+    const char* call = "bp_router_create";
+    set_error_message("");
+    if (out == nullptr) return fail(BP_EINVAL, "%s: NULL argument", call);
+    bp_status st = check_range(call, "n_experts", n_experts, 1, BP_MAX_EXPERTS);
+    if (st == BP_OK) st = check_range(call, "k", k, 1, n_experts < BP_MAX_CHOICES ? n_experts : BP_MAX_CHOICES);
+    if (st == BP_OK) st = check_dtype(call, dtype);
+    if (st == BP_OK) st = check_range(call, "max_patterns", max_patterns, 1, INT_MAX / k);
+    if (st == BP_OK && gates != BP_GATES_CHOSEN && gates != BP_GATES_ALL)
+        st = fail(BP_EINVAL, "%s: unknown gates %d", call, gates);
+    if (st != BP_OK) return st;
+    bp_router* r = new (std::nothrow) bp_router();
+    if (r == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
+    r->E = n_experts;
+    r->k = k;
+    r->dtype = dtype;
+    r->cap = max_patterns;
+    r->gates = gates;
+    const size_t blocks = ((size_t)max_patterns + kRoutePatterns - 1) / kRoutePatterns;
+    st = cuda_status(cudaMalloc(&r->hist, (blocks + 1) * n_experts * sizeof(int)), call);
+    if (st != BP_OK) {
+        delete r;
+        return st;
+    }
+    *out = r;
+    return BP_OK;
+}
+
+void bp_router_destroy(bp_router* r) {
+    if (r == nullptr) return;
+    cudaDeviceSynchronize();
+    cudaFree(r->hist);
+    delete r;
+}
+
+bp_status bp_route(bp_router* r, const void* d_logits, int n, int* d_expert, float* d_gate, int* d_offsets,
+                   int* d_source, int* d_place, void* stream) {
+    const char* call = "bp_route";
+    if (r == nullptr) return fail(BP_EINVAL, "%s: NULL router", call);
+    bp_status st = check_range(call, "n", n, 0, r->cap);
+    const bool rows = n > 0;
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_logits, "d_logits", r->dtype == BP_BF16 ? 2 : 4, rows},
+                                  {d_expert, "d_expert", 4, rows},
+                                  {d_gate, "d_gate", 4, rows},
+                                  {d_offsets, "d_offsets", 4, true},
+                                  {d_source, "d_source", 4, rows},
+                                  {d_place, "d_place", 4, rows}});
+    if (st != BP_OK) return st;
+    const RouteArgs a{n, r->E, r->k, r->gates, r->dtype, d_logits, d_expert, d_gate, d_offsets, d_source, d_place, r->hist};
+    return cuda_status(route_forward(a, (cudaStream_t)stream), call);
+}
+
+bp_status bp_route_backward(bp_router* r, const void* d_logits, int n, const int* d_expert, const float* d_gate,
+                            const float* d_dgate, void* d_dlogits, void* stream) {
+    const char* call = "bp_route_backward";
+    if (r == nullptr) return fail(BP_EINVAL, "%s: NULL router", call);
+    bp_status st = check_range(call, "n", n, 0, r->cap);
+    const bool rows = n > 0;
+    const int align = r->dtype == BP_BF16 ? 2 : 4;
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_logits, "d_logits", align, rows},
+                                  {d_expert, "d_expert", 4, rows},
+                                  {d_gate, "d_gate", 4, rows},
+                                  {d_dgate, "d_dgate", 4, rows},
+                                  {d_dlogits, "d_dlogits", align, rows}});
+    if (st != BP_OK || !rows) return st;
+    const RouteArgs a{n, r->E, r->k, r->gates, r->dtype, d_logits, const_cast<int*>(d_expert),
+                      const_cast<float*>(d_gate), nullptr, nullptr, nullptr, r->hist};
+    return cuda_status(route_backward(a, d_dgate, d_dlogits, (cudaStream_t)stream), call);
+}
+
+// ------------------------------------------------------------ mix
+static bp_status check_mix(const char* call, int n_rows, int n, int k, int n_out, int dtype) {
+    bp_status st = check_dtype(call, dtype);
+    if (st == BP_OK) st = check_range(call, "k", k, 1, BP_MAX_CHOICES);
+    if (st == BP_OK) st = check_range(call, "n", n, 0, INT_MAX / k);
+    if (st == BP_OK) st = check_range(call, "n_rows", n_rows, 0, INT_MAX);
+    if (st == BP_OK) st = check_units(call, 8, n_out, dtype);
+    return st;
+}
+
+bp_status bp_mix(const void* d_H, int n_rows, const int* d_place, const float* d_gate, int n, int k, int n_out,
+                 int dtype, void* d_Y, void* stream) {
+    const char* call = "bp_mix";
+    bp_status st = check_mix(call, n_rows, n, k, n_out, dtype);
+    const int align = dtype == BP_BF16 ? 16 : 4;
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_H, "d_H", align, n > 0 && n_rows > 0},
+                                  {d_place, "d_place", 4, n > 0},
+                                  {d_gate, "d_gate", 4, false},
+                                  {d_Y, "d_Y", align, n > 0}});
+    if (st != BP_OK || n == 0) return st;
+    MixArgs a{};
+    a.n = n, a.k = k, a.n_rows = n_rows, a.N = n_out, a.dtype = dtype;
+    a.H = d_H, a.place = d_place, a.gate = d_gate, a.Y = d_Y;
+    return cuda_status(mix_forward(a, (cudaStream_t)stream), call);
+}
+
+bp_status bp_mix_backward(const void* d_D, const void* d_H, int n_rows, const int* d_place, const float* d_gate, int n,
+                          int k, int n_out, int dtype, void* d_dH, float* d_dgate, void* stream) {
+    const char* call = "bp_mix_backward";
+    bp_status st = check_mix(call, n_rows, n, k, n_out, dtype);
+    const int align = dtype == BP_BF16 ? 16 : 4;
+    const bool rows = n > 0 && n_rows > 0;
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_D, "d_D", align, n > 0},
+                                  {d_H, "d_H", align, rows && d_dgate != nullptr},
+                                  {d_place, "d_place", 4, n > 0},
+                                  {d_gate, "d_gate", 4, false},
+                                  {d_dH, "d_dH", align, rows},
+                                  {d_dgate, "d_dgate", 4, false}});
+    if (st != BP_OK || n == 0) return st;
+    MixArgs a{};
+    a.n = n, a.k = k, a.n_rows = n_rows, a.N = n_out, a.dtype = dtype;
+    a.H = d_H, a.place = d_place, a.gate = d_gate, a.D = d_D, a.dH = d_dH, a.dgate = d_dgate;
+    return cuda_status(mix_backward(a, (cudaStream_t)stream), call);
+}
+
+// ------------------------------------------------------------ experts
+bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int max_rows, bp_experts** out) {
+    const char* call = "bp_experts_create";
+    set_error_message("");
+    if (out == nullptr) return fail(BP_EINVAL, "%s: NULL argument", call);
+    bp_status st = check_range(call, "n_experts", n_experts, 1, BP_MAX_EXPERTS);
+    if (st == BP_OK) st = check_dtype(call, dtype);
+    if (st == BP_OK) st = check_units(call, n_in, n_out, dtype);
+    if (st == BP_OK) st = check_range(call, "max_rows", max_rows, 1, INT_MAX);
+    if (st != BP_OK) return st;
+    bp_experts* l = new (std::nothrow) bp_experts();
+    if (l == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
+    l->E = n_experts;
+    l->n_in = n_in;
+    l->n_out = n_out;
+    l->dtype = dtype;
+    l->cap = max_rows;
+    st = make_flags(&l->flags, call);
+    if (st != BP_OK) {
+        bp_experts_destroy(l);
+        return st;
+    }
+    *out = l;
+    return BP_OK;
+}
+
+void bp_experts_destroy(bp_experts* l) {
+    if (l == nullptr) return;
+    cudaDeviceSynchronize();
+    cudaFree(l->flags);
+    delete l;
+}
+
+bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, const void* d_X, int n_x,
+                             const int* d_source, const int* d_offsets, int n_rows, int squash, void* d_Y,
+                             void* stream) {
+    const char* call = "bp_experts_forward";
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL layer", call);
+    bp_status st = check_range(call, "n_rows", n_rows, 0, l->cap);
+    const bool rows = n_rows > 0;
+    if (st == BP_OK && rows) st = check_range(call, "n_x", n_x, d_source != nullptr ? 1 : n_rows, INT_MAX);
+    const int align = l->dtype == BP_BF16 ? 16 : 4;
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_W, "d_W", align, rows},
+                                  {d_b, "d_b", 4, false},
+                                  {d_X, "d_X", align, rows},
+                                  {d_source, "d_source", 4, false},
+                                  {d_offsets, "d_offsets", 4, true},
+                                  {d_Y, "d_Y", align, rows}});
+    if (st != BP_OK || !rows) return st;
+    RowsArgs a{};
+    a.groups = {d_offsets, l->E, n_rows};
+    a.N = l->n_out;
+    a.K = l->n_in;
+    a.in = d_X;
+    a.n_in_rows = n_x;
+    a.source = d_source;
+    a.W = d_W;
+    a.bias = d_b;
+    a.squash = squash;
+    a.out = d_Y;
+    a.flags = l->flags;
+    return cuda_status(simt_rows(a, l->dtype, false, (cudaStream_t)stream), call);
+}
+
+bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, int n_x, const int* d_source,
+                              const int* d_offsets, int n_rows, const void* d_D, int squash, void* d_dX, float* d_GW,
+                              float* d_Gb, int accumulate, void* stream) {
+    const char* call = "bp_experts_backward";
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL layer", call);
+    bp_status st = check_range(call, "n_rows", n_rows, 0, l->cap);
+    const bool rows = n_rows > 0;
+    if (st == BP_OK && rows) st = check_range(call, "n_x", n_x, d_source != nullptr ? 1 : n_rows, INT_MAX);
+    const int align = l->dtype == BP_BF16 ? 16 : 4;
+    const bool needs_x = d_GW != nullptr || (d_dX != nullptr && squash != 0);
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_W, "d_W", align, rows && d_dX != nullptr},
+                                  {d_X, "d_X", align, rows && needs_x},
+                                  {d_source, "d_source", 4, false},
+                                  {d_offsets, "d_offsets", 4, true},
+                                  {d_D, "d_D", align, rows},
+                                  {d_dX, "d_dX", align, false},
+                                  {d_GW, "d_GW", align, false},
+                                  {d_Gb, "d_Gb", 4, false}});
+    if (st != BP_OK) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    const RowGroups groups{d_offsets, l->E, n_rows};
+    if (d_dX != nullptr && rows) {
+        RowsArgs a{};
+        a.groups = groups;
+        a.N = l->n_in;
+        a.K = l->n_out;
+        a.in = d_D;
+        a.n_in_rows = n_rows;
+        a.W = d_W;
+        a.squash = squash;
+        a.x = d_X;
+        a.x_source = d_source;
+        a.n_x = n_x;
+        a.out = d_dX;
+        a.flags = l->flags;
+        st = cuda_status(simt_rows(a, l->dtype, true, s), call);
+    }
+    if (st == BP_OK && d_GW != nullptr) {
+        const ChangeArgs a{groups, l->n_out, l->n_in, d_D, d_X, d_source, n_x, d_GW, accumulate, l->flags};
+        st = cuda_status(simt_change(a, l->dtype, s), call);
+    }
+    if (st == BP_OK && d_Gb != nullptr) {
+        const SumsArgs a{groups, l->n_out, d_D, d_Gb, accumulate, l->flags};
+        st = cuda_status(simt_sums(a, l->dtype, s), call);
+    }
+    return st;
+}
+
+bp_status bp_experts_check(bp_experts* l, void* stream) {
+    if (l == nullptr) return fail(BP_EINVAL, "bp_experts_check: NULL layer");
+    return read_flags(l->flags, stream, "bp_experts_check");
+}
+
+// ------------------------------------------------------------ adapters
+bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int dtype, int max_rows, int max_requests,
+                             bp_adapters** out) {
+    const char* call = "bp_adapters_create";
+    set_error_message("");
+    if (out == nullptr) return fail(BP_EINVAL, "%s: NULL argument", call);
+    bp_status st = check_range(call, "n_adapters", n_adapters, 1, kMaxAdapters);
+    if (st == BP_OK) st = check_range(call, "rank", rank, 1, BP_MAX_RANK);
+    if (st == BP_OK) st = check_dtype(call, dtype);
+    if (st == BP_OK) st = check_units(call, n_in, n_out, dtype);
+    if (st == BP_OK) st = check_range(call, "max_rows", max_rows, 1, INT_MAX / BP_MAX_RANK);
+    if (st == BP_OK) st = check_range(call, "max_requests", max_requests, 1, INT_MAX - 1);
+    if (st != BP_OK) return st;
+    bp_adapters* l = new (std::nothrow) bp_adapters();
+    if (l == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
+    l->n = n_adapters;
+    l->rank = rank;
+    l->n_in = n_in;
+    l->n_out = n_out;
+    l->dtype = dtype;
+    l->cap = max_rows;
+    l->max_requests = max_requests;
+    st = make_flags(&l->flags, call);
+    if (st == BP_OK) st = cuda_status(cudaMalloc(&l->low, (size_t)max_rows * rank * sizeof(float)), call);
+    if (st != BP_OK) {
+        bp_adapters_destroy(l);
+        return st;
+    }
+    *out = l;
+    return BP_OK;
+}
+
+void bp_adapters_destroy(bp_adapters* l) {
+    if (l == nullptr) return;
+    cudaDeviceSynchronize();
+    cudaFree(l->flags);
+    cudaFree(l->low);
+    delete l;
+}
+
+static bp_status check_requests(const char* call, const bp_adapters* l, int n_requests, int n_rows) {
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL layer", call);
+    bp_status st = check_range(call, "n_rows", n_rows, 0, l->cap);
+    if (st == BP_OK) st = check_range(call, "n_requests", n_requests, 0, l->max_requests);
+    return st;
+}
+
+bp_status bp_adapters_forward(bp_adapters* l, const void* d_W, const float* d_b, const void* d_A, const void* d_B,
+                              const float* d_scale, const void* d_X, const int* d_offsets, const int* d_adapter,
+                              int n_requests, int n_rows, int squash, float* d_U, void* d_Y, void* stream) {
+    const char* call = "bp_adapters_forward";
+    bp_status st = check_requests(call, l, n_requests, n_rows);
+    if (st != BP_OK) return st;
+    const bool rows = n_rows > 0, some = rows && n_requests > 0;
+    const int align = l->dtype == BP_BF16 ? 16 : 4;
+    st = check_buffers(call, {{d_W, "d_W", align, rows},
+                              {d_b, "d_b", 4, false},
+                              {d_A, "d_A", align, some},
+                              {d_B, "d_B", align, some},
+                              {d_scale, "d_scale", 4, false},
+                              {d_X, "d_X", align, rows},
+                              {d_offsets, "d_offsets", 4, some},
+                              {d_adapter, "d_adapter", 4, some},
+                              {d_U, "d_U", 4, rows},
+                              {d_Y, "d_Y", align, rows}});
+    if (st != BP_OK || !rows) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    const Requests req{d_offsets, d_adapter, n_requests, n_rows, l->n, l->rank};
+    const LowArgs low{req, l->n_in, d_X, d_A, nullptr, d_U, l->flags};
+    st = cuda_status(simt_low(low, l->dtype, s), call);
+    if (st != BP_OK) return st;
+    RowsArgs a{};
+    a.groups = {nullptr, 1, n_rows};
+    a.N = l->n_out;
+    a.K = l->n_in;
+    a.in = d_X;
+    a.n_in_rows = n_rows;
+    a.W = d_W;
+    a.bias = d_b;
+    a.squash = squash;
+    a.out = d_Y;
+    a.req = req;
+    a.low = d_U;
+    a.P = d_B;
+    a.scale = d_scale;
+    a.flags = l->flags;
+    return cuda_status(simt_rows(a, l->dtype, false, s), call);
+}
+
+bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A, const void* d_B, const float* d_scale,
+                               const void* d_X, const float* d_U, const int* d_offsets, const int* d_adapter,
+                               int n_requests, int n_rows, const void* d_D, int squash, void* d_dX, float* d_GA,
+                               float* d_GB, int accumulate, void* stream) {
+    const char* call = "bp_adapters_backward";
+    bp_status st = check_requests(call, l, n_requests, n_rows);
+    if (st != BP_OK) return st;
+    const bool rows = n_rows > 0, some = rows && n_requests > 0, dx = d_dX != nullptr, ga = d_GA != nullptr,
+               gb = d_GB != nullptr;
+    const int align = l->dtype == BP_BF16 ? 16 : 4;
+    st = check_buffers(call, {{d_W, "d_W", align, rows && dx},
+                              {d_A, "d_A", align, some && dx},
+                              {d_B, "d_B", align, some && (dx || ga)},
+                              {d_scale, "d_scale", 4, false},
+                              {d_X, "d_X", align, rows && (ga || (dx && squash != 0))},
+                              {d_U, "d_U", 4, some && gb},
+                              {d_offsets, "d_offsets", 4, some},
+                              {d_adapter, "d_adapter", 4, some},
+                              {d_D, "d_D", align, rows},
+                              {d_dX, "d_dX", align, false},
+                              {d_GA, "d_GA", align, false},
+                              {d_GB, "d_GB", align, false}});
+    if (st != BP_OK) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    const Requests req{d_offsets, d_adapter, rows ? n_requests : 0, n_rows, l->n, l->rank};
+    if (rows && (dx || ga)) {
+        const LowArgs low{req, l->n_out, d_D, d_B, d_scale, l->low, l->flags};
+        st = cuda_status(simt_low(low, l->dtype, s), call);
+    }
+    if (st == BP_OK && rows && dx) {
+        RowsArgs a{};
+        a.groups = {nullptr, 1, n_rows};
+        a.N = l->n_in;
+        a.K = l->n_out;
+        a.in = d_D;
+        a.n_in_rows = n_rows;
+        a.W = d_W;
+        a.squash = squash;
+        a.x = d_X;
+        a.n_x = n_rows;
+        a.out = d_dX;
+        a.req = req;
+        a.low = l->low;   // v: scaled already
+        a.P = d_A;
+        a.flags = l->flags;
+        st = cuda_status(simt_rows(a, l->dtype, true, s), call);
+    }
+    if (st == BP_OK && ga) {
+        const LowChangeArgs a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->flags};
+        st = cuda_status(simt_low_change(a, l->dtype, s), call);
+    }
+    if (st == BP_OK && gb) {
+        const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->flags};
+        st = cuda_status(simt_low_change(a, l->dtype, s), call);
+    }
+    return st;
+}
+
+bp_status bp_adapters_check(bp_adapters* l, void* stream) {
+    if (l == nullptr) return fail(BP_EINVAL, "bp_adapters_check: NULL layer");
+    return read_flags(l->flags, stream, "bp_adapters_check");
+}
+
+}  // extern "C"

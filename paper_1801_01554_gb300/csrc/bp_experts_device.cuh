@@ -1,0 +1,97 @@
+// Device helpers that the kernels of the expert and adapter layers share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "bp_experts_internal.h"
+
+namespace bp {
+
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <class T>
+__device__ __forceinline__ T from_f32(float x);
+template <>
+__device__ __forceinline__ float from_f32<float>(float x) { return x; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+
+// The rows of group g, clamped to [0, n_rows] and to ascending order.
+__device__ __forceinline__ void group_rows(const int* offsets, int n_rows, int g, int& lo, int& hi, int* flags) {
+    if (offsets == nullptr) {
+        lo = 0;
+        hi = n_rows;
+        return;
+    }
+    const int a = offsets[g], b = offsets[g + 1];
+    lo = min(max(a, 0), n_rows);
+    hi = min(max(b, lo), n_rows);
+    if (lo != a || hi != b) atomicOr(flags, kFlagBounds);
+}
+
+// A row's source, row 0 where it is out of range.
+__device__ __forceinline__ int source_row(const int* source, int r, int n, int* flags) {
+    if (source == nullptr) return r;
+    const int s = source[r];
+    if ((unsigned)s < (unsigned)n) return s;
+    atomicOr(flags, kFlagBounds);
+    return 0;
+}
+
+// The adapter of request i, -1 for none.
+__device__ __forceinline__ int request_adapter(const Requests& q, int i, int* flags) {
+    const int a = q.adapter[i];
+    if (a >= -1 && a < q.n_adapters) return a;
+    atomicOr(flags, kFlagBounds);
+    return -1;
+}
+
+// The first request that ends after row r (n_requests if none): offsets ascend.
+__device__ __forceinline__ int first_request(const Requests& q, int r) {
+    int lo = 0, hi = q.n_requests;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (q.offsets[mid + 1] > r) hi = mid;
+        else lo = mid + 1;
+    }
+    return lo;
+}
+
+// The `tile`-th block of TM rows of the groups, by one converged warp: group and first row, or
+// g = -1 past the last one.  Every lane gets the result.
+template <int TM>
+__device__ __forceinline__ void find_tile(const RowGroups& q, int tile, int& g, int& row0, int& end, int* flags) {
+    const int lane = threadIdx.x & 31;
+    for (int base = 0; base < q.n_groups; base += 32) {
+        int lo = 0, hi = 0;
+        if (base + lane < q.n_groups) group_rows(q.offsets, q.n_rows, base + lane, lo, hi, flags);
+        const int tiles = (hi - lo + TM - 1) / TM;
+        int sum = tiles;   // inclusive
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += x;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, sum > tile);
+        if (past != 0) {
+            const int l = __ffs(past) - 1;
+            g = base + l;
+            const int before = __shfl_sync(0xffffffffu, sum - tiles, l);
+            row0 = __shfl_sync(0xffffffffu, lo, l) + (tile - before) * TM;
+            end = __shfl_sync(0xffffffffu, hi, l);
+            return;
+        }
+        tile -= __shfl_sync(0xffffffffu, sum, 31);
+    }
+    g = -1;
+    row0 = end = 0;
+}
+
+// Most blocks of TM rows that n_rows rows in n_groups groups can make.
+inline int max_tiles(long long n_rows, long long n_groups, int TM) {
+    const long long t = n_rows / TM + n_groups;
+    return (int)(t < n_rows ? t : n_rows);
+}
+
+}  // namespace bp

@@ -1,0 +1,135 @@
+// Internal declarations of the layers whose weights depend on the pattern
+// (include/bp_experts.h): what the API passes to the kernels' launchers.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include "bp_experts.h"
+#include "bp_internal.h"
+
+namespace bp {
+
+// Rows in groups: group g's rows are [offsets[g], offsets[g + 1]), offsets on the device.
+// offsets NULL: one group of all n_rows rows.
+struct RowGroups {
+    const int* offsets;
+    int n_groups;
+    int n_rows;
+};
+
+// Requests over the rows of a layer with adapters; adapter[i] in [0, n_adapters) or -1.
+struct Requests {
+    const int* offsets;
+    const int* adapter;
+    int n_requests, n_rows, n_adapters, rank;
+};
+
+// Rows times the weights of their group.  K-major ("forward"): out[r, n] = sum over k of
+// in[src(r), k] W_g[n, k], W [groups, N, K]; the other way ("back"): out[r, n] = sum over k of
+// in[r, k] W_g[k, n], W [groups, K, N].  With low != NULL there is one group and
+// scale_a * sum over j of low[r, j] P_a[j, n] is added, a the adapter of the row's request.
+struct RowsArgs {
+    RowGroups groups;
+    int N, K;
+    const void* in;
+    int n_in_rows;          // rows of `in`
+    const int* source;      // forward: row of `in` for each row, or NULL
+    const void* W;
+    const float* bias;      // forward: [groups, N] or NULL
+    int squash;             // forward: logistic; back: times x (1 - x)
+    const void* x;          // back with squash: the layer's inputs [n_x, N], read through x_source
+    const int* x_source;
+    int n_x;
+    void* out;
+    // the adapters' part
+    Requests req;
+    const float* low;       // [n_rows, rank]
+    const void* P;          // [n_adapters, rank, N]
+    const float* scale;     // [n_adapters] or NULL
+    int* flags;
+};
+
+// low[r, j] = scale_a * sum over k of in[r, k] P_a[j, k], a the adapter of the row's request
+// (0 without one); P [n_adapters, rank, K].
+struct LowArgs {
+    Requests req;
+    int K;
+    const void* in;
+    const void* P;
+    const float* scale;     // or NULL
+    float* low;
+    int* flags;
+};
+
+// Changes of weights: G_g[m, n] (+)= sum over the group's rows of a[r, m] b[src(r), n].
+struct ChangeArgs {
+    RowGroups groups;
+    int M, N;
+    const void* a;
+    const void* b;
+    const int* source;
+    int n_b;                // rows of b
+    float* G;
+    int accumulate;
+    int* flags;
+};
+
+// Changes of adapters: G_a[j, n] (+)= scale_a * sum over the rows of the adapter's requests of
+// low[r, j] b[r, n].
+struct LowChangeArgs {
+    Requests req;
+    int N;
+    const float* low;
+    const void* b;
+    const float* scale;     // or NULL
+    float* G;
+    int accumulate;
+    int* flags;
+};
+
+// Column sums of a group's rows: S_g[n] (+)= sum over the group's rows of d[r, n].
+struct SumsArgs {
+    RowGroups groups;
+    int N;
+    const void* d;
+    float* S;
+    int accumulate;
+    int* flags;
+};
+
+// float32 FMA kernels, for both dtypes and every size (bp_grouped_simt.cu).
+cudaError_t simt_rows(const RowsArgs& a, int dtype, bool back, cudaStream_t s);
+cudaError_t simt_low(const LowArgs& a, int dtype, cudaStream_t s);
+cudaError_t simt_change(const ChangeArgs& a, int dtype, cudaStream_t s);
+cudaError_t simt_low_change(const LowChangeArgs& a, int dtype, cudaStream_t s);
+cudaError_t simt_sums(const SumsArgs& a, int dtype, cudaStream_t s);
+
+// Router and mix (bp_route.cu).
+struct RouteArgs {
+    int n, E, k, gates, dtype;
+    const void* logits;
+    int* expert;
+    float* gate;
+    int* offsets;
+    int* source;
+    int* place;
+    int* hist;              // [blocks of kRoutePatterns, E]
+};
+constexpr int kRoutePatterns = 128;   // patterns of a block
+cudaError_t route_forward(const RouteArgs& a, cudaStream_t s);
+cudaError_t route_backward(const RouteArgs& a, const float* dgate, void* dlogits, cudaStream_t s);
+struct MixArgs {
+    int n, k, n_rows, N, dtype;
+    const void* H;
+    const int* place;
+    const float* gate;
+    void* Y;
+    const void* D;
+    void* dH;
+    float* dgate;
+    int warps;              // of a pattern (set by the launcher)
+};
+cudaError_t mix_forward(const MixArgs& a, cudaStream_t s);
+cudaError_t mix_backward(const MixArgs& a, cudaStream_t s);
+
+}  // namespace bp
