@@ -17,12 +17,12 @@ struct bp_router {
 };
 
 struct bp_experts {
-    int E = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0;
+    int E = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, num_sms = 0;
     int* flags = nullptr;
 };
 
 struct bp_adapters {
-    int n = 0, rank = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, max_requests = 0;
+    int n = 0, rank = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, max_requests = 0, num_sms = 0;
     int* flags = nullptr;
     float* low = nullptr;   // [cap, rank] v of the backward pass
 };
@@ -84,8 +84,13 @@ bp_status check_units(const char* call, int n_in, int n_out, int dtype) {
     return st;
 }
 
-bp_status make_flags(int** flags, const char* call) {
-    cudaError_t e = cudaMalloc(flags, sizeof(int));
+// A layer's error word; the device's SMs and, for bfloat16, its kernels' set-up.
+bp_status make_layer(int dtype, int** flags, int* num_sms, const char* call) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(num_sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dtype == BP_BF16) e = tc_setup();
+    if (e == cudaSuccess) e = cudaMalloc(flags, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(*flags, 0, sizeof(int));
     return cuda_status(e, call);
 }
@@ -244,7 +249,7 @@ bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int m
     l->n_out = n_out;
     l->dtype = dtype;
     l->cap = max_rows;
-    st = make_flags(&l->flags, call);
+    st = make_layer(dtype, &l->flags, &l->num_sms, call);
     if (st != BP_OK) {
         bp_experts_destroy(l);
         return st;
@@ -258,6 +263,10 @@ void bp_experts_destroy(bp_experts* l) {
     cudaDeviceSynchronize();
     cudaFree(l->flags);
     delete l;
+}
+
+static cudaError_t rows_product(const RowsArgs& a, int dtype, bool back, int num_sms, cudaStream_t s) {
+    return dtype == BP_BF16 ? tc_rows(a, back, {}, num_sms, s) : simt_rows(a, dtype, back, s);
 }
 
 bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, const void* d_X, int n_x,
@@ -289,7 +298,7 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
     a.squash = squash;
     a.out = d_Y;
     a.flags = l->flags;
-    return cuda_status(simt_rows(a, l->dtype, false, (cudaStream_t)stream), call);
+    return cuda_status(rows_product(a, l->dtype, false, l->num_sms, (cudaStream_t)stream), call);
 }
 
 bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, int n_x, const int* d_source,
@@ -328,11 +337,11 @@ bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, i
         a.n_x = n_x;
         a.out = d_dX;
         a.flags = l->flags;
-        st = cuda_status(simt_rows(a, l->dtype, true, s), call);
+        st = cuda_status(rows_product(a, l->dtype, true, l->num_sms, s), call);
     }
     if (st == BP_OK && d_GW != nullptr) {
         const ChangeArgs a{groups, l->n_out, l->n_in, d_D, d_X, d_source, n_x, d_GW, accumulate, l->flags};
-        st = cuda_status(simt_change(a, l->dtype, s), call);
+        st = cuda_status(l->dtype == BP_BF16 ? tc_change(a, l->num_sms, s) : simt_change(a, l->dtype, s), call);
     }
     if (st == BP_OK && d_Gb != nullptr) {
         const SumsArgs a{groups, l->n_out, d_D, d_Gb, accumulate, l->flags};
@@ -368,7 +377,7 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
     l->dtype = dtype;
     l->cap = max_rows;
     l->max_requests = max_requests;
-    st = make_flags(&l->flags, call);
+    st = make_layer(dtype, &l->flags, &l->num_sms, call);
     if (st == BP_OK) st = cuda_status(cudaMalloc(&l->low, (size_t)max_rows * rank * sizeof(float)), call);
     if (st != BP_OK) {
         bp_adapters_destroy(l);

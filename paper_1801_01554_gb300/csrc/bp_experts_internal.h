@@ -104,6 +104,20 @@ cudaError_t simt_change(const ChangeArgs& a, int dtype, cudaStream_t s);
 cudaError_t simt_low_change(const LowChangeArgs& a, int dtype, cudaStream_t s);
 cudaError_t simt_sums(const SumsArgs& a, int dtype, cudaStream_t s);
 
+// Tensor-core kernels for bfloat16 (bp_grouped_tc.cu).
+// low as kLowTerms bfloat16 terms side by side, [n_rows, kLowTerms * roundup16(rank)] with zeros past
+// the rank, scaled, and the adapter of every block of 128 rows: -1 none, kTileMixed several requests.
+constexpr int kLowTerms = 2;
+constexpr int kTileRows = 128;
+constexpr int kTileMixed = -2;
+struct LowTerms {
+    const void* terms;
+    const int* tile_adapter;
+};
+cudaError_t tc_setup();
+cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_sms, cudaStream_t s);
+cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
+
 // Router and mix (bp_route.cu).
 struct RouteArgs {
     int n, E, k, gates, dtype;

@@ -1,0 +1,726 @@
+// Products of rows with the weights of their group on the tensor cores, in bfloat16 with float32
+// sums: the expert layers, and the adapter layers' shared product with the adapters' part added.
+//
+//   forward  out[r, n]  = sum over k of in[src(r), k] W_g[n, k]     both operands along K
+//   back     out[r, n]  = sum over k of in[r, k] W_g[k, n]          W as an MN-major operand
+//   change   G_g[m, n]  = sum over the group's rows of a[r, m] b[src(r), n]   both MN-major
+//
+// One persistent CTA per SM: a warp that issues TMA copies into a ring of stages, a warp that
+// issues tcgen05.mma (128 rows x BN columns x 64 of K a stage) into TMEM, eight epilogue warps.
+// The groups' ends lie on the device: each CTA turns them into first tiles in shared memory and
+// finds the group of a tile by bisection, so that no host knows the sizes and no list is written.
+//
+// Ragged groups need no padded copy of the rows.  A tile that runs over its group's end computes
+// the next group's rows too and does not store them; in a change, where rows are summed, the
+// stage's foreign rows are set to zero in shared memory in both operands (0 times a foreign
+// infinity would not be 0).  W's maps have a dimension of their own for the group, past whose
+// edges the copy engine fills in zeros.  Rows read through an index are gathered by the copy
+// engine, four rows an instruction, a lane each.
+//
+// The adapters' part of a tile whose rows all belong to one request is K beyond the layer's own:
+// the rows of low as two bfloat16 terms (its rounding and the rest) times the adapter's rows.  In
+// a tile of several requests the epilogue adds it row by row: as one product with the other
+// requests' rows at zero, an adapter's infinity would reach them.
+#include <cstdio>
+#include <mutex>
+
+#include "bp_experts_device.cuh"
+#include "bp_tc_device.cuh"
+
+namespace bp {
+namespace {
+
+constexpr int kEpiWarps = 8;         // two per TMEM lane quarter, each on half of the columns
+constexpr int kEpiThreads = 32 * kEpiWarps;
+constexpr int kThreads = 64 + kEpiThreads;   // warp 0 copies, warp 1 MMA, warps 2.. epilogue
+
+enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2 };
+
+struct TcArgs {
+    RowGroups groups;
+    int num_n, num_m;        // tiles along N; along M of a change
+    int M, N, K;             // M: rows of a change; K: not of a change
+    const int* source;       // rows of the gathered operand, or NULL
+    int n_src;
+    const float* bias;
+    int squash;
+    const bf16* x;
+    const int* x_source;
+    int n_x;
+    bf16* out;
+    float* G;
+    int accumulate;
+    // adapters
+    const int* tile_adapter;   // per 128 rows (kTileMixed: several requests), or NULL
+    int low_chunks;            // 16-wide pieces of the low-rank K
+    int rank16;                // 16-wide pieces of the rank
+    Requests req;
+    const float* low;
+    const bf16* P;
+    const float* scale;
+    int* flags;
+};
+
+template <int BN>
+struct Cfg {
+    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+    static constexpr int kABytes = BM * BK * 2;
+    static constexpr int kBBytes = BN * BK * 2;
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kRingBytes = kStages * kStageBytes;
+    static constexpr int kOutBytes = kEpiWarps * 32 * 32 * 2;   // a 32 x 32 bf16 block per epilogue warp
+    static constexpr int kBiasBytes = kEpiWarps * (BN / 2) * 4;   // a warp's half of the tile's biases
+    static constexpr int kGroupBytes = (3 * BP_MAX_EXPERTS + 32) * 4;
+    static constexpr int kSmemBytes = 1024 + kRingBytes + kOutBytes + kBiasBytes + kGroupBytes + 256;
+};
+
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(smem_u32(dst)),
+        "l"((unsigned long long)map), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
+        : "memory");
+}
+// Four rows of 64 columns (the map's box is one row high).
+__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int c0, const int (&r)[4], uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(smem_u32(dst)),
+        "l"((unsigned long long)map), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(smem_u32(bar))
+        : "memory");
+}
+
+// A tile: rows [row0, end) of a forward or back product, of group g; of a change, all rows of the
+// group and the block mb of M.
+struct Item {
+    int g, row0, end, mb, nb;
+    int kbs;        // K blocks
+    int adapter;    // whose low-rank K follows, kTileMixed, or -1
+};
+
+// Row blocks of a group are swept 16 at a time over all column blocks (row block fastest), so
+// that the tiles in flight share rows and weights in L2 (16: as square as 152 tiles of
+// 128 x 256 get).
+__device__ __forceinline__ void sweep(int tile, int num_m, int num_n, int& mb, int& nb) {
+    constexpr int kRun = 16;
+    const int run = tile / (kRun * num_n), first = run * kRun, m = min(num_m - first, kRun);
+    const int local = tile - run * kRun * num_n;
+    mb = first + local % m;
+    nb = local / m;
+}
+
+template <int FORM>
+struct Schedule {
+    const TcArgs& g;
+    const int *lo, *hi, *tile0;   // per group, in shared memory: first row, end; first row block (n_groups + 1)
+    __device__ int items() const {
+        return FORM == CHANGE ? g.groups.n_groups * g.num_m * g.num_n : tile0[g.groups.n_groups] * g.num_n;
+    }
+    __device__ Item item(int it) const {
+        Item w;
+        if (FORM == CHANGE) {
+            const int per = g.num_m * g.num_n;
+            w.g = it / per;
+            sweep(it - w.g * per, g.num_m, g.num_n, w.mb, w.nb);
+            w.row0 = lo[w.g];
+            w.end = hi[w.g];
+            w.kbs = (w.end - w.row0 + BK - 1) / BK;
+            w.adapter = -1;
+            return w;
+        }
+        int a = 0, b = g.groups.n_groups;   // the last group whose first tile is not past `it`, with tiles
+        while (b - a > 1) {
+            const int mid = (a + b) >> 1;
+            if (tile0[mid] * g.num_n <= it) a = mid;
+            else b = mid;
+        }
+        w.g = a;
+        int mb;
+        sweep(it - tile0[a] * g.num_n, tile0[a + 1] - tile0[a], g.num_n, mb, w.nb);
+        w.mb = tile0[a] + mb;
+        w.row0 = lo[a] + mb * BM;
+        w.kbs = (g.K + BK - 1) / BK;
+        w.adapter = g.tile_adapter != nullptr ? g.tile_adapter[mb] : -1;
+        w.end = min(hi[a], w.row0 + BM);
+        return w;
+    }
+};
+
+// Rows of one K block of an MN-major operand's 64-wide blocks from `from` up to `to` set to zero.
+__device__ __forceinline__ void zero_rows(uint8_t* block, int blocks, int from, int to) {
+    const int lane = threadIdx.x & 31, per = (to - from) * 8;   // 16-byte pieces of a block's rows
+    for (int i = lane; i < blocks * per; i += 32) {
+        const int b = i / per, p = i - b * per;
+        *reinterpret_cast<uint4*>(block + b * kMnBlockBytes + from * 128 + p * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// Stores a warp's 32 x 32 block of float32 sums as bfloat16 rows (see bp_tc_device.cuh).
+__device__ __forceinline__ void store_rows(bf16* out, int N, int row0, int end, int n0, const float (&v)[32], uint4* sS4) {
+    const int lane = threadIdx.x & 31, piece = lane & 3;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        __align__(16) __nv_bfloat162 h[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = __floats2bfloat162_rn(v[8 * k + 2 * q], v[8 * k + 2 * q + 1]);
+        *piece_at(sS4, lane, k) = *reinterpret_cast<const uint4*>(h);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = 8 * j + (lane >> 2);
+        const uint4 u = *piece_at(sS4, r, piece);
+        if (row0 + r < end && n0 + piece * 8 < N)
+            *reinterpret_cast<uint4*>(out + (size_t)(row0 + r) * N + n0 + piece * 8) = u;
+    }
+    __syncwarp();   // the block may be rewritten
+}
+
+// scale_a * sum over j of low[row, j] P_a[j, n0 .. n0 + 31] added to a row's sums (a: the adapter of
+// the row's request).
+__device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, int n0, float (&v)[32]) {
+    if (adapter < 0) return;
+    const int r = g.req.rank;
+    const float c = g.scale != nullptr ? g.scale[adapter] : 1.f;
+    const float* low = g.low + (size_t)row * r;
+    const bf16* P = g.P + (size_t)adapter * r * g.N + n0;
+    for (int j = 0; j < r; ++j) {
+        const float u = c * low[j];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (n0 + 8 * k >= g.N) break;
+            const uint4 p = *reinterpret_cast<const uint4*>(P + (size_t)j * g.N + 8 * k);
+            const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                v[8 * k + 2 * q] = fmaf(u, __uint_as_float(w[q] << 16), v[8 * k + 2 * q]);
+                v[8 * k + 2 * q + 1] = fmaf(u, __uint_as_float(w[q] & 0xffff0000u), v[8 * k + 2 * q + 1]);
+            }
+        }
+    }
+}
+
+// K blocks of one sum of a change in TMEM.  The tensor cores truncate as they accumulate, so that
+// a sum's error grows with its length; these sums are added in registers, rounding to nearest.
+// 2-norm error of the changes of 4096 x 4096 weights by 2,048 rows a group against float64:
+// see the measurements in the design notes' table; a drained sum costs the epilogue about 500 clocks,
+// which run beside the next sum's MMAs (8 K blocks of 128 x 256: 4,200).
+constexpr int kChain = 8;
+
+template <int BN, int FORM, bool GATHER>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_grouped(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+              const __grid_constant__ CUtensorMap map_low, const __grid_constant__ CUtensorMap map_p,
+              const __grid_constant__ TcArgs g) {
+    using C = Cfg<BN>;
+    constexpr int S = C::kStages;
+    constexpr bool kAMn = FORM == CHANGE, kBMn = FORM != FORWARD;
+    constexpr int kAcc = 2;   // the epilogue of a sum overlaps the next one's MMAs
+    constexpr int kTmemCols = kAcc * BN;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* ring = reinterpret_cast<uint8_t*>(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    bf16* stage_out = reinterpret_cast<bf16*>(ring + C::kRingBytes);
+    float* bias_s = reinterpret_cast<float*>(ring + C::kRingBytes + C::kOutBytes);   // [kEpiWarps][BN / 2]
+    int* s_lo = reinterpret_cast<int*>(ring + C::kRingBytes + C::kOutBytes + C::kBiasBytes);
+    int* s_hi = s_lo + BP_MAX_EXPERTS;
+    int* s_tile0 = s_hi + BP_MAX_EXPERTS;
+    uint64_t* full = reinterpret_cast<uint64_t*>(ring + C::kRingBytes + C::kOutBytes + C::kBiasBytes + C::kGroupBytes);
+    uint64_t* empty = full + S;
+    uint64_t* tfull = empty + S;
+    uint64_t* tempty = tfull + kAcc;
+    uint64_t* drain = tempty + kAcc;   // used only when a wait ran out
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    static_assert((2 * S + 2 * kAcc + 1) * 8 + 8 <= 256, "room for the barriers");
+
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    pdl_launch();
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        for (int a = 0; a < kAcc; ++a) {
+            mbar_init(&tfull[a], 1);
+            mbar_init(&tempty[a], kEpiThreads);
+        }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                     "r"(kTmemCols)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    pdl_wait();   // every thread, before its first access to what earlier kernels wrote or still read
+    if (warp == 2) {
+        // the groups' rows and first row blocks
+        int carry = 0;
+        for (int base = 0; base < g.groups.n_groups; base += 32) {
+            const int e = base + lane;
+            int lo = 0, hi = 0;
+            if (e < g.groups.n_groups) group_rows(g.groups.offsets, g.groups.n_rows, e, lo, hi, g.flags);
+            const int blocks = (hi - lo + BM - 1) / BM;
+            int sum = blocks;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += y;
+            }
+            if (e < g.groups.n_groups) {
+                s_lo[e] = lo;
+                s_hi[e] = hi;
+                s_tile0[e] = carry + sum - blocks;
+            }
+            carry += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (lane == 0) s_tile0[g.groups.n_groups] = carry;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_slot;
+    const Schedule<FORM> plan{g, s_lo, s_hi, s_tile0};
+    const int items = plan.items();
+
+    if (warp == 0) {
+        // ---------------- copies: one lane issues, or every lane where rows are gathered
+        const bool leader = elect_one();
+        if (GATHER || leader) {
+            int stage = 0, issued = 0;
+            unsigned phase = 0;
+            bool ok = true;
+            // The stage's buffer is free and its barrier expects `bytes`.
+            auto open = [&](unsigned bytes) {
+                if (issued >= S) {
+                    ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
+                    if (GATHER) ok = __all_sync(0xffffffffu, ok);
+                }
+                if (ok && leader) mbar_expect_tx(&full[stage], bytes);
+                if (GATHER) __syncwarp();
+                return ok;
+            };
+            auto close = [&] {
+                ++issued;
+                if (++stage == S) { stage = 0; phase ^= 1u; }
+            };
+            for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+                const Item w = plan.item(it);
+                // gathered rows: of the tile's 128, lane l the rows 4 l ..; of a change's K block of 64,
+                // the rows 4 (l % 16) .. (in the block's column blocks l / 16, l / 16 + 2, ..)
+                int rows[4] = {0, 0, 0, 0};
+                auto load_rows = [&](int first) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        rows[i] = first + i < w.end ? source_row(g.source, first + i, g.n_src, g.flags) : 0;
+                };
+                if (GATHER) load_rows(w.row0 + 4 * (FORM == CHANGE ? lane & 15 : lane));
+                for (int kb = 0; kb < w.kbs; ++kb) {
+                    if (!open(C::kStageBytes)) break;
+                    uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
+                    uint64_t* bar = &full[stage];
+                    if (FORM == CHANGE) {
+                        const int r = w.row0 + kb * BK;
+                        if (leader)
+                            for (int i = 0; i < BM / 64; ++i)
+                                tma_load_2d(sa + i * kMnBlockBytes, &map_a, w.mb * BM + 64 * i, r, bar);
+                        if (GATHER) {
+                            for (int i = lane >> 4; i < BN / 64; i += 2)
+                                tma_gather4(sb + i * kMnBlockBytes + (lane & 15) * 512, &map_b, w.nb * BN + 64 * i, rows, bar);
+                            load_rows(r + BK + 4 * (lane & 15));   // the next block's
+                        } else {
+                            for (int i = 0; i < BN / 64; ++i)
+                                tma_load_2d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, r, bar);
+                        }
+                    } else {
+                        if (GATHER) tma_gather4(sa + lane * 512, &map_a, kb * BK, rows, bar);
+                        else tma_load_2d(sa, &map_a, kb * BK, w.row0, bar);
+                        if (leader) {
+                            if (FORM == FORWARD) {
+                                tma_load_3d(sb, &map_b, kb * BK, w.nb * BN, w.g, bar);
+                            } else {
+                                for (int i = 0; i < BN / 64; ++i)
+                                    tma_load_3d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, kb * BK, w.g, bar);
+                            }
+                        }
+                    }
+                    close();
+                }
+                if (FORM != CHANGE && !GATHER && w.adapter >= 0) {   // the low-rank K, 4 pieces of 16 a stage
+                    for (int c0 = 0; c0 < g.low_chunks && ok; c0 += 4) {
+                        const int n = min(4, g.low_chunks - c0);
+                        if (!open(C::kABytes + n * 16 * BN * 2)) break;
+                        uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
+                        tma_load_2d(sa, &map_low, c0 * 16, w.row0, &full[stage]);
+                        for (int c = 0; c < n; ++c)
+                            for (int i = 0; i < BN / 64; ++i)
+                                tma_load_3d(sb + i * kMnBlockBytes + c * 16 * 128, &map_p, w.nb * BN + 64 * i,
+                                            (c0 + c) % g.rank16 * 16, w.adapter, &full[stage]);
+                        close();
+                    }
+                }
+            }
+            if (!ok && leader) {
+                // let every copy already issued land before the CTA can exit
+                for (int n = issued - 1; n >= 0 && n >= issued - S; --n) {   // each stage's last copy
+                    const unsigned long long t0 = global_ns();
+                    while (!mbar_try_wait(&full[n % S], (unsigned)(n / S) & 1u) && global_ns() - t0 < kWaitNs) {
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ---------------- MMA: one lane issues; of a change the warp clears foreign rows
+        const bool leader = elect_one();
+        if (FORM == CHANGE || leader) {
+            constexpr uint32_t idesc = idesc_bf16(BM, BN, kAMn, kBMn), idesc_low = idesc_bf16(BM, BN, false, true);
+            const uint32_t a0 = desc_lo<kAMn>(smem_u32(ring)), b0 = desc_lo<kBMn>(smem_u32(ring) + C::kABytes);
+            const uint32_t low_a0 = desc_lo<false>(smem_u32(ring)), low_b0 = desc_lo<true>(smem_u32(ring) + C::kABytes);
+            int stage = 0, acc = 0;
+            unsigned phase = 0, acc_phase = 0;
+            bool ok = true, issued_any = false;
+            auto wait = [&](uint64_t* bar, unsigned parity) {
+                ok = mbar_wait(bar, parity, abort_flag, g.flags);
+                if (FORM == CHANGE) ok = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
+                return ok;
+            };
+            auto close = [&] {
+                if (leader) umma_commit(&empty[stage]);
+                issued_any = true;
+                if (++stage == S) { stage = 0; phase ^= 1u; }
+            };
+            for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+                const Item w = plan.item(it);
+                const int chain = FORM == CHANGE ? kChain : w.kbs;
+                for (int k0 = 0; k0 < w.kbs && ok; k0 += chain) {
+                    const int k1 = min(w.kbs, k0 + chain);
+                    if (!wait(&tempty[acc], acc_phase ^ 1u)) break;
+                    const uint32_t tmem_d = tmem_base + (uint32_t)(acc * BN);
+                    for (int kb = k0; kb < k1; ++kb) {
+                        if (!wait(&full[stage], phase)) break;
+                        const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = b0 + stage * (C::kStageBytes >> 4);
+                        int steps = BK / UMMA_K;
+                        if (FORM == CHANGE) {
+                            const int valid = w.end - w.row0 - kb * BK;
+                            if (valid < BK) {   // (uniform) the group's last rows
+                                steps = (valid + UMMA_K - 1) / UMMA_K;
+                                uint8_t* sa = ring + stage * C::kStageBytes;
+                                zero_rows(sa, BM / 64 + BN / 64, valid, steps * UMMA_K);   // A's blocks, then B's
+                                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                                __syncwarp();
+                            }
+                        }
+                        if (leader) {
+                            umma_bf16<idesc>(tmem_d, al, bl, kb > k0 ? 1u : 0u);
+#pragma unroll
+                            for (int kk = 1; kk < BK / UMMA_K; ++kk)
+                                if (FORM != CHANGE || kk < steps)
+                                    umma_bf16<idesc>(tmem_d, al + kk * k_step_units<kAMn>(), bl + kk * k_step_units<kBMn>(), 1u);
+                        }
+                        close();
+                    }
+                    if (!ok) break;
+                    if (FORM != CHANGE && !GATHER && w.adapter >= 0) {
+                        for (int c0 = 0; c0 < g.low_chunks; c0 += 4) {
+                            if (!wait(&full[stage], phase)) break;
+                            const uint32_t al = low_a0 + stage * (C::kStageBytes >> 4), bl = low_b0 + stage * (C::kStageBytes >> 4);
+                            for (int c = 0; c < min(4, g.low_chunks - c0); ++c)
+                                umma_bf16<idesc_low>(tmem_d, al + c * k_step_units<false>(), bl + c * k_step_units<true>(), 1u);
+                            close();
+                        }
+                        if (!ok) break;
+                    }
+                    if (leader) umma_commit(&tfull[acc]);
+                    if (++acc == kAcc) { acc = 0; acc_phase ^= 1u; }
+                }
+            }
+            if (!ok && issued_any && leader) {
+                // let every MMA already issued finish before TMEM is released
+                umma_commit(drain);
+                const unsigned long long t0 = global_ns();
+                while (!mbar_try_wait(drain, 0) && global_ns() - t0 < kWaitNs) {
+                }
+            }
+        }
+    } else {
+        // ---------------- epilogue warps 2..9
+        const int q = warp & 3;                  // TMEM lane quarter this warp may access
+        const int ew = warp - 2;
+        const int cbeg = (ew >> 2) * (BN / 2);   // this warp's half of the columns
+        const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16);
+        uint4* sS4 = reinterpret_cast<uint4*>(stage_out + ew * 1024);
+        int acc = 0;
+        unsigned acc_phase = 0;
+        auto wait_acc = [&] {
+            const bool got = mbar_wait(&tfull[acc], acc_phase, abort_flag, g.flags);
+            const bool leave = __any_sync(0xffffffffu, !got);
+            tc_fence_after();
+            return !leave;
+        };
+        auto release = [&] {
+            tc_fence_before();
+            mbar_arrive(&tempty[acc]);
+            if (++acc == kAcc) { acc = 0; acc_phase ^= 1u; }
+        };
+        for (int it = blockIdx.x; it < items; it += gridDim.x) {
+            const Item w = plan.item(it);
+            if constexpr (FORM == CHANGE) {
+                float part[BN / 2];
+#pragma unroll
+                for (int c = 0; c < BN / 2; ++c) part[c] = 0.f;
+                bool stay = true;
+                for (int k0 = 0; k0 < w.kbs; k0 += kChain) {
+                    stay = wait_acc();
+                    if (!stay) break;
+#pragma unroll
+                    for (int i = 0; i < BN / 64; ++i) {
+                        float v[32];
+                        tmem_ld32(trow + (uint32_t)(acc * BN + cbeg + 32 * i), v);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) part[32 * i + c] += v[c];
+                    }
+                    release();
+                }
+                if (!stay) break;
+                const int m = w.mb * BM + q * 32 + lane;
+                float* dst = g.G + ((size_t)w.g * g.M + m) * g.N;
+                if (m < g.M) {
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 4) {
+                        const int n = w.nb * BN + cbeg + c;
+                        if (n >= g.N) break;   // N is a multiple of 8
+                        float4 o = make_float4(part[c], part[c + 1], part[c + 2], part[c + 3]);
+                        if (g.accumulate) {
+                            const float4 old = *reinterpret_cast<const float4*>(dst + n);
+                            o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
+                        }
+                        *reinterpret_cast<float4*>(dst + n) = o;
+                    }
+                }
+            } else {
+                const int m0 = w.row0 + q * 32, row = m0 + lane;
+                float* sbias = bias_s + ew * (BN / 2);
+                if (FORM == FORWARD) {
+                    __syncwarp();   // the tile before is read
+                    for (int c = lane; c < BN / 2; c += 32) {
+                        const int n = w.nb * BN + cbeg + c;
+                        sbias[c] = g.bias != nullptr && n < g.N ? g.bias[(size_t)w.g * g.N + n] : 0.f;
+                    }
+                    __syncwarp();
+                }
+                int xr[4] = {0, 0, 0, 0};   // source rows of this lane's pieces (back)
+                if (FORM == BACK && g.squash) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int r = m0 + 8 * j + (lane >> 2);
+                        xr[j] = r < w.end ? source_row(g.x_source, r, g.n_x, g.flags) : -1;
+                    }
+                }
+                int adapter = -1;   // of this lane's row, in a tile of several requests
+                if (!GATHER && w.adapter == kTileMixed && row < w.end) {
+                    const int i = first_request(g.req, row);
+                    if (i < g.req.n_requests) {
+                        int lo, hi;
+                        group_rows(g.req.offsets, g.req.n_rows, i, lo, hi, g.flags);
+                        if (row >= lo && row < hi) adapter = request_adapter(g.req, i, g.flags);
+                    }
+                }
+                if (!wait_acc()) break;
+#pragma unroll 1
+                for (int i = 0; i < BN / 64; ++i) {
+                    const int c0 = 32 * i, n0 = w.nb * BN + cbeg + c0;
+                    if (n0 >= g.N) break;
+                    Row32 a;
+                    if (FORM == BACK && g.squash) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int n = n0 + (lane & 3) * 8;
+                            a.u[j] = xr[j] >= 0 && n < g.N ? *reinterpret_cast<const uint4*>(g.x + (size_t)xr[j] * g.N + n)
+                                                           : make_uint4(0u, 0u, 0u, 0u);
+                        }
+                    }
+                    float v[32];
+                    tmem_ld32(trow + (uint32_t)(acc * BN + cbeg + c0), v);
+                    if (!GATHER && w.adapter == kTileMixed) add_low(g, row, adapter, n0, v);
+                    if (FORM == FORWARD) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float4 f = reinterpret_cast<const float4*>(sbias + c0)[k];
+                            v[4 * k] += f.x;
+                            v[4 * k + 1] += f.y;
+                            v[4 * k + 2] += f.z;
+                            v[4 * k + 3] += f.w;
+                        }
+                        if (g.squash) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) v[c] = sigmoid_fast(v[c]);
+                        }
+                    } else if (g.squash) {
+                        block_to_rows(a, sS4);
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            const float x = row_value(a, c);
+                            v[c] = v[c] * x * (1.f - x);
+                        }
+                    }
+                    store_rows(g.out, g.N, m0, w.end, n0, v, sS4);
+                }
+                release();
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+    }
+}
+
+// ------------------------------------------------------------ host
+PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
+
+// A row-major bfloat16 matrix, or `planes` of them (planes > 0), copied in boxes of 64 columns.
+bool make_map(CUtensorMap* map, const void* base, int rows, int cols, int planes, int box_rows) {
+    const int rank = planes > 0 ? 3 : 2;
+    cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+    cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * rows * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return g_encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(base), dims, strides, box, estr,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN>
+cudaError_t setup_width() {
+    const void* fns[] = {(const void*)k_grouped<BN, FORWARD, false>, (const void*)k_grouped<BN, FORWARD, true>,
+                         (const void*)k_grouped<BN, BACK, false>, (const void*)k_grouped<BN, CHANGE, false>,
+                         (const void*)k_grouped<BN, CHANGE, true>};
+    for (const void* f : fns) {
+        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::kSmemBytes);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+template <int FORM, bool GATHER>
+cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtensorMap (&m)[4], cudaStream_t s) {
+    const int grid = items < num_sms ? items : num_sms;
+    if (grid < 1) return cudaSuccess;
+    switch (bn) {
+        case 64: return launch_pdl(k_grouped<64, FORM, GATHER>, grid, 1, kThreads, Cfg<64>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+        case 128: return launch_pdl(k_grouped<128, FORM, GATHER>, grid, 1, kThreads, Cfg<128>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+        default: return launch_pdl(k_grouped<256, FORM, GATHER>, grid, 1, kThreads, Cfg<256>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+    }
+}
+
+int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
+
+// Tile width for row_tiles blocks of 128 rows: the time of the waves of tiles, at the clocks that
+// a K block of 64 takes with every SM busy (530, 330 and 230 for 256, 128 and 64 columns: each SM
+// reads A again for every column block) and an epilogue of 800 + 900 a 64 columns, whichever is
+// longer, plus the other one once.
+int pick_width(long long row_tiles, int N, int kbs, int num_sms) {
+    const int bns[3] = {256, 128, 64}, clocks[3] = {530, 330, 230};
+    int best = 256;
+    double best_t = 0;
+    for (int i = 0; i < 3; ++i) {
+        const double waves = ceil_div(row_tiles * ceil_div(N, bns[i]), num_sms);
+        const double k = (double)kbs * clocks[i], e = 800.0 + 900.0 * bns[i] / 64;
+        const double t = waves * (k > e ? k : e) + (k > e ? e : k);
+        if (i == 0 || t < best_t) best = bns[i], best_t = t;
+    }
+    return best;
+}
+
+}  // namespace
+
+cudaError_t tc_setup() {
+    static std::once_flag once;
+    static cudaError_t status;
+    std::call_once(once, [] {
+        g_encode = tensor_map_encoder();
+        status = g_encode == nullptr ? cudaErrorNotSupported : cudaSuccess;
+    });
+    if (status != cudaSuccess) return status;
+    cudaError_t e;
+    if ((e = setup_width<64>()) != cudaSuccess) return e;
+    if ((e = setup_width<128>()) != cudaSuccess) return e;
+    return setup_width<256>();
+}
+
+cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_sms, cudaStream_t s) {
+    TcArgs a{};
+    a.groups = r.groups;
+    a.N = r.N;
+    a.K = r.K;
+    a.source = r.source;
+    a.n_src = r.n_in_rows;
+    a.bias = r.bias;
+    a.squash = r.squash;
+    a.x = (const bf16*)r.x;
+    a.x_source = r.x_source;
+    a.n_x = r.n_x;
+    a.out = (bf16*)r.out;
+    a.flags = r.flags;
+    const int E = r.groups.n_groups, kbs = ceil_div(r.K, BK);
+    // row blocks: every group's, about as many rows in each (the groups' sizes are on the device)
+    const long long busy = E < r.groups.n_rows ? E : r.groups.n_rows;
+    const long long row_tiles = busy * ceil_div(r.groups.n_rows, busy * BM);
+    const int bn = pick_width(row_tiles, r.N, kbs, num_sms);
+    a.num_n = ceil_div(r.N, bn);
+    CUtensorMap m[4];
+    bool ok = make_map(&m[0], r.in, r.n_in_rows, r.K, 0, r.source != nullptr ? 1 : BM) &&
+              (back ? make_map(&m[1], r.W, r.K, r.N, E, BK) : make_map(&m[1], r.W, r.N, r.K, E, bn));
+    m[2] = m[3] = m[0];
+    if (r.low != nullptr) {
+        a.tile_adapter = low.tile_adapter;
+        a.rank16 = ceil_div(r.req.rank, 16);
+        a.low_chunks = kLowTerms * a.rank16;
+        a.req = r.req;
+        a.low = r.low;
+        a.P = (const bf16*)r.P;
+        a.scale = r.scale;
+        ok = ok && make_map(&m[2], low.terms, r.groups.n_rows, a.low_chunks * 16, 0, BM) &&
+             make_map(&m[3], r.P, r.req.rank, r.N, r.req.n_adapters, 16);
+    }
+    if (!ok) return cudaErrorInvalidValue;
+    const long long items = (long long)max_tiles(r.groups.n_rows, E, BM) * a.num_n;
+    const int n = items < num_sms ? (int)items : num_sms;
+    if (back) return launch<BACK, false>(a, bn, n, num_sms, m, s);
+    return r.source != nullptr ? launch<FORWARD, true>(a, bn, n, num_sms, m, s) : launch<FORWARD, false>(a, bn, n, num_sms, m, s);
+}
+
+cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
+    TcArgs a{};
+    a.groups = c.groups;
+    a.M = c.M;
+    a.N = c.N;
+    a.source = c.source;
+    a.n_src = c.n_b;
+    a.G = c.G;
+    a.accumulate = c.accumulate;
+    a.flags = c.flags;
+    a.num_m = ceil_div(c.M, BM);
+    const int E = c.groups.n_groups;
+    const int bn = pick_width((long long)E * a.num_m, c.N, ceil_div(c.groups.n_rows, (long long)E * BK), num_sms);
+    a.num_n = ceil_div(c.N, bn);
+    CUtensorMap m[4];
+    // without rows nothing is copied and the maps' addresses are not used; G stands in for them
+    const bool rows = c.groups.n_rows > 0;
+    if (!make_map(&m[0], rows ? c.a : c.G, rows ? c.groups.n_rows : 1, c.M, 0, BK) ||
+        !make_map(&m[1], rows ? c.b : c.G, rows ? c.n_b : 1, c.N, 0, c.source != nullptr ? 1 : BK))
+        return cudaErrorInvalidValue;
+    m[2] = m[3] = m[0];
+    const long long items = (long long)E * a.num_m * a.num_n;
+    const int n = items < num_sms ? (int)items : num_sms;
+    return c.source != nullptr ? launch<CHANGE, true>(a, bn, n, num_sms, m, s) : launch<CHANGE, false>(a, bn, n, num_sms, m, s);
+}
+
+}  // namespace bp
