@@ -19,6 +19,7 @@ struct bp_router {
 struct bp_experts {
     int E = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, num_sms = 0;
     int* flags = nullptr;
+    void* rows = nullptr;   // bfloat16: [cap, n_in] inputs in the rows' order
 };
 
 struct bp_adapters {
@@ -250,6 +251,7 @@ bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int m
     l->dtype = dtype;
     l->cap = max_rows;
     st = make_layer(dtype, &l->flags, &l->num_sms, call);
+    if (st == BP_OK && dtype == BP_BF16) st = cuda_status(cudaMalloc(&l->rows, (size_t)max_rows * n_in * 2), call);
     if (st != BP_OK) {
         bp_experts_destroy(l);
         return st;
@@ -262,7 +264,19 @@ void bp_experts_destroy(bp_experts* l) {
     if (l == nullptr) return;
     cudaDeviceSynchronize();
     cudaFree(l->flags);
+    cudaFree(l->rows);
     delete l;
+}
+
+// bfloat16 inputs that are read through an index: from here on a copy in the rows' order.
+static cudaError_t rows_in_order(bp_experts* l, const RowGroups& groups, const void*& X, int& n_x, const int*& source,
+                                 cudaStream_t s) {
+    if (source == nullptr || l->dtype != BP_BF16) return cudaSuccess;
+    const cudaError_t e = tc_gather(X, source, n_x, groups, l->n_in, l->rows, l->flags, l->num_sms, s);
+    X = l->rows;
+    n_x = groups.n_rows;
+    source = nullptr;
+    return e;
 }
 
 static cudaError_t rows_product(const RowsArgs& a, int dtype, bool back, int num_sms, cudaStream_t s) {
@@ -286,8 +300,11 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
                                   {d_offsets, "d_offsets", 4, true},
                                   {d_Y, "d_Y", align, rows}});
     if (st != BP_OK || !rows) return st;
+    cudaStream_t s = (cudaStream_t)stream;
     RowsArgs a{};
     a.groups = {d_offsets, l->E, n_rows};
+    st = cuda_status(rows_in_order(l, a.groups, d_X, n_x, d_source, s), call);
+    if (st != BP_OK) return st;
     a.N = l->n_out;
     a.K = l->n_in;
     a.in = d_X;
@@ -298,7 +315,7 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
     a.squash = squash;
     a.out = d_Y;
     a.flags = l->flags;
-    return cuda_status(rows_product(a, l->dtype, false, l->num_sms, (cudaStream_t)stream), call);
+    return cuda_status(rows_product(a, l->dtype, false, l->num_sms, s), call);
 }
 
 bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, int n_x, const int* d_source,
@@ -323,6 +340,10 @@ bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, i
     if (st != BP_OK) return st;
     cudaStream_t s = (cudaStream_t)stream;
     const RowGroups groups{d_offsets, l->E, n_rows};
+    if (rows && needs_x) {
+        st = cuda_status(rows_in_order(l, groups, d_X, n_x, d_source, s), call);
+        if (st != BP_OK) return st;
+    }
     if (d_dX != nullptr && rows) {
         RowsArgs a{};
         a.groups = groups;

@@ -115,6 +115,9 @@ struct LowTerms {
     const int* tile_adapter;
 };
 cudaError_t tc_setup();
+// Rows read through an index into the groups' order; tc_rows and tc_change take rows in order.
+cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGroups& groups, int cols, void* out, int* flags,
+                      int num_sms, cudaStream_t s);
 cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_sms, cudaStream_t s);
 cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
 

@@ -14,8 +14,10 @@
 // the next group's rows too and does not store them; in a change, where rows are summed, the
 // stage's foreign rows are set to zero in shared memory in both operands (0 times a foreign
 // infinity would not be 0).  W's maps have a dimension of their own for the group, past whose
-// edges the copy engine fills in zeros.  Rows read through an index are gathered by the copy
-// engine, four rows an instruction, a lane each.
+// edges the copy engine fills in zeros.  Rows read through an index are copied into the rows'
+// order first: gathered by the copy engine instead (four rows an instruction, a lane each), a
+// K block waited for its 32 instructions, 539 us for 32,768 rows of 2048-2048 against 181 without
+// an index; the copy takes 25 to 30.
 //
 // The adapters' part of a tile whose rows all belong to one request is K beyond the layer's own:
 // the rows of low as two bfloat16 terms (its rounding and the rest) times the adapter's rows.  In
@@ -40,8 +42,6 @@ struct TcArgs {
     RowGroups groups;
     int num_n, num_m;        // tiles along N; along M of a change
     int M, N, K;             // M: rows of a change; K: not of a change
-    const int* source;       // rows of the gathered operand, or NULL
-    int n_src;
     const float* bias;
     int squash;
     const bf16* x;
@@ -81,15 +81,6 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
         "l"((unsigned long long)map), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
         : "memory");
 }
-// Four rows of 64 columns (the map's box is one row high).
-__device__ __forceinline__ void tma_gather4(void* dst, const CUtensorMap* map, int c0, const int (&r)[4], uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes "
-        "[%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(smem_u32(dst)),
-        "l"((unsigned long long)map), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(smem_u32(bar))
-        : "memory");
-}
-
 // A tile: rows [row0, end) of a forward or back product, of group g; of a change, all rows of the
 // group and the block mb of M.
 struct Item {
@@ -207,7 +198,7 @@ __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, i
 // which run beside the next sum's MMAs (8 K blocks of 128 x 256: 4,200).
 constexpr int kChain = 8;
 
-template <int BN, int FORM, bool GATHER>
+template <int BN, int FORM>
 __global__ void __launch_bounds__(kThreads, 1)
     k_grouped(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
               const __grid_constant__ CUtensorMap map_low, const __grid_constant__ CUtensorMap map_p,
@@ -288,20 +279,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int items = plan.items();
 
     if (warp == 0) {
-        // ---------------- copies: one lane issues, or every lane where rows are gathered
-        const bool leader = elect_one();
-        if (GATHER || leader) {
+        // ---------------- copies
+        if (elect_one()) {
             int stage = 0, issued = 0;
             unsigned phase = 0;
             bool ok = true;
             // The stage's buffer is free and its barrier expects `bytes`.
             auto open = [&](unsigned bytes) {
-                if (issued >= S) {
-                    ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
-                    if (GATHER) ok = __all_sync(0xffffffffu, ok);
-                }
-                if (ok && leader) mbar_expect_tx(&full[stage], bytes);
-                if (GATHER) __syncwarp();
+                if (issued >= S) ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
+                if (ok) mbar_expect_tx(&full[stage], bytes);
                 return ok;
             };
             auto close = [&] {
@@ -310,47 +296,31 @@ __global__ void __launch_bounds__(kThreads, 1)
             };
             for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
                 const Item w = plan.item(it);
-                // gathered rows: of the tile's 128, lane l the rows 4 l ..; of a change's K block of 64,
-                // the rows 4 (l % 16) .. (in the block's column blocks l / 16, l / 16 + 2, ..)
-                int rows[4] = {0, 0, 0, 0};
-                auto load_rows = [&](int first) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        rows[i] = first + i < w.end ? source_row(g.source, first + i, g.n_src, g.flags) : 0;
-                };
-                if (GATHER) load_rows(w.row0 + 4 * (FORM == CHANGE ? lane & 15 : lane));
                 for (int kb = 0; kb < w.kbs; ++kb) {
                     if (!open(C::kStageBytes)) break;
                     uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
                     uint64_t* bar = &full[stage];
                     if (FORM == CHANGE) {
                         const int r = w.row0 + kb * BK;
-                        if (leader)
-                            for (int i = 0; i < BM / 64; ++i)
-                                tma_load_2d(sa + i * kMnBlockBytes, &map_a, w.mb * BM + 64 * i, r, bar);
-                        if (GATHER) {
-                            for (int i = lane >> 4; i < BN / 64; i += 2)
-                                tma_gather4(sb + i * kMnBlockBytes + (lane & 15) * 512, &map_b, w.nb * BN + 64 * i, rows, bar);
-                            load_rows(r + BK + 4 * (lane & 15));   // the next block's
-                        } else {
-                            for (int i = 0; i < BN / 64; ++i)
-                                tma_load_2d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, r, bar);
-                        }
+#pragma unroll
+                        for (int i = 0; i < BM / 64; ++i)
+                            tma_load_2d(sa + i * kMnBlockBytes, &map_a, w.mb * BM + 64 * i, r, bar);
+#pragma unroll
+                        for (int i = 0; i < BN / 64; ++i)
+                            tma_load_2d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, r, bar);
                     } else {
-                        if (GATHER) tma_gather4(sa + lane * 512, &map_a, kb * BK, rows, bar);
-                        else tma_load_2d(sa, &map_a, kb * BK, w.row0, bar);
-                        if (leader) {
-                            if (FORM == FORWARD) {
-                                tma_load_3d(sb, &map_b, kb * BK, w.nb * BN, w.g, bar);
-                            } else {
-                                for (int i = 0; i < BN / 64; ++i)
-                                    tma_load_3d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, kb * BK, w.g, bar);
-                            }
+                        tma_load_2d(sa, &map_a, kb * BK, w.row0, bar);
+                        if (FORM == FORWARD) {
+                            tma_load_3d(sb, &map_b, kb * BK, w.nb * BN, w.g, bar);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < BN / 64; ++i)
+                                tma_load_3d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, kb * BK, w.g, bar);
                         }
                     }
                     close();
                 }
-                if (FORM != CHANGE && !GATHER && w.adapter >= 0) {   // the low-rank K, 4 pieces of 16 a stage
+                if (FORM != CHANGE && w.adapter >= 0) {   // the low-rank K, 4 pieces of 16 a stage
                     for (int c0 = 0; c0 < g.low_chunks && ok; c0 += 4) {
                         const int n = min(4, g.low_chunks - c0);
                         if (!open(C::kABytes + n * 16 * BN * 2)) break;
@@ -364,7 +334,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
             }
-            if (!ok && leader) {
+            if (!ok) {
                 // let every copy already issued land before the CTA can exit
                 for (int n = issued - 1; n >= 0 && n >= issued - S; --n) {   // each stage's last copy
                     const unsigned long long t0 = global_ns();
@@ -425,7 +395,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         close();
                     }
                     if (!ok) break;
-                    if (FORM != CHANGE && !GATHER && w.adapter >= 0) {
+                    if (FORM != CHANGE && w.adapter >= 0) {
                         for (int c0 = 0; c0 < g.low_chunks; c0 += 4) {
                             if (!wait(&full[stage], phase)) break;
                             const uint32_t al = low_a0 + stage * (C::kStageBytes >> 4), bl = low_b0 + stage * (C::kStageBytes >> 4);
@@ -522,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 int adapter = -1;   // of this lane's row, in a tile of several requests
-                if (!GATHER && w.adapter == kTileMixed && row < w.end) {
+                if (w.adapter == kTileMixed && row < w.end) {
                     const int i = first_request(g.req, row);
                     if (i < g.req.n_requests) {
                         int lo, hi;
@@ -546,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     float v[32];
                     tmem_ld32(trow + (uint32_t)(acc * BN + cbeg + c0), v);
-                    if (!GATHER && w.adapter == kTileMixed) add_low(g, row, adapter, n0, v);
+                    if (w.adapter == kTileMixed) add_low(g, row, adapter, n0, v);
                     if (FORM == FORWARD) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
@@ -582,6 +552,27 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
 }
 
+// Rows read through an index, copied into the groups' order, 16 bytes a thread.
+__global__ void __launch_bounds__(256)
+    k_gather(const uint4* in, const int* source, int n_src, RowGroups q, int pieces, uint4* out, int* flags) {
+    pdl_launch();
+    pdl_wait();
+    const int first = max(q.offsets[0], 0), end = min(q.offsets[q.n_groups], q.n_rows);
+    for (int r = first + blockIdx.x * blockDim.y + threadIdx.y; r < end; r += gridDim.x * blockDim.y) {
+        const uint4* from = in + (size_t)source_row(source, r, n_src, flags) * pieces;
+        uint4* to = out + (size_t)r * pieces;
+        int c = threadIdx.x;
+        for (; c + 3 * (int)blockDim.x < pieces; c += 4 * blockDim.x) {
+            uint4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = from[c + i * blockDim.x];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) to[c + i * blockDim.x] = v[i];
+        }
+        for (; c < pieces; c += blockDim.x) to[c] = from[c];
+    }
+}
+
 // ------------------------------------------------------------ host
 PFN_cuTensorMapEncodeTiled_v12000 g_encode = nullptr;
 
@@ -599,9 +590,8 @@ bool make_map(CUtensorMap* map, const void* base, int rows, int cols, int planes
 
 template <int BN>
 cudaError_t setup_width() {
-    const void* fns[] = {(const void*)k_grouped<BN, FORWARD, false>, (const void*)k_grouped<BN, FORWARD, true>,
-                         (const void*)k_grouped<BN, BACK, false>, (const void*)k_grouped<BN, CHANGE, false>,
-                         (const void*)k_grouped<BN, CHANGE, true>};
+    const void* fns[] = {(const void*)k_grouped<BN, FORWARD>, (const void*)k_grouped<BN, BACK>,
+                         (const void*)k_grouped<BN, CHANGE>};
     for (const void* f : fns) {
         const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::kSmemBytes);
         if (e != cudaSuccess) return e;
@@ -609,14 +599,14 @@ cudaError_t setup_width() {
     return cudaSuccess;
 }
 
-template <int FORM, bool GATHER>
+template <int FORM>
 cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtensorMap (&m)[4], cudaStream_t s) {
     const int grid = items < num_sms ? items : num_sms;
     if (grid < 1) return cudaSuccess;
     switch (bn) {
-        case 64: return launch_pdl(k_grouped<64, FORM, GATHER>, grid, 1, kThreads, Cfg<64>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
-        case 128: return launch_pdl(k_grouped<128, FORM, GATHER>, grid, 1, kThreads, Cfg<128>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
-        default: return launch_pdl(k_grouped<256, FORM, GATHER>, grid, 1, kThreads, Cfg<256>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+        case 64: return launch_pdl(k_grouped<64, FORM>, grid, 1, kThreads, Cfg<64>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+        case 128: return launch_pdl(k_grouped<128, FORM>, grid, 1, kThreads, Cfg<128>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
+        default: return launch_pdl(k_grouped<256, FORM>, grid, 1, kThreads, Cfg<256>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
     }
 }
 
@@ -655,13 +645,29 @@ cudaError_t tc_setup() {
     return setup_width<256>();
 }
 
+cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGroups& groups, int cols, void* out, int* flags,
+                      int num_sms, cudaStream_t s) {
+    const int pieces = cols / 8;
+    int x = 32;
+    while (x < 256 && x * 4 < pieces) x *= 2;   // threads of a row
+    const int per = 256 / x, want = ceil_div(groups.n_rows, per);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(want < 8 * num_sms ? want : 8 * num_sms);
+    c.blockDim = dim3(x, per);
+    c.stream = s;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, k_gather, (const uint4*)in, source, n_src, groups, pieces, (uint4*)out, flags);
+}
+
 cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_sms, cudaStream_t s) {
     TcArgs a{};
     a.groups = r.groups;
     a.N = r.N;
     a.K = r.K;
-    a.source = r.source;
-    a.n_src = r.n_in_rows;
     a.bias = r.bias;
     a.squash = r.squash;
     a.x = (const bf16*)r.x;
@@ -676,7 +682,7 @@ cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_s
     const int bn = pick_width(row_tiles, r.N, kbs, num_sms);
     a.num_n = ceil_div(r.N, bn);
     CUtensorMap m[4];
-    bool ok = make_map(&m[0], r.in, r.n_in_rows, r.K, 0, r.source != nullptr ? 1 : BM) &&
+    bool ok = make_map(&m[0], r.in, r.n_in_rows, r.K, 0, BM) &&
               (back ? make_map(&m[1], r.W, r.K, r.N, E, BK) : make_map(&m[1], r.W, r.N, r.K, E, bn));
     m[2] = m[3] = m[0];
     if (r.low != nullptr) {
@@ -693,8 +699,7 @@ cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_s
     if (!ok) return cudaErrorInvalidValue;
     const long long items = (long long)max_tiles(r.groups.n_rows, E, BM) * a.num_n;
     const int n = items < num_sms ? (int)items : num_sms;
-    if (back) return launch<BACK, false>(a, bn, n, num_sms, m, s);
-    return r.source != nullptr ? launch<FORWARD, true>(a, bn, n, num_sms, m, s) : launch<FORWARD, false>(a, bn, n, num_sms, m, s);
+    return back ? launch<BACK>(a, bn, n, num_sms, m, s) : launch<FORWARD>(a, bn, n, num_sms, m, s);
 }
 
 cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
@@ -702,8 +707,6 @@ cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
     a.groups = c.groups;
     a.M = c.M;
     a.N = c.N;
-    a.source = c.source;
-    a.n_src = c.n_b;
     a.G = c.G;
     a.accumulate = c.accumulate;
     a.flags = c.flags;
@@ -715,12 +718,12 @@ cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
     // without rows nothing is copied and the maps' addresses are not used; G stands in for them
     const bool rows = c.groups.n_rows > 0;
     if (!make_map(&m[0], rows ? c.a : c.G, rows ? c.groups.n_rows : 1, c.M, 0, BK) ||
-        !make_map(&m[1], rows ? c.b : c.G, rows ? c.n_b : 1, c.N, 0, c.source != nullptr ? 1 : BK))
+        !make_map(&m[1], rows ? c.b : c.G, rows ? c.n_b : 1, c.N, 0, BK))
         return cudaErrorInvalidValue;
     m[2] = m[3] = m[0];
     const long long items = (long long)E * a.num_m * a.num_n;
     const int n = items < num_sms ? (int)items : num_sms;
-    return c.source != nullptr ? launch<CHANGE, true>(a, bn, n, num_sms, m, s) : launch<CHANGE, false>(a, bn, n, num_sms, m, s);
+    return launch<CHANGE>(a, bn, n, num_sms, m, s);
 }
 
 }  // namespace bp
