@@ -26,6 +26,12 @@ struct bp_adapters {
     int n = 0, rank = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, max_requests = 0, num_sms = 0;
     int* flags = nullptr;
     float* low = nullptr;   // [cap, rank] v of the backward pass
+    // bfloat16: u or v as bfloat16 terms, u's for its change, and the adapters of row blocks
+    void* terms = nullptr;
+    void* u_terms = nullptr;
+    int* tile_adapter = nullptr;
+    int n_terms = 0, stride = 0;
+    LowTerms low_terms() const { return {terms, n_terms, stride, tile_adapter}; }
 };
 
 namespace {
@@ -279,8 +285,8 @@ static cudaError_t rows_in_order(bp_experts* l, const RowGroups& groups, const v
     return e;
 }
 
-static cudaError_t rows_product(const RowsArgs& a, int dtype, bool back, int num_sms, cudaStream_t s) {
-    return dtype == BP_BF16 ? tc_rows(a, back, {}, num_sms, s) : simt_rows(a, dtype, back, s);
+static cudaError_t rows_product(const RowsArgs& a, int dtype, bool back, const LowTerms& low, int num_sms, cudaStream_t s) {
+    return dtype == BP_BF16 ? tc_rows(a, back, low, num_sms, s) : simt_rows(a, dtype, back, s);
 }
 
 bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, const void* d_X, int n_x,
@@ -315,7 +321,7 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
     a.squash = squash;
     a.out = d_Y;
     a.flags = l->flags;
-    return cuda_status(rows_product(a, l->dtype, false, l->num_sms, s), call);
+    return cuda_status(rows_product(a, l->dtype, false, {}, l->num_sms, s), call);
 }
 
 bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, int n_x, const int* d_source,
@@ -358,7 +364,7 @@ bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, i
         a.n_x = n_x;
         a.out = d_dX;
         a.flags = l->flags;
-        st = cuda_status(rows_product(a, l->dtype, true, l->num_sms, s), call);
+        st = cuda_status(rows_product(a, l->dtype, true, {}, l->num_sms, s), call);
     }
     if (st == BP_OK && d_GW != nullptr) {
         const ChangeArgs a{groups, l->n_out, l->n_in, d_D, d_X, d_source, n_x, d_GW, accumulate, l->flags};
@@ -400,6 +406,16 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
     l->max_requests = max_requests;
     st = make_layer(dtype, &l->flags, &l->num_sms, call);
     if (st == BP_OK) st = cuda_status(cudaMalloc(&l->low, (size_t)max_rows * rank * sizeof(float)), call);
+    if (st == BP_OK && dtype == BP_BF16) {
+        // four blocks of 64 columns at most: three terms up to rank 64, two above
+        l->stride = rank <= 64 ? 64 : 128;
+        l->n_terms = rank <= 64 ? 3 : 2;
+        const size_t bytes = (size_t)max_rows * l->n_terms * l->stride * 2;
+        st = cuda_status(cudaMalloc(&l->terms, bytes), call);
+        if (st == BP_OK) st = cuda_status(cudaMalloc(&l->u_terms, bytes), call);
+        if (st == BP_OK)
+            st = cuda_status(cudaMalloc(&l->tile_adapter, ((size_t)max_rows / kTileRows + 1) * sizeof(int)), call);
+    }
     if (st != BP_OK) {
         bp_adapters_destroy(l);
         return st;
@@ -413,7 +429,16 @@ void bp_adapters_destroy(bp_adapters* l) {
     cudaDeviceSynchronize();
     cudaFree(l->flags);
     cudaFree(l->low);
+    cudaFree(l->terms);
+    cudaFree(l->u_terms);
+    cudaFree(l->tile_adapter);
     delete l;
+}
+
+static cudaError_t low_of(const bp_adapters* l, const Requests& req, int K, const void* in, const void* P, const float* scale,
+                          int scaled_low, float* low, cudaStream_t s) {
+    const LowArgs a{req, K, in, P, scale, scaled_low, low, l->terms, l->n_terms, l->stride, l->tile_adapter, l->flags};
+    return l->dtype == BP_BF16 ? low_product(a, s) : simt_low(a, l->dtype, s);
 }
 
 static bp_status check_requests(const char* call, const bp_adapters* l, int n_requests, int n_rows) {
@@ -444,8 +469,7 @@ bp_status bp_adapters_forward(bp_adapters* l, const void* d_W, const float* d_b,
     if (st != BP_OK || !rows) return st;
     cudaStream_t s = (cudaStream_t)stream;
     const Requests req{d_offsets, d_adapter, n_requests, n_rows, l->n, l->rank};
-    const LowArgs low{req, l->n_in, d_X, d_A, nullptr, d_U, l->flags};
-    st = cuda_status(simt_low(low, l->dtype, s), call);
+    st = cuda_status(low_of(l, req, l->n_in, d_X, d_A, d_scale, 0, d_U, s), call);
     if (st != BP_OK) return st;
     RowsArgs a{};
     a.groups = {nullptr, 1, n_rows};
@@ -462,7 +486,7 @@ bp_status bp_adapters_forward(bp_adapters* l, const void* d_W, const float* d_b,
     a.P = d_B;
     a.scale = d_scale;
     a.flags = l->flags;
-    return cuda_status(simt_rows(a, l->dtype, false, s), call);
+    return cuda_status(rows_product(a, l->dtype, false, l->low_terms(), l->num_sms, s), call);
 }
 
 bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A, const void* d_B, const float* d_scale,
@@ -491,8 +515,7 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
     cudaStream_t s = (cudaStream_t)stream;
     const Requests req{d_offsets, d_adapter, rows ? n_requests : 0, n_rows, l->n, l->rank};
     if (rows && (dx || ga)) {
-        const LowArgs low{req, l->n_out, d_D, d_B, d_scale, l->low, l->flags};
-        st = cuda_status(simt_low(low, l->dtype, s), call);
+        st = cuda_status(low_of(l, req, l->n_out, d_D, d_B, d_scale, 1, l->low, s), call);
     }
     if (st == BP_OK && rows && dx) {
         RowsArgs a{};
@@ -510,15 +533,20 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
         a.low = l->low;   // v: scaled already
         a.P = d_A;
         a.flags = l->flags;
-        st = cuda_status(simt_rows(a, l->dtype, true, s), call);
+        st = cuda_status(rows_product(a, l->dtype, true, l->low_terms(), l->num_sms, s), call);
     }
+    const bool tc = l->dtype == BP_BF16;
     if (st == BP_OK && ga) {
         const LowChangeArgs a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->flags};
-        st = cuda_status(simt_low_change(a, l->dtype, s), call);
+        st = cuda_status(tc ? tc_low_change(a, l->low_terms(), l->num_sms, s) : simt_low_change(a, l->dtype, s), call);
     }
     if (st == BP_OK && gb) {
         const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->flags};
-        st = cuda_status(simt_low_change(a, l->dtype, s), call);
+        LowTerms u = l->low_terms();
+        u.terms = l->u_terms;
+        if (tc && some) st = cuda_status(low_terms(d_U, n_rows, l->rank, l->u_terms, u.stride, u.n_terms, l->num_sms, s), call);
+        if (st == BP_OK)
+            st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, l->dtype, s), call);
     }
     return st;
 }

@@ -57,7 +57,13 @@ struct LowArgs {
     const void* in;
     const void* P;
     const float* scale;     // or NULL
+    int scaled_low;         // 0: low without the scale
     float* low;
+    // bfloat16: the scaled sums as n_terms bfloat16 terms, [n_rows, n_terms, terms_stride] with zeros
+    // past the rank, and the adapter of every block of kTileRows rows
+    void* terms;
+    int n_terms, terms_stride;
+    int* tile_adapter;
     int* flags;
 };
 
@@ -105,13 +111,14 @@ cudaError_t simt_low_change(const LowChangeArgs& a, int dtype, cudaStream_t s);
 cudaError_t simt_sums(const SumsArgs& a, int dtype, cudaStream_t s);
 
 // Tensor-core kernels for bfloat16 (bp_grouped_tc.cu).
-// low as kLowTerms bfloat16 terms side by side, [n_rows, kLowTerms * roundup16(rank)] with zeros past
-// the rank, scaled, and the adapter of every block of 128 rows: -1 none, kTileMixed several requests.
-constexpr int kLowTerms = 2;
+// The adapters' low-rank sums come as bfloat16 terms (LowArgs); a block of rows is of one adapter,
+// of none (-1) or of several requests (kTileMixed).
 constexpr int kTileRows = 128;
 constexpr int kTileMixed = -2;
+constexpr int kForwardTerms = 2;   // of the terms, those that a bfloat16 result can tell: 2^-17
 struct LowTerms {
     const void* terms;
+    int n_terms, stride;
     const int* tile_adapter;
 };
 cudaError_t tc_setup();
@@ -120,6 +127,12 @@ cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGro
                       int num_sms, cudaStream_t s);
 cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_sms, cudaStream_t s);
 cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
+cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, int num_sms, cudaStream_t s);
+
+// Low-rank products of bfloat16 (bp_low.cu).
+cudaError_t low_product(const LowArgs& a, cudaStream_t s);
+cudaError_t low_terms(const float* low, int n_rows, int rank, void* terms, int stride, int n_terms, int num_sms,
+                      cudaStream_t s);
 
 // Router and mix (bp_route.cu).
 struct RouteArgs {

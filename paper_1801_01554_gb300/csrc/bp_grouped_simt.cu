@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kThreads) k_low_simt(LowArgs g) {
         if (lo >= row0 + rows) break;
         const int ad = request_adapter(g.req, i, g.flags);
         if (ad < 0 || hi <= lo) continue;
-        const float c = g.scale != nullptr ? g.scale[ad] : 1.f;
+        const float c = g.scaled_low && g.scale != nullptr ? g.scale[ad] : 1.f;
         const T* P = (const T*)g.P + (size_t)ad * r * g.K;
         float part[4][4] = {};
         accumulate<true, true>(

@@ -3,7 +3,8 @@
 //
 //   forward  out[r, n]  = sum over k of in[src(r), k] W_g[n, k]     both operands along K
 //   back     out[r, n]  = sum over k of in[r, k] W_g[k, n]          W as an MN-major operand
-//   change   G_g[m, n]  = sum over the group's rows of a[r, m] b[src(r), n]   both MN-major
+//   change   G_g[m, n]  = sum over the group's rows of a[r, m] b[r, n]   both MN-major
+//   low      G_a[j, n]  = scale_a * sum over the rows of the adapter's requests of low[r, j] b[r, n]
 //
 // One persistent CTA per SM: a warp that issues TMA copies into a ring of stages, a warp that
 // issues tcgen05.mma (128 rows x BN columns x 64 of K a stage) into TMEM, eight epilogue warps.
@@ -22,7 +23,10 @@
 // The adapters' part of a tile whose rows all belong to one request is K beyond the layer's own:
 // the rows of low as two bfloat16 terms (its rounding and the rest) times the adapter's rows.  In
 // a tile of several requests the epilogue adds it row by row: as one product with the other
-// requests' rows at zero, an adapter's infinity would reach them.
+// requests' rows at zero, an adapter's infinity would reach them.  In the low form every term is a
+// product of its own into the same sums (three terms up to rank 64: as exact as float32), the K
+// blocks run over the adapter's requests in order, and the rows of a tile past the rank hold
+// sums that nobody reads.
 #include <cstdio>
 #include <mutex>
 
@@ -36,7 +40,7 @@ constexpr int kEpiWarps = 8;         // two per TMEM lane quarter, each on half 
 constexpr int kEpiThreads = 32 * kEpiWarps;
 constexpr int kThreads = 64 + kEpiThreads;   // warp 0 copies, warp 1 MMA, warps 2.. epilogue
 
-enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2 };
+enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2, LOW = 3 };
 
 struct TcArgs {
     RowGroups groups;
@@ -52,8 +56,8 @@ struct TcArgs {
     int accumulate;
     // adapters
     const int* tile_adapter;   // per 128 rows (kTileMixed: several requests), or NULL
-    int low_chunks;            // 16-wide pieces of the low-rank K
     int rank16;                // 16-wide pieces of the rank
+    int n_terms, stride;       // bfloat16 terms of low, and their pitch (a multiple of 64)
     Requests req;
     const float* low;
     const bf16* P;
@@ -61,10 +65,13 @@ struct TcArgs {
     int* flags;
 };
 
-template <int BN>
+// An operand A of the low form holds all terms: up to four blocks of 64 columns.
+constexpr int kLowBlocks = 4;
+
+template <int BN, int FORM>
 struct Cfg {
-    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
-    static constexpr int kABytes = BM * BK * 2;
+    static constexpr int kStages = BN == 256 ? 4 : FORM == LOW ? (BN == 128 ? 4 : 5) : BN == 128 ? 6 : 8;
+    static constexpr int kABytes = FORM == LOW ? kLowBlocks * BK * 64 * 2 : BM * BK * 2;
     static constexpr int kBBytes = BN * BK * 2;
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kRingBytes = kStages * kStageBytes;
@@ -89,6 +96,37 @@ struct Item {
     int adapter;    // whose low-rank K follows, kTileMixed, or -1
 };
 
+// The runs of rows that a change sums over: the group's, or of the low form the requests of adapter
+// w.g in order, which the whole warp looks for.
+template <int FORM>
+struct Runs {
+    const TcArgs& g;
+    const Item& w;
+    int at;
+    __device__ bool next(int& lo, int& hi) {
+        if (FORM != LOW) {
+            lo = w.row0;
+            hi = w.end;
+            return at++ == 0 && hi > lo;
+        }
+        const int lane = threadIdx.x & 31;
+        while (at < g.req.n_requests) {
+            const int base = at & ~31, i = base + lane;
+            const bool mine = i >= at && i < g.req.n_requests && g.req.adapter[i] == w.g;
+            const unsigned m = __ballot_sync(0xffffffffu, mine);
+            if (m == 0) {
+                at = base + 32;
+                continue;
+            }
+            const int r = base + __ffs(m) - 1;
+            at = r + 1;
+            group_rows(g.req.offsets, g.req.n_rows, r, lo, hi, g.flags);
+            if (hi > lo) return true;
+        }
+        return false;
+    }
+};
+
 // Row blocks of a group are swept 16 at a time over all column blocks (row block fastest), so
 // that the tiles in flight share rows and weights in L2 (16: as square as 152 tiles of
 // 128 x 256 get).
@@ -105,10 +143,21 @@ struct Schedule {
     const TcArgs& g;
     const int *lo, *hi, *tile0;   // per group, in shared memory: first row, end; first row block (n_groups + 1)
     __device__ int items() const {
+        if (FORM == LOW) return g.req.n_adapters * g.num_n;
         return FORM == CHANGE ? g.groups.n_groups * g.num_m * g.num_n : tile0[g.groups.n_groups] * g.num_n;
     }
     __device__ Item item(int it) const {
         Item w;
+        if (FORM == LOW) {
+            w.g = it / g.num_n;
+            w.nb = it - w.g * g.num_n;
+            w.mb = w.row0 = w.end = w.kbs = 0;
+            w.adapter = -1;
+            Runs<LOW> runs{g, w, 0};
+            int lo, hi;
+            while (runs.next(lo, hi)) w.kbs += (hi - lo + BK - 1) / BK;
+            return w;
+        }
         if (FORM == CHANGE) {
             const int per = g.num_m * g.num_n;
             w.g = it / per;
@@ -203,9 +252,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     k_grouped(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
               const __grid_constant__ CUtensorMap map_low, const __grid_constant__ CUtensorMap map_p,
               const __grid_constant__ TcArgs g) {
-    using C = Cfg<BN>;
+    using C = Cfg<BN, FORM>;
     constexpr int S = C::kStages;
-    constexpr bool kAMn = FORM == CHANGE, kBMn = FORM != FORWARD;
+    constexpr bool kChange = FORM == CHANGE || FORM == LOW;
+    constexpr bool kAMn = kChange, kBMn = FORM != FORWARD;
     constexpr int kAcc = 2;   // the epilogue of a sum overlaps the next one's MMAs
     constexpr int kTmemCols = kAcc * BN;
     extern __shared__ uint8_t smem_raw[];
@@ -279,62 +329,76 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int items = plan.items();
 
     if (warp == 0) {
-        // ---------------- copies
-        if (elect_one()) {
+        // ---------------- copies, by one lane
+        const bool leader = elect_one();
+        if (FORM == LOW || leader) {   // (the warp looks for an adapter's requests)
             int stage = 0, issued = 0;
             unsigned phase = 0;
             bool ok = true;
             // The stage's buffer is free and its barrier expects `bytes`.
             auto open = [&](unsigned bytes) {
-                if (issued >= S) ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
-                if (ok) mbar_expect_tx(&full[stage], bytes);
+                if (issued >= S) {
+                    ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
+                    if (FORM == LOW) ok = __all_sync(0xffffffffu, ok);
+                }
+                if (ok && leader) mbar_expect_tx(&full[stage], bytes);
                 return ok;
             };
             auto close = [&] {
                 ++issued;
                 if (++stage == S) { stage = 0; phase ^= 1u; }
             };
+            const int a_blocks = FORM == LOW ? g.n_terms * (g.stride / 64) : BM / 64;
             for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
                 const Item w = plan.item(it);
-                for (int kb = 0; kb < w.kbs; ++kb) {
-                    if (!open(C::kStageBytes)) break;
-                    uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
-                    uint64_t* bar = &full[stage];
-                    if (FORM == CHANGE) {
-                        const int r = w.row0 + kb * BK;
+                if constexpr (kChange) {
+                    Runs<FORM> runs{g, w, 0};
+                    int lo, hi;
+                    while (ok && runs.next(lo, hi)) {
+                        for (int r = lo; r < hi; r += BK) {
+                            if (!open(a_blocks * kMnBlockBytes + C::kBBytes)) break;
+                            uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
+                            if (leader) {
+                                for (int i = 0; i < a_blocks; ++i)
+                                    tma_load_2d(sa + i * kMnBlockBytes, &map_a, w.mb * BM + 64 * i, r, &full[stage]);
 #pragma unroll
-                        for (int i = 0; i < BM / 64; ++i)
-                            tma_load_2d(sa + i * kMnBlockBytes, &map_a, w.mb * BM + 64 * i, r, bar);
-#pragma unroll
-                        for (int i = 0; i < BN / 64; ++i)
-                            tma_load_2d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, r, bar);
-                    } else {
-                        tma_load_2d(sa, &map_a, kb * BK, w.row0, bar);
+                                for (int i = 0; i < BN / 64; ++i)
+                                    tma_load_2d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, r, &full[stage]);
+                            }
+                            close();
+                        }
+                    }
+                } else {
+                    for (int kb = 0; kb < w.kbs; ++kb) {
+                        if (!open(C::kStageBytes)) break;
+                        uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
+                        tma_load_2d(sa, &map_a, kb * BK, w.row0, &full[stage]);
                         if (FORM == FORWARD) {
-                            tma_load_3d(sb, &map_b, kb * BK, w.nb * BN, w.g, bar);
+                            tma_load_3d(sb, &map_b, kb * BK, w.nb * BN, w.g, &full[stage]);
                         } else {
 #pragma unroll
                             for (int i = 0; i < BN / 64; ++i)
-                                tma_load_3d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, kb * BK, w.g, bar);
+                                tma_load_3d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, kb * BK, w.g, &full[stage]);
                         }
-                    }
-                    close();
-                }
-                if (FORM != CHANGE && w.adapter >= 0) {   // the low-rank K, 4 pieces of 16 a stage
-                    for (int c0 = 0; c0 < g.low_chunks && ok; c0 += 4) {
-                        const int n = min(4, g.low_chunks - c0);
-                        if (!open(C::kABytes + n * 16 * BN * 2)) break;
-                        uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
-                        tma_load_2d(sa, &map_low, c0 * 16, w.row0, &full[stage]);
-                        for (int c = 0; c < n; ++c)
-                            for (int i = 0; i < BN / 64; ++i)
-                                tma_load_3d(sb + i * kMnBlockBytes + c * 16 * 128, &map_p, w.nb * BN + 64 * i,
-                                            (c0 + c) % g.rank16 * 16, w.adapter, &full[stage]);
                         close();
+                    }
+                    if (w.adapter >= 0) {   // the low-rank K, up to 4 pieces of 16 of a term a stage
+                        for (int t = 0; t < kForwardTerms; ++t)
+                            for (int c0 = 0; c0 < g.rank16 && ok; c0 += 4) {
+                                const int n = min(4, g.rank16 - c0);
+                                if (!open(C::kABytes + n * 16 * BN * 2)) break;
+                                uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
+                                tma_load_2d(sa, &map_low, t * g.stride + c0 * 16, w.row0, &full[stage]);
+                                for (int c = 0; c < n; ++c)
+                                    for (int i = 0; i < BN / 64; ++i)
+                                        tma_load_3d(sb + i * kMnBlockBytes + c * 16 * 128, &map_p, w.nb * BN + 64 * i,
+                                                    (c0 + c) * 16, w.adapter, &full[stage]);
+                                close();
+                            }
                     }
                 }
             }
-            if (!ok) {
+            if (!ok && leader) {
                 // let every copy already issued land before the CTA can exit
                 for (int n = issued - 1; n >= 0 && n >= issued - S; --n) {   // each stage's last copy
                     const unsigned long long t0 = global_ns();
@@ -346,16 +410,15 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == 1) {
         // ---------------- MMA: one lane issues; of a change the warp clears foreign rows
         const bool leader = elect_one();
-        if (FORM == CHANGE || leader) {
+        if (kChange || leader) {
             constexpr uint32_t idesc = idesc_bf16(BM, BN, kAMn, kBMn), idesc_low = idesc_bf16(BM, BN, false, true);
             const uint32_t a0 = desc_lo<kAMn>(smem_u32(ring)), b0 = desc_lo<kBMn>(smem_u32(ring) + C::kABytes);
-            const uint32_t low_a0 = desc_lo<false>(smem_u32(ring)), low_b0 = desc_lo<true>(smem_u32(ring) + C::kABytes);
             int stage = 0, acc = 0;
             unsigned phase = 0, acc_phase = 0;
             bool ok = true, issued_any = false;
             auto wait = [&](uint64_t* bar, unsigned parity) {
                 ok = mbar_wait(bar, parity, abort_flag, g.flags);
-                if (FORM == CHANGE) ok = __all_sync(0xffffffffu, ok);
+                if (kChange) ok = __all_sync(0xffffffffu, ok);
                 tc_fence_after();
                 return ok;
             };
@@ -364,49 +427,69 @@ __global__ void __launch_bounds__(kThreads, 1)
                 issued_any = true;
                 if (++stage == S) { stage = 0; phase ^= 1u; }
             };
+            auto done = [&] {   // the accumulator's sum is complete
+                if (leader) umma_commit(&tfull[acc]);
+                if (++acc == kAcc) { acc = 0; acc_phase ^= 1u; }
+            };
             for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
                 const Item w = plan.item(it);
-                const int chain = FORM == CHANGE ? kChain : w.kbs;
-                for (int k0 = 0; k0 < w.kbs && ok; k0 += chain) {
-                    const int k1 = min(w.kbs, k0 + chain);
-                    if (!wait(&tempty[acc], acc_phase ^ 1u)) break;
-                    const uint32_t tmem_d = tmem_base + (uint32_t)(acc * BN);
-                    for (int kb = k0; kb < k1; ++kb) {
-                        if (!wait(&full[stage], phase)) break;
-                        const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = b0 + stage * (C::kStageBytes >> 4);
-                        int steps = BK / UMMA_K;
-                        if (FORM == CHANGE) {
-                            const int valid = w.end - w.row0 - kb * BK;
-                            if (valid < BK) {   // (uniform) the group's last rows
+                if constexpr (kChange) {
+                    const int terms = FORM == LOW ? g.n_terms : 1;
+                    const uint32_t term_step = FORM == LOW ? (uint32_t)(g.stride / 64) * (kMnBlockBytes >> 4) : 0u;
+                    Runs<FORM> runs{g, w, 0};
+                    int lo, hi, kb = 0;
+                    while (ok && runs.next(lo, hi)) {
+                        for (int r = lo; r < hi; r += BK, ++kb) {
+                            if (kb % kChain == 0 && !wait(&tempty[acc], acc_phase ^ 1u)) break;
+                            if (!wait(&full[stage], phase)) break;
+                            const uint32_t tmem_d = tmem_base + (uint32_t)(acc * BN);
+                            const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = b0 + stage * (C::kStageBytes >> 4);
+                            int steps = BK / UMMA_K;
+                            const int valid = hi - r;
+                            if (valid < BK) {   // (uniform) the run's last rows
                                 steps = (valid + UMMA_K - 1) / UMMA_K;
                                 uint8_t* sa = ring + stage * C::kStageBytes;
-                                zero_rows(sa, BM / 64 + BN / 64, valid, steps * UMMA_K);   // A's blocks, then B's
+                                zero_rows(sa, terms * (FORM == LOW ? g.stride : BM) / 64, valid, steps * UMMA_K);
+                                zero_rows(sa + C::kABytes, BN / 64, valid, steps * UMMA_K);
                                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                                 __syncwarp();
                             }
-                        }
-                        if (leader) {
-                            umma_bf16<idesc>(tmem_d, al, bl, kb > k0 ? 1u : 0u);
+                            if (leader) {
+                                for (int t = 0; t < terms; ++t)
 #pragma unroll
-                            for (int kk = 1; kk < BK / UMMA_K; ++kk)
-                                if (FORM != CHANGE || kk < steps)
-                                    umma_bf16<idesc>(tmem_d, al + kk * k_step_units<kAMn>(), bl + kk * k_step_units<kBMn>(), 1u);
+                                    for (int kk = 0; kk < BK / UMMA_K; ++kk)
+                                        if (kk < steps)
+                                            umma_bf16<idesc>(tmem_d, al + t * term_step + kk * k_step_units<kAMn>(),
+                                                             bl + kk * k_step_units<kBMn>(), kb % kChain != 0 || t > 0 || kk > 0 ? 1u : 0u);
+                            }
+                            close();
+                            if (kb % kChain == kChain - 1 || kb == w.kbs - 1) done();
                         }
+                    }
+                } else {
+                    if (!wait(&tempty[acc], acc_phase ^ 1u)) break;
+                    const uint32_t tmem_d = tmem_base + (uint32_t)(acc * BN);
+                    for (int kb = 0; kb < w.kbs; ++kb) {
+                        if (!wait(&full[stage], phase)) break;
+                        const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = b0 + stage * (C::kStageBytes >> 4);
+                        umma_bf16<idesc>(tmem_d, al, bl, kb > 0 ? 1u : 0u);
+#pragma unroll
+                        for (int kk = 1; kk < BK / UMMA_K; ++kk)
+                            umma_bf16<idesc>(tmem_d, al + kk * k_step_units<kAMn>(), bl + kk * k_step_units<kBMn>(), 1u);
                         close();
                     }
-                    if (!ok) break;
-                    if (FORM != CHANGE && w.adapter >= 0) {
-                        for (int c0 = 0; c0 < g.low_chunks; c0 += 4) {
-                            if (!wait(&full[stage], phase)) break;
-                            const uint32_t al = low_a0 + stage * (C::kStageBytes >> 4), bl = low_b0 + stage * (C::kStageBytes >> 4);
-                            for (int c = 0; c < min(4, g.low_chunks - c0); ++c)
-                                umma_bf16<idesc_low>(tmem_d, al + c * k_step_units<false>(), bl + c * k_step_units<true>(), 1u);
-                            close();
-                        }
-                        if (!ok) break;
+                    if (w.adapter >= 0) {
+                        const uint32_t low_b0 = desc_lo<true>(smem_u32(ring) + C::kABytes);
+                        for (int t = 0; t < kForwardTerms; ++t)
+                            for (int c0 = 0; c0 < g.rank16 && ok; c0 += 4) {
+                                if (!wait(&full[stage], phase)) break;
+                                const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = low_b0 + stage * (C::kStageBytes >> 4);
+                                for (int c = 0; c < min(4, g.rank16 - c0); ++c)
+                                    umma_bf16<idesc_low>(tmem_d, al + c * k_step_units<false>(), bl + c * k_step_units<true>(), 1u);
+                                close();
+                            }
                     }
-                    if (leader) umma_commit(&tfull[acc]);
-                    if (++acc == kAcc) { acc = 0; acc_phase ^= 1u; }
+                    if (ok) done();
                 }
             }
             if (!ok && issued_any && leader) {
@@ -439,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         for (int it = blockIdx.x; it < items; it += gridDim.x) {
             const Item w = plan.item(it);
-            if constexpr (FORM == CHANGE) {
+            if constexpr (kChange) {
                 float part[BN / 2];
 #pragma unroll
                 for (int c = 0; c < BN / 2; ++c) part[c] = 0.f;
@@ -459,12 +542,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!stay) break;
                 const int m = w.mb * BM + q * 32 + lane;
                 float* dst = g.G + ((size_t)w.g * g.M + m) * g.N;
+                const float scale = FORM == LOW && g.scale != nullptr ? g.scale[w.g] : 1.f;
                 if (m < g.M) {
 #pragma unroll
                     for (int c = 0; c < BN / 2; c += 4) {
                         const int n = w.nb * BN + cbeg + c;
                         if (n >= g.N) break;   // N is a multiple of 8
                         float4 o = make_float4(part[c], part[c + 1], part[c + 2], part[c + 3]);
+                        if (FORM == LOW) o.x *= scale, o.y *= scale, o.z *= scale, o.w *= scale;
                         if (g.accumulate) {
                             const float4 old = *reinterpret_cast<const float4*>(dst + n);
                             o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
@@ -588,26 +673,27 @@ bool make_map(CUtensorMap* map, const void* base, int rows, int cols, int planes
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <int BN, int FORM>
+cudaError_t setup_one() {
+    return cudaFuncSetAttribute(k_grouped<BN, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN, FORM>::kSmemBytes);
+}
 template <int BN>
 cudaError_t setup_width() {
-    const void* fns[] = {(const void*)k_grouped<BN, FORWARD>, (const void*)k_grouped<BN, BACK>,
-                         (const void*)k_grouped<BN, CHANGE>};
-    for (const void* f : fns) {
-        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN>::kSmemBytes);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    cudaError_t e;
+    if ((e = setup_one<BN, FORWARD>()) != cudaSuccess) return e;
+    if ((e = setup_one<BN, BACK>()) != cudaSuccess) return e;
+    return setup_one<BN, CHANGE>();
 }
 
 template <int FORM>
 cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtensorMap (&m)[4], cudaStream_t s) {
     const int grid = items < num_sms ? items : num_sms;
     if (grid < 1) return cudaSuccess;
-    switch (bn) {
-        case 64: return launch_pdl(k_grouped<64, FORM>, grid, 1, kThreads, Cfg<64>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
-        case 128: return launch_pdl(k_grouped<128, FORM>, grid, 1, kThreads, Cfg<128>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
-        default: return launch_pdl(k_grouped<256, FORM>, grid, 1, kThreads, Cfg<256>::kSmemBytes, s, m[0], m[1], m[2], m[3], a);
-    }
+    auto go = [&](auto k, int smem) { return launch_pdl(k, grid, 1, kThreads, smem, s, m[0], m[1], m[2], m[3], a); };
+    if (bn == 64) return go(k_grouped<64, FORM>, Cfg<64, FORM>::kSmemBytes);
+    if (bn == 128 || FORM == LOW) return go(k_grouped<128, FORM>, Cfg<128, FORM>::kSmemBytes);
+    if constexpr (FORM != LOW) return go(k_grouped<256, FORM>, Cfg<256, FORM>::kSmemBytes);
+    return cudaErrorInvalidValue;
 }
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
@@ -642,7 +728,9 @@ cudaError_t tc_setup() {
     cudaError_t e;
     if ((e = setup_width<64>()) != cudaSuccess) return e;
     if ((e = setup_width<128>()) != cudaSuccess) return e;
-    return setup_width<256>();
+    if ((e = setup_width<256>()) != cudaSuccess) return e;
+    if ((e = setup_one<64, LOW>()) != cudaSuccess) return e;
+    return setup_one<128, LOW>();
 }
 
 cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGroups& groups, int cols, void* out, int* flags,
@@ -688,12 +776,12 @@ cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_s
     if (r.low != nullptr) {
         a.tile_adapter = low.tile_adapter;
         a.rank16 = ceil_div(r.req.rank, 16);
-        a.low_chunks = kLowTerms * a.rank16;
+        a.stride = low.stride;
         a.req = r.req;
         a.low = r.low;
         a.P = (const bf16*)r.P;
         a.scale = r.scale;
-        ok = ok && make_map(&m[2], low.terms, r.groups.n_rows, a.low_chunks * 16, 0, BM) &&
+        ok = ok && make_map(&m[2], low.terms, r.groups.n_rows, low.n_terms * low.stride, 0, BM) &&
              make_map(&m[3], r.P, r.req.rank, r.N, r.req.n_adapters, 16);
     }
     if (!ok) return cudaErrorInvalidValue;
@@ -724,6 +812,32 @@ cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
     const long long items = (long long)E * a.num_m * a.num_n;
     const int n = items < num_sms ? (int)items : num_sms;
     return launch<CHANGE>(a, bn, n, num_sms, m, s);
+}
+
+// A CTA sums all rows of an adapter for a block of columns: 64 wide, so that a few adapters keep
+// the SMs busy, 128 where that many blocks do too (half the reads of low).
+cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, int num_sms, cudaStream_t s) {
+    TcArgs a{};
+    a.req = c.req;
+    a.M = c.req.rank;
+    a.N = c.N;
+    a.G = c.G;
+    a.scale = c.scale;
+    a.accumulate = c.accumulate;
+    a.n_terms = low.n_terms;
+    a.stride = low.stride;
+    a.flags = c.flags;
+    const int n_ad = c.req.n_adapters, busy = n_ad < c.req.n_requests ? n_ad : c.req.n_requests;
+    const int bn = (long long)busy * ceil_div(c.N, 128) >= num_sms ? 128 : 64;
+    a.num_n = ceil_div(c.N, bn);
+    CUtensorMap m[4];
+    const bool rows = c.req.n_rows > 0;   // (tc_change)
+    if (!make_map(&m[0], rows ? low.terms : c.G, rows ? c.req.n_rows : 1, low.n_terms * low.stride, 0, BK) ||
+        !make_map(&m[1], rows ? c.b : c.G, rows ? c.req.n_rows : 1, c.N, 0, BK))
+        return cudaErrorInvalidValue;
+    m[2] = m[3] = m[0];
+    const long long items = (long long)n_ad * a.num_n;
+    return launch<LOW>(a, bn, items < num_sms ? (int)items : num_sms, num_sms, m, s);
 }
 
 }  // namespace bp

@@ -1,0 +1,226 @@
+// The low-rank products of the adapter layers in bfloat16: low = scale_a P_a x for the rows of
+// every request, on mma.sync.
+//
+// A product with so few columns is bound by reading x (and, of requests of one row, by reading
+// their adapters): 16,384 rows of 4,096 are 134 MB and 20 us at the measured copy rate, the
+// 2 * 64 * 16,384 * 4,096 flops of rank 64 a fraction of that on mma.sync, whose 16-row tiles fit
+// short requests where a tcgen05 tile would hold 128 rows.  A CTA takes up to 64 rows of one
+// request and reads x and P_a straight into the operands' registers, 16 bytes a lane: a lane's
+// eight values of k stand for the four pairs that two MMAs want, the same eight in both operands,
+// so that the sum over k is merely taken in another order.  Warps share K and, from 32 on, the rank;
+// their sums are added in shared memory in a fixed order.
+#include "bp_experts_device.cuh"
+
+namespace bp {
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kRows = 64, kThreads = 256, kWarps = kThreads / 32;
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The unit-th run of up to kRows rows of one request; the whole block calls it.  Request, first row
+// and end, or request -1 past the last unit.
+__device__ __forceinline__ void find_unit(const Requests& q, int unit, int (&where)[3], int* warp_tot, int* flags) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) where[0] = -1;
+    for (int base = 0; base < q.n_requests; base += kThreads) {
+        const int i = base + threadIdx.x;
+        int lo = 0, hi = 0;
+        if (i < q.n_requests) group_rows(q.offsets, q.n_rows, i, lo, hi, flags);
+        const int units = (hi - lo + kRows - 1) / kRows;
+        int sum = units;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += y;
+        }
+        __syncthreads();
+        if (lane == 31) warp_tot[warp] = sum;
+        __syncthreads();
+        int before = 0, total = 0;
+        for (int w = 0; w < kWarps; ++w) {
+            if (w < warp) before += warp_tot[w];
+            total += warp_tot[w];
+        }
+        const int first = before + sum - units;
+        if (unit >= first && unit < first + units) {
+            where[0] = i;
+            where[1] = lo + (unit - first) * kRows;
+            where[2] = min(hi, where[1] + kRows);
+        }
+        if (unit < total) break;
+        unit -= total;
+    }
+    __syncthreads();
+}
+
+// A row's terms: x rounded to bfloat16, the rest rounded, ..; they add up to x but for 2^-17 (two)
+// or 2^-25 (three) of it.
+__device__ __forceinline__ void store_terms(bf16* terms, int stride, int n_terms, float x) {
+    for (int t = 0; t < n_terms; ++t) {
+        const bf16 h = __float2bfloat16_rn(x);
+        terms[t * stride] = h;
+        const float f = __bfloat162float(h);
+        x = isfinite(f) ? x - f : 0.f;
+    }
+}
+
+// What rows of one request hold in low and in the terms, from a sum or from `given`.
+struct Sink {
+    const LowArgs& g;
+    float scale_low, scale_terms;
+    __device__ __forceinline__ void put(int row, int j, float sum) const {
+        const int r = g.req.rank, stride = g.terms_stride;
+        if (j < r) g.low[(size_t)row * r + j] = scale_low * sum;
+        if (j < stride) store_terms((bf16*)g.terms + (size_t)row * g.n_terms * stride + j, stride, g.n_terms, j < r ? scale_terms * sum : 0.f);
+    }
+};
+
+// MT tiles of 16 rows by NT of 8 of the rank, over this warp's steps of 32 of K.
+template <int MT, int NT>
+__device__ __forceinline__ void accumulate(float (&acc)[MT][NT][4], const bf16* x, int rows, const bf16* P, int ranks, int K,
+                                           int first, int step) {
+    const int lane = threadIdx.x & 31, gr = lane >> 2, k8 = (lane & 3) * 8;
+#pragma unroll 2
+    for (int k0 = first * 32; k0 < K; k0 += step * 32) {
+        const int k = k0 + k8;
+        uint4 a[MT][2], b[NT];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = 16 * m + 8 * h + gr;
+                a[m][h] = row < rows && k < K ? *reinterpret_cast<const uint4*>(x + (size_t)row * K + k) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int j = 8 * n + gr;
+            b[n] = j < ranks && k < K ? *reinterpret_cast<const uint4*>(P + (size_t)j * K + k) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                mma_16816(acc[m][n], a[m][0].x, a[m][1].x, a[m][0].y, a[m][1].y, b[n].x, b[n].y);
+                mma_16816(acc[m][n], a[m][0].z, a[m][1].z, a[m][0].w, a[m][1].w, b[n].z, b[n].w);
+            }
+    }
+}
+
+template <int MT, int NT>
+__device__ __forceinline__ void low_rows(const LowArgs& g, const Sink& sink, int row0, int rows, int adapter, int rank_warps,
+                                         float* red) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = g.req.rank;
+    const int kw = warp / rank_warps, nw = warp - kw * rank_warps, k_warps = kWarps / rank_warps;   // this warp's share
+    const int j0 = nw * NT * 8;
+    float acc[MT][NT][4] = {};
+    accumulate<MT, NT>(acc, (const bf16*)g.in + (size_t)row0 * g.K, rows, (const bf16*)g.P + ((size_t)adapter * r + j0) * g.K, r - j0,
+                       g.K, kw, k_warps);
+    for (int s = k_warps / 2; s >= 1; s >>= 1) {
+        __syncthreads();
+        float* at = red + (size_t)((kw % s) * rank_warps + nw) * MT * NT * 128 + lane;
+        if (kw >= s && kw < 2 * s) {
+#pragma unroll
+            for (int i = 0; i < MT * NT * 4; ++i) at[i * 32] = acc[i / (NT * 4)][i / 4 % NT][i % 4];
+        }
+        __syncthreads();
+        if (kw < s) {
+#pragma unroll
+            for (int i = 0; i < MT * NT * 4; ++i) acc[i / (NT * 4)][i / 4 % NT][i % 4] += at[i * 32];
+        }
+    }
+    if (kw > 0) return;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * m + (lane >> 2) + 8 * (i >> 1), j = j0 + 8 * n + 2 * (lane & 3) + (i & 1);
+                if (row < rows) sink.put(row0 + row, j, acc[m][n][i]);
+            }
+    // ranks that no warp's tiles reach are only the terms' zeros
+    for (int i = lane + 32 * nw; i < rows * g.terms_stride; i += 32 * rank_warps) {
+        const int row = i / g.terms_stride, j = i - row * g.terms_stride;
+        if (j >= rank_warps * NT * 8) sink.put(row0 + row, j, 0.f);
+    }
+}
+
+// NT: eights of the rank of a warp.
+template <int NT>
+__global__ void __launch_bounds__(kThreads) k_low(LowArgs g, int rank_warps, int tiles) {
+    __shared__ int where[3];
+    __shared__ int warp_tot[kWarps];
+    __shared__ float red[kWarps / 2 * (kRows / 16) * NT * 128];
+    const Requests& q = g.req;
+    // the adapters of the blocks of kTileRows rows
+    for (int t = blockIdx.x + gridDim.x * threadIdx.x; t < tiles; t += gridDim.x * kThreads) {
+        const int row0 = t * kTileRows, end = min(row0 + kTileRows, q.n_rows), i = first_request(q, row0);
+        int lo = end, hi = end, a = -1;
+        if (i < q.n_requests) group_rows(q.offsets, q.n_rows, i, lo, hi, g.flags);
+        if (lo < end) a = lo <= row0 && hi >= end ? request_adapter(q, i, g.flags) : kTileMixed;
+        g.tile_adapter[t] = a;
+    }
+    if (blockIdx.x == 0) {   // rows outside every request
+        const int lo = q.n_requests > 0 ? min(max(q.offsets[0], 0), q.n_rows) : q.n_rows;
+        const int hi = q.n_requests > 0 ? min(max(q.offsets[q.n_requests], lo), q.n_rows) : q.n_rows;
+        const Sink none{g, 0.f, 0.f};
+        for (long long i = threadIdx.x; i < (long long)(lo + q.n_rows - hi) * g.terms_stride; i += kThreads) {
+            const int row = (int)(i / g.terms_stride), j = (int)(i - (long long)row * g.terms_stride);
+            none.put(row < lo ? row : row - lo + hi, j, 0.f);
+        }
+    }
+    find_unit(q, blockIdx.x, where, warp_tot, g.flags);
+    if (where[0] < 0) return;
+    const int row0 = where[1], rows = where[2] - where[1], adapter = request_adapter(q, where[0], g.flags);
+    if (adapter < 0) {
+        const Sink none{g, 0.f, 0.f};
+        for (int i = threadIdx.x; i < rows * g.terms_stride; i += kThreads) none.put(row0 + i / g.terms_stride, i % g.terms_stride, 0.f);
+        return;
+    }
+    const float c = g.scale != nullptr ? g.scale[adapter] : 1.f;
+    const Sink sink{g, g.scaled_low ? c : 1.f, c};
+    if (rows <= 16) low_rows<1, NT>(g, sink, row0, rows, adapter, rank_warps, red);
+    else low_rows<kRows / 16, NT>(g, sink, row0, rows, adapter, rank_warps, red);
+}
+
+// The terms of given float32 rows [n_rows, rank].
+__global__ void __launch_bounds__(kThreads) k_terms(const float* low, int n_rows, int rank, bf16* terms, int stride, int n_terms) {
+    const long long n = (long long)n_rows * stride;
+    for (long long i = (long long)blockIdx.x * kThreads + threadIdx.x; i < n; i += (long long)gridDim.x * kThreads) {
+        const long long row = i / stride;
+        const int j = (int)(i - row * stride);
+        store_terms(terms + row * n_terms * stride + j, stride, n_terms, j < rank ? low[row * rank + j] : 0.f);
+    }
+}
+
+}  // namespace
+
+cudaError_t low_product(const LowArgs& a, cudaStream_t s) {
+    const int tiles = (a.req.n_rows + kTileRows - 1) / kTileRows;
+    int units = max_tiles(a.req.n_rows, a.req.n_requests, kRows);
+    if (units < 1) units = 1;
+    if (a.req.rank <= 16) {
+        k_low<2><<<units, kThreads, 0, s>>>(a, 1, tiles);
+    } else {
+        const int w = a.req.rank <= 32 ? 1 : a.req.rank <= 64 ? 2 : 4;
+        k_low<4><<<units, kThreads, 0, s>>>(a, w, tiles);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t low_terms(const float* low, int n_rows, int rank, void* terms, int stride, int n_terms, int num_sms, cudaStream_t s) {
+    const long long want = ((long long)n_rows * stride + kThreads - 1) / kThreads;
+    k_terms<<<(int)(want < 8 * num_sms ? want : 8 * num_sms), kThreads, 0, s>>>(low, n_rows, rank, (bf16*)terms, stride, n_terms);
+    return cudaGetLastError();
+}
+
+}  // namespace bp
