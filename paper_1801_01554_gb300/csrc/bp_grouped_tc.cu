@@ -216,6 +216,32 @@ __device__ __forceinline__ void store_rows(bf16* out, int N, int row0, int end, 
     __syncwarp();   // the block may be rewritten
 }
 
+// Stores a warp's 32 x 16 block of float32 changes.  The block turns in shared memory (16-byte pieces
+// permuted by row), after which four lanes hold 64 bytes of a row: whole sectors.  Stored by rows as
+// TMEM gives them, 16 bytes a lane and row, a 128 x 256 tile took 20,000 clocks.
+__device__ __forceinline__ void store_change(float* G, int M, int N, int m0, int n0, const float (&v)[16], int accumulate,
+                                             float4* sF) {
+    const int lane = threadIdx.x & 31, piece = lane & 3, n = n0 + 4 * piece;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        sF[lane * 4 + (k ^ ((lane >> 1) & 3))] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int row = 8 * j + (lane >> 2), m = m0 + row;
+        float4 o = sF[row * 4 + (piece ^ ((row >> 1) & 3))];
+        if (m < M && n < N) {   // N is a multiple of 8
+            float4* p = reinterpret_cast<float4*>(G + (size_t)m * N + n);
+            if (accumulate) {
+                const float4 old = *p;
+                o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
+            }
+            __stcs(p, o);
+        }
+    }
+    __syncwarp();   // the block may be rewritten
+}
+
 // scale_a * sum over j of low[row, j] P_a[j, n0 .. n0 + 31] added to a row's sums (a: the adapter of
 // the row's request).
 __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, int n0, float (&v)[32]) {
@@ -245,7 +271,7 @@ __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, i
 // 2-norm error of the changes of 4096 x 4096 weights by 2,048 rows a group against float64:
 // see the measurements in the design notes' table; a drained sum costs the epilogue about 500 clocks,
 // which run beside the next sum's MMAs (8 K blocks of 128 x 256: 4,200).
-constexpr int kChain = 8;
+constexpr int kChain = 8, kLowChain = 2;
 
 template <int BN, int FORM>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -256,6 +282,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr int S = C::kStages;
     constexpr bool kChange = FORM == CHANGE || FORM == LOW;
     constexpr bool kAMn = kChange, kBMn = FORM != FORWARD;
+    constexpr int kChainBlocks = FORM == LOW ? kLowChain : kChain;
     constexpr int kAcc = 2;   // the epilogue of a sum overlaps the next one's MMAs
     constexpr int kTmemCols = kAcc * BN;
     extern __shared__ uint8_t smem_raw[];
@@ -440,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     int lo, hi, kb = 0;
                     while (ok && runs.next(lo, hi)) {
                         for (int r = lo; r < hi; r += BK, ++kb) {
-                            if (kb % kChain == 0 && !wait(&tempty[acc], acc_phase ^ 1u)) break;
+                            if (kb % kChainBlocks == 0 && !wait(&tempty[acc], acc_phase ^ 1u)) break;
                             if (!wait(&full[stage], phase)) break;
                             const uint32_t tmem_d = tmem_base + (uint32_t)(acc * BN);
                             const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = b0 + stage * (C::kStageBytes >> 4);
@@ -460,10 +487,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                                     for (int kk = 0; kk < BK / UMMA_K; ++kk)
                                         if (kk < steps)
                                             umma_bf16<idesc>(tmem_d, al + t * term_step + kk * k_step_units<kAMn>(),
-                                                             bl + kk * k_step_units<kBMn>(), kb % kChain != 0 || t > 0 || kk > 0 ? 1u : 0u);
+                                                             bl + kk * k_step_units<kBMn>(), kb % kChainBlocks != 0 || t > 0 || kk > 0 ? 1u : 0u);
                             }
                             close();
-                            if (kb % kChain == kChain - 1 || kb == w.kbs - 1) done();
+                            if (kb % kChainBlocks == kChainBlocks - 1 || kb == w.kbs - 1) done();
                         }
                     }
                 } else {
@@ -527,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int c = 0; c < BN / 2; ++c) part[c] = 0.f;
                 bool stay = true;
-                for (int k0 = 0; k0 < w.kbs; k0 += kChain) {
+                for (int k0 = 0; k0 < w.kbs; k0 += kChainBlocks) {
                     stay = wait_acc();
                     if (!stay) break;
 #pragma unroll
@@ -540,22 +567,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                     release();
                 }
                 if (!stay) break;
-                const int m = w.mb * BM + q * 32 + lane;
-                float* dst = g.G + ((size_t)w.g * g.M + m) * g.N;
                 const float scale = FORM == LOW && g.scale != nullptr ? g.scale[w.g] : 1.f;
-                if (m < g.M) {
+                const int m0 = w.mb * BM + q * 32;
+                float* G = g.G + (size_t)w.g * g.M * g.N;
 #pragma unroll
-                    for (int c = 0; c < BN / 2; c += 4) {
-                        const int n = w.nb * BN + cbeg + c;
-                        if (n >= g.N) break;   // N is a multiple of 8
-                        float4 o = make_float4(part[c], part[c + 1], part[c + 2], part[c + 3]);
-                        if (FORM == LOW) o.x *= scale, o.y *= scale, o.z *= scale, o.w *= scale;
-                        if (g.accumulate) {
-                            const float4 old = *reinterpret_cast<const float4*>(dst + n);
-                            o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
-                        }
-                        *reinterpret_cast<float4*>(dst + n) = o;
-                    }
+                for (int c = 0; c < BN / 2; c += 16) {
+                    const int n0 = w.nb * BN + cbeg + c;
+                    if (m0 >= g.M || n0 >= g.N) break;
+                    float v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = scale * part[c + i];
+                    store_change(G, g.M, g.N, m0, n0, v, g.accumulate, reinterpret_cast<float4*>(sS4));
                 }
             } else {
                 const int m0 = w.row0 + q * 32, row = m0 + lane;
