@@ -26,12 +26,12 @@ struct bp_adapters {
     int n = 0, rank = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, max_requests = 0, num_sms = 0;
     int* flags = nullptr;
     float* low = nullptr;   // [cap, rank] v of the backward pass
-    // bfloat16: u or v as bfloat16 terms, u's for its change, and the adapters of row blocks
+    // bfloat16: u or v as bfloat16 terms, u's for its change, and what row blocks hold
     void* terms = nullptr;
     void* u_terms = nullptr;
-    int* tile_adapter = nullptr;
+    int2* tiles = nullptr;
     int n_terms = 0, stride = 0;
-    LowTerms low_terms() const { return {terms, n_terms, stride, tile_adapter}; }
+    LowTerms low_terms() const { return {terms, n_terms, stride, tiles}; }
 };
 
 namespace {
@@ -414,7 +414,7 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
         st = cuda_status(cudaMalloc(&l->terms, bytes), call);
         if (st == BP_OK) st = cuda_status(cudaMalloc(&l->u_terms, bytes), call);
         if (st == BP_OK)
-            st = cuda_status(cudaMalloc(&l->tile_adapter, ((size_t)max_rows / kTileRows + 1) * sizeof(int)), call);
+            st = cuda_status(cudaMalloc(&l->tiles, ((size_t)max_rows / kTileRows + 1) * sizeof(int2)), call);
     }
     if (st != BP_OK) {
         bp_adapters_destroy(l);
@@ -431,14 +431,15 @@ void bp_adapters_destroy(bp_adapters* l) {
     cudaFree(l->low);
     cudaFree(l->terms);
     cudaFree(l->u_terms);
-    cudaFree(l->tile_adapter);
+    cudaFree(l->tiles);
     delete l;
 }
 
 static cudaError_t low_of(const bp_adapters* l, const Requests& req, int K, const void* in, const void* P, const float* scale,
                           int scaled_low, float* low, cudaStream_t s) {
-    const LowArgs a{req, K, in, P, scale, scaled_low, low, l->terms, l->n_terms, l->stride, l->tile_adapter, l->flags};
-    return l->dtype == BP_BF16 ? low_product(a, s) : simt_low(a, l->dtype, s);
+    const LowArgs a{req, K, in, P, scale, scaled_low, low, l->terms, l->n_terms, l->stride, l->tiles, l->flags};
+    if (l->dtype != BP_BF16) return simt_low(a, l->dtype, s);
+    return (long long)req.n_rows >= 64ll * req.n_requests && req.n_requests > 0 ? tc_low(a, l->num_sms, s) : low_product(a, s);
 }
 
 static bp_status check_requests(const char* call, const bp_adapters* l, int n_requests, int n_rows) {

@@ -88,6 +88,35 @@ __device__ __forceinline__ void find_tile(const RowGroups& q, int tile, int& g, 
     row0 = end = 0;
 }
 
+// What block t of kTileRows rows holds (see kTileRows).
+__device__ __forceinline__ int2 tile_info(const Requests& q, int t, int* flags) {
+    const int row0 = t * kTileRows, end = min(row0 + kTileRows, q.n_rows), first = first_request(q, row0);
+    int count = 0;
+    for (int i = first; i < q.n_requests; ++i) {
+        int lo, hi;
+        group_rows(q.offsets, q.n_rows, i, lo, hi, flags);
+        if (lo >= end) break;
+        if (hi <= lo) continue;
+        const int a = request_adapter(q, i, flags);
+        if (lo <= row0 && hi >= end) return make_int2(a, i);
+        if (a >= 0 && ++count > q.rank) return make_int2(kTileByRow, first);
+    }
+    return make_int2(count > 0 ? kTileMixed : -1, first);
+}
+
+// Rows outside every request: zeros in low [n_rows, rank] and in the terms [n_rows, pitch].
+__device__ __forceinline__ void zero_outside(const Requests& q, int thread, int threads, float* low, __nv_bfloat16* terms,
+                                             int pitch) {
+    const int lo = q.n_requests > 0 ? min(max(q.offsets[0], 0), q.n_rows) : q.n_rows;
+    const int hi = q.n_requests > 0 ? min(max(q.offsets[q.n_requests], lo), q.n_rows) : q.n_rows;
+    for (long long i = thread; i < (long long)(lo + q.n_rows - hi) * pitch; i += threads) {
+        const long long k = i / pitch, row = k < lo ? k : k - lo + hi;
+        const int j = (int)(i - k * pitch);
+        terms[row * pitch + j] = __float2bfloat16_rn(0.f);
+        if (j < q.rank) low[row * q.rank + j] = 0.f;
+    }
+}
+
 // Most blocks of TM rows that n_rows rows in n_groups groups can make.
 inline int max_tiles(long long n_rows, long long n_groups, int TM) {
     const long long t = n_rows / TM + n_groups;

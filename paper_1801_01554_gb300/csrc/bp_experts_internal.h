@@ -60,10 +60,10 @@ struct LowArgs {
     int scaled_low;         // 0: low without the scale
     float* low;
     // bfloat16: the scaled sums as n_terms bfloat16 terms, [n_rows, n_terms, terms_stride] with zeros
-    // past the rank, and the adapter of every block of kTileRows rows
+    // past the rank, and what every block of kTileRows rows holds
     void* terms;
     int n_terms, terms_stride;
-    int* tile_adapter;
+    int2* tiles;
     int* flags;
 };
 
@@ -111,15 +111,16 @@ cudaError_t simt_low_change(const LowChangeArgs& a, int dtype, cudaStream_t s);
 cudaError_t simt_sums(const SumsArgs& a, int dtype, cudaStream_t s);
 
 // Tensor-core kernels for bfloat16 (bp_grouped_tc.cu).
-// The adapters' low-rank sums come as bfloat16 terms (LowArgs); a block of rows is of one adapter,
-// of none (-1) or of several requests (kTileMixed).
+// The adapters' low-rank sums come as bfloat16 terms (LowArgs).  A block of kTileRows rows is of one
+// adapter (x: which), of none (-1), or of several requests, y being the first: whose sums are taken
+// apart (kTileMixed), or whose rows are (kTileByRow, where they are more than the rank).
 constexpr int kTileRows = 128;
-constexpr int kTileMixed = -2;
+constexpr int kTileMixed = -2, kTileByRow = -3;
 constexpr int kForwardTerms = 2;   // of the terms, those that a bfloat16 result can tell: 2^-17
 struct LowTerms {
     const void* terms;
     int n_terms, stride;
-    const int* tile_adapter;
+    int2* tiles;
 };
 cudaError_t tc_setup();
 // Rows read through an index into the groups' order; tc_rows and tc_change take rows in order.
@@ -127,6 +128,7 @@ cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGro
                       int num_sms, cudaStream_t s);
 cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_sms, cudaStream_t s);
 cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
+cudaError_t tc_low(const LowArgs& a, int num_sms, cudaStream_t s);
 cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, int num_sms, cudaStream_t s);
 
 // Low-rank products of bfloat16 (bp_low.cu).

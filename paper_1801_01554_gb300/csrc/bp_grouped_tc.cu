@@ -4,6 +4,7 @@
 //   forward  out[r, n]  = sum over k of in[src(r), k] W_g[n, k]     both operands along K
 //   back     out[r, n]  = sum over k of in[r, k] W_g[k, n]          W as an MN-major operand
 //   change   G_g[m, n]  = sum over the group's rows of a[r, m] b[r, n]   both MN-major
+//   up       low[r, j]  = scale_a * sum over k of in[r, k] P_a[j, k], a the adapter of the row's request
 //   low      G_a[j, n]  = scale_a * sum over the rows of the adapter's requests of low[r, j] b[r, n]
 //
 // One persistent CTA per SM: a warp that issues TMA copies into a ring of stages, a warp that
@@ -22,8 +23,10 @@
 //
 // The adapters' part of a tile whose rows all belong to one request is K beyond the layer's own:
 // the rows of low as two bfloat16 terms (its rounding and the rest) times the adapter's rows.  In
-// a tile of several requests the epilogue adds it row by row: as one product with the other
-// requests' rows at zero, an adapter's infinity would reach them.  In the low form every term is a
+// a tile of several requests each request's part is a sum of its own for all of the tile's rows, of
+// which the epilogue adds the request's rows (as one product with the other requests' rows at zero,
+// an adapter's infinity would reach them); with more requests than the rank has columns the
+// epilogue takes the rows one by one instead.  In the low form every term is a
 // product of its own into the same sums (three terms up to rank 64: as exact as float32), the K
 // blocks run over the adapter's requests in order, and the rows of a tile past the rank hold
 // sums that nobody reads.
@@ -40,7 +43,7 @@ constexpr int kEpiWarps = 8;         // two per TMEM lane quarter, each on half 
 constexpr int kEpiThreads = 32 * kEpiWarps;
 constexpr int kThreads = 64 + kEpiThreads;   // warp 0 copies, warp 1 MMA, warps 2.. epilogue
 
-enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2, LOW = 3 };
+enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2, LOW = 3, UP = 4 };
 
 struct TcArgs {
     RowGroups groups;
@@ -55,13 +58,18 @@ struct TcArgs {
     float* G;
     int accumulate;
     // adapters
-    const int* tile_adapter;   // per 128 rows (kTileMixed: several requests), or NULL
+    int2* tiles;               // per 128 rows: adapter or kind, first request; or NULL
     int rank16;                // 16-wide pieces of the rank
     int n_terms, stride;       // bfloat16 terms of low, and their pitch (a multiple of 64)
     Requests req;
     const float* low;
     const bf16* P;
     const float* scale;
+    // up
+    float* low_out;
+    bf16* terms;
+    int scaled_low, wide_low;   // low with the scale; in 16-byte pieces
+    int max_items;
     int* flags;
 };
 
@@ -93,7 +101,27 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
 struct Item {
     int g, row0, end, mb, nb;
     int kbs;        // K blocks
-    int adapter;    // whose low-rank K follows, kTileMixed, or -1
+    int adapter;    // whose low-rank K follows; of an up product, the rows'; -1, or a kind of tile
+    int request;    // the tile's first
+};
+
+// The requests with an adapter that have rows in a tile, in order.
+struct TileRequests {
+    const TcArgs& g;
+    const Item& w;
+    int at;
+    __device__ bool next(int& lo, int& hi, int& adapter) {
+        for (; at < g.req.n_requests; ++at) {
+            group_rows(g.req.offsets, g.req.n_rows, at, lo, hi, g.flags);
+            if (lo >= w.end) return false;
+            if (hi <= lo) continue;
+            adapter = request_adapter(g.req, at, g.flags);
+            if (adapter < 0) continue;
+            ++at;
+            return true;
+        }
+        return false;
+    }
 };
 
 // The runs of rows that a change sums over: the group's, or of the low form the requests of adapter
@@ -144,6 +172,7 @@ struct Schedule {
     const int *lo, *hi, *tile0;   // per group, in shared memory: first row, end; first row block (n_groups + 1)
     __device__ int items() const {
         if (FORM == LOW) return g.req.n_adapters * g.num_n;
+        if (FORM == UP) return g.max_items;
         return FORM == CHANGE ? g.groups.n_groups * g.num_m * g.num_n : tile0[g.groups.n_groups] * g.num_n;
     }
     __device__ Item item(int it) const {
@@ -152,10 +181,19 @@ struct Schedule {
             w.g = it / g.num_n;
             w.nb = it - w.g * g.num_n;
             w.mb = w.row0 = w.end = w.kbs = 0;
-            w.adapter = -1;
+            w.adapter = w.request = -1;
             Runs<LOW> runs{g, w, 0};
             int lo, hi;
             while (runs.next(lo, hi)) w.kbs += (hi - lo + BK - 1) / BK;
+            return w;
+        }
+        if (FORM == UP) {   // (the whole warp asks)
+            int end;
+            find_tile<BM>(RowGroups{g.req.offsets, g.req.n_requests, g.req.n_rows}, it, w.request, w.row0, end, g.flags);
+            w.g = w.nb = w.mb = 0;
+            w.end = min(end, w.row0 + BM);
+            w.adapter = w.request >= 0 ? request_adapter(g.req, w.request, g.flags) : -1;
+            w.kbs = w.adapter >= 0 ? (g.K + BK - 1) / BK : 0;
             return w;
         }
         if (FORM == CHANGE) {
@@ -165,7 +203,7 @@ struct Schedule {
             w.row0 = lo[w.g];
             w.end = hi[w.g];
             w.kbs = (w.end - w.row0 + BK - 1) / BK;
-            w.adapter = -1;
+            w.adapter = w.request = -1;
             return w;
         }
         int a = 0, b = g.groups.n_groups;   // the last group whose first tile is not past `it`, with tiles
@@ -180,7 +218,9 @@ struct Schedule {
         w.mb = tile0[a] + mb;
         w.row0 = lo[a] + mb * BM;
         w.kbs = (g.K + BK - 1) / BK;
-        w.adapter = g.tile_adapter != nullptr ? g.tile_adapter[mb] : -1;
+        const int2 t = g.tiles != nullptr ? g.tiles[mb] : make_int2(-1, 0);
+        w.adapter = t.x;
+        w.request = t.y;
         w.end = min(hi[a], w.row0 + BM);
         return w;
     }
@@ -242,6 +282,32 @@ __device__ __forceinline__ void store_change(float* G, int M, int N, int m0, int
     __syncwarp();   // the block may be rewritten
 }
 
+// The same for 16 columns of low [n_rows, rank], rows below `end`; in 16-byte pieces if they are whole.
+__device__ __forceinline__ void store_low(float* low, int rank, int row0, int end, int j0, const float (&v)[16], int wide,
+                                          float4* sF) {
+    const int lane = threadIdx.x & 31, piece = lane & 3, j = j0 + 4 * piece;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        sF[lane * 4 + (k ^ ((lane >> 1) & 3))] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 2);
+        const float4 o = sF[r * 4 + (piece ^ ((r >> 1) & 3))];
+        if (row0 + r >= end || j >= rank) continue;
+        float* p = low + (size_t)(row0 + r) * rank + j;
+        if (wide) {
+            *reinterpret_cast<float4*>(p) = o;
+        } else {
+            p[0] = o.x;
+            if (j + 1 < rank) p[1] = o.y;
+            if (j + 2 < rank) p[2] = o.z;
+            if (j + 3 < rank) p[3] = o.w;
+        }
+    }
+    __syncwarp();   // the block may be rewritten
+}
+
 // scale_a * sum over j of low[row, j] P_a[j, n0 .. n0 + 31] added to a row's sums (a: the adapter of
 // the row's request).
 __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, int n0, float (&v)[32]) {
@@ -271,6 +337,7 @@ __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, i
 // 2-norm error of the changes of 4096 x 4096 weights by 2,048 rows a group against float64:
 // see the measurements in the design notes' table; a drained sum costs the epilogue about 500 clocks,
 // which run beside the next sum's MMAs (8 K blocks of 128 x 256: 4,200).
+// (An adapter's change has three products a K block, and few columns to drain.)
 constexpr int kChain = 8, kLowChain = 2;
 
 template <int BN, int FORM>
@@ -281,7 +348,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     using C = Cfg<BN, FORM>;
     constexpr int S = C::kStages;
     constexpr bool kChange = FORM == CHANGE || FORM == LOW;
-    constexpr bool kAMn = kChange, kBMn = FORM != FORWARD;
+    constexpr bool kFinds = FORM == LOW || FORM == UP;   // the warp looks for requests together
+    constexpr bool kAMn = kChange, kBMn = FORM != FORWARD && FORM != UP;
     constexpr int kChainBlocks = FORM == LOW ? kLowChain : kChain;
     constexpr int kAcc = 2;   // the epilogue of a sum overlaps the next one's MMAs
     constexpr int kTmemCols = kAcc * BN;
@@ -352,13 +420,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    if (FORM == UP && warp >= 2) {
+        for (int t = blockIdx.x + gridDim.x * (threadIdx.x - 64); t < (g.req.n_rows + kTileRows - 1) / kTileRows;
+             t += gridDim.x * kEpiThreads)
+            g.tiles[t] = tile_info(g.req, t, g.flags);
+        if (blockIdx.x == 0) zero_outside(g.req, threadIdx.x - 64, kEpiThreads, g.low_out, g.terms, g.n_terms * g.stride);
+        __syncwarp();
+    }
     const Schedule<FORM> plan{g, s_lo, s_hi, s_tile0};
     const int items = plan.items();
 
     if (warp == 0) {
         // ---------------- copies, by one lane
         const bool leader = elect_one();
-        if (FORM == LOW || leader) {   // (the warp looks for an adapter's requests)
+        if (kFinds || leader) {
             int stage = 0, issued = 0;
             unsigned phase = 0;
             bool ok = true;
@@ -366,7 +441,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             auto open = [&](unsigned bytes) {
                 if (issued >= S) {
                     ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
-                    if (FORM == LOW) ok = __all_sync(0xffffffffu, ok);
+                    if (kFinds) ok = __all_sync(0xffffffffu, ok);
                 }
                 if (ok && leader) mbar_expect_tx(&full[stage], bytes);
                 return ok;
@@ -399,8 +474,10 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int kb = 0; kb < w.kbs; ++kb) {
                         if (!open(C::kStageBytes)) break;
                         uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
-                        tma_load_2d(sa, &map_a, kb * BK, w.row0, &full[stage]);
-                        if (FORM == FORWARD) {
+                        if (leader) tma_load_2d(sa, &map_a, kb * BK, w.row0, &full[stage]);
+                        if (FORM == UP) {
+                            if (leader) tma_load_3d(sb, &map_b, kb * BK, 0, w.adapter, &full[stage]);
+                        } else if (FORM == FORWARD) {
                             tma_load_3d(sb, &map_b, kb * BK, w.nb * BN, w.g, &full[stage]);
                         } else {
 #pragma unroll
@@ -409,19 +486,28 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         close();
                     }
-                    if (w.adapter >= 0) {   // the low-rank K, up to 4 pieces of 16 of a term a stage
-                        for (int t = 0; t < kForwardTerms; ++t)
-                            for (int c0 = 0; c0 < g.rank16 && ok; c0 += 4) {
-                                const int n = min(4, g.rank16 - c0);
-                                if (!open(C::kABytes + n * 16 * BN * 2)) break;
-                                uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
-                                tma_load_2d(sa, &map_low, t * g.stride + c0 * 16, w.row0, &full[stage]);
-                                for (int c = 0; c < n; ++c)
-                                    for (int i = 0; i < BN / 64; ++i)
-                                        tma_load_3d(sb + i * kMnBlockBytes + c * 16 * 128, &map_p, w.nb * BN + 64 * i,
-                                                    (c0 + c) * 16, w.adapter, &full[stage]);
-                                close();
-                            }
+                    if constexpr (FORM != UP) {
+                        // the low-rank K of one adapter, up to 4 pieces of 16 of a term a stage
+                        auto load_low = [&](int adapter) {
+                            for (int t = 0; t < kForwardTerms; ++t)
+                                for (int c0 = 0; c0 < g.rank16 && ok; c0 += 4) {
+                                    const int n = min(4, g.rank16 - c0);
+                                    if (!open(C::kABytes + n * 16 * BN * 2)) break;
+                                    uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
+                                    tma_load_2d(sa, &map_low, t * g.stride + c0 * 16, w.row0, &full[stage]);
+                                    for (int c = 0; c < n; ++c)
+                                        for (int i = 0; i < BN / 64; ++i)
+                                            tma_load_3d(sb + i * kMnBlockBytes + c * 16 * 128, &map_p, w.nb * BN + 64 * i,
+                                                        (c0 + c) * 16, adapter, &full[stage]);
+                                    close();
+                                }
+                        };
+                        if (ok && w.adapter >= 0) load_low(w.adapter);
+                        if (ok && w.adapter == kTileMixed) {
+                            TileRequests all{g, w, w.request};
+                            int lo, hi, adapter;
+                            while (ok && all.next(lo, hi, adapter)) load_low(adapter);
+                        }
                     }
                 }
             }
@@ -437,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == 1) {
         // ---------------- MMA: one lane issues; of a change the warp clears foreign rows
         const bool leader = elect_one();
-        if (kChange || leader) {
+        if (kChange || kFinds || leader) {
             constexpr uint32_t idesc = idesc_bf16(BM, BN, kAMn, kBMn), idesc_low = idesc_bf16(BM, BN, false, true);
             const uint32_t a0 = desc_lo<kAMn>(smem_u32(ring)), b0 = desc_lo<kBMn>(smem_u32(ring) + C::kABytes);
             int stage = 0, acc = 0;
@@ -445,7 +531,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             bool ok = true, issued_any = false;
             auto wait = [&](uint64_t* bar, unsigned parity) {
                 ok = mbar_wait(bar, parity, abort_flag, g.flags);
-                if (kChange) ok = __all_sync(0xffffffffu, ok);
+                if (kChange || kFinds) ok = __all_sync(0xffffffffu, ok);
                 tc_fence_after();
                 return ok;
             };
@@ -494,29 +580,50 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                     }
                 } else {
-                    if (!wait(&tempty[acc], acc_phase ^ 1u)) break;
-                    const uint32_t tmem_d = tmem_base + (uint32_t)(acc * BN);
-                    for (int kb = 0; kb < w.kbs; ++kb) {
-                        if (!wait(&full[stage], phase)) break;
-                        const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = b0 + stage * (C::kStageBytes >> 4);
-                        umma_bf16<idesc>(tmem_d, al, bl, kb > 0 ? 1u : 0u);
+                    const int chain = FORM == UP ? kChain : w.kbs;
+                    for (int k0 = 0; k0 < w.kbs && ok; k0 += chain) {
+                        const int k1 = min(w.kbs, k0 + chain);
+                        if (!wait(&tempty[acc], acc_phase ^ 1u)) break;
+                        const uint32_t tmem_d = tmem_base + (uint32_t)(acc * BN);
+                        for (int kb = k0; kb < k1; ++kb) {
+                            if (!wait(&full[stage], phase)) break;
+                            const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = b0 + stage * (C::kStageBytes >> 4);
+                            if (leader) {
+                                umma_bf16<idesc>(tmem_d, al, bl, kb > k0 ? 1u : 0u);
 #pragma unroll
-                        for (int kk = 1; kk < BK / UMMA_K; ++kk)
-                            umma_bf16<idesc>(tmem_d, al + kk * k_step_units<kAMn>(), bl + kk * k_step_units<kBMn>(), 1u);
-                        close();
-                    }
-                    if (w.adapter >= 0) {
-                        const uint32_t low_b0 = desc_lo<true>(smem_u32(ring) + C::kABytes);
-                        for (int t = 0; t < kForwardTerms; ++t)
-                            for (int c0 = 0; c0 < g.rank16 && ok; c0 += 4) {
-                                if (!wait(&full[stage], phase)) break;
-                                const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = low_b0 + stage * (C::kStageBytes >> 4);
-                                for (int c = 0; c < min(4, g.rank16 - c0); ++c)
-                                    umma_bf16<idesc_low>(tmem_d, al + c * k_step_units<false>(), bl + c * k_step_units<true>(), 1u);
-                                close();
+                                for (int kk = 1; kk < BK / UMMA_K; ++kk)
+                                    umma_bf16<idesc>(tmem_d, al + kk * k_step_units<kAMn>(), bl + kk * k_step_units<kBMn>(), 1u);
                             }
+                            close();
+                        }
+                        if constexpr (FORM != UP) {
+                            const uint32_t low_b0 = desc_lo<true>(smem_u32(ring) + C::kABytes);
+                            auto add_low = [&](bool fresh) {   // into accumulator acc
+                                const uint32_t d = tmem_base + (uint32_t)(acc * BN);
+                                for (int t = 0; t < kForwardTerms; ++t)
+                                    for (int c0 = 0; c0 < g.rank16 && ok; c0 += 4) {
+                                        if (!wait(&full[stage], phase)) break;
+                                        const uint32_t al = a0 + stage * (C::kStageBytes >> 4), bl = low_b0 + stage * (C::kStageBytes >> 4);
+                                        for (int c = 0; c < min(4, g.rank16 - c0); ++c) {
+                                            umma_bf16<idesc_low>(d, al + c * k_step_units<false>(), bl + c * k_step_units<true>(), fresh ? 0u : 1u);
+                                            fresh = false;
+                                        }
+                                        close();
+                                    }
+                            };
+                            if (ok && w.adapter >= 0) add_low(false);
+                            if (ok && w.adapter == kTileMixed) {
+                                TileRequests all{g, w, w.request};
+                                int lo, hi, adapter;
+                                while (ok && all.next(lo, hi, adapter)) {
+                                    done();
+                                    if (!wait(&tempty[acc], acc_phase ^ 1u)) break;
+                                    add_low(true);
+                                }
+                            }
+                        }
+                        if (ok) done();
                     }
-                    if (ok) done();
                 }
             }
             if (!ok && issued_any && leader) {
@@ -542,14 +649,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             tc_fence_after();
             return !leave;
         };
-        auto release = [&] {
+        auto free_acc = [&](int a) {
             tc_fence_before();
-            mbar_arrive(&tempty[acc]);
+            mbar_arrive(&tempty[a]);
+        };
+        auto next_acc = [&] {
             if (++acc == kAcc) { acc = 0; acc_phase ^= 1u; }
+        };
+        auto release = [&] {
+            free_acc(acc);
+            next_acc();
         };
         for (int it = blockIdx.x; it < items; it += gridDim.x) {
             const Item w = plan.item(it);
-            if constexpr (kChange) {
+            if constexpr (kChange || FORM == UP) {
                 float part[BN / 2];
 #pragma unroll
                 for (int c = 0; c < BN / 2; ++c) part[c] = 0.f;
@@ -567,6 +680,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                     release();
                 }
                 if (!stay) break;
+                if constexpr (FORM == UP) {
+                    if (w.request < 0) continue;
+                    const float scale = g.scale != nullptr && w.adapter >= 0 ? g.scale[w.adapter] : 1.f;
+                    const int row0 = w.row0 + q * 32;
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 16) {
+                        float v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = (g.scaled_low ? scale : 1.f) * part[c + i];
+                        store_low(g.low_out, g.req.rank, row0, w.end, cbeg + c, v, g.wide_low, reinterpret_cast<float4*>(sS4));
+                    }
+                    for (int t = 0; t < g.n_terms; ++t) {
+#pragma unroll
+                        for (int c = 0; c < BN / 2; c += 32) {
+                            float v[32];
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {   // part keeps what the terms so far leave
+                                const float x = t == 0 ? (cbeg + c + i < g.req.rank ? scale * part[c + i] : 0.f) : part[c + i];
+                                v[i] = x;
+                                const float h = __bfloat162float(__float2bfloat16_rn(x));
+                                part[c + i] = isfinite(h) ? x - h : 0.f;
+                            }
+                            store_rows(g.terms, g.n_terms * g.stride, row0, w.end, t * g.stride + cbeg + c, v, sS4);
+                        }
+                    }
+                    continue;
+                }
                 const float scale = FORM == LOW && g.scale != nullptr ? g.scale[w.g] : 1.f;
                 const int m0 = w.mb * BM + q * 32;
                 float* G = g.G + (size_t)w.g * g.M * g.N;
@@ -598,8 +738,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                         xr[j] = r < w.end ? source_row(g.x_source, r, g.n_x, g.flags) : -1;
                     }
                 }
-                int adapter = -1;   // of this lane's row, in a tile of several requests
-                if (w.adapter == kTileMixed && row < w.end) {
+                int adapter = -1;   // of this lane's row, in a tile that is taken row by row
+                if (w.adapter == kTileByRow && row < w.end) {
                     const int i = first_request(g.req, row);
                     if (i < g.req.n_requests) {
                         int lo, hi;
@@ -608,6 +748,31 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 if (!wait_acc()) break;
+                if (w.adapter == kTileMixed) {
+                    // each request's sums: its rows, with the sums so far, replace them
+                    TileRequests all{g, w, w.request};
+                    int lo, hi, a;
+                    bool stay = true;
+                    while (all.next(lo, hi, a)) {
+                        const int before = acc;
+                        next_acc();
+                        stay = wait_acc();
+                        if (!stay) break;
+                        const bool mine = row >= lo && row < hi;
+#pragma unroll 1
+                        for (int c = 0; c < BN / 2; c += 16) {
+                            float x[16], v[16];
+                            tmem_ld16(trow + (uint32_t)(before * BN + cbeg + c), x);
+                            tmem_ld16(trow + (uint32_t)(acc * BN + cbeg + c), v);
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) v[k] = mine ? x[k] + v[k] : x[k];
+                            tmem_st16(trow + (uint32_t)(acc * BN + cbeg + c), v);
+                        }
+                        tmem_wait_st();
+                        free_acc(before);
+                    }
+                    if (!stay) break;
+                }
 #pragma unroll 1
                 for (int i = 0; i < BN / 64; ++i) {
                     const int c0 = 32 * i, n0 = w.nb * BN + cbeg + c0;
@@ -623,7 +788,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     float v[32];
                     tmem_ld32(trow + (uint32_t)(acc * BN + cbeg + c0), v);
-                    if (w.adapter == kTileMixed) add_low(g, row, adapter, n0, v);
+                    if (w.adapter == kTileByRow) add_low(g, row, adapter, n0, v);
                     if (FORM == FORWARD) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
@@ -713,8 +878,8 @@ cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtens
     if (grid < 1) return cudaSuccess;
     auto go = [&](auto k, int smem) { return launch_pdl(k, grid, 1, kThreads, smem, s, m[0], m[1], m[2], m[3], a); };
     if (bn == 64) return go(k_grouped<64, FORM>, Cfg<64, FORM>::kSmemBytes);
-    if (bn == 128 || FORM == LOW) return go(k_grouped<128, FORM>, Cfg<128, FORM>::kSmemBytes);
-    if constexpr (FORM != LOW) return go(k_grouped<256, FORM>, Cfg<256, FORM>::kSmemBytes);
+    if (bn == 128 || FORM == LOW || FORM == UP) return go(k_grouped<128, FORM>, Cfg<128, FORM>::kSmemBytes);
+    if constexpr (FORM != LOW && FORM != UP) return go(k_grouped<256, FORM>, Cfg<256, FORM>::kSmemBytes);
     return cudaErrorInvalidValue;
 }
 
@@ -752,7 +917,9 @@ cudaError_t tc_setup() {
     if ((e = setup_width<128>()) != cudaSuccess) return e;
     if ((e = setup_width<256>()) != cudaSuccess) return e;
     if ((e = setup_one<64, LOW>()) != cudaSuccess) return e;
-    return setup_one<128, LOW>();
+    if ((e = setup_one<128, LOW>()) != cudaSuccess) return e;
+    if ((e = setup_one<64, UP>()) != cudaSuccess) return e;
+    return setup_one<128, UP>();
 }
 
 cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGroups& groups, int cols, void* out, int* flags,
@@ -796,7 +963,7 @@ cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_s
               (back ? make_map(&m[1], r.W, r.K, r.N, E, BK) : make_map(&m[1], r.W, r.N, r.K, E, bn));
     m[2] = m[3] = m[0];
     if (r.low != nullptr) {
-        a.tile_adapter = low.tile_adapter;
+        a.tiles = low.tiles;
         a.rank16 = ceil_div(r.req.rank, 16);
         a.stride = low.stride;
         a.req = r.req;
@@ -834,6 +1001,29 @@ cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
     const long long items = (long long)E * a.num_m * a.num_n;
     const int n = items < num_sms ? (int)items : num_sms;
     return launch<CHANGE>(a, bn, n, num_sms, m, s);
+}
+
+cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
+    TcArgs a{};
+    a.req = l.req;
+    a.K = l.K;
+    a.num_n = 1;
+    a.scale = l.scale;
+    a.scaled_low = l.scaled_low;
+    a.low_out = l.low;
+    a.wide_low = l.req.rank % 4 == 0 && ((uintptr_t)l.low & 15) == 0;
+    a.terms = (bf16*)l.terms;
+    a.n_terms = l.n_terms;
+    a.stride = l.terms_stride;
+    a.tiles = l.tiles;
+    a.flags = l.flags;
+    a.max_items = max_tiles(l.req.n_rows, l.req.n_requests, BM);
+    const int bn = l.req.rank <= 64 ? 64 : 128;   // = the terms' stride: the tile writes them in full
+    CUtensorMap m[4];
+    if (!make_map(&m[0], l.in, l.req.n_rows, l.K, 0, BM) || !make_map(&m[1], l.P, l.req.rank, l.K, l.req.n_adapters, bn))
+        return cudaErrorInvalidValue;
+    m[2] = m[3] = m[0];
+    return launch<UP>(a, bn, a.max_items < num_sms ? a.max_items : num_sms, num_sms, m, s);
 }
 
 // A CTA sums all rows of an adapter for a block of columns: 64 wide, so that a few adapters keep

@@ -161,23 +161,8 @@ __global__ void __launch_bounds__(kThreads) k_low(LowArgs g, int rank_warps, int
     __shared__ int warp_tot[kWarps];
     __shared__ float red[kWarps / 2 * (kRows / 16) * NT * 128];
     const Requests& q = g.req;
-    // the adapters of the blocks of kTileRows rows
-    for (int t = blockIdx.x + gridDim.x * threadIdx.x; t < tiles; t += gridDim.x * kThreads) {
-        const int row0 = t * kTileRows, end = min(row0 + kTileRows, q.n_rows), i = first_request(q, row0);
-        int lo = end, hi = end, a = -1;
-        if (i < q.n_requests) group_rows(q.offsets, q.n_rows, i, lo, hi, g.flags);
-        if (lo < end) a = lo <= row0 && hi >= end ? request_adapter(q, i, g.flags) : kTileMixed;
-        g.tile_adapter[t] = a;
-    }
-    if (blockIdx.x == 0) {   // rows outside every request
-        const int lo = q.n_requests > 0 ? min(max(q.offsets[0], 0), q.n_rows) : q.n_rows;
-        const int hi = q.n_requests > 0 ? min(max(q.offsets[q.n_requests], lo), q.n_rows) : q.n_rows;
-        const Sink none{g, 0.f, 0.f};
-        for (long long i = threadIdx.x; i < (long long)(lo + q.n_rows - hi) * g.terms_stride; i += kThreads) {
-            const int row = (int)(i / g.terms_stride), j = (int)(i - (long long)row * g.terms_stride);
-            none.put(row < lo ? row : row - lo + hi, j, 0.f);
-        }
-    }
+    for (int t = blockIdx.x + gridDim.x * threadIdx.x; t < tiles; t += gridDim.x * kThreads) g.tiles[t] = tile_info(q, t, g.flags);
+    if (blockIdx.x == 0) zero_outside(q, threadIdx.x, kThreads, g.low, (bf16*)g.terms, g.n_terms * g.terms_stride);
     find_unit(q, blockIdx.x, where, warp_tot, g.flags);
     if (where[0] < 0) return;
     const int row0 = where[1], rows = where[2] - where[1], adapter = request_adapter(q, where[0], g.flags);
