@@ -97,6 +97,7 @@ bp_status make_layer(int dtype, int** flags, int* num_sms, const char* call) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(num_sms, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess && dtype == BP_BF16) e = tc_setup();
+    if (e == cudaSuccess && dtype == BP_BF16) e = few_setup();
     if (e == cudaSuccess) e = cudaMalloc(flags, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(*flags, 0, sizeof(int));
     return cuda_status(e, call);
@@ -309,7 +310,8 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
     cudaStream_t s = (cudaStream_t)stream;
     RowsArgs a{};
     a.groups = {d_offsets, l->E, n_rows};
-    st = cuda_status(rows_in_order(l, a.groups, d_X, n_x, d_source, s), call);
+    const bool few = l->dtype == BP_BF16 && few_ok(n_rows, l->E);
+    if (!few) st = cuda_status(rows_in_order(l, a.groups, d_X, n_x, d_source, s), call);
     if (st != BP_OK) return st;
     a.N = l->n_out;
     a.K = l->n_in;
@@ -321,7 +323,7 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
     a.squash = squash;
     a.out = d_Y;
     a.flags = l->flags;
-    return cuda_status(rows_product(a, l->dtype, false, {}, l->num_sms, s), call);
+    return cuda_status(few ? few_rows(a, s) : rows_product(a, l->dtype, false, {}, l->num_sms, s), call);
 }
 
 bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, int n_x, const int* d_source,
@@ -436,9 +438,11 @@ void bp_adapters_destroy(bp_adapters* l) {
 }
 
 static cudaError_t low_of(const bp_adapters* l, const Requests& req, int K, const void* in, const void* P, const float* scale,
-                          int scaled_low, float* low, cudaStream_t s) {
-    const LowArgs a{req, K, in, P, scale, scaled_low, low, l->terms, l->n_terms, l->stride, l->tiles, l->flags};
+                          bool forward, float* low, cudaStream_t s) {
+    const bool few = forward && few_ok(req.n_rows, 1);
+    const LowArgs a{req, K, in, P, scale, forward ? 0 : 1, low, l->terms, few ? 0 : l->n_terms, l->stride, few ? nullptr : l->tiles, l->flags};
     if (l->dtype != BP_BF16) return simt_low(a, l->dtype, s);
+    if (few) return low_product(a, s);
     return (long long)req.n_rows >= 64ll * req.n_requests && req.n_requests > 0 ? tc_low(a, l->num_sms, s) : low_product(a, s);
 }
 
@@ -470,7 +474,7 @@ bp_status bp_adapters_forward(bp_adapters* l, const void* d_W, const float* d_b,
     if (st != BP_OK || !rows) return st;
     cudaStream_t s = (cudaStream_t)stream;
     const Requests req{d_offsets, d_adapter, n_requests, n_rows, l->n, l->rank};
-    st = cuda_status(low_of(l, req, l->n_in, d_X, d_A, d_scale, 0, d_U, s), call);
+    st = cuda_status(low_of(l, req, l->n_in, d_X, d_A, d_scale, true, d_U, s), call);
     if (st != BP_OK) return st;
     RowsArgs a{};
     a.groups = {nullptr, 1, n_rows};
@@ -487,6 +491,7 @@ bp_status bp_adapters_forward(bp_adapters* l, const void* d_W, const float* d_b,
     a.P = d_B;
     a.scale = d_scale;
     a.flags = l->flags;
+    if (l->dtype == BP_BF16 && few_ok(n_rows, 1)) return cuda_status(few_rows(a, s), call);
     return cuda_status(rows_product(a, l->dtype, false, l->low_terms(), l->num_sms, s), call);
 }
 
@@ -516,7 +521,7 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
     cudaStream_t s = (cudaStream_t)stream;
     const Requests req{d_offsets, d_adapter, rows ? n_requests : 0, n_rows, l->n, l->rank};
     if (rows && (dx || ga)) {
-        st = cuda_status(low_of(l, req, l->n_out, d_D, d_B, d_scale, 1, l->low, s), call);
+        st = cuda_status(low_of(l, req, l->n_out, d_D, d_B, d_scale, false, l->low, s), call);
     }
     if (st == BP_OK && rows && dx) {
         RowsArgs a{};

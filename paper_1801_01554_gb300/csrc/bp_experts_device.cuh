@@ -88,18 +88,35 @@ __device__ __forceinline__ void find_tile(const RowGroups& q, int tile, int& g, 
     row0 = end = 0;
 }
 
+// d += a b: 16 x 16 bfloat16 (rows of k) by 16 x 8 (columns of k), float32 sums.
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+                 "{%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
 // What block t of kTileRows rows holds (see kTileRows).
+// (a converged warp asks)
 __device__ __forceinline__ int2 tile_info(const Requests& q, int t, int* flags) {
     const int row0 = t * kTileRows, end = min(row0 + kTileRows, q.n_rows), first = first_request(q, row0);
     int count = 0;
-    for (int i = first; i < q.n_requests; ++i) {
-        int lo, hi;
-        group_rows(q.offsets, q.n_rows, i, lo, hi, flags);
-        if (lo >= end) break;
-        if (hi <= lo) continue;
-        const int a = request_adapter(q, i, flags);
-        if (lo <= row0 && hi >= end) return make_int2(a, i);
-        if (a >= 0 && ++count > q.rank) return make_int2(kTileByRow, first);
+    for (int base = first; base < q.n_requests; base += 32) {
+        const int i = base + (threadIdx.x & 31);
+        int lo = q.n_rows, hi = q.n_rows, a = -1;
+        if (i < q.n_requests) {
+            group_rows(q.offsets, q.n_rows, i, lo, hi, flags);
+            a = request_adapter(q, i, flags);
+        }
+        const unsigned whole = __ballot_sync(0xffffffffu, hi > lo && lo <= row0 && hi >= end);
+        if (whole != 0) {
+            const int l = __ffs(whole) - 1;
+            return make_int2(__shfl_sync(0xffffffffu, a, l), base + l);
+        }
+        count += __popc(__ballot_sync(0xffffffffu, hi > lo && lo < end && a >= 0));
+        if (count > q.rank) return make_int2(kTileByRow, first);
+        if (__any_sync(0xffffffffu, lo >= end)) break;
     }
     return make_int2(count > 0 ? kTileMixed : -1, first);
 }

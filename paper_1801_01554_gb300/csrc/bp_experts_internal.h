@@ -60,7 +60,8 @@ struct LowArgs {
     int scaled_low;         // 0: low without the scale
     float* low;
     // bfloat16: the scaled sums as n_terms bfloat16 terms, [n_rows, n_terms, terms_stride] with zeros
-    // past the rank, and what every block of kTileRows rows holds
+    // past the rank, and what every block of kTileRows rows holds (0 and NULL: not
+    // wanted)
     void* terms;
     int n_terms, terms_stride;
     int2* tiles;
@@ -130,6 +131,13 @@ cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_s
 cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
 cudaError_t tc_low(const LowArgs& a, int num_sms, cudaStream_t s);
 cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, int num_sms, cudaStream_t s);
+
+// The forward product of a few rows in bfloat16 (bp_few.cu), rows read through an index too; with low,
+// behind low_product, which a dependent launch overlaps.
+// few_ok: 64 rows of one group, or up to 8 a group on average (of at most 512: they may all be in one).
+cudaError_t few_setup();
+bool few_ok(int n_rows, int n_groups);
+cudaError_t few_rows(const RowsArgs& a, cudaStream_t s);
 
 // Low-rank products of bfloat16 (bp_low.cu).
 cudaError_t low_product(const LowArgs& a, cudaStream_t s);

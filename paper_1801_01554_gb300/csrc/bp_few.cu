@@ -1,0 +1,208 @@
+// The forward product of a few rows with bfloat16 weights: single patterns through their experts,
+// single rows of many requests through a shared layer and their adapters.
+//
+// The time is that of reading the weights once: five patterns of two experts each of 1024-2048 read
+// 42 MB, 6.3 us at the measured copy rate.  So the weights are streamed from global memory straight
+// into the registers of mma.sync, 16 units by 32 of K a step and warp, 16 bytes a lane (a lane's
+// eight values of k stand for the four pairs that two MMAs want, the same eight in both operands); the
+// rows, which every CTA reads again, come from L2.  Eight warps share K, their sums are added in
+// shared memory in order, and eight units of a row leave as one 16-byte store.
+//
+// Behind an adapter's low-rank product the launch is a dependent one that streams the weights while
+// that product runs, and waits for it before it reads low.
+#include "bp_experts_device.cuh"
+#include "bp_tc_device.cuh"
+
+namespace bp {
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps;
+
+__device__ __forceinline__ uint4 load_once(const bf16* p) {
+    uint4 u;
+    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                 : "l"(p));
+    return u;
+}
+
+// The slot-th group that has rows, by a converged warp; false if there are not so many.
+__device__ __forceinline__ bool busy_group(const RowGroups& q, int slot, int& g, int& lo, int& hi, int* flags) {
+    const int lane = threadIdx.x & 31;
+    for (int base = 0; base < q.n_groups; base += 32) {
+        int l = 0, h = 0;
+        if (base + lane < q.n_groups) group_rows(q.offsets, q.n_rows, base + lane, l, h, flags);
+        unsigned m = __ballot_sync(0xffffffffu, h > l);
+        if (slot < __popc(m)) {
+            for (; slot > 0; --slot) m &= m - 1;
+            const int at = __ffs(m) - 1;
+            g = base + at;
+            lo = __shfl_sync(0xffffffffu, l, at);
+            hi = __shfl_sync(0xffffffffu, h, at);
+            return true;
+        }
+        slot -= __popc(m);
+    }
+    return false;
+}
+
+// MU tiles of 16 units by NT of 8 rows a pass.  LOW: one group of all rows, the adapters' part added.
+template <int MU, int NT, bool LOW>
+__global__ void __launch_bounds__(kThreads) k_few(RowsArgs a) {
+    constexpr int U = 16 * MU, R = 8 * NT;
+    extern __shared__ float red[];   // [kWarps][R][U + 4]
+    __shared__ int s_adapter[R];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gr = lane >> 2, k8 = (lane & 3) * 8;
+    int g = 0, lo = 0, hi = a.groups.n_rows;
+    if (!LOW && !busy_group(a.groups, blockIdx.y, g, lo, hi, a.flags)) return;
+    const int u0 = blockIdx.x * U, K = a.K, N = a.N;
+    const bf16* W = (const bf16*)a.W + ((size_t)g * N + u0) * K;
+    const bf16* X = (const bf16*)a.in;
+    for (int row0 = lo; row0 < hi; row0 += R) {
+        const bf16* x[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int row = row0 + 8 * n + gr;
+            x[n] = row < hi ? X + (size_t)source_row(a.source, row, a.n_in_rows, a.flags) * K : nullptr;
+        }
+        float acc[MU][NT][4] = {};
+#pragma unroll(MU * NT <= 2 ? 4 : 2)
+        for (int k0 = warp * 32; k0 < K; k0 += kWarps * 32) {
+            const int k = k0 + k8;
+            uint4 w[MU][2], v[NT];
+#pragma unroll
+            for (int m = 0; m < MU; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int u = 16 * m + 8 * h + gr;
+                    w[m][h] = u0 + u < N && k < K ? load_once(W + (size_t)u * K + k) : make_uint4(0u, 0u, 0u, 0u);
+                }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                v[n] = x[n] != nullptr && k < K ? *reinterpret_cast<const uint4*>(x[n] + k) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+            for (int m = 0; m < MU; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    mma_16816(acc[m][n], w[m][0].x, w[m][1].x, w[m][0].y, w[m][1].y, v[n].x, v[n].y);
+                    mma_16816(acc[m][n], w[m][0].z, w[m][1].z, w[m][0].w, w[m][1].w, v[n].z, v[n].w);
+                }
+        }
+        __syncthreads();   // the pass before has read red
+#pragma unroll
+        for (int m = 0; m < MU; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int u = 16 * m + gr + 8 * (i >> 1), row = 8 * n + 2 * (lane & 3) + (i & 1);
+                    red[(warp * R + row) * (U + 4) + u] = acc[m][n][i];
+                }
+        if (LOW) {
+            for (int i = threadIdx.x; i < R; i += kThreads) {
+                int ad = -1;
+                const int row = row0 + i, q = row < hi ? first_request(a.req, row) : a.req.n_requests;
+                if (q < a.req.n_requests) {
+                    int l, h;
+                    group_rows(a.req.offsets, a.req.n_rows, q, l, h, a.flags);
+                    if (row >= l && row < h) ad = request_adapter(a.req, q, a.flags);
+                }
+                s_adapter[i] = ad;
+            }
+            if (row0 == lo) pdl_wait();
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < R * U / 8; i += kThreads) {   // eight units of a row
+            const int row = row0 + i / (U / 8), u = i % (U / 8) * 8, n = u0 + u;
+            if (row >= hi || n >= N) continue;   // N is a multiple of 8
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float4* p = reinterpret_cast<const float4*>(&red[(w * R + row - row0) * (U + 4) + u]);
+                const float4 p0 = p[0], p1 = p[1];
+                v[0] += p0.x, v[1] += p0.y, v[2] += p0.z, v[3] += p0.w;
+                v[4] += p1.x, v[5] += p1.y, v[6] += p1.z, v[7] += p1.w;
+            }
+            if (LOW) {
+                const int ad = s_adapter[row - row0];
+                if (ad >= 0) {
+                    const int r = a.req.rank;
+                    const float c = a.scale != nullptr ? a.scale[ad] : 1.f;
+                    const float* low = a.low + (size_t)row * r;
+                    const bf16* P = (const bf16*)a.P + (size_t)ad * r * N + n;
+                    float s[8] = {};
+#pragma unroll 8
+                    for (int j = 0; j < r; ++j) {
+                        const float t = low[j];
+                        const uint4 p = *reinterpret_cast<const uint4*>(P + (size_t)j * N);
+                        const uint32_t pw[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            s[2 * q] = fmaf(t, __uint_as_float(pw[q] << 16), s[2 * q]);
+                            s[2 * q + 1] = fmaf(t, __uint_as_float(pw[q] & 0xffff0000u), s[2 * q + 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] = fmaf(c, s[q], v[q]);
+                }
+            }
+            if (a.bias != nullptr) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] += a.bias[(size_t)g * N + n + q];
+            }
+            if (a.squash) {
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[q] = sigmoid_fast(v[q]);
+            }
+            __align__(16) __nv_bfloat162 o[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) o[q] = __floats2bfloat162_rn(v[2 * q], v[2 * q + 1]);
+            *reinterpret_cast<uint4*>((bf16*)a.out + (size_t)row * N + n) = *reinterpret_cast<const uint4*>(o);
+        }
+    }
+}
+
+template <int MU, int NT, bool LOW>
+cudaError_t launch(const RowsArgs& a, int slots, cudaStream_t s) {
+    constexpr int bytes = kWarps * 8 * NT * (16 * MU + 4) * 4;
+    const dim3 grid((a.N + 16 * MU - 1) / (16 * MU), slots);
+    static_assert(LOW || bytes <= 48 * 1024, "room without a set-up");
+    if (LOW) return launch_pdl(k_few<MU, NT, LOW>, grid.x, 1, kThreads, bytes, s, a);
+    k_few<MU, NT, LOW><<<grid, kThreads, bytes, s>>>(a);
+    return cudaGetLastError();
+}
+
+template <int MU, int NT>
+cudaError_t setup_low() {
+    return cudaFuncSetAttribute(k_few<MU, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                kWarps * 8 * NT * (16 * MU + 4) * 4);
+}
+
+}  // namespace
+
+cudaError_t few_setup() {
+    cudaError_t e = setup_low<2, 4>();
+    return e == cudaSuccess ? setup_low<2, 8>() : e;
+}
+
+bool few_ok(int n_rows, int n_groups) {
+    if (n_groups == 1) return n_rows <= 64;
+    const int busy = n_groups < n_rows ? n_groups : n_rows;
+    return n_rows <= 8 * busy && n_rows <= 512;
+}
+
+cudaError_t few_rows(const RowsArgs& a, cudaStream_t s) {
+    const int n = a.groups.n_rows;
+    if (a.low != nullptr) {
+        if (n <= 8) return launch<1, 1, true>(a, 1, s);
+        if (n <= 16) return launch<1, 2, true>(a, 1, s);
+        if (n <= 32) return launch<2, 4, true>(a, 1, s);
+        return launch<2, 8, true>(a, 1, s);
+    }
+    const int slots = a.groups.n_groups < n ? a.groups.n_groups : n;
+    return n <= 8 ? launch<1, 1, false>(a, slots, s) : launch<1, 2, false>(a, slots, s);
+}
+
+}  // namespace bp

@@ -421,9 +421,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
     if (FORM == UP && warp >= 2) {
-        for (int t = blockIdx.x + gridDim.x * (threadIdx.x - 64); t < (g.req.n_rows + kTileRows - 1) / kTileRows;
-             t += gridDim.x * kEpiThreads)
-            g.tiles[t] = tile_info(g.req, t, g.flags);
+        for (int t = blockIdx.x + gridDim.x * (warp - 2); t < (g.req.n_rows + kTileRows - 1) / kTileRows;
+             t += gridDim.x * kEpiWarps) {
+            const int2 info = tile_info(g.req, t, g.flags);
+            if (lane == 0) g.tiles[t] = info;
+        }
         if (blockIdx.x == 0) zero_outside(g.req, threadIdx.x - 64, kEpiThreads, g.low_out, g.terms, g.n_terms * g.stride);
         __syncwarp();
     }

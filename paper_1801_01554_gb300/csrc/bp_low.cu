@@ -10,21 +10,12 @@
 // so that the sum over k is merely taken in another order.  Warps share K and, from 32 on, the rank;
 // their sums are added in shared memory in a fixed order.
 #include "bp_experts_device.cuh"
+#include "bp_tc_device.cuh"
 
 namespace bp {
 namespace {
 
-using bf16 = __nv_bfloat16;
-
 constexpr int kRows = 64, kThreads = 256, kWarps = kThreads / 32;
-
-__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                          uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-                 "{%0, %1, %2, %3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
 
 // The unit-th run of up to kRows rows of one request; the whole block calls it.  Request, first row
 // and end, or request -1 past the last unit.
@@ -89,7 +80,7 @@ template <int MT, int NT>
 __device__ __forceinline__ void accumulate(float (&acc)[MT][NT][4], const bf16* x, int rows, const bf16* P, int ranks, int K,
                                            int first, int step) {
     const int lane = threadIdx.x & 31, gr = lane >> 2, k8 = (lane & 3) * 8;
-#pragma unroll 2
+#pragma unroll(MT == 1 ? 16 / NT : 2)
     for (int k0 = first * 32; k0 < K; k0 += step * 32) {
         const int k = k0 + k8;
         uint4 a[MT][2], b[NT];
@@ -148,7 +139,7 @@ __device__ __forceinline__ void low_rows(const LowArgs& g, const Sink& sink, int
                 if (row < rows) sink.put(row0 + row, j, acc[m][n][i]);
             }
     // ranks that no warp's tiles reach are only the terms' zeros
-    for (int i = lane + 32 * nw; i < rows * g.terms_stride; i += 32 * rank_warps) {
+    for (int i = lane + 32 * nw; g.n_terms > 0 && i < rows * g.terms_stride; i += 32 * rank_warps) {
         const int row = i / g.terms_stride, j = i - row * g.terms_stride;
         if (j >= rank_warps * NT * 8) sink.put(row0 + row, j, 0.f);
     }
@@ -161,7 +152,12 @@ __global__ void __launch_bounds__(kThreads) k_low(LowArgs g, int rank_warps, int
     __shared__ int warp_tot[kWarps];
     __shared__ float red[kWarps / 2 * (kRows / 16) * NT * 128];
     const Requests& q = g.req;
-    for (int t = blockIdx.x + gridDim.x * threadIdx.x; t < tiles; t += gridDim.x * kThreads) g.tiles[t] = tile_info(q, t, g.flags);
+    pdl_launch();
+    if (g.tiles != nullptr)
+        for (int t = blockIdx.x + gridDim.x * (threadIdx.x >> 5); t < tiles; t += gridDim.x * kWarps) {
+            const int2 info = tile_info(q, t, g.flags);
+            if ((threadIdx.x & 31) == 0) g.tiles[t] = info;
+        }
     if (blockIdx.x == 0) zero_outside(q, threadIdx.x, kThreads, g.low, (bf16*)g.terms, g.n_terms * g.terms_stride);
     find_unit(q, blockIdx.x, where, warp_tot, g.flags);
     if (where[0] < 0) return;
