@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "bp_experts_internal.h"
 
 namespace bp {
@@ -95,6 +97,119 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a
                  "{%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// acc += A B over one warp's steps of 32 of K (first, first + step, ..), A of NA tiles of 16 rows, B of
+// NB tiles of 8 columns, both with k contiguous; a and b point at this lane's rows (lane / 4, and 8
+// further for a[.][1]) and its eight values of k, 8 (lane % 4), or are NULL for rows whose sums are not
+// kept; `any` is a row that they may read instead.  The eight values stand for the four pairs of k that
+// two MMAs want, the same eight in both operands, so that the sum over k is only taken in another order.
+template <int NA, int NB>
+__device__ __forceinline__ void step_products(float (&acc)[NA][NB][4], const uint4 (&x)[NA][2], const uint4 (&y)[NB]) {
+#pragma unroll
+    for (int m = 0; m < NA; ++m)
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+            mma_16816(acc[m][c], x[m][0].x, x[m][1].x, x[m][0].y, x[m][1].y, y[c].x, y[c].y);
+            mma_16816(acc[m][c], x[m][0].z, x[m][1].z, x[m][0].w, x[m][1].w, y[c].z, y[c].w);
+        }
+}
+
+// Loads straight into registers, B steps under way.  No load hangs on a condition but in the last,
+// short step.
+template <int NA, int NB, int B>
+__device__ __forceinline__ void direct_products(float (&acc)[NA][NB][4], const __nv_bfloat16* (&a)[NA][2],
+                                                const __nv_bfloat16* (&b)[NB], const __nv_bfloat16* any, int K, int first,
+                                                int step) {
+    const int k8 = (threadIdx.x & 3) * 8, whole = K / 32;
+#pragma unroll
+    for (int m = 0; m < NA; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) a[m][h] = a[m][h] != nullptr ? a[m][h] : any + k8;
+#pragma unroll
+    for (int c = 0; c < NB; ++c) b[c] = b[c] != nullptr ? b[c] : any + k8;
+    int k = first;
+    auto load = [](const __nv_bfloat16* p) {   // volatile: ptxas may not sink it to its use
+        uint4 u;
+        asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+        return u;
+    };
+    auto batch = [&](auto count) {
+        constexpr int n = decltype(count)::value;
+        uint4 x[n][NA][2], y[n][NB];
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const int at = (k + i * step) * 32;
+#pragma unroll
+            for (int m = 0; m < NA; ++m) x[i][m][0] = load(a[m][0] + at), x[i][m][1] = load(a[m][1] + at);
+#pragma unroll
+            for (int c = 0; c < NB; ++c) y[i][c] = load(b[c] + at);
+        }
+#pragma unroll
+        for (int i = 0; i < n; ++i) step_products<NA, NB>(acc, x[i], y[i]);
+        k += n * step;
+    };
+    while (k + (B - 1) * step < whole) batch(std::integral_constant<int, B>{});
+    while (k < whole) batch(std::integral_constant<int, 1>{});
+    if (k == whole && k * 32 < K) {   // this warp has the rest of K
+        const bool in = k * 32 + k8 < K;
+        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+        uint4 x[NA][2], y[NB];
+#pragma unroll
+        for (int m = 0; m < NA; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x[m][h] = in ? *reinterpret_cast<const uint4*>(a[m][h] + k * 32) : zero;
+#pragma unroll
+        for (int c = 0; c < NB; ++c) y[c] = in ? *reinterpret_cast<const uint4*>(b[c] + k * 32) : zero;
+        step_products<NA, NB>(acc, x, y);
+    }
+}
+
+// Loads through S steps of shared memory by cp.async, each lane reading back what it copied itself: no
+// barriers, and more under way than registers would hold where a step is many pieces (61 rows of
+// 4096-4096: 14 us against 17; of few pieces the copies cost more than they hide, 9.5 against 6).
+// `ring`: this warp's ring_bytes<NA, NB, S>() of shared memory.
+template <int NA, int NB, int S>
+constexpr int ring_bytes() { return S * (2 * NA + NB) * 512; }
+template <int NA, int NB, int S>
+__device__ __forceinline__ void ring_products(float (&acc)[NA][NB][4], const __nv_bfloat16* (&a)[NA][2],
+                                              const __nv_bfloat16* (&b)[NB], const __nv_bfloat16* any, int K, int first,
+                                              int step, void* ring) {
+    constexpr int P = 2 * NA + NB;
+    const int lane = threadIdx.x & 31, k8 = (lane & 3) * 8;
+    uint4* mine = reinterpret_cast<uint4*>(ring) + lane;
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine);
+    const int steps = first * 32 < K ? ((K + 31) / 32 - first + step - 1) / step : 0;
+    auto copy = [&](int i) {
+        const int k = (first + i * step) * 32;
+        const bool in = i < steps && k + k8 < K;
+        const uint32_t at = to + (i % S) * P * 512;
+        auto piece = [&](int p, const __nv_bfloat16* src) {   // zeros where nothing is to be read
+            const bool read = in && src != nullptr;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at + p * 512), "l"(read ? src + k : any),
+                         "r"(read ? 16 : 0)
+                         : "memory");
+        };
+#pragma unroll
+        for (int m = 0; m < NA; ++m) piece(2 * m, a[m][0]), piece(2 * m + 1, a[m][1]);
+#pragma unroll
+        for (int c = 0; c < NB; ++c) piece(2 * NA + c, b[c]);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) copy(i);
+    for (int i = 0; i < steps; ++i) {
+        copy(i + S - 1);
+        asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+        const uint4* from = mine + (i % S) * P * 32;
+        uint4 x[NA][2], y[NB];
+#pragma unroll
+        for (int m = 0; m < NA; ++m) x[m][0] = from[2 * m * 32], x[m][1] = from[(2 * m + 1) * 32];
+#pragma unroll
+        for (int c = 0; c < NB; ++c) y[c] = from[(2 * NA + c) * 32];
+        step_products<NA, NB>(acc, x, y);
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 // What block t of kTileRows rows holds (see kTileRows).

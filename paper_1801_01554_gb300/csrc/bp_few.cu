@@ -2,10 +2,9 @@
 // single rows of many requests through a shared layer and their adapters.
 //
 // The time is that of reading the weights once: five patterns of two experts each of 1024-2048 read
-// 42 MB, 6.3 us at the measured copy rate.  So the weights are streamed from global memory straight
-// into the registers of mma.sync, 16 units by 32 of K a step and warp, 16 bytes a lane (a lane's
-// eight values of k stand for the four pairs that two MMAs want, the same eight in both operands); the
-// rows, which every CTA reads again, come from L2.  Eight warps share K, their sums are added in
+// 42 MB, 6.3 us at the measured copy rate.  So the weights are streamed into mma.sync, 16 units by
+// 32 of K a step and warp, 16 bytes a lane (direct_products); the rows, which every CTA reads again,
+// come from L2.  Eight warps share K, their sums are added in
 // shared memory in order, and eight units of a row leave as one 16-byte store.
 //
 // Behind an adapter's low-rank product the launch is a dependent one that streams the weights while
@@ -16,14 +15,18 @@
 namespace bp {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps;
+constexpr int kWarps = 8;
+// Beside the warps that stream, one that looks up the rows' adapters.
+constexpr int few_threads(bool low) { return 32 * (kWarps + (low ? 1 : 0)); }
 
-__device__ __forceinline__ uint4 load_once(const bf16* p) {
-    uint4 u;
-    asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
-                 : "l"(p));
-    return u;
+// Steps under way where they go through shared memory.
+constexpr int kRing = 4;
+template <int MU, int NT>
+constexpr bool kThroughRing = MU * NT > 2;
+template <int MU, int NT>
+constexpr int few_smem() {
+    constexpr int ring = kThroughRing<MU, NT> ? kWarps * ring_bytes<MU, NT, kRing>() : 0, sums = kWarps * 8 * NT * (16 * MU + 4) * 4;
+    return ring > sums ? ring : sums;
 }
 
 // The slot-th group that has rows, by a converged warp; false if there are not so many.
@@ -48,9 +51,10 @@ __device__ __forceinline__ bool busy_group(const RowGroups& q, int slot, int& g,
 
 // MU tiles of 16 units by NT of 8 rows a pass.  LOW: one group of all rows, the adapters' part added.
 template <int MU, int NT, bool LOW>
-__global__ void __launch_bounds__(kThreads) k_few(RowsArgs a) {
-    constexpr int U = 16 * MU, R = 8 * NT;
-    extern __shared__ float red[];   // [kWarps][R][U + 4]
+__global__ void __launch_bounds__(few_threads(LOW)) k_few(RowsArgs a) {
+    constexpr int U = 16 * MU, R = 8 * NT, kThreads = few_threads(LOW);
+    extern __shared__ __align__(16) uint8_t smem[];   // the warps' rings; then their sums [kWarps][R][U + 4]
+    float* red = reinterpret_cast<float*>(smem);
     __shared__ int s_adapter[R];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gr = lane >> 2, k8 = (lane & 3) * 8;
     int g = 0, lo = 0, hi = a.groups.n_rows;
@@ -59,47 +63,28 @@ __global__ void __launch_bounds__(kThreads) k_few(RowsArgs a) {
     const bf16* W = (const bf16*)a.W + ((size_t)g * N + u0) * K;
     const bf16* X = (const bf16*)a.in;
     for (int row0 = lo; row0 < hi; row0 += R) {
-        const bf16* x[NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int row = row0 + 8 * n + gr;
-            x[n] = row < hi ? X + (size_t)source_row(a.source, row, a.n_in_rows, a.flags) * K : nullptr;
-        }
+        __syncthreads();   // the pass before has read red
         float acc[MU][NT][4] = {};
-#pragma unroll(MU * NT <= 2 ? 4 : 2)
-        for (int k0 = warp * 32; k0 < K; k0 += kWarps * 32) {
-            const int k = k0 + k8;
-            uint4 w[MU][2], v[NT];
+        if (!LOW || warp < kWarps) {
+            const bf16 *x[NT], *w[MU][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int row = row0 + 8 * n + gr;
+                x[n] = row < hi ? X + (size_t)source_row(a.source, row, a.n_in_rows, a.flags) * K + k8 : nullptr;
+            }
 #pragma unroll
             for (int m = 0; m < MU; ++m)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int u = 16 * m + 8 * h + gr;
-                    w[m][h] = u0 + u < N && k < K ? load_once(W + (size_t)u * K + k) : make_uint4(0u, 0u, 0u, 0u);
+                    w[m][h] = u0 + u < N ? W + (size_t)u * K + k8 : nullptr;
                 }
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                v[n] = x[n] != nullptr && k < K ? *reinterpret_cast<const uint4*>(x[n] + k) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int m = 0; m < MU; ++m)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    mma_16816(acc[m][n], w[m][0].x, w[m][1].x, w[m][0].y, w[m][1].y, v[n].x, v[n].y);
-                    mma_16816(acc[m][n], w[m][0].z, w[m][1].z, w[m][0].w, w[m][1].w, v[n].z, v[n].w);
-                }
-        }
-        __syncthreads();   // the pass before has read red
-#pragma unroll
-        for (int m = 0; m < MU; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int u = 16 * m + gr + 8 * (i >> 1), row = 8 * n + 2 * (lane & 3) + (i & 1);
-                    red[(warp * R + row) * (U + 4) + u] = acc[m][n][i];
-                }
-        if (LOW) {
-            for (int i = threadIdx.x; i < R; i += kThreads) {
+            if constexpr (kThroughRing<MU, NT>)
+                ring_products<MU, NT, kRing>(acc, w, x, W, K, warp, kWarps, smem + warp * ring_bytes<MU, NT, kRing>());
+            else
+                direct_products<MU, NT, 8>(acc, w, x, W, K, warp, kWarps);
+        } else {
+            for (int i = lane; i < R; i += 32) {
                 int ad = -1;
                 const int row = row0 + i, q = row < hi ? first_request(a.req, row) : a.req.n_requests;
                 if (q < a.req.n_requests) {
@@ -109,7 +94,18 @@ __global__ void __launch_bounds__(kThreads) k_few(RowsArgs a) {
                 }
                 s_adapter[i] = ad;
             }
-            if (row0 == lo) pdl_wait();
+        }
+        __syncthreads();   // every warp is done with its ring
+        if (!LOW || warp < kWarps) {
+#pragma unroll
+            for (int m = 0; m < MU; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int u = 16 * m + gr + 8 * (i >> 1), row = 8 * n + 2 * (lane & 3) + (i & 1);
+                        red[(warp * R + row) * (U + 4) + u] = acc[m][n][i];
+                    }
         }
         __syncthreads();
         for (int i = threadIdx.x; i < R * U / 8; i += kThreads) {   // eight units of a row
@@ -126,22 +122,36 @@ __global__ void __launch_bounds__(kThreads) k_few(RowsArgs a) {
                 v[4] += p1.x, v[5] += p1.y, v[6] += p1.z, v[7] += p1.w;
             }
             if (LOW) {
-                const int ad = s_adapter[row - row0];
+                const int ad = s_adapter[row - row0], r = a.req.rank;
+                const bf16* P = (const bf16*)a.P + (size_t)max(ad, 0) * r * N + n;
+                constexpr int B = 8;   // the first of the adapter's rows arrive while low is waited for
+                uint4 p[B];
+#pragma unroll
+                for (int j = 0; j < B; ++j)
+                    p[j] = ad >= 0 && j < r ? *reinterpret_cast<const uint4*>(P + (size_t)j * N) : make_uint4(0u, 0u, 0u, 0u);
+                pdl_wait();
                 if (ad >= 0) {
-                    const int r = a.req.rank;
                     const float c = a.scale != nullptr ? a.scale[ad] : 1.f;
                     const float* low = a.low + (size_t)row * r;
-                    const bf16* P = (const bf16*)a.P + (size_t)ad * r * N + n;
                     float s[8] = {};
-#pragma unroll 8
-                    for (int j = 0; j < r; ++j) {
-                        const float t = low[j];
-                        const uint4 p = *reinterpret_cast<const uint4*>(P + (size_t)j * N);
-                        const uint32_t pw[4] = {p.x, p.y, p.z, p.w};
+                    for (int j0 = 0; j0 < r; j0 += B) {
+                        uint4 now[B];
+                        float t[B];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            s[2 * q] = fmaf(t, __uint_as_float(pw[q] << 16), s[2 * q]);
-                            s[2 * q + 1] = fmaf(t, __uint_as_float(pw[q] & 0xffff0000u), s[2 * q + 1]);
+                        for (int j = 0; j < B; ++j) {
+                            now[j] = p[j];
+                            t[j] = j0 + j < r ? low[j0 + j] : 0.f;
+                            if (j0 + B + j < r) p[j] = *reinterpret_cast<const uint4*>(P + (size_t)(j0 + B + j) * N);
+                        }
+#pragma unroll
+                        for (int j = 0; j < B; ++j) {
+                            if (j0 + j >= r) break;
+                            const uint32_t pw[4] = {now[j].x, now[j].y, now[j].z, now[j].w};
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                s[2 * q] = fmaf(t[j], __uint_as_float(pw[q] << 16), s[2 * q]);
+                                s[2 * q + 1] = fmaf(t[j], __uint_as_float(pw[q] & 0xffff0000u), s[2 * q + 1]);
+                            }
                         }
                     }
 #pragma unroll
@@ -166,25 +176,28 @@ __global__ void __launch_bounds__(kThreads) k_few(RowsArgs a) {
 
 template <int MU, int NT, bool LOW>
 cudaError_t launch(const RowsArgs& a, int slots, cudaStream_t s) {
-    constexpr int bytes = kWarps * 8 * NT * (16 * MU + 4) * 4;
     const dim3 grid((a.N + 16 * MU - 1) / (16 * MU), slots);
-    static_assert(LOW || bytes <= 48 * 1024, "room without a set-up");
-    if (LOW) return launch_pdl(k_few<MU, NT, LOW>, grid.x, 1, kThreads, bytes, s, a);
-    k_few<MU, NT, LOW><<<grid, kThreads, bytes, s>>>(a);
+    constexpr int threads = few_threads(LOW), smem = few_smem<MU, NT>();
+    if (LOW) return launch_pdl(k_few<MU, NT, LOW>, grid.x, 1, threads, smem, s, a);
+    k_few<MU, NT, LOW><<<grid, threads, smem, s>>>(a);
     return cudaGetLastError();
 }
 
-template <int MU, int NT>
-cudaError_t setup_low() {
-    return cudaFuncSetAttribute(k_few<MU, NT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                kWarps * 8 * NT * (16 * MU + 4) * 4);
+template <int MU, int NT, bool LOW>
+cudaError_t setup() {
+    return cudaFuncSetAttribute(k_few<MU, NT, LOW>, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem<MU, NT>());
 }
 
 }  // namespace
 
 cudaError_t few_setup() {
-    cudaError_t e = setup_low<2, 4>();
-    return e == cudaSuccess ? setup_low<2, 8>() : e;
+    cudaError_t e;
+    if ((e = setup<1, 1, false>()) != cudaSuccess) return e;
+    if ((e = setup<1, 2, false>()) != cudaSuccess) return e;
+    if ((e = setup<1, 1, true>()) != cudaSuccess) return e;
+    if ((e = setup<1, 2, true>()) != cudaSuccess) return e;
+    if ((e = setup<2, 4, true>()) != cudaSuccess) return e;
+    return setup<2, 8, true>();
 }
 
 bool few_ok(int n_rows, int n_groups) {

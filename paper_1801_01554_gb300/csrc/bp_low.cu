@@ -5,10 +5,8 @@
 // their adapters): 16,384 rows of 4,096 are 134 MB and 20 us at the measured copy rate, the
 // 2 * 64 * 16,384 * 4,096 flops of rank 64 a fraction of that on mma.sync, whose 16-row tiles fit
 // short requests where a tcgen05 tile would hold 128 rows.  A CTA takes up to 64 rows of one
-// request and reads x and P_a straight into the operands' registers, 16 bytes a lane: a lane's
-// eight values of k stand for the four pairs that two MMAs want, the same eight in both operands,
-// so that the sum over k is merely taken in another order.  Warps share K and, from 32 on, the rank;
-// their sums are added in shared memory in a fixed order.
+// request.  Warps share K and, from 32 on, the rank; their sums are added in shared memory in a
+// fixed order.
 #include "bp_experts_device.cuh"
 #include "bp_tc_device.cuh"
 
@@ -75,46 +73,23 @@ struct Sink {
     }
 };
 
-// MT tiles of 16 rows by NT of 8 of the rank, over this warp's steps of 32 of K.
-template <int MT, int NT>
-__device__ __forceinline__ void accumulate(float (&acc)[MT][NT][4], const bf16* x, int rows, const bf16* P, int ranks, int K,
-                                           int first, int step) {
-    const int lane = threadIdx.x & 31, gr = lane >> 2, k8 = (lane & 3) * 8;
-#pragma unroll(MT == 1 ? 16 / NT : 2)
-    for (int k0 = first * 32; k0 < K; k0 += step * 32) {
-        const int k = k0 + k8;
-        uint4 a[MT][2], b[NT];
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = 16 * m + 8 * h + gr;
-                a[m][h] = row < rows && k < K ? *reinterpret_cast<const uint4*>(x + (size_t)row * K + k) : make_uint4(0u, 0u, 0u, 0u);
-            }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int j = 8 * n + gr;
-            b[n] = j < ranks && k < K ? *reinterpret_cast<const uint4*>(P + (size_t)j * K + k) : make_uint4(0u, 0u, 0u, 0u);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                mma_16816(acc[m][n], a[m][0].x, a[m][1].x, a[m][0].y, a[m][1].y, b[n].x, b[n].y);
-                mma_16816(acc[m][n], a[m][0].z, a[m][1].z, a[m][0].w, a[m][1].w, b[n].z, b[n].w);
-            }
-    }
-}
-
 template <int MT, int NT>
 __device__ __forceinline__ void low_rows(const LowArgs& g, const Sink& sink, int row0, int rows, int adapter, int rank_warps,
                                          float* red) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = g.req.rank;
     const int kw = warp / rank_warps, nw = warp - kw * rank_warps, k_warps = kWarps / rank_warps;   // this warp's share
     const int j0 = nw * NT * 8;
+    const int gr = lane >> 2, k8 = (lane & 3) * 8;
+    const bf16 *in = (const bf16*)g.in + (size_t)row0 * g.K, *P = (const bf16*)g.P + (size_t)adapter * r * g.K;
+    const bf16 *x[MT][2], *p[NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[m][h] = 16 * m + 8 * h + gr < rows ? in + (size_t)(16 * m + 8 * h + gr) * g.K + k8 : nullptr;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) p[n] = j0 + 8 * n + gr < r ? P + (size_t)(j0 + 8 * n + gr) * g.K + k8 : nullptr;
     float acc[MT][NT][4] = {};
-    accumulate<MT, NT>(acc, (const bf16*)g.in + (size_t)row0 * g.K, rows, (const bf16*)g.P + ((size_t)adapter * r + j0) * g.K, r - j0,
-                       g.K, kw, k_warps);
+    direct_products<MT, NT, (MT == 1 ? 4 : 2)>(acc, x, p, in, g.K, kw, k_warps);
     for (int s = k_warps / 2; s >= 1; s >>= 1) {
         __syncthreads();
         float* at = red + (size_t)((kw % s) * rank_warps + nw) * MT * NT * 128 + lane;
@@ -147,7 +122,7 @@ __device__ __forceinline__ void low_rows(const LowArgs& g, const Sink& sink, int
 
 // NT: eights of the rank of a warp.
 template <int NT>
-__global__ void __launch_bounds__(kThreads) k_low(LowArgs g, int rank_warps, int tiles) {
+__global__ void __launch_bounds__(kThreads, 1) k_low(LowArgs g, int rank_warps, int tiles) {
     __shared__ int where[3];
     __shared__ int warp_tot[kWarps];
     __shared__ float red[kWarps / 2 * (kRows / 16) * NT * 128];
