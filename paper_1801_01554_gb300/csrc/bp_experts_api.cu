@@ -20,6 +20,8 @@ struct bp_experts {
     int E = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, num_sms = 0;
     int* flags = nullptr;
     void* rows = nullptr;   // bfloat16: [cap, n_in] inputs in the rows' order
+    float* sums = nullptr;  // bias changes of runs of rows
+    unsigned* arrived = nullptr;
 };
 
 struct bp_adapters {
@@ -259,6 +261,11 @@ bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int m
     l->cap = max_rows;
     st = make_layer(dtype, &l->flags, &l->num_sms, call);
     if (st == BP_OK && dtype == BP_BF16) st = cuda_status(cudaMalloc(&l->rows, (size_t)max_rows * n_in * 2), call);
+    // fewer rows make no more runs
+    const size_t planes = sums_runs(max_rows, n_experts, n_out, dtype, l->num_sms), cells = (size_t)n_experts * n_out;
+    if (st == BP_OK) st = cuda_status(cudaMalloc(&l->sums, planes * cells * sizeof(float)), call);
+    if (st == BP_OK) st = cuda_status(cudaMalloc(&l->arrived, cells * sizeof(unsigned)), call);
+    if (st == BP_OK) st = cuda_status(cudaMemset(l->arrived, 0, cells * sizeof(unsigned)), call);
     if (st != BP_OK) {
         bp_experts_destroy(l);
         return st;
@@ -272,6 +279,8 @@ void bp_experts_destroy(bp_experts* l) {
     cudaDeviceSynchronize();
     cudaFree(l->flags);
     cudaFree(l->rows);
+    cudaFree(l->sums);
+    cudaFree(l->arrived);
     delete l;
 }
 
@@ -287,7 +296,7 @@ static cudaError_t rows_in_order(bp_experts* l, const RowGroups& groups, const v
 }
 
 static cudaError_t rows_product(const RowsArgs& a, int dtype, bool back, const LowTerms& low, int num_sms, cudaStream_t s) {
-    return dtype == BP_BF16 ? tc_rows(a, back, low, num_sms, s) : simt_rows(a, dtype, back, s);
+    return dtype == BP_BF16 ? tc_rows(a, back, low, num_sms, s) : simt_rows(a, back, num_sms, s);
 }
 
 bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, const void* d_X, int n_x,
@@ -370,11 +379,11 @@ bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, i
     }
     if (st == BP_OK && d_GW != nullptr) {
         const ChangeArgs a{groups, l->n_out, l->n_in, d_D, d_X, d_source, n_x, d_GW, accumulate, l->flags};
-        st = cuda_status(l->dtype == BP_BF16 ? tc_change(a, l->num_sms, s) : simt_change(a, l->dtype, s), call);
+        st = cuda_status(l->dtype == BP_BF16 ? tc_change(a, l->num_sms, s) : simt_change(a, l->num_sms, s), call);
     }
     if (st == BP_OK && d_Gb != nullptr) {
-        const SumsArgs a{groups, l->n_out, d_D, d_Gb, accumulate, l->flags};
-        st = cuda_status(simt_sums(a, l->dtype, s), call);
+        const SumsArgs a{groups, l->n_out, d_D, d_Gb, accumulate, l->sums, l->arrived, l->flags};
+        st = cuda_status(group_sums(a, l->dtype, l->num_sms, s), call);
     }
     return st;
 }
@@ -441,7 +450,7 @@ static cudaError_t low_of(const bp_adapters* l, const Requests& req, int K, cons
                           bool forward, float* low, cudaStream_t s) {
     const bool few = forward && few_ok(req.n_rows, 1);
     const LowArgs a{req, K, in, P, scale, forward ? 0 : 1, low, l->terms, few ? 0 : l->n_terms, l->stride, few ? nullptr : l->tiles, l->flags};
-    if (l->dtype != BP_BF16) return simt_low(a, l->dtype, s);
+    if (l->dtype != BP_BF16) return simt_low(a, s);
     if (few) return low_product(a, s);
     return (long long)req.n_rows >= 64ll * req.n_requests && req.n_requests > 0 ? tc_low(a, l->num_sms, s) : low_product(a, s);
 }
@@ -544,7 +553,7 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
     const bool tc = l->dtype == BP_BF16;
     if (st == BP_OK && ga) {
         const LowChangeArgs a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->flags};
-        st = cuda_status(tc ? tc_low_change(a, l->low_terms(), l->num_sms, s) : simt_low_change(a, l->dtype, s), call);
+        st = cuda_status(tc ? tc_low_change(a, l->low_terms(), l->num_sms, s) : simt_low_change(a, s), call);
     }
     if (st == BP_OK && gb) {
         const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->flags};
@@ -552,7 +561,7 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
         u.terms = l->u_terms;
         if (tc && some) st = cuda_status(low_terms(d_U, n_rows, l->rank, l->u_terms, u.stride, u.n_terms, l->num_sms, s), call);
         if (st == BP_OK)
-            st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, l->dtype, s), call);
+            st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, s), call);
     }
     return st;
 }

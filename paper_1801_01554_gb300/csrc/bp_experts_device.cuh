@@ -236,7 +236,8 @@ __device__ __forceinline__ int2 tile_info(const Requests& q, int t, int* flags) 
     return make_int2(count > 0 ? kTileMixed : -1, first);
 }
 
-// Rows outside every request: zeros in low [n_rows, rank] and in the terms [n_rows, pitch].
+// Rows outside every request: zeros in low [n_rows, rank] and in the terms [n_rows, pitch], if any
+// (pitch at least the rank).
 __device__ __forceinline__ void zero_outside(const Requests& q, int thread, int threads, float* low, __nv_bfloat16* terms,
                                              int pitch) {
     const int lo = q.n_requests > 0 ? min(max(q.offsets[0], 0), q.n_rows) : q.n_rows;
@@ -244,7 +245,7 @@ __device__ __forceinline__ void zero_outside(const Requests& q, int thread, int 
     for (long long i = thread; i < (long long)(lo + q.n_rows - hi) * pitch; i += threads) {
         const long long k = i / pitch, row = k < lo ? k : k - lo + hi;
         const int j = (int)(i - k * pitch);
-        terms[row * pitch + j] = __float2bfloat16_rn(0.f);
+        if (terms != nullptr) terms[row * pitch + j] = __float2bfloat16_rn(0.f);
         if (j < q.rank) low[row * q.rank + j] = 0.f;
     }
 }

@@ -94,22 +94,28 @@ struct LowChangeArgs {
     int* flags;
 };
 
-// Column sums of a group's rows: S_g[n] (+)= sum over the group's rows of d[r, n].
+// Column sums of a group's rows: S_g[n] (+)= sum over the group's rows of d[r, n].  scratch: a plane of
+// [groups, N] for each run of rows (sums_runs); arrived: a zero for every block of columns of a group,
+// left zero.
 struct SumsArgs {
     RowGroups groups;
     int N;
     const void* d;
     float* S;
     int accumulate;
+    float* scratch;
+    unsigned* arrived;
     int* flags;
 };
+constexpr int kMaxSumRuns = 16;
+int sums_runs(int n_rows, int n_groups, int N, int dtype, int num_sms);
+cudaError_t group_sums(const SumsArgs& a, int dtype, int num_sms, cudaStream_t s);   // bp_sums.cu
 
-// float32 FMA kernels, for both dtypes and every size (bp_grouped_simt.cu).
-cudaError_t simt_rows(const RowsArgs& a, int dtype, bool back, cudaStream_t s);
-cudaError_t simt_low(const LowArgs& a, int dtype, cudaStream_t s);
-cudaError_t simt_change(const ChangeArgs& a, int dtype, cudaStream_t s);
-cudaError_t simt_low_change(const LowChangeArgs& a, int dtype, cudaStream_t s);
-cudaError_t simt_sums(const SumsArgs& a, int dtype, cudaStream_t s);
+// float32 FMA kernels (bp_grouped_simt.cu).
+cudaError_t simt_rows(const RowsArgs& a, bool back, int num_sms, cudaStream_t s);
+cudaError_t simt_low(const LowArgs& a, cudaStream_t s);
+cudaError_t simt_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
+cudaError_t simt_low_change(const LowChangeArgs& a, cudaStream_t s);
 
 // Tensor-core kernels for bfloat16 (bp_grouped_tc.cu).
 // The adapters' low-rank sums come as bfloat16 terms (LowArgs).  A block of kTileRows rows is of one

@@ -133,7 +133,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_low(LowArgs g, int rank_warps, 
             const int2 info = tile_info(q, t, g.flags);
             if ((threadIdx.x & 31) == 0) g.tiles[t] = info;
         }
-    if (blockIdx.x == 0) zero_outside(q, threadIdx.x, kThreads, g.low, (bf16*)g.terms, g.n_terms * g.terms_stride);
+    if (blockIdx.x == 0)
+        zero_outside(q, threadIdx.x, kThreads, g.low, g.n_terms > 0 ? (bf16*)g.terms : nullptr,
+                     g.n_terms > 0 ? g.n_terms * g.terms_stride : q.rank);
     find_unit(q, blockIdx.x, where, warp_tot, g.flags);
     if (where[0] < 0) return;
     const int row0 = where[1], rows = where[2] - where[1], adapter = request_adapter(q, where[0], g.flags);
