@@ -98,7 +98,7 @@ bp_status make_layer(int dtype, int** flags, int* num_sms, const char* call) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(num_sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess && dtype == BP_BF16) e = tc_setup();
+    if (e == cudaSuccess) e = dtype == BP_BF16 ? tc_setup() : simt_setup();
     if (e == cudaSuccess && dtype == BP_BF16) e = few_setup();
     if (e == cudaSuccess) e = cudaMalloc(flags, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(*flags, 0, sizeof(int));

@@ -112,6 +112,7 @@ int sums_runs(int n_rows, int n_groups, int N, int dtype, int num_sms);
 cudaError_t group_sums(const SumsArgs& a, int dtype, int num_sms, cudaStream_t s);   // bp_sums.cu
 
 // float32 FMA kernels (bp_grouped_simt.cu).
+cudaError_t simt_setup();
 cudaError_t simt_rows(const RowsArgs& a, bool back, int num_sms, cudaStream_t s);
 cudaError_t simt_low(const LowArgs& a, cudaStream_t s);
 cudaError_t simt_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
