@@ -160,9 +160,9 @@ struct RouteArgs {
     int* offsets;
     int* source;
     int* place;
-    int* hist;              // [blocks of kRoutePatterns, E]
+    int* hist;              // [E, blocks of kRoutePatterns + 1]
 };
-constexpr int kRoutePatterns = 128;   // patterns of a block
+constexpr int kRoutePatterns = 32;   // patterns of a block
 cudaError_t route_forward(const RouteArgs& a, cudaStream_t s);
 cudaError_t route_backward(const RouteArgs& a, const float* dgate, void* dlogits, cudaStream_t s);
 struct MixArgs {

@@ -3,14 +3,16 @@
 #include <cmath>
 
 #include "bp_experts_device.cuh"
+#include "bp_tc_device.cuh"
 
 namespace bp {
 namespace {
 
-using bf16 = __nv_bfloat16;
-
+// A call of up to kOneBlock patterns is one block of 1,024 threads, which orders its rows too: one
+// launch.  Longer ones take blocks of kRoutePatterns patterns, four a warp, and two more launches for
+// the order (16,384 patterns of 64 experts: 128 patterns a block took 21 us for the choice alone).
+constexpr int kOneBlock = 256, kOneThreads = 1024;
 constexpr int kRouteThreads = 256;
-constexpr int kWords = kRoutePatterns / 32;   // of a block's patterns as bits
 
 // Ascending whole numbers for ascending floats; 0 for NaN and for -infinity, which are never
 // chosen.  (x + 0 turns -0 into +0, so that the two tie.)
@@ -29,6 +31,7 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 
 // A block's patterns that chose expert e, as bits: bits[e * kWords + word].
+template <int kWords>
 __device__ __forceinline__ int rank_of(const unsigned* bits, int e, int p) {
     int r = 0;
 #pragma unroll
@@ -38,6 +41,7 @@ __device__ __forceinline__ int rank_of(const unsigned* bits, int e, int p) {
     }
     return r;
 }
+template <int kWords>
 __device__ __forceinline__ int count_of(const unsigned* bits, int e) {
     int r = 0;
 #pragma unroll
@@ -46,12 +50,13 @@ __device__ __forceinline__ int count_of(const unsigned* bits, int e) {
 }
 
 // Rows of a block's choices: base[e] is the row of the block's first pattern with expert e.
+template <int kWords>
 __device__ __forceinline__ void place_rows(const RouteArgs& g, const unsigned* bits, const int* base, int p0, int np) {
     for (int i = threadIdx.x; i < np * g.k; i += blockDim.x) {
         const int p = i / g.k, e = g.expert[(size_t)p0 * g.k + i];
         int at = -1;
         if (e >= 0) {
-            at = base[e] + rank_of(bits, e, p);
+            at = base[e] + rank_of<kWords>(bits, e, p);
             g.source[at] = p0 + p;
         }
         g.place[(size_t)p0 * g.k + i] = at;
@@ -85,17 +90,20 @@ __device__ __forceinline__ int block_scan(int* cnt, int E, int* warp_tot) {
 }
 
 // A warp a pattern, lane l with the logits of experts l, l + 32, ..: k times the largest one
-// left (by its order, then by the lowest index).  A call of one block orders its rows too.
-template <class T, int PER>
-__global__ void __launch_bounds__(kRouteThreads) k_route(RouteArgs g) {
+// left (by its order, then by the lowest index).
+template <class T, int PER, bool ONE>
+__global__ void __launch_bounds__(ONE ? kOneThreads : kRouteThreads) k_route(RouteArgs g) {
+    constexpr int kPatterns = ONE ? kOneBlock : kRoutePatterns, kThreads = ONE ? kOneThreads : kRouteThreads;
+    constexpr int kWords = kPatterns / 32;
     __shared__ unsigned bits[BP_MAX_EXPERTS * kWords];
-    __shared__ int base[BP_MAX_EXPERTS];
+    __shared__ int base[ONE ? BP_MAX_EXPERTS : 1];
     __shared__ int warp_tot[32];
-    const int p0 = blockIdx.x * kRoutePatterns, np = min(kRoutePatterns, g.n - p0);
+    pdl_launch();
+    const int p0 = blockIdx.x * kPatterns, np = min(kPatterns, g.n - p0);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < g.E * kWords; i += kRouteThreads) bits[i] = 0u;
+    for (int i = threadIdx.x; i < g.E * kWords; i += kThreads) bits[i] = 0u;
     __syncthreads();
-    for (int p = warp; p < np; p += kRouteThreads / 32) {
+    for (int p = warp; p < np; p += kThreads / 32) {
         const T* z = (const T*)g.logits + (size_t)(p0 + p) * g.E;
         unsigned o[PER];
         float v[PER];
@@ -147,47 +155,50 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(RouteArgs g) {
         }
     }
     __syncthreads();
-    if (gridDim.x > 1) {
-        for (int e = threadIdx.x; e < g.E; e += kRouteThreads) g.hist[(size_t)blockIdx.x * g.E + e] = count_of(bits, e);
-        return;
+    if constexpr (!ONE) {
+        for (int e = threadIdx.x; e < g.E; e += kThreads) g.hist[(size_t)e * (gridDim.x + 1) + blockIdx.x] = count_of<kWords>(bits, e);
+    } else {
+        for (int e = threadIdx.x; e < g.E; e += kThreads) base[e] = count_of<kWords>(bits, e);
+        __syncthreads();
+        const int total = block_scan(base, g.E, warp_tot);
+        for (int e = threadIdx.x; e < g.E; e += kThreads) g.offsets[e] = base[e];
+        if (threadIdx.x == 0) g.offsets[g.E] = total;
+        for (int i = total + threadIdx.x; i < g.n * g.k; i += kThreads) g.source[i] = -1;
+        place_rows<kWords>(g, bits, base, p0, np);
     }
-    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] = count_of(bits, e);
-    __syncthreads();
-    const int total = block_scan(base, g.E, warp_tot);
-    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) g.offsets[e] = base[e];
-    if (threadIdx.x == 0) g.offsets[g.E] = total;
-    for (int i = total + threadIdx.x; i < g.n * g.k; i += kRouteThreads) g.source[i] = -1;
-    place_rows(g, bits, base, p0, np);
 }
 
-// The blocks' counts turned into rows before each block, expert by expert (a warp each), and the
-// experts' totals into hist row `blocks`.
-__global__ void k_route_columns(RouteArgs g, int blocks) {
-    const int e = blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (e >= g.E) return;
+// An expert's counts, block after block, turned into its rows before each block, and their total
+// behind them: hist is [E, blocks + 1], a CTA an expert.
+__global__ void __launch_bounds__(kRouteThreads) k_route_columns(RouteArgs g, int blocks) {
+    __shared__ int warp_tot[32];
+    __shared__ int cnt[kRouteThreads];
+    pdl_launch();
+    pdl_wait();
+    int* h = g.hist + (size_t)blockIdx.x * (blocks + 1);
     int carry = 0;
-    for (int b = 0; b < blocks; b += 32) {
-        const int x = b + lane < blocks ? g.hist[(size_t)(b + lane) * g.E + e] : 0;
-        int s = x;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += y;
-        }
-        if (b + lane < blocks) g.hist[(size_t)(b + lane) * g.E + e] = carry + s - x;
-        carry += __shfl_sync(0xffffffffu, s, 31);
+    for (int b = 0; b < blocks; b += kRouteThreads) {
+        const int i = b + threadIdx.x;
+        cnt[threadIdx.x] = i < blocks ? h[i] : 0;
+        const int total = block_scan(cnt, kRouteThreads, warp_tot);
+        if (i < blocks) h[i] = carry + cnt[threadIdx.x];
+        carry += total;
+        __syncthreads();
     }
-    if (lane == 0) g.hist[(size_t)blocks * g.E + e] = carry;
+    if (threadIdx.x == 0) h[blocks] = carry;
 }
 
 // Rows of every block's choices, from the counts.
 __global__ void __launch_bounds__(kRouteThreads) k_route_place(RouteArgs g) {
+    constexpr int kWords = kRoutePatterns / 32;
     __shared__ unsigned bits[BP_MAX_EXPERTS * kWords];
     __shared__ int base[BP_MAX_EXPERTS];
     __shared__ int warp_tot[32];
     const int p0 = blockIdx.x * kRoutePatterns, np = min(kRoutePatterns, g.n - p0);
     for (int i = threadIdx.x; i < g.E * kWords; i += kRouteThreads) bits[i] = 0u;
-    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] = g.hist[(size_t)gridDim.x * g.E + e];
+    pdl_wait();
+    const int* h = g.hist;
+    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] = h[(size_t)e * (gridDim.x + 1) + gridDim.x];
     __syncthreads();
     for (int i = threadIdx.x; i < np * g.k; i += kRouteThreads) {
         const int p = i / g.k, e = g.expert[(size_t)p0 * g.k + i];
@@ -199,11 +210,11 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_place(RouteArgs g) {
         if (threadIdx.x == 0) g.offsets[g.E] = total;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] += g.hist[(size_t)blockIdx.x * g.E + e];
+    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] += h[(size_t)e * (gridDim.x + 1) + blockIdx.x];
     __syncthreads();
     for (int i = p0 * g.k + threadIdx.x; i < (p0 + np) * g.k; i += kRouteThreads)
         if (i >= total) g.source[i] = -1;
-    place_rows(g, bits, base, p0, np);
+    place_rows<kWords>(g, bits, base, p0, np);
 }
 
 // Gradient of the gates: dz = p (.. ) for every expert with gates over all, for the chosen ones else.
@@ -358,12 +369,13 @@ __global__ void __launch_bounds__(kMixThreads) k_mix_backward(MixArgs g) {
     }
 }
 
-template <class T>
+template <class T, bool ONE>
 cudaError_t launch_route(const RouteArgs& a, int blocks, cudaStream_t s) {
-    if (a.E <= 32) k_route<T, 1><<<blocks, kRouteThreads, 0, s>>>(a);
-    else if (a.E <= 64) k_route<T, 2><<<blocks, kRouteThreads, 0, s>>>(a);
-    else if (a.E <= 128) k_route<T, 4><<<blocks, kRouteThreads, 0, s>>>(a);
-    else k_route<T, BP_MAX_EXPERTS / 32><<<blocks, kRouteThreads, 0, s>>>(a);
+    constexpr int threads = ONE ? kOneThreads : kRouteThreads;
+    if (a.E <= 32) k_route<T, 1, ONE><<<blocks, threads, 0, s>>>(a);
+    else if (a.E <= 64) k_route<T, 2, ONE><<<blocks, threads, 0, s>>>(a);
+    else if (a.E <= 128) k_route<T, 4, ONE><<<blocks, threads, 0, s>>>(a);
+    else k_route<T, BP_MAX_EXPERTS / 32, ONE><<<blocks, threads, 0, s>>>(a);
     return cudaGetLastError();
 }
 
@@ -383,12 +395,13 @@ int mix_warps(int n, int N, int per_warp) {
 }  // namespace
 
 cudaError_t route_forward(const RouteArgs& a, cudaStream_t s) {
-    const int blocks = a.n > 0 ? (a.n + kRoutePatterns - 1) / kRoutePatterns : 1;
-    cudaError_t e = a.dtype == BP_F32 ? launch_route<float>(a, blocks, s) : launch_route<bf16>(a, blocks, s);
-    if (e != cudaSuccess || blocks == 1) return e;
-    k_route_columns<<<(a.E + 7) / 8, 256, 0, s>>>(a, blocks);
-    k_route_place<<<blocks, kRouteThreads, 0, s>>>(a);
-    return cudaGetLastError();
+    const bool f32 = a.dtype == BP_F32;
+    if (a.n <= kOneBlock) return f32 ? launch_route<float, true>(a, 1, s) : launch_route<bf16, true>(a, 1, s);
+    const int blocks = (a.n + kRoutePatterns - 1) / kRoutePatterns;
+    cudaError_t e = f32 ? launch_route<float, false>(a, blocks, s) : launch_route<bf16, false>(a, blocks, s);
+    if (e == cudaSuccess) e = launch_pdl(k_route_columns, a.E, 1, kRouteThreads, 0, s, a, blocks);
+    if (e == cudaSuccess) e = launch_pdl(k_route_place, blocks, 1, kRouteThreads, 0, s, a);
+    return e;
 }
 
 cudaError_t route_backward(const RouteArgs& a, const float* dgate, void* dlogits, cudaStream_t s) {
