@@ -3,13 +3,14 @@
 //
 // Each kernel is a tile of 16 P x 16 P by 256 threads (P x P sums a thread) over K, through a ring of
 // four steps in shared memory that cp.async fills three steps ahead.  What differs between the products
-// is where an operand's element lies, which the kernels pass as functions; operands are read along
-// whichever of their dimensions is contiguous, a float at a time (rows of 203 floats start on no 16-byte
-// boundary).  P = 8 where there are tiles for every SM: a thread then reads 16 floats of shared memory
-// for 64 FMAs, and the FMA pipe is the bound; P = 4 and 2 read two and four times as many for each, but
-// cut small products into enough tiles (128 rows of 203-120 in each of 8 groups: 48 tiles of P = 4 take a
-// third of the SMs).  Sums run over at most kSum values of k at a time, which are added up apart, so that
-// a long sum's error stays that of short ones (65,536 rows in one chain: ten times it).
+// is where an operand's rows start, which the kernels pass as functions; an operand is copied along
+// whichever of its dimensions is contiguous and kept as it lies, k by k or row by row, so that its copies
+// are 16 bytes wide where rows start on 16-byte boundaries (those of 203 floats do not: 4 bytes).  P = 8
+// where there are tiles for every SM: a thread then reads 16 floats of shared memory for 64 FMAs, and the
+// FMA pipe is the bound; P = 4 and 2 read two and four times as many for each, but cut small products
+// into enough tiles (128 rows of 203-120 in each of 8 groups: 48 tiles of P = 4 take a third of the
+// SMs).  Sums run over at most kSum values of k at a time, which are added up apart, so that a long sum's
+// error stays that of short ones (65,536 rows in one chain: ten times it).
 #include "bp_experts_device.cuh"
 
 namespace bp {
@@ -23,35 +24,79 @@ constexpr int kRing = 4;
 template <int P>
 struct Step {
     static constexpr int T = 16 * P, K = P == 8 ? 16 : 32;
-    float a[K][T + 4];
-    float b[K][T + 4];
+    static constexpr int kRowPitch = K + 4, kColPitch = T + 4;   // of an operand kept by rows; by k
+    static constexpr int kFloats = T * kRowPitch > K * kColPitch ? T * kRowPitch : K * kColPitch;
+    float a[kFloats];
+    float b[kFloats];
 };
 template <int P>
 constexpr int kSmem = kRing * sizeof(Step<P>);
 
-// total += A B^T over k in [0, K): a(m, k) and b(n, k) point at the operands' elements (NULL: 0).
-// A_KFAST, B_KFAST: the operand's k is contiguous in memory.  `any`: an address that may be named.
-template <int P, bool A_KFAST, bool B_KFAST, class FA, class FB>
-__device__ __forceinline__ void accumulate(Step<P>* ring, float (&total)[P][P], int K, const float* any, FA a, FB b) {
-    constexpr int T = Step<P>::T, TK = Step<P>::K, L = T * TK / kThreads;
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, steps = (K + TK - 1) / TK;
+// Row (column) of a tile that sum i of a thread is for, w its ty (tx): of an operand kept by rows w + 16 i
+// (a quarter warp's 16-byte reads then hit all banks), of one kept by k runs of four.
+template <int P, bool KFAST>
+__device__ __forceinline__ int tile_at(int w, int i) {
+    constexpr int V = P < 4 ? P : 4;
+    return KFAST ? w + 16 * i : 16 * V * (i / V) + V * w + i % V;
+}
+
+// One operand's part of step `step`.  KFAST: row(m) is where row m's k lie (NULL: zeros); else row(k) is
+// where k's columns lie, of which `cols` are there.
+template <int P, bool KFAST, bool WIDE, class F>
+__device__ __forceinline__ void copy_operand(float* to, int step, int K, int cols, const float* any, F row) {
+    constexpr int T = Step<P>::T, TK = Step<P>::K, V = WIDE ? 4 : 1, L = T * TK / V / kThreads;
+    constexpr int kPer = (KFAST ? TK : T) / V;   // copies along the contiguous dimension
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(to);
+    const int fast = threadIdx.x % kPer * V;
+    const bool in = KFAST ? step * TK + fast < K : fast < cols;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const int slow = threadIdx.x / kPer + i * (kThreads / kPer);
+        const float* p = nullptr;
+        if (in && (KFAST || step * TK + slow < K)) p = row(KFAST ? slow : step * TK + slow);
+        const uint32_t at = base + (slow * (KFAST ? Step<P>::kRowPitch : Step<P>::kColPitch) + fast) * 4;
+        const float* from = p != nullptr ? p + (KFAST ? step * TK + fast : fast) : any;
+        const int n = p != nullptr ? 4 * V : 0;
+        if constexpr (WIDE)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(at), "l"(from), "r"(n) : "memory");
+        else
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(at), "l"(from), "r"(n) : "memory");
+    }
+}
+// KN values of k of a thread's rows (columns).
+template <int P, bool KFAST, int KN>
+__device__ __forceinline__ void read_operand(float (&x)[KN][P], const float* t, int k, int w) {
+    if constexpr (KFAST) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const float4 f = *reinterpret_cast<const float4*>(t + tile_at<P, true>(w, i) * Step<P>::kRowPitch + k);
+            x[0][i] = f.x, x[1][i] = f.y, x[2][i] = f.z, x[3][i] = f.w;
+        }
+    } else {
+        constexpr int V = P < 4 ? P : 4;
+#pragma unroll
+        for (int j = 0; j < KN; ++j)
+#pragma unroll
+            for (int i = 0; i < P; i += V) {
+                const float* p = t + (k + j) * Step<P>::kColPitch + tile_at<P, false>(w, i);
+                if constexpr (V == 4) *reinterpret_cast<float4*>(&x[j][i]) = *reinterpret_cast<const float4*>(p);
+                else *reinterpret_cast<float2*>(&x[j][i]) = *reinterpret_cast<const float2*>(p);
+            }
+    }
+}
+
+// total += A B^T over k in [0, K).  WIDE: both operands' rows start on 16-byte boundaries, K is a
+// multiple of 4 if they are contiguous along it, their columns are if not.
+template <int P, bool A_KFAST, bool B_KFAST, bool WIDE, class FA, class FB>
+__device__ __forceinline__ void accumulate(Step<P>* ring, float (&total)[P][P], int K, const float* any, int a_cols, FA a,
+                                           int b_cols, FB b) {
+    constexpr int TK = Step<P>::K, KN = 4;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, steps = (K + TK - 1) / TK;
     float acc[P][P];
     auto copy = [&](int step) {
-        Step<P>& t = ring[step % kRing];
-        auto one = [&](float* to, const float* from) {
-            asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                         "l"(from != nullptr ? from : any), "r"(from != nullptr ? 4 : 0)
-                         : "memory");
-        };
         if (step < steps) {
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                const int e = tid + i * kThreads;
-                const int ak = A_KFAST ? e % TK : e / T, am = A_KFAST ? e / TK : e % T;
-                const int bk = B_KFAST ? e % TK : e / T, bn = B_KFAST ? e / TK : e % T;
-                one(&t.a[ak][am], step * TK + ak < K ? a(am, step * TK + ak) : nullptr);
-                one(&t.b[bk][bn], step * TK + bk < K ? b(bn, step * TK + bk) : nullptr);
-            }
+            copy_operand<P, A_KFAST, WIDE>(ring[step % kRing].a, step, K, a_cols, any, a);
+            copy_operand<P, B_KFAST, WIDE>(ring[step % kRing].b, step, K, b_cols, any, b);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -77,23 +122,17 @@ __device__ __forceinline__ void accumulate(Step<P>* ring, float (&total)[P][P], 
         __syncthreads();   // step i is there for all, and step i - 1 is read
         copy(i + kRing - 1);
         const Step<P>& t = ring[i % kRing];
+#pragma unroll(P == 8 ? 2 : 4)
+        for (int k = 0; k < TK; k += KN) {
+            float x[KN][P], y[KN][P];
+            read_operand<P, A_KFAST, KN>(x, t.a, k, ty);
+            read_operand<P, B_KFAST, KN>(y, t.b, k, tx);
 #pragma unroll
-        for (int k = 0; k < TK; ++k) {
-            float x[P], y[P];   // (tile_at)
-            if constexpr (P == 2) {
-                *reinterpret_cast<float2*>(x) = *reinterpret_cast<const float2*>(&t.a[k][2 * ty]);
-                *reinterpret_cast<float2*>(y) = *reinterpret_cast<const float2*>(&t.b[k][2 * tx]);
-            } else {
+            for (int j = 0; j < KN; ++j)
 #pragma unroll
-                for (int h = 0; h < P / 4; ++h) {
-                    *reinterpret_cast<float4*>(&x[4 * h]) = *reinterpret_cast<const float4*>(&t.a[k][64 * h + 4 * ty]);
-                    *reinterpret_cast<float4*>(&y[4 * h]) = *reinterpret_cast<const float4*>(&t.b[k][64 * h + 4 * tx]);
-                }
-            }
+                for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int p = 0; p < P; ++p)
-#pragma unroll
-                for (int q = 0; q < P; ++q) acc[p][q] = fmaf(x[p], y[q], acc[p][q]);
+                    for (int q = 0; q < P; ++q) acc[p][q] = fmaf(x[j][p], y[j][q], acc[p][q]);
         }
         if (i % (kSum / TK) == kSum / TK - 1) {
             add();
@@ -103,14 +142,8 @@ __device__ __forceinline__ void accumulate(Step<P>* ring, float (&total)[P][P], 
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     add();
 }
-// Row (or column) of a tile that sum i of a thread is for; w: its ty (tx).
-template <int P>
-__device__ __forceinline__ int tile_at(int w, int i) {
-    constexpr int V = P < 4 ? P : 4;
-    return 16 * V * (i / V) + V * w + i % V;
-}
 
-template <int P, bool BACK>
+template <int P, bool BACK, bool WIDE>
 __global__ void __launch_bounds__(kThreads) k_rows_simt(RowsArgs g) {
     constexpr int T = Step<P>::T;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -133,12 +166,15 @@ __global__ void __launch_bounds__(kThreads) k_rows_simt(RowsArgs g) {
     float acc[P][P] = {};
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     auto of_layer = [&] {
-        auto fa = [&](int m, int k) { return m < rows ? in + (size_t)src[m] * g.K + k : nullptr; };
+        auto fa = [&](int m) { return m < rows ? in + (size_t)src[m] * g.K : nullptr; };
         if (BACK)
-            accumulate<P, true, false>(t, acc, g.K, W, fa, [&](int n, int k) { return n0 + n < g.N ? W + (size_t)k * g.N + n0 + n : nullptr; });
+            accumulate<P, true, false, WIDE>(t, acc, g.K, W, 0, fa, g.N - n0, [&](int k) { return W + (size_t)k * g.N + n0; });
         else
-            accumulate<P, true, true>(t, acc, g.K, W, fa, [&](int n, int k) { return n0 + n < g.N ? W + (size_t)(n0 + n) * g.K + k : nullptr; });
+            accumulate<P, true, true, WIDE>(t, acc, g.K, W, 0, fa, 0, [&](int n) { return n0 + n < g.N ? W + (size_t)(n0 + n) * g.K : nullptr; });
     };
+    // this thread's rows and columns
+    auto row_of = [&](int i) { return tile_at<P, true>(ty, i); };
+    auto col_of = [&](int j) { return tile_at<P, !BACK>(tx, j); };
     if (g.low == nullptr) {
         of_layer();
     } else {
@@ -150,19 +186,33 @@ __global__ void __launch_bounds__(kThreads) k_rows_simt(RowsArgs g) {
             if (ad >= 0) {
                 const float c = g.scale != nullptr ? g.scale[ad] : 1.f;
                 const float* A = (const float*)g.P + (size_t)ad * r * g.N;
-                accumulate<P, true, false>(
-                    t, acc, r, A, [&](int m, int k) { return m < rows ? g.low + (size_t)(row0 + m) * r + k : nullptr; },
-                    [&](int n, int k) { return n0 + n < g.N ? A + (size_t)k * g.N + n0 + n : nullptr; });
+                float part[P][P] = {};   // by tile_at<P, false> along the columns
+                accumulate<P, true, false, false>(
+                    t, part, r, A, 0, [&](int m) { return m < rows ? g.low + (size_t)(row0 + m) * r : nullptr; }, g.N - n0,
+                    [&](int k) { return A + (size_t)k * g.N + n0; });
+                if (!BACK) {   // to the columns of the layer's product, through shared memory
+                    float* turn = reinterpret_cast<float*>(smem);
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < P; ++i)
+#pragma unroll
+                        for (int j = 0; j < P; ++j) turn[row_of(i) * (T + 1) + tile_at<P, false>(tx, j)] = part[i][j];
+                    __syncthreads();
+#pragma unroll
+                    for (int i = 0; i < P; ++i)
+#pragma unroll
+                        for (int j = 0; j < P; ++j) part[i][j] = turn[row_of(i) * (T + 1) + col_of(j)];
+                }
 #pragma unroll
                 for (int i = 0; i < P; ++i)
 #pragma unroll
-                    for (int j = 0; j < P; ++j) acc[i][j] *= c;
+                    for (int j = 0; j < P; ++j) acc[i][j] = c * part[i][j];
             }
         } else if (first < g.req.n_requests) {
             // several: each row with its own adapter's values and no others (0 times an infinity is not 0)
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                const int m = tile_at<P>(ty, i), row = row0 + m;
+                const int m = row_of(i), row = row0 + m;
                 if (m >= rows) continue;
                 const int q = first_request(g.req, row);
                 if (q >= g.req.n_requests) continue;
@@ -173,7 +223,7 @@ __global__ void __launch_bounds__(kThreads) k_rows_simt(RowsArgs g) {
                 const float *low = g.low + (size_t)row * r, *A = (const float*)g.P + (size_t)ad * r * g.N + n0;
                 int at[P];   // columns past the last one read the last one
 #pragma unroll
-                for (int j = 0; j < P; ++j) at[j] = min(tile_at<P>(tx, j), g.N - 1 - n0);
+                for (int j = 0; j < P; ++j) at[j] = min(col_of(j), g.N - 1 - n0);
 #pragma unroll 4
                 for (int k = 0; k < r; ++k) {
                     const float u = c * low[k];
@@ -186,13 +236,13 @@ __global__ void __launch_bounds__(kThreads) k_rows_simt(RowsArgs g) {
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
-        const int m = tile_at<P>(ty, i), row = row0 + m;
+        const int m = row_of(i), row = row0 + m;
         if (m >= rows) continue;
         const float* x = nullptr;
         if (BACK && g.squash) x = (const float*)g.x + (size_t)source_row(g.x_source, row, g.n_x, g.flags) * g.N;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const int n = n0 + tile_at<P>(tx, j);
+            const int n = n0 + col_of(j);
             if (n >= g.N) continue;
             float v = acc[i][j];
             if (!BACK) {
@@ -225,17 +275,17 @@ __global__ void __launch_bounds__(kThreads) k_low_simt(LowArgs g) {
     float acc[P][P] = {};
     if (ad >= 0) {
         const float *in = (const float*)g.in + (size_t)row0 * g.K, *A = (const float*)g.P + (size_t)ad * r * g.K;
-        accumulate<P, true, true>(
-            t, acc, g.K, A, [&](int m, int k) { return m < rows ? in + (size_t)m * g.K + k : nullptr; },
-            [&](int n, int k) { return n0 + n < r ? A + (size_t)(n0 + n) * g.K + k : nullptr; });
+        accumulate<P, true, true, false>(
+            t, acc, g.K, A, 0, [&](int m) { return m < rows ? in + (size_t)m * g.K : nullptr; }, 0,
+            [&](int n) { return n0 + n < r ? A + (size_t)(n0 + n) * g.K : nullptr; });
     }
     const float c = ad >= 0 && g.scaled_low && g.scale != nullptr ? g.scale[ad] : 1.f;
 #pragma unroll
     for (int i = 0; i < P; ++i)
 #pragma unroll
         for (int j = 0; j < P; ++j)
-            if (tile_at<P>(ty, i) < rows && n0 + tile_at<P>(tx, j) < r)
-                g.low[(size_t)(row0 + tile_at<P>(ty, i)) * r + n0 + tile_at<P>(tx, j)] = c * acc[i][j];
+            if (tile_at<P, true>(ty, i) < rows && n0 + tile_at<P, true>(tx, j) < r)
+                g.low[(size_t)(row0 + tile_at<P, true>(ty, i)) * r + n0 + tile_at<P, true>(tx, j)] = c * acc[i][j];
 }
 
 template <int P>
@@ -246,14 +296,14 @@ __device__ __forceinline__ void store_change(float* G, int M, int N, int m0, int
     for (int i = 0; i < P; ++i)
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const int m = m0 + tile_at<P>(ty, i), n = n0 + tile_at<P>(tx, j);
+            const int m = m0 + tile_at<P, false>(ty, i), n = n0 + tile_at<P, false>(tx, j);
             if (m >= M || n >= N) continue;
             float* p = G + (size_t)m * N + n;
             *p = accumulate ? *p + c * acc[i][j] : c * acc[i][j];
         }
 }
 
-template <int P>
+template <int P, bool WIDE>
 __global__ void __launch_bounds__(kThreads) k_change_simt(ChangeArgs g) {
     constexpr int T = Step<P>::T;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -263,11 +313,9 @@ __global__ void __launch_bounds__(kThreads) k_change_simt(ChangeArgs g) {
     group_rows(g.groups.offsets, g.groups.n_rows, e, lo, hi, g.flags);
     const float *a = (const float*)g.a, *b = (const float*)g.b;
     float acc[P][P] = {};
-    accumulate<P, false, false>(
-        t, acc, hi - lo, a, [&](int m, int k) { return m0 + m < g.M ? a + (size_t)(lo + k) * g.M + m0 + m : nullptr; },
-        [&](int n, int k) {
-            return n0 + n < g.N ? b + (size_t)source_row(g.source, lo + k, g.n_b, g.flags) * g.N + n0 + n : nullptr;
-        });
+    accumulate<P, false, false, WIDE>(
+        t, acc, hi - lo, a, g.M - m0, [&](int k) { return a + (size_t)(lo + k) * g.M + m0; }, g.N - n0,
+        [&](int k) { return b + (size_t)source_row(g.source, lo + k, g.n_b, g.flags) * g.N + n0; });
     store_change<P>(g.G + (size_t)e * g.M * g.N, g.M, g.N, m0, n0, acc, 1.f, g.accumulate);
 }
 
@@ -284,9 +332,9 @@ __global__ void __launch_bounds__(kThreads) k_low_change_simt(LowChangeArgs g) {
         for (; mine != 0; mine &= mine - 1) {
             int lo, hi;
             group_rows(g.req.offsets, g.req.n_rows, base + __ffs(mine) - 1, lo, hi, g.flags);
-            accumulate<P, false, false>(
-                t, acc, hi - lo, b, [&](int m, int k) { return m0 + m < r ? g.low + (size_t)(lo + k) * r + m0 + m : nullptr; },
-                [&](int n, int k) { return n0 + n < g.N ? b + (size_t)(lo + k) * g.N + n0 + n : nullptr; });
+            accumulate<P, false, false, false>(
+                t, acc, hi - lo, b, r - m0, [&](int k) { return g.low + (size_t)(lo + k) * r + m0; }, g.N - n0,
+                [&](int k) { return b + (size_t)(lo + k) * g.N + n0; });
         }
     }
     store_change<P>(g.G + (size_t)ad * r * g.N, r, g.N, m0, n0, acc, g.scale != nullptr ? g.scale[ad] : 1.f, g.accumulate);
@@ -300,18 +348,19 @@ template <class K>
 static cudaError_t allow(K k, int bytes) {
     return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
-template <int P>
+template <int P, bool WIDE>
 static cudaError_t setup_tile() {
     cudaError_t e;
-    if ((e = allow(k_rows_simt<P, false>, kSmem<P>)) != cudaSuccess) return e;
-    if ((e = allow(k_rows_simt<P, true>, kSmem<P>)) != cudaSuccess) return e;
-    return allow(k_change_simt<P>, kSmem<P>);
+    if ((e = allow(k_rows_simt<P, false, WIDE>, kSmem<P>)) != cudaSuccess) return e;
+    if ((e = allow(k_rows_simt<P, true, WIDE>, kSmem<P>)) != cudaSuccess) return e;
+    return allow(k_change_simt<P, WIDE>, kSmem<P>);
 }
 cudaError_t simt_setup() {
     cudaError_t e;
-    if ((e = setup_tile<2>()) != cudaSuccess) return e;
-    if ((e = setup_tile<4>()) != cudaSuccess) return e;
-    if ((e = setup_tile<8>()) != cudaSuccess) return e;
+    if ((e = setup_tile<2, false>()) != cudaSuccess) return e;
+    if ((e = setup_tile<4, false>()) != cudaSuccess) return e;
+    if ((e = setup_tile<8, false>()) != cudaSuccess) return e;
+    if ((e = setup_tile<8, true>()) != cudaSuccess) return e;
     if ((e = allow(k_low_simt, kSmem<kLowP>)) != cudaSuccess) return e;
     return allow(k_low_change_simt, kSmem<kLowP>);
 }
@@ -322,15 +371,22 @@ static int pick_tile(int num_sms, Tiles tiles) {
     return tiles(128) >= num_sms ? 8 : tiles(64) >= num_sms ? 4 : 2;
 }
 
+// Whether both operands' rows start on 16-byte boundaries.
+static bool wide(const void* a, const void* b, int a_row, int b_row) {
+    return (((uintptr_t)a | (uintptr_t)b) & 15) == 0 && a_row % 4 == 0 && b_row % 4 == 0;
+}
+
 cudaError_t simt_rows(const RowsArgs& a, bool back, int num_sms, cudaStream_t s) {
     // the groups' sizes are on the device: taken for even
     const long long busy = a.groups.n_groups < a.groups.n_rows ? a.groups.n_groups : a.groups.n_rows;
     const int p = pick_tile(num_sms, [&](int T) { return a.groups.n_rows / T < busy && T > 64 ? 0 : busy * blocks(a.groups.n_rows, busy * T) * blocks(a.N, T); });
     const dim3 grid(max_tiles(a.groups.n_rows, a.groups.n_groups, 16 * p), blocks(a.N, 16 * p));
     auto go = [&](auto k, int bytes) { k<<<grid, kThreads, bytes, s>>>(a); };
-    if (p == 8) back ? go(k_rows_simt<8, true>, kSmem<8>) : go(k_rows_simt<8, false>, kSmem<8>);
-    else if (p == 4) back ? go(k_rows_simt<4, true>, kSmem<4>) : go(k_rows_simt<4, false>, kSmem<4>);
-    else back ? go(k_rows_simt<2, true>, kSmem<2>) : go(k_rows_simt<2, false>, kSmem<2>);
+    if (p == 8 && wide(a.in, a.W, a.K, back ? a.N : a.K))
+        back ? go(k_rows_simt<8, true, true>, kSmem<8>) : go(k_rows_simt<8, false, true>, kSmem<8>);
+    else if (p == 8) back ? go(k_rows_simt<8, true, false>, kSmem<8>) : go(k_rows_simt<8, false, false>, kSmem<8>);
+    else if (p == 4) back ? go(k_rows_simt<4, true, false>, kSmem<4>) : go(k_rows_simt<4, false, false>, kSmem<4>);
+    else back ? go(k_rows_simt<2, true, false>, kSmem<2>) : go(k_rows_simt<2, false, false>, kSmem<2>);
     return cudaGetLastError();
 }
 
@@ -343,9 +399,10 @@ cudaError_t simt_low(const LowArgs& a, cudaStream_t s) {
 cudaError_t simt_change(const ChangeArgs& a, int num_sms, cudaStream_t s) {
     const int p = pick_tile(num_sms, [&](int T) { return (long long)a.groups.n_groups * blocks(a.M, T) * blocks(a.N, T); });
     const dim3 grid(blocks(a.N, 16 * p), blocks(a.M, 16 * p), a.groups.n_groups);
-    if (p == 8) k_change_simt<8><<<grid, kThreads, kSmem<8>, s>>>(a);
-    else if (p == 4) k_change_simt<4><<<grid, kThreads, kSmem<4>, s>>>(a);
-    else k_change_simt<2><<<grid, kThreads, kSmem<2>, s>>>(a);
+    if (p == 8 && wide(a.a, a.b, a.M, a.N)) k_change_simt<8, true><<<grid, kThreads, kSmem<8>, s>>>(a);
+    else if (p == 8) k_change_simt<8, false><<<grid, kThreads, kSmem<8>, s>>>(a);
+    else if (p == 4) k_change_simt<4, false><<<grid, kThreads, kSmem<4>, s>>>(a);
+    else k_change_simt<2, false><<<grid, kThreads, kSmem<2>, s>>>(a);
     return cudaGetLastError();
 }
 

@@ -339,25 +339,39 @@ __global__ void __launch_bounds__(kMixThreads) k_mix_backward(MixArgs g) {
     }
     const T *H = (const T*)g.H, *D = (const T*)g.D;
     float mine = 0.f;   // lane j: this warp's part of choice j's product
-    for (int j = 0; j < g.k; ++j) {
-        const int r = __shfl_sync(0xffffffffu, row, j);
-        const float w = __shfl_sync(0xffffffffu, gate, j);
-        if (r < 0) continue;
-        float dot = 0.f;
+    constexpr int C = 4;   // choices that share a read of D
+    for (int j0 = 0; j0 < g.k; j0 += C) {
+        int r[C];
+        float w[C], dot[C];
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            r[j] = __shfl_sync(0xffffffffu, row, j0 + j);   // (k is at most 16; lanes from k on hold -1)
+            w[j] = __shfl_sync(0xffffffffu, gate, j0 + j);
+            dot[j] = 0.f;
+        }
         for (int c = (part * 32 + lane) * V; c < g.N; c += g.warps * 32 * V) {
-            Piece<T, V> d, h, o;
-            d.load(D + (size_t)t * g.N + c);
+            Piece<T, V> d, h[C], o;
+            if (live) d.load(D + (size_t)t * g.N + c);
 #pragma unroll
-            for (int i = 0; i < V; ++i) o.v[i] = w * d.v[i];
-            o.store((T*)g.dH + (size_t)r * g.N + c);
-            if (g.dgate != nullptr) {
-                h.load(H + (size_t)r * g.N + c);
+            for (int j = 0; j < C; ++j)
+                if (r[j] >= 0 && g.dgate != nullptr) h[j].load(H + (size_t)r[j] * g.N + c);
 #pragma unroll
-                for (int i = 0; i < V; ++i) dot = fmaf(h.v[i], d.v[i], dot);
+            for (int j = 0; j < C; ++j) {
+                if (r[j] < 0) continue;
+#pragma unroll
+                for (int i = 0; i < V; ++i) o.v[i] = w[j] * d.v[i];
+                o.store((T*)g.dH + (size_t)r[j] * g.N + c);
+                if (g.dgate != nullptr) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) dot[j] = fmaf(h[j].v[i], d.v[i], dot[j]);
+                }
             }
         }
-        dot = warp_sum(dot);
-        if (lane == j) mine = dot;
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            const float x = warp_sum(dot[j]);
+            if (lane == j0 + j) mine = x;
+        }
     }
     if (g.dgate == nullptr) return;
     if (lane < g.k) dots[warp][lane] = mine;
