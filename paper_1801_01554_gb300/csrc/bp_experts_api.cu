@@ -32,6 +32,8 @@ struct bp_adapters {
     void* terms = nullptr;
     void* u_terms = nullptr;
     int2* tiles = nullptr;
+    float* scratch = nullptr;      // changes of shares of the rows
+    unsigned* arrived = nullptr;
     int n_terms = 0, stride = 0;
     LowTerms low_terms() const { return {terms, n_terms, stride, tiles}; }
 };
@@ -418,12 +420,16 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
     st = make_layer(dtype, &l->flags, &l->num_sms, call);
     if (st == BP_OK) st = cuda_status(cudaMalloc(&l->low, (size_t)max_rows * rank * sizeof(float)), call);
     if (st == BP_OK && dtype == BP_BF16) {
-        // four blocks of 64 columns at most: three terms up to rank 64, two above
-        l->stride = rank <= 64 ? 64 : 128;
+        // 256 columns at most: three terms up to rank 64, two above
+        l->stride = rank <= 32 ? 32 : rank <= 64 ? 64 : 128;
         l->n_terms = rank <= 64 ? 3 : 2;
         const size_t bytes = (size_t)max_rows * l->n_terms * l->stride * 2;
         st = cuda_status(cudaMalloc(&l->terms, bytes), call);
         if (st == BP_OK) st = cuda_status(cudaMalloc(&l->u_terms, bytes), call);
+        const size_t counts = low_change_counts(l->num_sms) * sizeof(unsigned);
+        if (st == BP_OK) st = cuda_status(cudaMalloc(&l->scratch, low_change_scratch(rank, l->num_sms) * sizeof(float)), call);
+        if (st == BP_OK) st = cuda_status(cudaMalloc(&l->arrived, counts), call);
+        if (st == BP_OK) st = cuda_status(cudaMemset(l->arrived, 0, counts), call);
         if (st == BP_OK)
             st = cuda_status(cudaMalloc(&l->tiles, ((size_t)max_rows / kTileRows + 1) * sizeof(int2)), call);
     }
@@ -443,6 +449,8 @@ void bp_adapters_destroy(bp_adapters* l) {
     cudaFree(l->terms);
     cudaFree(l->u_terms);
     cudaFree(l->tiles);
+    cudaFree(l->scratch);
+    cudaFree(l->arrived);
     delete l;
 }
 
@@ -552,11 +560,11 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
     }
     const bool tc = l->dtype == BP_BF16;
     if (st == BP_OK && ga) {
-        const LowChangeArgs a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->flags};
+        const LowChangeArgs a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->scratch, l->arrived, l->flags};
         st = cuda_status(tc ? tc_low_change(a, l->low_terms(), l->num_sms, s) : simt_low_change(a, s), call);
     }
     if (st == BP_OK && gb) {
-        const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->flags};
+        const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->scratch, l->arrived, l->flags};
         LowTerms u = l->low_terms();
         u.terms = l->u_terms;
         if (tc && some) st = cuda_status(low_terms(d_U, n_rows, l->rank, l->u_terms, u.stride, u.n_terms, l->num_sms, s), call);

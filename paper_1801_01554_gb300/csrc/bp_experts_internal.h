@@ -91,6 +91,9 @@ struct LowChangeArgs {
     const float* scale;     // or NULL
     float* G;
     int accumulate;
+    // bfloat16: sums of shares of the rows, and zeros that count their arrivals (low_change_scratch)
+    float* scratch;
+    unsigned* arrived;
     int* flags;
 };
 
@@ -137,6 +140,8 @@ cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGro
 cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_sms, cudaStream_t s);
 cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
 cudaError_t tc_low(const LowArgs& a, int num_sms, cudaStream_t s);
+size_t low_change_scratch(int rank, int num_sms);   // floats
+size_t low_change_counts(int num_sms);
 cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, int num_sms, cudaStream_t s);
 
 // The forward product of a few rows in bfloat16 (bp_few.cu), rows read through an index too; with low,

@@ -26,11 +26,10 @@
 // a tile of several requests each request's part is a sum of its own for all of the tile's rows, of
 // which the epilogue adds the request's rows (as one product with the other requests' rows at zero,
 // an adapter's infinity would reach them); with more requests than the rank has columns the
-// epilogue takes the rows one by one instead.  In the low form every term is a
-// product of its own into the same sums (three terms up to rank 64: as exact as float32), the K
-// blocks run over the adapter's requests in order, and the rows of a tile past the rank hold
-// sums that nobody reads.
-#include <cstdio>
+// epilogue takes the rows one by one instead.  In the low form the terms lie side by side along
+// M (three up to rank 64: as exact as float32), so that a rank of up to 32 costs one product and one
+// of 64 two instead of three; the epilogue warps of the other terms pass their sums on through shared
+// memory.  Its K blocks run over the adapter's requests in order.
 #include <mutex>
 
 #include "bp_experts_device.cuh"
@@ -57,14 +56,18 @@ struct TcArgs {
     bf16* out;
     float* G;
     int accumulate;
+    int sectors;             // G starts on a 32-byte boundary
     // adapters
     int2* tiles;               // per 128 rows: adapter or kind, first request; or NULL
     int rank16;                // 16-wide pieces of the rank
-    int n_terms, stride;       // bfloat16 terms of low, and their pitch (a multiple of 64)
+    int n_terms, stride;       // bfloat16 terms of low, and their pitch (32, 64 or 128)
     Requests req;
     const float* low;
     const bf16* P;
     const float* scale;
+    int runs;                  // of the low form: shares of an adapter's rows, of which the sums go to
+    float* scratch;            // [runs, n_adapters, rank, N]
+    unsigned* arrived;         // of every warp's part of a tile; zeros, left so
     // up
     float* low_out;
     bf16* terms;
@@ -73,6 +76,7 @@ struct TcArgs {
     int* flags;
 };
 
+constexpr int kBarBytes = 384;
 // An operand A of the low form holds all terms: up to four blocks of 64 columns.
 constexpr int kLowBlocks = 4;
 
@@ -86,7 +90,7 @@ struct Cfg {
     static constexpr int kOutBytes = kEpiWarps * 32 * 32 * 2;   // a 32 x 32 bf16 block per epilogue warp
     static constexpr int kBiasBytes = kEpiWarps * (BN / 2) * 4;   // a warp's half of the tile's biases
     static constexpr int kGroupBytes = (3 * BP_MAX_EXPERTS + 32) * 4;
-    static constexpr int kSmemBytes = 1024 + kRingBytes + kOutBytes + kBiasBytes + kGroupBytes + 256;
+    static constexpr int kSmemBytes = 1024 + kRingBytes + kOutBytes + kBiasBytes + kGroupBytes + kBarBytes;
 };
 
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, int c0, int c1, int c2, uint64_t* bar) {
@@ -96,11 +100,16 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
         "l"((unsigned long long)map), "r"(c0), "r"(c1), "r"(c2), "r"(smem_u32(bar))
         : "memory");
 }
+// Products that the low form takes for all terms: 128 of their columns each.
+__device__ __forceinline__ int low_sets(const TcArgs& g) { return (g.n_terms * g.stride + BM - 1) / BM; }
+
 // A tile: rows [row0, end) of a forward or back product, of group g; of a change, all rows of the
 // group and the block mb of M.
 struct Item {
     int g, row0, end, mb, nb;
     int kbs;        // K blocks
+    int kb0, kb1;   // of the low form: of the adapter's
+    int run;
     int adapter;    // whose low-rank K follows; of an up product, the rows'; -1, or a kind of tile
     int request;    // the tile's first
 };
@@ -124,23 +133,23 @@ struct TileRequests {
     }
 };
 
-// The runs of rows that a change sums over: the group's, or of the low form the requests of adapter
-// w.g in order, which the whole warp looks for.
+// The stretches of rows that a change sums over, K blocks kb0 to kb1 of them: the group's, or of the
+// low form those of the requests of adapter w.g in order, which the whole warp looks for.
+struct RequestTable {   // of the requests, in shared memory; adapter NULL: too many, read where they are
+    const int *adapter, *lo, *hi;
+};
 template <int FORM>
-struct Runs {
+struct Stretches {
     const TcArgs& g;
     const Item& w;
-    int at;
-    __device__ bool next(int& lo, int& hi) {
-        if (FORM != LOW) {
-            lo = w.row0;
-            hi = w.end;
-            return at++ == 0 && hi > lo;
-        }
+    const RequestTable& table;
+    int at, seen;   // next request; K blocks before it
+    __device__ bool request(int& lo, int& hi) {
         const int lane = threadIdx.x & 31;
+        const int* adapter = table.adapter != nullptr ? table.adapter : g.req.adapter;
         while (at < g.req.n_requests) {
             const int base = at & ~31, i = base + lane;
-            const bool mine = i >= at && i < g.req.n_requests && g.req.adapter[i] == w.g;
+            const bool mine = i >= at && i < g.req.n_requests && adapter[i] == w.g;
             const unsigned m = __ballot_sync(0xffffffffu, mine);
             if (m == 0) {
                 at = base + 32;
@@ -148,10 +157,28 @@ struct Runs {
             }
             const int r = base + __ffs(m) - 1;
             at = r + 1;
-            group_rows(g.req.offsets, g.req.n_rows, r, lo, hi, g.flags);
+            if (table.adapter != nullptr) lo = table.lo[r], hi = table.hi[r];
+            else group_rows(g.req.offsets, g.req.n_rows, r, lo, hi, g.flags);
             if (hi > lo) return true;
         }
         return false;
+    }
+    __device__ bool next(int& lo, int& hi) {
+        if constexpr (FORM != LOW) {
+            lo = w.row0;
+            hi = w.end;
+            return at++ == 0 && hi > lo;
+        } else {
+            while (seen < w.kb1 && request(lo, hi)) {
+                const int blocks = (hi - lo + BK - 1) / BK, s = max(w.kb0 - seen, 0), e = min(w.kb1 - seen, blocks);
+                seen += blocks;
+                if (s >= e) continue;
+                hi = min(hi, lo + e * BK);
+                lo += s * BK;
+                return true;
+            }
+            return false;
+        }
     }
 };
 
@@ -170,21 +197,27 @@ template <int FORM>
 struct Schedule {
     const TcArgs& g;
     const int *lo, *hi, *tile0;   // per group, in shared memory: first row, end; first row block (n_groups + 1)
+    const RequestTable table;
     __device__ int items() const {
-        if (FORM == LOW) return g.req.n_adapters * g.num_n;
+        if (FORM == LOW) return g.req.n_adapters * g.num_n * g.runs;
         if (FORM == UP) return g.max_items;
         return FORM == CHANGE ? g.groups.n_groups * g.num_m * g.num_n : tile0[g.groups.n_groups] * g.num_n;
     }
     __device__ Item item(int it) const {
         Item w;
         if (FORM == LOW) {
-            w.g = it / g.num_n;
-            w.nb = it - w.g * g.num_n;
-            w.mb = w.row0 = w.end = w.kbs = 0;
+            const int tile = it / g.runs;
+            w.run = it - tile * g.runs;
+            w.g = tile / g.num_n;
+            w.nb = tile - w.g * g.num_n;
+            w.mb = w.row0 = w.end = 0;
             w.adapter = w.request = -1;
-            Runs<LOW> runs{g, w, 0};
-            int lo, hi;
-            while (runs.next(lo, hi)) w.kbs += (hi - lo + BK - 1) / BK;
+            Stretches<LOW> all{g, w, table, 0, 0};
+            int lo, hi, blocks = 0;
+            while (all.request(lo, hi)) blocks += (hi - lo + BK - 1) / BK;
+            w.kb0 = (int)((long long)blocks * w.run / g.runs);
+            w.kb1 = (int)((long long)blocks * (w.run + 1) / g.runs);
+            w.kbs = w.kb1 - w.kb0;
             return w;
         }
         if (FORM == UP) {   // (the whole warp asks)
@@ -282,6 +315,16 @@ __device__ __forceinline__ void store_change(float* G, int M, int N, int m0, int
     __syncwarp();   // the block may be rewritten
 }
 
+// The same straight from a lane's row, a sector (32 bytes, and so aligned) an instruction.
+__device__ __forceinline__ void store_sectors(float* p, const float (&v)[16], int cols) {
+#pragma unroll
+    for (int c = 0; c < 16; c += 8)
+        if (c < cols)   // cols is a multiple of 8
+            asm volatile("st.global.L1::no_allocate.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + c), "f"(v[c]),
+                         "f"(v[c + 1]), "f"(v[c + 2]), "f"(v[c + 3]), "f"(v[c + 4]), "f"(v[c + 5]), "f"(v[c + 6]), "f"(v[c + 7])
+                         : "memory");
+}
+
 // The same for 16 columns of low [n_rows, rank], rows below `end`; in 16-byte pieces if they are whole.
 __device__ __forceinline__ void store_low(float* low, int rank, int row0, int end, int j0, const float (&v)[16], int wide,
                                           float4* sF) {
@@ -365,9 +408,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint64_t* tfull = empty + S;
     uint64_t* tempty = tfull + kAcc;
     uint64_t* drain = tempty + kAcc;   // used only when a wait ran out
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain + 1);
+    uint64_t* xfull = drain + 1;       // of the low form: a warp's block of sums is there for another one; is read
+    uint64_t* xempty = xfull + kEpiWarps;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(xempty + kEpiWarps);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    static_assert((2 * S + 2 * kAcc + 1) * 8 + 8 <= 256, "room for the barriers");
+    static_assert((2 * S + 2 * kAcc + 1 + 2 * kEpiWarps) * 8 + 8 <= kBarBytes, "room for the barriers");
 
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     pdl_launch();
@@ -381,6 +426,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             mbar_init(&tempty[a], kEpiThreads);
         }
         mbar_init(drain, 1);
+        for (int e = 0; e < kEpiWarps; ++e) {
+            mbar_init(&xfull[e], 32);
+            mbar_init(&xempty[e], 32);
+        }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_map(&map_a);
@@ -393,7 +442,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     pdl_wait();   // every thread, before its first access to what earlier kernels wrote or still read
-    if (warp == 2) {
+    if (FORM == LOW) {
+        if (g.req.n_requests <= BP_MAX_EXPERTS)   // the table of requests
+            for (int i = threadIdx.x; i < g.req.n_requests; i += kThreads) {
+                int lo, hi;
+                group_rows(g.req.offsets, g.req.n_rows, i, lo, hi, g.flags);
+                s_lo[i] = lo;
+                s_hi[i] = hi;
+                s_tile0[i] = g.req.adapter[i];
+            }
+    } else if (warp == 2) {
         // the groups' rows and first row blocks
         int carry = 0;
         for (int base = 0; base < g.groups.n_groups; base += 32) {
@@ -429,7 +487,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (blockIdx.x == 0) zero_outside(g.req, threadIdx.x - 64, kEpiThreads, g.low_out, g.terms, g.n_terms * g.stride);
         __syncwarp();
     }
-    const Schedule<FORM> plan{g, s_lo, s_hi, s_tile0};
+    const bool kept = FORM == LOW && g.req.n_requests <= BP_MAX_EXPERTS;
+    const Schedule<FORM> plan{g, s_lo, s_hi, s_tile0, {kept ? s_tile0 : nullptr, s_lo, s_hi}};
     const int items = plan.items();
 
     if (warp == 0) {
@@ -452,13 +511,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ++issued;
                 if (++stage == S) { stage = 0; phase ^= 1u; }
             };
-            const int a_blocks = FORM == LOW ? g.n_terms * (g.stride / 64) : BM / 64;
+            const int a_blocks = FORM == LOW ? 2 * low_sets(g) : BM / 64;
             for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
                 const Item w = plan.item(it);
                 if constexpr (kChange) {
-                    Runs<FORM> runs{g, w, 0};
+                    Stretches<FORM> rows{g, w, plan.table, 0, 0};
                     int lo, hi;
-                    while (ok && runs.next(lo, hi)) {
+                    while (ok && rows.next(lo, hi)) {
                         for (int r = lo; r < hi; r += BK) {
                             if (!open(a_blocks * kMnBlockBytes + C::kBBytes)) break;
                             uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
@@ -549,11 +608,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
                 const Item w = plan.item(it);
                 if constexpr (kChange) {
-                    const int terms = FORM == LOW ? g.n_terms : 1;
-                    const uint32_t term_step = FORM == LOW ? (uint32_t)(g.stride / 64) * (kMnBlockBytes >> 4) : 0u;
-                    Runs<FORM> runs{g, w, 0};
+                    const int sets = FORM == LOW ? low_sets(g) : 1;   // of 128 rows of M
+                    Stretches<FORM> rows{g, w, plan.table, 0, 0};
                     int lo, hi, kb = 0;
-                    while (ok && runs.next(lo, hi)) {
+                    while (ok && rows.next(lo, hi)) {
                         for (int r = lo; r < hi; r += BK, ++kb) {
                             if (kb % kChainBlocks == 0 && !wait(&tempty[acc], acc_phase ^ 1u)) break;
                             if (!wait(&full[stage], phase)) break;
@@ -564,17 +622,17 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (valid < BK) {   // (uniform) the run's last rows
                                 steps = (valid + UMMA_K - 1) / UMMA_K;
                                 uint8_t* sa = ring + stage * C::kStageBytes;
-                                zero_rows(sa, terms * (FORM == LOW ? g.stride : BM) / 64, valid, steps * UMMA_K);
+                                zero_rows(sa, 2 * sets, valid, steps * UMMA_K);
                                 zero_rows(sa + C::kABytes, BN / 64, valid, steps * UMMA_K);
                                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                                 __syncwarp();
                             }
                             if (leader) {
-                                for (int t = 0; t < terms; ++t)
+                                for (int t = 0; t < sets; ++t)
 #pragma unroll
                                     for (int kk = 0; kk < BK / UMMA_K; ++kk)
                                         if (kk < steps)
-                                            umma_bf16<idesc>(tmem_d, al + t * term_step + kk * k_step_units<kAMn>(),
+                                            umma_bf16<idesc>(tmem_d, al + t * (2 * kMnBlockBytes >> 4) + kk * k_step_units<kAMn>(),
                                                              bl + kk * k_step_units<kBMn>(), kb % kChainBlocks != 0 || t > 0 || kk > 0 ? 1u : 0u);
                             }
                             close();
@@ -644,7 +702,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t trow = tmem_base + ((uint32_t)(q * 32) << 16);
         uint4* sS4 = reinterpret_cast<uint4*>(stage_out + ew * 1024);
         int acc = 0;
-        unsigned acc_phase = 0;
+        unsigned acc_phase = 0, xphase = 0;
+        // the warp of this one's half of the columns that has row quarter `quarter`
+        auto half_warp = [&](int quarter) { return (ew & 4) + ((quarter + 2) & 3); };
         auto wait_acc = [&] {
             const bool got = mbar_wait(&tfull[acc], acc_phase, abort_flag, g.flags);
             const bool leave = __any_sync(0xffffffffu, !got);
@@ -696,6 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int t = 0; t < g.n_terms; ++t) {
 #pragma unroll
                         for (int c = 0; c < BN / 2; c += 32) {
+                            if (cbeg + c >= g.stride) break;
                             float v[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) {   // part keeps what the terms so far leave
@@ -709,9 +770,95 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     continue;
                 }
+                if (FORM == LOW && g.stride < BM) {
+                    // row quarters past the first term's: the same ranks of other terms, passed on to it
+                    const int own = g.stride / 32, last = min(4, own * g.n_terms);
+                    float* block = reinterpret_cast<float*>(stage_out);   // [warp][16][32]
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 16) {
+                        if (q >= own) {
+                            if (q < last) {
+                                stay = mbar_wait(&xempty[ew], xphase ^ 1u, abort_flag, g.flags);
+                                stay = !__any_sync(0xffffffffu, !stay);
+                                if (!stay) break;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) block[ew * 512 + i * 32 + lane] = part[c + i];
+                                mbar_arrive(&xfull[ew]);
+                            }
+                        } else {
+                            for (int from = q + own; from < last; from += own) {
+                                const int src = half_warp(from);
+                                stay = mbar_wait(&xfull[src], xphase, abort_flag, g.flags);
+                                stay = !__any_sync(0xffffffffu, !stay);
+                                if (!stay) break;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) part[c + i] += block[src * 512 + i * 32 + lane];
+                                mbar_arrive(&xempty[src]);
+                            }
+                            if (!stay) break;
+                        }
+                        xphase ^= 1u;
+                    }
+                    if (!stay) break;
+                    __syncwarp();
+                    if (q >= own) continue;
+                }
                 const float scale = FORM == LOW && g.scale != nullptr ? g.scale[w.g] : 1.f;
                 const int m0 = w.mb * BM + q * 32;
                 float* G = g.G + (size_t)w.g * g.M * g.N;
+                if (FORM == LOW && g.runs > 1) {
+                    // the run's sums to scratch; the last warp to arrive adds the runs' in their order
+                    if (m0 >= g.M || w.nb * BN + cbeg >= g.N) continue;
+                    const size_t plane = (size_t)g.req.n_adapters * g.M * g.N;
+                    float* mine = g.scratch + w.run * plane + (size_t)w.g * g.M * g.N;
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 16) {
+                        const int n0 = w.nb * BN + cbeg + c;
+                        if (n0 >= g.N) break;
+                        float v[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] = part[c + i];
+                        store_change(mine, g.M, g.N, m0, n0, v, 0, reinterpret_cast<float4*>(sS4));
+                    }
+                    __threadfence();
+                    __syncwarp();
+                    unsigned before = 0;
+                    unsigned* count = g.arrived + ((size_t)w.g * g.num_n + w.nb) * kEpiWarps + ew;
+                    if (lane == 0) before = atomicAdd(count, 1u);
+                    before = __shfl_sync(0xffffffffu, before, 0);
+                    if (before != (unsigned)g.runs - 1) continue;
+                    if (lane == 0) *count = 0u;
+                    __threadfence();
+                    const float* all = g.scratch + (size_t)w.g * g.M * g.N;
+                    // pieces of four columns: lane + 32 i of the part's, by rows; all loads of a run under way at once
+                    constexpr int kPer = BN / 2 / 4;   // of a row
+                    float4 sum[kPer];
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    // rows and columns past the last ones read the last ones, so that no load hangs on a condition
+                    const float* at = all + (size_t)min(m0 + lane / kPer, g.M - 1) * g.N + min(w.nb * BN + cbeg + lane % kPer * 4, g.N - 4);
+                    for (int z = 0; z < g.runs; ++z) {
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i) {
+                            const int row = min(32 / kPer * i, max(g.M - 1 - m0 - lane / kPer, 0));
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(at + z * plane + (size_t)row * g.N));
+                            sum[i].x += x.x, sum[i].y += x.y, sum[i].z += x.z, sum[i].w += x.w;
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) {
+                        const int m = m0 + (lane + 32 * i) / kPer, n = w.nb * BN + cbeg + (lane + 32 * i) % kPer * 4;
+                        if (m >= g.M || n >= g.N) continue;
+                        float4 o = make_float4(scale * sum[i].x, scale * sum[i].y, scale * sum[i].z, scale * sum[i].w);
+                        float4* to = reinterpret_cast<float4*>(G + (size_t)m * g.N + n);
+                        if (g.accumulate) {
+                            const float4 old = *to;
+                            o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
+                        }
+                        *to = o;
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (int c = 0; c < BN / 2; c += 16) {
                     const int n0 = w.nb * BN + cbeg + c;
@@ -719,7 +866,11 @@ __global__ void __launch_bounds__(kThreads, 1)
                     float v[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = scale * part[c + i];
-                    store_change(G, g.M, g.N, m0, n0, v, g.accumulate, reinterpret_cast<float4*>(sS4));
+                    if (g.sectors && !g.accumulate) {
+                        if (m0 + lane < g.M) store_sectors(G + (size_t)(m0 + lane) * g.N + n0, v, g.N - n0);
+                    } else {
+                        store_change(G, g.M, g.N, m0, n0, v, g.accumulate, reinterpret_cast<float4*>(sS4));
+                    }
                 }
             } else {
                 const int m0 = w.row0 + q * 32, row = m0 + lane;
@@ -887,6 +1038,10 @@ cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtens
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
+struct LowCut {
+    int bn, num_n, runs;
+};
+
 // Tile width for row_tiles blocks of 128 rows: the time of the waves of tiles, at the clocks that
 // a K block of 64 takes with every SM busy (530, 330 and 230 for 256, 128 and 64 columns: each SM
 // reads A again for every column block) and an epilogue of 800 + 900 a 64 columns, whichever is
@@ -988,6 +1143,7 @@ cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
     a.N = c.N;
     a.G = c.G;
     a.accumulate = c.accumulate;
+    a.sectors = ((uintptr_t)c.G & 31) == 0;
     a.flags = c.flags;
     a.num_m = ceil_div(c.M, BM);
     const int E = c.groups.n_groups;
@@ -1020,7 +1176,7 @@ cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
     a.tiles = l.tiles;
     a.flags = l.flags;
     a.max_items = max_tiles(l.req.n_rows, l.req.n_requests, BM);
-    const int bn = l.req.rank <= 64 ? 64 : 128;   // = the terms' stride: the tile writes them in full
+    const int bn = l.req.rank <= 64 ? 64 : 128;   // at least the terms' stride: the tile writes them in full
     CUtensorMap m[4];
     if (!make_map(&m[0], l.in, l.req.n_rows, l.K, 0, BM) || !make_map(&m[1], l.P, l.req.rank, l.K, l.req.n_adapters, bn))
         return cudaErrorInvalidValue;
@@ -1028,8 +1184,26 @@ cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
     return launch<UP>(a, bn, a.max_items < num_sms ? a.max_items : num_sms, num_sms, m, s);
 }
 
-// A CTA sums all rows of an adapter for a block of columns: 64 wide, so that a few adapters keep
-// the SMs busy, 128 where that many blocks do too (half the reads of low).
+// How the low change is cut: 128 columns, 64 where that leaves SMs without a tile, and shares of an
+// adapter's rows while the SMs are more than the tiles twice over.  More shares than that cost more than
+// they balance: each is an exchange, a store and a fence of 5 us beside its 0.5 us a K block (us, both
+// changes of a layer of 16,384 rows, 1 / 2 / 4 / 16 shares: 5 adapters of rank 64 of 4096-4096, 160 tiles,
+// 142 / 194 / 295 / 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of 512-512, 32 tiles, 206 /
+// 118 / 75 / 63).
+static LowCut low_cut(int n_adapters, int n_requests, int N, int num_sms) {
+    const int busy = n_adapters < n_requests ? n_adapters : n_requests;
+    LowCut c;
+    c.bn = (long long)busy * ceil_div(N, 128) >= num_sms / 4 ? 128 : 64;
+    c.num_n = ceil_div(N, c.bn);
+    c.runs = 1;
+    while ((long long)n_adapters * c.num_n * c.runs * 2 <= num_sms) c.runs *= 2;
+    return c;
+}
+
+// Of any call of a layer.
+size_t low_change_scratch(int rank, int num_sms) { return (size_t)num_sms * 128 * rank; }
+size_t low_change_counts(int num_sms) { return (size_t)num_sms * kEpiWarps; }
+
 cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, int num_sms, cudaStream_t s) {
     TcArgs a{};
     a.req = c.req;
@@ -1038,20 +1212,23 @@ cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, int num_s
     a.G = c.G;
     a.scale = c.scale;
     a.accumulate = c.accumulate;
+    a.sectors = ((uintptr_t)c.G & 31) == 0;
     a.n_terms = low.n_terms;
     a.stride = low.stride;
     a.flags = c.flags;
-    const int n_ad = c.req.n_adapters, busy = n_ad < c.req.n_requests ? n_ad : c.req.n_requests;
-    const int bn = (long long)busy * ceil_div(c.N, 128) >= num_sms ? 128 : 64;
-    a.num_n = ceil_div(c.N, bn);
+    const LowCut cut = low_cut(c.req.n_adapters, c.req.n_requests, c.N, num_sms);
+    a.num_n = cut.num_n;
+    a.runs = cut.runs;
+    a.scratch = c.scratch;
+    a.arrived = c.arrived;
     CUtensorMap m[4];
     const bool rows = c.req.n_rows > 0;   // (tc_change)
     if (!make_map(&m[0], rows ? low.terms : c.G, rows ? c.req.n_rows : 1, low.n_terms * low.stride, 0, BK) ||
         !make_map(&m[1], rows ? c.b : c.G, rows ? c.req.n_rows : 1, c.N, 0, BK))
         return cudaErrorInvalidValue;
     m[2] = m[3] = m[0];
-    const long long items = (long long)n_ad * a.num_n;
-    return launch<LOW>(a, bn, items < num_sms ? (int)items : num_sms, num_sms, m, s);
+    const long long items = (long long)c.req.n_adapters * a.num_n * a.runs;
+    return launch<LOW>(a, cut.bn, items < num_sms ? (int)items : num_sms, num_sms, m, s);
 }
 
 }  // namespace bp
