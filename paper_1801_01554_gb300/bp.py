@@ -299,34 +299,50 @@ def bp_last_error() -> str:
 
 
 # ------------------------------------------------- C names of include/bp_experts.h
-def _typed(x, dtype, what):
-    """Device address as _dptr, of a tensor whose element type is checked: the kernels read
-    raw memory, and an int64 index or a float64 gate would be read as something else."""
-    if x is None or isinstance(x, int):
+# Each call's tensors are checked for their element type (the kernels read raw memory: an int64
+# index or a float64 gate would be read as something else) and for room for what the call reads or
+# writes there, where the layer's sizes are known (`room`: values needed, from the classes below).
+_dtypes = None
+
+
+def _torch_types():
+    """(float32, bfloat16, int32) of torch, looked up once: bp itself imports without torch."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+
+        _dtypes = (torch.float32, torch.bfloat16, torch.int32)
+    return _dtypes
+
+
+def _typed(x, kind, what, n=0):
+    """Device address of a tensor of element type `kind` (an index of _torch_types) with n values."""
+    if x is None or type(x) is int:
         return x
-    name = str(x.dtype)
-    if name != dtype:
-        raise ValueError(f"{what} must be {dtype} (got {name})")
-    return _dptr(x)
+    if x.dtype is not _torch_types()[kind]:
+        raise ValueError(f"{what} must be {_torch_types()[kind]} (got {x.dtype})")
+    if x.numel() < n:
+        raise ValueError(f"{what} holds {x.numel()} values; the call needs {n}")
+    if not x.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    if not x.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
+    return x.data_ptr()
 
 
-def _room(**needed):
-    """Refuses tensors that are shorter than what the kernels read or write there."""
-    for what, (x, n) in needed.items():
-        if x is not None and not isinstance(x, int) and x.numel() < n:
-            raise ValueError(f"{what} holds {x.numel()} values; the call needs {n}")
+def _values(x, dtype, what, n=0):
+    return _typed(x, 1 if dtype == BP_BF16 else 0, what, n)
 
 
-def _values(x, dtype, what):
-    return _typed(x, "torch.bfloat16" if dtype == BP_BF16 else "torch.float32", what)
+def _ints(x, what, n=0):
+    return _typed(x, 2, what, n)
 
 
-def _ints(x, what):
-    return _typed(x, "torch.int32", what)
+def _floats(x, what, n=0):
+    return _typed(x, 0, what, n)
 
 
-def _floats(x, what):
-    return _typed(x, "torch.float32", what)
+_NO_ROOM = (0,) * 12
 
 
 def bp_router_create(n_experts, k, dtype=BP_F32, max_patterns=1024, gates=BP_GATES_CHOSEN):
@@ -340,31 +356,30 @@ def bp_router_destroy(h):
     load().bp_router_destroy(h)
 
 
-def bp_route(h, logits, n, expert, gate, offsets, source, place, dtype=BP_F32, stream=None):
-    _check(load().bp_route(h, _values(logits, dtype, "logits"), int(n), _ints(expert, "expert"),
-                           _floats(gate, "gate"), _ints(offsets, "offsets"), _ints(source, "source"),
-                           _ints(place, "place"), _stream(stream)))
+def bp_route(h, logits, n, expert, gate, offsets, source, place, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_route(h, _values(logits, dtype, "logits", room[0]), n, _ints(expert, "expert", room[1]),
+                           _floats(gate, "gate", room[1]), _ints(offsets, "offsets", room[2]),
+                           _ints(source, "source", room[1]), _ints(place, "place", room[1]), _stream(stream)))
 
 
-def bp_route_backward(h, logits, n, expert, gate, dgate, dlogits, dtype=BP_F32, stream=None):
-    _check(load().bp_route_backward(h, _values(logits, dtype, "logits"), int(n), _ints(expert, "expert"),
-                                    _floats(gate, "gate"), _floats(dgate, "dgate"),
-                                    _values(dlogits, dtype, "dlogits"), _stream(stream)))
+def bp_route_backward(h, logits, n, expert, gate, dgate, dlogits, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_route_backward(h, _values(logits, dtype, "logits", room[0]), n,
+                                    _ints(expert, "expert", room[1]), _floats(gate, "gate", room[1]),
+                                    _floats(dgate, "dgate", room[1]), _values(dlogits, dtype, "dlogits", room[0]),
+                                    _stream(stream)))
 
 
 def bp_mix(H, n_rows, place, gate, n, k, n_out, dtype, Y, stream=None):
-    _room(H=(H, n_rows * n_out), place=(place, n * k), gate=(gate, n * k), Y=(Y, n * n_out))
-    _check(load().bp_mix(_values(H, dtype, "H"), int(n_rows), _ints(place, "place"), _floats(gate, "gate"),
-                         int(n), int(k), int(n_out), int(dtype), _values(Y, dtype, "Y"), _stream(stream)))
+    _check(load().bp_mix(_values(H, dtype, "H", n_rows * n_out), n_rows, _ints(place, "place", n * k),
+                         _floats(gate, "gate", n * k), n, k, n_out, dtype, _values(Y, dtype, "Y", n * n_out),
+                         _stream(stream)))
 
 
 def bp_mix_backward(D, H, n_rows, place, gate, n, k, n_out, dtype, dH, dgate=None, stream=None):
-    _room(D=(D, n * n_out), H=(H, n_rows * n_out), place=(place, n * k), gate=(gate, n * k),
-          dH=(dH, n_rows * n_out), dgate=(dgate, n * k))
-    _check(load().bp_mix_backward(_values(D, dtype, "D"), _values(H, dtype, "H"), int(n_rows),
-                                  _ints(place, "place"), _floats(gate, "gate"), int(n), int(k), int(n_out),
-                                  int(dtype), _values(dH, dtype, "dH"), _floats(dgate, "dgate"),
-                                  _stream(stream)))
+    _check(load().bp_mix_backward(_values(D, dtype, "D", n * n_out), _values(H, dtype, "H", n_rows * n_out),
+                                  n_rows, _ints(place, "place", n * k), _floats(gate, "gate", n * k), n, k,
+                                  n_out, dtype, _values(dH, dtype, "dH", n_rows * n_out),
+                                  _floats(dgate, "dgate", n * k), _stream(stream)))
 
 
 def bp_experts_create(n_experts, n_in, n_out, dtype=BP_F32, max_rows=1024):
@@ -378,19 +393,21 @@ def bp_experts_destroy(h):
     load().bp_experts_destroy(h)
 
 
-def bp_experts_forward(h, W, b, X, n_x, source, offsets, n_rows, Y, squash=False, dtype=BP_F32, stream=None):
-    _check(load().bp_experts_forward(h, _values(W, dtype, "W"), _floats(b, "b"), _values(X, dtype, "X"),
-                                     int(n_x), _ints(source, "source"), _ints(offsets, "offsets"),
-                                     int(n_rows), int(bool(squash)), _values(Y, dtype, "Y"), _stream(stream)))
+def bp_experts_forward(h, W, b, X, n_x, source, offsets, n_rows, Y, squash=False, dtype=BP_F32, stream=None,
+                       room=_NO_ROOM):
+    _check(load().bp_experts_forward(h, _values(W, dtype, "W", room[0]), _floats(b, "b", room[1]),
+                                     _values(X, dtype, "X", room[2]), n_x, _ints(source, "source", room[3]),
+                                     _ints(offsets, "offsets", room[4]), n_rows, 1 if squash else 0,
+                                     _values(Y, dtype, "Y", room[5]), _stream(stream)))
 
 
 def bp_experts_backward(h, W, X, n_x, source, offsets, n_rows, D, dX=None, GW=None, Gb=None, squash=False,
-                        accumulate=False, dtype=BP_F32, stream=None):
-    _check(load().bp_experts_backward(h, _values(W, dtype, "W"), _values(X, dtype, "X"), int(n_x),
-                                      _ints(source, "source"), _ints(offsets, "offsets"), int(n_rows),
-                                      _values(D, dtype, "D"), int(bool(squash)), _values(dX, dtype, "dX"),
-                                      _floats(GW, "GW"), _floats(Gb, "Gb"), int(bool(accumulate)),
-                                      _stream(stream)))
+                        accumulate=False, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_experts_backward(h, _values(W, dtype, "W", room[0]), _values(X, dtype, "X", room[2]), n_x,
+                                      _ints(source, "source", room[3]), _ints(offsets, "offsets", room[4]),
+                                      n_rows, _values(D, dtype, "D", room[5]), 1 if squash else 0,
+                                      _values(dX, dtype, "dX", room[6]), _floats(GW, "GW", room[0]),
+                                      _floats(Gb, "Gb", room[1]), 1 if accumulate else 0, _stream(stream)))
 
 
 def bp_experts_check(h, stream=None):
@@ -409,23 +426,24 @@ def bp_adapters_destroy(h):
 
 
 def bp_adapters_forward(h, W, b, A, B, scale, X, offsets, adapter, n_requests, n_rows, U, Y, squash=False,
-                        dtype=BP_F32, stream=None):
-    _check(load().bp_adapters_forward(h, _values(W, dtype, "W"), _floats(b, "b"), _values(A, dtype, "A"),
-                                      _values(B, dtype, "B"), _floats(scale, "scale"), _values(X, dtype, "X"),
-                                      _ints(offsets, "offsets"), _ints(adapter, "adapter"), int(n_requests),
-                                      int(n_rows), int(bool(squash)), _floats(U, "U"), _values(Y, dtype, "Y"),
-                                      _stream(stream)))
+                        dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_adapters_forward(h, _values(W, dtype, "W", room[0]), _floats(b, "b", room[1]),
+                                      _values(A, dtype, "A", room[2]), _values(B, dtype, "B", room[3]),
+                                      _floats(scale, "scale", room[4]), _values(X, dtype, "X", room[5]),
+                                      _ints(offsets, "offsets", room[6]), _ints(adapter, "adapter", room[7]),
+                                      n_requests, n_rows, 1 if squash else 0, _floats(U, "U", room[8]),
+                                      _values(Y, dtype, "Y", room[9]), _stream(stream)))
 
 
 def bp_adapters_backward(h, W, A, B, scale, X, U, offsets, adapter, n_requests, n_rows, D, dX=None, GA=None,
-                         GB=None, squash=False, accumulate=False, dtype=BP_F32, stream=None):
-    _check(load().bp_adapters_backward(h, _values(W, dtype, "W"), _values(A, dtype, "A"),
-                                       _values(B, dtype, "B"), _floats(scale, "scale"),
-                                       _values(X, dtype, "X"), _floats(U, "U"), _ints(offsets, "offsets"),
-                                       _ints(adapter, "adapter"), int(n_requests), int(n_rows),
-                                       _values(D, dtype, "D"), int(bool(squash)), _values(dX, dtype, "dX"),
-                                       _floats(GA, "GA"), _floats(GB, "GB"), int(bool(accumulate)),
-                                       _stream(stream)))
+                         GB=None, squash=False, accumulate=False, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_adapters_backward(h, _values(W, dtype, "W", room[0]), _values(A, dtype, "A", room[2]),
+                                       _values(B, dtype, "B", room[3]), _floats(scale, "scale", room[4]),
+                                       _values(X, dtype, "X", room[5]), _floats(U, "U", room[8]),
+                                       _ints(offsets, "offsets", room[6]), _ints(adapter, "adapter", room[7]),
+                                       n_requests, n_rows, _values(D, dtype, "D", room[9]), 1 if squash else 0,
+                                       _values(dX, dtype, "dX", room[5]), _floats(GA, "GA", room[2]),
+                                       _floats(GB, "GB", room[3]), 1 if accumulate else 0, _stream(stream)))
 
 
 def bp_adapters_check(h, stream=None):
@@ -466,14 +484,12 @@ class Router(_Handle):
         self.h = bp_router_create(n_experts, k, dtype, max_patterns, gates)
 
     def forward(self, logits, n, expert, gate, offsets, source, place, stream=None):
-        _room(logits=(logits, n * self.n_experts), expert=(expert, n * self.k), gate=(gate, n * self.k),
-              offsets=(offsets, self.n_experts + 1), source=(source, n * self.k), place=(place, n * self.k))
-        bp_route(self.h, logits, n, expert, gate, offsets, source, place, self.dtype, stream)
+        bp_route(self.h, logits, n, expert, gate, offsets, source, place, self.dtype, stream,
+                 (n * self.n_experts, n * self.k, self.n_experts + 1))
 
     def backward(self, logits, n, expert, gate, dgate, dlogits, stream=None):
-        _room(logits=(logits, n * self.n_experts), expert=(expert, n * self.k), gate=(gate, n * self.k),
-              dgate=(dgate, n * self.k), dlogits=(dlogits, n * self.n_experts))
-        bp_route_backward(self.h, logits, n, expert, gate, dgate, dlogits, self.dtype, stream)
+        bp_route_backward(self.h, logits, n, expert, gate, dgate, dlogits, self.dtype, stream,
+                          (n * self.n_experts, n * self.k))
 
 
 class Experts(_Handle):
@@ -485,19 +501,18 @@ class Experts(_Handle):
         self.n_experts, self.n_in, self.n_out, self.dtype = int(n_experts), int(n_in), int(n_out), dtype
         self.h = bp_experts_create(n_experts, n_in, n_out, dtype, max_rows)
 
-    def forward(self, W, b, X, n_x, source, offsets, n_rows, Y, squash=False, stream=None):
+    def _room(self, n_x, n_rows):
         E, i, o = self.n_experts, self.n_in, self.n_out
-        _room(W=(W, E * o * i), b=(b, E * o), X=(X, n_x * i), source=(source, n_rows), offsets=(offsets, E + 1),
-              Y=(Y, n_rows * o))
-        bp_experts_forward(self.h, W, b, X, n_x, source, offsets, n_rows, Y, squash, self.dtype, stream)
+        return E * o * i, E * o, n_x * i, n_rows, E + 1, n_rows * o, n_rows * i
+
+    def forward(self, W, b, X, n_x, source, offsets, n_rows, Y, squash=False, stream=None):
+        bp_experts_forward(self.h, W, b, X, n_x, source, offsets, n_rows, Y, squash, self.dtype, stream,
+                           self._room(n_x, n_rows))
 
     def backward(self, W, X, n_x, source, offsets, n_rows, D, dX=None, GW=None, Gb=None, squash=False,
                  accumulate=False, stream=None):
-        E, i, o = self.n_experts, self.n_in, self.n_out
-        _room(W=(W, E * o * i), X=(X, n_x * i), source=(source, n_rows), offsets=(offsets, E + 1),
-              D=(D, n_rows * o), dX=(dX, n_rows * i), GW=(GW, E * o * i), Gb=(Gb, E * o))
         bp_experts_backward(self.h, W, X, n_x, source, offsets, n_rows, D, dX, GW, Gb, squash, accumulate,
-                            self.dtype, stream)
+                            self.dtype, stream, self._room(n_x, n_rows))
 
     def check(self, stream=None):
         bp_experts_check(self.h, stream)
@@ -513,23 +528,20 @@ class Adapters(_Handle):
         self.n_in, self.n_out = int(n_in), int(n_out)
         self.h = bp_adapters_create(n_adapters, rank, n_in, n_out, dtype, max_rows, max_requests)
 
+    def _room(self, n_requests, n_rows):
+        a, r, i, o = self.n_adapters, self.rank, self.n_in, self.n_out
+        return (o * i, o, a * r * i, a * r * o, a, n_rows * i, n_requests + 1 if n_requests > 0 else 0,
+                n_requests, n_rows * r, n_rows * o)
+
     def forward(self, W, b, A, B, scale, X, offsets, adapter, n_requests, n_rows, U, Y, squash=False,
                 stream=None):
-        a, r, i, o = self.n_adapters, self.rank, self.n_in, self.n_out
-        _room(W=(W, o * i), b=(b, o), A=(A, a * r * i), B=(B, a * r * o), scale=(scale, a), X=(X, n_rows * i),
-              offsets=(offsets, n_requests + 1), adapter=(adapter, n_requests), U=(U, n_rows * r),
-              Y=(Y, n_rows * o))
         bp_adapters_forward(self.h, W, b, A, B, scale, X, offsets, adapter, n_requests, n_rows, U, Y, squash,
-                            self.dtype, stream)
+                            self.dtype, stream, self._room(n_requests, n_rows))
 
     def backward(self, W, A, B, scale, X, U, offsets, adapter, n_requests, n_rows, D, dX=None, GA=None,
                  GB=None, squash=False, accumulate=False, stream=None):
-        a, r, i, o = self.n_adapters, self.rank, self.n_in, self.n_out
-        _room(W=(W, o * i), A=(A, a * r * i), B=(B, a * r * o), scale=(scale, a), X=(X, n_rows * i),
-              U=(U, n_rows * r), offsets=(offsets, n_requests + 1), adapter=(adapter, n_requests),
-              D=(D, n_rows * o), dX=(dX, n_rows * i), GA=(GA, a * r * i), GB=(GB, a * r * o))
         bp_adapters_backward(self.h, W, A, B, scale, X, U, offsets, adapter, n_requests, n_rows, D, dX, GA, GB,
-                             squash, accumulate, self.dtype, stream)
+                             squash, accumulate, self.dtype, stream, self._room(n_requests, n_rows))
 
     def check(self, stream=None):
         bp_adapters_check(self.h, stream)

@@ -206,7 +206,7 @@ struct Schedule {
     __device__ Item item(int it) const {
         Item w;
         if (FORM == LOW) {
-            const int tile = it / g.runs;
+            const int tile = g.runs == 1 ? it : it / g.runs;
             w.run = it - tile * g.runs;
             w.g = tile / g.num_n;
             w.nb = tile - w.g * g.num_n;
@@ -215,8 +215,9 @@ struct Schedule {
             Stretches<LOW> all{g, w, table, 0, 0};
             int lo, hi, blocks = 0;
             while (all.request(lo, hi)) blocks += (hi - lo + BK - 1) / BK;
-            w.kb0 = (int)((long long)blocks * w.run / g.runs);
-            w.kb1 = (int)((long long)blocks * (w.run + 1) / g.runs);
+            const int share = blocks / g.runs, more = blocks - share * g.runs;   // the first `more` shares have one more
+            w.kb0 = w.run * share + min(w.run, more);
+            w.kb1 = w.kb0 + share + (w.run < more ? 1 : 0);
             w.kbs = w.kb1 - w.kb0;
             return w;
         }
@@ -770,7 +771,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     continue;
                 }
-                if (FORM == LOW && g.stride < BM) {
+                if (FORM == LOW && g.stride < BM && w.kbs == 0) {
+                    if (q >= g.stride / 32) continue;   // no sums to pass on
+                } else if (FORM == LOW && g.stride < BM) {
                     // row quarters past the first term's: the same ranks of other terms, passed on to it
                     const int own = g.stride / 32, last = min(4, own * g.n_terms);
                     float* block = reinterpret_cast<float*>(stage_out);   // [warp][16][32]

@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kMixThreads) k_mix_backward(MixArgs g) {
     }
     const T *H = (const T*)g.H, *D = (const T*)g.D;
     float mine = 0.f;   // lane j: this warp's part of choice j's product
-    constexpr int C = 4;   // choices that share a read of D
+    constexpr int C = 2;   // choices that share a read of D
     for (int j0 = 0; j0 < g.k; j0 += C) {
         int r[C];
         float w[C], dot[C];
