@@ -12,24 +12,37 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = 32 * kWarps;
 
-// V columns a lane.
-template <class T, int V>
-__device__ __forceinline__ void add_piece(float (&s)[V], const T* p) {
-    if constexpr (sizeof(T) == 2) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
+// V columns a lane: 16 bytes of bfloat16, one float32.  The loads are volatile so that a batch of them is
+// under way before the first is added: ptxas sinks plain ones to their uses.
+template <class T>
+struct Piece;
+template <>
+struct Piece<__nv_bfloat16> {
+    static constexpr int V = 8;
+    uint4 u;
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    }
+    __device__ __forceinline__ void add(float (&s)[V]) const {
         const unsigned w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             s[2 * i] += __uint_as_float(w[i] << 16);
             s[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u);
         }
-    } else {
-        s[0] += *p;
     }
-}
+};
+template <>
+struct Piece<float> {
+    static constexpr int V = 1;
+    float x;
+    __device__ __forceinline__ void load(const float* p) { asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(x) : "l"(p)); }
+    __device__ __forceinline__ void add(float (&s)[V]) const { s[0] += x; }
+};
 
-template <class T, int V>
+template <class T>
 __global__ void __launch_bounds__(kThreads) k_sums(SumsArgs g) {
+    constexpr int V = Piece<T>::V, B = 8;
     __shared__ float part[kWarps][32 * V];
     __shared__ int last;
     const int e = blockIdx.y, runs = gridDim.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -40,8 +53,21 @@ __global__ void __launch_bounds__(kThreads) k_sums(SumsArgs g) {
     float s[V] = {};
     if (n < g.N) {
         const T* d = (const T*)g.d + n;
-#pragma unroll 8
-        for (int r = r0 + warp; r < r1; r += kWarps) add_piece<T, V>(s, d + (size_t)r * g.N);
+        Piece<T> p[B];
+        int r = r0 + warp;
+        for (; r + (B - 1) * kWarps < r1; r += B * kWarps) {
+#pragma unroll
+            for (int i = 0; i < B; ++i) p[i].load(d + (size_t)(r + i * kWarps) * g.N);
+#pragma unroll
+            for (int i = 0; i < B; ++i) p[i].add(s);
+        }
+        if (r < r1) {   // fewer than B left: the last row again in place of those past it
+#pragma unroll
+            for (int i = 0; i < B; ++i) p[i].load(d + (size_t)min(r + i * kWarps, r1 - 1) * g.N);
+#pragma unroll
+            for (int i = 0; i < B; ++i)
+                if (r + i * kWarps < r1) p[i].add(s);
+        }
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) part[warp][lane * V + i] = s[i];
@@ -90,8 +116,8 @@ int sums_runs(int n_rows, int n_groups, int N, int dtype, int num_sms) {
 cudaError_t group_sums(const SumsArgs& a, int dtype, int num_sms, cudaStream_t s) {
     const int cols = 32 * (dtype == BP_F32 ? 1 : 8);
     const dim3 grid((a.N + cols - 1) / cols, a.groups.n_groups, sums_runs(a.groups.n_rows, a.groups.n_groups, a.N, dtype, num_sms));
-    if (dtype == BP_F32) k_sums<float, 1><<<grid, kThreads, 0, s>>>(a);
-    else k_sums<__nv_bfloat16, 8><<<grid, kThreads, 0, s>>>(a);
+    if (dtype == BP_F32) k_sums<float><<<grid, kThreads, 0, s>>>(a);
+    else k_sums<__nv_bfloat16><<<grid, kThreads, 0, s>>>(a);
     return cudaGetLastError();
 }
 
