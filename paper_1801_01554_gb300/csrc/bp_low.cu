@@ -62,20 +62,39 @@ __device__ __forceinline__ void store_terms(bf16* terms, int stride, int n_terms
     }
 }
 
-// What rows of one request hold in low and in the terms, from a sum or from `given`.
-struct Sink {
-    const LowArgs& g;
-    float scale_low, scale_terms;
-    __device__ __forceinline__ void put(int row, int j, float sum) const {
-        const int r = g.req.rank, stride = g.terms_stride;
-        if (j < r) g.low[(size_t)row * r + j] = scale_low * sum;
-        if (j < stride) store_terms((bf16*)g.terms + (size_t)row * g.n_terms * stride + j, stride, g.n_terms, j < r ? scale_terms * sum : 0.f);
+// Rows of one request in low and in the terms, from their sums [rows, pitch] in shared memory (NULL:
+// zeros), by the whole block: eight ranks of a row a thread, a term's in one 16-byte store.  (A value at a
+// time from the registers of the warp that has the sums: 24 us for 66 rows of rank 16, where the sums
+// take 8.)
+__device__ __forceinline__ void store_rows_low(const LowArgs& g, int row0, int rows, const float* sums, int pitch, float scale_low,
+                                               float scale_terms) {
+    const int r = g.req.rank, per = g.n_terms > 0 ? g.terms_stride / 8 : (r + 7) / 8;
+    for (int i = threadIdx.x; i < rows * per; i += kThreads) {
+        const int m = i / per, j0 = i % per * 8;
+        const size_t row = row0 + m;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            v[j] = sums != nullptr && j0 + j < r ? sums[m * pitch + j0 + j] : 0.f;
+            if (j0 + j < r) g.low[row * r + j0 + j] = scale_low * v[j];
+            v[j] *= scale_terms;
+        }
+        for (int t = 0; t < g.n_terms; ++t) {
+            __align__(16) bf16 h[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                h[j] = __float2bfloat16_rn(v[j]);
+                const float f = __bfloat162float(h[j]);
+                v[j] = isfinite(f) ? v[j] - f : 0.f;
+            }
+            *reinterpret_cast<uint4*>((bf16*)g.terms + (row * g.n_terms + t) * g.terms_stride + j0) = *reinterpret_cast<const uint4*>(h);
+        }
     }
-};
+}
 
 template <int MT, int NT>
-__device__ __forceinline__ void low_rows(const LowArgs& g, const Sink& sink, int row0, int rows, int adapter, int rank_warps,
-                                         float* red) {
+__device__ __forceinline__ void low_rows(const LowArgs& g, float scale_low, float scale_terms, int row0, int rows, int adapter,
+                                         int rank_warps, float* red) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = g.req.rank;
     const int kw = warp / rank_warps, nw = warp - kw * rank_warps, k_warps = kWarps / rank_warps;   // this warp's share
     const int j0 = nw * NT * 8;
@@ -103,21 +122,22 @@ __device__ __forceinline__ void low_rows(const LowArgs& g, const Sink& sink, int
             for (int i = 0; i < MT * NT * 4; ++i) acc[i / (NT * 4)][i / 4 % NT][i % 4] += at[i * 32];
         }
     }
-    if (kw > 0) return;
+    // the sums by rows, for the whole block
+    const int pitch = rank_warps * NT * 8;
+    __syncthreads();
+    if (kw == 0) {
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 16 * m + (lane >> 2) + 8 * (i >> 1), j = j0 + 8 * n + 2 * (lane & 3) + (i & 1);
-                if (row < rows) sink.put(row0 + row, j, acc[m][n][i]);
-            }
-    // ranks that no warp's tiles reach are only the terms' zeros
-    for (int i = lane + 32 * nw; g.n_terms > 0 && i < rows * g.terms_stride; i += 32 * rank_warps) {
-        const int row = i / g.terms_stride, j = i - row * g.terms_stride;
-        if (j >= rank_warps * NT * 8) sink.put(row0 + row, j, 0.f);
+                for (int i = 0; i < 4; ++i) {
+                    const int row = 16 * m + (lane >> 2) + 8 * (i >> 1), j = j0 + 8 * n + 2 * (lane & 3) + (i & 1);
+                    red[row * pitch + j] = acc[m][n][i];
+                }
     }
+    __syncthreads();
+    store_rows_low(g, row0, rows, red, pitch, scale_low, scale_terms);
 }
 
 // NT: eights of the rank of a warp.
@@ -126,6 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_low(LowArgs g, int rank_warps, 
     __shared__ int where[3];
     __shared__ int warp_tot[kWarps];
     __shared__ float red[kWarps / 2 * (kRows / 16) * NT * 128];
+    static_assert(kRows * 4 * NT * 8 <= kWarps / 2 * (kRows / 16) * NT * 128, "room for the sums by rows");
     const Requests& q = g.req;
     pdl_launch();
     if (g.tiles != nullptr)
@@ -140,14 +161,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_low(LowArgs g, int rank_warps, 
     if (where[0] < 0) return;
     const int row0 = where[1], rows = where[2] - where[1], adapter = request_adapter(q, where[0], g.flags);
     if (adapter < 0) {
-        const Sink none{g, 0.f, 0.f};
-        for (int i = threadIdx.x; i < rows * g.terms_stride; i += kThreads) none.put(row0 + i / g.terms_stride, i % g.terms_stride, 0.f);
+        store_rows_low(g, row0, rows, nullptr, 0, 0.f, 0.f);
         return;
     }
-    const float c = g.scale != nullptr ? g.scale[adapter] : 1.f;
-    const Sink sink{g, g.scaled_low ? c : 1.f, c};
-    if (rows <= 16) low_rows<1, NT>(g, sink, row0, rows, adapter, rank_warps, red);
-    else low_rows<kRows / 16, NT>(g, sink, row0, rows, adapter, rank_warps, red);
+    const float c = g.scale != nullptr ? g.scale[adapter] : 1.f, scale_low = g.scaled_low ? c : 1.f;
+    if (rows <= 16) low_rows<1, NT>(g, scale_low, c, row0, rows, adapter, rank_warps, red);
+    else low_rows<kRows / 16, NT>(g, scale_low, c, row0, rows, adapter, rank_warps, red);
 }
 
 // The terms of given float32 rows [n_rows, rank].
