@@ -426,7 +426,7 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
         const size_t bytes = (size_t)max_rows * l->n_terms * l->stride * 2;
         st = cuda_status(cudaMalloc(&l->terms, bytes), call);
         if (st == BP_OK) st = cuda_status(cudaMalloc(&l->u_terms, bytes), call);
-        const size_t counts = low_change_counts(l->num_sms) * sizeof(unsigned);
+        const size_t counts = low_change_counts(n_adapters, l->num_sms) * sizeof(unsigned);
         if (st == BP_OK) st = cuda_status(cudaMalloc(&l->scratch, low_change_scratch(rank, l->num_sms) * sizeof(float)), call);
         if (st == BP_OK) st = cuda_status(cudaMalloc(&l->arrived, counts), call);
         if (st == BP_OK) st = cuda_status(cudaMemset(l->arrived, 0, counts), call);

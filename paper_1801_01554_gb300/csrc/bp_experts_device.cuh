@@ -230,7 +230,7 @@ __device__ __forceinline__ int2 tile_info(const Requests& q, int t, int* flags) 
             return make_int2(__shfl_sync(0xffffffffu, a, l), base + l);
         }
         count += __popc(__ballot_sync(0xffffffffu, hi > lo && lo < end && a >= 0));
-        if (count > q.rank) return make_int2(kTileByRow, first);
+        if (2 * count > q.rank) return make_int2(kTileByRow, first);
         if (__any_sync(0xffffffffu, lo >= end)) break;
     }
     return make_int2(count > 0 ? kTileMixed : -1, first);

@@ -124,7 +124,8 @@ cudaError_t simt_low_change(const LowChangeArgs& a, cudaStream_t s);
 // Tensor-core kernels for bfloat16 (bp_grouped_tc.cu).
 // The adapters' low-rank sums come as bfloat16 terms (LowArgs).  A block of kTileRows rows is of one
 // adapter (x: which), of none (-1), or of several requests, y being the first: whose sums are taken
-// apart (kTileMixed), or whose rows are (kTileByRow, where they are more than the rank).
+// apart (kTileMixed), or whose rows are (kTileByRow, where they are more than half the rank: a request's
+// sums are 0.85 us of a tile, a rank of a tile by rows 0.2 to 0.8, by its width).
 constexpr int kTileRows = 128;
 constexpr int kTileMixed = -2, kTileByRow = -3;
 constexpr int kForwardTerms = 2;   // of the terms, those that a bfloat16 result can tell: 2^-17
@@ -141,7 +142,7 @@ cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_s
 cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
 cudaError_t tc_low(const LowArgs& a, int num_sms, cudaStream_t s);
 size_t low_change_scratch(int rank, int num_sms);   // floats
-size_t low_change_counts(int num_sms);
+size_t low_change_counts(int n_adapters, int num_sms);
 cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, int num_sms, cudaStream_t s);
 
 // The forward product of a few rows in bfloat16 (bp_few.cu), rows read through an index too; with low,

@@ -109,7 +109,7 @@ struct Item {
     int g, row0, end, mb, nb;
     int kbs;        // K blocks
     int kb0, kb1;   // of the low form: of the adapter's
-    int run;
+    int run, shares;
     int adapter;    // whose low-rank K follows; of an up product, the rows'; -1, or a kind of tile
     int request;    // the tile's first
 };
@@ -215,9 +215,11 @@ struct Schedule {
             Stretches<LOW> all{g, w, table, 0, 0};
             int lo, hi, blocks = 0;
             while (all.request(lo, hi)) blocks += (hi - lo + BK - 1) / BK;
-            const int share = blocks / g.runs, more = blocks - share * g.runs;   // the first `more` shares have one more
+            // an adapter of few rows is left whole to the first share: another share costs what 10 K blocks do
+            w.shares = blocks >= 8 * g.runs ? g.runs : 1;
+            const int share = blocks / w.shares, more = blocks - share * w.shares;   // the first `more` shares have one more
             w.kb0 = w.run * share + min(w.run, more);
-            w.kb1 = w.kb0 + share + (w.run < more ? 1 : 0);
+            w.kb1 = w.run < w.shares ? w.kb0 + share + (w.run < more ? 1 : 0) : w.kb0;
             w.kbs = w.kb1 - w.kb0;
             return w;
         }
@@ -359,18 +361,35 @@ __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, i
     const int r = g.req.rank;
     const float c = g.scale != nullptr ? g.scale[adapter] : 1.f;
     const float* low = g.low + (size_t)row * r;
-    const bf16* P = g.P + (size_t)adapter * r * g.N + n0;
-    for (int j = 0; j < r; ++j) {
-        const float u = c * low[j];
+    const bf16* P = g.P + (size_t)adapter * r * g.N;
+    int at[4];   // columns past the last ones read the last ones: their sums are not kept
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (n0 + 8 * k >= g.N) break;
-            const uint4 p = *reinterpret_cast<const uint4*>(P + (size_t)j * g.N + 8 * k);
-            const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+    for (int k = 0; k < 4; ++k) at[k] = min(n0 + 8 * k, g.N - 8);
+    constexpr int B = 2;   // rows of the adapter under way (volatile: ptxas would sink the loads)
+    for (int j0 = 0; j0 < r; j0 += B) {
+        uint4 p[B][4];
+        float u[B];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                v[8 * k + 2 * q] = fmaf(u, __uint_as_float(w[q] << 16), v[8 * k + 2 * q]);
-                v[8 * k + 2 * q + 1] = fmaf(u, __uint_as_float(w[q] & 0xffff0000u), v[8 * k + 2 * q + 1]);
+        for (int j = 0; j < B; ++j) {
+            const int row_of = min(j0 + j, r - 1);
+            u[j] = j0 + j < r ? c * low[row_of] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(p[j][k].x), "=r"(p[j][k].y), "=r"(p[j][k].z), "=r"(p[j][k].w)
+                             : "l"(P + (size_t)row_of * g.N + at[k]));
+        }
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+            if (j0 + j >= r) break;   // (0 times an infinity is not 0)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t w[4] = {p[j][k].x, p[j][k].y, p[j][k].z, p[j][k].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[8 * k + 2 * q] = fmaf(u[j], __uint_as_float(w[q] << 16), v[8 * k + 2 * q]);
+                    v[8 * k + 2 * q + 1] = fmaf(u[j], __uint_as_float(w[q] & 0xffff0000u), v[8 * k + 2 * q + 1]);
+                }
             }
         }
     }
@@ -726,6 +745,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int it = blockIdx.x; it < items; it += gridDim.x) {
             const Item w = plan.item(it);
             if constexpr (kChange || FORM == UP) {
+                if (FORM == LOW && w.run >= w.shares) continue;   // left to the first share
                 float part[BN / 2];
 #pragma unroll
                 for (int c = 0; c < BN / 2; ++c) part[c] = 0.f;
@@ -809,7 +829,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const float scale = FORM == LOW && g.scale != nullptr ? g.scale[w.g] : 1.f;
                 const int m0 = w.mb * BM + q * 32;
                 float* G = g.G + (size_t)w.g * g.M * g.N;
-                if (FORM == LOW && g.runs > 1) {
+                if (FORM == LOW && w.shares > 1) {
                     // the run's sums to scratch; the last warp to arrive adds the runs' in their order
                     if (m0 >= g.M || w.nb * BN + cbeg >= g.N) continue;
                     const size_t plane = (size_t)g.req.n_adapters * g.M * g.N;
@@ -829,7 +849,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     unsigned* count = g.arrived + ((size_t)w.g * g.num_n + w.nb) * kEpiWarps + ew;
                     if (lane == 0) before = atomicAdd(count, 1u);
                     before = __shfl_sync(0xffffffffu, before, 0);
-                    if (before != (unsigned)g.runs - 1) continue;
+                    if (before != (unsigned)w.shares - 1) continue;
                     if (lane == 0) *count = 0u;
                     __threadfence();
                     const float* all = g.scratch + (size_t)w.g * g.M * g.N;
@@ -840,7 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int i = 0; i < kPer; ++i) sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                     // rows and columns past the last ones read the last ones, so that no load hangs on a condition
                     const float* at = all + (size_t)min(m0 + lane / kPer, g.M - 1) * g.N + min(w.nb * BN + cbeg + lane % kPer * 4, g.N - 4);
-                    for (int z = 0; z < g.runs; ++z) {
+                    for (int z = 0; z < w.shares; ++z) {
 #pragma unroll
                         for (int i = 0; i < kPer; ++i) {
                             const int row = min(32 / kPer * i, max(g.M - 1 - m0 - lane / kPer, 0));
@@ -1041,6 +1061,7 @@ cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtens
 
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
+constexpr int kShareColumns = 1024;   // an SM
 struct LowCut {
     int bn, num_n, runs;
 };
@@ -1188,7 +1209,8 @@ cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
 }
 
 // How the low change is cut: 128 columns, 64 where that leaves SMs without a tile, and shares of an
-// adapter's rows while the SMs are more than the tiles twice over.  More shares than that cost more than
+// adapter's rows while the SMs are more than the busy tiles twice over and the shares' sums fit their
+// scratch.  More shares than that cost more than
 // they balance: each is an exchange, a store and a fence of 5 us beside its 0.5 us a K block (us, both
 // changes of a layer of 16,384 rows, 1 / 2 / 4 / 16 shares: 5 adapters of rank 64 of 4096-4096, 160 tiles,
 // 142 / 194 / 295 / 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of 512-512, 32 tiles, 206 /
@@ -1199,13 +1221,15 @@ static LowCut low_cut(int n_adapters, int n_requests, int N, int num_sms) {
     c.bn = (long long)busy * ceil_div(N, 128) >= num_sms / 4 ? 128 : 64;
     c.num_n = ceil_div(N, c.bn);
     c.runs = 1;
-    while ((long long)n_adapters * c.num_n * c.runs * 2 <= num_sms) c.runs *= 2;
+    while ((long long)busy * c.num_n * c.runs * 2 <= num_sms && 2ll * c.runs * n_adapters * N <= kShareColumns * num_sms) c.runs *= 2;
     return c;
 }
 
-// Of any call of a layer.
-size_t low_change_scratch(int rank, int num_sms) { return (size_t)num_sms * 128 * rank; }
-size_t low_change_counts(int num_sms) { return (size_t)num_sms * kEpiWarps; }
+// Of any call of a layer: columns of shares, and the warps' parts of 64 of them.
+size_t low_change_scratch(int rank, int num_sms) { return (size_t)kShareColumns * num_sms * rank; }
+size_t low_change_counts(int n_adapters, int num_sms) {
+    return ((size_t)kShareColumns / 64 * num_sms + n_adapters) * kEpiWarps;
+}
 
 cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, int num_sms, cudaStream_t s) {
     TcArgs a{};
