@@ -322,8 +322,6 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
     RowsArgs a{};
     a.groups = {d_offsets, l->E, n_rows};
     const bool few = l->dtype == BP_BF16 && few_ok(n_rows, l->E);
-    if (!few) st = cuda_status(rows_in_order(l, a.groups, d_X, n_x, d_source, s), call);
-    if (st != BP_OK) return st;
     a.N = l->n_out;
     a.K = l->n_in;
     a.in = d_X;

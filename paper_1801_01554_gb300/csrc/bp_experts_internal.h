@@ -135,7 +135,7 @@ struct LowTerms {
     int2* tiles;
 };
 cudaError_t tc_setup();
-// Rows read through an index into the groups' order; tc_rows and tc_change take rows in order.
+// Rows read through an index into the groups' order; tc_change and the back product take rows in order.
 cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGroups& groups, int cols, void* out, int* flags,
                       int num_sms, cudaStream_t s);
 cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_sms, cudaStream_t s);

@@ -16,10 +16,11 @@
 // the next group's rows too and does not store them; in a change, where rows are summed, the
 // stage's foreign rows are set to zero in shared memory in both operands (0 times a foreign
 // infinity would not be 0).  W's maps have a dimension of their own for the group, past whose
-// edges the copy engine fills in zeros.  Rows read through an index are copied into the rows'
-// order first: gathered by the copy engine instead (four rows an instruction, a lane each), a
-// K block waited for its 32 instructions, 539 us for 32,768 rows of 2048-2048 against 181 without
-// an index; the copy takes 25 to 30.
+// edges the copy engine fills in zeros.  Rows that the forward product reads through an index are
+// gathered by four more warps, eight lanes a row, with cp.async into the swizzled stage (gathered by the
+// copy engine, four rows an instruction, a K block waited for its 32 instructions: 539 us for 32,768
+// rows of 2048-2048 against 181 without an index; copied into order first: 224).  A change, whose
+// epilogue wants the registers of such warps, takes rows that are copied into order first.
 //
 // The adapters' part of a tile whose rows all belong to one request is K beyond the layer's own:
 // the rows of low as two bfloat16 terms (its rounding and the rest) times the adapter's rows.  In
@@ -41,6 +42,8 @@ namespace {
 constexpr int kEpiWarps = 8;         // two per TMEM lane quarter, each on half of the columns
 constexpr int kEpiThreads = 32 * kEpiWarps;
 constexpr int kThreads = 64 + kEpiThreads;   // warp 0 copies, warp 1 MMA, warps 2.. epilogue
+constexpr int kGatherWarps = 4;              // of a forward product with an index, behind them
+constexpr int threads_of(bool gather) { return kThreads + (gather ? 32 * kGatherWarps : 0); }
 
 enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2, LOW = 3, UP = 4 };
 
@@ -48,6 +51,9 @@ struct TcArgs {
     RowGroups groups;
     int num_n, num_m;        // tiles along N; along M of a change
     int M, N, K;             // M: rows of a change; K: not of a change
+    const bf16* in;          // forward with an index: rows [n_in_rows, K]
+    const int* source;
+    int n_in_rows;
     const float* bias;
     int squash;
     const bf16* x;
@@ -403,8 +409,8 @@ __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, i
 // (An adapter's change has three products a K block, and few columns to drain.)
 constexpr int kChain = 8, kLowChain = 2;
 
-template <int BN, int FORM>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int BN, int FORM, bool GATHER = false>
+__global__ void __launch_bounds__(threads_of(GATHER), 1)
     k_grouped(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
               const __grid_constant__ CUtensorMap map_low, const __grid_constant__ CUtensorMap map_p,
               const __grid_constant__ TcArgs g) {
@@ -438,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     pdl_launch();
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(&full[s], 1);
+            mbar_init(&full[s], GATHER ? 1 + kGatherWarps : 1);
             mbar_init(&empty[s], 1);
         }
         for (int a = 0; a < kAcc; ++a) {
@@ -553,9 +559,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 } else {
                     for (int kb = 0; kb < w.kbs; ++kb) {
-                        if (!open(C::kStageBytes)) break;
+                        if (!open(GATHER ? C::kBBytes : C::kStageBytes)) break;
                         uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
-                        if (leader) tma_load_2d(sa, &map_a, kb * BK, w.row0, &full[stage]);
+                        if (!GATHER && leader) tma_load_2d(sa, &map_a, kb * BK, w.row0, &full[stage]);
                         if (FORM == UP) {
                             if (leader) tma_load_3d(sb, &map_b, kb * BK, 0, w.adapter, &full[stage]);
                         } else if (FORM == FORWARD) {
@@ -567,7 +573,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         close();
                     }
-                    if constexpr (FORM != UP) {
+                    if constexpr (FORM != UP && !GATHER) {
                         // the low-rank K of one adapter, up to 4 pieces of 16 of a term a stage
                         auto load_low = [&](int adapter) {
                             for (int t = 0; t < kForwardTerms; ++t)
@@ -676,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                             }
                             close();
                         }
-                        if constexpr (FORM != UP) {
+                        if constexpr (FORM != UP && !GATHER) {
                             const uint32_t low_b0 = desc_lo<true>(smem_u32(ring) + C::kABytes);
                             auto add_low = [&](bool fresh) {   // into accumulator acc
                                 const uint32_t d = tmem_base + (uint32_t)(acc * BN);
@@ -714,6 +720,48 @@ __global__ void __launch_bounds__(kThreads, 1)
                 }
             }
         }
+    } else if (GATHER && warp >= 2 + kEpiWarps) {
+        // ---------------- gather: a warp 32 rows of the tile, eight lanes the 128 bytes of a row in a K block
+        const int m0 = (warp - 2 - kEpiWarps) * 32 + (lane >> 3), c = lane & 7;   // rows m0, m0 + 4, ..; piece c
+        constexpr int kAhead = S - 2;   // K blocks whose copies are under way when the next one's are issued
+        int stage = 0, issued = 0;
+        unsigned phase = 0;
+        bool ok = true;
+        auto signal = [&](int block) {   // this warp's rows of a block are there, for the tensor cores to read
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&full[block % S]);
+        };
+        for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+            const Item w = plan.item(it);
+            const bf16* from[8];   // (rows past the group's end are not stored)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                from[i] = g.in + (size_t)source_row(g.source, min(w.row0 + m0 + 4 * i, w.end - 1), g.n_in_rows, g.flags) * g.K;
+            for (int kb = 0; kb < w.kbs; ++kb) {
+                if (issued >= S) {
+                    ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                }
+                const uint32_t to = smem_u32(ring + stage * C::kStageBytes) + m0 * 128;
+                const int k = kb * BK + 8 * c, n = k < g.K ? 16 : 0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)   // (128-byte swizzle: piece c of row m lies at c ^ (m mod 8))
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 512 * i + ((c ^ ((m0 + 4 * i) & 7)) << 4)),
+                                 "l"(n > 0 ? from[i] + k : from[i]), "r"(n)
+                                 : "memory");
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                ++issued;
+                if (++stage == S) { stage = 0; phase ^= 1u; }
+                if (issued > kAhead) {
+                    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+                    signal(issued - 1 - kAhead);
+                }
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");   // every copy lands before the CTA can exit
+        for (int b = max(issued - kAhead, 0); ok && b < issued; ++b) signal(b);
     } else {
         // ---------------- epilogue warps 2..9
         const int q = warp & 3;                  // TMEM lane quarter this warp may access
@@ -915,7 +963,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 int adapter = -1;   // of this lane's row, in a tile that is taken row by row
-                if (w.adapter == kTileByRow && row < w.end) {
+                if (!GATHER && w.adapter == kTileByRow && row < w.end) {
                     const int i = first_request(g.req, row);
                     if (i < g.req.n_requests) {
                         int lo, hi;
@@ -924,7 +972,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                 }
                 if (!wait_acc()) break;
-                if (w.adapter == kTileMixed) {
+                if (!GATHER && w.adapter == kTileMixed) {
                     // each request's sums: its rows, with the sums so far, replace them
                     TileRequests all{g, w, w.request};
                     int lo, hi, a;
@@ -964,7 +1012,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     float v[32];
                     tmem_ld32(trow + (uint32_t)(acc * BN + cbeg + c0), v);
-                    if (w.adapter == kTileByRow) add_low(g, row, adapter, n0, v);
+                    if (!GATHER && w.adapter == kTileByRow) add_low(g, row, adapter, n0, v);
                     if (FORM == FORWARD) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
@@ -1036,26 +1084,27 @@ bool make_map(CUtensorMap* map, const void* base, int rows, int cols, int planes
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, int FORM>
+template <int BN, int FORM, bool GATHER = false>
 cudaError_t setup_one() {
-    return cudaFuncSetAttribute(k_grouped<BN, FORM>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN, FORM>::kSmemBytes);
+    return cudaFuncSetAttribute(k_grouped<BN, FORM, GATHER>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<BN, FORM>::kSmemBytes);
 }
 template <int BN>
 cudaError_t setup_width() {
     cudaError_t e;
     if ((e = setup_one<BN, FORWARD>()) != cudaSuccess) return e;
+    if ((e = setup_one<BN, FORWARD, true>()) != cudaSuccess) return e;
     if ((e = setup_one<BN, BACK>()) != cudaSuccess) return e;
     return setup_one<BN, CHANGE>();
 }
 
-template <int FORM>
+template <int FORM, bool GATHER = false>
 cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtensorMap (&m)[4], cudaStream_t s) {
     const int grid = items < num_sms ? items : num_sms;
     if (grid < 1) return cudaSuccess;
-    auto go = [&](auto k, int smem) { return launch_pdl(k, grid, 1, kThreads, smem, s, m[0], m[1], m[2], m[3], a); };
-    if (bn == 64) return go(k_grouped<64, FORM>, Cfg<64, FORM>::kSmemBytes);
-    if (bn == 128 || FORM == LOW || FORM == UP) return go(k_grouped<128, FORM>, Cfg<128, FORM>::kSmemBytes);
-    if constexpr (FORM != LOW && FORM != UP) return go(k_grouped<256, FORM>, Cfg<256, FORM>::kSmemBytes);
+    auto go = [&](auto k, int smem) { return launch_pdl(k, grid, 1, threads_of(GATHER), smem, s, m[0], m[1], m[2], m[3], a); };
+    if (bn == 64) return go(k_grouped<64, FORM, GATHER>, Cfg<64, FORM>::kSmemBytes);
+    if (bn == 128 || FORM == LOW || FORM == UP) return go(k_grouped<128, FORM, GATHER>, Cfg<128, FORM>::kSmemBytes);
+    if constexpr (FORM != LOW && FORM != UP) return go(k_grouped<256, FORM, GATHER>, Cfg<256, FORM>::kSmemBytes);
     return cudaErrorInvalidValue;
 }
 
@@ -1126,6 +1175,9 @@ cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_s
     a.groups = r.groups;
     a.N = r.N;
     a.K = r.K;
+    a.in = (const bf16*)r.in;
+    a.source = r.source;
+    a.n_in_rows = r.n_in_rows;
     a.bias = r.bias;
     a.squash = r.squash;
     a.x = (const bf16*)r.x;
@@ -1157,7 +1209,8 @@ cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_s
     if (!ok) return cudaErrorInvalidValue;
     const long long items = (long long)max_tiles(r.groups.n_rows, E, BM) * a.num_n;
     const int n = items < num_sms ? (int)items : num_sms;
-    return back ? launch<BACK>(a, bn, n, num_sms, m, s) : launch<FORWARD>(a, bn, n, num_sms, m, s);
+    if (back) return launch<BACK>(a, bn, n, num_sms, m, s);
+    return r.source != nullptr ? launch<FORWARD, true>(a, bn, n, num_sms, m, s) : launch<FORWARD>(a, bn, n, num_sms, m, s);
 }
 
 cudaError_t tc_change(const ChangeArgs& c, int num_sms, cudaStream_t s) {
