@@ -573,8 +573,14 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
 }
 
 bp_status bp_adapters_check(bp_adapters* l, void* stream) {
-    if (l == nullptr) return fail(BP_EINVAL, "bp_adapters_check: NULL layer");
-    return read_flags(l->flags, stream, "bp_adapters_check");
+    const char* call = "bp_adapters_check";
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL layer", call);
+    const bp_status st = read_flags(l->flags, stream, call);
+    if (st == BP_ETIMEOUT && l->arrived != nullptr) {   // a launch that stopped early leaves counts behind
+        const cudaError_t e = cudaMemset(l->arrived, 0, low_change_counts(l->n, l->num_sms) * sizeof(unsigned));
+        if (e != cudaSuccess) return cuda_status(e, call);
+    }
+    return st;
 }
 
 }  // extern "C"

@@ -99,6 +99,24 @@ def test_larger_layer_of_many_tiles():
     check(5, 48, 1024, 1536, 5000, 6, bp.BP_BF16, True, 2)
 
 
+@pytest.mark.parametrize("dtype", [bp.BP_F32, bp.BP_BF16])
+def test_more_requests_than_a_table_holds(dtype):
+    """700 requests in 1,500 rows: blocks of rows with many requests, and the long list of them."""
+    check(3, 16, 128, 64, 1500, 700, dtype, True, 31)
+
+
+def test_few_adapters_of_many_rows_and_many_without_any():
+    """Changes whose rows are shared out, beside adapters that nobody asks for."""
+    p = problem(40, 40, 192, 136, 5000, 4, bp.BP_BF16, False, 17)
+    p["adapter"][:] = [7, -1, 7, 39]
+    check(40, 40, 192, 136, 5000, 4, bp.BP_BF16, p=p)
+
+
+def test_one_long_request_among_single_rows():
+    offsets = list(range(0, 90)) + [700] + list(range(701, 760))
+    check(9, 24, 264, 136, offsets[-1], len(offsets) - 1, bp.BP_BF16, True, 18, offsets)
+
+
 def test_other_requests_do_not_leak():
     """NaN rows and an infinite adapter of one request stay in it."""
     for dtype in (bp.BP_F32, bp.BP_BF16):
