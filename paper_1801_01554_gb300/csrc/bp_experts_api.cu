@@ -535,7 +535,10 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
     if (st != BP_OK) return st;
     cudaStream_t s = (cudaStream_t)stream;
     const Requests req{d_offsets, d_adapter, rows ? n_requests : 0, n_rows, l->n, l->rank};
-    if (rows && (dx || ga)) {
+    // u's terms first: the launches after it depend on one another one by one
+    if (gb && some && l->dtype == BP_BF16)
+        st = cuda_status(low_terms(d_U, n_rows, l->rank, l->u_terms, l->stride, l->n_terms, l->num_sms, s), call);
+    if (st == BP_OK && rows && (dx || ga)) {
         st = cuda_status(low_of(l, req, l->n_out, d_D, d_B, d_scale, false, l->low, s), call);
     }
     if (st == BP_OK && rows && dx) {
@@ -565,9 +568,7 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
         const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->scratch, l->arrived, l->flags};
         LowTerms u = l->low_terms();
         u.terms = l->u_terms;
-        if (tc && some) st = cuda_status(low_terms(d_U, n_rows, l->rank, l->u_terms, u.stride, u.n_terms, l->num_sms, s), call);
-        if (st == BP_OK)
-            st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, s), call);
+        st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, s), call);
     }
     return st;
 }

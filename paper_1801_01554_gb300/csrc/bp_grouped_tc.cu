@@ -71,7 +71,8 @@ struct TcArgs {
     const float* low;
     const bf16* P;
     const float* scale;
-    int runs;                  // of the low form: shares of an adapter's rows, of which the sums go to
+    int num_sms;
+    int runs;                  // of the low form: most shares of an adapter's rows, of which the sums go to
     float* scratch;            // [runs, n_adapters, rank, N]
     unsigned* arrived;         // of every warp's part of a tile; zeros, left so
     // up
@@ -204,6 +205,12 @@ struct Schedule {
     const TcArgs& g;
     const int *lo, *hi, *tile0;   // per group, in shared memory: first row, end; first row block (n_groups + 1)
     const RequestTable table;
+    __device__ int table_blocks(int i) const {   // K blocks of a request
+        int l, h;
+        if (table.adapter != nullptr) l = table.lo[i], h = table.hi[i];
+        else group_rows(g.req.offsets, g.req.n_rows, i, l, h, g.flags);
+        return (h - l + BK - 1) / BK;
+    }
     __device__ int items() const {
         if (FORM == LOW) return g.req.n_adapters * g.num_n * g.runs;
         if (FORM == UP) return g.max_items;
@@ -212,8 +219,10 @@ struct Schedule {
     __device__ Item item(int it) const {
         Item w;
         if (FORM == LOW) {
-            const int tile = g.runs == 1 ? it : it / g.runs;
-            w.run = it - tile * g.runs;
+            // all tiles' first shares, then their second ones, ..: those that there are lie together
+            const int tiles = g.req.n_adapters * g.num_n;
+            w.run = g.runs == 1 ? 0 : it / tiles;
+            const int tile = it - w.run * tiles;
             w.g = tile / g.num_n;
             w.nb = tile - w.g * g.num_n;
             w.mb = w.row0 = w.end = 0;
@@ -221,8 +230,18 @@ struct Schedule {
             Stretches<LOW> all{g, w, table, 0, 0};
             int lo, hi, blocks = 0;
             while (all.request(lo, hi)) blocks += (hi - lo + BK - 1) / BK;
-            // an adapter of few rows is left whole to the first share: another share costs what 10 K blocks do
-            w.shares = blocks >= 8 * g.runs ? g.runs : 1;
+            // as many shares as an adapter has times an SM's part of all K blocks, to the nearest; one of few
+            // rows is left whole (another share costs what 10 K blocks do)
+            w.shares = 1;
+            if (g.runs > 1 && blocks >= 16) {
+                int all_blocks = 0;
+                for (int i = threadIdx.x & 31; i < g.req.n_requests; i += 32)
+                    if ((table.adapter != nullptr ? table.adapter : g.req.adapter)[i] >= 0) all_blocks += table_blocks(i);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) all_blocks += __shfl_xor_sync(0xffffffffu, all_blocks, o);
+                const int part = max((int)((long long)all_blocks * g.num_n / g.num_sms), 8);
+                w.shares = min(max((2 * blocks + part) / (2 * part), 1), g.runs);
+            }
             const int share = blocks / w.shares, more = blocks - share * w.shares;   // the first `more` shares have one more
             w.kb0 = w.run * share + min(w.run, more);
             w.kb1 = w.run < w.shares ? w.kb0 + share + (w.run < more ? 1 : 0) : w.kb0;
@@ -1261,20 +1280,22 @@ cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
     return launch<UP>(a, bn, a.max_items < num_sms ? a.max_items : num_sms, num_sms, m, s);
 }
 
-// How the low change is cut: 128 columns, 64 where that leaves SMs without a tile, and shares of an
-// adapter's rows while the SMs are more than the busy tiles twice over and the shares' sums fit their
-// scratch.  More shares than that cost more than
-// they balance: each is an exchange, a store and a fence of 5 us beside its 0.5 us a K block (us, both
-// changes of a layer of 16,384 rows, 1 / 2 / 4 / 16 shares: 5 adapters of rank 64 of 4096-4096, 160 tiles,
-// 142 / 194 / 295 / 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of 512-512, 32 tiles, 206 /
-// 118 / 75 / 63).
-static LowCut low_cut(int n_adapters, int n_requests, int N, int num_sms) {
+// How the low change is cut: 128 columns, 64 where that leaves SMs without a tile, and up to 16 shares of
+// an adapter's rows, as many as the device finds that it has times an SM's part (Schedule::item), where
+// there are rows for them, the items stay few (each is a look at the requests, 0.8 us) and the shares'
+// sums fit their scratch.  A share is an exchange, a store and a fence of 5 us beside its 0.5 us a K block:
+// us, both changes of a layer of 16,384 rows, every adapter in 1 / 2 / 4 / 16 shares: 5 adapters of rank 64
+// of 4096-4096, 160 tiles, 142 / 194 / 295 / 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of
+// 512-512, 32 tiles, 206 / 118 / 75 / 63.
+static LowCut low_cut(int n_adapters, int n_requests, int n_rows, int N, int num_sms) {
     const int busy = n_adapters < n_requests ? n_adapters : n_requests;
     LowCut c;
     c.bn = (long long)busy * ceil_div(N, 128) >= num_sms / 4 ? 128 : 64;
     c.num_n = ceil_div(N, c.bn);
     c.runs = 1;
-    while ((long long)busy * c.num_n * c.runs * 2 <= num_sms && 2ll * c.runs * n_adapters * N <= kShareColumns * num_sms) c.runs *= 2;
+    while (c.runs < 16 && n_rows >= 2 * c.runs * 16 * BK && 2ll * c.runs * n_adapters * c.num_n <= 8 * num_sms &&
+           2ll * c.runs * n_adapters * N <= kShareColumns * num_sms)
+        c.runs *= 2;
     return c;
 }
 
@@ -1296,9 +1317,10 @@ cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, int num_s
     a.n_terms = low.n_terms;
     a.stride = low.stride;
     a.flags = c.flags;
-    const LowCut cut = low_cut(c.req.n_adapters, c.req.n_requests, c.N, num_sms);
+    const LowCut cut = low_cut(c.req.n_adapters, c.req.n_requests, c.req.n_rows, c.N, num_sms);
     a.num_n = cut.num_n;
     a.runs = cut.runs;
+    a.num_sms = num_sms;
     a.scratch = c.scratch;
     a.arrived = c.arrived;
     CUtensorMap m[4];
