@@ -753,10 +753,14 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
         };
         for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
             const Item w = plan.item(it);
-            const bf16* from[8];   // (rows past the group's end are not stored)
+            // rows past the group's end are zeros, which cost no read (the last row again in their place: a
+            // tile of 15 rows took 52 us for 14, its copies all of one line)
+            const bf16* from[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                from[i] = g.in + (size_t)source_row(g.source, min(w.row0 + m0 + 4 * i, w.end - 1), g.n_in_rows, g.flags) * g.K;
+            for (int i = 0; i < 8; ++i) {
+                const int row = w.row0 + m0 + 4 * i;
+                from[i] = row < w.end ? g.in + (size_t)source_row(g.source, row, g.n_in_rows, g.flags) * g.K : nullptr;
+            }
             for (int kb = 0; kb < w.kbs; ++kb) {
                 if (issued >= S) {
                     ok = mbar_wait(&empty[stage], phase ^ 1u, abort_flag, g.flags);
@@ -764,12 +768,14 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                     if (!ok) break;
                 }
                 const uint32_t to = smem_u32(ring + stage * C::kStageBytes) + m0 * 128;
-                const int k = kb * BK + 8 * c, n = k < g.K ? 16 : 0;
+                const int k = kb * BK + 8 * c;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)   // (128-byte swizzle: piece c of row m lies at c ^ (m mod 8))
+                for (int i = 0; i < 8; ++i) {   // (128-byte swizzle: piece c of row m lies at c ^ (m mod 8))
+                    const bool read = k < g.K && from[i] != nullptr;
                     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 512 * i + ((c ^ ((m0 + 4 * i) & 7)) << 4)),
-                                 "l"(n > 0 ? from[i] + k : from[i]), "r"(n)
+                                 "l"(read ? from[i] + k : g.in), "r"(read ? 16 : 0)
                                  : "memory");
+                }
                 asm volatile("cp.async.commit_group;" ::: "memory");
                 ++issued;
                 if (++stage == S) { stage = 0; phase ^= 1u; }
