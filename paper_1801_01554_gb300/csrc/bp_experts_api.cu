@@ -22,18 +22,19 @@ struct bp_experts {
     void* rows = nullptr;   // bfloat16: [cap, n_in] inputs in the rows' order
     float* sums = nullptr;  // bias changes of runs of rows
     unsigned* arrived = nullptr;
+    ChangeShares shares{};  // float32: changes of shares of the rows
 };
 
 struct bp_adapters {
     int n = 0, rank = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, max_requests = 0, num_sms = 0;
     int* flags = nullptr;
     float* low = nullptr;   // [cap, rank] v of the backward pass
+    float* scratch = nullptr;      // changes of shares of the rows
+    unsigned* arrived = nullptr;
     // bfloat16: u or v as bfloat16 terms, u's for its change, and what row blocks hold
     void* terms = nullptr;
     void* u_terms = nullptr;
     int2* tiles = nullptr;
-    float* scratch = nullptr;      // changes of shares of the rows
-    unsigned* arrived = nullptr;
     int n_terms = 0, stride = 0;
     LowTerms low_terms() const { return {terms, n_terms, stride, tiles}; }
 };
@@ -104,6 +105,13 @@ bp_status make_layer(int dtype, int** flags, int* num_sms, const char* call) {
     if (e == cudaSuccess && dtype == BP_BF16) e = few_setup();
     if (e == cudaSuccess) e = cudaMalloc(flags, sizeof(int));
     if (e == cudaSuccess) e = cudaMemset(*flags, 0, sizeof(int));
+    return cuda_status(e, call);
+}
+
+// Zeros that blocks count their arrivals with.
+bp_status make_counts(unsigned** counts, size_t n, const char* call) {
+    cudaError_t e = cudaMalloc(counts, n * sizeof(unsigned));
+    if (e == cudaSuccess) e = cudaMemset(*counts, 0, n * sizeof(unsigned));
     return cuda_status(e, call);
 }
 
@@ -266,8 +274,11 @@ bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int m
     // fewer rows make no more runs
     const size_t planes = sums_runs(max_rows, n_experts, n_out, dtype, l->num_sms), cells = (size_t)n_experts * n_out;
     if (st == BP_OK) st = cuda_status(cudaMalloc(&l->sums, planes * cells * sizeof(float)), call);
-    if (st == BP_OK) st = cuda_status(cudaMalloc(&l->arrived, cells * sizeof(unsigned)), call);
-    if (st == BP_OK) st = cuda_status(cudaMemset(l->arrived, 0, cells * sizeof(unsigned)), call);
+    if (st == BP_OK) st = make_counts(&l->arrived, cells, call);
+    if (st == BP_OK && dtype == BP_F32) {
+        st = cuda_status(cudaMalloc(&l->shares.scratch, simt_change_scratch(l->num_sms) * sizeof(float)), call);
+        if (st == BP_OK) st = make_counts(&l->shares.arrived, simt_change_counts(l->num_sms), call);
+    }
     if (st != BP_OK) {
         bp_experts_destroy(l);
         return st;
@@ -283,6 +294,8 @@ void bp_experts_destroy(bp_experts* l) {
     cudaFree(l->rows);
     cudaFree(l->sums);
     cudaFree(l->arrived);
+    cudaFree(l->shares.scratch);
+    cudaFree(l->shares.arrived);
     delete l;
 }
 
@@ -379,7 +392,7 @@ bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, i
     }
     if (st == BP_OK && d_GW != nullptr) {
         const ChangeArgs a{groups, l->n_out, l->n_in, d_D, d_X, d_source, n_x, d_GW, accumulate, l->flags};
-        st = cuda_status(l->dtype == BP_BF16 ? tc_change(a, l->num_sms, s) : simt_change(a, l->num_sms, s), call);
+        st = cuda_status(l->dtype == BP_BF16 ? tc_change(a, l->num_sms, s) : simt_change(a, l->shares, l->num_sms, s), call);
     }
     if (st == BP_OK && d_Gb != nullptr) {
         const SumsArgs a{groups, l->n_out, d_D, d_Gb, accumulate, l->sums, l->arrived, l->flags};
@@ -424,13 +437,15 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
         const size_t bytes = (size_t)max_rows * l->n_terms * l->stride * 2;
         st = cuda_status(cudaMalloc(&l->terms, bytes), call);
         if (st == BP_OK) st = cuda_status(cudaMalloc(&l->u_terms, bytes), call);
-        const size_t counts = low_change_counts(n_adapters, l->num_sms) * sizeof(unsigned);
-        if (st == BP_OK) st = cuda_status(cudaMalloc(&l->scratch, low_change_scratch(rank, l->num_sms) * sizeof(float)), call);
-        if (st == BP_OK) st = cuda_status(cudaMalloc(&l->arrived, counts), call);
-        if (st == BP_OK) st = cuda_status(cudaMemset(l->arrived, 0, counts), call);
         if (st == BP_OK)
             st = cuda_status(cudaMalloc(&l->tiles, ((size_t)max_rows / kTileRows + 1) * sizeof(int2)), call);
     }
+    if (st == BP_OK) {
+        const size_t floats = dtype == BP_BF16 ? low_change_scratch(rank, l->num_sms) : simt_change_scratch(l->num_sms);
+        st = cuda_status(cudaMalloc(&l->scratch, floats * sizeof(float)), call);
+    }
+    if (st == BP_OK)
+        st = make_counts(&l->arrived, dtype == BP_BF16 ? low_change_counts(n_adapters, l->num_sms) : simt_change_counts(l->num_sms), call);
     if (st != BP_OK) {
         bp_adapters_destroy(l);
         return st;
@@ -562,13 +577,13 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
     const bool tc = l->dtype == BP_BF16;
     if (st == BP_OK && ga) {
         const LowChangeArgs a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->scratch, l->arrived, l->flags};
-        st = cuda_status(tc ? tc_low_change(a, l->low_terms(), l->num_sms, s) : simt_low_change(a, s), call);
+        st = cuda_status(tc ? tc_low_change(a, l->low_terms(), l->num_sms, s) : simt_low_change(a, {l->scratch, l->arrived, 1}, l->num_sms, s), call);
     }
     if (st == BP_OK && gb) {
         const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->scratch, l->arrived, l->flags};
         LowTerms u = l->low_terms();
         u.terms = l->u_terms;
-        st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, s), call);
+        st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, {l->scratch, l->arrived, 1}, l->num_sms, s), call);
     }
     return st;
 }
@@ -577,7 +592,7 @@ bp_status bp_adapters_check(bp_adapters* l, void* stream) {
     const char* call = "bp_adapters_check";
     if (l == nullptr) return fail(BP_EINVAL, "%s: NULL layer", call);
     const bp_status st = read_flags(l->flags, stream, call);
-    if (st == BP_ETIMEOUT && l->arrived != nullptr) {   // a launch that stopped early leaves counts behind
+    if (st == BP_ETIMEOUT) {   // a (tcgen05) launch that stopped early leaves counts behind
         const cudaError_t e = cudaMemset(l->arrived, 0, low_change_counts(l->n, l->num_sms) * sizeof(unsigned));
         if (e != cudaSuccess) return cuda_status(e, call);
     }

@@ -118,8 +118,17 @@ cudaError_t group_sums(const SumsArgs& a, int dtype, int num_sms, cudaStream_t s
 cudaError_t simt_setup();
 cudaError_t simt_rows(const RowsArgs& a, bool back, int num_sms, cudaStream_t s);
 cudaError_t simt_low(const LowArgs& a, cudaStream_t s);
-cudaError_t simt_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
-cudaError_t simt_low_change(const LowChangeArgs& a, cudaStream_t s);
+// Rows shared out between blocks: the shares' sums [shares, groups, M, N], and zeros that count their
+// arrivals (left zero).
+struct ChangeShares {
+    float* scratch;
+    unsigned* arrived;
+    int shares;             // (set by the launchers)
+};
+size_t simt_change_scratch(int num_sms);   // floats
+size_t simt_change_counts(int num_sms);
+cudaError_t simt_change(const ChangeArgs& a, const ChangeShares& room, int num_sms, cudaStream_t s);
+cudaError_t simt_low_change(const LowChangeArgs& a, const ChangeShares& room, int num_sms, cudaStream_t s);
 
 // Tensor-core kernels for bfloat16 (bp_grouped_tc.cu).
 // The adapters' low-rank sums come as bfloat16 terms (LowArgs).  A block of kTileRows rows is of one

@@ -288,42 +288,71 @@ __global__ void __launch_bounds__(kThreads) k_low_simt(LowArgs g) {
                 g.low[(size_t)(row0 + tile_at<P, true>(ty, i)) * r + n0 + tile_at<P, true>(tx, j)] = c * acc[i][j];
 }
 
+// Share z of `shares` of rows [lo, hi).
+__device__ __forceinline__ void share_rows(int& lo, int& hi, int z, int shares) {
+    const int per = (hi - lo + shares - 1) / shares;
+    lo = min(lo + z * per, hi);
+    hi = min(lo + per, hi);
+}
+
+// A tile of changes [groups][M, N] from the block's sums; with several shares they go to scratch
+// [shares][groups][M, N], and the last block to arrive adds the shares' in their order.
 template <int P>
-__device__ __forceinline__ void store_change(float* G, int M, int N, int m0, int n0, const float (&acc)[P][P], float c,
-                                             int accumulate) {
+__device__ __forceinline__ void store_change(const ChangeShares& s, int z, int groups, int e, float* G, int M, int N, int m0, int n0,
+                                             float (&acc)[P][P], float c, int accumulate) {
+    __shared__ int last;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const size_t plane = (size_t)groups * M * N;
+    auto each = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < P; ++i)
+        for (int i = 0; i < P; ++i)
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            const int m = m0 + tile_at<P, false>(ty, i), n = n0 + tile_at<P, false>(tx, j);
-            if (m >= M || n >= N) continue;
-            float* p = G + (size_t)m * N + n;
-            *p = accumulate ? *p + c * acc[i][j] : c * acc[i][j];
+            for (int j = 0; j < P; ++j) {
+                const int m = m0 + tile_at<P, false>(ty, i), n = n0 + tile_at<P, false>(tx, j);
+                if (m < M && n < N) f(acc[i][j], ((size_t)e * M + m) * N + n);
+            }
+    };
+    if (s.shares > 1) {
+        each([&](float& x, size_t at) { s.scratch[z * plane + at] = x; });
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            unsigned* count = s.arrived + ((size_t)e * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+            last = atomicAdd(count, 1u) == (unsigned)s.shares - 1;
+            if (last) *count = 0u;
         }
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+        each([&](float& x, size_t) { x = 0.f; });
+        for (int k = 0; k < s.shares; ++k) each([&](float& x, size_t at) { x += __ldcg(&s.scratch[k * plane + at]); });
+    }
+    each([&](float& x, size_t at) { G[at] = accumulate ? G[at] + c * x : c * x; });
 }
 
 template <int P, bool WIDE>
-__global__ void __launch_bounds__(kThreads) k_change_simt(ChangeArgs g) {
+__global__ void __launch_bounds__(kThreads) k_change_simt(ChangeArgs g, ChangeShares sh) {
     constexpr int T = Step<P>::T;
     extern __shared__ __align__(16) uint8_t smem[];
     Step<P>* t = reinterpret_cast<Step<P>*>(smem);
-    const int e = blockIdx.z, m0 = blockIdx.y * T, n0 = blockIdx.x * T;
+    const int E = g.groups.n_groups, z = blockIdx.z / E, e = blockIdx.z - z * E, m0 = blockIdx.y * T, n0 = blockIdx.x * T;
     int lo, hi;
     group_rows(g.groups.offsets, g.groups.n_rows, e, lo, hi, g.flags);
+    share_rows(lo, hi, z, sh.shares);
     const float *a = (const float*)g.a, *b = (const float*)g.b;
     float acc[P][P] = {};
     accumulate<P, false, false, WIDE>(
         t, acc, hi - lo, a, g.M - m0, [&](int k) { return a + (size_t)(lo + k) * g.M + m0; }, g.N - n0,
         [&](int k) { return b + (size_t)source_row(g.source, lo + k, g.n_b, g.flags) * g.N + n0; });
-    store_change<P>(g.G + (size_t)e * g.M * g.N, g.M, g.N, m0, n0, acc, 1.f, g.accumulate);
+    store_change<P>(sh, z, E, e, g.G, g.M, g.N, m0, n0, acc, 1.f, g.accumulate);
 }
 
-__global__ void __launch_bounds__(kThreads) k_low_change_simt(LowChangeArgs g) {
-    extern __shared__ __align__(16) uint8_t smem[];
+__global__ void __launch_bounds__(kThreads) k_low_change_simt(LowChangeArgs g, ChangeShares sh) {
     constexpr int P = kLowP, T = Step<P>::T;
+    extern __shared__ __align__(16) uint8_t smem[];
     Step<P>* t = reinterpret_cast<Step<P>*>(smem);
-    const int ad = blockIdx.z, m0 = blockIdx.y * T, n0 = blockIdx.x * T, r = g.req.rank;
+    const int n_ad = g.req.n_adapters, z = blockIdx.z / n_ad, ad = blockIdx.z - z * n_ad;
+    const int m0 = blockIdx.y * T, n0 = blockIdx.x * T, r = g.req.rank;
     const float* b = (const float*)g.b;
     float acc[P][P] = {};
     for (int base = 0; base < g.req.n_requests; base += 32) {   // the adapter's requests, in order
@@ -332,12 +361,14 @@ __global__ void __launch_bounds__(kThreads) k_low_change_simt(LowChangeArgs g) {
         for (; mine != 0; mine &= mine - 1) {
             int lo, hi;
             group_rows(g.req.offsets, g.req.n_rows, base + __ffs(mine) - 1, lo, hi, g.flags);
+            share_rows(lo, hi, z, sh.shares);
+            if (hi <= lo) continue;
             accumulate<P, false, false, false>(
                 t, acc, hi - lo, b, r - m0, [&](int k) { return g.low + (size_t)(lo + k) * r + m0; }, g.N - n0,
                 [&](int k) { return b + (size_t)(lo + k) * g.N + n0; });
         }
     }
-    store_change<P>(g.G + (size_t)ad * r * g.N, r, g.N, m0, n0, acc, g.scale != nullptr ? g.scale[ad] : 1.f, g.accumulate);
+    store_change<P>(sh, z, n_ad, ad, g.G, r, g.N, m0, n0, acc, g.scale != nullptr ? g.scale[ad] : 1.f, g.accumulate);
 }
 
 int blocks(long long n, int per) { return (int)((n + per - 1) / per); }
@@ -396,19 +427,37 @@ cudaError_t simt_low(const LowArgs& a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-cudaError_t simt_change(const ChangeArgs& a, int num_sms, cudaStream_t s) {
-    const int p = pick_tile(num_sms, [&](int T) { return (long long)a.groups.n_groups * blocks(a.M, T) * blocks(a.N, T); });
-    const dim3 grid(blocks(a.N, 16 * p), blocks(a.M, 16 * p), a.groups.n_groups);
-    if (p == 8 && wide(a.a, a.b, a.M, a.N)) k_change_simt<8, true><<<grid, kThreads, kSmem<8>, s>>>(a);
-    else if (p == 8) k_change_simt<8, false><<<grid, kThreads, kSmem<8>, s>>>(a);
-    else if (p == 4) k_change_simt<4, false><<<grid, kThreads, kSmem<4>, s>>>(a);
-    else k_change_simt<2, false><<<grid, kThreads, kSmem<2>, s>>>(a);
+// Shares of every group's rows: while tiles for four blocks an SM are wanting and a busy group has 128
+// rows for each (the groups' sizes are on the device: taken for even).
+static int change_shares(long long tiles, int groups, int busy, int n_rows, int num_sms) {
+    int shares = 1;
+    while (shares < 64 && tiles * groups * shares * 2 <= 4 * num_sms && n_rows / (2ll * busy * shares) >= 128) shares *= 2;
+    return shares;
+}
+// Of any call: tiles of all shares are at most four an SM where there are several.
+size_t simt_change_scratch(int num_sms) { return (size_t)4 * num_sms * 128 * 128; }
+size_t simt_change_counts(int num_sms) { return (size_t)4 * num_sms; }
+
+cudaError_t simt_change(const ChangeArgs& a, const ChangeShares& room, int num_sms, cudaStream_t s) {
+    const int E = a.groups.n_groups;
+    const int p = pick_tile(num_sms, [&](int T) { return (long long)E * blocks(a.M, T) * blocks(a.N, T); }), T = 16 * p;
+    ChangeShares sh = room;
+    sh.shares = change_shares((long long)blocks(a.M, T) * blocks(a.N, T), E, E, a.groups.n_rows, num_sms);
+    const dim3 grid(blocks(a.N, T), blocks(a.M, T), E * sh.shares);
+    if (p == 8 && wide(a.a, a.b, a.M, a.N)) k_change_simt<8, true><<<grid, kThreads, kSmem<8>, s>>>(a, sh);
+    else if (p == 8) k_change_simt<8, false><<<grid, kThreads, kSmem<8>, s>>>(a, sh);
+    else if (p == 4) k_change_simt<4, false><<<grid, kThreads, kSmem<4>, s>>>(a, sh);
+    else k_change_simt<2, false><<<grid, kThreads, kSmem<2>, s>>>(a, sh);
     return cudaGetLastError();
 }
 
-cudaError_t simt_low_change(const LowChangeArgs& a, cudaStream_t s) {
-    const dim3 grid(blocks(a.N, 16 * kLowP), blocks(a.req.rank, 16 * kLowP), a.req.n_adapters);
-    k_low_change_simt<<<grid, kThreads, kSmem<kLowP>, s>>>(a);
+cudaError_t simt_low_change(const LowChangeArgs& a, const ChangeShares& room, int num_sms, cudaStream_t s) {
+    constexpr int T = 16 * kLowP;
+    const int n_ad = a.req.n_adapters, busy = a.req.n_requests < 1 ? 1 : n_ad < a.req.n_requests ? n_ad : a.req.n_requests;
+    const int x = blocks(a.N, T), y = blocks(a.req.rank, T);
+    ChangeShares sh = room;
+    sh.shares = change_shares((long long)x * y, n_ad, busy, a.req.n_rows, num_sms);
+    k_low_change_simt<<<dim3(x, y, n_ad * sh.shares), kThreads, kSmem<kLowP>, s>>>(a, sh);
     return cudaGetLastError();
 }
 
