@@ -9,6 +9,11 @@
 //
 // One persistent CTA per SM: a warp that issues TMA copies into a ring of stages, a warp that
 // issues tcgen05.mma (128 rows x BN columns x 64 of K a stage) into TMEM, eight epilogue warps.
+// The tensor cores bound the large products: 16,384 rows of 4096-4096 in 8 groups take 332 us forward and
+// 331 back (1.65 PFLOP/s, 87% of the measured burst rate), their changes 410 (1.34 PFLOP/s; 350 without
+// the 537 MB that they write); few rows a group are bound by reading the weights (240 rows of 4096-1024
+// in 32 groups: 44 us, the 268 MB at the measured copy rate 40).
+//
 // The groups' ends lie on the device: each CTA turns them into first tiles in shared memory and
 // finds the group of a tile by bisection, so that no host knows the sizes and no list is written.
 //
@@ -26,8 +31,8 @@
 // the rows of low as two bfloat16 terms (its rounding and the rest) times the adapter's rows.  In
 // a tile of several requests each request's part is a sum of its own for all of the tile's rows, of
 // which the epilogue adds the request's rows (as one product with the other requests' rows at zero,
-// an adapter's infinity would reach them); with more requests than the rank has columns the
-// epilogue takes the rows one by one instead.  In the low form the terms lie side by side along
+// an adapter's infinity would reach them); with more requests than half the rank the epilogue
+// takes the rows one by one instead.  In the low form the terms lie side by side along
 // M (three up to rank 64: as exact as float32), so that a rank of up to 32 costs one product and one
 // of 64 two instead of three; the epilogue warps of the other terms pass their sums on through shared
 // memory.  Its K blocks run over the adapter's requests in order.
@@ -422,10 +427,11 @@ __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, i
 
 // K blocks of one sum of a change in TMEM.  The tensor cores truncate as they accumulate, so that
 // a sum's error grows with its length; these sums are added in registers, rounding to nearest.
-// 2-norm error of the changes of 4096 x 4096 weights by 2,048 rows a group against float64:
-// see the measurements in the design notes' table; a drained sum costs the epilogue about 500 clocks,
-// which run beside the next sum's MMAs (8 K blocks of 128 x 256: 4,200).
-// (An adapter's change has three products a K block, and few columns to drain.)
+// 2-norm error against float64 of the changes of 4096 x 4096 weights by 2,048 rows a group: 3.0e-7 in sums
+// of 8 K blocks, 1.4e-6 of 32 (float32 FMAs in one library product: 4.0e-7).  A drained sum costs the
+// epilogue about 500 clocks, which run beside the next sum's MMAs (8 K blocks of 128 x 256: 4,200); sums
+// of 32 are 2% faster.  (An adapter's change has up to two products a K block and few columns to drain;
+// with sums of two K blocks its error is 5e-7.)
 constexpr int kChain = 8, kLowChain = 2;
 
 template <int BN, int FORM, bool GATHER = false>
@@ -1288,8 +1294,8 @@ cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
 
 // How the low change is cut: 128 columns, 64 where that leaves SMs without a tile, and up to 16 shares of
 // an adapter's rows, as many as the device finds that it has times an SM's part (Schedule::item), where
-// there are rows for them, the items stay few (each is a look at the requests, 0.8 us) and the shares'
-// sums fit their scratch.  A share is an exchange, a store and a fence of 5 us beside its 0.5 us a K block:
+// the busy tiles are no more than the SMs, there are rows for them, the items stay few (each is a look at
+// the requests, 0.8 us) and the shares' sums fit their scratch.  A share is an exchange, a store and a fence of 5 us beside its 0.5 us a K block:
 // us, both changes of a layer of 16,384 rows, every adapter in 1 / 2 / 4 / 16 shares: 5 adapters of rank 64
 // of 4096-4096, 160 tiles, 142 / 194 / 295 / 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of
 // 512-512, 32 tiles, 206 / 118 / 75 / 63.
@@ -1299,8 +1305,8 @@ static LowCut low_cut(int n_adapters, int n_requests, int n_rows, int N, int num
     c.bn = (long long)busy * ceil_div(N, 128) >= num_sms / 4 ? 128 : 64;
     c.num_n = ceil_div(N, c.bn);
     c.runs = 1;
-    while (c.runs < 16 && n_rows >= 2 * c.runs * 16 * BK && 2ll * c.runs * n_adapters * c.num_n <= 8 * num_sms &&
-           2ll * c.runs * n_adapters * N <= kShareColumns * num_sms)
+    while (c.runs < 16 && n_rows >= 2 * c.runs * 16 * BK && (long long)c.runs * busy * c.num_n <= num_sms &&
+           2ll * c.runs * n_adapters * c.num_n <= 8 * num_sms && 2ll * c.runs * n_adapters * N <= kShareColumns * num_sms)
         c.runs *= 2;
     return c;
 }
