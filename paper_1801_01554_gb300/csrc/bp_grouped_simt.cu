@@ -354,6 +354,8 @@ __global__ void __launch_bounds__(kThreads) k_low_change_simt(LowChangeArgs g, C
     const int n_ad = g.req.n_adapters, z = blockIdx.z / n_ad, ad = blockIdx.z - z * n_ad;
     const int m0 = blockIdx.y * T, n0 = blockIdx.x * T, r = g.req.rank;
     const float* b = (const float*)g.b;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0)   // adapters out of range belong to no block
+        for (int i = threadIdx.x; i < g.req.n_requests; i += kThreads) request_adapter(g.req, i, g.flags);
     float acc[P][P] = {};
     for (int base = 0; base < g.req.n_requests; base += 32) {   // the adapter's requests, in order
         const int i = base + (threadIdx.x & 31);

@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                 group_rows(g.req.offsets, g.req.n_rows, i, lo, hi, g.flags);
                 s_lo[i] = lo;
                 s_hi[i] = hi;
-                s_tile0[i] = g.req.adapter[i];
+                s_tile0[i] = request_adapter(g.req, i, g.flags);
             }
     } else if (warp == 2) {
         // the groups' rows and first row blocks

@@ -66,6 +66,32 @@ def test_f32_matches_oracle(n, rank, n_in, n_out, rows, requests, squash):
     check(n, rank, n_in, n_out, rows, requests, bp.BP_F32, squash)
 
 
+# tiles of 128 with one request and with several; changes of long requests shared out
+@pytest.mark.parametrize("n,rank,n_in,n_out,rows,requests", [
+    (3, 24, 64, 1280, 2048, 3), (3, 24, 1280, 64, 2048, 3), (2, 8, 64, 48, 3000, 2)])
+def test_f32_large_tiles_and_shares(n, rank, n_in, n_out, rows, requests):
+    check(n, rank, n_in, n_out, rows, requests, bp.BP_F32, True, 3)
+
+
+@pytest.mark.parametrize("n,rank,n_in,n_out,rows,requests", [
+    (1, 100, 256, 192, 3000, 2), (2, 17, 512, 64, 4000, 3), (1, 64, 64, 4096, 2500, 1)])
+def test_bf16_changes_shared_out(n, rank, n_in, n_out, rows, requests):
+    check(n, rank, n_in, n_out, rows, requests, bp.BP_BF16, False, 4)
+
+
+@pytest.mark.parametrize("dtype", [bp.BP_F32, bp.BP_BF16])
+def test_a_bad_adapter_is_reported_by_a_change_alone(dtype):
+    rows = 40
+    p = problem(2, 8, 64, 32, rows, 2, dtype, False, 4, [0, 20, 40])
+    U, GB = torch.zeros(rows, 8, device="cuda"), empty((2, 8, 32), bp.BP_F32)
+    with bp.Adapters(2, 8, 64, 32, dtype, max_rows=rows, max_requests=2) as layer:
+        layer.backward(None, None, None, None, None, U, dev(p["offsets"]), dev(np.array([0, 2])), 2, rows, dev(p["D"], dtype),
+                       GB=GB)
+        with pytest.raises(bp.BPError) as e:
+            layer.check()
+        assert e.value.status == bp.BP_ESTATE
+
+
 @pytest.mark.parametrize("n,rank,n_in,n_out,rows,requests", [
     (1, 1, 8, 8, 1, 1), (7, 16, 256, 128, 1, 1), (50, 16, 1024, 264, 61, 61), (9, 8, 128, 64, 16, 16), (6, 32, 512, 392, 700, 11),
     (5, 64, 264, 520, 1025, 7), (3, 5, 72, 136, 130, 4), (2, 128, 320, 256, 400, 3), (4, 100, 136, 72, 257, 5),

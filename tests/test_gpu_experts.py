@@ -60,6 +60,33 @@ def test_f32_matches_oracle(E, n_in, n_out, rows, gather, squash):
     check(E, n_in, n_out, rows, bp.BP_F32, gather, squash)
 
 
+# tiles of 128 in each of the three products, rows on 16-byte boundaries and not; long groups shared out
+@pytest.mark.parametrize("E,n_in,n_out,rows", [
+    (1, 64, 1280, 2048), (1, 65, 1281, 2047), (1, 1280, 64, 2048), (1, 1281, 63, 2050), (1, 1280, 2048, 300),
+    (1, 1281, 2047, 300), (2, 64, 32, 5000), (3, 33, 130, 3000)])
+def test_f32_large_tiles_and_shares(E, n_in, n_out, rows):
+    check(E, n_in, n_out, rows, bp.BP_F32, True, True, 2)
+
+
+@pytest.mark.parametrize("dtype", [bp.BP_F32, bp.BP_BF16])
+def test_changes_off_32_bytes(dtype):
+    """G on a 16-byte boundary that is no 32-byte one (and, float32, inputs on a 4-byte one)."""
+    E, n_in, n_out, rows = 2, 264, 136, 300
+    X, W, b, D, _, offsets = problem(E, n_in, n_out, rows, dtype, False, False, 13)
+    buf = torch.full((E * n_out * n_in + 4,), float("nan"), device="cuda")
+    GW, Xd = buf[4:].view(E, n_out, n_in), dev(X, dtype)
+    assert GW.data_ptr() % 32 == 16
+    if dtype == bp.BP_F32:
+        shifted = torch.zeros(X.size + 1, device="cuda")[1:].view(rows, n_in)
+        Xd = shifted.copy_(Xd)
+    with bp.Experts(E, n_in, n_out, dtype, max_rows=rows) as layer:
+        layer.backward(None, Xd, rows, None, dev(offsets), rows, dev(D, dtype), GW=GW)
+        layer.check()
+    _, (ww, mw), _ = O.experts_backward(W, X, None, offsets, D, False)
+    assert_sum(host(GW), ww, mw, bp.BP_F32, what="GW")
+    assert torch.isnan(buf[:4]).all()
+
+
 # rows that end on, before and after 16-, 64- and 128-row blocks; widths off the tiles' 64 and 128
 @pytest.mark.parametrize("E,n_in,n_out,rows", [
     (1, 8, 8, 1), (4, 64, 32, 3), (16, 1024, 256, 10), (3, 72, 264, 129), (7, 320, 520, 500), (32, 128, 72, 1000),
