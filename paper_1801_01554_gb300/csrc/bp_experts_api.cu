@@ -574,17 +574,18 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
         a.flags = l->flags;
         st = cuda_status(rows_product(a, l->dtype, true, l->low_terms(), l->num_sms, s), call);
     }
-    const bool tc = l->dtype == BP_BF16;
-    if (st == BP_OK && ga) {
-        const LowChangeArgs a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->scratch, l->arrived, l->flags};
-        st = cuda_status(tc ? tc_low_change(a, l->low_terms(), l->num_sms, s) : simt_low_change(a, {l->scratch, l->arrived, 1}, l->num_sms, s), call);
-    }
-    if (st == BP_OK && gb) {
-        const LowChangeArgs a{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->scratch, l->arrived, l->flags};
-        LowTerms u = l->low_terms();
+    if (st != BP_OK || (!ga && !gb)) return st;
+    const LowChangeArgs of_a{req, l->n_in, l->low, d_X, nullptr, d_GA, accumulate, l->scratch, l->arrived, l->flags};
+    const LowChangeArgs of_b{req, l->n_out, d_U, d_D, d_scale, d_GB, accumulate, l->scratch, l->arrived, l->flags};
+    if (l->dtype == BP_BF16) {
+        const LowTerms v = l->low_terms();
+        LowTerms u = v;
         u.terms = l->u_terms;
-        st = cuda_status(tc ? tc_low_change(a, u, l->num_sms, s) : simt_low_change(a, {l->scratch, l->arrived, 1}, l->num_sms, s), call);
+        return cuda_status(tc_low_change(ga ? of_a : of_b, ga ? v : u, ga && gb ? &of_b : nullptr, u, l->num_sms, s), call);
     }
+    const ChangeShares room{l->scratch, l->arrived, 1};
+    if (ga) st = cuda_status(simt_low_change(of_a, room, l->num_sms, s), call);
+    if (st == BP_OK && gb) st = cuda_status(simt_low_change(of_b, room, l->num_sms, s), call);
     return st;
 }
 

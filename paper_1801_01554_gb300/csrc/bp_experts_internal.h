@@ -152,7 +152,9 @@ cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
 cudaError_t tc_low(const LowArgs& a, int num_sms, cudaStream_t s);
 size_t low_change_scratch(int rank, int num_sms);   // floats
 size_t low_change_counts(int n_adapters, int num_sms);
-cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, int num_sms, cudaStream_t s);
+// One launch of one change, or of two of the same requests (second NULL: one).
+cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, const LowChangeArgs* second, const LowTerms& second_low,
+                          int num_sms, cudaStream_t s);
 
 // The forward product of a few rows in bfloat16 (bp_few.cu), rows read through an index too; with low,
 // behind low_product, which a dependent launch overlaps.

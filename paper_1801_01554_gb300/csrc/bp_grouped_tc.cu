@@ -6,6 +6,7 @@
 //   change   G_g[m, n]  = sum over the group's rows of a[r, m] b[r, n]   both MN-major
 //   up       low[r, j]  = scale_a * sum over k of in[r, k] P_a[j, k], a the adapter of the row's request
 //   low      G_a[j, n]  = scale_a * sum over the rows of the adapter's requests of low[r, j] b[r, n]
+//            (of A and of B in one launch: twice the tiles to balance the SMs with)
 //
 // One persistent CTA per SM: a warp that issues TMA copies into a ring of stages, a warp that
 // issues tcgen05.mma (128 rows x BN columns x 64 of K a stage) into TMEM, eight epilogue warps.
@@ -76,9 +77,14 @@ struct TcArgs {
     const float* low;
     const bf16* P;
     const float* scale;
+    // of the low form: a second product's changes G2 [n_adapters, rank, N2], whose tiles follow the first's
+    int N2, num_n2;            // (num_n2 0: none)
+    float* G2;
+    const float* scale2;
+    int sectors2;
     int num_sms;
     int runs;                  // of the low form: most shares of an adapter's rows, of which the sums go to
-    float* scratch;            // [runs, n_adapters, rank, N]
+    float* scratch;            // [runs, n_adapters, rank, N], and behind it the second's
     unsigned* arrived;         // of every warp's part of a tile; zeros, left so
     // up
     float* low_out;
@@ -122,6 +128,7 @@ struct Item {
     int kbs;        // K blocks
     int kb0, kb1;   // of the low form: of the adapter's
     int run, shares;
+    bool second;    // of the low form: the second product
     int adapter;    // whose low-rank K follows; of an up product, the rows'; -1, or a kind of tile
     int request;    // the tile's first
 };
@@ -217,7 +224,7 @@ struct Schedule {
         return (h - l + BK - 1) / BK;
     }
     __device__ int items() const {
-        if (FORM == LOW) return g.req.n_adapters * g.num_n * g.runs;
+        if (FORM == LOW) return g.req.n_adapters * (g.num_n + g.num_n2) * g.runs;
         if (FORM == UP) return g.max_items;
         return FORM == CHANGE ? g.groups.n_groups * g.num_m * g.num_n : tile0[g.groups.n_groups] * g.num_n;
     }
@@ -225,11 +232,14 @@ struct Schedule {
         Item w;
         if (FORM == LOW) {
             // all tiles' first shares, then their second ones, ..: those that there are lie together
-            const int tiles = g.req.n_adapters * g.num_n;
+            const int first = g.req.n_adapters * g.num_n, tiles = first + g.req.n_adapters * g.num_n2;
             w.run = g.runs == 1 ? 0 : it / tiles;
-            const int tile = it - w.run * tiles;
-            w.g = tile / g.num_n;
-            w.nb = tile - w.g * g.num_n;
+            int tile = it - w.run * tiles;
+            w.second = tile >= first;
+            if (w.second) tile -= first;
+            const int num_n = w.second ? g.num_n2 : g.num_n;
+            w.g = tile / num_n;
+            w.nb = tile - w.g * num_n;
             w.mb = w.row0 = w.end = 0;
             w.adapter = w.request = -1;
             Stretches<LOW> all{g, w, table, 0, 0};
@@ -244,7 +254,7 @@ struct Schedule {
                     if ((table.adapter != nullptr ? table.adapter : g.req.adapter)[i] >= 0) all_blocks += table_blocks(i);
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) all_blocks += __shfl_xor_sync(0xffffffffu, all_blocks, o);
-                const int part = max((int)((long long)all_blocks * g.num_n / g.num_sms), 8);
+                const int part = max((int)((long long)all_blocks * (g.num_n + g.num_n2) / g.num_sms), 8);
                 w.shares = min(max((2 * blocks + part) / (2 * part), 1), g.runs);
             }
             const int share = blocks / w.shares, more = blocks - share * w.shares;   // the first `more` shares have one more
@@ -573,11 +583,13 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                             if (!open(a_blocks * kMnBlockBytes + C::kBBytes)) break;
                             uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
                             if (leader) {
+                                const CUtensorMap* ma = FORM == LOW && w.second ? &map_low : &map_a;
+                                const CUtensorMap* mb = FORM == LOW && w.second ? &map_p : &map_b;
                                 for (int i = 0; i < a_blocks; ++i)
-                                    tma_load_2d(sa + i * kMnBlockBytes, &map_a, w.mb * BM + 64 * i, r, &full[stage]);
+                                    tma_load_2d(sa + i * kMnBlockBytes, ma, w.mb * BM + 64 * i, r, &full[stage]);
 #pragma unroll
                                 for (int i = 0; i < BN / 64; ++i)
-                                    tma_load_2d(sb + i * kMnBlockBytes, &map_b, w.nb * BN + 64 * i, r, &full[stage]);
+                                    tma_load_2d(sb + i * kMnBlockBytes, mb, w.nb * BN + 64 * i, r, &full[stage]);
                             }
                             close();
                         }
@@ -905,54 +917,59 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                     __syncwarp();
                     if (q >= own) continue;
                 }
-                const float scale = FORM == LOW && g.scale != nullptr ? g.scale[w.g] : 1.f;
+                const bool second = FORM == LOW && w.second;
+                const int N = second ? g.N2 : g.N;
+                const float* scales = second ? g.scale2 : g.scale;
+                const float scale = FORM == LOW && scales != nullptr ? scales[w.g] : 1.f;
                 const int m0 = w.mb * BM + q * 32;
-                float* G = g.G + (size_t)w.g * g.M * g.N;
+                float* G = (second ? g.G2 : g.G) + (size_t)w.g * g.M * N;
                 if (FORM == LOW && w.shares > 1) {
                     // the run's sums to scratch; the last warp to arrive adds the runs' in their order
-                    if (m0 >= g.M || w.nb * BN + cbeg >= g.N) continue;
-                    const size_t plane = (size_t)g.req.n_adapters * g.M * g.N;
-                    float* mine = g.scratch + w.run * plane + (size_t)w.g * g.M * g.N;
+                    if (m0 >= g.M || w.nb * BN + cbeg >= N) continue;
+                    const size_t plane = (size_t)g.req.n_adapters * g.M * N;
+                    float* shared_out = g.scratch + (second ? (size_t)g.runs * g.req.n_adapters * g.M * g.N : 0);
+                    float* mine = shared_out + w.run * plane + (size_t)w.g * g.M * N;
 #pragma unroll
                     for (int c = 0; c < BN / 2; c += 16) {
                         const int n0 = w.nb * BN + cbeg + c;
-                        if (n0 >= g.N) break;
+                        if (n0 >= N) break;
                         float v[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) v[i] = part[c + i];
-                        store_change(mine, g.M, g.N, m0, n0, v, 0, reinterpret_cast<float4*>(sS4));
+                        store_change(mine, g.M, N, m0, n0, v, 0, reinterpret_cast<float4*>(sS4));
                     }
                     __threadfence();
                     __syncwarp();
                     unsigned before = 0;
-                    unsigned* count = g.arrived + ((size_t)w.g * g.num_n + w.nb) * kEpiWarps + ew;
+                    unsigned* count = g.arrived + (second ? (size_t)g.req.n_adapters * g.num_n * kEpiWarps : 0) +
+                                      ((size_t)w.g * (second ? g.num_n2 : g.num_n) + w.nb) * kEpiWarps + ew;
                     if (lane == 0) before = atomicAdd(count, 1u);
                     before = __shfl_sync(0xffffffffu, before, 0);
                     if (before != (unsigned)w.shares - 1) continue;
                     if (lane == 0) *count = 0u;
                     __threadfence();
-                    const float* all = g.scratch + (size_t)w.g * g.M * g.N;
+                    const float* all = shared_out + (size_t)w.g * g.M * N;
                     // pieces of four columns: lane + 32 i of the part's, by rows; all loads of a run under way at once
                     constexpr int kPer = BN / 2 / 4;   // of a row
                     float4 sum[kPer];
 #pragma unroll
                     for (int i = 0; i < kPer; ++i) sum[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                     // rows and columns past the last ones read the last ones, so that no load hangs on a condition
-                    const float* at = all + (size_t)min(m0 + lane / kPer, g.M - 1) * g.N + min(w.nb * BN + cbeg + lane % kPer * 4, g.N - 4);
+                    const float* at = all + (size_t)min(m0 + lane / kPer, g.M - 1) * N + min(w.nb * BN + cbeg + lane % kPer * 4, N - 4);
                     for (int z = 0; z < w.shares; ++z) {
 #pragma unroll
                         for (int i = 0; i < kPer; ++i) {
                             const int row = min(32 / kPer * i, max(g.M - 1 - m0 - lane / kPer, 0));
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(at + z * plane + (size_t)row * g.N));
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(at + z * plane + (size_t)row * N));
                             sum[i].x += x.x, sum[i].y += x.y, sum[i].z += x.z, sum[i].w += x.w;
                         }
                     }
 #pragma unroll
                     for (int i = 0; i < kPer; ++i) {
                         const int m = m0 + (lane + 32 * i) / kPer, n = w.nb * BN + cbeg + (lane + 32 * i) % kPer * 4;
-                        if (m >= g.M || n >= g.N) continue;
+                        if (m >= g.M || n >= N) continue;
                         float4 o = make_float4(scale * sum[i].x, scale * sum[i].y, scale * sum[i].z, scale * sum[i].w);
-                        float4* to = reinterpret_cast<float4*>(G + (size_t)m * g.N + n);
+                        float4* to = reinterpret_cast<float4*>(G + (size_t)m * N + n);
                         if (g.accumulate) {
                             const float4 old = *to;
                             o.x += old.x, o.y += old.y, o.z += old.z, o.w += old.w;
@@ -964,14 +981,14 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
 #pragma unroll
                 for (int c = 0; c < BN / 2; c += 16) {
                     const int n0 = w.nb * BN + cbeg + c;
-                    if (m0 >= g.M || n0 >= g.N) break;
+                    if (m0 >= g.M || n0 >= N) break;
                     float v[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) v[i] = scale * part[c + i];
-                    if (g.sectors && !g.accumulate) {
-                        if (m0 + lane < g.M) store_sectors(G + (size_t)(m0 + lane) * g.N + n0, v, g.N - n0);
+                    if ((second ? g.sectors2 : g.sectors) && !g.accumulate) {
+                        if (m0 + lane < g.M) store_sectors(G + (size_t)(m0 + lane) * N + n0, v, N - n0);
                     } else {
-                        store_change(G, g.M, g.N, m0, n0, v, g.accumulate, reinterpret_cast<float4*>(sS4));
+                        store_change(G, g.M, N, m0, n0, v, g.accumulate, reinterpret_cast<float4*>(sS4));
                     }
                 }
             } else {
@@ -1143,7 +1160,7 @@ int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 constexpr int kShareColumns = 1024;   // an SM
 struct LowCut {
-    int bn, num_n, runs;
+    int bn, num_n, num_n2, runs;
 };
 
 // Tile width for row_tiles blocks of 128 rows: the time of the waves of tiles, at the clocks that
@@ -1299,14 +1316,16 @@ cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
 // us, both changes of a layer of 16,384 rows, every adapter in 1 / 2 / 4 / 16 shares: 5 adapters of rank 64
 // of 4096-4096, 160 tiles, 142 / 194 / 295 / 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of
 // 512-512, 32 tiles, 206 / 118 / 75 / 63.
-static LowCut low_cut(int n_adapters, int n_requests, int n_rows, int N, int num_sms) {
+static LowCut low_cut(int n_adapters, int n_requests, int n_rows, int N, int N2, int num_sms) {
     const int busy = n_adapters < n_requests ? n_adapters : n_requests;
     LowCut c;
-    c.bn = (long long)busy * ceil_div(N, 128) >= num_sms / 4 ? 128 : 64;
+    c.bn = (long long)busy * (ceil_div(N, 128) + ceil_div(N2, 128)) >= num_sms / 4 ? 128 : 64;
     c.num_n = ceil_div(N, c.bn);
+    c.num_n2 = ceil_div(N2, c.bn);
     c.runs = 1;
-    while (c.runs < 16 && n_rows >= 2 * c.runs * 16 * BK && (long long)c.runs * busy * c.num_n <= num_sms &&
-           2ll * c.runs * n_adapters * c.num_n <= 8 * num_sms && 2ll * c.runs * n_adapters * N <= kShareColumns * num_sms)
+    const long long tiles = c.num_n + c.num_n2;
+    while (c.runs < 16 && n_rows >= 2 * c.runs * 16 * BK && c.runs * busy * tiles <= num_sms &&
+           2 * c.runs * n_adapters * tiles <= 8 * num_sms && 2ll * c.runs * n_adapters * ((long long)N + N2) <= kShareColumns * num_sms)
         c.runs *= 2;
     return c;
 }
@@ -1314,10 +1333,11 @@ static LowCut low_cut(int n_adapters, int n_requests, int n_rows, int N, int num
 // Of any call of a layer: columns of shares, and the warps' parts of 64 of them.
 size_t low_change_scratch(int rank, int num_sms) { return (size_t)kShareColumns * num_sms * rank; }
 size_t low_change_counts(int n_adapters, int num_sms) {
-    return ((size_t)kShareColumns / 64 * num_sms + n_adapters) * kEpiWarps;
+    return ((size_t)kShareColumns / 64 * num_sms + 2 * n_adapters) * kEpiWarps;
 }
 
-cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, int num_sms, cudaStream_t s) {
+cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, const LowChangeArgs* c2, const LowTerms& low2, int num_sms,
+                          cudaStream_t s) {
     TcArgs a{};
     a.req = c.req;
     a.M = c.req.rank;
@@ -1326,22 +1346,30 @@ cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, int num_s
     a.scale = c.scale;
     a.accumulate = c.accumulate;
     a.sectors = ((uintptr_t)c.G & 31) == 0;
+    if (c2 != nullptr) {
+        a.N2 = c2->N;
+        a.G2 = c2->G;
+        a.scale2 = c2->scale;
+        a.sectors2 = ((uintptr_t)c2->G & 31) == 0;
+    }
     a.n_terms = low.n_terms;
     a.stride = low.stride;
     a.flags = c.flags;
-    const LowCut cut = low_cut(c.req.n_adapters, c.req.n_requests, c.req.n_rows, c.N, num_sms);
+    const LowCut cut = low_cut(c.req.n_adapters, c.req.n_requests, c.req.n_rows, c.N, a.N2, num_sms);
     a.num_n = cut.num_n;
+    a.num_n2 = cut.num_n2;
     a.runs = cut.runs;
     a.num_sms = num_sms;
     a.scratch = c.scratch;
     a.arrived = c.arrived;
     CUtensorMap m[4];
-    const bool rows = c.req.n_rows > 0;   // (tc_change)
-    if (!make_map(&m[0], rows ? low.terms : c.G, rows ? c.req.n_rows : 1, low.n_terms * low.stride, 0, BK) ||
-        !make_map(&m[1], rows ? c.b : c.G, rows ? c.req.n_rows : 1, c.N, 0, BK))
-        return cudaErrorInvalidValue;
-    m[2] = m[3] = m[0];
-    const long long items = (long long)c.req.n_adapters * a.num_n * a.runs;
+    auto maps = [&](const LowChangeArgs& x, const LowTerms& l, CUtensorMap* to) {
+        const bool rows = x.req.n_rows > 0;   // (tc_change)
+        return make_map(&to[0], rows ? l.terms : x.G, rows ? x.req.n_rows : 1, l.n_terms * l.stride, 0, BK) &&
+               make_map(&to[1], rows ? x.b : x.G, rows ? x.req.n_rows : 1, x.N, 0, BK);
+    };
+    if (!maps(c, low, &m[0]) || !maps(c2 != nullptr ? *c2 : c, c2 != nullptr ? low2 : low, &m[2])) return cudaErrorInvalidValue;
+    const long long items = (long long)c.req.n_adapters * (a.num_n + a.num_n2) * a.runs;
     return launch<LOW>(a, cut.bn, items < num_sms ? (int)items : num_sms, num_sms, m, s);
 }
 
