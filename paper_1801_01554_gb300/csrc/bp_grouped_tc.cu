@@ -1206,16 +1206,8 @@ cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGro
     int x = 32;
     while (x < 256 && x * 4 < pieces) x *= 2;   // threads of a row
     const int per = 256 / x, want = ceil_div(groups.n_rows, per);
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t c{};
-    c.gridDim = dim3(want < 8 * num_sms ? want : 8 * num_sms);
-    c.blockDim = dim3(x, per);
-    c.stream = s;
-    c.attrs = at;
-    c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, k_gather, (const uint4*)in, source, n_src, groups, pieces, (uint4*)out, flags);
+    return launch_pdl_grid(k_gather, dim3(want < 8 * num_sms ? want : 8 * num_sms), dim3(x, per), 0, s, (const uint4*)in, source, n_src,
+                           groups, pieces, (uint4*)out, flags);
 }
 
 cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_sms, cudaStream_t s) {

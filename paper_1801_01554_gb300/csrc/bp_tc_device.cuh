@@ -265,18 +265,22 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
 
 // Launch whose setup may overlap the previous kernel's tail (the kernel calls pdl_wait).
 template <class... P, class... A>
-cudaError_t launch_pdl(void (*k)(P...), int grid_x, int grid_y, int threads, size_t smem, cudaStream_t s, A&&... args) {
+cudaError_t launch_pdl_grid(void (*k)(P...), dim3 grid, dim3 threads, size_t smem, cudaStream_t s, A&&... args) {
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3(grid_x, grid_y);
-    c.blockDim = dim3(threads);
+    c.gridDim = grid;
+    c.blockDim = threads;
     c.dynamicSmemBytes = smem;
     c.stream = s;
     c.attrs = at;
     c.numAttrs = 1;
     return cudaLaunchKernelEx(&c, k, std::forward<A>(args)...);
+}
+template <class... P, class... A>
+cudaError_t launch_pdl(void (*k)(P...), int grid_x, int grid_y, int threads, size_t smem, cudaStream_t s, A&&... args) {
+    return launch_pdl_grid(k, dim3(grid_x, grid_y), dim3(threads), smem, s, std::forward<A>(args)...);
 }
 
 }  // namespace
