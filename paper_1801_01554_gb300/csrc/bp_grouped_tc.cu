@@ -1301,13 +1301,13 @@ cudaError_t tc_low(const LowArgs& l, int num_sms, cudaStream_t s) {
     return launch<UP>(a, bn, a.max_items < num_sms ? a.max_items : num_sms, num_sms, m, s);
 }
 
-// How the low change is cut: 128 columns, 64 where that leaves SMs without a tile, and up to 16 shares of
+// How a low change is cut: 128 columns, 64 where that leaves SMs without a tile, and up to 16 shares of
 // an adapter's rows, as many as the device finds that it has times an SM's part (Schedule::item), where
 // the busy tiles are no more than the SMs, there are rows for them, the items stay few (each is a look at
-// the requests, 0.8 us) and the shares' sums fit their scratch.  A share is an exchange, a store and a fence of 5 us beside its 0.5 us a K block:
-// us, both changes of a layer of 16,384 rows, every adapter in 1 / 2 / 4 / 16 shares: 5 adapters of rank 64
-// of 4096-4096, 160 tiles, 142 / 194 / 295 / 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of
-// 512-512, 32 tiles, 206 / 118 / 75 / 63.
+// the requests, 0.8 us) and the shares' sums fit their scratch.  A share is an exchange, a store and a
+// fence of 5 us beside its 0.5 us a K block: us of both changes of a layer of 16,384 rows, a launch each,
+// every adapter in 1 / 2 / 4 / 16 shares: 5 adapters of rank 64 of 4096-4096, 160 tiles, 142 / 194 / 295 /
+// 297; one of rank 16, 64 tiles, 233 / 145 / 159 / 268; 4 of 512-512, 32 tiles, 206 / 118 / 75 / 63.
 static LowCut low_cut(int n_adapters, int n_requests, int n_rows, int N, int N2, int num_sms) {
     const int busy = n_adapters < n_requests ? n_adapters : n_requests;
     LowCut c;
