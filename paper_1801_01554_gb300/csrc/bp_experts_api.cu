@@ -108,6 +108,10 @@ bp_status make_layer(int dtype, int** flags, int* num_sms, const char* call) {
     return cuda_status(e, call);
 }
 
+bp_status make_floats(float** p, size_t n, const char* call) {
+    return n == 0 ? BP_OK : cuda_status(cudaMalloc(p, n * sizeof(float)), call);
+}
+
 // Zeros that blocks count their arrivals with.
 bp_status make_counts(unsigned** counts, size_t n, const char* call) {
     cudaError_t e = cudaMalloc(counts, n * sizeof(unsigned));
@@ -276,7 +280,7 @@ bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int m
     if (st == BP_OK) st = cuda_status(cudaMalloc(&l->sums, planes * cells * sizeof(float)), call);
     if (st == BP_OK) st = make_counts(&l->arrived, cells, call);
     if (st == BP_OK && dtype == BP_F32) {
-        st = cuda_status(cudaMalloc(&l->shares.scratch, simt_change_scratch(l->num_sms) * sizeof(float)), call);
+        st = make_floats(&l->shares.scratch, simt_change_scratch(n_experts, n_experts, (size_t)n_in * n_out, max_rows, l->num_sms), call);
         if (st == BP_OK) st = make_counts(&l->shares.arrived, simt_change_counts(l->num_sms), call);
     }
     if (st != BP_OK) {
@@ -441,8 +445,9 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
             st = cuda_status(cudaMalloc(&l->tiles, ((size_t)max_rows / kTileRows + 1) * sizeof(int2)), call);
     }
     if (st == BP_OK) {
-        const size_t floats = dtype == BP_BF16 ? low_change_scratch(rank, l->num_sms) : simt_change_scratch(l->num_sms);
-        st = cuda_status(cudaMalloc(&l->scratch, floats * sizeof(float)), call);
+        const size_t cells = (size_t)rank * (n_in > n_out ? n_in : n_out);
+        st = make_floats(&l->scratch, dtype == BP_BF16 ? low_change_scratch(n_adapters, rank, n_in + n_out, max_rows, l->num_sms)
+                                                       : simt_change_scratch(n_adapters, 1, cells, max_rows, l->num_sms), call);
     }
     if (st == BP_OK)
         st = make_counts(&l->arrived, dtype == BP_BF16 ? low_change_counts(n_adapters, l->num_sms) : simt_change_counts(l->num_sms), call);

@@ -125,7 +125,8 @@ struct ChangeShares {
     unsigned* arrived;
     int shares;             // (set by the launchers)
 };
-size_t simt_change_scratch(int num_sms);   // floats
+// Floats of scratch for changes of `cells` values in each of `groups` groups, at least `least_busy` with rows.
+size_t simt_change_scratch(int groups, int least_busy, size_t cells, int max_rows, int num_sms);
 size_t simt_change_counts(int num_sms);
 cudaError_t simt_change(const ChangeArgs& a, const ChangeShares& room, int num_sms, cudaStream_t s);
 cudaError_t simt_low_change(const LowChangeArgs& a, const ChangeShares& room, int num_sms, cudaStream_t s);
@@ -150,7 +151,7 @@ cudaError_t tc_gather(const void* in, const int* source, int n_src, const RowGro
 cudaError_t tc_rows(const RowsArgs& a, bool back, const LowTerms& low, int num_sms, cudaStream_t s);
 cudaError_t tc_change(const ChangeArgs& a, int num_sms, cudaStream_t s);
 cudaError_t tc_low(const LowArgs& a, int num_sms, cudaStream_t s);
-size_t low_change_scratch(int rank, int num_sms);   // floats
+size_t low_change_scratch(int n_adapters, int rank, int columns, int max_rows, int num_sms);   // floats
 size_t low_change_counts(int n_adapters, int num_sms);
 // One launch of one change, or of two of the same requests (second NULL: one).
 cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, const LowChangeArgs* second, const LowTerms& second_low,

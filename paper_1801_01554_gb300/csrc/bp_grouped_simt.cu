@@ -436,8 +436,13 @@ static int change_shares(long long tiles, int groups, int busy, int n_rows, int 
     while (shares < 64 && tiles * groups * shares * 2 <= 4 * num_sms && n_rows / (2ll * busy * shares) >= 128) shares *= 2;
     return shares;
 }
-// Of any call: tiles of all shares are at most four an SM where there are several.
-size_t simt_change_scratch(int num_sms) { return (size_t)4 * num_sms * 128 * 128; }
+// Of any call of a layer: tiles of all shares are at most four an SM where there are several.
+size_t simt_change_scratch(int groups, int least_busy, size_t cells, int max_rows, int num_sms) {
+    size_t shares = 1;
+    while (shares < 64 && max_rows / (2ll * least_busy * (long long)shares) >= 128) shares *= 2;
+    const size_t most = (size_t)4 * num_sms * 128 * 128, all = shares * groups * cells;
+    return shares == 1 ? 0 : all < most ? all : most;
+}
 size_t simt_change_counts(int num_sms) { return (size_t)4 * num_sms; }
 
 cudaError_t simt_change(const ChangeArgs& a, const ChangeShares& room, int num_sms, cudaStream_t s) {

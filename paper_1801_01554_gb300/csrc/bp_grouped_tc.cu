@@ -1159,6 +1159,7 @@ cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtens
 int ceil_div(long long a, long long b) { return (int)((a + b - 1) / b); }
 
 constexpr int kShareColumns = 1024;   // an SM
+constexpr int kMaxShares = 16, kShareRows = 16 * BK;   // of an adapter; rows that a share is for
 struct LowCut {
     int bn, num_n, num_n2, runs;
 };
@@ -1316,14 +1317,18 @@ static LowCut low_cut(int n_adapters, int n_requests, int n_rows, int N, int N2,
     c.num_n2 = ceil_div(N2, c.bn);
     c.runs = 1;
     const long long tiles = c.num_n + c.num_n2;
-    while (c.runs < 16 && n_rows >= 2 * c.runs * 16 * BK && c.runs * busy * tiles <= num_sms &&
+    while (c.runs < kMaxShares && n_rows >= 2 * c.runs * kShareRows && c.runs * busy * tiles <= num_sms &&
            2 * c.runs * n_adapters * tiles <= 8 * num_sms && 2ll * c.runs * n_adapters * ((long long)N + N2) <= kShareColumns * num_sms)
         c.runs *= 2;
     return c;
 }
 
 // Of any call of a layer: columns of shares, and the warps' parts of 64 of them.
-size_t low_change_scratch(int rank, int num_sms) { return (size_t)kShareColumns * num_sms * rank; }
+size_t low_change_scratch(int n_adapters, int rank, int columns, int max_rows, int num_sms) {
+    if (max_rows < 2 * kShareRows) return 0;
+    const size_t most = (size_t)kShareColumns * num_sms, all = (size_t)kMaxShares * n_adapters * columns;
+    return rank * (all < most ? all : most);
+}
 size_t low_change_counts(int n_adapters, int num_sms) {
     return ((size_t)kShareColumns / 64 * num_sms + 2 * n_adapters) * kEpiWarps;
 }
