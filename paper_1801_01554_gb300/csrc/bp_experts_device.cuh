@@ -117,8 +117,10 @@ __device__ __forceinline__ void step_products(float (&acc)[NA][NB][4], const uin
 
 // Loads straight into registers, B steps under way.  No load hangs on a condition but in the last,
 // short step.
-template <int NA, int NB, int B>
-__device__ __forceinline__ void direct_products(float (&acc)[NA][NB][4], const __nv_bfloat16* (&a)[NA][2],
+// PART > 0: after PART steps a sum is added to the total by rounding to nearest, because mma.sync truncates
+// as it accumulates (a sum of positive products comes out 7e-8 of itself too small for every 16 of them).
+template <int NA, int NB, int B, int PART = 0>
+__device__ __forceinline__ void direct_products(float (&total)[NA][NB][4], const __nv_bfloat16* (&a)[NA][2],
                                                 const __nv_bfloat16* (&b)[NB], const __nv_bfloat16* any, int K, int first,
                                                 int step) {
     const int k8 = (threadIdx.x & 3) * 8, whole = K / 32;
@@ -128,7 +130,16 @@ __device__ __forceinline__ void direct_products(float (&acc)[NA][NB][4], const _
         for (int h = 0; h < 2; ++h) a[m][h] = a[m][h] != nullptr ? a[m][h] : any + k8;
 #pragma unroll
     for (int c = 0; c < NB; ++c) b[c] = b[c] != nullptr ? b[c] : any + k8;
-    int k = first;
+    int k = first, steps = 0;
+    float acc[NA][NB][4] = {};
+    auto add = [&] {
+#pragma unroll
+        for (int m = 0; m < NA; ++m)
+#pragma unroll
+            for (int c = 0; c < NB; ++c)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) total[m][c][i] += acc[m][c][i], acc[m][c][i] = 0.f;
+    };
     auto load = [](const __nv_bfloat16* p) {   // volatile: ptxas may not sink it to its use
         uint4 u;
         asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
@@ -149,7 +160,14 @@ __device__ __forceinline__ void direct_products(float (&acc)[NA][NB][4], const _
         for (int i = 0; i < n; ++i) step_products<NA, NB>(acc, x[i], y[i]);
         k += n * step;
     };
-    while (k + (B - 1) * step < whole) batch(std::integral_constant<int, B>{});
+    while (k + (B - 1) * step < whole) {
+        batch(std::integral_constant<int, B>{});
+        if constexpr (PART > 0) {
+            static_assert(PART % B == 0);
+            steps += B;
+            if (steps % PART == 0) add();
+        }
+    }
     while (k < whole) batch(std::integral_constant<int, 1>{});
     if (k == whole && k * 32 < K) {   // this warp has the rest of K
         const bool in = k * 32 + k8 < K;
@@ -163,6 +181,7 @@ __device__ __forceinline__ void direct_products(float (&acc)[NA][NB][4], const _
         for (int c = 0; c < NB; ++c) y[c] = in ? *reinterpret_cast<const uint4*>(b[c] + k * 32) : zero;
         step_products<NA, NB>(acc, x, y);
     }
+    add();
 }
 
 // Loads through S steps of shared memory by cp.async, each lane reading back what it copied itself: no

@@ -203,7 +203,10 @@ cudaError_t few_setup() {
 // us of the experts' forward here / on tcgen05: 32 rows of 512-512 in 8 groups 6.8 / 10.8, 16 of 1024-1024 in
 // 4 8.8 / 12.9, 48 of 2048-2048 in 16 26.2 / 21.2, 100 of 2048-2048 in 16 39.6 / 25.2 (16 rows a pass:
 // larger groups read their weights again).
-bool few_ok(int n_rows, int n_groups) {
+// A warp's sum is one chain of mma.sync, which truncates: up to 128 steps of 16 of K, as in a part of the
+// tcgen05 products.
+bool few_ok(int n_rows, int n_groups, int K) {
+    if (K > 128 * 16 * kWarps) return false;
     if (n_groups == 1) return n_rows <= 64;
     const int busy = n_groups < n_rows ? n_groups : n_rows;
     return n_rows <= 4 * busy && n_rows <= 512;

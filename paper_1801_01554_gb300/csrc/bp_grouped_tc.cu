@@ -443,6 +443,11 @@ __device__ __forceinline__ void add_low(const TcArgs& g, int row, int adapter, i
 // of 32 are 2% faster.  (An adapter's change has up to two products a K block and few columns to drain;
 // with sums of two K blocks its error is 5e-7.)
 constexpr int kChain = 8, kLowChain = 2;
+// And of outputs and hidden deltas, which leave as bfloat16 (an adapter's K of up to 16 steps comes on top):
+// the sum of positive products comes out too small by 1e-7 a step of 16, 1.6e-3 over 2^18 products in one
+// accumulator, 1.2e-5 in parts of 32 K blocks.  The next part's accumulator takes the last one's sum in, for
+// which the MMAs wait once a part: 16,384 rows of 4096-4096 take 1% longer.
+constexpr int kRowChain = 32;
 
 template <int BN, int FORM, bool GATHER = false>
 __global__ void __launch_bounds__(threads_of(GATHER), 1)
@@ -703,7 +708,7 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                         }
                     }
                 } else {
-                    const int chain = FORM == UP ? kChain : w.kbs;
+                    constexpr int chain = FORM == UP ? kChain : kRowChain;
                     for (int k0 = 0; k0 < w.kbs && ok; k0 += chain) {
                         const int k1 = min(w.kbs, k0 + chain);
                         if (!wait(&tempty[acc], acc_phase ^ 1u)) break;
@@ -734,8 +739,8 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                                         close();
                                     }
                             };
-                            if (ok && w.adapter >= 0) add_low(false);
-                            if (ok && w.adapter == kTileMixed) {
+                            if (ok && k1 == w.kbs && w.adapter >= 0) add_low(false);
+                            if (ok && k1 == w.kbs && w.adapter == kTileMixed) {
                                 TileRequests all{g, w, w.request};
                                 int lo, hi, adapter;
                                 while (ok && all.next(lo, hi, adapter)) {
@@ -1020,29 +1025,32 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                     }
                 }
                 if (!wait_acc()) break;
-                if (!GATHER && w.adapter == kTileMixed) {
-                    // each request's sums: its rows, with the sums so far, replace them
+                // The next accumulator, with the sums so far added to its own or, in rows that its own are
+                // not for, in place of them.
+                auto join = [&](bool mine) {
+                    const int before = acc;
+                    next_acc();
+                    if (!wait_acc()) return false;
+#pragma unroll 1
+                    for (int c = 0; c < BN / 2; c += 16) {
+                        float x[16], v[16];
+                        tmem_ld16(trow + (uint32_t)(before * BN + cbeg + c), x);
+                        tmem_ld16(trow + (uint32_t)(acc * BN + cbeg + c), v);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) v[k] = mine ? x[k] + v[k] : x[k];
+                        tmem_st16(trow + (uint32_t)(acc * BN + cbeg + c), v);
+                    }
+                    tmem_wait_st();
+                    free_acc(before);
+                    return true;
+                };
+                bool stay = true;
+                for (int k0 = kRowChain; k0 < w.kbs && stay; k0 += kRowChain) stay = join(true);
+                if (!stay) break;
+                if (!GATHER && w.adapter == kTileMixed) {   // each request's sums, for its rows
                     TileRequests all{g, w, w.request};
                     int lo, hi, a;
-                    bool stay = true;
-                    while (all.next(lo, hi, a)) {
-                        const int before = acc;
-                        next_acc();
-                        stay = wait_acc();
-                        if (!stay) break;
-                        const bool mine = row >= lo && row < hi;
-#pragma unroll 1
-                        for (int c = 0; c < BN / 2; c += 16) {
-                            float x[16], v[16];
-                            tmem_ld16(trow + (uint32_t)(before * BN + cbeg + c), x);
-                            tmem_ld16(trow + (uint32_t)(acc * BN + cbeg + c), v);
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) v[k] = mine ? x[k] + v[k] : x[k];
-                            tmem_st16(trow + (uint32_t)(acc * BN + cbeg + c), v);
-                        }
-                        tmem_wait_st();
-                        free_acc(before);
-                    }
+                    while (stay && all.next(lo, hi, a)) stay = join(row >= lo && row < hi);
                     if (!stay) break;
                 }
 #pragma unroll 1

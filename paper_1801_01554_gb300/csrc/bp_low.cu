@@ -14,6 +14,8 @@ namespace bp {
 namespace {
 
 constexpr int kRows = 64, kThreads = 256, kWarps = kThreads / 32;
+// Steps of 32 of a warp's sum in one part (direct_products): the sums are float32 results.
+constexpr int kPart = 16;
 
 // The unit-th run of up to kRows rows of one request; the whole block calls it.  Request, first row
 // and end, or request -1 past the last unit.
@@ -108,7 +110,7 @@ __device__ __forceinline__ void low_rows(const LowArgs& g, float scale_low, floa
 #pragma unroll
     for (int n = 0; n < NT; ++n) p[n] = j0 + 8 * n + gr < r ? P + (size_t)(j0 + 8 * n + gr) * g.K + k8 : nullptr;
     float acc[MT][NT][4] = {};
-    direct_products<MT, NT, (MT == 1 ? 4 : 2)>(acc, x, p, in, g.K, kw, k_warps);
+    direct_products<MT, NT, (MT == 1 ? 4 : 2), kPart>(acc, x, p, in, g.K, kw, k_warps);
     for (int s = k_warps / 2; s >= 1; s >>= 1) {
         __syncthreads();
         float* at = red + (size_t)((kw % s) * rank_warps + nw) * MT * NT * 128 + lane;
