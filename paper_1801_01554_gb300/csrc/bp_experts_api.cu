@@ -31,6 +31,7 @@ struct bp_adapters {
     float* low = nullptr;   // [cap, rank] v of the backward pass
     float* scratch = nullptr;      // changes of shares of the rows
     unsigned* arrived = nullptr;
+    size_t n_counts = 0;
     // bfloat16: u or v as bfloat16 terms, u's for its change, and what row blocks hold
     void* terms = nullptr;
     void* u_terms = nullptr;
@@ -96,7 +97,7 @@ bp_status check_units(const char* call, int n_in, int n_out, int dtype) {
     return st;
 }
 
-// A layer's error word; the device's SMs and, for bfloat16, its kernels' set-up.
+// A layer's error word (zero once layer_ready has returned); the device's SMs and, for bfloat16, its kernels' set-up.
 bp_status make_layer(int dtype, int** flags, int* num_sms, const char* call) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -112,18 +113,30 @@ bp_status make_floats(float** p, size_t n, const char* call) {
     return n == 0 ? BP_OK : cuda_status(cudaMalloc(p, n * sizeof(float)), call);
 }
 
-// Zeros that blocks count their arrivals with.
+// Zeros that blocks count their arrivals with (there once layer_ready has returned).
 bp_status make_counts(unsigned** counts, size_t n, const char* call) {
     cudaError_t e = cudaMalloc(counts, n * sizeof(unsigned));
     if (e == cudaSuccess) e = cudaMemset(*counts, 0, n * sizeof(unsigned));
     return cuda_status(e, call);
 }
 
-bp_status read_flags(int* flags, void* stream, const char* call) {
+// The memsets of a new layer run on the legacy default stream, behind what it has queued: waited for, as the
+// layer's first call may be on a stream that does not wait for that one.
+bp_status layer_ready(const char* call) { return cuda_status(cudaStreamSynchronize(cudaStreamLegacy), call); }
+
+// Waits for the stream, then reports and clears the error word, and after a wait that ran out the counts
+// (n_counts of them) that its launch left behind.  All on that stream and waited for: the next call
+// may be on any.
+bp_status read_flags(int* flags, unsigned* counts, size_t n_counts, void* stream, const char* call) {
+    cudaStream_t s = (cudaStream_t)stream;
     int f = 0;
-    cudaError_t e = cudaStreamSynchronize((cudaStream_t)stream);
-    if (e == cudaSuccess) e = cudaMemcpy(&f, flags, sizeof f, cudaMemcpyDeviceToHost);
-    if (e == cudaSuccess && f != 0) e = cudaMemset(flags, 0, sizeof f);
+    cudaError_t e = cudaMemcpyAsync(&f, flags, sizeof f, cudaMemcpyDeviceToHost, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess && f != 0) {
+        e = cudaMemsetAsync(flags, 0, sizeof f, s);
+        if (e == cudaSuccess && (f & kFlagTimeout) && n_counts > 0) e = cudaMemsetAsync(counts, 0, n_counts * sizeof(unsigned), s);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    }
     if (e != cudaSuccess) return cuda_status(e, call);
     if (f & kFlagTimeout)
         return fail(BP_ETIMEOUT, "a bounded device-side wait ran out; the launch stopped early");
@@ -283,6 +296,7 @@ bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int m
         st = make_floats(&l->shares.scratch, simt_change_scratch(n_experts, n_experts, (size_t)n_in * n_out, max_rows, l->num_sms), call);
         if (st == BP_OK) st = make_counts(&l->shares.arrived, simt_change_counts(l->num_sms), call);
     }
+    if (st == BP_OK) st = layer_ready(call);
     if (st != BP_OK) {
         bp_experts_destroy(l);
         return st;
@@ -407,7 +421,7 @@ bp_status bp_experts_backward(bp_experts* l, const void* d_W, const void* d_X, i
 
 bp_status bp_experts_check(bp_experts* l, void* stream) {
     if (l == nullptr) return fail(BP_EINVAL, "bp_experts_check: NULL layer");
-    return read_flags(l->flags, stream, "bp_experts_check");
+    return read_flags(l->flags, nullptr, 0, stream, "bp_experts_check");   // (its counting launches do not wait)
 }
 
 // ------------------------------------------------------------ adapters
@@ -449,8 +463,9 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
         st = make_floats(&l->scratch, dtype == BP_BF16 ? low_change_scratch(n_adapters, rank, n_in + n_out, max_rows, l->num_sms)
                                                        : simt_change_scratch(n_adapters, 1, cells, max_rows, l->num_sms), call);
     }
-    if (st == BP_OK)
-        st = make_counts(&l->arrived, dtype == BP_BF16 ? low_change_counts(n_adapters, l->num_sms) : simt_change_counts(l->num_sms), call);
+    l->n_counts = dtype == BP_BF16 ? low_change_counts(n_adapters, l->num_sms) : simt_change_counts(l->num_sms);
+    if (st == BP_OK) st = make_counts(&l->arrived, l->n_counts, call);
+    if (st == BP_OK) st = layer_ready(call);
     if (st != BP_OK) {
         bp_adapters_destroy(l);
         return st;
@@ -597,12 +612,7 @@ bp_status bp_adapters_backward(bp_adapters* l, const void* d_W, const void* d_A,
 bp_status bp_adapters_check(bp_adapters* l, void* stream) {
     const char* call = "bp_adapters_check";
     if (l == nullptr) return fail(BP_EINVAL, "%s: NULL layer", call);
-    const bp_status st = read_flags(l->flags, stream, call);
-    if (st == BP_ETIMEOUT) {   // a (tcgen05) launch that stopped early leaves counts behind
-        const cudaError_t e = cudaMemset(l->arrived, 0, low_change_counts(l->n, l->num_sms) * sizeof(unsigned));
-        if (e != cudaSuccess) return cuda_status(e, call);
-    }
-    return st;
+    return read_flags(l->flags, l->arrived, l->n_counts, stream, call);   // (tcgen05 launches wait)
 }
 
 }  // extern "C"
