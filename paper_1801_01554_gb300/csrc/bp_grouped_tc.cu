@@ -1244,7 +1244,7 @@ cudaError_t tc_rows(const RowsArgs& r, bool back, const LowTerms& low, int num_s
     bool ok = make_map(&m[0], r.in, r.n_in_rows, r.K, 0, BM) &&
               (back ? make_map(&m[1], r.W, r.K, r.N, E, BK) : make_map(&m[1], r.W, r.N, r.K, E, bn));
     m[2] = m[3] = m[0];
-    if (r.low != nullptr) {
+    if (r.low != nullptr && r.req.n_requests > 0) {   // (without requests P may be NULL)
         a.tiles = low.tiles;
         a.rank16 = ceil_div(r.req.rank, 16);
         a.stride = low.stride;
