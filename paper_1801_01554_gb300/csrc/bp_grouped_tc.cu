@@ -509,13 +509,14 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
     }
     pdl_wait();   // every thread, before its first access to what earlier kernels wrote or still read
     if (FORM == LOW) {
-        if (g.req.n_requests <= BP_MAX_EXPERTS)   // the table of requests
+        // the table of requests; of more than it holds block 0 reports those out of range
+        const bool fits = g.req.n_requests <= BP_MAX_EXPERTS;
+        if (fits || blockIdx.x == 0)
             for (int i = threadIdx.x; i < g.req.n_requests; i += kThreads) {
                 int lo, hi;
                 group_rows(g.req.offsets, g.req.n_rows, i, lo, hi, g.flags);
-                s_lo[i] = lo;
-                s_hi[i] = hi;
-                s_tile0[i] = request_adapter(g.req, i, g.flags);
+                const int adapter = request_adapter(g.req, i, g.flags);
+                if (fits) s_lo[i] = lo, s_hi[i] = hi, s_tile0[i] = adapter;
             }
     } else if (warp == 2) {
         // the groups' rows and first row blocks

@@ -30,3 +30,25 @@ def test_no_requests_need_no_adapters(dtype, rows):
     assert_sum(host(dX), D @ W, np.abs(D) @ np.abs(W), dtype, what="dX")
     for z in (U, GA, GB):
         assert (host(z) == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [bp.BP_F32, bp.BP_BF16])
+@pytest.mark.parametrize("requests,bad", [(700, 650), (700, 3), (513, 512)])
+def test_a_bad_adapter_of_many_requests_is_reported_by_a_change_alone(dtype, requests, bad):
+    rows = 2 * requests
+    rng = np.random.default_rng(bad)
+    D, U = rounded(rng.standard_normal((rows, 32)), dtype), rounded(rng.standard_normal((rows, 8)), bp.BP_F32)
+    off, adapter = np.arange(requests + 1) * 2, np.arange(requests) % 3 - 1
+    GB = empty((2, 8, 32), bp.BP_F32)
+    with bp.Adapters(2, 8, 64, 32, dtype, max_rows=rows, max_requests=requests) as layer:
+        def change():
+            layer.backward(None, None, None, None, None, dev(U), dev(off), dev(adapter), requests, rows, dev(D, dtype), GB=GB)
+            layer.check()
+        adapter[bad] = 2
+        with pytest.raises(bp.BPError) as e:
+            change()
+        assert e.value.status == bp.BP_ESTATE
+        adapter[bad] = -1   # and as one without it is treated
+        kept = host(GB)
+        change()
+        np.testing.assert_array_equal(host(GB), kept)
