@@ -449,9 +449,8 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
     st = make_layer(dtype, &l->flags, &l->num_sms, call);
     if (st == BP_OK) st = cuda_status(cudaMalloc(&l->low, (size_t)max_rows * rank * sizeof(float)), call);
     if (st == BP_OK && dtype == BP_BF16) {
-        // 256 columns at most: three terms up to rank 64, two above
         l->stride = rank <= 32 ? 32 : rank <= 64 ? 64 : 128;
-        l->n_terms = rank <= 64 ? 3 : 2;
+        l->n_terms = 3;   // 2^-25 of a float32 value is lost; of two terms 2^-17
         const size_t bytes = (size_t)max_rows * l->n_terms * l->stride * 2;
         st = cuda_status(cudaMalloc(&l->terms, bytes), call);
         if (st == BP_OK) st = cuda_status(cudaMalloc(&l->u_terms, bytes), call);

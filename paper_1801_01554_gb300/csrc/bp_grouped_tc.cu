@@ -34,8 +34,8 @@
 // which the epilogue adds the request's rows (as one product with the other requests' rows at zero,
 // an adapter's infinity would reach them); with more requests than half the rank the epilogue
 // takes the rows one by one instead.  In the low form the terms lie side by side along
-// M (three up to rank 64: as exact as float32), so that a rank of up to 32 costs one product and one
-// of 64 two instead of three; the epilogue warps of the other terms pass their sums on through shared
+// M (three: as exact as float32), so that a rank of up to 32 costs one product and one of 64 two
+// instead of three; the epilogue warps of the other terms pass their sums on through shared
 // memory.  Its K blocks run over the adapter's requests in order.
 #include <mutex>
 
@@ -51,7 +51,9 @@ constexpr int kThreads = 64 + kEpiThreads;   // warp 0 copies, warp 1 MMA, warps
 constexpr int kGatherWarps = 4;              // of a forward product with an index, behind them
 constexpr int threads_of(bool gather) { return kThreads + (gather ? 32 * kGatherWarps : 0); }
 
-enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2, LOW = 3, UP = 4 };
+// LOW_WIDE: the low form of ranks above 64.
+enum Form : int { FORWARD = 0, BACK = 1, CHANGE = 2, LOW = 3, UP = 4, LOW_WIDE = 5 };
+constexpr bool is_low(int form) { return form == LOW || form == LOW_WIDE; }
 
 struct TcArgs {
     RowGroups groups;
@@ -95,13 +97,13 @@ struct TcArgs {
 };
 
 constexpr int kBarBytes = 384;
-// An operand A of the low form holds all terms: up to four blocks of 64 columns.
-constexpr int kLowBlocks = 4;
+// An operand A of the low form holds all terms: up to four blocks of 64 columns, six of ranks above 64.
+constexpr int low_blocks(int form) { return form == LOW_WIDE ? 6 : 4; }
 
 template <int BN, int FORM>
 struct Cfg {
-    static constexpr int kStages = BN == 256 ? 4 : FORM == LOW ? (BN == 128 ? 4 : 5) : BN == 128 ? 6 : 8;
-    static constexpr int kABytes = FORM == LOW ? kLowBlocks * BK * 64 * 2 : BM * BK * 2;
+    static constexpr int kStages = BN == 256 ? 4 : FORM == LOW_WIDE ? 3 : FORM == LOW ? (BN == 128 ? 4 : 5) : BN == 128 ? 6 : 8;
+    static constexpr int kABytes = is_low(FORM) ? low_blocks(FORM) * BK * 64 * 2 : BM * BK * 2;
     static constexpr int kBBytes = BN * BK * 2;
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kRingBytes = kStages * kStageBytes;
@@ -119,7 +121,7 @@ __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* map, i
         : "memory");
 }
 // Products that the low form takes for all terms: 128 of their columns each.
-__device__ __forceinline__ int low_sets(const TcArgs& g) { return (g.n_terms * g.stride + BM - 1) / BM; }
+__host__ __device__ __forceinline__ int low_sets(const TcArgs& g) { return (g.n_terms * g.stride + BM - 1) / BM; }
 
 // A tile: rows [row0, end) of a forward or back product, of group g; of a change, all rows of the
 // group and the block mb of M.
@@ -183,7 +185,7 @@ struct Stretches {
         return false;
     }
     __device__ bool next(int& lo, int& hi) {
-        if constexpr (FORM != LOW) {
+        if constexpr (!is_low(FORM)) {
             lo = w.row0;
             hi = w.end;
             return at++ == 0 && hi > lo;
@@ -224,13 +226,13 @@ struct Schedule {
         return (h - l + BK - 1) / BK;
     }
     __device__ int items() const {
-        if (FORM == LOW) return g.req.n_adapters * (g.num_n + g.num_n2) * g.runs;
+        if (is_low(FORM)) return g.req.n_adapters * (g.num_n + g.num_n2) * g.runs;
         if (FORM == UP) return g.max_items;
         return FORM == CHANGE ? g.groups.n_groups * g.num_m * g.num_n : tile0[g.groups.n_groups] * g.num_n;
     }
     __device__ Item item(int it) const {
         Item w;
-        if (FORM == LOW) {
+        if (is_low(FORM)) {
             // all tiles' first shares, then their second ones, ..: those that there are lie together
             const int first = g.req.n_adapters * g.num_n, tiles = first + g.req.n_adapters * g.num_n2;
             w.run = g.runs == 1 ? 0 : it / tiles;
@@ -456,10 +458,10 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
               const __grid_constant__ TcArgs g) {
     using C = Cfg<BN, FORM>;
     constexpr int S = C::kStages;
-    constexpr bool kChange = FORM == CHANGE || FORM == LOW;
-    constexpr bool kFinds = FORM == LOW || FORM == UP;   // the warp looks for requests together
+    constexpr bool kLow = is_low(FORM), kChange = FORM == CHANGE || kLow;
+    constexpr bool kFinds = kLow || FORM == UP;   // the warp looks for requests together
     constexpr bool kAMn = kChange, kBMn = FORM != FORWARD && FORM != UP;
-    constexpr int kChainBlocks = FORM == LOW ? kLowChain : kChain;
+    constexpr int kChainBlocks = kLow ? kLowChain : kChain;
     constexpr int kAcc = 2;   // the epilogue of a sum overlaps the next one's MMAs
     constexpr int kTmemCols = kAcc * BN;
     extern __shared__ uint8_t smem_raw[];
@@ -508,7 +510,7 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     pdl_wait();   // every thread, before its first access to what earlier kernels wrote or still read
-    if (FORM == LOW) {
+    if (kLow) {
         // the table of requests; of more than it holds block 0 reports those out of range
         const bool fits = g.req.n_requests <= BP_MAX_EXPERTS;
         if (fits || blockIdx.x == 0)
@@ -554,7 +556,7 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
         if (blockIdx.x == 0) zero_outside(g.req, threadIdx.x - 64, kEpiThreads, g.low_out, g.terms, g.n_terms * g.stride);
         __syncwarp();
     }
-    const bool kept = FORM == LOW && g.req.n_requests <= BP_MAX_EXPERTS;
+    const bool kept = kLow && g.req.n_requests <= BP_MAX_EXPERTS;
     const Schedule<FORM> plan{g, s_lo, s_hi, s_tile0, {kept ? s_tile0 : nullptr, s_lo, s_hi}};
     const int items = plan.items();
 
@@ -578,7 +580,7 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                 ++issued;
                 if (++stage == S) { stage = 0; phase ^= 1u; }
             };
-            const int a_blocks = FORM == LOW ? 2 * low_sets(g) : BM / 64;
+            const int a_blocks = kLow ? 2 * low_sets(g) : BM / 64;
             for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
                 const Item w = plan.item(it);
                 if constexpr (kChange) {
@@ -589,8 +591,8 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                             if (!open(a_blocks * kMnBlockBytes + C::kBBytes)) break;
                             uint8_t *sa = ring + stage * C::kStageBytes, *sb = sa + C::kABytes;
                             if (leader) {
-                                const CUtensorMap* ma = FORM == LOW && w.second ? &map_low : &map_a;
-                                const CUtensorMap* mb = FORM == LOW && w.second ? &map_p : &map_b;
+                                const CUtensorMap* ma = kLow && w.second ? &map_low : &map_a;
+                                const CUtensorMap* mb = kLow && w.second ? &map_p : &map_b;
                                 for (int i = 0; i < a_blocks; ++i)
                                     tma_load_2d(sa + i * kMnBlockBytes, ma, w.mb * BM + 64 * i, r, &full[stage]);
 #pragma unroll
@@ -677,7 +679,7 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
             for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
                 const Item w = plan.item(it);
                 if constexpr (kChange) {
-                    const int sets = FORM == LOW ? low_sets(g) : 1;   // of 128 rows of M
+                    const int sets = kLow ? low_sets(g) : 1;   // of 128 rows of M
                     Stretches<FORM> rows{g, w, plan.table, 0, 0};
                     int lo, hi, kb = 0;
                     while (ok && rows.next(lo, hi)) {
@@ -842,7 +844,7 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
         for (int it = blockIdx.x; it < items; it += gridDim.x) {
             const Item w = plan.item(it);
             if constexpr (kChange || FORM == UP) {
-                if (FORM == LOW && w.run >= w.shares) continue;   // left to the first share
+                if (kLow && w.run >= w.shares) continue;   // left to the first share
                 float part[BN / 2];
 #pragma unroll
                 for (int c = 0; c < BN / 2; ++c) part[c] = 0.f;
@@ -888,9 +890,9 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                     }
                     continue;
                 }
-                if (FORM == LOW && g.stride < BM && w.kbs == 0) {
+                if (kLow && g.stride < BM && w.kbs == 0) {
                     if (q >= g.stride / 32) continue;   // no sums to pass on
-                } else if (FORM == LOW && g.stride < BM) {
+                } else if (kLow && g.stride < BM) {
                     // row quarters past the first term's: the same ranks of other terms, passed on to it
                     const int own = g.stride / 32, last = min(4, own * g.n_terms);
                     float* block = reinterpret_cast<float*>(stage_out);   // [warp][16][32]
@@ -923,13 +925,13 @@ __global__ void __launch_bounds__(threads_of(GATHER), 1)
                     __syncwarp();
                     if (q >= own) continue;
                 }
-                const bool second = FORM == LOW && w.second;
+                const bool second = kLow && w.second;
                 const int N = second ? g.N2 : g.N;
                 const float* scales = second ? g.scale2 : g.scale;
-                const float scale = FORM == LOW && scales != nullptr ? scales[w.g] : 1.f;
+                const float scale = kLow && scales != nullptr ? scales[w.g] : 1.f;
                 const int m0 = w.mb * BM + q * 32;
                 float* G = (second ? g.G2 : g.G) + (size_t)w.g * g.M * N;
-                if (FORM == LOW && w.shares > 1) {
+                if (kLow && w.shares > 1) {
                     // the run's sums to scratch; the last warp to arrive adds the runs' in their order
                     if (m0 >= g.M || w.nb * BN + cbeg >= N) continue;
                     const size_t plane = (size_t)g.req.n_adapters * g.M * N;
@@ -1160,8 +1162,8 @@ cudaError_t launch(const TcArgs& a, int bn, int items, int num_sms, const CUtens
     if (grid < 1) return cudaSuccess;
     auto go = [&](auto k, int smem) { return launch_pdl(k, grid, 1, threads_of(GATHER), smem, s, m[0], m[1], m[2], m[3], a); };
     if (bn == 64) return go(k_grouped<64, FORM, GATHER>, Cfg<64, FORM>::kSmemBytes);
-    if (bn == 128 || FORM == LOW || FORM == UP) return go(k_grouped<128, FORM, GATHER>, Cfg<128, FORM>::kSmemBytes);
-    if constexpr (FORM != LOW && FORM != UP) return go(k_grouped<256, FORM, GATHER>, Cfg<256, FORM>::kSmemBytes);
+    if (bn == 128 || is_low(FORM) || FORM == UP) return go(k_grouped<128, FORM, GATHER>, Cfg<128, FORM>::kSmemBytes);
+    if constexpr (!is_low(FORM) && FORM != UP) return go(k_grouped<256, FORM, GATHER>, Cfg<256, FORM>::kSmemBytes);
     return cudaErrorInvalidValue;
 }
 
@@ -1206,6 +1208,8 @@ cudaError_t tc_setup() {
     if ((e = setup_width<256>()) != cudaSuccess) return e;
     if ((e = setup_one<64, LOW>()) != cudaSuccess) return e;
     if ((e = setup_one<128, LOW>()) != cudaSuccess) return e;
+    if ((e = setup_one<64, LOW_WIDE>()) != cudaSuccess) return e;
+    if ((e = setup_one<128, LOW_WIDE>()) != cudaSuccess) return e;
     if ((e = setup_one<64, UP>()) != cudaSuccess) return e;
     return setup_one<128, UP>();
 }
@@ -1376,7 +1380,8 @@ cudaError_t tc_low_change(const LowChangeArgs& c, const LowTerms& low, const Low
     };
     if (!maps(c, low, &m[0]) || !maps(c2 != nullptr ? *c2 : c, c2 != nullptr ? low2 : low, &m[2])) return cudaErrorInvalidValue;
     const long long items = (long long)c.req.n_adapters * (a.num_n + a.num_n2) * a.runs;
-    return launch<LOW>(a, cut.bn, items < num_sms ? (int)items : num_sms, num_sms, m, s);
+    const int n = items < num_sms ? (int)items : num_sms;
+    return low_sets(a) > low_blocks(LOW) / 2 ? launch<LOW_WIDE>(a, cut.bn, n, num_sms, m, s) : launch<LOW>(a, cut.bn, n, num_sms, m, s);
 }
 
 }  // namespace bp

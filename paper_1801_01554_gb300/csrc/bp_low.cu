@@ -53,8 +53,7 @@ __device__ __forceinline__ void find_unit(const Requests& q, int unit, int (&whe
     __syncthreads();
 }
 
-// A row's terms: x rounded to bfloat16, the rest rounded, ..; they add up to x but for 2^-17 (two)
-// or 2^-25 (three) of it.
+// A row's terms: x rounded to bfloat16, the rest rounded, ..; three add up to x but for 2^-25 of it.
 __device__ __forceinline__ void store_terms(bf16* terms, int stride, int n_terms, float x) {
     for (int t = 0; t < n_terms; ++t) {
         const bf16 h = __float2bfloat16_rn(x);
