@@ -20,7 +20,8 @@
  *   - BP_BF16 needs n_in and n_out to be multiples of 8 and pattern, weight, U and G
  *     buffers on 16-byte boundaries; float32 and int buffers otherwise lie on 4-byte
  *     boundaries.
- *   - A call may have no rows (n or n_rows 0); row buffers may then be NULL.
+ *   - A call may have no rows (n or n_rows 0); row buffers may then be NULL.  Rows (of a router and
+ *     a mix: n * k, of adapters: max_rows * BP_MAX_RANK) and requests are at most INT_MAX - 1023.
  *   - Index buffers (source, offsets, adapter, place) lie on the device and are not
  *     read by the host.  Kernels clamp offsets to [0, n_rows] and to ascending order,
  *     read a source row outside [0, n_x) as row 0, and treat an adapter outside

@@ -44,6 +44,7 @@ namespace {
 
 constexpr int kMaxUnits = 1 << 20;
 constexpr int kMaxAdapters = 65535;   // a grid dimension
+constexpr int kMaxRows = INT_MAX - 1023;   // kernels round up to tiles of rows and look some rows ahead
 
 bp_status fail(bp_status st, const char* fmt, ...) {
     char buf[512];
@@ -157,7 +158,7 @@ bp_status bp_router_create(int n_experts, int k, int dtype, int max_patterns, in
     bp_status st = check_range(call, "n_experts", n_experts, 1, BP_MAX_EXPERTS);
     if (st == BP_OK) st = check_range(call, "k", k, 1, n_experts < BP_MAX_CHOICES ? n_experts : BP_MAX_CHOICES);
     if (st == BP_OK) st = check_dtype(call, dtype);
-    if (st == BP_OK) st = check_range(call, "max_patterns", max_patterns, 1, INT_MAX / k);
+    if (st == BP_OK) st = check_range(call, "max_patterns", max_patterns, 1, kMaxRows / k);
     if (st == BP_OK && gates != BP_GATES_CHOSEN && gates != BP_GATES_ALL)
         st = fail(BP_EINVAL, "%s: unknown gates %d", call, gates);
     if (st != BP_OK) return st;
@@ -226,7 +227,7 @@ bp_status bp_route_backward(bp_router* r, const void* d_logits, int n, const int
 static bp_status check_mix(const char* call, int n_rows, int n, int k, int n_out, int dtype) {
     bp_status st = check_dtype(call, dtype);
     if (st == BP_OK) st = check_range(call, "k", k, 1, BP_MAX_CHOICES);
-    if (st == BP_OK) st = check_range(call, "n", n, 0, INT_MAX / k);
+    if (st == BP_OK) st = check_range(call, "n", n, 0, kMaxRows / k);
     if (st == BP_OK) st = check_range(call, "n_rows", n_rows, 0, INT_MAX);
     if (st == BP_OK) st = check_units(call, 8, n_out, dtype);
     return st;
@@ -277,7 +278,7 @@ bp_status bp_experts_create(int n_experts, int n_in, int n_out, int dtype, int m
     bp_status st = check_range(call, "n_experts", n_experts, 1, BP_MAX_EXPERTS);
     if (st == BP_OK) st = check_dtype(call, dtype);
     if (st == BP_OK) st = check_units(call, n_in, n_out, dtype);
-    if (st == BP_OK) st = check_range(call, "max_rows", max_rows, 1, INT_MAX);
+    if (st == BP_OK) st = check_range(call, "max_rows", max_rows, 1, kMaxRows);
     if (st != BP_OK) return st;
     bp_experts* l = new (std::nothrow) bp_experts();
     if (l == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
@@ -434,8 +435,8 @@ bp_status bp_adapters_create(int n_adapters, int rank, int n_in, int n_out, int 
     if (st == BP_OK) st = check_range(call, "rank", rank, 1, BP_MAX_RANK);
     if (st == BP_OK) st = check_dtype(call, dtype);
     if (st == BP_OK) st = check_units(call, n_in, n_out, dtype);
-    if (st == BP_OK) st = check_range(call, "max_rows", max_rows, 1, INT_MAX / BP_MAX_RANK);
-    if (st == BP_OK) st = check_range(call, "max_requests", max_requests, 1, INT_MAX - 1);
+    if (st == BP_OK) st = check_range(call, "max_rows", max_rows, 1, kMaxRows / BP_MAX_RANK);
+    if (st == BP_OK) st = check_range(call, "max_requests", max_requests, 1, kMaxRows);
     if (st != BP_OK) return st;
     bp_adapters* l = new (std::nothrow) bp_adapters();
     if (l == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
