@@ -353,7 +353,7 @@ bp_status bp_experts_forward(bp_experts* l, const void* d_W, const float* d_b, c
     cudaStream_t s = (cudaStream_t)stream;
     RowsArgs a{};
     a.groups = {d_offsets, l->E, n_rows};
-    const bool few = l->dtype == BP_BF16 && few_ok(n_rows, l->E, l->n_in);
+    const bool few = l->dtype == BP_BF16 && few_experts(n_rows, l->E, l->n_out, l->n_in);
     a.N = l->n_out;
     a.K = l->n_in;
     a.in = d_X;
@@ -489,7 +489,7 @@ void bp_adapters_destroy(bp_adapters* l) {
 
 static cudaError_t low_of(const bp_adapters* l, const Requests& req, int K, const void* in, const void* P, const float* scale,
                           bool forward, float* low, cudaStream_t s) {
-    const bool few = forward && few_ok(req.n_rows, 1, K);
+    const bool few = forward && few_with_adapters(req.n_rows, K);
     const LowArgs a{req, K, in, P, scale, forward ? 0 : 1, low, l->terms, few ? 0 : l->n_terms, l->stride, few ? nullptr : l->tiles, l->flags};
     if (l->dtype != BP_BF16) return simt_low(a, s);
     if (few) return low_product(a, s);
@@ -541,7 +541,7 @@ bp_status bp_adapters_forward(bp_adapters* l, const void* d_W, const float* d_b,
     a.P = d_B;
     a.scale = d_scale;
     a.flags = l->flags;
-    if (l->dtype == BP_BF16 && few_ok(n_rows, 1, l->n_in)) return cuda_status(few_rows(a, s), call);
+    if (l->dtype == BP_BF16 && few_with_adapters(n_rows, l->n_in)) return cuda_status(few_rows(a, s), call);
     return cuda_status(rows_product(a, l->dtype, false, l->low_terms(), l->num_sms, s), call);
 }
 

@@ -159,10 +159,10 @@ cudaError_t tc_low_change(const LowChangeArgs& a, const LowTerms& low, const Low
 
 // The forward product of a few rows in bfloat16 (bp_few.cu), rows read through an index too; with low,
 // behind low_product, which a dependent launch overlaps.
-// few_ok: 64 rows of one group, or up to 4 a group on average (of at most 512: they may all be in one), and
-// no longer sums than one chain takes.
+// Which calls it is for, by rows, groups and weights (its sums are no longer than one chain takes).
+bool few_experts(int n_rows, int n_groups, int N, int K);
+bool few_with_adapters(int n_rows, int K);
 cudaError_t few_setup();
-bool few_ok(int n_rows, int n_groups, int K);
 cudaError_t few_rows(const RowsArgs& a, cudaStream_t s);
 
 // Low-rank products of bfloat16 (bp_low.cu).

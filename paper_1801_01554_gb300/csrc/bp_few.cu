@@ -200,17 +200,36 @@ cudaError_t few_setup() {
     return setup<2, 8, true>();
 }
 
-// us of the experts' forward here / on tcgen05: 32 rows of 512-512 in 8 groups 6.8 / 10.8, 16 of 1024-1024 in
-// 4 8.8 / 12.9, 48 of 2048-2048 in 16 26.2 / 21.2, 100 of 2048-2048 in 16 39.6 / 25.2 (16 rows a pass:
-// larger groups read their weights again).
 // A warp's sum is one chain of mma.sync, which truncates: up to 128 steps of 16 of K, as in a part of the
 // tcgen05 products.
-bool few_ok(int n_rows, int n_groups, int K) {
-    if (K > 128 * 16 * kWarps) return false;
-    if (n_groups == 1) return n_rows <= 64;
-    const int busy = n_groups < n_rows ? n_groups : n_rows;
-    return n_rows <= 4 * busy && n_rows <= 512;
+static bool few_sums(int K) { return K <= 128 * 16 * kWarps; }
+
+bool few_with_adapters(int n_rows, int K) { return n_rows <= 64 && few_sums(K); }
+
+// us of the experts' forward here / on tcgen05, weights from DRAM: 8 rows of 1024-1024 of 16 experts 12.0 /
+// 13.3, of 4096-4096 63.1 / 63.4; 12 of 1024-2048 of 16 16.4 / 18.4 (their 29 MB in L2: 10 of them 9.6 /
+// 12.4), 16 of 2048-2048 of 16 32.8 / 28.7; 32 of 512-512 of 8 8.2 / 10.2, of 4096-256 18.4 / 26.6, of
+// 1024-2048 20.5 / 16.2; 48 of 2048-2048 of 16 51 / 37; 512 of 512-512 in one of 128 76 / 16 (16 rows a
+// pass: larger groups read their weights again); 64 of 4096-256 of 16 20.5 / 26.6.  So: up to 8 rows; to 16
+// where their experts' weights may lie in L2; to 32 or 64 where their units are so few that tcgen05 tiles leave
+// SMs idle; of one expert up to two passes (32 of 4096-4096 30.7 / 34.8, 64 51 / 35).
+bool few_experts(int n_rows, int n_groups, int N, int K) {
+    if (!few_sums(K)) return false;
+    if (n_groups == 1) return n_rows <= 32;
+    const int busy = n_groups < n_rows ? n_groups : n_rows;   // at most: their sizes are on the device
+    const long long units = (long long)busy * N;
+    return n_rows <= 4 * busy && (n_rows <= 8 || (n_rows <= 16 && units * K <= 1 << 25) || (n_rows <= 32 && units <= 8192) ||
+                                  (n_rows <= 64 && units <= 4096));
 }
+
+}  // namespace bp
+
+// What few_experts says, for tests.
+extern "C" int bp_internal_few_experts(int n_rows, int n_experts, int n_in, int n_out) {
+    return bp::few_experts(n_rows, n_experts, n_out, n_in) ? 1 : 0;
+}
+
+namespace bp {
 
 cudaError_t few_rows(const RowsArgs& a, cudaStream_t s) {
     const int n = a.groups.n_rows;
