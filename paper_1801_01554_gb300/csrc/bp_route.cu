@@ -399,10 +399,17 @@ bool pieces(const MixArgs& a, int size) {
     return (p & 15) == 0 && (size_t)a.N * size % 16 == 0;
 }
 
+int device_sms() {
+    int dev = 0, n = 1;
+    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+    return n;
+}
+
 // Warps of a pattern: as many as its row has pieces for, while patterns are few.
 int mix_warps(int n, int N, int per_warp) {
+    static const int num_sms = device_sms();   // (no handle keeps it)
     int w = 1;
-    while (w < kMixThreads / 32 && w * per_warp < N && (long long)n * w < 152 * 16) w *= 2;
+    while (w < kMixThreads / 32 && w * per_warp < N && (long long)n * w < 16 * num_sms) w *= 2;
     return w;
 }
 
