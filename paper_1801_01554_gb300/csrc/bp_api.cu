@@ -259,6 +259,10 @@ bp_status bp_create(const int* sizes, int n_layers, float lr, float momentum, in
         if (e != cudaSuccess) return bail(cuda_fail(e, "cudaMalloc(flags)"));
         bf16_set_flags(b, net->flags);
     }
+    // the memsets run on the legacy default stream, behind what it has queued; the net's first call may be
+    // on a stream that does not wait for that one
+    e = cudaStreamSynchronize(cudaStreamLegacy);
+    if (e != cudaSuccess) return bail(cuda_fail(e, "cudaMemset"));
     *out = net;
     return BP_OK;
 }
@@ -305,7 +309,10 @@ bp_status bp_get_faults(bp_net* net, int64_t* count, int reset) {
     unsigned c = 0;
     BP_CUDA(cudaMemcpy(&c, net->flags + 1, sizeof(unsigned), cudaMemcpyDeviceToHost), "bp_get_faults");
     *count = (int64_t)c;
-    if (reset) BP_CUDA(cudaMemset(net->flags + 1, 0, sizeof(unsigned)), "bp_get_faults");
+    if (reset) {
+        BP_CUDA(cudaMemset(net->flags + 1, 0, sizeof(unsigned)), "bp_get_faults");
+        BP_CUDA(cudaStreamSynchronize(cudaStreamLegacy), "bp_get_faults");
+    }
     return BP_OK;
 }
 
@@ -520,13 +527,15 @@ bp_status bp_train_epoch(bp_net* net, const void* d_X, const void* d_T, int n_pa
 bp_status bp_check(bp_net* net, void* stream) {
     if (net == nullptr) return fail(BP_EINVAL, "NULL net");
     cudaStream_t s = (cudaStream_t)stream;
-    BP_CUDA(cudaStreamSynchronize(s), "bp_check");
     int flags = 0;
-    BP_CUDA(cudaMemcpy(&flags, net->flags, sizeof(int), cudaMemcpyDeviceToHost), "bp_check");
+    BP_CUDA(cudaMemcpyAsync(&flags, net->flags, sizeof(int), cudaMemcpyDeviceToHost, s), "bp_check");
+    BP_CUDA(cudaStreamSynchronize(s), "bp_check");
     if (flags == 0) return BP_OK;
-    BP_CUDA(cudaMemset(net->flags, 0, sizeof(int)), "bp_check");
+    // cleared before the next call, whatever stream that is on
+    BP_CUDA(cudaMemsetAsync(net->flags, 0, sizeof(int), s), "bp_check");
     if (net->bar)
-        BP_CUDA(cudaMemset(net->bar, 0, (size_t)bp::kBarWords * sizeof(unsigned)), "bp_check");
+        BP_CUDA(cudaMemsetAsync(net->bar, 0, (size_t)bp::kBarWords * sizeof(unsigned), s), "bp_check");
+    BP_CUDA(cudaStreamSynchronize(s), "bp_check");
     if (flags & kFlagTimeout)
         return fail(BP_ETIMEOUT, "a bounded device-side wait ran out; the launch stopped early");
     if (flags & kFlagBounds)
