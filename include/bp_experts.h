@@ -118,7 +118,7 @@ bp_status bp_experts_forward(bp_experts* layer, const void* d_W, const float* d_
  *   d_dX [n_rows, n_in]    W_e^T d of each row in a group, in the rows' order (bp_mix with
  *                          gates of 1 adds up the rows of a pattern); squash != 0: times
  *                          x (1 - x), the hidden delta of an input that is itself a
- *                          logistic's output.  May be NULL.
+ *                          logistic's output.  May be NULL; must not overlap d_X or d_D.
  *   d_GW [E, n_out, n_in]  sum over the expert's rows of d x^T, zeros for one without rows;
  *   d_Gb [E, n_out]        sum over the expert's rows of d.  Either may be NULL.
  * accumulate != 0 adds to d_GW and d_Gb instead of writing them.  d_W may be NULL without
@@ -155,7 +155,8 @@ bp_status bp_adapters_forward(bp_adapters* layer, const void* d_W, const float* 
 
 /* The gradients for d_D [n_rows, n_out], the gradient of the sum before the squashing function;
  * the shared layer has none (its weights are not trained here).  With v = scale_a B_a d:
- *   d_dX [n_rows, n_in]              W^T d + A_a^T v, squash != 0: times x (1 - x); may be NULL;
+ *   d_dX [n_rows, n_in]              W^T d + A_a^T v, squash != 0: times x (1 - x); may be NULL; must
+ *                                    not overlap d_X or d_D;
  *   d_GA [n_adapters, rank, n_in]    sum over the rows of the adapter's requests of v x^T;
  *   d_GB [n_adapters, rank, n_out]   scale_a times the sum of u d^T.  Either may be NULL.
  * accumulate != 0 adds to d_GA and d_GB; else adapters without rows get zeros.

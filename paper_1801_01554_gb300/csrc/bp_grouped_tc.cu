@@ -10,8 +10,8 @@
 //
 // One persistent CTA per SM: a warp that issues TMA copies into a ring of stages, a warp that
 // issues tcgen05.mma (128 rows x BN columns x 64 of K a stage) into TMEM, eight epilogue warps.
-// The tensor cores bound the large products: 16,384 rows of 4096-4096 in 8 groups take 332 us forward and
-// 331 back (1.65 PFLOP/s, 87% of the measured burst rate), their changes 410 (1.34 PFLOP/s; 350 without
+// The tensor cores bound the large products: 16,384 rows of 4096-4096 in 8 ragged groups take 336 us forward
+// and 340 back (1.63 PFLOP/s, 86% of the measured burst rate), their changes 404 (1.36 PFLOP/s; 350 without
 // the 537 MB that they write); few rows a group are bound by reading the weights (240 rows of 4096-1024
 // in 32 groups: 44 us, the 268 MB at the measured copy rate 40).
 //
