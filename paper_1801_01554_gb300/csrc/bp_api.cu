@@ -258,11 +258,13 @@ bp_status bp_create(const int* sizes, int n_layers, float lr, float momentum, in
         if (e == cudaSuccess) e = cudaMemset(net->flags, 0, 4 * sizeof(int));
         if (e != cudaSuccess) return bail(cuda_fail(e, "cudaMalloc(flags)"));
         bf16_set_flags(b, net->flags);
+        e = bf16_refresh_weights(b, nullptr);   // the bfloat16 copies of weights that are 0
+        if (e != cudaSuccess) return bail(cuda_fail(e, "bp_create(bf16 copies)"));
     }
-    // the memsets run on the legacy default stream, behind what it has queued; the net's first call may be
-    // on a stream that does not wait for that one
+    // all that runs on the legacy default stream, behind what it has queued; the net's first call may be on a
+    // stream that does not wait for that one
     e = cudaStreamSynchronize(cudaStreamLegacy);
-    if (e != cudaSuccess) return bail(cuda_fail(e, "cudaMemset"));
+    if (e != cudaSuccess) return bail(cuda_fail(e, "bp_create"));
     *out = net;
     return BP_OK;
 }
