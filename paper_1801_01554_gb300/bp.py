@@ -1,4 +1,4 @@
-"""ctypes binding of libbp.so (the C ABI declared in include/bp.h and include/bp_experts.h).
+"""ctypes binding of libbp.so (the C ABI declared in include/bp.h, include/bp_experts.h and include/bp_blocks.h).
 
 Argument marshalling only: every step of the back-propagation path runs in the
 library's CUDA kernels.  Functions keep the C names; device buffers are passed
@@ -23,8 +23,9 @@ BP_SIGMOID_LOGISTIC, BP_SIGMOID_TABLE = 0, 1
 BP_MAX_SIZES = 9
 BP_MAX_EXPERTS, BP_MAX_CHOICES, BP_MAX_RANK = 512, 16, 128
 BP_GATES_CHOSEN, BP_GATES_ALL = 0, 1
+BP_MAX_TOKENS, BP_MAX_IDS = 1 << 24, 1 << 26
 
-# name -> (restype, argtypes); every symbol declared in include/bp.h and include/bp_experts.h
+# name -> (restype, argtypes); every symbol declared in include/
 _VP = ctypes.c_void_p
 _I = ctypes.c_int
 _F = ctypes.c_float
@@ -73,6 +74,11 @@ SIGNATURES = {
     "bp_adapters_backward": (_I, [_VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _I, _I, _VP, _I, _VP, _VP,
                                   _VP, _I, _VP]),
     "bp_adapters_check": (_I, [_VP, _VP]),
+    "bp_embedding_create": (_I, [_I, _I, _I, _I, ctypes.POINTER(_VP)]),
+    "bp_embedding_destroy": (None, [_VP]),
+    "bp_embed": (_I, [_VP, _VP, _VP, _I, _F, _VP, _VP]),
+    "bp_embed_backward": (_I, [_VP, _VP, _I, _VP, _F, _VP, _I, _VP]),
+    "bp_embedding_check": (_I, [_VP, _VP]),
 }
 
 
@@ -450,6 +456,31 @@ def bp_adapters_check(h, stream=None):
     _check(load().bp_adapters_check(h, _stream(stream)))
 
 
+# ------------------------------------------------- C names of include/bp_blocks.h
+def bp_embedding_create(n_tokens, width, dtype=BP_F32, max_ids=1024):
+    out = ctypes.c_void_p()
+    _check(load().bp_embedding_create(int(n_tokens), int(width), int(dtype), int(max_ids), ctypes.byref(out)))
+    return out.value
+
+
+def bp_embedding_destroy(h):
+    load().bp_embedding_destroy(h)
+
+
+def bp_embed(h, table, ids, n, Y, scale=1.0, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_embed(h, _values(table, dtype, "table", room[0]), _ints(ids, "ids", n), n, scale,
+                           _values(Y, dtype, "Y", room[1]), _stream(stream)))
+
+
+def bp_embed_backward(h, ids, n, D, G, scale=1.0, accumulate=False, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_embed_backward(h, _ints(ids, "ids", n), n, _values(D, dtype, "D", room[1]), scale,
+                                    _floats(G, "G", room[0]), 1 if accumulate else 0, _stream(stream)))
+
+
+def bp_embedding_check(h, stream=None):
+    _check(load().bp_embedding_check(h, _stream(stream)))
+
+
 # ------------------------------------------------------------------ convenience
 class _Handle:
     """A handle of the library, freed by close() or at the end of a with block."""
@@ -545,6 +576,26 @@ class Adapters(_Handle):
 
     def check(self, stream=None):
         bp_adapters_check(self.h, stream)
+
+
+class Embedding(_Handle):
+    """Owns one bp_embedding handle; methods forward to the C names above."""
+
+    _free = staticmethod(bp_embedding_destroy)
+
+    def __init__(self, n_tokens, width, dtype=BP_F32, max_ids=1024):
+        self.n_tokens, self.width, self.dtype = int(n_tokens), int(width), dtype
+        self.h = bp_embedding_create(n_tokens, width, dtype, max_ids)
+
+    def forward(self, table, ids, n, Y, scale=1.0, stream=None):
+        bp_embed(self.h, table, ids, n, Y, scale, self.dtype, stream, (self.n_tokens * self.width, n * self.width))
+
+    def backward(self, ids, n, D, G, scale=1.0, accumulate=False, stream=None):
+        bp_embed_backward(self.h, ids, n, D, G, scale, accumulate, self.dtype, stream,
+                          (self.n_tokens * self.width, n * self.width))
+
+    def check(self, stream=None):
+        bp_embedding_check(self.h, stream)
 
 
 class Net:

@@ -1,0 +1,452 @@
+// Embeddings: rows of a table by token, and the pooled change of every token's row.
+#include "bp_blocks_internal.h"
+#include "bp_experts_device.cuh"
+#include "bp_tc_device.cuh"
+
+namespace bp {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+
+// V values of a row, 16 bytes of it (or one float32 where rows are not whole 16-byte pieces).
+template <class T, int V>
+struct Piece {
+    uint4 u;
+    __device__ __forceinline__ void load(const T* p) {   // (volatile: a batch of loads stays a batch)
+        if constexpr (V == 1) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(u.x) : "l"(p));
+        else asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
+    }
+    __device__ __forceinline__ void values(float (&v)[V]) const {
+        const unsigned w[4] = {u.x, u.y, u.z, u.w};
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = __uint_as_float(w[i]);
+        }
+    }
+};
+template <class T, int V>
+__device__ __forceinline__ void store_values(T* p, const float (&v)[V]) {
+    if constexpr (V == 1) {
+        *p = from_f32<T>(v[0]);
+    } else if constexpr (sizeof(T) == 2) {
+        __align__(16) __nv_bfloat162 h[V / 2];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    }
+}
+
+// ------------------------------------------------------------ lookup
+// A warp takes up to kLook pieces a lane of one row, or several short rows.  Bound by reading the rows that
+// are named and writing n.
+constexpr int kLook = 4;
+
+template <class T, int V>
+__global__ void __launch_bounds__(kThreads) k_embed(EmbedArgs g, int lanes, int chunks) {
+    const int lane = threadIdx.x & 31, nv = g.width / V;
+    const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    const long long row = w / chunks * (32 / lanes) + lane / lanes;
+    if (row >= g.n) return;
+    const int id = g.ids[row];
+    const bool ok = (unsigned)id < (unsigned)g.n_tokens;
+    if (!ok && id != -1) atomicOr(g.flags, kFlagBounds);
+    const int v0 = (int)(w % chunks) * lanes * kLook + lane % lanes;
+    const T* in = (const T*)g.table + (size_t)(ok ? id : 0) * g.width;
+    T* out = (T*)g.Y + (size_t)row * g.width;
+    Piece<T, V> p[kLook];
+#pragma unroll
+    for (int i = 0; i < kLook; ++i)
+        if (ok && v0 + i * lanes < nv) p[i].load(in + (size_t)(v0 + i * lanes) * V);
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) {
+        if (v0 + i * lanes >= nv) break;
+        float v[V] = {};
+        if (ok) {
+            p[i].values(v);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] *= g.scale;
+        }
+        store_values<T, V>(out + (size_t)(v0 + i * lanes) * V, v);
+    }
+}
+
+// ------------------------------------------------------------ ids in order
+// A stable radix sort of (token, place) by one cluster, which takes two passes of up to nine bits for up to
+// 2^18 - 1 tokens, three beyond.  Each warp has a run of the ids; a pass counts every warp's digits in shared memory, adds the
+// counts up over the warps, the cluster's CTAs (distributed shared memory) and the digits, and moves each id behind
+// those before it.  The ids lie in L2 between passes.  No launch waits for another one's progress: the
+// cluster's barrier is the hardware's.
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+constexpr int kMaxDigits = 512;
+constexpr int kSortCtas = 8;
+constexpr int kSortAlone = 4096;   // ids that one CTA takes
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ int cluster_rank() {
+    int r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ int cluster_size() {
+    int r;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ unsigned of_cta(const unsigned* p, int cta) {   // a word of another CTA's shared memory
+    unsigned a, v;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(cta));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(kSortThreads) k_sort(EmbedArgs g, int passes, int bits) {
+    extern __shared__ unsigned sm[];
+    const int D = 1 << bits;
+    unsigned* total = sm;              // [D] of this CTA
+    unsigned* base = total + D;        // [D] where this CTA's ids of a digit go
+    unsigned* count = base + D;        // [warps, D]
+    __shared__ unsigned scan[kSortWarps];
+    pdl_launch();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ctas = cluster_size(), rank = cluster_rank();
+    const int shares = ctas * kSortWarps, per = (int)(((long long)g.n + shares * 32 - 1) / (shares * 32)) * 32;
+    const long long first = (long long)(rank * kSortWarps + warp) * per;
+    const int lo = (int)min(first, (long long)g.n), hi = (int)min(first + per, (long long)g.n);
+    unsigned* mine = count + (size_t)warp * D;
+    for (int pass = 0; pass < passes; ++pass) {
+        const unsigned* in = g.keys[(pass + 1) & 1];
+        const int* at = g.places[(pass + 1) & 1];
+        unsigned* out = g.keys[pass & 1];
+        int* to = g.places[pass & 1];
+        const int shift = pass * bits;
+        const auto key_of = [&](int i) -> unsigned {
+            if (pass > 0) return __ldcg(in + i);
+            const int id = g.ids[i];
+            if ((unsigned)id < (unsigned)g.n_tokens) return (unsigned)id;
+            if (id != -1) atomicOr(g.flags, kFlagBounds);
+            return (unsigned)g.n_tokens;   // behind every token
+        };
+        for (int i = threadIdx.x; i < kSortWarps * D; i += kSortThreads) count[i] = 0u;
+        __syncthreads();
+        for (int b = lo; b < hi; b += 32) {
+            const bool live = b + lane < hi;
+            const unsigned who = __ballot_sync(0xffffffffu, live);
+            if (live) {
+                const unsigned d = (key_of(b + lane) >> shift) & (D - 1), peers = __match_any_sync(who, d);
+                if (lane == __ffs(peers) - 1) mine[d] += __popc(peers);
+            }
+            __syncwarp();
+        }
+        __syncthreads();
+        if (threadIdx.x < D) {
+            unsigned sum = 0;
+            for (int w = 0; w < kSortWarps; ++w) {
+                const unsigned x = count[(size_t)w * D + threadIdx.x];
+                count[(size_t)w * D + threadIdx.x] = sum;
+                sum += x;
+            }
+            total[threadIdx.x] = sum;
+        }
+        cluster_sync();
+        unsigned before = 0, all = 0;
+        if (threadIdx.x < D) {
+            for (int c = 0; c < ctas; ++c) {
+                const unsigned x = of_cta(total + threadIdx.x, c);
+                if (c < rank) before += x;
+                all += x;
+            }
+        }
+        unsigned s = all;   // digits below this one
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned x = __shfl_up_sync(0xffffffffu, s, o);
+            if (lane >= o) s += x;
+        }
+        if (lane == 31) scan[warp] = s;
+        __syncthreads();
+        if (threadIdx.x < D) {
+            for (int w = 0; w < warp; ++w) before += scan[w];
+            base[threadIdx.x] = before + s - all;
+        }
+        __syncthreads();
+        for (int b = lo; b < hi; b += 32) {
+            const bool live = b + lane < hi;
+            const unsigned who = __ballot_sync(0xffffffffu, live);
+            unsigned d = 0, peers = 0, r = 0;
+            if (live) {
+                const unsigned key = key_of(b + lane);
+                d = (key >> shift) & (D - 1);
+                peers = __match_any_sync(who, d);
+                r = base[d] + mine[d] + __popc(peers & ((1u << lane) - 1u));
+                out[r] = key;
+                to[r] = pass > 0 ? __ldcg(at + b + lane) : b + lane;
+            }
+            __syncwarp();
+            if (live && lane == __ffs(peers) - 1) mine[d] += __popc(peers);
+            __syncwarp();
+        }
+        cluster_sync();   // the ids are there for the next pass; no CTA leaves while another reads its counts
+    }
+}
+
+// ------------------------------------------------------------ changes
+// keys[lo, hi) ascend: the first index whose key is at least k, by a converged warp.
+__device__ __forceinline__ int warp_lower_bound(const unsigned* keys, int lo, int hi, unsigned k) {
+    const int lane = threadIdx.x & 31;
+    while (lo < hi) {
+        const int step = max(1, (int)(((long long)hi - lo + 31) / 32));
+        const long long i = lo + (long long)(lane + 1) * step - 1;
+        const bool there = i >= hi || __ldg(keys + i) >= k;
+        const unsigned m = __ballot_sync(0xffffffffu, there);
+        if (m == 0) return hi;
+        const int f = __ffs(m) - 1;
+        const long long at = lo + (long long)(f + 1) * step - 1;
+        lo += f * step;
+        hi = (int)min((long long)hi, at);
+    }
+    return lo;
+}
+
+constexpr int kBatch = 8;         // rows under way
+constexpr int kZeroTokens = 16;   // tokens of a warp that writes zeros
+
+// A warp takes kEmbedTile sorted ids and 32 pieces of their rows, and adds up runs of equal tokens in registers.
+// A run of at most kEmbedTile ids is summed by the tile that it starts in, also past that tile's end, and is stored at
+// once.  A longer one is cut at the tiles' ends: its pieces go to scratch, and the warp whose piece comes
+// last adds them in order, so that sums do not depend on which that is.  Further warps write the zeros of
+// tokens without ids.  Bound by reading D once and writing G once.
+template <class T, int V>
+__global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const unsigned* keys, const int* places, long long sum_warps,
+                                                         int slabs) {
+    const int lane = threadIdx.x & 31;
+    const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    pdl_wait();
+    const int n = g.n, N = g.width;
+    if (w >= sum_warps) {   // zeros
+        if (g.accumulate) return;
+        const long long t0 = (w - sum_warps) * kZeroTokens;
+        if (t0 >= g.n_tokens) return;
+        bool absent = false;
+        if (lane < kZeroTokens && t0 + lane < g.n_tokens) {
+            const unsigned t = (unsigned)(t0 + lane);
+            int lo = 0, hi = n;
+            while (lo < hi) {
+                const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
+                if (__ldg(keys + mid) < t) lo = mid + 1;
+                else hi = mid;
+            }
+            absent = lo >= n || __ldg(keys + lo) != t;
+        }
+        unsigned m = __ballot_sync(0xffffffffu, absent);
+        while (m != 0) {
+            float* row = g.G + (size_t)(t0 + __ffs(m) - 1) * N;
+            m &= m - 1;
+            if constexpr (V > 1) {
+                for (int c = lane * 4; c < N; c += 128) *reinterpret_cast<float4*>(row + c) = make_float4(0.f, 0.f, 0.f, 0.f);
+            } else {
+                for (int c = lane; c < N; c += 32) row[c] = 0.f;
+            }
+        }
+        return;
+    }
+    constexpr unsigned kNone = 0xffffffffu;
+    const int tile = (int)(w / slabs), slab = (int)(w % slabs), t0 = tile * kEmbedTile;
+    const unsigned tokens = (unsigned)g.n_tokens;
+    const unsigned kp = tile > 0 ? __ldg(keys + t0 - 32 + lane) : kNone;
+    const unsigned kc = t0 + lane < n ? __ldg(keys + t0 + lane) : kNone;
+    const unsigned kn = t0 + 32 + lane < n ? __ldg(keys + t0 + 32 + lane) : kNone;
+    const int pc = t0 + lane < n ? __ldg(places + t0 + lane) : 0;
+    const int pn = t0 + 32 + lane < n ? __ldg(places + t0 + 32 + lane) : 0;
+    const unsigned first = __shfl_sync(0xffffffffu, kc, 0), last = __shfl_sync(0xffffffffu, kc, 31);
+    if (first >= tokens) return;   // ids of no token, behind all others
+    // the rows [a, b) of this tile (from 32 on: the next one's); long runs at its ends
+    int a = 0, b = __popc(__ballot_sync(0xffffffffu, kc < tokens));
+    int head = 0, tail = 32;       // rows [0, head) and [tail, 32) are pieces of longer runs
+    const int came = __clz(~__ballot_sync(0xffffffffu, kp == first));   // ids of the first run before this tile (32: or more)
+    const unsigned of_first = __ballot_sync(0xffffffffu, kc == first), of_last = __ballot_sync(0xffffffffu, kc == last);
+    const int lead = of_first == 0xffffffffu ? 32 : __ffs(~of_first) - 1;
+    if (came > 0) {
+        const bool lng = came == 32 || __shfl_sync(0xffffffffu, kc, (32 - came) & 31) == first;
+        if (lng) head = lead;
+        else a = lead;
+    }
+    if (last < tokens && __shfl_sync(0xffffffffu, kn, 0) == last && head < 32) {   // the last run goes on
+        const int start = 32 - __clz(~of_last);
+        if (__shfl_sync(0xffffffffu, kn, start & 31) == last) {
+            tail = start;
+        } else {
+            const unsigned more = __ballot_sync(0xffffffffu, kn == last);
+            b = 32 + __ffs(~more) - 1;   // (at most 31 more)
+        }
+    }
+    const int c0 = (slab * 32 + lane) * V;
+    const bool in_row = c0 < N;
+    const T* D = (const T*)g.D + c0;
+    float acc[V] = {};
+    const auto write = [&](unsigned token) {
+        if (!in_row) return;
+        float* p = g.G + (size_t)token * N + c0;
+        float v[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = acc[i] * g.scale;
+        if (g.accumulate) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += p[i];
+        }
+        store_values<float, V>(p, v);
+    };
+    // A piece of a long run: to its slot, and all of the run's pieces to G if it is the last one.
+    const auto join = [&](unsigned token, int slot) {
+        if (in_row) {
+            float* p = g.partial + (size_t)slot * N + c0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) __stcg(p + i, acc[i]);
+        }
+        const int s = warp_lower_bound(keys, 0, min(t0 + 32, n), token), e = warp_lower_bound(keys, t0, n, token + 1);
+        const int from = s / kEmbedTile, to = (e - 1) / kEmbedTile;
+        __threadfence();
+        __syncwarp();
+        unsigned mine = 0;
+        if (lane == 0) {
+            unsigned* count = g.arrived + (size_t)from * slabs + slab;
+            mine = atomicAdd(count, 1u);
+            if (mine == (unsigned)(to - from)) *count = 0;   // for the next call
+        }
+        mine = __shfl_sync(0xffffffffu, mine, 0);
+        if (mine != (unsigned)(to - from)) return;
+        __threadfence();
+        if (!in_row) return;
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = __ldcg(g.partial + (size_t)(2 * from + 1) * N + c0 + i);
+        for (int t = from + 1; t <= to; t += kBatch) {
+            float x[kBatch][V];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[j][i] = t + j <= to ? __ldcg(g.partial + (size_t)(2 * (t + j)) * N + c0 + i) : 0.f;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j)
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += x[j][i];
+        }
+        write(token);
+    };
+    unsigned now = kNone;
+    const auto row_key = [&](int r) { return r < 32 ? __shfl_sync(0xffffffffu, kc, r) : __shfl_sync(0xffffffffu, kn, r & 31); };
+    const auto row_place = [&](int r) { return r < 32 ? __shfl_sync(0xffffffffu, pc, r) : __shfl_sync(0xffffffffu, pn, r & 31); };
+    for (int r0 = a; r0 < b; r0 += kBatch) {
+        Piece<T, V> x[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int p = row_place(min(r0 + j, b - 1));
+            if (in_row) x[j].load(D + (size_t)p * N);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int r = r0 + j;
+            if (r >= b) break;
+            const unsigned k = row_key(r);
+            if (k != now) {
+                if (now != kNone) {
+                    if (r == head) join(now, 2 * tile);
+                    else write(now);
+                }
+                now = k;
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] = 0.f;
+            }
+            if (in_row) {
+                float v[V];
+                x[j].values(v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += v[i];
+            }
+        }
+    }
+    if (now == kNone) return;
+    if (head == b) join(now, 2 * tile);
+    else if (tail < 32) join(now, 2 * tile + 1);
+    else write(now);
+}
+
+int sort_bits(int n_tokens, int& passes) {
+    int bits = 1;
+    while ((n_tokens >> bits) != 0) ++bits;   // tokens and n_tokens itself
+    passes = (bits + 8) / 9;
+    return (bits + passes - 1) / passes;
+}
+
+template <class T, int V>
+cudaError_t lookup(const EmbedArgs& a, cudaStream_t s) {
+    const int nv = a.width / V;
+    int lanes = 1;
+    while (lanes < 32 && lanes < nv) lanes *= 2;
+    const int chunks = (nv + lanes * kLook - 1) / (lanes * kLook), rows = 32 / lanes;
+    const long long warps = (long long)((a.n + rows - 1) / rows) * chunks;
+    k_embed<T, V><<<(unsigned)((warps + kWarps - 1) / kWarps), kThreads, 0, s>>>(a, lanes, chunks);
+    return cudaGetLastError();
+}
+
+template <class T, int V>
+cudaError_t sums(const EmbedArgs& a, int passes, cudaStream_t s) {
+    const int tiles = (a.n + kEmbedTile - 1) / kEmbedTile, slabs = (a.width + 32 * V - 1) / (32 * V);
+    const long long sum_warps = (long long)tiles * slabs;
+    const long long zero_warps = a.accumulate ? 0 : (a.n_tokens + kZeroTokens - 1) / kZeroTokens;
+    const long long blocks = (sum_warps + zero_warps + kWarps - 1) / kWarps;
+    if (blocks == 0) return cudaSuccess;
+    const int at = (passes - 1) & 1;
+    return launch_pdl(k_embed_sums<T, V>, (int)blocks, 1, kThreads, 0, s, a, (const unsigned*)a.keys[at], (const int*)a.places[at],
+                      sum_warps, slabs);
+}
+
+bool pieces16(const void* a, const void* b, int width) { return (((uintptr_t)a | (uintptr_t)b) & 15) == 0 && width % 4 == 0; }
+
+}  // namespace
+
+size_t embed_counts(int max_ids, int width, int dtype) {
+    const size_t slab = dtype == BP_BF16 ? 256 : 32;
+    return ((size_t)max_ids + kEmbedTile - 1) / kEmbedTile * ((width + slab - 1) / slab);
+}
+
+cudaError_t embed_setup() {
+    return cudaFuncSetAttribute(k_sort, cudaFuncAttributeMaxDynamicSharedMemorySize, (kSortWarps + 2) * kMaxDigits * (int)sizeof(unsigned));
+}
+
+cudaError_t embed_forward(const EmbedArgs& a, cudaStream_t s) {
+    if (a.dtype == BP_BF16) return lookup<__nv_bfloat16, 8>(a, s);
+    return pieces16(a.table, a.Y, a.width) ? lookup<float, 4>(a, s) : lookup<float, 1>(a, s);
+}
+
+cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s) {
+    int passes = 1;
+    const int bits = sort_bits(a.n_tokens, passes);
+    if (a.n > 0) {
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = a.n <= kSortAlone ? 1 : kSortCtas;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cudaLaunchConfig_t c{};
+        c.gridDim = dim3(at[0].val.clusterDim.x);
+        c.blockDim = dim3(kSortThreads);
+        c.dynamicSmemBytes = (size_t)(kSortWarps + 2) * (1u << bits) * sizeof(unsigned);
+        c.stream = s;
+        c.attrs = at;
+        c.numAttrs = 1;
+        const cudaError_t e = cudaLaunchKernelEx(&c, k_sort, a, passes, bits);
+        if (e != cudaSuccess) return e;
+    }
+    if (a.dtype == BP_BF16) return sums<__nv_bfloat16, 8>(a, passes, s);
+    return pieces16(a.D, a.G, a.width) ? sums<float, 4>(a, passes, s) : sums<float, 1>(a, passes, s);
+}
+
+}  // namespace bp

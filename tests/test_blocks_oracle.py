@@ -1,0 +1,59 @@
+"""The blocks' oracle against differences, and what the library refuses before it touches the GPU (no GPU)."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+from oracle import blocks_oracle as O
+from paper_1801_01554_gb300 import bp, build
+
+P = 0x10000   # an address that is never read
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(bp.lib_path()):
+        build.build()
+    return bp.load()
+
+
+def difference(f, x, step=1e-6):
+    """The gradient of f() by x, a value at a time."""
+    g = np.zeros_like(x)
+    for i in np.ndindex(*x.shape):
+        was = x[i]
+        x[i] = was + step
+        up = f()
+        x[i] = was - step
+        g[i] = (up - f()) / (2 * step)
+        x[i] = was
+    return g
+
+
+# ------------------------------------------------------------------ embedding
+def test_embedding_gradient_is_the_difference():
+    rng = np.random.default_rng(0)
+    table, D = rng.standard_normal((5, 3)), rng.standard_normal((9, 3))
+    ids = np.array([0, 4, 4, -1, 2, 0, 4, 7, -3])
+    G, mag = O.embed_backward(ids, D, 1.5, 5)
+    np.testing.assert_allclose(G, difference(lambda: (O.embed(table, ids, 1.5) * D).sum(), table), atol=1e-8)
+    assert (G[[1, 3]] == 0).all() and (mag >= np.abs(G)).all()
+
+
+@pytest.mark.parametrize("args,status", [((0, 8, 0, 1), bp.BP_EINVAL), (((1 << 24) + 1, 8, 0, 1), bp.BP_EINVAL),
+                                         ((4, 0, 0, 1), bp.BP_EINVAL), ((4, (1 << 20) + 1, 0, 1), bp.BP_EINVAL),
+                                         ((4, 8, 2, 1), bp.BP_EINVAL), ((4, 8, 0, 0), bp.BP_EINVAL),
+                                         ((4, 8, 0, (1 << 26) + 1), bp.BP_EINVAL), ((4, 12, 1, 1), bp.BP_ESHAPE)])
+def test_embedding_create_refuses(lib, args, status):
+    out = ctypes.c_void_p()
+    assert lib.bp_embedding_create(*args, ctypes.byref(out)) == status
+    assert out.value is None and lib.bp_last_error()
+    assert lib.bp_embedding_create(4, 8, 0, 1, None) == bp.BP_EINVAL
+
+
+def test_null_embeddings_are_refused(lib):
+    assert lib.bp_embed(None, P, P, 1, 1.0, P, None) == bp.BP_EINVAL
+    assert lib.bp_embed_backward(None, P, 1, P, 1.0, P, 0, None) == bp.BP_EINVAL
+    assert lib.bp_embedding_check(None, None) == bp.BP_EINVAL
+    lib.bp_embedding_destroy(None)   # NULL-safe
