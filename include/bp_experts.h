@@ -3,7 +3,8 @@
  * the pattern.
  *
  *   Router    chooses k of E experts for each pattern, their gates, and the order
- *             in which the experts' rows lie;
+ *             in which the experts' rows lie, by the logits (Router) or by scores and a
+ *             bias within groups of experts (ScoredRouter);
  *   Experts   E fully connected layers of one shape; each row is multiplied by the
  *             weights of its own expert (products grouped by expert, ragged);
  *   Mix       each pattern's gated sum of its experts' outputs;
@@ -42,12 +43,14 @@ extern "C" {
 #endif
 
 typedef struct bp_router bp_router;
+typedef struct bp_scored_router bp_scored_router;
 typedef struct bp_experts bp_experts;
 typedef struct bp_adapters bp_adapters;
 
 #define BP_MAX_EXPERTS 512     /* experts of a router or of an expert layer */
 #define BP_MAX_CHOICES 16      /* experts of one pattern (k) */
 #define BP_MAX_RANK 128        /* rank of an adapter */
+#define BP_MAX_GROUPS 32       /* groups of experts of a router by scores */
 
 /* Gates of the chosen experts S of a pattern with logits z:
  *   BP_GATES_CHOSEN  g_j = exp(z_j) / sum over S of exp(z);
@@ -80,6 +83,35 @@ bp_status bp_route(bp_router* router, const void* d_logits, int n, int* d_expert
  * is not read.  Errors: BP_EINVAL, BP_ECUDA. */
 bp_status bp_route_backward(bp_router* router, const void* d_logits, int n, const int* d_expert,
                             const float* d_gate, const float* d_dgate, void* d_dlogits, void* stream);
+
+/* Scores of a pattern with logits z, over all E experts:
+ *   BP_SCORES_SOFTMAX  s_e = exp(z_e) / sum of exp(z);
+ *   BP_SCORES_SIGMOID  s_e = 1 / (1 + exp(-z_e)). */
+enum { BP_SCORES_SOFTMAX = 0, BP_SCORES_SIGMOID = 1 };
+
+/* A router that chooses by scores: experts lie in n_groups groups of n_experts / n_groups consecutive ones
+ * (1 <= n_groups <= BP_MAX_GROUPS, a divisor of n_experts), of which a pattern's open_groups best stay open;
+ * a group's value is its largest score (group_top 1) or the sum of its two largest (2).  k is at most
+ * BP_MAX_CHOICES and the experts of open_groups groups.  scale: finite.  Errors: as bp_router_create. */
+bp_status bp_scored_router_create(int n_experts, int k, int dtype, int max_patterns, int scores, int n_groups,
+                                  int open_groups, int group_top, int renormalise, float scale,
+                                  bp_scored_router** out);
+void bp_scored_router_destroy(bp_scored_router* router);   /* NULL-safe; synchronises the device */
+
+/* Choice, gates and order for n patterns with logits d_logits [n, E] and a bias d_bias [E] (float32; NULL: 0):
+ * the open groups are those of largest value by s + bias, and the choice the k experts of largest s + bias in them,
+ * both as float64 has them, ties to the lowest index.  An expert whose logit or bias is -infinity or NaN is closed:
+ * not chosen, and no part of its group's value.  A gate is scale * s_j, without the bias; with renormalise
+ * scale * s_j / (sum of the chosen experts' s).  The outputs are as bp_route writes them, NaN gates included.
+ * Errors: BP_EINVAL, BP_ECUDA. */
+bp_status bp_route_scored(bp_scored_router* router, const void* d_logits, const float* d_bias, int n, int* d_expert,
+                          float* d_gate, int* d_offsets, int* d_source, int* d_place, void* stream);
+
+/* d_dlogits [n, E] (the router's dtype, written in full) from the gradient d_dgate [n, k] of the gates; d_expert as
+ * bp_route_scored wrote it.  dgate beside an expert of -1 is not read.  The choice and the bias have no
+ * gradient.  Errors: BP_EINVAL, BP_ECUDA. */
+bp_status bp_route_scored_backward(bp_scored_router* router, const void* d_logits, int n, const int* d_expert,
+                                   const float* d_dgate, void* d_dlogits, void* stream);
 
 /* d_Y [n, n_out] = sum over j < k of d_gate[t, j] * d_H[d_place[t, j]], d_H [n_rows, n_out];
  * d_gate NULL: gates of 1 (the sum of a pattern's rows, as the gradient of inputs that

@@ -60,6 +60,90 @@ def route_backward(z, expert, gate, dgate, gates):
 
 
 # ------------------------------------------------------------------ mix
+def scores_of(z, kind):
+    """Softmax or sigmoid scores of the logits; 0 for a logit of -infinity or NaN (among those that are none)."""
+    closed = ~(z > -np.inf)
+    with np.errstate(invalid="ignore", over="ignore", divide="ignore"):
+        if kind == "sigmoid":
+            p = 1.0 / (1.0 + np.exp(-z))
+        else:
+            peak = np.max(np.where(closed, -np.inf, z), axis=1, keepdims=True)
+            up = np.where(z == peak, 1.0, np.exp(z - peak))   # (infinite logits too)
+            up[closed] = 0.0
+            p = up / up.sum(1, keepdims=True)
+    return np.where(closed, 0.0, p)
+
+
+def route_scored(z, bias, k, kind, n_groups=1, open_groups=1, group_top=1, renormalise=False, scale=1.0):
+    """(expert, gate, offsets, source, place) of logits z [n, E] by scores and a bias [E] (None: 0)."""
+    n, E = z.shape
+    b = np.zeros(E) if bias is None else bias
+    p = scores_of(z, kind)
+    c = np.where((z > -np.inf) & (b > -np.inf), p + b, -np.inf)
+    if n_groups > 1:
+        by = np.sort(c.reshape(n, n_groups, -1), axis=2)[:, :, ::-1]
+        worth = by[:, :, 0].copy()
+        if group_top == 2 and by.shape[2] > 1:
+            two = by[:, :, 1] > -np.inf
+            worth[two] += by[:, :, 1][two]
+        best = np.argsort(-worth, axis=1, kind="stable")[:, :open_groups]
+        stays = np.zeros((n, n_groups), dtype=bool)
+        np.put_along_axis(stays, best, True, axis=1)
+        c = np.where(np.repeat(stays, E // n_groups, axis=1), c, -np.inf)
+    expert = np.argsort(-c, axis=1, kind="stable")[:, :k].astype(np.int32)
+    chosen = np.take_along_axis(c, expert, 1) > -np.inf
+    gate = np.where(chosen, scale * _shares(z, p, expert, chosen, kind, renormalise), 0.0)
+    gate[np.isnan(z).any(1, keepdims=True) & chosen] = np.nan
+    expert[~chosen] = -1
+    flat = expert.ravel().astype(np.int64)
+    rows = np.argsort(np.where(flat < 0, E, flat), kind="stable")
+    offsets = np.concatenate([[0], np.cumsum(np.bincount(flat[flat >= 0], minlength=E))]).astype(np.int32)
+    source, place = np.full(n * k, -1, dtype=np.int32), np.full(n * k, -1, dtype=np.int32)
+    rows = rows[:offsets[E]]
+    source[:len(rows)] = rows // k
+    place[rows] = np.arange(len(rows))
+    return expert, gate, offsets, source, place.reshape(n, k)
+
+
+def _shares(z, p, expert, chosen, kind, renormalise):
+    """Scores of the chosen experts, or their parts of the sum, by logarithms (which do not vanish)."""
+    if not renormalise:
+        return np.where(chosen, np.take_along_axis(p, np.maximum(expert, 0), 1), 0.0)
+    zc = np.take_along_axis(z, np.maximum(expert, 0), 1)
+    a = np.minimum(zc, 0.0) if kind == "sigmoid" else zc
+    peak = np.max(np.where(chosen, a, -np.inf), axis=1, keepdims=True)
+    with np.errstate(invalid="ignore"):
+        w = np.where(a == peak, 1.0, np.exp(a - peak))
+        if kind == "sigmoid":
+            w = w / (1.0 + np.exp(-np.abs(zc)))
+    w = np.where(chosen, w, 0.0)
+    total = w.sum(1, keepdims=True)
+    return w / np.where(total > 0, total, 1.0)
+
+
+def route_scored_backward(z, expert, dgate, kind, renormalise=False, scale=1.0):
+    """The gates' gradient by the logits, and the magnitudes of its terms."""
+    out, mag = np.zeros(z.shape), np.zeros(z.shape)
+    p, chosen = scores_of(z, kind), expert >= 0
+    share = _shares(z, p, expert, chosen, kind, renormalise)
+    u = np.where(chosen, scale * dgate, 0.0)
+    pull, pull_mag = (share * u).sum(1, keepdims=True), (share * np.abs(u)).sum(1, keepdims=True)
+    if kind == "softmax" and not renormalise:
+        out, mag = -p * pull, p * pull_mag
+    at = np.maximum(expert, 0)
+    if renormalise or kind == "softmax":
+        d, m = share * (u - pull), share * (np.abs(u) + pull_mag)
+    else:
+        d, m = share * u, share * np.abs(u)
+    if kind == "sigmoid":
+        with np.errstate(over="ignore"):
+            d, m = (x / (1.0 + np.exp(np.take_along_axis(z, at, 1))) for x in (d, m))
+    for j in range(expert.shape[1]):
+        t = np.nonzero(chosen[:, j])[0]
+        out[t, expert[t, j]], mag[t, expert[t, j]] = d[t, j], m[t, j]
+    return out, mag
+
+
 def mix(H, place, gate):
     y = np.zeros((place.shape[0], H.shape[1]))
     for t in range(place.shape[0]):

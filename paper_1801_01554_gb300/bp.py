@@ -23,6 +23,8 @@ BP_SIGMOID_LOGISTIC, BP_SIGMOID_TABLE = 0, 1
 BP_MAX_SIZES = 9
 BP_MAX_EXPERTS, BP_MAX_CHOICES, BP_MAX_RANK = 512, 16, 128
 BP_GATES_CHOSEN, BP_GATES_ALL = 0, 1
+BP_MAX_GROUPS = 32
+BP_SCORES_SOFTMAX, BP_SCORES_SIGMOID = 0, 1
 BP_MAX_TOKENS, BP_MAX_IDS = 1 << 24, 1 << 26
 
 # name -> (restype, argtypes); every symbol declared in include/
@@ -61,6 +63,10 @@ SIGNATURES = {
     "bp_router_destroy": (None, [_VP]),
     "bp_route": (_I, [_VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _VP]),
     "bp_route_backward": (_I, [_VP, _VP, _I, _VP, _VP, _VP, _VP, _VP]),
+    "bp_scored_router_create": (_I, [_I, _I, _I, _I, _I, _I, _I, _I, _I, _F, ctypes.POINTER(_VP)]),
+    "bp_scored_router_destroy": (None, [_VP]),
+    "bp_route_scored": (_I, [_VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "bp_route_scored_backward": (_I, [_VP, _VP, _I, _VP, _VP, _VP, _VP]),
     "bp_mix": (_I, [_VP, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP]),
     "bp_mix_backward": (_I, [_VP, _VP, _I, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _VP]),
     "bp_experts_create": (_I, [_I, _I, _I, _I, _I, ctypes.POINTER(_VP)]),
@@ -375,6 +381,32 @@ def bp_route_backward(h, logits, n, expert, gate, dgate, dlogits, dtype=BP_F32, 
                                     _stream(stream)))
 
 
+def bp_scored_router_create(n_experts, k, dtype=BP_F32, max_patterns=1024, scores=BP_SCORES_SOFTMAX, n_groups=1,
+                            open_groups=1, group_top=1, renormalise=False, scale=1.0):
+    out = ctypes.c_void_p()
+    _check(load().bp_scored_router_create(int(n_experts), int(k), int(dtype), int(max_patterns), int(scores),
+                                          int(n_groups), int(open_groups), int(group_top), 1 if renormalise else 0,
+                                          float(scale), ctypes.byref(out)))
+    return out.value
+
+
+def bp_scored_router_destroy(h):
+    load().bp_scored_router_destroy(h)
+
+
+def bp_route_scored(h, logits, bias, n, expert, gate, offsets, source, place, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_route_scored(h, _values(logits, dtype, "logits", room[0]), _floats(bias, "bias", room[3]), n,
+                                  _ints(expert, "expert", room[1]), _floats(gate, "gate", room[1]),
+                                  _ints(offsets, "offsets", room[2]), _ints(source, "source", room[1]),
+                                  _ints(place, "place", room[1]), _stream(stream)))
+
+
+def bp_route_scored_backward(h, logits, n, expert, dgate, dlogits, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    _check(load().bp_route_scored_backward(h, _values(logits, dtype, "logits", room[0]), n,
+                                           _ints(expert, "expert", room[1]), _floats(dgate, "dgate", room[1]),
+                                           _values(dlogits, dtype, "dlogits", room[0]), _stream(stream)))
+
+
 def bp_mix(H, n_rows, place, gate, n, k, n_out, dtype, Y, stream=None):
     _check(load().bp_mix(_values(H, dtype, "H", n_rows * n_out), n_rows, _ints(place, "place", n * k),
                          _floats(gate, "gate", n * k), n, k, n_out, dtype, _values(Y, dtype, "Y", n * n_out),
@@ -521,6 +553,26 @@ class Router(_Handle):
     def backward(self, logits, n, expert, gate, dgate, dlogits, stream=None):
         bp_route_backward(self.h, logits, n, expert, gate, dgate, dlogits, self.dtype, stream,
                           (n * self.n_experts, n * self.k))
+
+
+class ScoredRouter(_Handle):
+    """Owns one bp_scored_router handle; methods forward to bp_route_scored and bp_route_scored_backward."""
+
+    _free = staticmethod(bp_scored_router_destroy)
+
+    def __init__(self, n_experts, k, dtype=BP_F32, max_patterns=1024, scores=BP_SCORES_SOFTMAX, n_groups=1, open_groups=1,
+                 group_top=1, renormalise=False, scale=1.0):
+        self.n_experts, self.k, self.dtype = int(n_experts), int(k), dtype
+        self.h = bp_scored_router_create(n_experts, k, dtype, max_patterns, scores, n_groups, open_groups, group_top,
+                                         renormalise, scale)
+
+    def forward(self, logits, bias, n, expert, gate, offsets, source, place, stream=None):
+        bp_route_scored(self.h, logits, bias, n, expert, gate, offsets, source, place, self.dtype, stream,
+                        (n * self.n_experts, n * self.k, self.n_experts + 1, self.n_experts))
+
+    def backward(self, logits, n, expert, dgate, dlogits, stream=None):
+        bp_route_scored_backward(self.h, logits, n, expert, dgate, dlogits, self.dtype, stream,
+                                 (n * self.n_experts, n * self.k))
 
 
 class Experts(_Handle):

@@ -60,6 +60,15 @@ inline bp_status check_range(const char* call, const char* what, long long v, lo
     return fail(BP_EINVAL, "%s: %s must be in [%lld, %lld] (got %lld)", call, what, lo, hi, v);
 }
 
+// A handle's scratch is the device's that was current when it was made.
+inline bp_status check_device(const char* call, int device) {
+    int now = 0;
+    const cudaError_t e = cudaGetDevice(&now);
+    if (e != cudaSuccess) return cuda_status(e, call);
+    if (now == device) return BP_OK;
+    return fail(BP_EINVAL, "%s: the handle belongs to device %d (current: %d)", call, device, now);
+}
+
 // Zeros that blocks count their arrivals with (there once layer_ready has returned).
 inline bp_status make_counts(unsigned** counts, size_t n, const char* call) {
     cudaError_t e = cudaMalloc(counts, n * sizeof(unsigned));

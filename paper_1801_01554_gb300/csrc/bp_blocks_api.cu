@@ -29,15 +29,6 @@ bp_status check_width(const char* call, int width, int most, int dtype) {
     return st;
 }
 
-// The handle's scratch and its kernels' addresses are the device's that was current when it was made.
-bp_status check_device(const char* call, int device) {
-    int now = 0;
-    const cudaError_t e = cudaGetDevice(&now);
-    if (e != cudaSuccess) return cuda_status(e, call);
-    if (now == device) return BP_OK;
-    return fail(BP_EINVAL, "%s: the handle belongs to device %d (current: %d)", call, device, now);
-}
-
 bp_status check_finite(const char* call, const char* what, float x) {
     if (std::isfinite(x)) return BP_OK;
     return fail(BP_EINVAL, "%s: %s must be finite", call, what);

@@ -2,6 +2,7 @@
 // argument checks, handles and the choice of kernels.
 #include <cuda_runtime.h>
 
+#include <cmath>
 #include <new>
 
 #include "bp_api_checks.h"
@@ -14,6 +15,10 @@ struct bp_router {
     int* hist = nullptr;
 };
 
+struct bp_scored_router {
+    ScoredArgs a{};
+    int cap = 0, device = 0;
+};
 struct bp_experts {
     int E = 0, n_in = 0, n_out = 0, dtype = BP_F32, cap = 0, num_sms = 0;
     int* flags = nullptr;
@@ -142,6 +147,98 @@ bp_status bp_route_backward(bp_router* r, const void* d_logits, int n, const int
     const RouteArgs a{n, r->E, r->k, r->gates, r->dtype, d_logits, const_cast<int*>(d_expert),
                       const_cast<float*>(d_gate), nullptr, nullptr, nullptr, r->hist};
     return cuda_status(route_backward(a, d_dgate, d_dlogits, (cudaStream_t)stream), call);
+}
+
+// ------------------------------------------------------------ router by scores
+bp_status bp_scored_router_create(int n_experts, int k, int dtype, int max_patterns, int scores, int n_groups,
+                                  int open_groups, int group_top, int renormalise, float scale, bp_scored_router** out) {
+    const char* call = "bp_scored_router_create";
+    set_error_message("");
+    if (out == nullptr) return fail(BP_EINVAL, "%s: NULL argument", call);
+    bp_status st = check_range(call, "n_experts", n_experts, 1, BP_MAX_EXPERTS);
+    if (st == BP_OK) st = check_range(call, "n_groups", n_groups, 1, BP_MAX_GROUPS);
+    if (st == BP_OK && n_experts % n_groups != 0)
+        st = fail(BP_EINVAL, "%s: n_groups must divide n_experts (got %d of %d)", call, n_groups, n_experts);
+    if (st == BP_OK) st = check_range(call, "open_groups", open_groups, 1, n_groups);
+    if (st == BP_OK) st = check_range(call, "group_top", group_top, 1, 2);
+    if (st != BP_OK) return st;
+    const int most = n_experts / n_groups * open_groups;
+    st = check_range(call, "k", k, 1, most < BP_MAX_CHOICES ? most : BP_MAX_CHOICES);
+    if (st == BP_OK) st = check_dtype(call, dtype);
+    if (st == BP_OK) st = check_range(call, "max_patterns", max_patterns, 1, kMaxRows / k);
+    if (st == BP_OK && scores != BP_SCORES_SOFTMAX && scores != BP_SCORES_SIGMOID)
+        st = fail(BP_EINVAL, "%s: unknown scores %d", call, scores);
+    if (st == BP_OK && !std::isfinite(scale)) st = fail(BP_EINVAL, "%s: scale must be finite", call);
+    if (st != BP_OK) return st;
+    bp_scored_router* r = new (std::nothrow) bp_scored_router();
+    if (r == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
+    r->cap = max_patterns;
+    r->a.E = r->a.r.E = n_experts;
+    r->a.r.k = k;
+    r->a.r.dtype = dtype;
+    r->a.scores = scores;
+    r->a.n_groups = n_groups;
+    r->a.open_groups = open_groups;
+    r->a.group_top = group_top;
+    r->a.renormalise = renormalise != 0;
+    r->a.scale = scale;
+    const size_t blocks = ((size_t)max_patterns + kRoutePatterns - 1) / kRoutePatterns;
+    st = cuda_status(cudaGetDevice(&r->device), call);
+    if (st == BP_OK) st = cuda_status(cudaMalloc(&r->a.r.hist, (blocks + 1) * n_experts * sizeof(int)), call);
+    if (st != BP_OK) {
+        delete r;
+        return st;
+    }
+    *out = r;
+    return BP_OK;
+}
+
+void bp_scored_router_destroy(bp_scored_router* r) {
+    if (r == nullptr) return;
+    cudaDeviceSynchronize();
+    cudaFree(r->a.r.hist);
+    delete r;
+}
+
+bp_status bp_route_scored(bp_scored_router* r, const void* d_logits, const float* d_bias, int n, int* d_expert, float* d_gate,
+                          int* d_offsets, int* d_source, int* d_place, void* stream) {
+    const char* call = "bp_route_scored";
+    if (r == nullptr) return fail(BP_EINVAL, "%s: NULL router", call);
+    bp_status st = check_range(call, "n", n, 0, r->cap);
+    const bool rows = n > 0;
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_logits, "d_logits", r->a.r.dtype == BP_BF16 ? 2 : 4, rows},
+                                  {d_bias, "d_bias", 4, false},
+                                  {d_expert, "d_expert", 4, rows},
+                                  {d_gate, "d_gate", 4, rows},
+                                  {d_offsets, "d_offsets", 4, true},
+                                  {d_source, "d_source", 4, rows},
+                                  {d_place, "d_place", 4, rows}});
+    if (st == BP_OK) st = check_device(call, r->device);
+    if (st != BP_OK) return st;
+    ScoredArgs a = r->a;
+    a.r.n = n, a.r.logits = d_logits, a.r.expert = d_expert, a.r.gate = d_gate;
+    a.r.offsets = d_offsets, a.r.source = d_source, a.r.place = d_place, a.bias = d_bias;
+    return cuda_status(route_scored_forward(a, (cudaStream_t)stream), call);
+}
+
+bp_status bp_route_scored_backward(bp_scored_router* r, const void* d_logits, int n, const int* d_expert, const float* d_dgate,
+                                   void* d_dlogits, void* stream) {
+    const char* call = "bp_route_scored_backward";
+    if (r == nullptr) return fail(BP_EINVAL, "%s: NULL router", call);
+    bp_status st = check_range(call, "n", n, 0, r->cap);
+    const bool rows = n > 0;
+    const int align = r->a.r.dtype == BP_BF16 ? 2 : 4;
+    if (st == BP_OK)
+        st = check_buffers(call, {{d_logits, "d_logits", align, rows},
+                                  {d_expert, "d_expert", 4, rows},
+                                  {d_dgate, "d_dgate", 4, rows},
+                                  {d_dlogits, "d_dlogits", align, rows}});
+    if (st == BP_OK) st = check_device(call, r->device);
+    if (st != BP_OK || !rows) return st;
+    ScoredArgs a = r->a;
+    a.r.n = n, a.r.logits = d_logits, a.r.expert = const_cast<int*>(d_expert);
+    return cuda_status(route_scored_backward(a, d_dgate, d_dlogits, (cudaStream_t)stream), call);
 }
 
 // ------------------------------------------------------------ mix

@@ -184,6 +184,18 @@ struct RouteArgs {
 constexpr int kRoutePatterns = 32;   // patterns of a block
 cudaError_t route_forward(const RouteArgs& a, cudaStream_t s);
 cudaError_t route_backward(const RouteArgs& a, const float* dgate, void* dlogits, cudaStream_t s);
+// Rows of the choices in a.expert, from the counts in a.hist (the last two launches of a long call).
+cudaError_t route_order(const RouteArgs& a, cudaStream_t s);
+// The router by scores (bp_route_scored.cu).
+struct ScoredArgs {
+    RouteArgs r;
+    int E, scores, n_groups, open_groups, group_top, renormalise;
+    float scale;
+    const float* bias;      // [E] or NULL
+    int group_lanes, per;   // lanes of a group, experts of a lane (set by the launcher)
+};
+cudaError_t route_scored_forward(ScoredArgs a, cudaStream_t s);
+cudaError_t route_scored_backward(const ScoredArgs& a, const float* dgate, void* dlogits, cudaStream_t s);
 struct MixArgs {
     int n, k, n_rows, N, dtype;
     const void* H;

@@ -2,7 +2,7 @@
 // experts' outputs, with their gradients.
 #include <cmath>
 
-#include "bp_experts_device.cuh"
+#include "bp_route_device.cuh"
 #include "bp_tc_device.cuh"
 
 namespace bp {
@@ -13,81 +13,6 @@ namespace {
 // the order (16,384 patterns of 64 experts: 128 patterns a block took 21 us for the choice alone).
 constexpr int kOneBlock = 256, kOneThreads = 1024;
 constexpr int kRouteThreads = 256;
-
-// Ascending whole numbers for ascending floats; 0 for NaN and for -infinity, which are never
-// chosen.  (x + 0 turns -0 into +0, so that the two tie.)
-__device__ __forceinline__ unsigned order_of(float x) {
-    const unsigned u = __float_as_uint(x + 0.f);
-    if (!(x > -INFINITY)) return 0u;
-    return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-}
-__device__ __forceinline__ float value_of(unsigned o) {
-    return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o);
-}
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-}
-
-// A block's patterns that chose expert e, as bits: bits[e * kWords + word].
-template <int kWords>
-__device__ __forceinline__ int rank_of(const unsigned* bits, int e, int p) {
-    int r = 0;
-#pragma unroll
-    for (int w = 0; w < kWords; ++w) {
-        const unsigned m = p >= 32 * (w + 1) ? 0xffffffffu : p > 32 * w ? (1u << (p - 32 * w)) - 1u : 0u;
-        r += __popc(bits[e * kWords + w] & m);
-    }
-    return r;
-}
-template <int kWords>
-__device__ __forceinline__ int count_of(const unsigned* bits, int e) {
-    int r = 0;
-#pragma unroll
-    for (int w = 0; w < kWords; ++w) r += __popc(bits[e * kWords + w]);
-    return r;
-}
-
-// Rows of a block's choices: base[e] is the row of the block's first pattern with expert e.
-template <int kWords>
-__device__ __forceinline__ void place_rows(const RouteArgs& g, const unsigned* bits, const int* base, int p0, int np) {
-    for (int i = threadIdx.x; i < np * g.k; i += blockDim.x) {
-        const int p = i / g.k, e = g.expert[(size_t)p0 * g.k + i];
-        int at = -1;
-        if (e >= 0) {
-            at = base[e] + rank_of<kWords>(bits, e, p);
-            g.source[at] = p0 + p;
-        }
-        g.place[(size_t)p0 * g.k + i] = at;
-    }
-}
-
-// Exclusive sums of cnt[0 .. E) by the block, and the total.
-__device__ __forceinline__ int block_scan(int* cnt, int E, int* warp_tot) {
-    int carry = 0;
-    for (int b = 0; b < E; b += blockDim.x) {
-        const int i = b + threadIdx.x, lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-        const int x = i < E ? cnt[i] : 0;
-        int s = x;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += y;
-        }
-        __syncthreads();
-        if (lane == 31) warp_tot[w] = s;
-        __syncthreads();
-        int before = carry;
-        for (int v = 0; v < (int)blockDim.x / 32; ++v) {
-            if (v < w) before += warp_tot[v];
-            carry += warp_tot[v];
-        }
-        if (i < E) cnt[i] = before + s - x;
-    }
-    __syncthreads();
-    return carry;
-}
 
 // A warp a pattern, lane l with the logits of experts l, l + 32, ..: k times the largest one
 // left (by its order, then by the lowest index).
@@ -415,14 +340,18 @@ int mix_warps(int n, int N, int per_warp) {
 
 }  // namespace
 
+cudaError_t route_order(const RouteArgs& a, cudaStream_t s) {
+    const int blocks = (a.n + kRoutePatterns - 1) / kRoutePatterns;
+    const cudaError_t e = launch_pdl(k_route_columns, a.E, 1, kRouteThreads, 0, s, a, blocks);
+    return e != cudaSuccess ? e : launch_pdl(k_route_place, blocks, 1, kRouteThreads, 0, s, a);
+}
+
 cudaError_t route_forward(const RouteArgs& a, cudaStream_t s) {
     const bool f32 = a.dtype == BP_F32;
     if (a.n <= kOneBlock) return f32 ? launch_route<float, true>(a, 1, s) : launch_route<bf16, true>(a, 1, s);
     const int blocks = (a.n + kRoutePatterns - 1) / kRoutePatterns;
-    cudaError_t e = f32 ? launch_route<float, false>(a, blocks, s) : launch_route<bf16, false>(a, blocks, s);
-    if (e == cudaSuccess) e = launch_pdl(k_route_columns, a.E, 1, kRouteThreads, 0, s, a, blocks);
-    if (e == cudaSuccess) e = launch_pdl(k_route_place, blocks, 1, kRouteThreads, 0, s, a);
-    return e;
+    const cudaError_t e = f32 ? launch_route<float, false>(a, blocks, s) : launch_route<bf16, false>(a, blocks, s);
+    return e != cudaSuccess ? e : route_order(a, s);
 }
 
 cudaError_t route_backward(const RouteArgs& a, const float* dgate, void* dlogits, cudaStream_t s) {
