@@ -25,7 +25,8 @@ BP_MAX_EXPERTS, BP_MAX_CHOICES, BP_MAX_RANK = 512, 16, 128
 BP_GATES_CHOSEN, BP_GATES_ALL = 0, 1
 BP_MAX_GROUPS = 32
 BP_SCORES_SOFTMAX, BP_SCORES_SIGMOID = 0, 1
-BP_MAX_TOKENS, BP_MAX_IDS = 1 << 24, 1 << 26
+BP_MAX_TOKENS, BP_MAX_IDS, BP_MAX_WIDTH = 1 << 24, 1 << 26, 8192
+BP_NORM_NONE, BP_NORM_RMS, BP_NORM_LAYER = 0, 1, 2
 
 # name -> (restype, argtypes); every symbol declared in include/
 _VP = ctypes.c_void_p
@@ -85,6 +86,12 @@ SIGNATURES = {
     "bp_embed": (_I, [_VP, _VP, _VP, _I, _F, _VP, _VP]),
     "bp_embed_backward": (_I, [_VP, _VP, _I, _VP, _F, _VP, _I, _VP]),
     "bp_embedding_check": (_I, [_VP, _VP]),
+    "bp_residual_create": (_I, [_I, _I, _I, _I, _I, _I, _F, ctypes.POINTER(_VP)]),
+    "bp_residual_destroy": (None, [_VP]),
+    "bp_residual_forward": (_I, [_VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _I, _F, _VP, _VP, _VP, _VP, _VP, _VP]),
+    "bp_residual_backward": (_I, [_VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _I, _F, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
+                                  _VP, _VP, _VP, _I, _VP]),
+    "bp_residual_check": (_I, [_VP, _VP]),
 }
 
 
@@ -513,6 +520,43 @@ def bp_embedding_check(h, stream=None):
     _check(load().bp_embedding_check(h, _stream(stream)))
 
 
+def bp_residual_create(width, dtype=BP_F32, max_rows=1024, max_gates=1, norm_out=BP_NORM_NONE, norm_in=BP_NORM_RMS, eps=1e-5):
+    out = ctypes.c_void_p()
+    _check(load().bp_residual_create(int(width), int(dtype), int(max_rows), int(max_gates), int(norm_out), int(norm_in),
+                                     float(eps), ctypes.byref(out)))
+    return out.value
+
+
+def bp_residual_destroy(h):
+    load().bp_residual_destroy(h)
+
+
+def bp_residual_forward(h, X, F, n, wo, bo, gate, offsets, n_gates, scale, wi, bi, Y, H, stats, dtype=BP_F32, stream=None,
+                        room=_NO_ROOM):
+    w = room[1]
+    _check(load().bp_residual_forward(
+        h, _values(X, dtype, "X", room[0]), _values(F, dtype, "F", room[0]), n, _floats(wo, "wo", w), _floats(bo, "bo", w),
+        _floats(gate, "gate", n_gates * w), _ints(offsets, "offsets", n_gates + 1 if w else 0), n_gates, scale,
+        _floats(wi, "wi", w), _floats(bi, "bi", w), _values(Y, dtype, "Y", room[0]), _values(H, dtype, "H", room[0]),
+        _floats(stats, "stats", room[2]), _stream(stream)))
+
+
+def bp_residual_backward(h, Y, F, n, wo, bo, gate, offsets, n_gates, scale, wi, stats, dY, dH, dX, dF, Gwo, Gbo, Ggate, Gwi,
+                         Gbi, accumulate=False, dtype=BP_F32, stream=None, room=_NO_ROOM):
+    r, w = room[0], room[1]
+    _check(load().bp_residual_backward(
+        h, _values(Y, dtype, "Y", r), _values(F, dtype, "F", r), n, _floats(wo, "wo", w), _floats(bo, "bo", w),
+        _floats(gate, "gate", n_gates * w), _ints(offsets, "offsets", n_gates + 1 if w else 0), n_gates, scale,
+        _floats(wi, "wi", w), _floats(stats, "stats", room[2]), _values(dY, dtype, "dY", r), _values(dH, dtype, "dH", r),
+        _values(dX, dtype, "dX", r), _values(dF, dtype, "dF", r), _floats(Gwo, "Gwo", w), _floats(Gbo, "Gbo", w),
+        _floats(Ggate, "Ggate", n_gates * w), _floats(Gwi, "Gwi", w), _floats(Gbi, "Gbi", w), 1 if accumulate else 0,
+        _stream(stream)))
+
+
+def bp_residual_check(h, stream=None):
+    _check(load().bp_residual_check(h, _stream(stream)))
+
+
 # ------------------------------------------------------------------ convenience
 class _Handle:
     """A handle of the library, freed by close() or at the end of a with block."""
@@ -648,6 +692,29 @@ class Embedding(_Handle):
 
     def check(self, stream=None):
         bp_embedding_check(self.h, stream)
+
+
+class Residual(_Handle):
+    """Owns one bp_residual handle; methods forward to the C names above."""
+
+    _free = staticmethod(bp_residual_destroy)
+
+    def __init__(self, width, dtype=BP_F32, max_rows=1024, norm_out=BP_NORM_NONE, norm_in=BP_NORM_RMS, eps=1e-5, max_gates=1):
+        self.width, self.dtype = int(width), dtype
+        self.h = bp_residual_create(width, dtype, max_rows, max_gates, norm_out, norm_in, eps)
+
+    def forward(self, X, F, n, Y, H=None, stats=None, wo=None, bo=None, gate=None, offsets=None, n_gates=0, scale=1.0, wi=None,
+                bi=None, stream=None):
+        bp_residual_forward(self.h, X, F, n, wo, bo, gate, offsets, n_gates, scale, wi, bi, Y, H, stats, self.dtype, stream,
+                            (n * self.width, self.width, 4 * n))
+
+    def backward(self, Y, F, n, stats, dY, dH, dX=None, dF=None, wo=None, bo=None, gate=None, offsets=None, n_gates=0, scale=1.0,
+                 wi=None, Gwo=None, Gbo=None, Ggate=None, Gwi=None, Gbi=None, accumulate=False, stream=None):
+        bp_residual_backward(self.h, Y, F, n, wo, bo, gate, offsets, n_gates, scale, wi, stats, dY, dH, dX, dF, Gwo, Gbo, Ggate,
+                             Gwi, Gbi, accumulate, self.dtype, stream, (n * self.width, self.width, 4 * n))
+
+    def check(self, stream=None):
+        bp_residual_check(self.h, stream)
 
 
 class Net:

@@ -19,6 +19,12 @@ struct bp_embedding {
     unsigned* arrived = nullptr;
 };
 
+struct bp_residual {
+    ResidualArgs a{};
+    int cap = 0, max_gates = 0, device = 0;
+    float* sums = nullptr;
+};
+
 namespace {
 
 bp_status check_width(const char* call, int width, int most, int dtype) {
@@ -140,6 +146,146 @@ bp_status bp_embedding_check(bp_embedding* l, void* stream) {
     if (l == nullptr) return fail(BP_EINVAL, "%s: NULL layer", call);
     const bp_status st = check_device(call, l->device);
     return st != BP_OK ? st : read_flags(l->flags, nullptr, 0, stream, call, "an id of a call was out of range");
+}
+
+// ------------------------------------------------------------ residual stream
+bp_status bp_residual_create(int width, int dtype, int max_rows, int max_gates, int norm_out, int norm_in, float eps,
+                             bp_residual** out) {
+    const char* call = "bp_residual_create";
+    set_error_message("");
+    if (out == nullptr) return fail(BP_EINVAL, "%s: NULL argument", call);
+    bp_status st = check_width(call, width, BP_MAX_WIDTH, dtype);
+    if (st == BP_OK) st = check_range(call, "max_rows", max_rows, 1, kMaxRows);
+    if (st == BP_OK) st = check_range(call, "max_gates", max_gates, 0, kMaxRows);
+    if (st == BP_OK) st = check_range(call, "norm_out", norm_out, BP_NORM_NONE, BP_NORM_LAYER);
+    if (st == BP_OK) st = check_range(call, "norm_in", norm_in, BP_NORM_NONE, BP_NORM_LAYER);
+    if (st == BP_OK && !(std::isfinite(eps) && eps > 0.f)) st = fail(BP_EINVAL, "%s: eps must be finite and above 0", call);
+    if (st != BP_OK) return st;
+    bp_residual* l = new (std::nothrow) bp_residual();
+    if (l == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
+    l->cap = max_rows;
+    l->max_gates = max_gates;
+    l->a.width = width, l->a.dtype = dtype, l->a.norm_out = norm_out, l->a.norm_in = norm_in, l->a.eps = eps;
+    st = make_flags(&l->device, &l->a.flags, call);
+    if (st == BP_OK) st = cuda_status(cudaDeviceGetAttribute(&l->a.num_sms, cudaDevAttrMultiProcessorCount, l->device), call);
+    if (st == BP_OK) {
+        const size_t blocks = residual_most_ctas(l->a.num_sms, width, dtype), w = width;
+        const bool layer = norm_out == BP_NORM_LAYER || norm_in == BP_NORM_LAYER;
+        const size_t by_gates = max_gates > 0 ? (blocks + max_gates) * w : 0;
+        st = make_array(&l->sums, 2 * blocks * w + by_gates + (layer ? 2 * blocks * w + by_gates : 0), call);
+        float* p = l->sums;
+        const auto take = [&](size_t n) { return p += n, p - n; };
+        if (st == BP_OK) {
+            l->a.A = take(by_gates), l->a.W = take(blocks * w), l->a.C = take(blocks * w);
+            if (layer) l->a.B = take(by_gates), l->a.WB = take(blocks * w), l->a.D = take(blocks * w);
+        }
+    }
+    if (st == BP_OK) st = layer_ready(call);
+    if (st != BP_OK) {
+        bp_residual_destroy(l);
+        return st;
+    }
+    *out = l;
+    return BP_OK;
+}
+
+void bp_residual_destroy(bp_residual* l) {
+    if (l == nullptr) return;
+    cudaDeviceSynchronize();
+    cudaFree(l->a.flags);
+    cudaFree(l->sums);
+    delete l;
+}
+
+// What both directions check: rows, gates, and operands that the handle's norms do not have.
+static bp_status check_residual(const char* call, const bp_residual* l, int n, const void* F, const float* wo, const float* bo,
+                                const float* gate, const int* offsets, int n_gates, float scale, const float* wi, const float* bi) {
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL stream_layer", call);
+    bp_status st = check_range(call, "n", n, 0, l->cap);
+    if (st == BP_OK) st = check_range(call, "n_gates", n_gates, 0, l->max_gates);
+    if (st == BP_OK) st = check_finite(call, "scale", scale);
+    if (st != BP_OK) return st;
+    if ((gate != nullptr) != (n_gates > 0)) return fail(BP_EINVAL, "%s: d_gate and n_gates do not agree", call);
+    if (offsets == nullptr && n_gates > 1) return fail(BP_EINVAL, "%s: d_offsets is NULL for %d rows of gates", call, n_gates);
+    if (offsets != nullptr && n_gates == 0) return fail(BP_EINVAL, "%s: d_offsets without gates", call);
+    const int out = l->a.norm_out, in = l->a.norm_in;
+    if ((wo != nullptr && out == BP_NORM_NONE) || (bo != nullptr && out != BP_NORM_LAYER))
+        return fail(BP_EINVAL, "%s: the norm of a block's output has no such weight or bias", call);
+    if ((wi != nullptr && in == BP_NORM_NONE) || (bi != nullptr && in != BP_NORM_LAYER))
+        return fail(BP_EINVAL, "%s: the norm before a block has no such weight or bias", call);
+    return check_buffers(call, {{F, "d_F", l->a.dtype == BP_BF16 ? 16 : 4, false}, {wo, "d_wo", 4, false}, {bo, "d_bo", 4, false},
+                                {gate, "d_gate", 4, false}, {offsets, "d_offsets", 4, false}, {wi, "d_wi", 4, false},
+                                {bi, "d_bi", 4, false}});
+}
+
+static ResidualArgs residual_args(const bp_residual* l, int n, const void* F, const float* wo, const float* bo, const float* gate,
+                                  const int* offsets, int n_gates, float scale, const float* wi) {
+    ResidualArgs a = l->a;
+    a.n = n, a.F = F, a.scale = scale, a.wi = wi;
+    if (F != nullptr) a.wo = wo, a.bo = bo, a.gate = gate, a.offsets = offsets, a.n_gates = n_gates;
+    return a;
+}
+
+bp_status bp_residual_forward(bp_residual* l, const void* d_X, const void* d_F, int n, const float* d_wo, const float* d_bo,
+                              const float* d_gate, const int* d_offsets, int n_gates, float scale, const float* d_wi,
+                              const float* d_bi, void* d_Y, void* d_H, float* d_stats, void* stream) {
+    const char* call = "bp_residual_forward";
+    bp_status st = check_residual(call, l, n, d_F, d_wo, d_bo, d_gate, d_offsets, n_gates, scale, d_wi, d_bi);
+    if (st != BP_OK) return st;
+    const int align = l->a.dtype == BP_BF16 ? 16 : 4;
+    st = check_buffers(call, {{d_X, "d_X", align, n > 0}, {d_Y, "d_Y", align, n > 0 && d_F != nullptr}, {d_H, "d_H", align, false},
+                              {d_stats, "d_stats", 4, false}});
+    if (st == BP_OK && d_H != nullptr && l->a.norm_in == BP_NORM_NONE)
+        st = fail(BP_EINVAL, "%s: d_H without a norm before the next block", call);
+    if (st == BP_OK) st = check_device(call, l->device);
+    if (st != BP_OK || n == 0) return st;
+    ResidualArgs a = residual_args(l, n, d_F, d_wo, d_bo, d_gate, d_offsets, n_gates, scale, d_wi);
+    a.X = d_X, a.bi = d_bi, a.Y = d_Y, a.H = d_H, a.stats = d_stats;
+    return cuda_status(residual_forward(a, (cudaStream_t)stream), call);
+}
+
+bp_status bp_residual_backward(bp_residual* l, const void* d_Y, const void* d_F, int n, const float* d_wo, const float* d_bo,
+                               const float* d_gate, const int* d_offsets, int n_gates, float scale, const float* d_wi,
+                               const float* d_stats, const void* d_dY, const void* d_dH, void* d_dX, void* d_dF, float* d_Gwo,
+                               float* d_Gbo, float* d_Ggate, float* d_Gwi, float* d_Gbi, int accumulate, void* stream) {
+    const char* call = "bp_residual_backward";
+    bp_status st = check_residual(call, l, n, d_F, d_wo, d_bo, d_gate, d_offsets, n_gates, scale, d_wi, nullptr);
+    if (st != BP_OK) return st;
+    const int align = l->a.dtype == BP_BF16 ? 16 : 4, out = l->a.norm_out, in = l->a.norm_in;
+    const bool rows = n > 0;
+    st = check_buffers(call, {{d_Y, "d_Y", align, rows && d_dH != nullptr}, {d_stats, "d_stats", 4, rows}, {d_dY, "d_dY", align, false},
+                              {d_dH, "d_dH", align, false}, {d_dX, "d_dX", align, false}, {d_dF, "d_dF", align, false},
+                              {d_Gwo, "d_Gwo", 4, false}, {d_Gbo, "d_Gbo", 4, false}, {d_Ggate, "d_Ggate", 4, false},
+                              {d_Gwi, "d_Gwi", 4, false}, {d_Gbi, "d_Gbi", 4, false}});
+    if (st != BP_OK) return st;
+    if (d_dH != nullptr && in == BP_NORM_NONE) return fail(BP_EINVAL, "%s: d_dH without a norm before the next block", call);
+    if (rows && d_F == nullptr && (d_dF != nullptr || d_Gwo != nullptr || d_Gbo != nullptr || d_Ggate != nullptr))
+        return fail(BP_EINVAL, "%s: gradients of a block's output without d_F", call);
+    if ((d_Gwo != nullptr && out == BP_NORM_NONE) || (d_Gbo != nullptr && out != BP_NORM_LAYER) ||
+        (d_Gwi != nullptr && in == BP_NORM_NONE) || (d_Gbi != nullptr && in != BP_NORM_LAYER))
+        return fail(BP_EINVAL, "%s: a gradient of a weight or bias that the norms do not have", call);
+    if (d_Ggate != nullptr && n_gates == 0) return fail(BP_EINVAL, "%s: d_Ggate without gates", call);
+    st = check_device(call, l->device);
+    if (st != BP_OK) return st;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (!rows) {   // sums of no rows
+        const size_t row = (size_t)l->a.width * sizeof(float);
+        float* const sums[] = {d_Gwo, d_Gbo, d_Gwi, d_Gbi, d_Ggate};
+        for (int i = 0; i < 5 && st == BP_OK && !accumulate; ++i)
+            if (sums[i] != nullptr) st = cuda_status(cudaMemsetAsync(sums[i], 0, i < 4 ? row : row * n_gates, s), call);
+        return st;
+    }
+    ResidualArgs a = residual_args(l, n, d_F, d_wo, d_bo, d_gate, d_offsets, n_gates, scale, d_wi);
+    a.Y = const_cast<void*>(d_Y), a.stats = const_cast<float*>(d_stats), a.dY = d_dY, a.dH = d_dH, a.dX = d_dX, a.dF = d_dF;
+    a.Gwo = d_Gwo, a.Gbo = d_Gbo, a.Ggate = d_Ggate, a.Gwi = d_Gwi, a.Gbi = d_Gbi, a.accumulate = accumulate != 0;
+    return cuda_status(residual_backward(a, s), call);
+}
+
+bp_status bp_residual_check(bp_residual* l, void* stream) {
+    const char* call = "bp_residual_check";
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL stream_layer", call);
+    const bp_status st = check_device(call, l->device);
+    return st != BP_OK ? st : read_flags(l->a.flags, nullptr, 0, stream, call, "the gates' offsets of a call do not go up from 0 to its rows");
 }
 
 }  // extern "C"

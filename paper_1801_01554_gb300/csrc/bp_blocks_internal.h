@@ -32,4 +32,30 @@ cudaError_t embed_setup();
 cudaError_t embed_forward(const EmbedArgs& a, cudaStream_t s);
 cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s);
 
+// ------------------------------------------------------------ residual stream (bp_residual.cu)
+struct ResidualArgs {
+    int n, width, dtype, norm_out, norm_in, num_sms;
+    float eps, scale;
+    const void *X, *F;
+    const float *wo, *bo, *gate, *wi, *bi;
+    const int* offsets;     // of the gates' rows, or NULL
+    int n_gates;
+    void *Y, *H;            // forward: written; backward: Y read
+    float* stats;
+    const void *dY, *dH;    // backward
+    void *dX, *dF;
+    float *Gwo, *Gbo, *Ggate, *Gwi, *Gbi;
+    int accumulate;
+    // A block's sums by column.  A, B [blocks + gates, width]: of dy f^ and dy over the rows that a block b and a row g
+    // of gates share, at b + g (pairs of rows in order never share that number); W, WB [blocks, width]: the
+    // same times scale * gate, over the block's rows; C, D [blocks, width]: of dH y^ and dH.
+    float *A, *B, *W, *WB, *C, *D;
+    int ctas;               // blocks (set by the launchers)
+    int* flags;
+};
+int residual_ctas(int num_sms, int threads);
+int residual_most_ctas(int num_sms, int width, int dtype);   // of any call
+cudaError_t residual_forward(ResidualArgs a, cudaStream_t s);
+cudaError_t residual_backward(ResidualArgs a, cudaStream_t s);
+
 }  // namespace bp

@@ -1,49 +1,12 @@
 // Embeddings: rows of a table by token, and the pooled change of every token's row.
 #include "bp_blocks_internal.h"
-#include "bp_experts_device.cuh"
+#include "bp_pieces.cuh"
 #include "bp_tc_device.cuh"
 
 namespace bp {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-
-// V values of a row, 16 bytes of it (or one float32 where rows are not whole 16-byte pieces).
-template <class T, int V>
-struct Piece {
-    uint4 u;
-    __device__ __forceinline__ void load(const T* p) {   // (volatile: a batch of loads stays a batch)
-        if constexpr (V == 1) asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(u.x) : "l"(p));
-        else asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
-    }
-    __device__ __forceinline__ void values(float (&v)[V]) const {
-        const unsigned w[4] = {u.x, u.y, u.z, u.w};
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < V / 2; ++i) {
-                v[2 * i] = __uint_as_float(w[i] << 16);
-                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = __uint_as_float(w[i]);
-        }
-    }
-};
-template <class T, int V>
-__device__ __forceinline__ void store_values(T* p, const float (&v)[V]) {
-    if constexpr (V == 1) {
-        *p = from_f32<T>(v[0]);
-    } else if constexpr (sizeof(T) == 2) {
-        __align__(16) __nv_bfloat162 h[V / 2];
-#pragma unroll
-        for (int i = 0; i < V / 2; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(h);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    }
-}
 
 // ------------------------------------------------------------ lookup
 // A warp takes up to kLook pieces a lane of one row, or several short rows.  Bound by reading the rows that
@@ -75,7 +38,8 @@ __global__ void __launch_bounds__(kThreads) k_embed(EmbedArgs g, int lanes, int 
 #pragma unroll
             for (int j = 0; j < V; ++j) v[j] *= g.scale;
         }
-        store_values<T, V>(out + (size_t)(v0 + i * lanes) * V, v);
+        p[i].set(v);
+        p[i].store(out + (size_t)(v0 + i * lanes) * V);
     }
 }
 
@@ -303,7 +267,7 @@ __global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const unsi
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] += p[i];
         }
-        store_values<float, V>(p, v);
+        store_floats<V>(p, v);
     };
     // A piece of a long run: to its slot, and all of the run's pieces to G if it is the last one.
     const auto join = [&](unsigned token, int slot) {

@@ -57,3 +57,56 @@ def test_null_embeddings_are_refused(lib):
     assert lib.bp_embed_backward(None, P, 1, P, 1.0, P, 0, None) == bp.BP_EINVAL
     assert lib.bp_embedding_check(None, None) == bp.BP_EINVAL
     lib.bp_embedding_destroy(None)   # NULL-safe
+
+
+# ------------------------------------------------------------------ residual stream
+@pytest.mark.parametrize("out", [0, 1, 2])
+@pytest.mark.parametrize("into", [0, 1, 2])
+def test_residual_gradient_is_the_difference(out, into):
+    rng = np.random.default_rng(out * 3 + into)
+    n, w, eps, scale = 6, 5, 1e-3, 0.7
+    v = dict(X=rng.standard_normal((n, w)), F=rng.standard_normal((n, w)) + 1, gate=rng.standard_normal((3, w)))
+    if out:
+        v["wo"] = rng.standard_normal(w)
+    if out == 2:
+        v["bo"] = rng.standard_normal(w)
+    if into:
+        v["wi"] = rng.standard_normal(w)
+    if into == 2:
+        v["bi"] = rng.standard_normal(w)
+    off = np.array([0, 2, 2, 5])   # an empty range, and a row of none
+    dY, dH = rng.standard_normal((n, w)), rng.standard_normal((n, w)) if into else None
+
+    def forward():
+        y = O.residual(v["X"], v["F"], v.get("wo"), v.get("bo"), v["gate"], off, scale, out, eps)[0]
+        return y, O.norm_in(y, v.get("wi"), v.get("bi"), into, eps)[0] if into else 0.0
+
+    def loss():
+        y, h = forward()
+        return (y * dY).sum() + ((h * dH).sum() if into else 0.0)
+    got = O.residual_backward(forward()[0], v["F"], v.get("wo"), v.get("bo"), v["gate"], off, scale, v.get("wi"), dY, dH, out, into, eps)
+    for name, x in v.items():
+        g, mag = got["d" + name if name in "XF" else "G" + name]
+        np.testing.assert_allclose(g, difference(loss, x), atol=2e-8, err_msg=name)
+        assert (mag >= np.abs(g) - 1e-12).all()
+
+
+@pytest.mark.parametrize("args,status", [((0, 0, 4, 1, 1, 1, 1e-5), bp.BP_EINVAL), ((8193, 0, 4, 1, 1, 1, 1e-5), bp.BP_EINVAL),
+                                         ((12, 1, 4, 1, 1, 1, 1e-5), bp.BP_ESHAPE), ((8, 3, 4, 1, 1, 1, 1e-5), bp.BP_EINVAL),
+                                         ((8, 0, 0, 1, 1, 1, 1e-5), bp.BP_EINVAL), ((8, 0, 2 ** 31 - 1, 1, 1, 1, 1e-5), bp.BP_EINVAL),
+                                         ((8, 0, 4, -1, 1, 1, 1e-5), bp.BP_EINVAL), ((8, 0, 4, 1, 3, 1, 1e-5), bp.BP_EINVAL),
+                                         ((8, 0, 4, 1, 1, -1, 1e-5), bp.BP_EINVAL), ((8, 0, 4, 1, 1, 1, 0.0), bp.BP_EINVAL),
+                                         ((8, 0, 4, 1, 1, 1, float("nan")), bp.BP_EINVAL),
+                                         ((8, 0, 4, 1, 1, 1, float("inf")), bp.BP_EINVAL)])
+def test_residual_create_refuses(lib, args, status):
+    out = ctypes.c_void_p()
+    assert lib.bp_residual_create(*args, ctypes.byref(out)) == status
+    assert out.value is None and lib.bp_last_error()
+    assert lib.bp_residual_create(8, 0, 4, 1, 1, 1, 1e-5, None) == bp.BP_EINVAL
+
+
+def test_null_streams_are_refused(lib):
+    assert lib.bp_residual_forward(None, P, P, 1, P, P, P, P, 1, 1.0, P, P, P, P, P, None) == bp.BP_EINVAL
+    assert lib.bp_residual_backward(None, P, P, 1, P, P, P, P, 1, 1.0, P, P, P, P, P, P, P, P, P, P, P, 0, None) == bp.BP_EINVAL
+    assert lib.bp_residual_check(None, None) == bp.BP_EINVAL
+    lib.bp_residual_destroy(None)   # NULL-safe
