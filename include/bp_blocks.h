@@ -5,7 +5,8 @@
  *   Embedding  rows of a table by token, and the pooled change of every token's row
  *              (a layer whose input is one unit out of many);
  *   Residual   the stream between blocks: a block's output is normed, gated, scaled and
- *              added, and the sum is normed again for the next block.
+ *              added, and the sum is normed again for the next block;
+ *   Clip       the norm of many changes together, and the changes scaled down to a bound.
  *
  * The conventions of bp.h and bp_experts.h hold (row-major contiguous buffers, caller-owned device
  * memory, streams, status codes, bp_last_error; values float32 or bfloat16 as the handle's dtype says;
@@ -29,10 +30,12 @@ extern "C" {
 
 typedef struct bp_embedding bp_embedding;
 typedef struct bp_residual bp_residual;
+typedef struct bp_clip bp_clip;
 
 #define BP_MAX_TOKENS (1 << 24)   /* rows of a table */
 #define BP_MAX_IDS (1 << 26)      /* ids of one call */
 #define BP_MAX_WIDTH 8192         /* units of a residual stream */
+#define BP_MAX_TENSORS 65535      /* changes that are clipped together */
 
 /* A table of n_tokens rows of `width` units, for up to max_ids ids a call.
  * 1 <= n_tokens <= BP_MAX_TOKENS, 1 <= max_ids <= BP_MAX_IDS.
@@ -106,6 +109,27 @@ bp_status bp_residual_backward(bp_residual* stream_layer, const void* d_Y, const
                                int accumulate, void* stream);
 
 bp_status bp_residual_check(bp_residual* stream_layer, void* stream);   /* as bp_embedding_check; offsets */
+
+/* The changes that are clipped together: n tensors (1 .. BP_MAX_TENSORS) of h_sizes[i] values of type h_dtypes[i] at
+ * device address h_in[i], which go, clipped, to h_out[i] (h_out NULL: in place).  The three or four arrays are
+ * host arrays and not kept; the device addresses are, and stay valid while the handle is used.  A size may
+ * be 0; sizes add up to 2^40 at most.  Tensors lie on their values' boundaries.  A tensor's output is its input or apart from
+ * every input, and outputs are apart from one another (else BP_EINVAL).
+ * Errors: BP_EINVAL, BP_ENOMEM, BP_ECUDA. */
+bp_status bp_clip_create(const void* const* h_in, void* const* h_out, const int64_t* h_sizes, const int* h_dtypes,
+                         int n, bp_clip** out);
+void bp_clip_destroy(bp_clip* clip);   /* NULL-safe; synchronises the device */
+
+/* d_norm [1] (float32; may be NULL) = sqrt of the sum of the squares of all values; where it is above max_norm
+ * every value is multiplied by max_norm / norm on its way to its output, else the outputs are the inputs.
+ * Squares and sums neither overflow nor vanish (32 values at a time are float32's,
+ * scaled by a power of two where need be; beyond they are float64).  A norm that is not
+ * finite (a NaN or an infinity among the values) clips nothing, and is latched for bp_clip_check.  max_norm >= 0; infinity: the norm
+ * alone, outputs are not written.  Errors: BP_EINVAL, BP_ECUDA. */
+bp_status bp_clip_run(bp_clip* clip, float max_norm, float* d_norm, void* stream);
+
+/* Wait for `stream`, then report and clear what was latched: BP_ENONFINITE.  Errors: also BP_EINVAL, BP_ECUDA. */
+bp_status bp_clip_check(bp_clip* clip, void* stream);
 
 #ifdef __cplusplus
 }

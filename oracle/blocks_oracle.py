@@ -110,3 +110,10 @@ def residual_backward(Y, F, wo, bo, gate, offsets, scale, wi, dY, dH, norm_out, 
                     M[of[t]] += np.abs(scale) * my[t] * um[t]
             out["Ggate"] = G, M
     return out
+
+
+# ------------------------------------------------------------------ clipping
+def clip(tensors, max_norm):
+    """(norm, the tensors times max_norm / norm where the norm is above max_norm)."""
+    norm = np.sqrt(sum((x * x).sum() for x in tensors))
+    return norm, [x * (max_norm / norm) for x in tensors] if norm > max_norm else tensors

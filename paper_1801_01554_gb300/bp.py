@@ -25,7 +25,7 @@ BP_MAX_EXPERTS, BP_MAX_CHOICES, BP_MAX_RANK = 512, 16, 128
 BP_GATES_CHOSEN, BP_GATES_ALL = 0, 1
 BP_MAX_GROUPS = 32
 BP_SCORES_SOFTMAX, BP_SCORES_SIGMOID = 0, 1
-BP_MAX_TOKENS, BP_MAX_IDS, BP_MAX_WIDTH = 1 << 24, 1 << 26, 8192
+BP_MAX_TOKENS, BP_MAX_IDS, BP_MAX_WIDTH, BP_MAX_TENSORS = 1 << 24, 1 << 26, 8192, 65535
 BP_NORM_NONE, BP_NORM_RMS, BP_NORM_LAYER = 0, 1, 2
 
 # name -> (restype, argtypes); every symbol declared in include/
@@ -92,6 +92,11 @@ SIGNATURES = {
     "bp_residual_backward": (_I, [_VP, _VP, _VP, _I, _VP, _VP, _VP, _VP, _I, _F, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
                                   _VP, _VP, _VP, _I, _VP]),
     "bp_residual_check": (_I, [_VP, _VP]),
+    "bp_clip_create": (_I, [ctypes.POINTER(_VP), ctypes.POINTER(_VP), ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(_I), _I,
+                            ctypes.POINTER(_VP)]),
+    "bp_clip_destroy": (None, [_VP]),
+    "bp_clip_run": (_I, [_VP, _F, _VP, _VP]),
+    "bp_clip_check": (_I, [_VP, _VP]),
 }
 
 
@@ -557,6 +562,39 @@ def bp_residual_check(h, stream=None):
     _check(load().bp_residual_check(h, _stream(stream)))
 
 
+def bp_clip_create(tensors, outputs=None):
+    """A handle for these float32 or bfloat16 CUDA tensors, clipped into `outputs` (None: in place)."""
+    f32, bf16, _ = _torch_types()
+    n = len(tensors)
+    if outputs is not None and len(outputs) != n:
+        raise ValueError(f"{n} tensors and {len(outputs)} outputs")
+    kinds = []
+    for i, x in enumerate(tensors):
+        if x.dtype is not f32 and x.dtype is not bf16:
+            raise ValueError(f"tensor {i} must be {f32} or {bf16} (got {x.dtype})")
+        kinds.append(BP_BF16 if x.dtype is bf16 else BP_F32)
+    ins = [_values(x, k, f"tensor {i}") for i, (x, k) in enumerate(zip(tensors, kinds))]
+    outs = None
+    if outputs is not None:
+        outs = [_values(x, k, f"output {i}", t.numel()) for i, (x, k, t) in enumerate(zip(outputs, kinds, tensors))]
+    out = ctypes.c_void_p()
+    _check(load().bp_clip_create((_VP * n)(*ins), None if outs is None else (_VP * n)(*outs),
+                                 (ctypes.c_int64 * n)(*(x.numel() for x in tensors)), (_I * n)(*kinds), n, ctypes.byref(out)))
+    return out.value
+
+
+def bp_clip_destroy(h):
+    load().bp_clip_destroy(h)
+
+
+def bp_clip_run(h, max_norm, norm=None, stream=None):
+    _check(load().bp_clip_run(h, max_norm, _floats(norm, "norm", 1), _stream(stream)))
+
+
+def bp_clip_check(h, stream=None):
+    _check(load().bp_clip_check(h, _stream(stream)))
+
+
 # ------------------------------------------------------------------ convenience
 class _Handle:
     """A handle of the library, freed by close() or at the end of a with block."""
@@ -715,6 +753,22 @@ class Residual(_Handle):
 
     def check(self, stream=None):
         bp_residual_check(self.h, stream)
+
+
+class Clip(_Handle):
+    """Owns one bp_clip handle, and holds its tensors; methods forward to the C names above."""
+
+    _free = staticmethod(bp_clip_destroy)
+
+    def __init__(self, tensors, outputs=None):
+        self.tensors, self.outputs = list(tensors), None if outputs is None else list(outputs)
+        self.h = bp_clip_create(self.tensors, self.outputs)
+
+    def run(self, max_norm, norm=None, stream=None):
+        bp_clip_run(self.h, max_norm, norm, stream)
+
+    def check(self, stream=None):
+        bp_clip_check(self.h, stream)
 
 
 class Net:

@@ -97,6 +97,8 @@ inline bp_status read_flags(int* flags, unsigned* counts, size_t n_counts, void*
     if (e != cudaSuccess) return cuda_status(e, call);
     if (f & kFlagTimeout)
         return fail(BP_ETIMEOUT, "a bounded device-side wait ran out; the launch stopped early");
+    if (f & kFlagNonfinite)
+        return fail(BP_ENONFINITE, "the norm of a call's values was not finite");
     if (f & kFlagBounds)
         return fail(BP_ESTATE, "%s", bounds);
     return BP_OK;

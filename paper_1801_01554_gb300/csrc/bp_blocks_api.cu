@@ -2,8 +2,10 @@
 // checks, handles and scratch.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <new>
+#include <vector>
 
 #include "bp_api_checks.h"
 #include "bp_blocks_internal.h"
@@ -23,6 +25,12 @@ struct bp_residual {
     ResidualArgs a{};
     int cap = 0, max_gates = 0, device = 0;
     float* sums = nullptr;
+};
+
+struct bp_clip {
+    ClipArgs a{};
+    int device = 0, num_sms = 1;
+    ClipChunk* chunks = nullptr;
 };
 
 namespace {
@@ -286,6 +294,126 @@ bp_status bp_residual_check(bp_residual* l, void* stream) {
     if (l == nullptr) return fail(BP_EINVAL, "%s: NULL stream_layer", call);
     const bp_status st = check_device(call, l->device);
     return st != BP_OK ? st : read_flags(l->a.flags, nullptr, 0, stream, call, "the gates' offsets of a call do not go up from 0 to its rows");
+}
+
+// ------------------------------------------------------------ clipping
+namespace {
+
+struct Span {
+    uintptr_t first, end;
+    int tensor;
+};
+
+// Outputs are apart from one another, and from every input but their own, which they may be.
+bp_status check_spans(const char* call, const std::vector<Span>& in, std::vector<Span>& out) {
+    std::sort(out.begin(), out.end(), [](const Span& a, const Span& b) { return a.first < b.first; });
+    for (size_t i = 1; i < out.size(); ++i)
+        if (out[i].first < out[i - 1].end)
+            return fail(BP_EINVAL, "%s: the outputs of tensors %d and %d overlap", call, out[i - 1].tensor, out[i].tensor);
+    for (const Span& s : in) {
+        auto o = std::lower_bound(out.begin(), out.end(), s.first, [](const Span& a, uintptr_t x) { return a.end <= x; });
+        for (; o != out.end() && o->first < s.end; ++o)
+            if (o->tensor != s.tensor || o->first != s.first)
+                return fail(BP_EINVAL, "%s: the input of tensor %d overlaps the output of tensor %d", call, s.tensor, o->tensor);
+    }
+    return BP_OK;
+}
+
+}  // namespace
+
+bp_status bp_clip_create(const void* const* h_in, void* const* h_out, const int64_t* h_sizes, const int* h_dtypes, int n,
+                         bp_clip** out) {
+    const char* call = "bp_clip_create";
+    set_error_message("");
+    if (out == nullptr || h_in == nullptr || h_sizes == nullptr || h_dtypes == nullptr) return fail(BP_EINVAL, "%s: NULL argument", call);
+    bp_status st = check_range(call, "n", n, 1, BP_MAX_TENSORS);
+    if (st != BP_OK) return st;
+    constexpr long long kMost = 1ll << 40;
+    long long total = 0;
+    bool in_place = true;
+    for (int i = 0; i < n; ++i) {
+        st = check_dtype(call, h_dtypes[i]);
+        if (st == BP_OK) st = check_range(call, "a tensor's size", h_sizes[i], 0, kMost);
+        if (st == BP_OK) st = check_range(call, "the sizes' sum", total += h_sizes[i], 0, kMost);
+        if (st != BP_OK) return st;
+        const void* to = h_out != nullptr ? h_out[i] : h_in[i];
+        const int align = h_dtypes[i] == BP_BF16 ? 2 : 4;
+        const bool some = h_sizes[i] > 0;
+        st = check_buffers(call, {{h_in[i], "a tensor's input", align, some}, {to, "a tensor's output", align, some}});
+        if (st != BP_OK) return st;
+        in_place = in_place && (to == h_in[i] || !some);
+    }
+    bp_clip* l = nullptr;
+    try {
+        std::vector<Span> in, to;
+        std::vector<ClipChunk> chunks;
+        // chunks of whole tiles, from a 16-byte boundary on where a tensor goes on; some 2^16 and one a tensor at most
+        const long long chunk = (total / 65536 / kClipTile + 1) * kClipTile;
+        for (int i = 0; i < n; ++i) {
+            const long long size = h_dtypes[i] == BP_BF16 ? 2 : 4;
+            if (h_sizes[i] == 0) continue;
+            const char* x = (const char*)h_in[i];
+            char* y = h_out != nullptr ? (char*)h_out[i] : const_cast<char*>(x);
+            const uintptr_t bytes = (uintptr_t)(h_sizes[i] * size);
+            in.push_back({(uintptr_t)x, (uintptr_t)x + bytes, i});
+            to.push_back({(uintptr_t)y, (uintptr_t)y + bytes, i});
+            const long long head = (long long)((16 - ((uintptr_t)x & 15)) & 15) / size;
+            for (long long at = 0; at < h_sizes[i];) {
+                const long long count = std::min(h_sizes[i] - at, at == 0 ? head + chunk : chunk);
+                chunks.push_back({x + at * size, y + at * size, (unsigned)count, h_dtypes[i]});
+                at += count;
+            }
+        }
+        st = check_spans(call, in, to);
+        if (st != BP_OK) return st;
+        l = new bp_clip();
+        l->a.n_chunks = (int)chunks.size();
+        l->a.in_place = in_place;
+        st = make_flags(&l->device, &l->a.flags, call);
+        if (st == BP_OK) st = cuda_status(cudaDeviceGetAttribute(&l->num_sms, cudaDevAttrMultiProcessorCount, l->device), call);
+        if (st == BP_OK) st = make_array(&l->chunks, chunks.size(), call);
+        if (st == BP_OK) st = make_array(&l->a.partial, (size_t)clip_blocks(l->num_sms), call);
+        if (st == BP_OK && !chunks.empty())
+            st = cuda_status(cudaMemcpy(l->chunks, chunks.data(), chunks.size() * sizeof(ClipChunk), cudaMemcpyHostToDevice), call);
+        if (st == BP_OK) st = layer_ready(call);
+        l->a.chunks = l->chunks;
+    } catch (const std::bad_alloc&) {
+        st = fail(BP_ENOMEM, "%s: out of memory", call);
+    }
+    if (st != BP_OK) {
+        bp_clip_destroy(l);
+        return st;
+    }
+    *out = l;
+    return BP_OK;
+}
+
+void bp_clip_destroy(bp_clip* l) {
+    if (l == nullptr) return;
+    cudaDeviceSynchronize();
+    cudaFree(l->a.flags);
+    cudaFree(l->chunks);
+    cudaFree(l->a.partial);
+    delete l;
+}
+
+bp_status bp_clip_run(bp_clip* l, float max_norm, float* d_norm, void* stream) {
+    const char* call = "bp_clip_run";
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL clip", call);
+    if (!(max_norm >= 0.f)) return fail(BP_EINVAL, "%s: max_norm must be at least 0", call);
+    bp_status st = check_buffers(call, {{d_norm, "d_norm", 4, false}});
+    if (st == BP_OK) st = check_device(call, l->device);
+    if (st != BP_OK) return st;
+    ClipArgs a = l->a;
+    a.max_norm = max_norm, a.norm = d_norm, a.write = std::isfinite(max_norm);
+    return cuda_status(clip_run(a, l->num_sms, (cudaStream_t)stream), call);
+}
+
+bp_status bp_clip_check(bp_clip* l, void* stream) {
+    const char* call = "bp_clip_check";
+    if (l == nullptr) return fail(BP_EINVAL, "%s: NULL clip", call);
+    const bp_status st = check_device(call, l->device);
+    return st != BP_OK ? st : read_flags(l->a.flags, nullptr, 0, stream, call);
 }
 
 }  // extern "C"

@@ -58,4 +58,24 @@ int residual_most_ctas(int num_sms, int width, int dtype);   // of any call
 cudaError_t residual_forward(ResidualArgs a, cudaStream_t s);
 cudaError_t residual_backward(ResidualArgs a, cudaStream_t s);
 
+// ------------------------------------------------------------ clipping (bp_clip.cu)
+struct ClipChunk {
+    const void* in;
+    void* out;
+    unsigned count;
+    int dtype;
+};
+struct ClipArgs {
+    const ClipChunk* chunks;   // of the tensors, in order
+    int n_chunks, in_place;    // in_place: every output is its input
+    int write;                 // 0: the norm alone
+    float max_norm;
+    float* norm;               // or NULL
+    double* partial;           // [clip_blocks]
+    int* flags;
+};
+constexpr int kClipTile = 8192;   // values that a block takes at a time
+int clip_blocks(int num_sms);
+cudaError_t clip_run(const ClipArgs& a, int num_sms, cudaStream_t s);
+
 }  // namespace bp

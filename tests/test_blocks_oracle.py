@@ -110,3 +110,43 @@ def test_null_streams_are_refused(lib):
     assert lib.bp_residual_backward(None, P, P, 1, P, P, P, P, 1, 1.0, P, P, P, P, P, P, P, P, P, P, P, 0, None) == bp.BP_EINVAL
     assert lib.bp_residual_check(None, None) == bp.BP_EINVAL
     lib.bp_residual_destroy(None)   # NULL-safe
+
+
+# ------------------------------------------------------------------ clipping
+def test_clip_oracle():
+    norm, out = O.clip([np.array([3.0, 0.0]), np.zeros(0), np.array([[-4.0]])], 2.5)
+    assert norm == 5.0 and [x.tolist() for x in out] == [[1.5, 0.0], [], [[-2.0]]]
+    norm, out = O.clip([np.array([3.0, 4.0]) * 2.0 ** 120], np.inf)
+    assert norm == 5 * 2.0 ** 120 and out[0].tolist() == [3 * 2.0 ** 120, 2.0 ** 122]
+
+
+def clip_create(lib, ins, outs, sizes, dtypes, n=None):
+    out = ctypes.c_void_p()
+    k = len(ins)
+    st = lib.bp_clip_create((ctypes.c_void_p * k)(*ins), None if outs is None else (ctypes.c_void_p * k)(*outs),
+                            (ctypes.c_int64 * k)(*sizes), (ctypes.c_int * k)(*dtypes), k if n is None else n, ctypes.byref(out))
+    assert out.value is None
+    return st, lib.bp_last_error().decode()
+
+
+@pytest.mark.parametrize("ins,outs,sizes,dtypes,word", [
+    ([P], None, [4], [2], "dtype"), ([P], None, [-1], [0], "size"), ([P], None, [2 ** 41], [0], "size"),
+    ([P, P << 20], None, [2 ** 40, 1], [1, 1], "sum"), ([None], None, [1], [0], "NULL"), ([P + 2], None, [1], [0], "aligned"),
+    ([P + 1], None, [1], [1], "aligned"), ([P], [P + 0x1002], [1], [0], "aligned"), ([P], [None], [1], [0], "NULL"),
+    ([P, P + 12], None, [4, 4], [0, 0], "overlap"), ([P, P + 4096], [P + 8192, P + 8200], [4, 4], [0, 0], "overlap"),
+    ([P], [P + 4], [4], [0], "overlaps"), ([P + 4], [P], [4], [0], "overlaps"),
+    ([P, P + 4096], [P + 4096, P + 8192], [4, 4], [0, 0], "overlaps"), ([P, P + 16], [P, P + 8], [4, 4], [0, 1], "overlap"),
+    ([P, P, P + 4096], [P, P + 8192, P + 4096], [4, 4, 1], [0, 0, 0], "overlaps")])
+def test_clip_create_refuses(lib, ins, outs, sizes, dtypes, word):
+    st, message = clip_create(lib, ins, outs, sizes, dtypes)
+    assert st == bp.BP_EINVAL and word in message, message
+
+
+def test_clip_numbers_of_tensors(lib):
+    for n in (0, -1, 65536):
+        assert clip_create(lib, [P], None, [1], [0], n)[0] == bp.BP_EINVAL
+    out = ctypes.c_void_p()
+    assert lib.bp_clip_create(None, None, None, None, 1, ctypes.byref(out)) == bp.BP_EINVAL
+    assert lib.bp_clip_run(None, 1.0, P, None) == bp.BP_EINVAL
+    assert lib.bp_clip_check(None, None) == bp.BP_EINVAL
+    lib.bp_clip_destroy(None)   # NULL-safe
