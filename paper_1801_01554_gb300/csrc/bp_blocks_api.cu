@@ -176,16 +176,17 @@ bp_status bp_residual_create(int width, int dtype, int max_rows, int max_gates, 
     l->a.width = width, l->a.dtype = dtype, l->a.norm_out = norm_out, l->a.norm_in = norm_in, l->a.eps = eps;
     st = make_flags(&l->device, &l->a.flags, call);
     if (st == BP_OK) st = cuda_status(cudaDeviceGetAttribute(&l->a.num_sms, cudaDevAttrMultiProcessorCount, l->device), call);
+    if (st == BP_OK) st = cuda_status(residual_setup(width, dtype), call);
     if (st == BP_OK) {
-        const size_t blocks = residual_most_ctas(l->a.num_sms, width, dtype), w = width;
+        const size_t w = width, workers = residual_workers(l->a.num_sms, width, dtype) * w;
+        const size_t records = workers + max_gates * w;
         const bool layer = norm_out == BP_NORM_LAYER || norm_in == BP_NORM_LAYER;
-        const size_t by_gates = max_gates > 0 ? (blocks + max_gates) * w : 0;
-        st = make_array(&l->sums, 2 * blocks * w + by_gates + (layer ? 2 * blocks * w + by_gates : 0), call);
+        st = make_array(&l->sums, (layer ? 2 : 1) * (records + 2 * workers), call);
         float* p = l->sums;
         const auto take = [&](size_t n) { return p += n, p - n; };
         if (st == BP_OK) {
-            l->a.A = take(by_gates), l->a.W = take(blocks * w), l->a.C = take(blocks * w);
-            if (layer) l->a.B = take(by_gates), l->a.WB = take(blocks * w), l->a.D = take(blocks * w);
+            l->a.A = take(records), l->a.W = take(workers), l->a.C = take(workers);
+            if (layer) l->a.B = take(records), l->a.WB = take(workers), l->a.D = take(workers);
         }
     }
     if (st == BP_OK) st = layer_ready(call);

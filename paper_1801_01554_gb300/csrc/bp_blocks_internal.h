@@ -46,15 +46,16 @@ struct ResidualArgs {
     void *dX, *dF;
     float *Gwo, *Gbo, *Ggate, *Gwi, *Gbi;
     int accumulate;
-    // A block's sums by column.  A, B [blocks + gates, width]: of dy f^ and dy over the rows that a block b and a row g
-    // of gates share, at b + g (pairs of rows in order never share that number); W, WB [blocks, width]: the
-    // same times scale * gate, over the block's rows; C, D [blocks, width]: of dH y^ and dH.
+    // Sums by column.  A, B: of dy f^ and dy, a row for a block's rows [blocks, width]; gates by range: [workers + gates,
+    // width], a row for the rows that a worker w and a range g share, at w + g (pairs of rows in order never share
+    // that number), and W, WB [workers, width]: the same times scale * gate, over the worker's rows.  C, D
+    // [blocks, width]: of dH y^ and dH.
     float *A, *B, *W, *WB, *C, *D;
-    int ctas;               // blocks (set by the launchers)
+    int worker_warps, workers, workers_a_block;   // (set by the launchers)
     int* flags;
 };
-int residual_ctas(int num_sms, int threads);
-int residual_most_ctas(int num_sms, int width, int dtype);   // of any call
+int residual_workers(int num_sms, int width, int dtype);   // of a backward call, at most
+cudaError_t residual_setup(int width, int dtype);
 cudaError_t residual_forward(ResidualArgs a, cudaStream_t s);
 cudaError_t residual_backward(ResidualArgs a, cudaStream_t s);
 

@@ -8,28 +8,59 @@ namespace bp {
 namespace {
 
 constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
+constexpr int kSums = 10;        // of a reduction, at most
+constexpr int kWorkerRows = 4;   // of a worker of the backward pass, at least: its sums by column are added up at the end
 
-// Sums of the block's values, in one order, in every thread.  The two halves of `red` are used in turn, so
-// that one barrier a call is enough.
+// A worker is `warps` warps that take a row at a time, a thread C pieces of V columns; a block has one or more.
+// (Rows of 2,048 bytes and more have a block to themselves; with narrow ones a worker is a warp, whose reductions
+// need no barrier.)
+struct Worker {
+    int id, warps, tid, threads;   // id: in the block
+    float* red;                    // two halves of kMaxWarps * kSums, used in turn: one barrier a reduction
+    int turn;
+    __device__ __forceinline__ Worker(int warps_, float* shared) : warps(warps_) {
+        threads = warps * 32;
+        id = threadIdx.x / threads;
+        tid = threadIdx.x - id * threads;
+        red = shared + id * warps * kSums;
+        turn = 0;
+    }
+    __device__ __forceinline__ void sync() const {
+        if (warps == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(threads) : "memory");
+    }
+    __device__ __forceinline__ float* next() {
+        float* at = red + turn * kMaxWarps * kSums;
+        turn ^= 1;
+        return at;
+    }
+};
+
+// Sums of the worker's values, in one order, in every thread.
 template <int N>
-__device__ __forceinline__ void block_sums(float (&v)[N], float (*red)[kMaxWarps * 8], int& turn) {
+__device__ __forceinline__ void warp_sums(float (&v)[N], int lanes) {
+    for (int o = lanes / 2; o > 0; o >>= 1)
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+}
+template <int N>
+__device__ __forceinline__ void worker_sums(float (&v)[N], Worker& w) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) return;
-    float* at = red[turn];
-    turn ^= 1;
-    if ((threadIdx.x & 31) == 0)
+    for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
-        for (int i = 0; i < N; ++i) at[(threadIdx.x >> 5) * N + i] = v[i];
-    __syncthreads();
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    if (w.warps == 1) return;
+    const int lane = threadIdx.x & 31;
+    float* at = w.next();
+    if (lane == 0)
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = at[i];
-    for (int w = 1; w < warps; ++w)
+        for (int i = 0; i < N; ++i) at[(w.tid >> 5) * N + i] = v[i];
+    w.sync();
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += at[w * N + i];
+    for (int i = 0; i < N; ++i) v[i] = lane < w.warps ? at[lane * N + i] : 0.f;
+    warp_sums(v, 16);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
 }
 
 // Number, mean and sum of squared differences from it, of two sets together: no cancellation where the mean
@@ -44,32 +75,33 @@ struct Moments {
         m2 += m22 + d * d * n * part;
         n = all;
     }
+    __device__ __forceinline__ void join_lanes(int lanes) {   // lane 0's is the one to use: others' last bits differ
+        for (int o = lanes / 2; o > 0; o >>= 1)
+            join(__shfl_xor_sync(0xffffffffu, n, o), __shfl_xor_sync(0xffffffffu, mean, o), __shfl_xor_sync(0xffffffffu, m2, o));
+    }
 };
-__device__ __forceinline__ void block_moments(Moments& m, float (*red)[kMaxWarps * 8], int& turn) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        m.join(__shfl_xor_sync(0xffffffffu, m.n, o), __shfl_xor_sync(0xffffffffu, m.mean, o), __shfl_xor_sync(0xffffffffu, m.m2, o));
-    m.n = __shfl_sync(0xffffffffu, m.n, 0);   // (joined in another order, other lanes have other last bits)
+__device__ __forceinline__ void worker_moments(Moments& m, Worker& w) {
+    m.join_lanes(32);
+    if (w.warps > 1) {
+        const int lane = threadIdx.x & 31, at_warp = (w.tid >> 5) * 3;
+        float* at = w.next();
+        if (lane == 0) at[at_warp] = m.n, at[at_warp + 1] = m.mean, at[at_warp + 2] = m.m2;
+        w.sync();
+        m = {0.f, 0.f, 0.f};
+        if (lane < w.warps) m = {at[lane * 3], at[lane * 3 + 1], at[lane * 3 + 2]};
+        m.join_lanes(16);
+    }
+    m.n = __shfl_sync(0xffffffffu, m.n, 0);
     m.mean = __shfl_sync(0xffffffffu, m.mean, 0);
     m.m2 = __shfl_sync(0xffffffffu, m.m2, 0);
-    const int warps = blockDim.x >> 5;
-    if (warps == 1) return;
-    float* at = red[turn];
-    turn ^= 1;
-    if ((threadIdx.x & 31) == 0) {
-        const int w = threadIdx.x >> 5;
-        at[w * 3] = m.n, at[w * 3 + 1] = m.mean, at[w * 3 + 2] = m.m2;
-    }
-    __syncthreads();
-    m = {at[0], at[1], at[2]};
-    for (int w = 1; w < warps; ++w) m.join(at[w * 3], at[w * 3 + 1], at[w * 3 + 2]);
 }
 
-// A thread's columns: C pieces of V, the block's width apart.
+// A thread's columns: C pieces of V, the worker's width apart.
 template <int V, int C>
 struct Columns {
-    int width;
-    __device__ __forceinline__ int at(int j) const { return (j * (int)blockDim.x + (int)threadIdx.x) * V; }
+    int width, tid, threads;
+    __device__ __forceinline__ Columns(int width_, const Worker& w) : width(width_), tid(w.tid), threads(w.threads) {}
+    __device__ __forceinline__ int at(int j) const { return (j * threads + tid) * V; }
     __device__ __forceinline__ bool in(int j) const { return at(j) < width; }
 };
 
@@ -81,13 +113,45 @@ __device__ __forceinline__ void load_floats(const Columns<V, C>& cols, const flo
         for (int i = 0; i < V; ++i) out[j * V + i] = p != nullptr && cols.in(j) ? __ldg(p + cols.at(j) + i) : none;
 }
 
-template <class T, int V, int C>
-__device__ __forceinline__ void load_row(const Columns<V, C>& cols, const void* p, long long row, Piece<T, V> (&out)[C]) {
+// Rows on their way: S rows of N arrays, each thread's pieces in places of its own in shared memory, so that a thread
+// waits for its own copies alone.
+template <class T, int V, int C, int N, int S>
+struct Ring {
+    static constexpr int kBytes = V * (int)sizeof(T);
+    unsigned base;
+    int lanes;
+    __device__ __forceinline__ Ring(const void* shared) : base(smem_u32(shared) + threadIdx.x * kBytes), lanes(blockDim.x * kBytes) {}
+    __device__ __forceinline__ unsigned place(int stage, int n, int j) const { return base + ((stage * N + n) * C + j) * lanes; }
+    __device__ __forceinline__ void ask(const Columns<V, C>& cols, const void* p, long long row, int stage, int n) const {
+        if (p == nullptr) return;
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-        out[j].u = make_uint4(0u, 0u, 0u, 0u);
-        if (p != nullptr && cols.in(j)) out[j].load_rw((const T*)p + (size_t)row * cols.width + cols.at(j));
+        for (int j = 0; j < C; ++j) {
+            if (!cols.in(j)) continue;
+            const T* from = (const T*)p + (size_t)row * cols.width + cols.at(j);
+            if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(stage, n, j)), "l"(from) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(place(stage, n, j)), "l"(from) : "memory");
+        }
     }
+    __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory"); }
+    // The row's pieces; zeros for an array that is not there and past the row's end.
+    __device__ __forceinline__ void take(const Columns<V, C>& cols, const void* p, int stage, int n, Piece<T, V> (&out)[C]) const {
+#pragma unroll
+        for (int j = 0; j < C; ++j) {
+            out[j].u = make_uint4(0u, 0u, 0u, 0u);
+            if (p == nullptr || !cols.in(j)) continue;
+            uint4& u = out[j].u;
+            if constexpr (kBytes == 16)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(stage, n, j)) : "memory");
+            else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u.x) : "r"(place(stage, n, j)) : "memory");
+        }
+    }
+};
+// Stages: as many as fit twice (forward) or once on an SM beside 512 threads.
+template <class T, int V, int C>
+constexpr int stages(bool back) {
+    constexpr int bytes = V * C * (int)sizeof(T);
+    return bytes <= 16 ? 6 : bytes <= 32 ? 3 : back ? 1 : 3;
 }
 
 // Rows that share a row of gates: of row r, the gates' row (-1: none) and the first row from r on that is not of it.
@@ -114,7 +178,7 @@ __device__ __forceinline__ void check_offsets(const ResidualArgs& g) {
         if (x < 0 || x > y || y > g.n) atomicOr(g.flags, kFlagBounds);
     }
 }
-__device__ __forceinline__ int first_row(const ResidualArgs& g, int cta) { return (int)((long long)g.n * cta / (int)gridDim.x); }
+__device__ __forceinline__ int first_row(const ResidualArgs& g, int worker) { return (int)((long long)g.n * worker / g.workers); }
 
 // scale * gate of a stretch, by column.
 template <int V, int C>
@@ -125,8 +189,8 @@ __device__ __forceinline__ void load_gate(const ResidualArgs& g, const Columns<V
 }
 
 template <bool MEAN, int V, int C>
-__device__ __forceinline__ void norm_stats(const ResidualArgs& g, const Columns<V, C>& cols, const float (&v)[V * C], int kind,
-                                           float (*red)[kMaxWarps * 8], int& turn, float& mean, float& rinv) {
+__device__ __forceinline__ void norm_stats(const ResidualArgs& g, const Columns<V, C>& cols, const float (&v)[V * C], int kind, Worker& w,
+                                           float& mean, float& rinv) {
     if constexpr (MEAN) {
         Moments m{0.f, 0.f, 0.f};
         float sum = 0.f;
@@ -148,7 +212,7 @@ __device__ __forceinline__ void norm_stats(const ResidualArgs& g, const Columns<
                     const float d = v[j * V + i] - m.mean;
                     m.m2 += d * d;
                 }
-        block_moments(m, red, turn);
+        worker_moments(m, w);
         const float var = m.m2 / m.n + (kind == BP_NORM_LAYER ? 0.f : m.mean * m.mean);
         mean = kind == BP_NORM_LAYER ? m.mean : 0.f;
         rinv = 1.f / sqrtf(var + g.eps);
@@ -156,24 +220,37 @@ __device__ __forceinline__ void norm_stats(const ResidualArgs& g, const Columns<
         float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < V * C; ++i) s[0] = fmaf(v[i], v[i], s[0]);   // (columns past the row's end are 0)
-        block_sums(s, red, turn);
+        worker_sums(s, w);
         mean = 0.f;
         rinv = 1.f / sqrtf(s[0] / (float)g.width + g.eps);
     }
 }
 
-// A block takes consecutive rows, a thread the same columns of each, whose weights stay in its registers; the next row is
-// under way while one is worked on.  MEAN: a norm takes means off.  Bound by reading X and F once and writing Y
+// A worker takes consecutive rows, a thread the same columns of each, whose weights stay in its registers; rows ahead
+// are on their way in shared memory.  MEAN: a norm takes means off.  Bound by reading X and F once and writing Y
 // and H once.
 template <class T, int V, int C, bool MEAN>
 __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
-    constexpr int P = V * C;
-    __shared__ float red[2][kMaxWarps * 8];
-    int turn = 0;
-    const Columns<V, C> cols{g.width};
-    const int r0 = first_row(g, blockIdx.x), r1 = first_row(g, blockIdx.x + 1);
-    const bool block = g.F != nullptr, normed_in = g.norm_in != BP_NORM_NONE && (g.H != nullptr || g.stats != nullptr);
+    constexpr int P = V * C, S = stages<T, V, C>(false);
+    extern __shared__ __align__(16) unsigned char room[];
+    __shared__ float red[2 * kMaxWarps * kSums];
+    Worker w(g.worker_warps, red);
+    const Columns<V, C> cols(g.width, w);
+    const Ring<T, V, C, 2, S> ring(room);
+    const int mine = blockIdx.x * g.workers_a_block + w.id;
     check_offsets(g);
+    if (mine >= g.workers) return;
+    const int r0 = first_row(g, mine), r1 = first_row(g, mine + 1);
+    const auto ask = [&](int r) {
+        if (r < r1) {
+            ring.ask(cols, g.X, r, (r - r0) % S, 0);
+            ring.ask(cols, g.F, r, (r - r0) % S, 1);
+        }
+        ring.commit();
+    };
+#pragma unroll
+    for (int i = 0; i < S; ++i) ask(r0 + i);
+    const bool block = g.F != nullptr, normed_in = g.norm_in != BP_NORM_NONE && (g.H != nullptr || g.stats != nullptr);
     float wo[P], wi[P], bo[MEAN ? P : 1], bi[MEAN ? P : 1], k[P];
     load_floats(cols, g.wo, 1.f, wo);
     load_floats(cols, g.wi, 1.f, wi);
@@ -181,20 +258,16 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
         load_floats(cols, g.bo, 0.f, bo);
         load_floats(cols, g.bi, 0.f, bi);
     }
-    Piece<T, V> x[C], f[C];
-    load_row(cols, g.X, r0, x);
-    load_row(cols, g.F, r0, f);
     Stretch now{0, r0};
     for (int r = r0; r < r1; ++r) {
         if (r >= now.end) {
             now = stretch_of(g, r);
             load_gate(g, cols, now.seg, k);
         }
-        Piece<T, V> xn[C], fn[C];
-        if (r + 1 < r1) {
-            load_row(cols, g.X, r + 1, xn);
-            load_row(cols, g.F, r + 1, fn);
-        }
+        Piece<T, V> x[C], f[C];
+        ring.wait();
+        ring.take(cols, g.X, (r - r0) % S, 0, x);
+        ring.take(cols, g.F, (r - r0) % S, 1, f);
         float y[P], u[P], mf = 0.f, rf = 1.f, my = 0.f, ry = 1.f;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -205,7 +278,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
             for (int i = 0; i < V; ++i) y[j * V + i] = a[i], u[j * V + i] = b[i];
         }
         if (block) {
-            if (g.norm_out != BP_NORM_NONE) norm_stats<MEAN>(g, cols, u, g.norm_out, red, turn, mf, rf);
+            if (g.norm_out != BP_NORM_NONE) norm_stats<MEAN>(g, cols, u, g.norm_out, w, mf, rf);
 #pragma unroll
             for (int j = 0; j < C; ++j) {
                 float a[V];
@@ -226,7 +299,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
 #pragma unroll
             for (int j = 0; j < C; ++j)
                 if (cols.in(j)) x[j].store((T*)g.Y + (size_t)r * g.width + cols.at(j));
-        if (normed_in) norm_stats<MEAN>(g, cols, y, g.norm_in, red, turn, my, ry);
+        if (normed_in) norm_stats<MEAN>(g, cols, y, g.norm_in, w, my, ry);
         if (g.H != nullptr) {
 #pragma unroll
             for (int j = 0; j < C; ++j) {
@@ -243,10 +316,9 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
                 p.store((T*)g.H + (size_t)r * g.width + cols.at(j));
             }
         }
-        if (g.stats != nullptr && threadIdx.x < 4)
-            g.stats[(size_t)r * 4 + threadIdx.x] = threadIdx.x == 0 ? mf : threadIdx.x == 1 ? rf : threadIdx.x == 2 ? my : ry;
-#pragma unroll
-        for (int j = 0; j < C; ++j) x[j] = xn[j], f[j] = fn[j];
+        if (g.stats != nullptr && w.tid < 4)
+            g.stats[(size_t)r * 4 + w.tid] = w.tid == 0 ? mf : w.tid == 1 ? rf : w.tid == 2 ? my : ry;
+        ask(r + S);   // (the stage's values are in registers)
     }
 }
 
@@ -254,61 +326,66 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
 //   dy = dY + r_y (e - mean(e) - y^ mean(e y^)),   dF = r_f (k dy - mean(k dy) - f^ mean(k dy f^))
 // (means of e and k dy for BP_NORM_LAYER only).  dy is linear in the first two means, so those of k dy are
 // sums that need not wait for them: one reduction a row.  The sums by column stay in registers over a
-// block's rows: of dy f^ and dy by stretch (what gates and output weights want), of dH y^ and dH.
-// Bound by reading Y, F, dY and dH once and writing dX and dF once.
+// worker's rows: of dy f^ and dy (what gates and output weights want, by stretch where gates are by range), of dH y^
+// and dH.  Bound by reading Y, F, dY and dH once and writing dX and dF once.
 template <class T, int V, int C, bool MEAN>
 __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs g) {
-    constexpr int P = V * C, S = MEAN ? 8 : 3;
-    __shared__ float red[2][kMaxWarps * 8];
-    int turn = 0;
+    constexpr int P = V * C, N = MEAN ? 10 : 4, S = stages<T, V, C>(true);
+    extern __shared__ __align__(16) unsigned char room[];
+    __shared__ float red[2 * kMaxWarps * kSums];
     pdl_launch();
-    const Columns<V, C> cols{g.width};
-    const int r0 = first_row(g, blockIdx.x), r1 = first_row(g, blockIdx.x + 1);
+    Worker w(g.worker_warps, red);
+    const Columns<V, C> cols(g.width, w);
+    const Ring<T, V, C, 4, S> ring(room);
+    const int mine = blockIdx.x * g.workers_a_block + w.id;
+    check_offsets(g);
+    const bool live = mine < g.workers;
+    const int r0 = live ? first_row(g, mine) : 0, r1 = live ? first_row(g, mine + 1) : 0;
+    const void* Y = g.dH != nullptr ? g.Y : nullptr;
+    const auto ask = [&](int r) {
+        if (r < r1) {
+            const int stage = (r - r0) % S;
+            ring.ask(cols, Y, r, stage, 0);
+            ring.ask(cols, g.F, r, stage, 1);
+            ring.ask(cols, g.dY, r, stage, 2);
+            ring.ask(cols, g.dH, r, stage, 3);
+        }
+        ring.commit();
+    };
+#pragma unroll
+    for (int i = 0; i < S; ++i) ask(r0 + i);
     const bool out_normed = g.norm_out != BP_NORM_NONE;
     const float layer_in = g.norm_in == BP_NORM_LAYER ? 1.f : 0.f, layer_out = g.norm_out == BP_NORM_LAYER ? 1.f : 0.f;
     const float each = 1.f / (float)g.width;
-    const bool sum_out = g.Gwo != nullptr || g.Gbo != nullptr || g.Ggate != nullptr;
-    check_offsets(g);
+    const bool by_range = g.n_gates > 0 && g.offsets != nullptr;
     float k[P], wi[P];
     load_floats(cols, g.wi, 1.f, wi);
     float A[P] = {}, B[MEAN ? P : 1] = {}, CI[P] = {}, D[MEAN ? P : 1] = {};
-    bool fresh = true;   // nothing of this block in W and WB
-    // The sums of a stretch: to its record, and times scale * gate to this block's part of the weights' gradients.
+    bool fresh = true;   // nothing of this worker in W and WB
+    // Gates by range: the sums of a stretch to its record, and times scale * gate to this worker's part of the weights'
+    // gradients.
     const auto flush = [&](int seg) {
-        if (!sum_out) return;
         float q[P];
         load_gate(g, cols, seg, q);
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             if (!cols.in(j)) continue;
-            const size_t w = (size_t)blockIdx.x * g.width + cols.at(j);
-            const size_t rec = (size_t)(blockIdx.x + max(seg, 0)) * g.width + cols.at(j);
+            const size_t row = (size_t)mine * g.width + cols.at(j), rec = row + (size_t)max(seg, 0) * g.width;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int c = j * V + i;
                 if (seg >= 0 && g.Ggate != nullptr) g.A[rec + i] = A[c];
-                if (g.Gwo != nullptr) g.W[w + i] = (fresh ? 0.f : g.W[w + i]) + q[c] * A[c];
+                if (g.Gwo != nullptr) g.W[row + i] = (fresh ? 0.f : g.W[row + i]) + q[c] * A[c];
+                A[c] = 0.f;
                 if constexpr (MEAN) {
-                    if (seg >= 0 && g.Ggate != nullptr && g.bo != nullptr) g.B[rec + i] = B[c];
-                    if (g.Gbo != nullptr) g.WB[w + i] = (fresh ? 0.f : g.WB[w + i]) + q[c] * B[c];
+                    if (seg >= 0 && g.Ggate != nullptr) g.B[rec + i] = B[c];
+                    if (g.Gbo != nullptr) g.WB[row + i] = (fresh ? 0.f : g.WB[row + i]) + q[c] * B[c];
+                    B[c] = 0.f;
                 }
             }
         }
         fresh = false;
-#pragma unroll
-        for (int c = 0; c < P; ++c) {
-            A[c] = 0.f;
-            if constexpr (MEAN) B[c] = 0.f;
-        }
     };
-    Piece<T, V> y[C], f[C], a[C], b[C];
-    const auto load = [&](int r, Piece<T, V>(&y)[C], Piece<T, V>(&f)[C], Piece<T, V>(&a)[C], Piece<T, V>(&b)[C]) {
-        load_row(cols, g.dH != nullptr ? g.Y : nullptr, r, y);
-        load_row(cols, g.F, r, f);
-        load_row(cols, g.dY, r, a);
-        load_row(cols, g.dH, r, b);
-    };
-    load(r0, y, f, a, b);
     Stretch now{0, r0};
     for (int r = r0; r < r1; ++r) {
         if (r >= now.end) {
@@ -320,11 +397,16 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
 #pragma unroll
             for (int c = 0; c < P; ++c) k[c] *= wo[c];
         }
-        Piece<T, V> yn[C], fn[C], an[C], bn[C];
-        if (r + 1 < r1) load(r + 1, yn, fn, an, bn);
         const float* st = g.stats + (size_t)r * 4;
         const float mf = __ldg(st), rf = __ldg(st + 1), my = __ldg(st + 2), ry = __ldg(st + 3);
-        float s[S] = {};
+        const int stage = (r - r0) % S;
+        Piece<T, V> y[C], f[C], a[C], b[C];
+        ring.wait();
+        ring.take(cols, Y, stage, 0, y);
+        ring.take(cols, g.F, stage, 1, f);
+        ring.take(cols, g.dY, stage, 2, a);
+        ring.take(cols, g.dH, stage, 3, b);
+        float s[N] = {};
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             if (!cols.in(j)) continue;
@@ -333,31 +415,35 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int c = j * V + i;
-                const float e = bv[i] * wi[c], yh = (yv[i] - my) * ry, fh = (fv[i] - mf) * rf, base = av[i] + ry * e;
-                s[0] = fmaf(e, yh, s[0]);
-                s[1] = fmaf(k[c] * base, fh, s[1]);
-                s[2] = fmaf(k[c] * yh, fh, s[2]);
+                const float y0 = MEAN ? yv[i] - my : yv[i], f0 = MEAN ? fv[i] - mf : fv[i];
+                const float e = bv[i] * wi[c], t = k[c] * f0;
+                s[0] = fmaf(e, y0, s[0]);
+                s[1] = fmaf(t, av[i], s[1]);
+                s[2] = fmaf(t, e, s[2]);
+                s[3] = fmaf(t, y0, s[3]);
                 if constexpr (MEAN) {
-                    s[3] += e;
-                    s[4] = fmaf(k[c], fh, s[4]);
-                    s[5] = fmaf(k[c], base, s[5]);
-                    s[6] = fmaf(k[c], yh, s[6]);
-                    s[7] += k[c];
+                    s[4] += e;
+                    s[5] += t;
+                    s[6] = fmaf(k[c], av[i], s[6]);
+                    s[7] = fmaf(k[c], e, s[7]);
+                    s[8] = fmaf(k[c], y0, s[8]);
+                    s[9] += k[c];
                 }
             }
         }
-        block_sums(s, red, turn);
-        const float c1 = s[0] * each;
+        worker_sums(s, w);
+        const float c1 = ry * s[0] * each;
         float c0 = 0.f, d0 = 0.f, d1 = 0.f;
-        if constexpr (MEAN) c0 = layer_in * s[3] * each;
+        if constexpr (MEAN) c0 = layer_in * s[4] * each;
         if (out_normed) {
-            d1 = s[1] - ry * c1 * s[2];
+            float x = s[2] - c1 * ry * s[3];
             if constexpr (MEAN) {
-                d1 -= ry * c0 * s[4];
-                d0 = layer_out * (s[5] - ry * (c0 * s[7] + c1 * s[6])) * each;
+                x -= c0 * s[5];
+                d0 = layer_out * (s[6] + ry * (s[7] - c0 * s[9] - c1 * ry * s[8])) * each;
             }
-            d1 *= each;
+            d1 = rf * (s[1] + ry * x) * each;
         }
+        const float by_y = -ry * c1, by_f = -rf * d1, shift_y = ry * c0, shift_f = rf * d0;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             if (!cols.in(j)) continue;
@@ -366,10 +452,13 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int c = j * V + i;
-                const float e = bv[i] * wi[c], yh = (yv[i] - my) * ry, fh = (fv[i] - mf) * rf;
-                const float dy = av[i] + ry * (e - c0 - yh * c1);
+                const float yh = (MEAN ? yv[i] - my : yv[i]) * ry, fh = (MEAN ? fv[i] - mf : fv[i]) * rf;
+                float dy = fmaf(yh, by_y, fmaf(bv[i] * wi[c], ry, av[i]));
+                if constexpr (MEAN) dy -= shift_y;
+                float x = fmaf(fh, by_f, rf * (k[c] * dy));
+                if constexpr (MEAN) x -= shift_f;
                 dx[i] = dy;
-                df[i] = rf * (k[c] * dy - d0 - fh * d1);
+                df[i] = x;
                 A[c] = fmaf(dy, fh, A[c]);
                 CI[c] = fmaf(bv[i], yh, CI[c]);
                 if constexpr (MEAN) {
@@ -388,63 +477,80 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
                 p.store((T*)g.dF + at);
             }
         }
-#pragma unroll
-        for (int j = 0; j < C; ++j) y[j] = yn[j], f[j] = fn[j], a[j] = an[j], b[j] = bn[j];
+        ask(r + S);   // (the stage's values are in registers)
     }
-    flush(now.seg);
+    if (by_range && live && (g.Gwo != nullptr || g.Gbo != nullptr || g.Ggate != nullptr)) flush(now.seg);
+    // The block's sums over its rows.
+    const auto put = [&](const float* acc, float* to) {
+        if (g.workers_a_block == 1) {
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-        if (!cols.in(j)) continue;
-        const size_t w = (size_t)blockIdx.x * g.width + cols.at(j);
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (g.Gwi != nullptr) g.C[w + i] = CI[j * V + i];
-            if constexpr (MEAN)
-                if (g.Gbi != nullptr) g.D[w + i] = D[j * V + i];
-        }
-    }
-}
-
-// The blocks' sums, added up in the blocks' order: blocks (x) of 32 columns by (y) the four sums of weights and
-// biases, then the rows of gates.
-constexpr int kJoinWarps = 8;
-__global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(ResidualArgs g) {
-    __shared__ float part[2][kJoinWarps][32];
-    pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
-    const bool in = col < g.width;
-    const int job = blockIdx.y;
-    float *out = nullptr, *from = nullptr, *from2 = nullptr;
-    int lo = 0, hi = g.ctas, seg = 0;
-    if (job < 4) {
-        out = job == 0 ? g.Gwo : job == 1 ? g.Gbo : job == 2 ? g.Gwi : g.Gbi;
-        from = job == 0 ? g.W : job == 1 ? g.WB : job == 2 ? g.C : g.D;
-    }
-    for (int it = 0;; ++it) {
-        if (job >= 4) {   // gates, a block several rows of them
-            seg = job - 4 + it * ((int)gridDim.y - 4);
-            if (seg >= g.n_gates) return;
-            out = g.Ggate;
-            from = g.A, from2 = g.bo != nullptr ? g.B : nullptr;
-            int a = 0, b = g.n;
-            if (g.offsets != nullptr) {
-                a = min(max(__ldg(g.offsets + seg), 0), g.n);
-                b = min(max(__ldg(g.offsets + seg + 1), a), g.n);
-            }
-            lo = hi = 0;
-            if (b > a) {   // the blocks that hold rows a and b - 1
-                lo = (int)((((long long)a + 1) * g.ctas - 1) / g.n) + seg;
-                hi = (int)(((long long)b * g.ctas - 1) / g.n) + seg + 1;
-            }
-        } else if (it > 0) {
+            for (int c = 0; c < P; ++c)
+                if (cols.in(c / V)) to[(size_t)blockIdx.x * g.width + cols.at(c / V) + c % V] = acc[c];
             return;
         }
-        if (out == nullptr) return;
+        float* part = reinterpret_cast<float*>(room);
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < P; ++c)
+            if (cols.in(c / V)) part[w.id * g.width + cols.at(c / V) + c % V] = acc[c];
+        __syncthreads();
+        for (int c = threadIdx.x; c < g.width; c += blockDim.x) {
+            float x = part[c];
+            for (int i = 1; i < g.workers_a_block; ++i) x += part[i * g.width + c];
+            to[(size_t)blockIdx.x * g.width + c] = x;
+        }
+    };
+    if (!by_range) {
+        if (g.Gwo != nullptr || g.Ggate != nullptr) put(A, g.A);
+        if constexpr (MEAN)
+            if (g.Gbo != nullptr || g.Ggate != nullptr) put(B, g.B);
+    }
+    if (g.Gwi != nullptr) put(CI, g.C);
+    if constexpr (MEAN)
+        if (g.Gbi != nullptr) put(D, g.D);
+}
+
+// The blocks' and workers' sums, added up in their order: blocks (x) of 32 columns by (y) output weights, biases and one row
+// of gates for all; input weights and biases; then the rows of gates by range.
+constexpr int kJoinWarps = 32;
+__global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(ResidualArgs g) {
+    __shared__ float part[2][kJoinWarps][33];
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    const bool in = col < g.width, by_range = g.n_gates > 0 && g.offsets != nullptr;
+    const bool layer = g.B != nullptr;
+    const int job = blockIdx.y;
+    const float *from = nullptr, *from2 = nullptr;
+    int lo = 0, hi = (int)((g.workers + g.workers_a_block - 1) / g.workers_a_block);   // blocks
+    if (job == 0) {
+        if (by_range) hi = g.workers;
+        if (g.Gwo != nullptr || (!by_range && g.Ggate != nullptr)) from = by_range ? g.W : g.A;
+        if (layer && (g.Gbo != nullptr || (!by_range && g.Ggate != nullptr))) from2 = by_range ? g.WB : g.B;
+    } else if (job == 1) {
+        if (g.Gwi != nullptr) from = g.C;
+        if (g.Gbi != nullptr) from2 = g.D;
+    } else {
+        from = g.A;
+        from2 = layer && g.bo != nullptr ? g.B : nullptr;
+    }
+    if (from == nullptr && from2 == nullptr) return;
+    const auto give = [&](float* out, size_t at, float x) {
+        if (out != nullptr) out[at] = g.accumulate ? out[at] + x : x;
+    };
+    for (int seg = job - 2; seg < g.n_gates; seg += (int)gridDim.y - 2) {
+        if (job >= 2) {
+            const int a = min(max(__ldg(g.offsets + seg), 0), g.n), b = min(max(__ldg(g.offsets + seg + 1), a), g.n);
+            lo = hi = 0;
+            if (b > a) {   // the records of the workers that hold rows a and b - 1, and those between
+                lo = (int)((((long long)a + 1) * g.workers - 1) / g.n) + seg;
+                hi = (int)(((long long)b * g.workers - 1) / g.n) + seg + 1;
+            }
+        }
         float s = 0.f, s2 = 0.f;
         if (in) {
 #pragma unroll 4
             for (int r = lo + warp; r < hi; r += kJoinWarps) {
-                s += __ldcg(from + (size_t)r * g.width + col);
+                if (from != nullptr) s += __ldcg(from + (size_t)r * g.width + col);
                 if (from2 != nullptr) s2 += __ldcg(from2 + (size_t)r * g.width + col);
             }
         }
@@ -452,32 +558,38 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(ResidualArgs 
         part[1][warp][lane] = s2;
         __syncthreads();
         if (warp == 0 && in) {
-            for (int w = 1; w < kJoinWarps; ++w) s += part[0][w][lane], s2 += part[1][w][lane];
-            float* to = out + col;
-            if (job >= 4) {
-                to += (size_t)seg * g.width;
-                s *= g.wo != nullptr ? __ldg(g.wo + col) : 1.f;
-                if (from2 != nullptr) s = fmaf(__ldg(g.bo + col), s2, s);
-                s *= g.scale;
+            s = s2 = 0.f;
+            for (int w = 0; w < kJoinWarps; ++w) s += part[0][w][lane], s2 += part[1][w][lane];
+            const float wo = g.wo != nullptr ? __ldg(g.wo + col) : 1.f, bo = g.bo != nullptr ? __ldg(g.bo + col) : 0.f;
+            if (job == 1) {
+                give(g.Gwi, col, s);
+                give(g.Gbi, col, s2);
+            } else if (job == 0) {
+                const float k = by_range ? 1.f : g.scale * (g.n_gates > 0 ? __ldg(g.gate + col) : 1.f);
+                give(g.Gwo, col, k * s);
+                give(g.Gbo, col, k * s2);
+                if (!by_range) give(g.Ggate, col, g.scale * (bo * s2 + wo * s));
+            } else {
+                give(g.Ggate, (size_t)seg * g.width + col, g.scale * (bo * s2 + wo * s));
             }
-            *to = g.accumulate ? *to + s : s;
         }
+        if (job < 2) return;
         __syncthreads();
     }
 }
 
-// Threads and pieces a thread for rows of `width`.
+// How rows of `width` are shared out: pieces of v values, c of them a thread, `warps` a worker, `workers` a block.
 struct Shape {
-    int v, c, threads;
+    int v, c, warps, workers;
 };
-template <class T>
-Shape shape_of(int width, bool pieces) {
+Shape shape_of(int width, int size, bool pieces) {
     Shape s;
-    s.v = pieces ? 16 / (int)sizeof(T) : 1;
+    s.v = pieces ? 16 / size : 1;
     const int nv = (width + s.v - 1) / s.v;
     s.c = 1;
-    while ((nv + s.c - 1) / s.c > kMaxThreads) s.c *= s.v == 1 ? 4 : 2;
-    s.threads = ((nv + s.c - 1) / s.c + 31) / 32 * 32;
+    while ((nv + s.c - 1) / s.c > kMaxThreads) s.c *= 2;
+    s.warps = ((nv + s.c - 1) / s.c + 31) / 32;
+    s.workers = kMaxWarps / s.warps;
     return s;
 }
 
@@ -487,55 +599,86 @@ bool pieces16(const ResidualArgs& a) {
     return (p & 15) == 0 && a.width % 4 == 0;
 }
 
-template <class T, int V, int C>
-cudaError_t run(const ResidualArgs& a, bool back, int threads, cudaStream_t s) {
-    const bool mean = a.norm_out == BP_NORM_LAYER || a.norm_in == BP_NORM_LAYER;
-    if (!back) {
-        if (mean) k_residual<T, V, C, true><<<a.ctas, threads, 0, s>>>(a);
-        else k_residual<T, V, C, false><<<a.ctas, threads, 0, s>>>(a);
-    } else if (mean) {
-        k_residual_backward<T, V, C, true><<<a.ctas, threads, 0, s>>>(a);
-    } else {
-        k_residual_backward<T, V, C, false><<<a.ctas, threads, 0, s>>>(a);
+// What to do with the kernels of a shape: launch one, or set up both.
+struct Launch {
+    const ResidualArgs* a;
+    bool back;
+    cudaStream_t s;
+    template <class T, int V, int C>
+    cudaError_t shape() const {
+        const bool mean = a->norm_out == BP_NORM_LAYER || a->norm_in == BP_NORM_LAYER;
+        const int threads = a->workers_a_block * a->worker_warps * 32, blocks = (a->workers + a->workers_a_block - 1) / a->workers_a_block;
+        const int bytes = stages<T, V, C>(back) * (back ? 4 : 2) * C * V * (int)sizeof(T) * threads;
+        if (!back) {
+            if (mean) k_residual<T, V, C, true><<<blocks, threads, bytes, s>>>(*a);
+            else k_residual<T, V, C, false><<<blocks, threads, bytes, s>>>(*a);
+        } else if (mean) {
+            k_residual_backward<T, V, C, true><<<blocks, threads, bytes, s>>>(*a);
+        } else {
+            k_residual_backward<T, V, C, false><<<blocks, threads, bytes, s>>>(*a);
+        }
+        return cudaGetLastError();
     }
-    return cudaGetLastError();
+};
+struct Setup {
+    template <class T, int V, int C>
+    cudaError_t shape() const {
+        const int out = stages<T, V, C>(false) * 2 * C * V * (int)sizeof(T) * kMaxThreads;
+        const int back = stages<T, V, C>(true) * 4 * C * V * (int)sizeof(T) * kMaxThreads;
+        const auto set = [](auto k, int bytes) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+        cudaError_t e = set(k_residual<T, V, C, false>, out);
+        if (e == cudaSuccess) e = set(k_residual<T, V, C, true>, out);
+        if (e == cudaSuccess) e = set(k_residual_backward<T, V, C, false>, back);
+        return e != cudaSuccess ? e : set(k_residual_backward<T, V, C, true>, back);
+    }
+};
+template <class F>
+cudaError_t with_shape(const F& f, int dtype, const Shape& h) {
+    if (dtype == BP_BF16) return h.c == 1 ? f.template shape<__nv_bfloat16, 8, 1>() : f.template shape<__nv_bfloat16, 8, 2>();
+    if (h.v == 4) return h.c == 1 ? f.template shape<float, 4, 1>() : h.c == 2 ? f.template shape<float, 4, 2>() : f.template shape<float, 4, 4>();
+    switch (h.c) {
+        case 1: return f.template shape<float, 1, 1>();
+        case 2: return f.template shape<float, 1, 2>();
+        case 4: return f.template shape<float, 1, 4>();
+        case 8: return f.template shape<float, 1, 8>();
+        default: return f.template shape<float, 1, 16>();
+    }
 }
-
-cudaError_t run_shape(ResidualArgs& a, bool back, cudaStream_t s) {
-    const bool f32 = a.dtype == BP_F32, pieces = !f32 || pieces16(a);
-    const Shape h = f32 ? shape_of<float>(a.width, pieces) : shape_of<__nv_bfloat16>(a.width, true);
-    a.ctas = min(a.n, residual_ctas(a.num_sms, h.threads));
-    if (!f32) {
-        if (h.c == 1) return run<__nv_bfloat16, 8, 1>(a, back, h.threads, s);
-        return run<__nv_bfloat16, 8, 2>(a, back, h.threads, s);
-    }
-    if (h.v == 4) {
-        if (h.c == 1) return run<float, 4, 1>(a, back, h.threads, s);
-        if (h.c == 2) return run<float, 4, 2>(a, back, h.threads, s);
-        return run<float, 4, 4>(a, back, h.threads, s);
-    }
-    if (h.c == 1) return run<float, 1, 1>(a, back, h.threads, s);
-    if (h.c == 4) return run<float, 1, 4>(a, back, h.threads, s);
-    return run<float, 1, 16>(a, back, h.threads, s);
-}
+Shape shape_of(const ResidualArgs& a) { return shape_of(a.width, a.dtype == BP_F32 ? 4 : 2, a.dtype == BP_BF16 || pieces16(a)); }
 
 }  // namespace
 
-int residual_ctas(int num_sms, int threads) { return num_sms * max(1, min(16, 1024 / threads)); }
-int residual_most_ctas(int num_sms, int width, int dtype) {
-    if (dtype == BP_BF16) return residual_ctas(num_sms, shape_of<__nv_bfloat16>(width, true).threads);
-    // a call's rows may be whole pieces or not
-    return max(residual_ctas(num_sms, shape_of<float>(width, true).threads), residual_ctas(num_sms, shape_of<float>(width, false).threads));
+int residual_workers(int num_sms, int width, int dtype) {
+    const Shape s = shape_of(width, dtype == BP_F32 ? 4 : 2, true);
+    if (dtype == BP_BF16) return num_sms * s.workers;
+    return num_sms * max(s.workers, shape_of(width, 4, false).workers);   // a call's rows may be whole pieces or not
 }
 
-cudaError_t residual_forward(ResidualArgs a, cudaStream_t s) { return run_shape(a, false, s); }
+cudaError_t residual_setup(int width, int dtype) {
+    const cudaError_t e = with_shape(Setup{}, dtype, shape_of(width, dtype == BP_F32 ? 4 : 2, dtype == BP_BF16 || width % 4 == 0));
+    return e != cudaSuccess || dtype == BP_BF16 ? e : with_shape(Setup{}, dtype, shape_of(width, 4, false));
+}
+
+cudaError_t residual_forward(ResidualArgs a, cudaStream_t s) {
+    const Shape h = shape_of(a);
+    const int blocks = 2 * a.num_sms;
+    a.worker_warps = h.warps;
+    a.workers = min(a.n, blocks * h.workers);
+    a.workers_a_block = (a.workers + blocks - 1) / blocks;
+    return with_shape(Launch{&a, false, s}, a.dtype, h);
+}
 
 cudaError_t residual_backward(ResidualArgs a, cudaStream_t s) {
-    const cudaError_t e = run_shape(a, true, s);
+    const Shape h = shape_of(a);
+    a.worker_warps = h.warps;
+    a.workers = min((a.n + kWorkerRows - 1) / kWorkerRows, a.num_sms * h.workers);
+    a.workers_a_block = (a.workers + a.num_sms - 1) / a.num_sms;
+    const cudaError_t e = with_shape(Launch{&a, true, s}, a.dtype, h);
     if (e != cudaSuccess) return e;
-    const bool weights = a.Gwo != nullptr || a.Gbo != nullptr || a.Gwi != nullptr || a.Gbi != nullptr, gates = a.Ggate != nullptr;
-    if (!weights && !gates) return cudaSuccess;
-    return launch_pdl(k_residual_join, (a.width + 31) / 32, 4 + (gates ? min(a.n_gates, 4096) : 0), kJoinWarps * 32, 0, s, a);
+    const bool weights = a.Gwo != nullptr || a.Gbo != nullptr || a.Gwi != nullptr || a.Gbi != nullptr;
+    if (!weights && a.Ggate == nullptr) return cudaSuccess;
+    const int ranges = a.Ggate != nullptr && a.offsets != nullptr ? min(a.n_gates, 4096) : 0;
+    return launch_pdl(k_residual_join, (a.width + 31) / 32, 2 + ranges, kJoinWarps * 32, 0, s, a);
 }
 
 }  // namespace bp
