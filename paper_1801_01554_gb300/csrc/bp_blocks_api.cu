@@ -173,7 +173,7 @@ bp_status bp_residual_create(int width, int dtype, int max_rows, int max_gates, 
     if (l == nullptr) return fail(BP_ENOMEM, "%s: out of memory", call);
     l->cap = max_rows;
     l->max_gates = max_gates;
-    l->a.width = width, l->a.dtype = dtype, l->a.norm_out = norm_out, l->a.norm_in = norm_in, l->a.eps = eps;
+    l->a.width = width, l->a.dtype = dtype, l->a.norm_out = norm_out, l->a.norm_in = norm_in, l->a.eps = eps, l->a.each = 1.f / (float)width;
     st = make_flags(&l->device, &l->a.flags, call);
     if (st == BP_OK) st = cuda_status(cudaDeviceGetAttribute(&l->a.num_sms, cudaDevAttrMultiProcessorCount, l->device), call);
     if (st == BP_OK) st = cuda_status(residual_setup(width, dtype), call);

@@ -35,7 +35,7 @@ cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s);
 // ------------------------------------------------------------ residual stream (bp_residual.cu)
 struct ResidualArgs {
     int n, width, dtype, norm_out, norm_in, num_sms;
-    float eps, scale;
+    float eps, scale, each;   // each: 1 / width
     const void *X, *F;
     const float *wo, *bo, *gate, *wi, *bi;
     const int* offsets;     // of the gates' rows, or NULL

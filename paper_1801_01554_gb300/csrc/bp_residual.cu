@@ -8,7 +8,7 @@ namespace bp {
 namespace {
 
 constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
-constexpr int kSums = 10;        // of a reduction, at most
+constexpr int kSums = 16;        // of a reduction, at most
 constexpr int kWorkerRows = 4;   // of a worker of the backward pass, at least: its sums by column are added up at the end
 
 // A worker is `warps` warps that take a row at a time, a thread C pieces of V columns; a block has one or more.
@@ -36,31 +36,38 @@ struct Worker {
     }
 };
 
-// Sums of the worker's values, in one order, in every thread.
-template <int N>
-__device__ __forceinline__ void warp_sums(float (&v)[N], int lanes) {
-    for (int o = lanes / 2; o > 0; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-}
+// Sums of the worker's N values, in one order, in every thread.  A step that halves the lanes of a sum also halves the
+// sums of a lane (M, N rounded up to a power of two, to one), which takes M + 4 shuffles and as many to hand them out, not 5 N.
 template <int N>
 __device__ __forceinline__ void worker_sums(float (&v)[N], Worker& w) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if (w.warps == 1) return;
+    constexpr int M = N <= 1 ? 1 : N <= 4 ? 4 : 16, L = 32 / M;   // lanes of a sum, in the end
+    static_assert(N <= M && N <= kSums, "");
     const int lane = threadIdx.x & 31;
-    float* at = w.next();
-    if (lane == 0)
+    float x[M];
 #pragma unroll
-        for (int i = 0; i < N; ++i) at[(w.tid >> 5) * N + i] = v[i];
-    w.sync();
+    for (int i = 0; i < M; ++i) x[i] = i < N ? v[i < N ? i : 0] : 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = lane < w.warps ? at[lane * N + i] : 0.f;
-    warp_sums(v, 16);
+    for (int h = M / 2, bit = 16; h >= 1; h /= 2, bit /= 2) {
+        const bool upper = lane & bit;
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, v[i], 0);
+        for (int i = 0; i < h; ++i) {
+            const float send = upper ? x[i] : x[i + h], keep = upper ? x[i + h] : x[i];
+            x[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+        }
+    }
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+    if (w.warps > 1) {
+        float* at = w.next();
+        if (lane % L == 0) at[(w.tid >> 5) * M + lane / L] = x[0];
+        w.sync();
+        x[0] = 0.f;
+        for (int i = lane % L; i < w.warps; i += L) x[0] += at[i * M + lane / L];
+#pragma unroll
+        for (int o = (L < kMaxWarps ? L : kMaxWarps) / 2; o > 0; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, x[0], i * L);
 }
 
 // Number, mean and sum of squared differences from it, of two sets together: no cancellation where the mean
@@ -118,32 +125,37 @@ __device__ __forceinline__ void load_floats(const Columns<V, C>& cols, const flo
 template <class T, int V, int C, int N, int S>
 struct Ring {
     static constexpr int kBytes = V * (int)sizeof(T);
-    unsigned base;
+    unsigned base, slot;   // slot: of the row that is taken next, and that is asked for S rows ahead
     int lanes;
-    __device__ __forceinline__ Ring(const void* shared) : base(smem_u32(shared) + threadIdx.x * kBytes), lanes(blockDim.x * kBytes) {}
-    __device__ __forceinline__ unsigned place(int stage, int n, int j) const { return base + ((stage * N + n) * C + j) * lanes; }
-    __device__ __forceinline__ void ask(const Columns<V, C>& cols, const void* p, long long row, int stage, int n) const {
+    __device__ __forceinline__ Ring(const void* shared) : base(smem_u32(shared) + threadIdx.x * kBytes), slot(base), lanes(blockDim.x * kBytes) {}
+    __device__ __forceinline__ unsigned place(int n, int j) const { return slot + (n * C + j) * lanes; }
+    __device__ __forceinline__ void step() {
+        slot += N * C * lanes;
+        if (slot == base + S * N * C * lanes) slot = base;
+    }
+    // Pieces of array n from its element `at` on.
+    __device__ __forceinline__ void ask(const Columns<V, C>& cols, const void* p, long long at, int n) const {
         if (p == nullptr) return;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             if (!cols.in(j)) continue;
-            const T* from = (const T*)p + (size_t)row * cols.width + cols.at(j);
-            if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(stage, n, j)), "l"(from) : "memory");
-            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(place(stage, n, j)), "l"(from) : "memory");
+            const T* from = (const T*)p + (at + j * cols.threads * V);
+            if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(n, j)), "l"(from) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(place(n, j)), "l"(from) : "memory");
         }
     }
     __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
     __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory"); }
     // The row's pieces; zeros for an array that is not there and past the row's end.
-    __device__ __forceinline__ void take(const Columns<V, C>& cols, const void* p, int stage, int n, Piece<T, V> (&out)[C]) const {
+    __device__ __forceinline__ void take(const Columns<V, C>& cols, const void* p, int n, Piece<T, V> (&out)[C]) const {
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             out[j].u = make_uint4(0u, 0u, 0u, 0u);
             if (p == nullptr || !cols.in(j)) continue;
             uint4& u = out[j].u;
             if constexpr (kBytes == 16)
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(stage, n, j)) : "memory");
-            else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u.x) : "r"(place(stage, n, j)) : "memory");
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(n, j)) : "memory");
+            else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u.x) : "r"(place(n, j)) : "memory");
         }
     }
 };
@@ -215,14 +227,14 @@ __device__ __forceinline__ void norm_stats(const ResidualArgs& g, const Columns<
         worker_moments(m, w);
         const float var = m.m2 / m.n + (kind == BP_NORM_LAYER ? 0.f : m.mean * m.mean);
         mean = kind == BP_NORM_LAYER ? m.mean : 0.f;
-        rinv = 1.f / sqrtf(var + g.eps);
+        rinv = rsqrtf(var + g.eps);
     } else {
         float s[1] = {0.f};
 #pragma unroll
         for (int i = 0; i < V * C; ++i) s[0] = fmaf(v[i], v[i], s[0]);   // (columns past the row's end are 0)
         worker_sums(s, w);
         mean = 0.f;
-        rinv = 1.f / sqrtf(s[0] / (float)g.width + g.eps);
+        rinv = rsqrtf(fmaf(s[0], g.each, g.eps));
     }
 }
 
@@ -236,20 +248,22 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
     __shared__ float red[2 * kMaxWarps * kSums];
     Worker w(g.worker_warps, red);
     const Columns<V, C> cols(g.width, w);
-    const Ring<T, V, C, 2, S> ring(room);
+    Ring<T, V, C, 2, S> ring(room);
     const int mine = blockIdx.x * g.workers_a_block + w.id;
     check_offsets(g);
     if (mine >= g.workers) return;
     const int r0 = first_row(g, mine), r1 = first_row(g, mine + 1);
-    const auto ask = [&](int r) {
-        if (r < r1) {
-            ring.ask(cols, g.X, r, (r - r0) % S, 0);
-            ring.ask(cols, g.F, r, (r - r0) % S, 1);
+    long long at = (long long)r0 * g.width + cols.at(0);   // this thread's first value of the row
+    const auto ask = [&](int ahead) {
+        if (at + (long long)ahead * g.width < (long long)r1 * g.width) {
+            ring.ask(cols, g.X, at + (long long)ahead * g.width, 0);
+            ring.ask(cols, g.F, at + (long long)ahead * g.width, 1);
         }
         ring.commit();
+        ring.step();
     };
 #pragma unroll
-    for (int i = 0; i < S; ++i) ask(r0 + i);
+    for (int i = 0; i < S; ++i) ask(i);
     const bool block = g.F != nullptr, normed_in = g.norm_in != BP_NORM_NONE && (g.H != nullptr || g.stats != nullptr);
     float wo[P], wi[P], bo[MEAN ? P : 1], bi[MEAN ? P : 1], k[P];
     load_floats(cols, g.wo, 1.f, wo);
@@ -266,8 +280,8 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
         }
         Piece<T, V> x[C], f[C];
         ring.wait();
-        ring.take(cols, g.X, (r - r0) % S, 0, x);
-        ring.take(cols, g.F, (r - r0) % S, 1, f);
+        ring.take(cols, g.X, 0, x);
+        ring.take(cols, g.F, 1, f);
         float y[P], u[P], mf = 0.f, rf = 1.f, my = 0.f, ry = 1.f;
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -298,7 +312,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
         if (g.Y != nullptr)
 #pragma unroll
             for (int j = 0; j < C; ++j)
-                if (cols.in(j)) x[j].store((T*)g.Y + (size_t)r * g.width + cols.at(j));
+                if (cols.in(j)) x[j].store((T*)g.Y + at + j * w.threads * V);
         if (normed_in) norm_stats<MEAN>(g, cols, y, g.norm_in, w, my, ry);
         if (g.H != nullptr) {
 #pragma unroll
@@ -313,12 +327,13 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
                 }
                 Piece<T, V> p;
                 p.set(h);
-                p.store((T*)g.H + (size_t)r * g.width + cols.at(j));
+                p.store((T*)g.H + at + j * w.threads * V);
             }
         }
         if (g.stats != nullptr && w.tid < 4)
             g.stats[(size_t)r * 4 + w.tid] = w.tid == 0 ? mf : w.tid == 1 ? rf : w.tid == 2 ? my : ry;
-        ask(r + S);   // (the stage's values are in registers)
+        ask(S);   // (the row's values are in registers)
+        at += g.width;
     }
 }
 
@@ -336,27 +351,28 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
     pdl_launch();
     Worker w(g.worker_warps, red);
     const Columns<V, C> cols(g.width, w);
-    const Ring<T, V, C, 4, S> ring(room);
+    Ring<T, V, C, 4, S> ring(room);
     const int mine = blockIdx.x * g.workers_a_block + w.id;
     check_offsets(g);
     const bool live = mine < g.workers;
     const int r0 = live ? first_row(g, mine) : 0, r1 = live ? first_row(g, mine + 1) : 0;
     const void* Y = g.dH != nullptr ? g.Y : nullptr;
-    const auto ask = [&](int r) {
-        if (r < r1) {
-            const int stage = (r - r0) % S;
-            ring.ask(cols, Y, r, stage, 0);
-            ring.ask(cols, g.F, r, stage, 1);
-            ring.ask(cols, g.dY, r, stage, 2);
-            ring.ask(cols, g.dH, r, stage, 3);
+    long long at = (long long)r0 * g.width + cols.at(0);   // this thread's first value of the row
+    const auto ask = [&](int ahead) {
+        const long long x = at + (long long)ahead * g.width;
+        if (x < (long long)r1 * g.width) {
+            ring.ask(cols, Y, x, 0);
+            ring.ask(cols, g.F, x, 1);
+            ring.ask(cols, g.dY, x, 2);
+            ring.ask(cols, g.dH, x, 3);
         }
         ring.commit();
+        ring.step();
     };
 #pragma unroll
-    for (int i = 0; i < S; ++i) ask(r0 + i);
+    for (int i = 0; i < S; ++i) ask(i);
     const bool out_normed = g.norm_out != BP_NORM_NONE;
     const float layer_in = g.norm_in == BP_NORM_LAYER ? 1.f : 0.f, layer_out = g.norm_out == BP_NORM_LAYER ? 1.f : 0.f;
-    const float each = 1.f / (float)g.width;
     const bool by_range = g.n_gates > 0 && g.offsets != nullptr;
     float k[P], wi[P];
     load_floats(cols, g.wi, 1.f, wi);
@@ -386,6 +402,12 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
         }
         fresh = false;
     };
+    float next[4] = {};   // the row's statistics
+    const auto load_stats = [&](int r) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) next[i] = __ldg(g.stats + (size_t)r * 4 + i);
+    };
+    if (r0 < r1) load_stats(r0);
     Stretch now{0, r0};
     for (int r = r0; r < r1; ++r) {
         if (r >= now.end) {
@@ -397,15 +419,14 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
 #pragma unroll
             for (int c = 0; c < P; ++c) k[c] *= wo[c];
         }
-        const float* st = g.stats + (size_t)r * 4;
-        const float mf = __ldg(st), rf = __ldg(st + 1), my = __ldg(st + 2), ry = __ldg(st + 3);
-        const int stage = (r - r0) % S;
+        const float mf = next[0], rf = next[1], my = next[2], ry = next[3];
+        if (r + 1 < r1) load_stats(r + 1);
         Piece<T, V> y[C], f[C], a[C], b[C];
         ring.wait();
-        ring.take(cols, Y, stage, 0, y);
-        ring.take(cols, g.F, stage, 1, f);
-        ring.take(cols, g.dY, stage, 2, a);
-        ring.take(cols, g.dH, stage, 3, b);
+        ring.take(cols, Y, 0, y);
+        ring.take(cols, g.F, 1, f);
+        ring.take(cols, g.dY, 2, a);
+        ring.take(cols, g.dH, 3, b);
         float s[N] = {};
 #pragma unroll
         for (int j = 0; j < C; ++j) {
@@ -432,16 +453,16 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
             }
         }
         worker_sums(s, w);
-        const float c1 = ry * s[0] * each;
+        const float c1 = ry * s[0] * g.each;
         float c0 = 0.f, d0 = 0.f, d1 = 0.f;
-        if constexpr (MEAN) c0 = layer_in * s[4] * each;
+        if constexpr (MEAN) c0 = layer_in * s[4] * g.each;
         if (out_normed) {
             float x = s[2] - c1 * ry * s[3];
             if constexpr (MEAN) {
                 x -= c0 * s[5];
-                d0 = layer_out * (s[6] + ry * (s[7] - c0 * s[9] - c1 * ry * s[8])) * each;
+                d0 = layer_out * (s[6] + ry * (s[7] - c0 * s[9] - c1 * ry * s[8])) * g.each;
             }
-            d1 = rf * (s[1] + ry * x) * each;
+            d1 = rf * (s[1] + ry * x) * g.each;
         }
         const float by_y = -ry * c1, by_f = -rf * d1, shift_y = ry * c0, shift_f = rf * d0;
 #pragma unroll
@@ -467,17 +488,17 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
                 }
             }
             Piece<T, V> p;
-            const size_t at = (size_t)r * g.width + cols.at(j);
             if (g.dX != nullptr) {
                 p.set(dx);
-                p.store((T*)g.dX + at);
+                p.store((T*)g.dX + at + j * w.threads * V);
             }
             if (g.dF != nullptr) {
                 p.set(df);
-                p.store((T*)g.dF + at);
+                p.store((T*)g.dF + at + j * w.threads * V);
             }
         }
-        ask(r + S);   // (the stage's values are in registers)
+        ask(S);   // (the row's values are in registers)
+        at += g.width;
     }
     if (by_range && live && (g.Gwo != nullptr || g.Gbo != nullptr || g.Ggate != nullptr)) flush(now.seg);
     // The block's sums over its rows.
