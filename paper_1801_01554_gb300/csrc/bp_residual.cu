@@ -6,9 +6,9 @@
 
 namespace bp {
 namespace {
-
 constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
-constexpr int kSums = 16;        // of a reduction, at most
+constexpr int kSums = 16;        // of the reductions between two barriers, at most
+constexpr int kRed = kMaxWarps * kSums;
 constexpr int kWorkerRows = 4;   // of a worker of the backward pass, at least: its sums by column are added up at the end
 
 // A worker is `warps` warps that take a row at a time, a thread C pieces of V columns; a block has one or more.
@@ -16,59 +16,67 @@ constexpr int kWorkerRows = 4;   // of a worker of the backward pass, at least: 
 // need no barrier.)
 struct Worker {
     int id, warps, tid, threads;   // id: in the block
-    float* red;                    // two halves of kMaxWarps * kSums, used in turn: one barrier a reduction
-    int turn;
+    float* red;
     __device__ __forceinline__ Worker(int warps_, float* shared) : warps(warps_) {
         threads = warps * 32;
         id = threadIdx.x / threads;
         tid = threadIdx.x - id * threads;
         red = shared + id * warps * kSums;
-        turn = 0;
     }
     __device__ __forceinline__ void sync() const {
         if (warps == 1) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(id + 1), "r"(threads) : "memory");
     }
-    __device__ __forceinline__ float* next() {
-        float* at = red + turn * kMaxWarps * kSums;
-        turn ^= 1;
-        return at;
-    }
 };
 
-// Sums of the worker's N values, in one order, in every thread.  A step that halves the lanes of a sum also halves the
-// sums of a lane (M, N rounded up to a power of two, to one), which takes M + 4 shuffles and as many to hand them out, not 5 N.
+// Sums of the worker's N values, in one order, in every thread: each warp gives its part before the worker's barrier,
+// and takes the sums after it.  (Two places, used in turn, so that one barrier a reduction is enough.)  A step that
+// halves the lanes of a sum also halves the sums of a lane (M, N rounded up to a power of two, to one), which takes M + 4
+// shuffles and as many to hand them out, not 5 N.
 template <int N>
-__device__ __forceinline__ void worker_sums(float (&v)[N], Worker& w) {
-    constexpr int M = N <= 1 ? 1 : N <= 4 ? 4 : 16, L = 32 / M;   // lanes of a sum, in the end
-    static_assert(N <= M && N <= kSums, "");
-    const int lane = threadIdx.x & 31;
-    float x[M];
+struct Sums {
+    static constexpr int M = N <= 1 ? 1 : N <= 4 ? 4 : 16, L = 32 / M;   // lanes of a sum, in the end
+    static_assert(N <= M && M <= kSums, "");
+    float* at;
+    int turn = 0;
+    float mine = 0.f;
+    __device__ __forceinline__ explicit Sums(const Worker& w, int place = 0) : at(w.red + place * w.warps) {}
+    __device__ __forceinline__ void give(const float (&v)[N], const Worker& w) {
+        const int lane = threadIdx.x & 31;
+        float x[M];
 #pragma unroll
-    for (int i = 0; i < M; ++i) x[i] = i < N ? v[i < N ? i : 0] : 0.f;
+        for (int i = 0; i < M; ++i) x[i] = i < N ? v[i < N ? i : 0] : 0.f;
 #pragma unroll
-    for (int h = M / 2, bit = 16; h >= 1; h /= 2, bit /= 2) {
-        const bool upper = lane & bit;
+        for (int h = M / 2, bit = 16; h >= 1; h /= 2, bit /= 2) {
+            const bool upper = lane & bit;
 #pragma unroll
-        for (int i = 0; i < h; ++i) {
-            const float send = upper ? x[i] : x[i + h], keep = upper ? x[i + h] : x[i];
-            x[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+            for (int i = 0; i < h; ++i) {
+                const float send = upper ? x[i] : x[i + h], keep = upper ? x[i + h] : x[i];
+                x[i] = keep + __shfl_xor_sync(0xffffffffu, send, bit);
+            }
+        }
+#pragma unroll
+        for (int o = L / 2; o > 0; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+        if (w.warps > 1) {
+            if (lane % L == 0) at[turn * kRed + (w.tid >> 5) * M + lane / L] = x[0];
+        } else {
+            mine = x[0];
         }
     }
+    __device__ __forceinline__ void take(float (&v)[N], const Worker& w) {
+        const int lane = threadIdx.x & 31;
+        float x = mine;
+        if (w.warps > 1) {
+            x = 0.f;
+            for (int i = lane % L; i < w.warps; i += L) x += at[turn * kRed + i * M + lane / L];
 #pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
-    if (w.warps > 1) {
-        float* at = w.next();
-        if (lane % L == 0) at[(w.tid >> 5) * M + lane / L] = x[0];
-        w.sync();
-        x[0] = 0.f;
-        for (int i = lane % L; i < w.warps; i += L) x[0] += at[i * M + lane / L];
+            for (int o = (L < kMaxWarps ? L : kMaxWarps) / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            turn ^= 1;
+        }
 #pragma unroll
-        for (int o = (L < kMaxWarps ? L : kMaxWarps) / 2; o > 0; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, x, i * L);
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, x[0], i * L);
-}
+};
 
 // Number, mean and sum of squared differences from it, of two sets together: no cancellation where the mean
 // is far from 0.
@@ -77,7 +85,7 @@ struct Moments {
     __device__ __forceinline__ void join(float n2, float mean2, float m22) {
         const float all = n + n2;
         if (all == 0.f) return;
-        const float d = mean2 - mean, part = n2 / all;
+        const float d = mean2 - mean, part = __fdividef(n2, all);
         mean += d * part;
         m2 += m22 + d * d * n * part;
         n = all;
@@ -87,20 +95,59 @@ struct Moments {
             join(__shfl_xor_sync(0xffffffffu, n, o), __shfl_xor_sync(0xffffffffu, mean, o), __shfl_xor_sync(0xffffffffu, m2, o));
     }
 };
-__device__ __forceinline__ void worker_moments(Moments& m, Worker& w) {
-    m.join_lanes(32);
-    if (w.warps > 1) {
-        const int lane = threadIdx.x & 31, at_warp = (w.tid >> 5) * 3;
-        float* at = w.next();
-        if (lane == 0) at[at_warp] = m.n, at[at_warp + 1] = m.mean, at[at_warp + 2] = m.m2;
-        w.sync();
-        m = {0.f, 0.f, 0.f};
-        if (lane < w.warps) m = {at[lane * 3], at[lane * 3 + 1], at[lane * 3 + 2]};
-        m.join_lanes(16);
+
+// Two float32 operations an instruction, over a thread's P values (one at a time where P is 1).
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(unsigned long long x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ unsigned long long fma_pair(unsigned long long a, unsigned long long b, unsigned long long c) {
+    unsigned long long r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ unsigned long long mul_pair(unsigned long long a, unsigned long long b) {
+    unsigned long long r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// One value for all places, or a value each.
+struct Same {
+    float x;
+    __device__ __forceinline__ float operator[](int) const { return x; }
+};
+template <int P, class A, class B>
+__device__ __forceinline__ void mul(float (&d)[P], const A& a, const B& b) {
+    if constexpr (P == 1) d[0] = a[0] * b[0];
+    else
+#pragma unroll
+        for (int i = 0; i < P; i += 2) unpair(mul_pair(pair(a[i], a[i + 1]), pair(b[i], b[i + 1])), d[i], d[i + 1]);
+}
+template <int P, class A, class B, class D>
+__device__ __forceinline__ void fma(float (&d)[P], const A& a, const B& b, const D& c) {
+    if constexpr (P == 1) d[0] = fmaf(a[0], b[0], c[0]);
+    else
+#pragma unroll
+        for (int i = 0; i < P; i += 2)
+            unpair(fma_pair(pair(a[i], a[i + 1]), pair(b[i], b[i + 1]), pair(c[i], c[i + 1])), d[i], d[i + 1]);
+}
+template <int P>
+__device__ __forceinline__ void sub(float (&d)[P], const float (&a)[P], float b) {   // a - b, exact where a times 1 is
+    fma(d, a, Same{1.f}, Same{-b});
+}
+template <int P, class A>
+__device__ __forceinline__ float dot(const A& a, const float (&b)[P]) {
+    if constexpr (P == 1) return a[0] * b[0];
+    else {
+        unsigned long long s = mul_pair(pair(a[0], a[1]), pair(b[0], b[1]));
+#pragma unroll
+        for (int i = 2; i < P; i += 2) s = fma_pair(pair(a[i], a[i + 1]), pair(b[i], b[i + 1]), s);
+        float x, y;
+        unpair(s, x, y);
+        return x + y;
     }
-    m.n = __shfl_sync(0xffffffffu, m.n, 0);
-    m.mean = __shfl_sync(0xffffffffu, m.mean, 0);
-    m.m2 = __shfl_sync(0xffffffffu, m.m2, 0);
 }
 
 // A thread's columns: C pieces of V, the worker's width apart.
@@ -112,12 +159,39 @@ struct Columns {
     __device__ __forceinline__ bool in(int j) const { return at(j) < width; }
 };
 
+// A value a column; 0 past the row's end, which keeps what is there out of every sum.
 template <int V, int C>
 __device__ __forceinline__ void load_floats(const Columns<V, C>& cols, const float* p, float none, float (&out)[V * C]) {
 #pragma unroll
     for (int j = 0; j < C; ++j)
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[j * V + i] = p != nullptr && cols.in(j) ? __ldg(p + cols.at(j) + i) : none;
+        for (int i = 0; i < V; ++i) out[j * V + i] = !cols.in(j) ? 0.f : p != nullptr ? __ldg(p + cols.at(j) + i) : none;
+}
+template <class T, int V, int C>
+__device__ __forceinline__ void values(const Piece<T, V> (&p)[C], float (&out)[V * C]) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        float x[V];
+        p[j].values(x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) out[j * V + i] = x[i];
+    }
+}
+template <class T, int V, int C>
+__device__ __forceinline__ void round_to(const float (&x)[V * C], Piece<T, V> (&p)[C]) {
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+        float y[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) y[i] = x[j * V + i];
+        p[j].set(y);
+    }
+}
+template <class T, int V, int C>
+__device__ __forceinline__ void store_row(const Columns<V, C>& cols, const Piece<T, V> (&p)[C], T* to) {
+#pragma unroll
+    for (int j = 0; j < C; ++j)
+        if (cols.in(j)) p[j].store(to + j * cols.threads * V);
 }
 
 // Rows on their way: S rows of N arrays, each thread's pieces in places of its own in shared memory, so that a thread
@@ -125,45 +199,45 @@ __device__ __forceinline__ void load_floats(const Columns<V, C>& cols, const flo
 template <class T, int V, int C, int N, int S>
 struct Ring {
     static constexpr int kBytes = V * (int)sizeof(T);
-    unsigned base, slot;   // slot: of the row that is taken next, and that is asked for S rows ahead
+    unsigned base;
     int lanes;
-    __device__ __forceinline__ Ring(const void* shared) : base(smem_u32(shared) + threadIdx.x * kBytes), slot(base), lanes(blockDim.x * kBytes) {}
-    __device__ __forceinline__ unsigned place(int n, int j) const { return slot + (n * C + j) * lanes; }
-    __device__ __forceinline__ void step() {
+    __device__ __forceinline__ Ring(const void* shared) : base(smem_u32(shared) + threadIdx.x * kBytes), lanes(blockDim.x * kBytes) {}
+    __device__ __forceinline__ unsigned place(unsigned slot, int n, int j) const { return slot + (n * C + j) * lanes; }
+    __device__ __forceinline__ void step(unsigned& slot) const {
         slot += N * C * lanes;
         if (slot == base + S * N * C * lanes) slot = base;
     }
-    // Pieces of array n from its element `at` on.
-    __device__ __forceinline__ void ask(const Columns<V, C>& cols, const void* p, long long at, int n) const {
-        if (p == nullptr) return;
+    // Pieces of array n from p on.
+    __device__ __forceinline__ void ask(const Columns<V, C>& cols, const T* p, unsigned slot, int n) const {
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             if (!cols.in(j)) continue;
-            const T* from = (const T*)p + (at + j * cols.threads * V);
-            if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(n, j)), "l"(from) : "memory");
-            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(place(n, j)), "l"(from) : "memory");
+            const T* from = p + j * cols.threads * V;
+            if constexpr (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(place(slot, n, j)), "l"(from) : "memory");
+            else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(place(slot, n, j)), "l"(from) : "memory");
         }
     }
     __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-    __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory"); }
+    __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory"); }   // for the first of S rows
     // The row's pieces; zeros for an array that is not there and past the row's end.
-    __device__ __forceinline__ void take(const Columns<V, C>& cols, const void* p, int n, Piece<T, V> (&out)[C]) const {
+    __device__ __forceinline__ void take(const Columns<V, C>& cols, bool there, unsigned slot, int n, Piece<T, V> (&out)[C]) const {
 #pragma unroll
         for (int j = 0; j < C; ++j) {
             out[j].u = make_uint4(0u, 0u, 0u, 0u);
-            if (p == nullptr || !cols.in(j)) continue;
+            if (!there || !cols.in(j)) continue;
             uint4& u = out[j].u;
             if constexpr (kBytes == 16)
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(n, j)) : "memory");
-            else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u.x) : "r"(place(n, j)) : "memory");
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(slot, n, j)) : "memory");
+            else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u.x) : "r"(place(slot, n, j)) : "memory");
         }
     }
 };
-// Stages: as many as fit twice (forward) or once on an SM beside 512 threads.
+// Stages.  Three rows are enough to keep the memory busy (16,384 rows of 4,096 bfloat16 units, forward: 2 stages 100.0 us,
+// 3 98.5, 6 as 4: what more of them take from the L1 cache is missed).
 template <class T, int V, int C>
 constexpr int stages(bool back) {
     constexpr int bytes = V * C * (int)sizeof(T);
-    return bytes <= 16 ? 6 : bytes <= 32 ? 3 : back ? 1 : 3;
+    return bytes <= 32 ? 3 : back ? 1 : 3;
 }
 
 // Rows that share a row of gates: of row r, the gates' row (-1: none) and the first row from r on that is not of it.
@@ -200,140 +274,161 @@ __device__ __forceinline__ void load_gate(const ResidualArgs& g, const Columns<V
     for (int i = 0; i < V * C; ++i) k[i] *= g.scale;
 }
 
+// Mean and 1 / sqrt of a row, in the same two steps as Sums.
 template <bool MEAN, int V, int C>
-__device__ __forceinline__ void norm_stats(const ResidualArgs& g, const Columns<V, C>& cols, const float (&v)[V * C], int kind, Worker& w,
-                                           float& mean, float& rinv) {
-    if constexpr (MEAN) {
-        Moments m{0.f, 0.f, 0.f};
-        float sum = 0.f;
-        int n = 0;
+struct NormStats {
+    Sums<1> sums;
+    Moments m;
+    float* at;
+    int turn = 0;
+    __device__ __forceinline__ NormStats(const Worker& w, int place) : sums(w, place), at(w.red + place * w.warps) {}
+    __device__ __forceinline__ void give(const Columns<V, C>& cols, const float (&v)[V * C], const Worker& w) {
+        if constexpr (MEAN) {
+            float sum = 0.f;
+            int n = 0;
 #pragma unroll
-        for (int j = 0; j < C; ++j)
-            if (cols.in(j)) {
-                n += V;
+            for (int j = 0; j < C; ++j)
+                if (cols.in(j)) {
+                    n += V;
 #pragma unroll
-                for (int i = 0; i < V; ++i) sum += v[j * V + i];
-            }
-        m.n = (float)n;
-        m.mean = n > 0 ? sum / m.n : 0.f;
-#pragma unroll
-        for (int j = 0; j < C; ++j)
-            if (cols.in(j))
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float d = v[j * V + i] - m.mean;
-                    m.m2 += d * d;
+                    for (int i = 0; i < V; ++i) sum += v[j * V + i];
                 }
-        worker_moments(m, w);
-        const float var = m.m2 / m.n + (kind == BP_NORM_LAYER ? 0.f : m.mean * m.mean);
-        mean = kind == BP_NORM_LAYER ? m.mean : 0.f;
-        rinv = rsqrtf(var + g.eps);
-    } else {
-        float s[1] = {0.f};
+            m = {(float)n, n > 0 ? __fdividef(sum, (float)n) : 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < V * C; ++i) s[0] = fmaf(v[i], v[i], s[0]);   // (columns past the row's end are 0)
-        worker_sums(s, w);
-        mean = 0.f;
-        rinv = rsqrtf(fmaf(s[0], g.each, g.eps));
+            for (int j = 0; j < C; ++j)
+                if (cols.in(j))
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float d = v[j * V + i] - m.mean;
+                        m.m2 += d * d;
+                    }
+            m.join_lanes(32);
+            float* to = at + turn * kRed + (w.tid >> 5) * 3;
+            if (w.warps > 1 && (threadIdx.x & 31) == 0) to[0] = m.n, to[1] = m.mean, to[2] = m.m2;
+        } else {
+            const float s[1] = {dot(v, v)};   // (columns past the row's end are 0)
+            sums.give(s, w);
+        }
     }
-}
+    __device__ __forceinline__ void take(const ResidualArgs& g, int kind, const Worker& w, float& mean, float& rinv) {
+        if constexpr (MEAN) {
+            if (w.warps > 1) {
+                const int lane = threadIdx.x & 31;
+                const float* from = at + turn * kRed + lane * 3;
+                m = {0.f, 0.f, 0.f};
+                if (lane < w.warps) m = {from[0], from[1], from[2]};
+                m.join_lanes(16);
+                turn ^= 1;
+            }
+            m.mean = __shfl_sync(0xffffffffu, m.mean, 0);
+            const float var = __shfl_sync(0xffffffffu, m.m2, 0) * g.each + (kind == BP_NORM_LAYER ? 0.f : m.mean * m.mean);
+            mean = kind == BP_NORM_LAYER ? m.mean : 0.f;
+            rinv = rsqrtf(var + g.eps);
+        } else {
+            float s[1];
+            sums.take(s, w);
+            mean = 0.f;
+            rinv = rsqrtf(fmaf(s[0], g.each, g.eps));
+        }
+    }
+};
 
 // A worker takes consecutive rows, a thread the same columns of each, whose weights stay in its registers; rows ahead
-// are on their way in shared memory.  MEAN: a norm takes means off.  Bound by reading X and F once and writing Y
-// and H once.
-template <class T, int V, int C, bool MEAN>
-__global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
+// are on their way in shared memory.  MEAN: a norm takes means off.  FULL: every operand and both norms are there, known
+// to the compiler.  Bound by reading X and F once and writing Y and H once.
+template <class T, int V, int C, bool MEAN, bool FULL>
+__global__ void __maxnreg__(V * C <= 8 && !MEAN ? 64 : 128) k_residual(ResidualArgs g) {
     constexpr int P = V * C, S = stages<T, V, C>(false);
     extern __shared__ __align__(16) unsigned char room[];
-    __shared__ float red[2 * kMaxWarps * kSums];
+    __shared__ float red[2 * kRed];
     Worker w(g.worker_warps, red);
     const Columns<V, C> cols(g.width, w);
-    Ring<T, V, C, 2, S> ring(room);
+    const Ring<T, V, C, 2, S> ring(room);
     const int mine = blockIdx.x * g.workers_a_block + w.id;
     check_offsets(g);
     if (mine >= g.workers) return;
-    const int r0 = first_row(g, mine), r1 = first_row(g, mine + 1);
-    long long at = (long long)r0 * g.width + cols.at(0);   // this thread's first value of the row
-    const auto ask = [&](int ahead) {
-        if (at + (long long)ahead * g.width < (long long)r1 * g.width) {
-            ring.ask(cols, g.X, at + (long long)ahead * g.width, 0);
-            ring.ask(cols, g.F, at + (long long)ahead * g.width, 1);
+    const int r0 = first_row(g, mine), r1 = first_row(g, mine + 1), n = r1 - r0;
+    const bool block = FULL || g.F != nullptr, normed_out = FULL || (block && g.norm_out != BP_NORM_NONE);
+    const bool gives_y = FULL || g.Y != nullptr, gives_h = FULL || g.H != nullptr;
+    const bool normed_in = FULL || (g.norm_in != BP_NORM_NONE && (gives_h || g.stats != nullptr));
+    const size_t at = (size_t)r0 * g.width + cols.at(0);   // this thread's first value
+    const T *X = (const T*)g.X + at, *F = (const T*)g.F + at;
+    T *Y = (T*)g.Y + at, *H = (T*)g.H + at;
+    float* stats = g.stats != nullptr && w.tid < 4 ? g.stats + (size_t)r0 * 4 + w.tid : nullptr;
+    unsigned slot = ring.base;
+    int left = n;   // rows to ask for
+    const auto ask = [&] {
+        if (left > 0) {
+            ring.ask(cols, X, slot, 0);
+            if (block) ring.ask(cols, F, slot, 1);
         }
+        --left;
+        X += g.width, F += g.width;
         ring.commit();
-        ring.step();
+        ring.step(slot);
     };
 #pragma unroll
-    for (int i = 0; i < S; ++i) ask(i);
-    const bool block = g.F != nullptr, normed_in = g.norm_in != BP_NORM_NONE && (g.H != nullptr || g.stats != nullptr);
-    float wo[P], wi[P], bo[MEAN ? P : 1], bi[MEAN ? P : 1], k[P];
-    load_floats(cols, g.wo, 1.f, wo);
+    for (int i = 0; i < S; ++i) ask();
+    float k[P], wi[P], kb[MEAN ? P : 1], bi[MEAN ? P : 1];   // k: scale * gate * w_out, kb: scale * gate * b_out
     load_floats(cols, g.wi, 1.f, wi);
-    if constexpr (MEAN) {
-        load_floats(cols, g.bo, 0.f, bo);
-        load_floats(cols, g.bi, 0.f, bi);
-    }
+    if constexpr (MEAN) load_floats(cols, g.bi, 0.f, bi);
+    NormStats<MEAN, V, C> of_f(w, 0), of_y(w, 4);
     Stretch now{0, r0};
     for (int r = r0; r < r1; ++r) {
         if (r >= now.end) {
             now = stretch_of(g, r);
             load_gate(g, cols, now.seg, k);
+            if constexpr (MEAN) {
+                load_floats(cols, g.bo, 0.f, kb);
+                mul(kb, kb, k);
+            }
+            float wo[P];
+            load_floats(cols, g.wo, 1.f, wo);
+            mul(k, k, wo);
         }
-        Piece<T, V> x[C], f[C];
+        float y[P], mf = 0.f, rf = 1.f, my = 0.f, ry = 1.f;
+        Piece<T, V> p[C];
         ring.wait();
-        ring.take(cols, g.X, 0, x);
-        ring.take(cols, g.F, 1, f);
-        float y[P], u[P], mf = 0.f, rf = 1.f, my = 0.f, ry = 1.f;
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            float a[V], b[V];
-            x[j].values(a);
-            f[j].values(b);
-#pragma unroll
-            for (int i = 0; i < V; ++i) y[j * V + i] = a[i], u[j * V + i] = b[i];
-        }
+        ring.take(cols, true, slot, 0, p);
+        values<T, V, C>(p, y);
         if (block) {
-            if (g.norm_out != BP_NORM_NONE) norm_stats<MEAN>(g, cols, u, g.norm_out, w, mf, rf);
-#pragma unroll
-            for (int j = 0; j < C; ++j) {
-                float a[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const int c = j * V + i;
-                    float h = (u[c] - mf) * rf * wo[c];
-                    if constexpr (MEAN) h += bo[c];
-                    a[i] = cols.in(j) ? fmaf(k[c], h, y[c]) : 0.f;
-                }
-                x[j].set(a);
-                x[j].values(a);
-#pragma unroll
-                for (int i = 0; i < V; ++i) y[j * V + i] = a[i];
+            float u[P];
+            ring.take(cols, true, slot, 1, p);
+            values<T, V, C>(p, u);
+            if (normed_out) {
+                of_f.give(cols, u, w);
+                w.sync();
+                of_f.take(g, g.norm_out, w, mf, rf);
             }
+            if constexpr (MEAN) sub(u, u, mf);
+            mul(u, u, Same{rf});
+            fma(y, k, u, y);
+            if constexpr (MEAN) fma(y, kb, Same{1.f}, y);
+            round_to<T, V, C>(y, p);
+            values<T, V, C>(p, y);
+        } else {
+            round_to<T, V, C>(y, p);
         }
-        if (g.Y != nullptr)
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-                if (cols.in(j)) x[j].store((T*)g.Y + at + j * w.threads * V);
-        if (normed_in) norm_stats<MEAN>(g, cols, y, g.norm_in, w, my, ry);
-        if (g.H != nullptr) {
-#pragma unroll
-            for (int j = 0; j < C; ++j) {
-                if (!cols.in(j)) continue;
-                float h[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const int c = j * V + i;
-                    h[i] = (y[c] - my) * ry * wi[c];
-                    if constexpr (MEAN) h[i] += bi[c];
-                }
-                Piece<T, V> p;
-                p.set(h);
-                p.store((T*)g.H + at + j * w.threads * V);
-            }
+        if (gives_y) store_row<T>(cols, p, Y);
+        if (normed_in) {
+            of_y.give(cols, y, w);
+            w.sync();
+            of_y.take(g, g.norm_in, w, my, ry);
         }
-        if (g.stats != nullptr && w.tid < 4)
-            g.stats[(size_t)r * 4 + w.tid] = w.tid == 0 ? mf : w.tid == 1 ? rf : w.tid == 2 ? my : ry;
-        ask(S);   // (the row's values are in registers)
-        at += g.width;
+        if (gives_h) {
+            if constexpr (MEAN) sub(y, y, my);
+            mul(y, y, Same{ry});
+            if constexpr (MEAN) fma(y, wi, y, bi);
+            else mul(y, wi, y);
+            round_to<T, V, C>(y, p);
+            store_row<T>(cols, p, H);
+        }
+        if (stats != nullptr) {
+            *stats = w.tid == 0 ? mf : w.tid == 1 ? rf : w.tid == 2 ? my : ry;
+            stats += 4;
+        }
+        ask();   // (the row's values are in registers)
+        Y += g.width, H += g.width;
     }
 }
 
@@ -343,35 +438,41 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual(ResidualArgs g) {
 // sums that need not wait for them: one reduction a row.  The sums by column stay in registers over a
 // worker's rows: of dy f^ and dy (what gates and output weights want, by stretch where gates are by range), of dH y^
 // and dH.  Bound by reading Y, F, dY and dH once and writing dX and dF once.
-template <class T, int V, int C, bool MEAN>
+template <class T, int V, int C, bool MEAN, bool FULL>
 __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs g) {
     constexpr int P = V * C, N = MEAN ? 10 : 4, S = stages<T, V, C>(true);
     extern __shared__ __align__(16) unsigned char room[];
-    __shared__ float red[2 * kMaxWarps * kSums];
+    __shared__ float red[2 * kRed];
     pdl_launch();
     Worker w(g.worker_warps, red);
     const Columns<V, C> cols(g.width, w);
-    Ring<T, V, C, 4, S> ring(room);
+    const Ring<T, V, C, 4, S> ring(room);
     const int mine = blockIdx.x * g.workers_a_block + w.id;
     check_offsets(g);
     const bool live = mine < g.workers;
     const int r0 = live ? first_row(g, mine) : 0, r1 = live ? first_row(g, mine + 1) : 0;
-    const void* Y = g.dH != nullptr ? g.Y : nullptr;
-    long long at = (long long)r0 * g.width + cols.at(0);   // this thread's first value of the row
-    const auto ask = [&](int ahead) {
-        const long long x = at + (long long)ahead * g.width;
-        if (x < (long long)r1 * g.width) {
-            ring.ask(cols, Y, x, 0);
-            ring.ask(cols, g.F, x, 1);
-            ring.ask(cols, g.dY, x, 2);
-            ring.ask(cols, g.dH, x, 3);
+    const bool has_f = FULL || g.F != nullptr, has_y = FULL || g.dY != nullptr, has_h = FULL || g.dH != nullptr;
+    const bool gives_x = FULL || g.dX != nullptr, gives_f = FULL || g.dF != nullptr;
+    const size_t at = (size_t)r0 * g.width + cols.at(0);   // this thread's first value
+    const T *Y = (const T*)g.Y + at, *F = (const T*)g.F + at, *dY = (const T*)g.dY + at, *dH = (const T*)g.dH + at;
+    T *dX = (T*)g.dX + at, *dF = (T*)g.dF + at;
+    unsigned slot = ring.base;
+    int left = r1 - r0;   // rows to ask for
+    const auto ask = [&] {
+        if (left > 0) {
+            if (has_h) ring.ask(cols, Y, slot, 0);
+            if (has_f) ring.ask(cols, F, slot, 1);
+            if (has_y) ring.ask(cols, dY, slot, 2);
+            if (has_h) ring.ask(cols, dH, slot, 3);
         }
+        --left;
+        Y += g.width, F += g.width, dY += g.width, dH += g.width;
         ring.commit();
-        ring.step();
+        ring.step(slot);
     };
 #pragma unroll
-    for (int i = 0; i < S; ++i) ask(i);
-    const bool out_normed = g.norm_out != BP_NORM_NONE;
+    for (int i = 0; i < S; ++i) ask();
+    const bool out_normed = FULL || g.norm_out != BP_NORM_NONE;
     const float layer_in = g.norm_in == BP_NORM_LAYER ? 1.f : 0.f, layer_out = g.norm_out == BP_NORM_LAYER ? 1.f : 0.f;
     const bool by_range = g.n_gates > 0 && g.offsets != nullptr;
     float k[P], wi[P];
@@ -402,6 +503,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
         }
         fresh = false;
     };
+    Sums<N> sums(w);
     float next[4] = {};   // the row's statistics
     const auto load_stats = [&](int r) {
 #pragma unroll
@@ -416,43 +518,34 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
             load_gate(g, cols, now.seg, k);
             float wo[P];
             load_floats(cols, g.wo, 1.f, wo);
-#pragma unroll
-            for (int c = 0; c < P; ++c) k[c] *= wo[c];
+            mul(k, k, wo);
         }
         const float mf = next[0], rf = next[1], my = next[2], ry = next[3];
         if (r + 1 < r1) load_stats(r + 1);
-        Piece<T, V> y[C], f[C], a[C], b[C];
         ring.wait();
-        ring.take(cols, Y, 0, y);
-        ring.take(cols, g.F, 1, f);
-        ring.take(cols, g.dY, 2, a);
-        ring.take(cols, g.dH, 3, b);
-        float s[N] = {};
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            if (!cols.in(j)) continue;
-            float yv[V], fv[V], av[V], bv[V];
-            y[j].values(yv), f[j].values(fv), a[j].values(av), b[j].values(bv);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = j * V + i;
-                const float y0 = MEAN ? yv[i] - my : yv[i], f0 = MEAN ? fv[i] - mf : fv[i];
-                const float e = bv[i] * wi[c], t = k[c] * f0;
-                s[0] = fmaf(e, y0, s[0]);
-                s[1] = fmaf(t, av[i], s[1]);
-                s[2] = fmaf(t, e, s[2]);
-                s[3] = fmaf(t, y0, s[3]);
-                if constexpr (MEAN) {
-                    s[4] += e;
-                    s[5] += t;
-                    s[6] = fmaf(k[c], av[i], s[6]);
-                    s[7] = fmaf(k[c], e, s[7]);
-                    s[8] = fmaf(k[c], y0, s[8]);
-                    s[9] += k[c];
-                }
+        float yv[P], fv[P], av[P], bv[P], s[N];
+        {
+            Piece<T, V> y[C], f[C], a[C], b[C];
+            ring.take(cols, has_h, slot, 0, y);
+            ring.take(cols, has_f, slot, 1, f);
+            ring.take(cols, has_y, slot, 2, a);
+            ring.take(cols, has_h, slot, 3, b);
+            values<T, V, C>(y, yv), values<T, V, C>(f, fv), values<T, V, C>(a, av), values<T, V, C>(b, bv);
+        }
+        if constexpr (MEAN) sub(yv, yv, my), sub(fv, fv, mf);
+        {
+            float e[P], t[P];
+            mul(e, bv, wi);
+            mul(t, k, fv);
+            s[0] = dot(e, yv), s[1] = dot(t, av), s[2] = dot(t, e), s[3] = dot(t, yv);
+            if constexpr (MEAN) {
+                const Same one{1.f};
+                s[4] = dot(one, e), s[5] = dot(one, t), s[6] = dot(k, av), s[7] = dot(k, e), s[8] = dot(k, yv), s[9] = dot(one, k);
             }
         }
-        worker_sums(s, w);
+        sums.give(s, w);
+        w.sync();
+        sums.take(s, w);
         const float c1 = ry * s[0] * g.each;
         float c0 = 0.f, d0 = 0.f, d1 = 0.f;
         if constexpr (MEAN) c0 = layer_in * s[4] * g.each;
@@ -464,41 +557,31 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
             }
             d1 = rf * (s[1] + ry * x) * g.each;
         }
-        const float by_y = -ry * c1, by_f = -rf * d1, shift_y = ry * c0, shift_f = rf * d0;
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            if (!cols.in(j)) continue;
-            float yv[V], fv[V], av[V], bv[V], dx[V], df[V];
-            y[j].values(yv), f[j].values(fv), a[j].values(av), b[j].values(bv);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = j * V + i;
-                const float yh = (MEAN ? yv[i] - my : yv[i]) * ry, fh = (MEAN ? fv[i] - mf : fv[i]) * rf;
-                float dy = fmaf(yh, by_y, fmaf(bv[i] * wi[c], ry, av[i]));
-                if constexpr (MEAN) dy -= shift_y;
-                float x = fmaf(fh, by_f, rf * (k[c] * dy));
-                if constexpr (MEAN) x -= shift_f;
-                dx[i] = dy;
-                df[i] = x;
-                A[c] = fmaf(dy, fh, A[c]);
-                CI[c] = fmaf(bv[i], yh, CI[c]);
-                if constexpr (MEAN) {
-                    B[c] += dy;
-                    D[c] += bv[i];
-                }
-            }
-            Piece<T, V> p;
-            if (g.dX != nullptr) {
-                p.set(dx);
-                p.store((T*)g.dX + at + j * w.threads * V);
-            }
-            if (g.dF != nullptr) {
-                p.set(df);
-                p.store((T*)g.dF + at + j * w.threads * V);
-            }
+        mul(yv, yv, Same{ry});
+        mul(fv, fv, Same{rf});
+        fma(CI, bv, yv, CI);
+        if constexpr (MEAN) fma(D, bv, Same{1.f}, D);
+        mul(bv, bv, wi);
+        fma(av, bv, Same{ry}, av);
+        fma(av, yv, Same{-ry * c1}, av);   // dy
+        if constexpr (MEAN) sub(av, av, ry * c0);
+        fma(A, av, fv, A);
+        if constexpr (MEAN) fma(B, av, Same{1.f}, B);
+        Piece<T, V> p[C];
+        if (gives_x) {
+            round_to<T, V, C>(av, p);
+            store_row<T>(cols, p, dX);
         }
-        ask(S);   // (the row's values are in registers)
-        at += g.width;
+        if (gives_f) {
+            mul(av, av, k);
+            mul(av, av, Same{rf});
+            fma(av, fv, Same{-rf * d1}, av);
+            if constexpr (MEAN) sub(av, av, rf * d0);
+            round_to<T, V, C>(av, p);
+            store_row<T>(cols, p, dF);
+        }
+        ask();   // (the row's values are in registers)
+        dX += g.width, dF += g.width;
     }
     if (by_range && live && (g.Gwo != nullptr || g.Gbo != nullptr || g.Ggate != nullptr)) flush(now.seg);
     // The block's sums over its rows.
@@ -599,16 +682,20 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(ResidualArgs 
     }
 }
 
-// How rows of `width` are shared out: pieces of v values, c of them a thread, `warps` a worker, `workers` a block.
+// How rows of `width` are shared out: pieces of v values, c of them a thread, `warps` a worker, `workers` a block; one block
+// an SM.  Going forward, 16 values a thread where a row has them: what a thread does once a row (its part of
+// two reductions, addresses) is a third of its instructions then (16,384 rows of 4,096 bfloat16 units: 88.7 us, 6.05 TB/s;
+// 98.5 us with 8).  Backward that would take more registers than 512 threads have, and half the threads are no faster
+// (143 us, 5.6 TB/s, with 8 values and 512 threads; the same with 16 and 256).
 struct Shape {
     int v, c, warps, workers;
 };
-Shape shape_of(int width, int size, bool pieces) {
+Shape shape_of(int width, int size, bool pieces, bool back) {
     Shape s;
     s.v = pieces ? 16 / size : 1;
     const int nv = (width + s.v - 1) / s.v;
     s.c = 1;
-    while ((nv + s.c - 1) / s.c > kMaxThreads) s.c *= 2;
+    while ((nv + s.c - 1) / s.c > (back ? kMaxThreads : kMaxThreads / 2) && s.c * s.v < 16) s.c *= 2;
     s.warps = ((nv + s.c - 1) / s.c + 31) / 32;
     s.workers = kMaxWarps / s.warps;
     return s;
@@ -630,13 +717,15 @@ struct Launch {
         const bool mean = a->norm_out == BP_NORM_LAYER || a->norm_in == BP_NORM_LAYER;
         const int threads = a->workers_a_block * a->worker_warps * 32, blocks = (a->workers + a->workers_a_block - 1) / a->workers_a_block;
         const int bytes = stages<T, V, C>(back) * (back ? 4 : 2) * C * V * (int)sizeof(T) * threads;
-        if (!back) {
-            if (mean) k_residual<T, V, C, true><<<blocks, threads, bytes, s>>>(*a);
-            else k_residual<T, V, C, false><<<blocks, threads, bytes, s>>>(*a);
-        } else if (mean) {
-            k_residual_backward<T, V, C, true><<<blocks, threads, bytes, s>>>(*a);
+        const bool norms = a->F != nullptr && a->norm_out != BP_NORM_NONE && a->norm_in != BP_NORM_NONE;
+        const bool full = V > 1 && norms && (back ? a->dY != nullptr && a->dH != nullptr && a->dX != nullptr && a->dF != nullptr : a->H != nullptr);
+        const auto go = [&](auto k) { k<<<blocks, threads, bytes, s>>>(*a); };
+        if (back) {
+            if (mean) full ? go(k_residual_backward<T, V, C, true, (V > 1)>) : go(k_residual_backward<T, V, C, true, false>);
+            else full ? go(k_residual_backward<T, V, C, false, (V > 1)>) : go(k_residual_backward<T, V, C, false, false>);
         } else {
-            k_residual_backward<T, V, C, false><<<blocks, threads, bytes, s>>>(*a);
+            if (mean) full ? go(k_residual<T, V, C, true, (V > 1)>) : go(k_residual<T, V, C, true, false>);
+            else full ? go(k_residual<T, V, C, false, (V > 1)>) : go(k_residual<T, V, C, false, false>);
         }
         return cudaGetLastError();
     }
@@ -647,10 +736,14 @@ struct Setup {
         const int out = stages<T, V, C>(false) * 2 * C * V * (int)sizeof(T) * kMaxThreads;
         const int back = stages<T, V, C>(true) * 4 * C * V * (int)sizeof(T) * kMaxThreads;
         const auto set = [](auto k, int bytes) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
-        cudaError_t e = set(k_residual<T, V, C, false>, out);
-        if (e == cudaSuccess) e = set(k_residual<T, V, C, true>, out);
-        if (e == cudaSuccess) e = set(k_residual_backward<T, V, C, false>, back);
-        return e != cudaSuccess ? e : set(k_residual_backward<T, V, C, true>, back);
+        cudaError_t e = cudaSuccess;
+        const auto both = [&](auto full, auto mean) {
+            if (e == cudaSuccess) e = set(k_residual<T, V, C, decltype(mean)::value, decltype(full)::value>, out);
+            if (e == cudaSuccess) e = set(k_residual_backward<T, V, C, decltype(mean)::value, decltype(full)::value>, back);
+        };
+        both(std::false_type{}, std::false_type{}), both(std::false_type{}, std::true_type{});
+        if constexpr (V > 1) both(std::true_type{}, std::false_type{}), both(std::true_type{}, std::true_type{});
+        return e;
     }
 };
 template <class F>
@@ -665,24 +758,27 @@ cudaError_t with_shape(const F& f, int dtype, const Shape& h) {
         default: return f.template shape<float, 1, 16>();
     }
 }
-Shape shape_of(const ResidualArgs& a) { return shape_of(a.width, a.dtype == BP_F32 ? 4 : 2, a.dtype == BP_BF16 || pieces16(a)); }
+Shape shape_of(const ResidualArgs& a, bool back) { return shape_of(a.width, a.dtype == BP_F32 ? 4 : 2, a.dtype == BP_BF16 || pieces16(a), back); }
 
 }  // namespace
 
 int residual_workers(int num_sms, int width, int dtype) {
-    const Shape s = shape_of(width, dtype == BP_F32 ? 4 : 2, true);
+    const Shape s = shape_of(width, dtype == BP_F32 ? 4 : 2, true, true);
     if (dtype == BP_BF16) return num_sms * s.workers;
-    return num_sms * max(s.workers, shape_of(width, 4, false).workers);   // a call's rows may be whole pieces or not
+    return num_sms * max(s.workers, shape_of(width, 4, false, true).workers);   // a call's rows may be whole pieces or not
 }
 
 cudaError_t residual_setup(int width, int dtype) {
-    const cudaError_t e = with_shape(Setup{}, dtype, shape_of(width, dtype == BP_F32 ? 4 : 2, dtype == BP_BF16 || width % 4 == 0));
-    return e != cudaSuccess || dtype == BP_BF16 ? e : with_shape(Setup{}, dtype, shape_of(width, 4, false));
+    const int size = dtype == BP_F32 ? 4 : 2;
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < 4 && e == cudaSuccess; ++i)   // rows in whole pieces or not, either direction
+        if ((i & 1) == 0 || dtype == BP_F32) e = with_shape(Setup{}, dtype, shape_of(width, size, (i & 1) == 0, i >= 2));
+    return e;
 }
 
 cudaError_t residual_forward(ResidualArgs a, cudaStream_t s) {
-    const Shape h = shape_of(a);
-    const int blocks = 2 * a.num_sms;
+    const Shape h = shape_of(a, false);
+    const int blocks = a.num_sms;
     a.worker_warps = h.warps;
     a.workers = min(a.n, blocks * h.workers);
     a.workers_a_block = (a.workers + blocks - 1) / blocks;
@@ -690,7 +786,7 @@ cudaError_t residual_forward(ResidualArgs a, cudaStream_t s) {
 }
 
 cudaError_t residual_backward(ResidualArgs a, cudaStream_t s) {
-    const Shape h = shape_of(a);
+    const Shape h = shape_of(a, true);
     a.worker_warps = h.warps;
     a.workers = min((a.n + kWorkerRows - 1) / kWorkerRows, a.num_sms * h.workers);
     a.workers_a_block = (a.workers + a.num_sms - 1) / a.num_sms;
