@@ -184,6 +184,7 @@ bp_status bp_scored_router_create(int n_experts, int k, int dtype, int max_patte
     r->a.scale = scale;
     const size_t blocks = ((size_t)max_patterns + kRoutePatterns - 1) / kRoutePatterns;
     st = cuda_status(cudaGetDevice(&r->device), call);
+    if (st == BP_OK) st = cuda_status(cudaDeviceGetAttribute(&r->a.num_sms, cudaDevAttrMultiProcessorCount, r->device), call);
     if (st == BP_OK) st = cuda_status(cudaMalloc(&r->a.r.hist, (blocks + 1) * n_experts * sizeof(int)), call);
     if (st != BP_OK) {
         delete r;

@@ -192,7 +192,8 @@ struct ScoredArgs {
     int E, scores, n_groups, open_groups, group_top, renormalise;
     float scale;
     const float* bias;      // [E] or NULL
-    int group_lanes, per;   // lanes of a group, experts of a lane (set by the launcher)
+    int num_sms;
+    int group_lanes, per, pieces;   // lanes of a group, experts of a lane, whether they are 16-byte pieces (set by the launcher)
 };
 cudaError_t route_scored_forward(ScoredArgs a, cudaStream_t s);
 cudaError_t route_scored_backward(const ScoredArgs& a, const float* dgate, void* dlogits, cudaStream_t s);

@@ -10,12 +10,12 @@ namespace {
 
 constexpr int kThreads = 256, kBackThreads = 256;
 constexpr int kOneBlock = 256;   // patterns of a call that one block takes
+constexpr float kNone = -INFINITY;
 
 // A warp takes a pattern: each group of experts has 32 / (groups, rounded up to a power of two) lanes, a lane
 // `per` consecutive experts of its group.  So the lowest index among equals is the first lane's first.
 struct Share {
     int first, count, group, group_lanes;
-    bool leads;   // the first lane of a group
 };
 __device__ __forceinline__ Share share_of(const ScoredArgs& g) {
     const int lane = threadIdx.x & 31, size = g.E / g.n_groups, sub = lane % g.group_lanes;
@@ -24,89 +24,111 @@ __device__ __forceinline__ Share share_of(const ScoredArgs& g) {
     s.group_lanes = g.group_lanes;
     s.first = s.group * size + sub * g.per;
     s.count = s.group < g.n_groups ? min(max(size - sub * g.per, 0), g.per) : 0;
-    s.leads = s.group < g.n_groups && sub == 0;
     return s;
 }
 
-using bp::order_of;
-__device__ __forceinline__ double order_value(unsigned long long o) {
-    return __longlong_as_double((long long)((o >> 63) ? (o & 0x7fffffffffffffffull) : ~o));
-}
-__device__ __forceinline__ unsigned long long order_of(double x) {
-    const unsigned long long u = (unsigned long long)__double_as_longlong(x + 0.0);
+// float64 values as whole numbers that ascend with them (the float64 unit is slow, 16 cycles a warp's operation,
+// comparisons too).
+using Order64 = unsigned long long;
+__device__ __forceinline__ Order64 order64(double x) {
+    const Order64 u = (Order64)__double_as_longlong(x + 0.0);   // (-0 and 0 are equal)
     if (!(x > -INFINITY)) return 0ull;
     return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
 }
-__device__ __forceinline__ float order_value(unsigned o) { return value_of(o); }
-__device__ __forceinline__ unsigned warp_most(unsigned x) { return __reduce_max_sync(0xffffffffu, x); }
-__device__ __forceinline__ unsigned long long warp_most(unsigned long long x) {
+__device__ __forceinline__ double value64(Order64 o) {
+    return __longlong_as_double((long long)((o >> 63) ? (o & 0x7fffffffffffffffull) : ~o));
+}
+// What is below every value: of an expert that is closed.
+template <class F>
+constexpr F kClosed = kNone;
+template <>
+constexpr Order64 kClosed<Order64> = 0ull;
+__device__ __forceinline__ float plus(float a, float b) { return a + b; }
+__device__ __forceinline__ Order64 plus(Order64 a, Order64 b) { return order64(value64(a) + value64(b)); }
+// The largest value of the warp.
+__device__ __forceinline__ float warp_max(float x) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ Order64 warp_max(Order64 x) {
     const unsigned hi = __reduce_max_sync(0xffffffffu, (unsigned)(x >> 32));
     const unsigned lo = __reduce_max_sync(0xffffffffu, (unsigned)(x >> 32) == hi ? (unsigned)x : 0u);
-    return ((unsigned long long)hi << 32) | lo;
+    return ((Order64)hi << 32) | lo;
 }
 
-// Closes the groups beyond the open ones of largest value.  With err > 0: whether two groups on either side
-// are nearer to one another than that.
-template <class F, class K, int PER>
-__device__ __forceinline__ bool close_groups(const ScoredArgs& g, const Share& s, K (&o)[PER], F err) {
-    F m1 = -INFINITY, m2 = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const F x = o[i] != 0 ? (F)order_value(o[i]) : (F)-INFINITY;
-        m2 = max(m2, min(m1, x));
-        m1 = max(m1, x);
+// A lane's two largest values and where they are, ties to the lowest index.
+template <class F, int PER>
+struct Best {
+    F v1, v2;
+    int at1, at2;
+    bool known2;   // v2 is the second largest (and not: was taken)
+    __device__ __forceinline__ void start() { v1 = v2 = kClosed<F>, at1 = at2 = 0, known2 = true; }
+    __device__ __forceinline__ void see(F x, int i) {
+        const bool first = x > v1, second = x > v2;
+        v2 = first ? v1 : second ? x : v2;
+        at2 = first ? at1 : second ? i : at2;
+        v1 = first ? x : v1;
+        at1 = first ? i : at1;
     }
+    __device__ __forceinline__ void scan(const F (&c)[PER]) {
+        start();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) see(c[i], i);
+    }
+    // Without the largest one.
+    __device__ __forceinline__ void pop(const F (&c)[PER]) {
+        if (known2) {
+            v1 = v2, at1 = at2, known2 = false;
+            return;
+        }
+        const F last = v1;
+        const int last_at = at1;
+        start();
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (c[i] < last || (c[i] == last && i > last_at)) see(c[i], i);
+    }
+};
+
+// What the lane's group is worth: its largest value, or the sum of its two largest.
+template <class F, int PER>
+__device__ __forceinline__ F group_worth(const ScoredArgs& g, const Share& s, const Best<F, PER>& b) {
+    F m1 = b.v1, m2 = b.v2;
     for (int d = 1; d < s.group_lanes; d <<= 1) {
         const F p1 = __shfl_xor_sync(0xffffffffu, m1, d), p2 = __shfl_xor_sync(0xffffffffu, m2, d);
         m2 = max(min(m1, p1), max(m2, p2));
         m1 = max(m1, p1);
     }
-    const F worth = g.group_top == 2 && m2 > (F)-INFINITY ? m1 + m2 : m1;   // (-infinity: a group with none open)
+    return g.group_top == 2 && m2 > kClosed<F> ? plus(m1, m2) : m1;   // (kClosed: a group with none open)
+}
+// Whether the lane's group is one of the open ones, those of largest worth, ties to the lowest index.  A group's lanes compare it
+// with some of the others each.
+template <class F>
+__device__ __forceinline__ bool group_stays(const ScoredArgs& g, const Share& s, F worth) {
+    const int sub = (threadIdx.x & 31) & (s.group_lanes - 1);
     int above = 0;
-    for (int h = 0; h < g.n_groups; ++h) {
-        const F w = __shfl_sync(0xffffffffu, worth, h * s.group_lanes);
-        above += w > worth || (w == worth && h < s.group);
+    for (int h0 = 0; h0 < g.n_groups; h0 += s.group_lanes) {
+        const int h = h0 + sub;
+        const F w = __shfl_sync(0xffffffffu, worth, (h * s.group_lanes) & 31);
+        above += h < g.n_groups && (w > worth || (w == worth && h < s.group));
     }
-    const bool stays = above < g.open_groups;
-    bool near = false;
-    if (err > (F)0) {
-        const K kept = warp_most(s.leads && stays ? ~order_of(worth) : (K)0);    // the least of those that stay
-        const K left = warp_most(s.leads && !stays ? order_of(worth) : (K)0);
-        near = left != 0 && !((F)order_value((K)~kept) - (F)order_value(left) > err);
-    }
-    if (!stays)
-#pragma unroll
-        for (int i = 0; i < PER; ++i) o[i] = 0;
-    return near;
+    for (int d = 1; d < s.group_lanes; d <<= 1) above += __shfl_xor_sync(0xffffffffu, above, d);
+    return above < g.open_groups;
 }
 
-// The `rounds` largest of the warp's values, ties to the lowest index: lane j gets the j-th one's expert (-1: none) and order.
-template <class K, int PER>
-__device__ __forceinline__ void take_largest(const Share& s, K (&o)[PER], int rounds, int& mine, K& order) {
+// The largest of the warp's values left, ties to the lowest index: lane j of [j0, j1) gets the expert (or keeps -1: none) and
+// value of the j-th one.
+template <class F, int PER>
+__device__ __forceinline__ void take_largest(const Share& s, const F (&c)[PER], Best<F, PER>& b, int j0, int j1, int& mine, F& value) {
     const int lane = threadIdx.x & 31;
-    mine = -1;
-    order = 0;
-    K best = 0;
-    int at = 0;
-    const auto again = [&] {
-        best = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (o[i] > best) best = o[i], at = i;
-    };
-    again();
-    for (int j = 0; j < rounds; ++j) {
-        const K most = warp_most(best);
-        if (most == 0) break;
-        const int owner = __ffs(__ballot_sync(0xffffffffu, best == most)) - 1;
-        const int e = __shfl_sync(0xffffffffu, s.first + at, owner);
-        if (lane == j) mine = e, order = most;
-        if (lane == owner) {
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (i == at) o[i] = 0;
-            again();
-        }
+    for (int j = j0; j < j1; ++j) {
+        const F most = warp_max(b.v1);
+        if (!(most > kClosed<F>)) break;
+        const int owner = __ffs(__ballot_sync(0xffffffffu, b.v1 == most)) - 1;
+        const int e = __shfl_sync(0xffffffffu, s.first + b.at1, owner);
+        if (lane == j) mine = e, value = most;
+        if (lane == owner) b.pop(c);
     }
 }
 
@@ -120,32 +142,39 @@ __device__ __forceinline__ double warp_sum64(double x) {
 template <class T, int PER>
 __device__ __noinline__ int choose64(const ScoredArgs& g, const T* z) {
     const Share s = share_of(g);
-    unsigned long long o[PER];
-    double v[PER], peak = -INFINITY;
+    const bool soft = g.scores == BP_SCORES_SOFTMAX;
+    float v[PER], peak = kNone;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        v[i] = i < s.count ? (double)to_f32(z[s.first + i]) : -INFINITY;
-        if (v[i] > peak) peak = v[i];
+        v[i] = i < s.count ? to_f32(z[s.first + i]) : kNone;
+        peak = fmaxf(peak, v[i]);   // (not a NaN's)
     }
-    double total = 1.0;
-    if (g.scores == BP_SCORES_SOFTMAX) {
-        peak = order_value(warp_most(order_of(peak)));   // (a pattern with an open expert: there is one)
+    double up[PER], total = 1.0;
+    if (soft) {
+        peak = warp_max(peak);   // (a number: a pattern that comes here has an open expert)
         total = 0.0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i) total += v[i] > -INFINITY ? (v[i] == peak ? 1.0 : exp(v[i] - peak)) : 0.0;
+        for (int i = 0; i < PER; ++i) {
+            up[i] = v[i] == peak ? 1.0 : v[i] > kNone ? exp((double)v[i] - (double)peak) : 0.0;
+            total += up[i];
+        }
         total = warp_sum64(total);
     }
+    Order64 c[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        o[i] = 0;
-        if (!(v[i] > -INFINITY)) continue;
-        const double p = g.scores == BP_SCORES_SOFTMAX ? (v[i] == peak ? 1.0 : exp(v[i] - peak)) / total : 1.0 / (1.0 + exp(-v[i]));
-        o[i] = order_of(g.bias != nullptr ? p + (double)g.bias[s.first + i] : p);
+        c[i] = 0ull;
+        if (!(v[i] > kNone)) continue;
+        double p = soft ? up[i] / total : 1.0 / (1.0 + exp(-(double)v[i]));
+        if (g.bias != nullptr) p += (double)g.bias[s.first + i];
+        c[i] = order64(p);
     }
-    if (g.n_groups > 1) close_groups<double>(g, s, o, 0.0);
-    int mine;
-    unsigned long long order;
-    take_largest(s, o, g.r.k, mine, order);
+    Best<Order64, PER> best;
+    best.scan(c);
+    if (g.n_groups > 1 && !group_stays(g, s, group_worth(g, s, best))) best.start();
+    int mine = -1;
+    Order64 value;
+    take_largest(s, c, best, 0, g.r.k, mine, value);
     return mine;
 }
 
@@ -164,13 +193,50 @@ __device__ __forceinline__ float share_of_chosen(const ScoredArgs& g, float z, b
     return live ? w / total : 0.f;
 }
 
+// e^x and 1 / x with the errors that k_route_scored counts.
+__device__ __forceinline__ float fast_exp(float x) {
+    float r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"(x * 1.4426950408889634f));
+    return r;
+}
+__device__ __forceinline__ float fast_reciprocal(float x) {
+    float r;
+    asm("rcp.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// A lane's logits, in 16-byte pieces where each lane has whole ones (`pieces`).
+template <class T, int PER>
+__device__ __forceinline__ void load_logits(const T* z, const Share& s, bool pieces, float (&v)[PER]) {
+    constexpr int V = 16 / (int)sizeof(T);
+    if constexpr (PER >= V) {
+        if (pieces) {
+#pragma unroll
+            for (int i = 0; i < PER; i += V) {
+                uint4 u = make_uint4(0u, 0u, 0u, 0u);
+                if (i < s.count) u = __ldg(reinterpret_cast<const uint4*>(z + s.first + i));
+                const unsigned w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float x = sizeof(T) == 4 ? __uint_as_float(w[j % 4]) : __uint_as_float((j & 1) ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+                    v[i + j] = i < s.count ? x : kNone;
+                }
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = i < s.count ? to_f32(z[s.first + i]) : kNone;
+}
+
 // A choice in float32, and again in float64 where two scores that it tells apart (or two groups) are nearer
-// than float32 can: the choice is that of float64 scores.  Errors of float32 scores: a sigmoid 2^-21 of itself
-// (expf 2 units, a sum and a quotient); a softmax 1e-5 of itself (its difference from the peak half a unit of up to 90,
-// 2^-17.5; a sum of 512 terms 2^-19), and nothing that matters below e^-90.
-template <class T, int PER, bool ONE>
-__global__ void __launch_bounds__(ONE ? (PER <= 8 ? 1024 : 512) : kThreads) k_route_scored(ScoredArgs g) {
-    constexpr int kBlock = ONE ? (PER <= 8 ? 1024 : 512) : kThreads;
+// than float32 can: the choice is that of float64 scores.  Errors of float32 scores, with x log2(e) half a unit off,
+// 2^x and a quotient two units each:  e^x is off by |x| 9e-8 + 3e-7 of itself, so that a sigmoid s is by
+// s (1 - s) (|x| 9e-8 + 3e-7) + s 3e-7, at most 5e-7, and of itself at most 1e-5 (|x| up to 88); a softmax 1e-5 of itself (its
+// difference from the peak is half a unit off too, |x| 6e-8, and a sum of 512 terms 2^-19).  Scores below e^-88 are
+// as good as none.
+template <class T, int PER, bool ONE, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 : 1) k_route_scored(ScoredArgs g) {
     constexpr int kPatterns = ONE ? kOneBlock : kRoutePatterns, kWords = kPatterns / 32;
     __shared__ unsigned bits[BP_MAX_EXPERTS * kWords];
     __shared__ int base[ONE ? BP_MAX_EXPERTS : 1];
@@ -178,72 +244,92 @@ __global__ void __launch_bounds__(ONE ? (PER <= 8 ? 1024 : 512) : kThreads) k_ro
     pdl_launch();
     const int p0 = blockIdx.x * kPatterns, np = min(kPatterns, g.r.n - p0), E = g.E;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < E * kWords; i += kBlock) bits[i] = 0u;
-    __syncthreads();
     const Share s = share_of(g);
     const bool soft = g.scores == BP_SCORES_SOFTMAX;
+    const T* z = (const T*)g.r.logits + (size_t)(p0 + warp) * E;
+    float v[PER];
+    if (warp < np) load_logits(z, s, g.pieces, v);
+    for (int i = threadIdx.x; i < E * kWords; i += THREADS) bits[i] = 0u;
     float b[PER], b_most = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        b[i] = g.bias != nullptr && i < s.count ? g.bias[s.first + i] : 0.f;
-        b_most = fmaxf(b_most, fabsf(b[i]));
+        b[i] = g.bias != nullptr && i < s.count ? __ldg(g.bias + s.first + i) : 0.f;
+        if (!(b[i] > kNone)) b[i] = kNone;   // (no bias of its own: closed)
+        else b_most = fmaxf(b_most, fabsf(b[i]));
     }
-    b_most = value_of(__reduce_max_sync(0xffffffffu, order_of(b_most)));
-    for (int p = warp; p < np; p += kBlock / 32) {
-        const T* z = (const T*)g.r.logits + (size_t)(p0 + p) * E;
-        float v[PER];
+    b_most = warp_max(b_most);
+    __syncthreads();
+    for (int p = warp; p < np; p += THREADS / 32) {
         bool nan = false;
+        float c[PER], peak = 0.f, total = 1.f, most = 1.f;   // most: the largest score, at most
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            v[i] = i < s.count ? to_f32(z[s.first + i]) : -INFINITY;
-            nan |= v[i] != v[i];
-        }
+        for (int i = 0; i < PER; ++i) nan |= v[i] != v[i];
         nan = __any_sync(0xffffffffu, nan);
-        unsigned o[PER];
-        float peak = 0.f, total = 1.f, most = 1.f;   // most: the largest score, at most
         if (soft) {
-            unsigned top = 0;
+            peak = v[0];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) top = max(top, order_of(v[i]));
-            peak = value_of(__reduce_max_sync(0xffffffffu, top));
+            for (int i = 1; i < PER; ++i) peak = fmaxf(peak, v[i]);   // (not a NaN's)
+            peak = warp_max(peak);
             total = 0.f;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                o[i] = __float_as_uint(v[i] == peak ? 1.f : v[i] > -INFINITY ? expf(v[i] - peak) : 0.f);
-                total += __uint_as_float(o[i]);
+                c[i] = v[i] == peak ? 1.f : fast_exp(v[i] - peak);
+                total += v[i] > kNone ? c[i] : 0.f;
             }
             total = warp_sum(total);
-            most = 1.f / total;
-        }
+            most = fast_reciprocal(total);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const float score = soft ? __uint_as_float(o[i]) / total : 1.f / (1.f + expf(-v[i]));
-            o[i] = v[i] > -INFINITY ? order_of(score + b[i]) : 0u;
+            for (int i = 0; i < PER; ++i) c[i] = v[i] > kNone ? fmaf(c[i], most, b[i]) : kNone;
+        } else {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) c[i] = v[i] > kNone ? fast_reciprocal(1.f + fast_exp(-v[i])) + b[i] : kNone;
         }
-        const float unit = soft ? 1e-5f : 5e-7f;
+        const float unit = soft ? 1e-5f : 5e-7f;   // (of `most`: of itself, 1e-5)
         const float err = unit * most + 1.2e-7f * (1.f + b_most);   // of any score and its bias
         bool near = false;
-        if (g.n_groups > 1) near = close_groups<float>(g, s, o, 6.f * err);
-        int mine;
-        unsigned order;
-        take_largest(s, o, g.r.k + 1, mine, order);
-        float logit = mine >= 0 ? to_f32(z[mine]) : -INFINITY;
-        {   // each choice against the next one; equal logits with equal biases are equal in float64 too
-            const float bias = mine >= 0 && g.bias != nullptr ? g.bias[mine] : 0.f;
-            const int next = __shfl_down_sync(0xffffffffu, mine, 1);
-            const unsigned next_order = __shfl_down_sync(0xffffffffu, order, 1);
+        Best<float, PER> best;
+        best.scan(c);
+        if (g.n_groups > 1) {
+            const float worth = group_worth(g, s, best);
+            const bool real = s.group < g.n_groups, stays = group_stays(g, s, worth);
+            const float kept = -warp_max(real && stays ? -worth : kNone), left = warp_max(real && !stays ? worth : kNone);
+            near = left > kNone && !(kept - left > 6.f * err);   // (a worth is off by 2 err, and by its sum's rounding)
+            if (!stays) best.start();
+        }
+        int mine = -1;
+        float value = kNone;
+        take_largest(s, c, best, 0, g.r.k + 1, mine, value);
+        // Whether the choice from the first `taken` values can be told: 1, 0, or -1 with more of them.  Equal logits with equal
+        // biases are equal in float64 too; where the last choice has such equals behind it, what comes after them
+        // has to be far enough away.
+        const auto told = [&](int taken) -> int {
+            const float next = __shfl_down_sync(0xffffffffu, value, 1);
+            const bool close = lane < taken - 1 && next > kNone &&
+                               !(value - next > (g.bias != nullptr ? 2.f * err : 2e-5f * value + 1e-36f));
+            if (!__any_sync(0xffffffffu, close)) return 1;
+            const float logit = mine >= 0 ? to_f32(z[mine]) : 0.f, bias = mine >= 0 && g.bias != nullptr ? __ldg(g.bias + mine) : 0.f;
             const float next_logit = __shfl_down_sync(0xffffffffu, logit, 1), next_bias = __shfl_down_sync(0xffffffffu, bias, 1);
-            if (lane < g.r.k && next >= 0 && !(logit == next_logit && bias == next_bias)) {
-                const float x = value_of(order);
-                near |= !(x - value_of(next_order) > (g.bias != nullptr ? 2.f * err : 2.f * unit * x + 1e-36f));
+            const bool same = logit == next_logit && bias == next_bias;
+            const unsigned last = 1u << (g.r.k - 1), unlike = __ballot_sync(0xffffffffu, close && !same);
+            const unsigned run = __ballot_sync(0xffffffffu, close && same) & ~(last - 1);   // of equals, from the last choice on
+            const unsigned behind = (run + last) & ~run;                                     // the first place that is not
+            if ((unlike & ((last - 1) | behind)) != 0) return 0;
+            return behind < 1u << (taken - 1) ? 1 : -1;
+        };
+        if (!near) {
+            int t = told(g.r.k + 1);
+            if (t < 0) {
+                take_largest(s, c, best, g.r.k + 1, g.r.k + 9, mine, value);
+                t = told(g.r.k + 9);
             }
+            near = t != 1;
         }
-        if (__any_sync(0xffffffffu, near)) {
-            mine = choose64<T, PER>(g, z);
-            logit = mine >= 0 ? to_f32(z[mine]) : -INFINITY;
-        }
+        if (near) mine = choose64<T, PER>(g, z);
         if (lane >= g.r.k) mine = -1;
         const bool live = mine >= 0;
+        const float logit = live ? to_f32(z[mine]) : kNone;
+        z += (size_t)(THREADS / 32) * E;
+        if (p + THREADS / 32 < np) load_logits(z, s, g.pieces, v);
         float gate;
         if (g.renormalise) gate = share_of_chosen(g, logit, live);
         else if (soft) gate = live ? (logit == peak ? 1.f : expf(logit - peak)) / total : 0.f;
@@ -257,14 +343,14 @@ __global__ void __launch_bounds__(ONE ? (PER <= 8 ? 1024 : 512) : kThreads) k_ro
     }
     __syncthreads();
     if constexpr (!ONE) {
-        for (int e = threadIdx.x; e < E; e += kBlock) g.r.hist[(size_t)e * (gridDim.x + 1) + blockIdx.x] = count_of<kWords>(bits, e);
+        for (int e = threadIdx.x; e < E; e += THREADS) g.r.hist[(size_t)e * (gridDim.x + 1) + blockIdx.x] = count_of<kWords>(bits, e);
     } else {
-        for (int e = threadIdx.x; e < E; e += kBlock) base[e] = count_of<kWords>(bits, e);
+        for (int e = threadIdx.x; e < E; e += THREADS) base[e] = count_of<kWords>(bits, e);
         __syncthreads();
         const int rows = block_scan(base, E, warp_tot);
-        for (int e = threadIdx.x; e < E; e += kBlock) g.r.offsets[e] = base[e];
+        for (int e = threadIdx.x; e < E; e += THREADS) g.r.offsets[e] = base[e];
         if (threadIdx.x == 0) g.r.offsets[E] = rows;
-        for (int i = rows + threadIdx.x; i < g.r.n * g.r.k; i += kBlock) g.r.source[i] = -1;
+        for (int i = rows + threadIdx.x; i < g.r.n * g.r.k; i += THREADS) g.r.source[i] = -1;
         place_rows<kWords>(g.r, bits, base, p0, np);
     }
 }
@@ -333,8 +419,10 @@ __global__ void __launch_bounds__(kBackThreads) k_route_scored_backward(ScoredAr
 
 template <class T, int PER>
 cudaError_t launch(const ScoredArgs& a, int blocks, cudaStream_t s) {
-    if (blocks == 1 && a.r.n <= kOneBlock) k_route_scored<T, PER, true><<<1, PER <= 8 ? 1024 : 512, 0, s>>>(a);
-    else k_route_scored<T, PER, false><<<blocks, kThreads, 0, s>>>(a);
+    constexpr int kMany = PER <= 8 ? 1024 : 512;
+    if (a.r.n <= kOneBlock) k_route_scored<T, PER, true, kMany><<<1, kMany, 0, s>>>(a);
+    else if (blocks <= a.num_sms) k_route_scored<T, PER, false, kMany><<<blocks, kMany, 0, s>>>(a);   // a pattern a warp
+    else k_route_scored<T, PER, false, kThreads><<<blocks, kThreads, 0, s>>>(a);
     return cudaGetLastError();
 }
 template <class T>
@@ -353,6 +441,8 @@ cudaError_t route_scored_forward(ScoredArgs a, cudaStream_t s) {
     a.group_lanes = 32;
     while (32 / a.group_lanes < a.n_groups) a.group_lanes /= 2;
     a.per = (a.E / a.n_groups + a.group_lanes - 1) / a.group_lanes;
+    const int size = a.r.dtype == BP_F32 ? 4 : 2, whole = 16 / size;   // rows of which every lane has whole 16-byte pieces, or none
+    a.pieces = a.per % whole == 0 && a.E / a.n_groups % whole == 0 && ((uintptr_t)a.r.logits & 15) == 0;
     const bool one = a.r.n <= kOneBlock;
     const int blocks = one ? 1 : (a.r.n + kRoutePatterns - 1) / kRoutePatterns;
     const cudaError_t e = a.r.dtype == BP_F32 ? launch<float>(a, blocks, s) : launch<__nv_bfloat16>(a, blocks, s);
