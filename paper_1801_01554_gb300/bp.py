@@ -343,15 +343,15 @@ def _typed(x, kind, what, n=0):
     """Device address of a tensor of element type `kind` (an index of _torch_types) with n values."""
     if x is None or type(x) is int:
         return x
-    if x.dtype is not _torch_types()[kind]:
-        raise ValueError(f"{what} must be {_torch_types()[kind]} (got {x.dtype})")
+    if x.dtype is (_dtypes or _torch_types())[kind] and x.is_cuda and x.numel() >= n and x.is_contiguous():
+        return x.data_ptr()
+    if x.dtype is not _dtypes[kind]:
+        raise ValueError(f"{what} must be {_dtypes[kind]} (got {x.dtype})")
     if x.numel() < n:
         raise ValueError(f"{what} holds {x.numel()} values; the call needs {n}")
     if not x.is_cuda:
         raise ValueError(f"{what} must be a CUDA tensor")
-    if not x.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    return x.data_ptr()
+    raise ValueError(f"{what} must be contiguous")
 
 
 def _values(x, dtype, what, n=0):
@@ -407,16 +407,16 @@ def bp_scored_router_destroy(h):
 
 
 def bp_route_scored(h, logits, bias, n, expert, gate, offsets, source, place, dtype=BP_F32, stream=None, room=_NO_ROOM):
-    _check(load().bp_route_scored(h, _values(logits, dtype, "logits", room[0]), _floats(bias, "bias", room[3]), n,
-                                  _ints(expert, "expert", room[1]), _floats(gate, "gate", room[1]),
-                                  _ints(offsets, "offsets", room[2]), _ints(source, "source", room[1]),
-                                  _ints(place, "place", room[1]), _stream(stream)))
+    _check(load().bp_route_scored(h, _typed(logits, dtype, "logits", room[0]), _typed(bias, 0, "bias", room[3]), n,
+                                  _typed(expert, 2, "expert", room[1]), _typed(gate, 0, "gate", room[1]),
+                                  _typed(offsets, 2, "offsets", room[2]), _typed(source, 2, "source", room[1]),
+                                  _typed(place, 2, "place", room[1]), _stream(stream)))
 
 
 def bp_route_scored_backward(h, logits, n, expert, dgate, dlogits, dtype=BP_F32, stream=None, room=_NO_ROOM):
-    _check(load().bp_route_scored_backward(h, _values(logits, dtype, "logits", room[0]), n,
-                                           _ints(expert, "expert", room[1]), _floats(dgate, "dgate", room[1]),
-                                           _values(dlogits, dtype, "dlogits", room[0]), _stream(stream)))
+    _check(load().bp_route_scored_backward(h, _typed(logits, dtype, "logits", room[0]), n,
+                                           _typed(expert, 2, "expert", room[1]), _typed(dgate, 0, "dgate", room[1]),
+                                           _typed(dlogits, dtype, "dlogits", room[0]), _stream(stream)))
 
 
 def bp_mix(H, n_rows, place, gate, n, k, n_out, dtype, Y, stream=None):
@@ -512,13 +512,13 @@ def bp_embedding_destroy(h):
 
 
 def bp_embed(h, table, ids, n, Y, scale=1.0, dtype=BP_F32, stream=None, room=_NO_ROOM):
-    _check(load().bp_embed(h, _values(table, dtype, "table", room[0]), _ints(ids, "ids", n), n, scale,
-                           _values(Y, dtype, "Y", room[1]), _stream(stream)))
+    _check(load().bp_embed(h, _typed(table, dtype, "table", room[0]), _typed(ids, 2, "ids", n), n, scale,
+                           _typed(Y, dtype, "Y", room[1]), _stream(stream)))
 
 
 def bp_embed_backward(h, ids, n, D, G, scale=1.0, accumulate=False, dtype=BP_F32, stream=None, room=_NO_ROOM):
-    _check(load().bp_embed_backward(h, _ints(ids, "ids", n), n, _values(D, dtype, "D", room[1]), scale,
-                                    _floats(G, "G", room[0]), 1 if accumulate else 0, _stream(stream)))
+    _check(load().bp_embed_backward(h, _typed(ids, 2, "ids", n), n, _typed(D, dtype, "D", room[1]), scale,
+                                    _typed(G, 0, "G", room[0]), 1 if accumulate else 0, _stream(stream)))
 
 
 def bp_embedding_check(h, stream=None):
@@ -540,21 +540,21 @@ def bp_residual_forward(h, X, F, n, wo, bo, gate, offsets, n_gates, scale, wi, b
                         room=_NO_ROOM):
     w = room[1]
     _check(load().bp_residual_forward(
-        h, _values(X, dtype, "X", room[0]), _values(F, dtype, "F", room[0]), n, _floats(wo, "wo", w), _floats(bo, "bo", w),
-        _floats(gate, "gate", n_gates * w), _ints(offsets, "offsets", n_gates + 1 if w else 0), n_gates, scale,
-        _floats(wi, "wi", w), _floats(bi, "bi", w), _values(Y, dtype, "Y", room[0]), _values(H, dtype, "H", room[0]),
-        _floats(stats, "stats", room[2]), _stream(stream)))
+        h, _typed(X, dtype, "X", room[0]), _typed(F, dtype, "F", room[0]), n, _typed(wo, 0, "wo", w), _typed(bo, 0, "bo", w),
+        _typed(gate, 0, "gate", n_gates * w), _typed(offsets, 2, "offsets", n_gates + 1 if w else 0), n_gates, scale,
+        _typed(wi, 0, "wi", w), _typed(bi, 0, "bi", w), _typed(Y, dtype, "Y", room[0]), _typed(H, dtype, "H", room[0]),
+        _typed(stats, 0, "stats", room[2]), _stream(stream)))
 
 
 def bp_residual_backward(h, Y, F, n, wo, bo, gate, offsets, n_gates, scale, wi, stats, dY, dH, dX, dF, Gwo, Gbo, Ggate, Gwi,
                          Gbi, accumulate=False, dtype=BP_F32, stream=None, room=_NO_ROOM):
     r, w = room[0], room[1]
     _check(load().bp_residual_backward(
-        h, _values(Y, dtype, "Y", r), _values(F, dtype, "F", r), n, _floats(wo, "wo", w), _floats(bo, "bo", w),
-        _floats(gate, "gate", n_gates * w), _ints(offsets, "offsets", n_gates + 1 if w else 0), n_gates, scale,
-        _floats(wi, "wi", w), _floats(stats, "stats", room[2]), _values(dY, dtype, "dY", r), _values(dH, dtype, "dH", r),
-        _values(dX, dtype, "dX", r), _values(dF, dtype, "dF", r), _floats(Gwo, "Gwo", w), _floats(Gbo, "Gbo", w),
-        _floats(Ggate, "Ggate", n_gates * w), _floats(Gwi, "Gwi", w), _floats(Gbi, "Gbi", w), 1 if accumulate else 0,
+        h, _typed(Y, dtype, "Y", r), _typed(F, dtype, "F", r), n, _typed(wo, 0, "wo", w), _typed(bo, 0, "bo", w),
+        _typed(gate, 0, "gate", n_gates * w), _typed(offsets, 2, "offsets", n_gates + 1 if w else 0), n_gates, scale,
+        _typed(wi, 0, "wi", w), _typed(stats, 0, "stats", room[2]), _typed(dY, dtype, "dY", r), _typed(dH, dtype, "dH", r),
+        _typed(dX, dtype, "dX", r), _typed(dF, dtype, "dF", r), _typed(Gwo, 0, "Gwo", w), _typed(Gbo, 0, "Gbo", w),
+        _typed(Ggate, 0, "Ggate", n_gates * w), _typed(Gwi, 0, "Gwi", w), _typed(Gbi, 0, "Gbi", w), 1 if accumulate else 0,
         _stream(stream)))
 
 
@@ -588,7 +588,7 @@ def bp_clip_destroy(h):
 
 
 def bp_clip_run(h, max_norm, norm=None, stream=None):
-    _check(load().bp_clip_run(h, max_norm, _floats(norm, "norm", 1), _stream(stream)))
+    _check(load().bp_clip_run(h, max_norm, _typed(norm, 0, "norm", 1), _stream(stream)))
 
 
 def bp_clip_check(h, stream=None):
