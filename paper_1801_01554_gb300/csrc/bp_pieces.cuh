@@ -64,5 +64,19 @@ __device__ __forceinline__ void store_floats(float* p, const float (&v)[V]) {
     }
 }
 
+// As another SM has just written them (from L2).
+template <int V>
+__device__ __forceinline__ void load_floats_l2(const float* p, float (&v)[V]) {
+    if constexpr (V == 1) {
+        v[0] = __ldcg(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(p + i));
+            v[i] = x.x, v[i + 1] = x.y, v[i + 2] = x.z, v[i + 3] = x.w;
+        }
+    }
+}
+
 }  // namespace
 }  // namespace bp
