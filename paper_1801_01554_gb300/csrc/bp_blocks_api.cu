@@ -15,8 +15,8 @@ using namespace bp;
 struct bp_embedding {
     int device = 0, n_tokens = 0, width = 0, dtype = BP_F32, cap = 0;
     int* flags = nullptr;
-    unsigned* keys = nullptr;   // [2, cap]
-    int* places = nullptr;      // [2, cap]
+    IdPlace* in_order = nullptr;   // [2, cap]
+    int sort_ctas = 1;
     float* partial = nullptr;
     unsigned* arrived = nullptr;
 };
@@ -81,9 +81,8 @@ bp_status bp_embedding_create(int n_tokens, int width, int dtype, int max_ids, b
     l->cap = max_ids;
     const size_t tiles = ((size_t)max_ids + kEmbedTile - 1) / kEmbedTile;
     st = make_flags(&l->device, &l->flags, call);
-    if (st == BP_OK) st = cuda_status(embed_setup(), call);
-    if (st == BP_OK) st = make_array(&l->keys, 2 * (size_t)max_ids, call);
-    if (st == BP_OK) st = make_array(&l->places, 2 * (size_t)max_ids, call);
+    if (st == BP_OK) st = cuda_status(embed_setup(&l->sort_ctas), call);
+    if (st == BP_OK) st = make_array(&l->in_order, 2 * (size_t)max_ids, call);
     if (st == BP_OK) st = make_array(&l->partial, 2 * tiles * width, call);
     if (st == BP_OK) st = make_counts(&l->arrived, embed_counts(max_ids, width, dtype), call);
     if (st == BP_OK) st = layer_ready(call);
@@ -99,8 +98,7 @@ void bp_embedding_destroy(bp_embedding* l) {
     if (l == nullptr) return;
     cudaDeviceSynchronize();
     cudaFree(l->flags);
-    cudaFree(l->keys);
-    cudaFree(l->places);
+    cudaFree(l->in_order);
     cudaFree(l->partial);
     cudaFree(l->arrived);
     delete l;
@@ -116,8 +114,8 @@ static bp_status check_embed(const char* call, const bp_embedding* l, int n, flo
 static EmbedArgs embed_args(const bp_embedding* l, const int* ids, int n, float scale) {
     EmbedArgs a{};
     a.n = n, a.n_tokens = l->n_tokens, a.width = l->width, a.dtype = l->dtype, a.ids = ids, a.scale = scale;
-    a.keys[0] = l->keys, a.keys[1] = l->keys + l->cap;
-    a.places[0] = l->places, a.places[1] = l->places + l->cap;
+    a.ids_in_order[0] = l->in_order, a.ids_in_order[1] = l->in_order + l->cap;
+    a.sort_ctas = l->sort_ctas;
     a.partial = l->partial, a.arrived = l->arrived, a.flags = l->flags;
     return a;
 }

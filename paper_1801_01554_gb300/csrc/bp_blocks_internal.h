@@ -10,6 +10,7 @@
 namespace bp {
 
 // ------------------------------------------------------------ embedding (bp_embed.cu)
+using IdPlace = unsigned long long;   // a token (above) and the place of its id
 struct EmbedArgs {
     int n, n_tokens, width, dtype;
     const int* ids;
@@ -19,16 +20,15 @@ struct EmbedArgs {
     const void* D;          // backward
     float* G;
     int accumulate;
-    // ids in order: two buffers of tokens and of the ids' places, as the passes need them (embed_passes)
-    unsigned* keys[2];
-    int* places[2];
+    IdPlace* ids_in_order[2];   // [n] each; a pass of the sort reads one and writes the other
+    int sort_ctas;
     float* partial;         // [2 * tiles, width] sums of pieces of long runs
     unsigned* arrived;      // a zero for every tile and slab, left zero
     int* flags;
 };
 constexpr int kEmbedTile = 32;   // sorted ids of a warp
 size_t embed_counts(int max_ids, int width, int dtype);   // of `arrived`
-cudaError_t embed_setup();
+cudaError_t embed_setup(int* sort_ctas);
 cudaError_t embed_forward(const EmbedArgs& a, cudaStream_t s);
 cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s);
 

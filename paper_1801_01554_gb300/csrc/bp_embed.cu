@@ -47,13 +47,15 @@ __global__ void __launch_bounds__(kThreads) k_embed(EmbedArgs g, int lanes, int 
 // A stable radix sort of (token, place) by one cluster, which takes two passes of up to nine bits for up to
 // 2^18 - 1 tokens, three beyond.  Each warp has a run of the ids; a pass counts every warp's digits in shared memory, adds the
 // counts up over the warps, the cluster's CTAs (distributed shared memory) and the digits, and moves each id behind
-// those before it.  The ids lie in L2 between passes, and in a warp's registers within one, up to kHold times 32 of
-// them.  No launch waits for another one's progress: the cluster's barrier is the hardware's.
+// those before it.  Up to kHold times 32 ids a warp stay in registers within a pass, and go out by way of the CTA's shared memory,
+// where they are put in order first: scattered words cost a CTA 32 cycles a warp's store, runs of them a few.  The ids lie in L2
+// between passes.  No launch waits for another one's progress: the cluster's barrier is the hardware's.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kMaxDigits = 512;
-constexpr int kSortCtas = 8;
+constexpr int kMostCtas = 16;
 constexpr int kSortAlone = 1024;   // ids that one CTA takes
 constexpr int kHold = 8;
+constexpr int kSortBytes = (kSortWarps + 3) * kMaxDigits * 4 + kSortWarps * kHold * 32 * 8;
 
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -74,14 +76,18 @@ __device__ __forceinline__ unsigned of_cta(const unsigned* p, int cta) {   // a 
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
     return v;
 }
+__device__ __forceinline__ unsigned key_of(IdPlace x) { return (unsigned)(x >> 32); }
+__device__ __forceinline__ int place_of(IdPlace x) { return (int)(unsigned)x; }
 
 __global__ void __launch_bounds__(kSortThreads) k_sort(EmbedArgs g, int passes, int bits) {
-    extern __shared__ unsigned sm[];
+    extern __shared__ __align__(16) IdPlace sorted[];   // [warps * kHold * 32] the CTA's ids in order
+    unsigned* const sm = reinterpret_cast<unsigned*>(sorted + kSortWarps * kHold * 32);
     const int D = 1 << bits;
     unsigned* total = sm;              // [D] of this CTA
-    unsigned* base = total + D;        // [D] where this CTA's ids of a digit go
-    unsigned* count = base + D;        // [warps, D]
-    __shared__ unsigned scan[kSortWarps];
+    unsigned* base = total + D;        // [D] where this CTA's ids of a digit go, less `own`
+    unsigned* own = base + D;          // [D] this CTA's ids of lower digits
+    unsigned* count = own + D;         // [warps, D]
+    __shared__ unsigned scan[2][kSortWarps];
     pdl_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ctas = cluster_size(), rank = cluster_rank();
     const int shares = ctas * kSortWarps, per = (int)(((long long)g.n + shares * 32 - 1) / (shares * 32)) * 32;
@@ -90,19 +96,17 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(EmbedArgs g, int passes, 
     const bool held = per <= kHold * 32;
     unsigned* mine = count + (size_t)warp * D;
     for (int pass = 0; pass < passes; ++pass) {
-        const unsigned* in = g.keys[(pass + 1) & 1];
-        const int* at = g.places[(pass + 1) & 1];
-        unsigned* out = g.keys[pass & 1];
-        int* to = g.places[pass & 1];
+        const IdPlace* in = g.ids_in_order[(pass + 1) & 1];
+        IdPlace* out = g.ids_in_order[pass & 1];
         const int shift = pass * bits;
-        const auto key_of = [&](int i) -> unsigned {
+        const auto load = [&](int i) -> IdPlace {
             if (pass > 0) return __ldcg(in + i);
             const int id = __ldg(g.ids + i);
-            if ((unsigned)id < (unsigned)g.n_tokens) return (unsigned)id;
+            if ((unsigned)id < (unsigned)g.n_tokens) return (IdPlace)(unsigned)id << 32 | (unsigned)i;
             if (id != -1) atomicOr(g.flags, kFlagBounds);
-            return (unsigned)g.n_tokens;   // behind every token
+            return (IdPlace)(unsigned)g.n_tokens << 32 | (unsigned)i;   // behind every token
         };
-        const auto place_of = [&](int i) { return pass > 0 ? __ldcg(at + i) : i; };
+        const auto digit = [&](IdPlace x) { return (key_of(x) >> shift) & (unsigned)(D - 1); };
         // How many ids of a lane's digit this warp has had before it; its ids are counted.
         const auto see = [&](unsigned d, bool live) -> unsigned {
             const unsigned peers = __match_any_sync(0xffffffffu, live ? d : 0xffffffffu);
@@ -112,14 +116,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(EmbedArgs g, int passes, 
             __syncwarp();
             return before + __popc(peers & ((1u << lane) - 1u));
         };
-        unsigned key[kHold], before[kHold];
-        int place[kHold];
+        IdPlace x[kHold];
+        unsigned before[kHold];
         if (held) {
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
                 const int i = lo + 32 * j + lane;
-                key[j] = i < hi ? key_of(i) : 0u;
-                place[j] = i < hi ? place_of(i) : 0;
+                x[j] = i < hi ? load(i) : 0ull;
             }
         }
         for (int i = threadIdx.x; i < kSortWarps * D; i += kSortThreads) count[i] = 0u;
@@ -128,72 +131,75 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(EmbedArgs g, int passes, 
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
                 before[j] = 0;
-                if (lo + 32 * j < hi) before[j] = see((key[j] >> shift) & (D - 1), lo + 32 * j + lane < hi);
+                if (lo + 32 * j < hi) before[j] = see(digit(x[j]), lo + 32 * j + lane < hi);
             }
         } else {
             for (int b = lo; b < hi; b += 32) {
                 const bool live = b + lane < hi;
-                see(live ? (key_of(b + lane) >> shift) & (D - 1) : 0u, live);
+                see(live ? digit(load(b + lane)) : 0u, live);
             }
         }
         __syncthreads();
+        unsigned of_own = 0, ahead = 0, all = 0;
         if (threadIdx.x < D) {
-            unsigned sum = 0;
             for (int w0 = 0; w0 < kSortWarps; w0 += 8) {
-                unsigned x[8];
+                unsigned c[8];
 #pragma unroll
-                for (int w = 0; w < 8; ++w) x[w] = count[(size_t)(w0 + w) * D + threadIdx.x];
+                for (int w = 0; w < 8; ++w) c[w] = count[(size_t)(w0 + w) * D + threadIdx.x];
 #pragma unroll
                 for (int w = 0; w < 8; ++w) {
-                    count[(size_t)(w0 + w) * D + threadIdx.x] = sum;
-                    sum += x[w];
+                    count[(size_t)(w0 + w) * D + threadIdx.x] = of_own;
+                    of_own += c[w];
                 }
             }
-            total[threadIdx.x] = sum;
+            total[threadIdx.x] = of_own;
         }
         cluster_sync();
-        unsigned ahead = 0, all = 0;
         if (threadIdx.x < D) {
-            unsigned x[kSortCtas];
+            unsigned c[kMostCtas];
 #pragma unroll
-            for (int c = 0; c < kSortCtas; ++c) x[c] = c < ctas ? of_cta(total + threadIdx.x, c) : 0u;
+            for (int r = 0; r < kMostCtas; ++r) c[r] = r < ctas ? of_cta(total + threadIdx.x, r) : 0u;
 #pragma unroll
-            for (int c = 0; c < kSortCtas; ++c) {
-                if (c < rank) ahead += x[c];
-                all += x[c];
+            for (int r = 0; r < kMostCtas; ++r) {
+                if (r < rank) ahead += c[r];
+                all += c[r];
             }
         }
-        unsigned s = all;   // digits below this one
+        unsigned s = all, t = of_own;   // digits up to this one
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const unsigned x = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += x;
+            const unsigned a = __shfl_up_sync(0xffffffffu, s, o), b = __shfl_up_sync(0xffffffffu, t, o);
+            if (lane >= o) s += a, t += b;
         }
-        if (lane == 31) scan[warp] = s;
+        if (lane == 31) scan[0][warp] = s, scan[1][warp] = t;
         __syncthreads();
         if (threadIdx.x < D) {
-            for (int w = 0; w < warp; ++w) ahead += scan[w];
-            base[threadIdx.x] = ahead + s - all;
+            for (int w = 0; w < warp; ++w) s += scan[0][w], t += scan[1][w];
+            own[threadIdx.x] = t - of_own;
+            base[threadIdx.x] = ahead + (s - all) - (t - of_own);
         }
         __syncthreads();
         if (held) {
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
                 if (lo + 32 * j + lane < hi) {
-                    const unsigned d = (key[j] >> shift) & (D - 1), r = base[d] + mine[d] + before[j];
-                    out[r] = key[j];
-                    to[r] = place[j];
+                    const unsigned d = digit(x[j]);
+                    sorted[own[d] + mine[d] + before[j]] = x[j];
                 }
+            }
+            __syncthreads();
+            const long long cta_first = (long long)rank * kSortWarps * per;
+            const int here = (int)(min(cta_first + (long long)kSortWarps * per, (long long)g.n) - min(cta_first, (long long)g.n));
+            for (int i = threadIdx.x; i < here; i += kSortThreads) {
+                const IdPlace y = sorted[i];
+                out[base[digit(y)] + i] = y;
             }
         } else {
             for (int b = lo; b < hi; b += 32) {   // (mine goes on from the ids of the warps before)
                 const bool live = b + lane < hi;
-                const unsigned key = live ? key_of(b + lane) : 0u, d = (key >> shift) & (D - 1);
-                const unsigned r = see(d, live) + (live ? base[d] : 0u);
-                if (live) {
-                    out[r] = key;
-                    to[r] = place_of(b + lane);
-                }
+                const IdPlace y = live ? load(b + lane) : 0ull;
+                const unsigned d = digit(y), r = see(d, live);
+                if (live) out[base[d] + own[d] + r] = y;
             }
         }
         cluster_sync();   // the ids are there for the next pass; no CTA leaves while another reads its counts
@@ -202,12 +208,12 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(EmbedArgs g, int passes, 
 
 // ------------------------------------------------------------ changes
 // keys[lo, hi) ascend: the first index whose key is at least k, by a converged warp.
-__device__ __forceinline__ int warp_lower_bound(const unsigned* keys, int lo, int hi, unsigned k) {
+__device__ __forceinline__ int warp_lower_bound(const IdPlace* keys, int lo, int hi, unsigned k) {
     const int lane = threadIdx.x & 31;
     while (lo < hi) {
         const int step = max(1, (int)(((long long)hi - lo + 31) / 32));
         const long long i = lo + (long long)(lane + 1) * step - 1;
-        const bool there = i >= hi || __ldg(keys + i) >= k;
+        const bool there = i >= hi || key_of(__ldg(keys + i)) >= k;
         const unsigned m = __ballot_sync(0xffffffffu, there);
         if (m == 0) return hi;
         const int f = __ffs(m) - 1;
@@ -227,8 +233,7 @@ constexpr int kZeroTokens = 16;   // tokens of a warp that writes zeros
 // last adds them in order, so that sums do not depend on which that is.  Further warps write the zeros of
 // tokens without ids.  Bound by reading D once and writing G once.
 template <class T, int V>
-__global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const unsigned* keys, const int* places, long long sum_warps,
-                                                         int slabs) {
+__global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const IdPlace* keys, long long sum_warps, int slabs) {
     const int lane = threadIdx.x & 31;
     const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
     pdl_wait();
@@ -243,10 +248,10 @@ __global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const unsi
             int lo = 0, hi = n;
             while (lo < hi) {
                 const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
-                if (__ldg(keys + mid) < t) lo = mid + 1;
+                if (key_of(__ldg(keys + mid)) < t) lo = mid + 1;
                 else hi = mid;
             }
-            absent = lo >= n || __ldg(keys + lo) != t;
+            absent = lo >= n || key_of(__ldg(keys + lo)) != t;
         }
         unsigned m = __ballot_sync(0xffffffffu, absent);
         while (m != 0) {
@@ -263,11 +268,10 @@ __global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const unsi
     constexpr unsigned kNone = 0xffffffffu;
     const int tile = (int)(w / slabs), slab = (int)(w % slabs), t0 = tile * kEmbedTile;
     const unsigned tokens = (unsigned)g.n_tokens;
-    const unsigned kp = tile > 0 ? __ldg(keys + t0 - 32 + lane) : kNone;
-    const unsigned kc = t0 + lane < n ? __ldg(keys + t0 + lane) : kNone;
-    const unsigned kn = t0 + 32 + lane < n ? __ldg(keys + t0 + 32 + lane) : kNone;
-    const int pc = t0 + lane < n ? __ldg(places + t0 + lane) : 0;
-    const int pn = t0 + 32 + lane < n ? __ldg(places + t0 + 32 + lane) : 0;
+    const auto at = [&](int i) { return i < n ? __ldg(keys + i) : (IdPlace)kNone << 32; };
+    const IdPlace here = at(t0 + lane), after = at(t0 + 32 + lane);
+    const unsigned kp = tile > 0 ? key_of(at(t0 - 32 + lane)) : kNone, kc = key_of(here), kn = key_of(after);
+    const int pc = place_of(here), pn = place_of(after);
     const unsigned first = __shfl_sync(0xffffffffu, kc, 0), last = __shfl_sync(0xffffffffu, kc, 31);
     if (first >= tokens) return;   // ids of no token, behind all others
     // the rows [a, b) of this tile (from 32 on: the next one's); long runs at its ends
@@ -498,8 +502,7 @@ cudaError_t sums(const EmbedArgs& a, int passes, cudaStream_t s) {
     const long long blocks = (sum_warps + zero_warps + kWarps - 1) / kWarps;
     if (blocks == 0) return cudaSuccess;
     const int at = (passes - 1) & 1;
-    return launch_pdl(k_embed_sums<T, V>, (int)blocks, 1, kThreads, 0, s, a, (const unsigned*)a.keys[at], (const int*)a.places[at],
-                      sum_warps, slabs);
+    return launch_pdl(k_embed_sums<T, V>, (int)blocks, 1, kThreads, 0, s, a, (const IdPlace*)a.ids_in_order[at], sum_warps, slabs);
 }
 
 bool pieces16(const void* a, const void* b, int width) { return (((uintptr_t)a | (uintptr_t)b) & 15) == 0 && width % 4 == 0; }
@@ -511,8 +514,34 @@ size_t embed_counts(int max_ids, int width, int dtype) {
     return ((size_t)max_ids + kEmbedTile - 1) / kEmbedTile * ((width + slab - 1) / slab);
 }
 
-cudaError_t embed_setup() {
-    return cudaFuncSetAttribute(k_sort, cudaFuncAttributeMaxDynamicSharedMemorySize, (kSortWarps + 2) * kMaxDigits * (int)sizeof(unsigned));
+namespace {
+cudaLaunchConfig_t sort_config(int ctas, cudaLaunchAttribute* at, cudaStream_t s) {
+    at->id = cudaLaunchAttributeClusterDimension;
+    at->val.clusterDim.x = ctas;
+    at->val.clusterDim.y = at->val.clusterDim.z = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(ctas);
+    c.blockDim = dim3(kSortThreads);
+    c.dynamicSmemBytes = kSortBytes;
+    c.stream = s;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return c;
+}
+}  // namespace
+
+// The CTAs of a cluster that sorts: 16 where the device has room for them, else the 8 that any has.
+cudaError_t embed_setup(int* sort_ctas) {
+    cudaError_t e = cudaFuncSetAttribute(k_sort, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortBytes);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_sort, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute at;
+    const cudaLaunchConfig_t c = sort_config(kMostCtas, &at, nullptr);
+    int clusters = 0;
+    e = cudaOccupancyMaxActiveClusters(&clusters, k_sort, &c);
+    *sort_ctas = e == cudaSuccess && clusters > 0 ? kMostCtas : 8;
+    if (e != cudaSuccess) cudaGetLastError();
+    return cudaSuccess;
 }
 
 cudaError_t embed_forward(const EmbedArgs& a, cudaStream_t s) {
@@ -528,17 +557,8 @@ cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s) {
     int passes = 1;
     const int bits = sort_bits(a.n_tokens, passes);
     if (a.n > 0) {
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = a.n <= kSortAlone ? 1 : kSortCtas;
-        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-        cudaLaunchConfig_t c{};
-        c.gridDim = dim3(at[0].val.clusterDim.x);
-        c.blockDim = dim3(kSortThreads);
-        c.dynamicSmemBytes = (size_t)(kSortWarps + 2) * (1u << bits) * sizeof(unsigned);
-        c.stream = s;
-        c.attrs = at;
-        c.numAttrs = 1;
+        cudaLaunchAttribute at;
+        const cudaLaunchConfig_t c = sort_config(a.n <= kSortAlone ? 1 : a.sort_ctas, &at, s);
         const cudaError_t e = cudaLaunchKernelEx(&c, k_sort, a, passes, bits);
         if (e != cudaSuccess) return e;
     }
