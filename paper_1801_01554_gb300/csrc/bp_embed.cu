@@ -224,16 +224,16 @@ __device__ __forceinline__ int warp_lower_bound(const IdPlace* keys, int lo, int
     return lo;
 }
 
-constexpr int kBatch = 8;         // rows under way
 constexpr int kZeroTokens = 16;   // tokens of a warp that writes zeros
 
-// A warp takes kEmbedTile sorted ids and 32 pieces of their rows, and adds up runs of equal tokens in registers.
+// A warp takes kEmbedTile sorted ids and 32 C pieces of their rows (two a lane for bfloat16: 40,001 rows of 1,024 units in 46 us,
+// 48 with one), and adds up runs of equal tokens in registers.
 // A run of at most kEmbedTile ids is summed by the tile that it starts in, also past that tile's end, and is stored at
 // once.  A longer one is cut at the tiles' ends: its pieces go to scratch, and the warp whose piece comes
 // last adds them in order, so that sums do not depend on which that is.  Further warps write the zeros of
 // tokens without ids.  Bound by reading D once and writing G once.
-template <class T, int V>
-__global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const IdPlace* keys, long long sum_warps, int slabs) {
+template <class T, int V, int C>
+__global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const IdPlace* keys, long long sum_warps, int slabs) {
     const int lane = threadIdx.x & 31;
     const long long w = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
     pdl_wait();
@@ -294,29 +294,36 @@ __global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const IdPl
             b = 32 + __ffs(~more) - 1;   // (at most 31 more)
         }
     }
-    const int c0 = (slab * 32 + lane) * V;
-    const bool in_row = c0 < N;
+    constexpr int B = 8 / C;                     // rows, and pieces of a run, under way
+    const int c0 = (slab * 32 * C + lane) * V;   // and every 32 V columns on
+    bool in[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) in[c] = c0 + c * 32 * V < N;
     const T* D = (const T*)g.D + c0;
-    float acc[V] = {};
+    float acc[C][V] = {};
     const auto write = [&](unsigned token) {
-        if (!in_row) return;
         float* p = g.G + (size_t)token * N + c0;
-        float v[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = acc[i] * g.scale;
-        if (g.accumulate) {
-            float x[V];
-            load_floats_l2<V>(p, x);
+        for (int c = 0; c < C; ++c) {
+            if (!in[c]) continue;
+            float v[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] += x[i];
+            for (int i = 0; i < V; ++i) v[i] = acc[c][i] * g.scale;
+            if (g.accumulate) {
+                float x[V];
+                load_floats_l2<V>(p + c * 32 * V, x);
+#pragma unroll
+                for (int i = 0; i < V; ++i) v[i] += x[i];
+            }
+            store_floats<V>(p + c * 32 * V, v);
         }
-        store_floats<V>(p, v);
     };
     // A piece of a long run: to its slot, and all of the run's pieces to G if it is the last one.
     const auto join = [&](unsigned token, int slot) {
-        if (in_row) {
-            store_floats<V>(g.partial + (size_t)slot * N + c0, acc);
-        }
+        const auto piece_of = [&](int at, int c) { return g.partial + (size_t)at * N + c0 + c * 32 * V; };
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if (in[c]) store_floats<V>(piece_of(slot, c), acc[c]);
         const int s = warp_lower_bound(keys, 0, min(t0 + 32, n), token), e = warp_lower_bound(keys, t0, n, token + 1);
         const int from = s / kEmbedTile, to = (e - 1) / kEmbedTile;
         __threadfence();
@@ -330,32 +337,39 @@ __global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const IdPl
         mine = __shfl_sync(0xffffffffu, mine, 0);
         if (mine != (unsigned)(to - from)) return;
         __threadfence();
-        if (!in_row) return;
-        load_floats_l2<V>(g.partial + (size_t)(2 * from + 1) * N + c0, acc);
-        for (int t = from + 1; t <= to; t += kBatch) {
-            float x[kBatch][V] = {};
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j)
-                if (t + j <= to) load_floats_l2<V>(g.partial + (size_t)(2 * (t + j)) * N + c0, x[j]);
+        for (int c = 0; c < C; ++c)
+            if (in[c]) load_floats_l2<V>(piece_of(2 * from + 1, c), acc[c]);
+        for (int t = from + 1; t <= to; t += B) {
+            float x[B][C][V] = {};
 #pragma unroll
-            for (int j = 0; j < kBatch; ++j)
+            for (int j = 0; j < B; ++j)
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] += x[j][i];
+                for (int c = 0; c < C; ++c)
+                    if (t + j <= to && in[c]) load_floats_l2<V>(piece_of(2 * (t + j), c), x[j][c]);
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) acc[c][i] += x[j][c][i];
         }
         write(token);
     };
     unsigned now = kNone;
     const auto row_key = [&](int r) { return r < 32 ? __shfl_sync(0xffffffffu, kc, r) : __shfl_sync(0xffffffffu, kn, r & 31); };
     const auto row_place = [&](int r) { return r < 32 ? __shfl_sync(0xffffffffu, pc, r) : __shfl_sync(0xffffffffu, pn, r & 31); };
-    for (int r0 = a; r0 < b; r0 += kBatch) {
-        Piece<T, V> x[kBatch];
+    for (int r0 = a; r0 < b; r0 += B) {
+        Piece<T, V> x[B][C];
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
+        for (int j = 0; j < B; ++j) {
             const int p = row_place(min(r0 + j, b - 1));
-            if (in_row) x[j].load(D + (size_t)p * N);
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+                if (in[c]) x[j][c].load(D + (size_t)p * N + c * 32 * V);
         }
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
+        for (int j = 0; j < B; ++j) {
             const int r = r0 + j;
             if (r >= b) break;
             const unsigned k = row_key(r);
@@ -366,13 +380,17 @@ __global__ void __launch_bounds__(kThreads) k_embed_sums(EmbedArgs g, const IdPl
                 }
                 now = k;
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] = 0.f;
-            }
-            if (in_row) {
-                float v[V];
-                x[j].values(v);
+                for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] += v[i];
+                    for (int i = 0; i < V; ++i) acc[c][i] = 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (!in[c]) continue;
+                float v[V];
+                x[j][c].values(v);
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[c][i] += v[i];
             }
         }
     }
@@ -494,15 +512,15 @@ cudaError_t lookup(const EmbedArgs& a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-template <class T, int V>
+template <class T, int V, int C>
 cudaError_t sums(const EmbedArgs& a, int passes, cudaStream_t s) {
-    const int tiles = (a.n + kEmbedTile - 1) / kEmbedTile, slabs = (a.width + 32 * V - 1) / (32 * V);
+    const int tiles = (a.n + kEmbedTile - 1) / kEmbedTile, slabs = (a.width + 32 * V * C - 1) / (32 * V * C);
     const long long sum_warps = (long long)tiles * slabs;
     const long long zero_warps = a.accumulate ? 0 : (a.n_tokens + kZeroTokens - 1) / kZeroTokens;
     const long long blocks = (sum_warps + zero_warps + kWarps - 1) / kWarps;
     if (blocks == 0) return cudaSuccess;
     const int at = (passes - 1) & 1;
-    return launch_pdl(k_embed_sums<T, V>, (int)blocks, 1, kThreads, 0, s, a, (const IdPlace*)a.ids_in_order[at], sum_warps, slabs);
+    return launch_pdl(k_embed_sums<T, V, C>, (int)blocks, 1, kThreads, 0, s, a, (const IdPlace*)a.ids_in_order[at], sum_warps, slabs);
 }
 
 bool pieces16(const void* a, const void* b, int width) { return (((uintptr_t)a | (uintptr_t)b) & 15) == 0 && width % 4 == 0; }
@@ -562,8 +580,8 @@ cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s) {
         const cudaError_t e = cudaLaunchKernelEx(&c, k_sort, a, passes, bits);
         if (e != cudaSuccess) return e;
     }
-    if (a.dtype == BP_BF16) return sums<__nv_bfloat16, 8>(a, passes, s);
-    return pieces ? sums<float, 4>(a, passes, s) : sums<float, 1>(a, passes, s);
+    if (a.dtype == BP_BF16) return sums<__nv_bfloat16, 8, 2>(a, passes, s);
+    return pieces ? sums<float, 4, 1>(a, passes, s) : sums<float, 1, 1>(a, passes, s);
 }
 
 }  // namespace bp
