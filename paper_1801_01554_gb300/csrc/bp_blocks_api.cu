@@ -31,6 +31,7 @@ struct bp_clip {
     ClipArgs a{};
     int device = 0, num_sms = 1;
     ClipChunk* chunks = nullptr;
+    ClipFew few{};
 };
 
 namespace {
@@ -370,12 +371,14 @@ bp_status bp_clip_create(const void* const* h_in, void* const* h_out, const int6
         l->a.in_place = in_place;
         st = make_flags(&l->device, &l->a.flags, call);
         if (st == BP_OK) st = cuda_status(cudaDeviceGetAttribute(&l->num_sms, cudaDevAttrMultiProcessorCount, l->device), call);
+        if (st == BP_OK) st = cuda_status(clip_setup(l->a.n_chunks, chunk == kClipTile, &l->a.few), call);
         if (st == BP_OK) st = make_array(&l->chunks, chunks.size(), call);
         if (st == BP_OK) st = make_array(&l->a.partial, (size_t)clip_blocks(l->num_sms), call);
         if (st == BP_OK && !chunks.empty())
             st = cuda_status(cudaMemcpy(l->chunks, chunks.data(), chunks.size() * sizeof(ClipChunk), cudaMemcpyHostToDevice), call);
         if (st == BP_OK) st = layer_ready(call);
         l->a.chunks = l->chunks;
+        for (size_t i = 0; i < chunks.size() && i < kClipFew; ++i) l->few.chunks[i] = chunks[i];
     } catch (const std::bad_alloc&) {
         st = fail(BP_ENOMEM, "%s: out of memory", call);
     }
@@ -405,7 +408,7 @@ bp_status bp_clip_run(bp_clip* l, float max_norm, float* d_norm, void* stream) {
     if (st != BP_OK) return st;
     ClipArgs a = l->a;
     a.max_norm = max_norm, a.norm = d_norm, a.write = std::isfinite(max_norm);
-    return cuda_status(clip_run(a, l->num_sms, (cudaStream_t)stream), call);
+    return cuda_status(clip_run(a, l->few, l->num_sms, (cudaStream_t)stream), call);
 }
 
 bp_status bp_clip_check(bp_clip* l, void* stream) {

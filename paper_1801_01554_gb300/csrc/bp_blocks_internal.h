@@ -66,9 +66,14 @@ struct ClipChunk {
     unsigned count;
     int dtype;
 };
+constexpr int kClipFew = 16;
+struct ClipFew {
+    ClipChunk chunks[kClipFew];   // where there are no more: they go with the launch
+};
 struct ClipArgs {
     const ClipChunk* chunks;   // of the tensors, in order
     int n_chunks, in_place;    // in_place: every output is its input
+    int few;                   // (clip_setup)
     int write;                 // 0: the norm alone
     float max_norm;
     float* norm;               // or NULL
@@ -77,6 +82,7 @@ struct ClipArgs {
 };
 constexpr int kClipTile = 8192;   // values that a block takes at a time
 int clip_blocks(int num_sms);
-cudaError_t clip_run(const ClipArgs& a, int num_sms, cudaStream_t s);
+cudaError_t clip_setup(int n_chunks, bool tiles, int* few);   // tiles: no chunk has more than a tile, and less than 16 bytes before it
+cudaError_t clip_run(const ClipArgs& a, const ClipFew& few, int num_sms, cudaStream_t s);
 
 }  // namespace bp

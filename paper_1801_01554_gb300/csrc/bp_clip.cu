@@ -137,17 +137,30 @@ __global__ void __launch_bounds__(kThreads) k_clip_norm(ClipArgs g) {
     if (threadIdx.x == 0) g.partial[blockIdx.x] = sum;
 }
 
-// What the values are multiplied by, the same in every block: 1 where nothing is clipped.
+// What the values are multiplied by, the same in every block: 1 where nothing is clipped.  The root is float32's, of the sum
+// times an even power of two (float64's root and quotient take some 2 us).
 __device__ __forceinline__ float clip_factor(const ClipArgs& g, double total) {
-    const double norm = sqrt(total);
-    const bool finite = norm <= 1.7e308;
+    const bool finite = total <= 1.7e308;   // (not a NaN)
+    const int half = total > 0.0 && finite ? (((__double2hiint(total) >> 20) & 0x7ff) - 1023) >> 1 : 0;
+    // total * 4^-half lies in [1, 4): a normal number, as sums of squares are none or at least 2^-298
+    const double m = __hiloint2double(__double2hiint(total) - (half << 21), __double2loint(total));
+    const float root = finite ? sqrtf((float)(total > 0.0 ? m : 0.0)) : (float)total, norm = ldexpf(root, half);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
-        if (g.norm != nullptr) *g.norm = (float)norm;
+        if (g.norm != nullptr) *g.norm = norm;
         if (!finite) atomicOr(g.flags, kFlagNonfinite);
     }
-    return finite && norm > (double)g.max_norm ? (float)((double)g.max_norm / norm) : 1.f;
+    return finite && norm > g.max_norm ? ldexpf(g.max_norm / root, -half) : 1.f;
 }
 
+__device__ __forceinline__ void scale(const ClipArgs& g, int i, float by) {
+    const ClipChunk c = g.chunks[i];
+    if (by == 1.f && c.in == c.out) return;
+    if (c.dtype == BP_BF16) scale_chunk<__nv_bfloat16>(c, by);
+    else scale_chunk<float>(c, by);
+}
+
+// Bound by reading the values again and writing them.  (Of 1 GB that the norm has read L2 keeps nothing to speak of: the same time
+// from the last chunk to the first.)
 __global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs g, int blocks) {
     __shared__ double part[kWarps];
     pdl_wait();
@@ -155,19 +168,118 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs g, int blocks)
     for (int i = threadIdx.x; i < blocks; i += kThreads) sum += __ldcg(g.partial + i);
     const float by = clip_factor(g, block_sum(sum, part));
     if (!g.write || (by == 1.f && g.in_place)) return;
-    for (int i = blockIdx.x; i < g.n_chunks; i += gridDim.x) {
-        const ClipChunk c = g.chunks[i];
-        if (by == 1.f && c.in == c.out) continue;
-        if (c.dtype == BP_BF16) scale_chunk<__nv_bfloat16>(c, by);
-        else scale_chunk<float>(c, by);
+    for (int i = blockIdx.x; i < g.n_chunks; i += gridDim.x) scale(g, i, by);
+}
+
+// Few chunks: one launch of one cluster, a CTA a chunk, whose values stay in registers while the CTAs read one
+// another's sums.
+constexpr int kFewCtas = kClipFew;
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <class T>
+__device__ __forceinline__ void clip_chunk(const ClipArgs& g, const ClipChunk& c, double* part, double* mine) {
+    constexpr int V = Split<T>::V, J = kValues / V;
+    const Split<T> s(c);
+    const T* body = s.in + s.head;
+    T* out = (T*)c.out;
+    const bool whole = (((uintptr_t)c.in ^ (uintptr_t)c.out) & 15) == 0, edge = (int)threadIdx.x < s.head + s.tail;
+    const long long edge_at = (int)threadIdx.x < s.head ? (long long)threadIdx.x : s.pieces * V + (long long)threadIdx.x;
+    Piece<T, V> p[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const long long at = j * kThreads + threadIdx.x;
+        p[j].u = make_uint4(0u, 0u, 0u, 0u);
+        if (at < s.pieces) p[j].load_rw(body + at * V);
     }
+    const float e[1] = {edge ? to_f32(s.in[edge_at]) : 0.f};
+    float v[J * V];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        float x[V];
+        p[j].values(x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[j * V + i] = x[i];
+    }
+    const double sum = block_sum(squares(v) + squares(e), part);
+    if (threadIdx.x == 0) *mine = sum;
+    cluster_sync();
+    double sums[kFewCtas], total = 0.0;
+#pragma unroll
+    for (int r = 0; r < kFewCtas; ++r) {
+        unsigned a;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(mine)), "r"(r));
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(sums[r]) : "r"(a) : "memory");
+    }
+#pragma unroll
+    for (int r = 0; r < kFewCtas; ++r) total += sums[r];
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // this CTA has read the sums
+    const float by = clip_factor(g, total);
+    if (g.write && !(by == 1.f && c.in == c.out)) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const long long at = j * kThreads + threadIdx.x;
+            if (at >= s.pieces) continue;
+            float x[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = v[j * V + i] * by;
+            T* to = out + s.head + at * V;
+            if (whole) {
+                p[j].set(x);
+                p[j].store(to);
+            } else {
+#pragma unroll
+                for (int i = 0; i < V; ++i) to[i] = from_f32<T>(x[i]);
+            }
+        }
+        if (edge) out[edge_at] = from_f32<T>(e[0] * by);
+    }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");   // no CTA leaves while another reads its sum
+}
+__global__ void __launch_bounds__(kThreads) k_clip_few(ClipArgs g, __grid_constant__ const ClipFew few) {
+    __shared__ double part[kWarps];
+    __shared__ double mine;
+    const ClipChunk c = few.chunks[blockIdx.x];   // (empty ones behind the last)
+    if (c.dtype == BP_BF16) clip_chunk<__nv_bfloat16>(g, c, part, &mine);
+    else clip_chunk<float>(g, c, part, &mine);
+}
+
+cudaLaunchConfig_t few_config(cudaLaunchAttribute* at, cudaStream_t s) {
+    at->id = cudaLaunchAttributeClusterDimension;
+    at->val.clusterDim.x = kFewCtas;
+    at->val.clusterDim.y = at->val.clusterDim.z = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(kFewCtas);
+    c.blockDim = dim3(kThreads);
+    c.stream = s;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return c;
 }
 
 }  // namespace
 
+// Whether the device holds a cluster of kFewCtas, so that calls of as many chunks, of a tile at most, go to k_clip_few.
+cudaError_t clip_setup(int n_chunks, bool tiles, int* few) {
+    *few = 0;
+    cudaError_t e = cudaFuncSetAttribute(k_clip_few, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess || n_chunks > kFewCtas || !tiles) return e;
+    cudaLaunchAttribute at;
+    const cudaLaunchConfig_t c = few_config(&at, nullptr);
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, k_clip_few, &c) == cudaSuccess) *few = clusters > 0;
+    else cudaGetLastError();
+    return cudaSuccess;
+}
+
 int clip_blocks(int num_sms) { return num_sms * kBlocksPerSm; }
 
-cudaError_t clip_run(const ClipArgs& a, int num_sms, cudaStream_t s) {
+cudaError_t clip_run(const ClipArgs& a, const ClipFew& few, int num_sms, cudaStream_t s) {
+    if (a.few) {
+        cudaLaunchAttribute at;
+        const cudaLaunchConfig_t c = few_config(&at, s);
+        return cudaLaunchKernelEx(&c, k_clip_few, a, few);
+    }
     const int blocks = max(1, min(a.n_chunks, clip_blocks(num_sms)));
     k_clip_norm<<<blocks, kThreads, 0, s>>>(a);
     const cudaError_t e = cudaGetLastError();
