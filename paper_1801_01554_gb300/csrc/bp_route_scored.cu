@@ -92,9 +92,8 @@ struct Best {
 };
 
 // What the lane's group is worth: its largest value, or the sum of its two largest.
-template <class F, int PER>
-__device__ __forceinline__ F group_worth(const ScoredArgs& g, const Share& s, const Best<F, PER>& b) {
-    F m1 = b.v1, m2 = b.v2;
+template <class F>
+__device__ __forceinline__ F group_worth(const ScoredArgs& g, const Share& s, F m1, F m2) {   // a lane's two largest
     for (int d = 1; d < s.group_lanes; d <<= 1) {
         const F p1 = __shfl_xor_sync(0xffffffffu, m1, d), p2 = __shfl_xor_sync(0xffffffffu, m2, d);
         m2 = max(min(m1, p1), max(m2, p2));
@@ -171,7 +170,7 @@ __device__ __noinline__ int choose64(const ScoredArgs& g, const T* z) {
     }
     Best<Order64, PER> best;
     best.scan(c);
-    if (g.n_groups > 1 && !group_stays(g, s, group_worth(g, s, best))) best.start();
+    if (g.n_groups > 1 && !group_stays(g, s, group_worth(g, s, best.v1, best.v2))) best.start();
     int mine = -1;
     Order64 value;
     take_largest(s, c, best, 0, g.r.k, mine, value);
@@ -241,6 +240,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 :
     __shared__ unsigned bits[BP_MAX_EXPERTS * kWords];
     __shared__ int base[ONE ? BP_MAX_EXPERTS : 1];
     __shared__ int warp_tot[32];
+    __shared__ float2 lists[THREADS / 32][32];   // a warp's values and experts
     pdl_launch();
     const int p0 = blockIdx.x * kPatterns, np = min(kPatterns, g.r.n - p0), E = g.E;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -286,43 +286,86 @@ __global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 :
         }
         const float unit = soft ? 1e-5f : 5e-7f;   // (of `most`: of itself, 1e-5)
         const float err = unit * most + 1.2e-7f * (1.f + b_most);   // of any score and its bias
-        bool near = false;
-        Best<float, PER> best;
-        best.scan(c);
-        if (g.n_groups > 1) {
-            const float worth = group_worth(g, s, best);
-            const bool real = s.group < g.n_groups, stays = group_stays(g, s, worth);
-            const float kept = -warp_max(real && stays ? -worth : kNone), left = warp_max(real && !stays ? worth : kNone);
-            near = left > kNone && !(kept - left > 6.f * err);   // (a worth is off by 2 err, and by its sum's rounding)
-            if (!stays) best.start();
+        bool near = false, open = true;
+        float m1 = c[0], m2 = kNone;   // the lane's two largest
+#pragma unroll
+        for (int i = 1; i < PER; ++i) {
+            m2 = fmaxf(m2, fminf(m1, c[i]));
+            m1 = fmaxf(m1, c[i]);
         }
+        if (g.n_groups > 1) {
+            const float worth = group_worth(g, s, m1, m2);
+            const bool real = s.group < g.n_groups;
+            open = group_stays(g, s, worth);
+            const float kept = -warp_max(real && open ? -worth : kNone), left = warp_max(real && !open ? worth : kNone);
+            near = left > kNone && !(kept - left > 6.f * err);   // (a worth is off by 2 err, and by its sum's rounding)
+            if (!open) m1 = kNone;
+        }
+        // The values from the (k + 1)-th largest lane's largest on: as many as are wanted, and few more.  They go to a lane
+        // each, in the experts' order, and from there to the place that they have by size.
+        float least = kNone;
+        {
+            float t = m1;
+            for (int j = 0; j <= g.r.k; ++j) {
+                least = warp_max(t);
+                if (!(least > kNone)) break;
+                t = t == least ? kNone : t;
+            }
+        }
+        unsigned found = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) found |= open && c[i] > kNone && c[i] >= least ? 1u << i : 0u;
+        int upto = __popc(found);
+        const int own = upto;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        int taken = __shfl_sync(0xffffffffu, upto, 31);   // entries of the list
+        bool whole = !(least > kNone);                     // there are no others
         int mine = -1;
         float value = kNone;
-        take_largest(s, c, best, 0, g.r.k + 1, mine, value);
-        // Whether the choice from the first `taken` values can be told: 1, 0, or -1 with more of them.  Equal logits with equal
-        // biases are equal in float64 too; where the last choice has such equals behind it, what comes after them
-        // has to be far enough away.
-        const auto told = [&](int taken) -> int {
+        if (taken <= 32) {
+            int at = upto - own;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (found >> i & 1) lists[warp][at++] = make_float2(c[i], __int_as_float(s.first + i));
+            __syncwarp();
+            const float2 entry = lane < taken ? lists[warp][lane] : make_float2(kNone, 0.f);
+            int place = 0;
+            for (int j = 0; j < taken; ++j) {
+                const float x = __shfl_sync(0xffffffffu, entry.x, j);
+                place += x > entry.x || (x == entry.x && j < lane);
+            }
+            __syncwarp();
+            if (lane < taken) lists[warp][place] = entry;
+            __syncwarp();
+            if (lane < taken) value = lists[warp][lane].x, mine = __float_as_int(lists[warp][lane].y);
+            __syncwarp();
+        } else {   // more of them: one after another
+            Best<float, PER> best;
+            best.scan(c);
+            if (!open) best.start();
+            taken = g.r.k + 9;
+            whole = false;
+            take_largest(s, c, best, 0, taken, mine, value);
+        }
+        // Whether the choice can be told from the list.  Equal logits with equal biases are equal in float64 too; where
+        // the last choice has such equals behind it, what comes after them has to be far enough away.
+        if (!near) {
             const float next = __shfl_down_sync(0xffffffffu, value, 1);
             const bool close = lane < taken - 1 && next > kNone &&
                                !(value - next > (g.bias != nullptr ? 2.f * err : 2e-5f * value + 1e-36f));
-            if (!__any_sync(0xffffffffu, close)) return 1;
-            const float logit = mine >= 0 ? to_f32(z[mine]) : 0.f, bias = mine >= 0 && g.bias != nullptr ? __ldg(g.bias + mine) : 0.f;
-            const float next_logit = __shfl_down_sync(0xffffffffu, logit, 1), next_bias = __shfl_down_sync(0xffffffffu, bias, 1);
-            const bool same = logit == next_logit && bias == next_bias;
-            const unsigned last = 1u << (g.r.k - 1), unlike = __ballot_sync(0xffffffffu, close && !same);
-            const unsigned run = __ballot_sync(0xffffffffu, close && same) & ~(last - 1);   // of equals, from the last choice on
-            const unsigned behind = (run + last) & ~run;                                     // the first place that is not
-            if ((unlike & ((last - 1) | behind)) != 0) return 0;
-            return behind < 1u << (taken - 1) ? 1 : -1;
-        };
-        if (!near) {
-            int t = told(g.r.k + 1);
-            if (t < 0) {
-                take_largest(s, c, best, g.r.k + 1, g.r.k + 9, mine, value);
-                t = told(g.r.k + 9);
+            if (__any_sync(0xffffffffu, close)) {
+                const float logit = mine >= 0 ? to_f32(z[mine]) : 0.f, bias = mine >= 0 && g.bias != nullptr ? __ldg(g.bias + mine) : 0.f;
+                const float next_logit = __shfl_down_sync(0xffffffffu, logit, 1), next_bias = __shfl_down_sync(0xffffffffu, bias, 1);
+                const bool same = logit == next_logit && bias == next_bias;
+                const unsigned last = 1u << (g.r.k - 1), unlike = __ballot_sync(0xffffffffu, close && !same);
+                const unsigned run = __ballot_sync(0xffffffffu, close && same) & ~(last - 1);   // of equals, from the last choice on
+                const unsigned behind = (run + last) & ~run;                                     // the first place that is not
+                near = (unlike & ((last - 1) | behind)) != 0 || (!whole && behind >= 1u << (taken - 1));
             }
-            near = t != 1;
         }
         if (near) mine = choose64<T, PER>(g, z);
         if (lane >= g.r.k) mine = -1;
