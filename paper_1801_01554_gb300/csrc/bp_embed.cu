@@ -401,11 +401,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
 }
 
 // Few ids of few tokens: a block a token and slab of columns, which looks the ids through for its own, in order, and shares
-// out their rows to its warps, 32 rows a sum and the sums in order.  One launch, no order of all ids; the ids
-// are read once a block.
+// out their rows to its warps, 32 rows a sum and the sums in order.  One launch, no order of all ids.
 constexpr int kFewThreads = 1024, kFewWarps = kFewThreads / 32;
 constexpr int kFewIds = 4096, kFewChunks = kFewIds / kFewThreads;   // of a call; of a warp, 32 at a time
-constexpr long long kFewReads = 1 << 22;                            // blocks times ids
+constexpr long long kFewBlocks = 256;                               // of a call: as many as run at a time
 
 template <class T, int V>
 __global__ void __launch_bounds__(kFewThreads) k_embed_few(EmbedArgs g) {
@@ -483,7 +482,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(EmbedArgs g) {
     }
 }
 // Whether a call is for it: measured beside the sort at 3,584 ids of 29 tokens and 15 units, 7 us of 27.
-bool is_few(const EmbedArgs& a, int slabs) { return a.n <= kFewIds && (long long)a.n_tokens * slabs * max(a.n, 256) <= kFewReads; }
+bool is_few(const EmbedArgs& a, int slabs) { return a.n <= kFewIds && (long long)a.n_tokens * slabs <= kFewBlocks; }
 
 template <class T, int V>
 bool few(const EmbedArgs& a, cudaStream_t s, cudaError_t& e) {
@@ -492,6 +491,153 @@ bool few(const EmbedArgs& a, cudaStream_t s, cudaError_t& e) {
     k_embed_few<T, V><<<dim3(a.n_tokens, slabs), kFewThreads, 0, s>>>(a);
     e = cudaGetLastError();
     return true;
+}
+
+// Few ids of many tokens: zeros everywhere first, then a block an id, which looks all ids through for its token.  The block
+// of every 32nd id of a token (the first one, mostly the only one, among them) adds up the rows of it and the 31 behind it;
+// more than 32 are joined as pieces, as in k_embed_sums, in the slots that the ids' order would give them.
+constexpr int kScanIds = 4096;
+
+__global__ void __launch_bounds__(kThreads) k_zero(float* G, long long n) {
+    pdl_launch();
+    const long long i = (long long)blockIdx.x * kThreads + threadIdx.x, all = (long long)gridDim.x * kThreads;
+    if (((uintptr_t)G & 15) == 0) {
+        for (long long j = i; j < n / 4; j += all) reinterpret_cast<float4*>(G)[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < n % 4) G[n / 4 * 4 + i] = 0.f;
+    } else {
+        for (long long j = i; j < n; j += all) G[j] = 0.f;
+    }
+}
+
+template <class T, int V>
+__global__ void __launch_bounds__(kThreads) k_embed_scan(EmbedArgs g, int slabs) {
+    constexpr int kEach = kScanIds / kThreads, B = 8;   // ids of a thread; rows, and pieces, under way
+    __shared__ int list[kEmbedTile];
+    __shared__ unsigned of_warp[3][kWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = g.n, N = g.width, i = blockIdx.x;
+    const int token = __ldg(g.ids + i);
+    if ((unsigned)token >= (unsigned)g.n_tokens) {
+        if (token != -1 && threadIdx.x == 0) atomicOr(g.flags, kFlagBounds);
+        pdl_wait();   // (no block is gone before the zeros are there: the stream goes on behind this kernel)
+        return;
+    }
+    // A warp takes a run of the ids, 32 at a time: of this token, before this id; of lower tokens.
+    const int chunks = (n + kThreads - 1) / kThreads, first = warp * chunks * 32;
+    unsigned same[kEach], all = 0, before = 0, lower = 0;
+    int id[kEach];
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        const int at = first + j * 32 + lane;
+        id[j] = j < chunks && at < n ? __ldg(g.ids + at) : -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+        same[j] = __ballot_sync(0xffffffffu, id[j] == token);
+        all += __popc(same[j]);
+        const int left = i - (first + j * 32);   // ids of the 32 that come before this one
+        before += __popc(same[j] & (left <= 0 ? 0u : left >= 32 ? 0xffffffffu : (1u << left) - 1u));
+        lower += (unsigned)id[j] < (unsigned)token;
+    }
+    lower = __reduce_add_sync(0xffffffffu, lower);
+    if (lane == 0) of_warp[0][warp] = all, of_warp[1][warp] = before, of_warp[2][warp] = lower;
+    __syncthreads();
+    unsigned at = 0;   // the token's ids of the warps before
+    all = before = lower = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) at += of_warp[0][w];
+        all += of_warp[0][w];
+        before += of_warp[1][w];
+        lower += of_warp[2][w];
+    }
+    if (before % kEmbedTile != 0) {
+        pdl_wait();
+        return;
+    }
+    const int rows = (int)min(all - before, (unsigned)kEmbedTile);
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {   // the places of the rows
+        const unsigned rank = at + __popc(same[j] & ((1u << lane) - 1u)) - before;
+        if ((same[j] >> lane & 1) && rank < (unsigned)kEmbedTile) list[rank] = first + j * 32 + lane;
+        at += __popc(same[j]);
+    }
+    __syncthreads();
+    pdl_wait();
+    for (int slab = warp; slab < slabs; slab += kWarps) {
+        const int c0 = (slab * 32 + lane) * V;
+        const bool in_row = c0 < N;
+        const T* D = (const T*)g.D + c0;
+        float acc[V] = {};
+        for (int r0 = 0; r0 < rows; r0 += B) {
+            Piece<T, V> x[B];
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+                if (in_row && r0 + j < rows) x[j].load(D + (size_t)list[r0 + j] * N);
+#pragma unroll
+            for (int j = 0; j < B; ++j) {
+                if (!in_row || r0 + j >= rows) break;
+                float v[V];
+                x[j].values(v);
+#pragma unroll
+                for (int c = 0; c < V; ++c) acc[c] += v[c];
+            }
+        }
+        if (all > kEmbedTile) {
+            const int pieces = (int)(all + kEmbedTile - 1) / kEmbedTile, from = (int)lower / kEmbedTile;
+            const auto piece_of = [&](int p) { return g.partial + (size_t)(p == 0 ? 2 * from + 1 : 2 * (((int)lower + p * kEmbedTile) / kEmbedTile)) * N + c0; };
+            if (in_row) store_floats<V>(piece_of((int)before / kEmbedTile), acc);
+            __threadfence();
+            __syncwarp();
+            unsigned mine = 0;
+            if (lane == 0) {
+                unsigned* arrived = g.arrived + (size_t)from * slabs + slab;
+                mine = atomicAdd(arrived, 1u);
+                if (mine == (unsigned)pieces - 1) *arrived = 0;   // for the next call
+            }
+            mine = __shfl_sync(0xffffffffu, mine, 0);
+            if (mine != (unsigned)pieces - 1) continue;
+            __threadfence();
+            if (in_row) {
+                load_floats_l2<V>(piece_of(0), acc);
+                for (int p = 1; p < pieces; p += B) {
+                    float x[B][V] = {};
+#pragma unroll
+                    for (int j = 0; j < B; ++j)
+                        if (p + j < pieces) load_floats_l2<V>(piece_of(p + j), x[j]);
+#pragma unroll
+                    for (int j = 0; j < B; ++j)
+#pragma unroll
+                        for (int c = 0; c < V; ++c) acc[c] += x[j][c];
+                }
+            }
+        }
+        if (in_row) {
+            float* to = g.G + (size_t)token * N + c0;
+#pragma unroll
+            for (int c = 0; c < V; ++c) acc[c] *= g.scale;
+            if (g.accumulate) {
+                float x[V];
+                load_floats_l2<V>(to, x);
+#pragma unroll
+                for (int c = 0; c < V; ++c) acc[c] += x[c];
+            }
+            store_floats<V>(to, acc);
+        }
+    }
+}
+
+template <class T, int V>
+cudaError_t scan(const EmbedArgs& a, cudaStream_t s) {
+    if (!a.accumulate) {
+        const long long values = (long long)a.n_tokens * a.width, blocks = (values / 4 + kThreads - 1) / kThreads;
+        k_zero<<<(unsigned)max(1ll, min(blocks, 2048ll)), kThreads, 0, s>>>(a.G, values);
+        const cudaError_t e = cudaGetLastError();
+        if (e != cudaSuccess) return e;
+    }
+    const int slabs = (a.width + 32 * V - 1) / (32 * V);
+    if (!a.accumulate) return launch_pdl(k_embed_scan<T, V>, a.n, 1, kThreads, 0, s, a, slabs);
+    k_embed_scan<T, V><<<a.n, kThreads, 0, s>>>(a, slabs);
+    return cudaGetLastError();
 }
 
 int sort_bits(int n_tokens, int& passes) {
@@ -572,6 +718,8 @@ cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s) {
     cudaError_t few_status = cudaSuccess;
     if (a.dtype == BP_BF16 ? few<__nv_bfloat16, 8>(a, s, few_status) : pieces ? few<float, 4>(a, s, few_status) : few<float, 1>(a, s, few_status))
         return few_status;
+    if (a.n > 0 && a.n <= kScanIds)
+        return a.dtype == BP_BF16 ? scan<__nv_bfloat16, 8>(a, s) : pieces ? scan<float, 4>(a, s) : scan<float, 1>(a, s);
     int passes = 1;
     const int bits = sort_bits(a.n_tokens, passes);
     if (a.n > 0) {
