@@ -207,21 +207,35 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(EmbedArgs g, int passes, 
 }
 
 // ------------------------------------------------------------ changes
-// keys[lo, hi) ascend: the first index whose key is at least k, by a converged warp.
-__device__ __forceinline__ int warp_lower_bound(const IdPlace* keys, int lo, int hi, unsigned k) {
+// keys[0, n) ascend: the first indexes whose keys are at least k1 and k2, by a converged warp.
+__device__ __forceinline__ void warp_lower_bounds(const IdPlace* keys, int n, unsigned k1, unsigned k2, int& first, int& second) {
     const int lane = threadIdx.x & 31;
-    while (lo < hi) {
-        const int step = max(1, (int)(((long long)hi - lo + 31) / 32));
-        const long long i = lo + (long long)(lane + 1) * step - 1;
-        const bool there = i >= hi || key_of(__ldg(keys + i)) >= k;
-        const unsigned m = __ballot_sync(0xffffffffu, there);
-        if (m == 0) return hi;
-        const int f = __ffs(m) - 1;
-        const long long at = lo + (long long)(f + 1) * step - 1;
-        lo += f * step;
-        hi = (int)min((long long)hi, at);
+    int lo[2] = {0, 0}, hi[2] = {n, n};
+    const unsigned k[2] = {k1, k2};
+    while (lo[0] < hi[0] || lo[1] < hi[1]) {
+        unsigned key[2];
+        int step[2];
+        long long at[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            step[i] = max(1, (int)(((long long)hi[i] - lo[i] + 31) / 32));
+            at[i] = lo[i] + (long long)(lane + 1) * step[i] - 1;
+            key[i] = at[i] < hi[i] ? key_of(__ldg(keys + at[i])) : 0xffffffffu;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned m = __ballot_sync(0xffffffffu, at[i] >= hi[i] || key[i] >= k[i]);
+            if (lo[i] >= hi[i]) continue;
+            if (m == 0) {
+                lo[i] = hi[i];
+                continue;
+            }
+            const int f = __ffs(m) - 1;
+            hi[i] = (int)min((long long)hi[i], lo[i] + (long long)(f + 1) * step[i] - 1);
+            lo[i] += f * step[i];
+        }
     }
-    return lo;
+    first = lo[0], second = lo[1];
 }
 
 constexpr int kZeroTokens = 16;   // tokens of a warp that writes zeros
@@ -242,18 +256,28 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
         if (g.accumulate) return;
         const long long t0 = (w - sum_warps) * kZeroTokens;
         if (t0 >= g.n_tokens) return;
-        bool absent = false;
-        if (lane < kZeroTokens && t0 + lane < g.n_tokens) {
-            const unsigned t = (unsigned)(t0 + lane);
-            int lo = 0, hi = n;
-            while (lo < hi) {
-                const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
-                if (key_of(__ldg(keys + mid)) < t) lo = mid + 1;
-                else hi = mid;
+        const int last = (int)min(t0 + kZeroTokens, (long long)g.n_tokens);
+        int at, end;
+        warp_lower_bounds(keys, n, (unsigned)t0, (unsigned)last, at, end);
+        unsigned m = 0;   // tokens that have ids
+        if (end - at <= 128) {
+            for (; at < end; at += 32)
+                m |= __reduce_or_sync(0xffffffffu, at + lane < end ? 1u << (key_of(__ldg(keys + at + lane)) - (unsigned)t0) : 0u);
+        } else {
+            bool there = false;
+            if (t0 + lane < last) {
+                const unsigned t = (unsigned)(t0 + lane);
+                int lo = at, hi = end;
+                while (lo < hi) {
+                    const int mid = (int)(((unsigned)lo + (unsigned)hi) >> 1);
+                    if (key_of(__ldg(keys + mid)) < t) lo = mid + 1;
+                    else hi = mid;
+                }
+                there = lo < end && key_of(__ldg(keys + lo)) == t;
             }
-            absent = lo >= n || key_of(__ldg(keys + lo)) != t;
+            m = __ballot_sync(0xffffffffu, there);
         }
-        unsigned m = __ballot_sync(0xffffffffu, absent);
+        m = ~m & ((1u << (last - (int)t0)) - 1u);
         while (m != 0) {
             float* row = g.G + (size_t)(t0 + __ffs(m) - 1) * N;
             m &= m - 1;
@@ -294,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
             b = 32 + __ffs(~more) - 1;   // (at most 31 more)
         }
     }
-    constexpr int B = 8 / C;                     // rows, and pieces of a run, under way
+    constexpr int B = C > 1 ? 4 : 16, J = 4;     // rows, and pieces of a run, under way
     const int c0 = (slab * 32 * C + lane) * V;   // and every 32 V columns on
     bool in[C];
 #pragma unroll
@@ -324,7 +348,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (in[c]) store_floats<V>(piece_of(slot, c), acc[c]);
-        const int s = warp_lower_bound(keys, 0, min(t0 + 32, n), token), e = warp_lower_bound(keys, t0, n, token + 1);
+        int s, e;
+        warp_lower_bounds(keys, n, token, token + 1, s, e);
         const int from = s / kEmbedTile, to = (e - 1) / kEmbedTile;
         __threadfence();
         __syncwarp();
@@ -340,15 +365,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
 #pragma unroll
         for (int c = 0; c < C; ++c)
             if (in[c]) load_floats_l2<V>(piece_of(2 * from + 1, c), acc[c]);
-        for (int t = from + 1; t <= to; t += B) {
-            float x[B][C][V] = {};
+        for (int t = from + 1; t <= to; t += J) {
+            float x[J][C][V] = {};
 #pragma unroll
-            for (int j = 0; j < B; ++j)
+            for (int j = 0; j < J; ++j)
 #pragma unroll
                 for (int c = 0; c < C; ++c)
                     if (t + j <= to && in[c]) load_floats_l2<V>(piece_of(2 * (t + j), c), x[j][c]);
 #pragma unroll
-            for (int j = 0; j < B; ++j)
+            for (int j = 0; j < J; ++j)
 #pragma unroll
                 for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -728,7 +753,7 @@ cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s) {
         const cudaError_t e = cudaLaunchKernelEx(&c, k_sort, a, passes, bits);
         if (e != cudaSuccess) return e;
     }
-    if (a.dtype == BP_BF16) return sums<__nv_bfloat16, 8, 2>(a, passes, s);
+    if (a.dtype == BP_BF16) return a.width > 256 ? sums<__nv_bfloat16, 8, 2>(a, passes, s) : sums<__nv_bfloat16, 8, 1>(a, passes, s);
     return pieces ? sums<float, 4, 1>(a, passes, s) : sums<float, 1, 1>(a, passes, s);
 }
 
