@@ -177,6 +177,30 @@ __device__ __noinline__ int choose64(const ScoredArgs& g, const T* z) {
     return mine;
 }
 
+// The experts of a list (lane j < n its j-th) by their float64 values, for sigmoid scores: lane j gets the j-th.
+template <class T>
+__device__ __forceinline__ int order_list(const ScoredArgs& g, const T* z, int mine, int n) {
+    const int lane = threadIdx.x & 31;
+    Order64 o = 0ull;
+    if (lane < n) {
+        double p = 1.0 / (1.0 + exp(-(double)to_f32(z[mine])));
+        if (g.bias != nullptr) p += (double)g.bias[mine];
+        o = order64(p);
+    }
+    int place = 0;
+    for (int j = 0; j < n; ++j) {
+        const Order64 x = __shfl_sync(0xffffffffu, o, j);
+        const int e = __shfl_sync(0xffffffffu, mine, j);
+        place += x > o || (x == o && e < mine);
+    }
+    int sorted = -1;
+    for (int j = 0; j < n; ++j) {
+        const int at = __shfl_sync(0xffffffffu, place, j), e = __shfl_sync(0xffffffffu, mine, j);
+        if (lane == at) sorted = e;
+    }
+    return sorted;
+}
+
 // Gate of a chosen expert of logit z (live), by lane; every lane takes part.
 __device__ __forceinline__ float share_of_chosen(const ScoredArgs& g, float z, bool live) {
     // Renormalised scores: a factor that all have in common drops out, which keeps them apart from zero.
@@ -286,7 +310,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 :
         }
         const float unit = soft ? 1e-5f : 5e-7f;   // (of `most`: of itself, 1e-5)
         const float err = unit * most + 1.2e-7f * (1.f + b_most);   // of any score and its bias
-        bool near = false, open = true;
+        bool near = false, near_groups = false, open = true;
         float m1 = c[0], m2 = kNone;   // the lane's two largest
 #pragma unroll
         for (int i = 1; i < PER; ++i) {
@@ -298,7 +322,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 :
             const bool real = s.group < g.n_groups;
             open = group_stays(g, s, worth);
             const float kept = -warp_max(real && open ? -worth : kNone), left = warp_max(real && !open ? worth : kNone);
-            near = left > kNone && !(kept - left > 6.f * err);   // (a worth is off by 2 err, and by its sum's rounding)
+            near = near_groups = left > kNone && !(kept - left > 6.f * err);   // (a worth is off by 2 err, and by its sum's rounding)
             if (!open) m1 = kNone;
         }
         // The values from the (k + 1)-th largest lane's largest on: as many as are wanted, and few more.  They go to a lane
@@ -323,10 +347,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 :
             if (lane >= o) upto += x;
         }
         int taken = __shfl_sync(0xffffffffu, upto, 31);   // entries of the list
+        const bool listed = taken <= 32;                   // the list has them all
         bool whole = !(least > kNone);                     // there are no others
         int mine = -1;
         float value = kNone;
-        if (taken <= 32) {
+        if (listed) {
             int at = upto - own;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
@@ -367,7 +392,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 :
                 near = (unlike & ((last - 1) | behind)) != 0 || (!whole && behind >= 1u << (taken - 1));
             }
         }
-        if (near) mine = choose64<T, PER>(g, z);
+        if (near) {
+            // The list again by float64 scores, where float32 can tell that it has every expert of the choice (sigmoid scores: they are
+            // each their own); else all experts.
+            const float kth = __shfl_sync(0xffffffffu, value, g.r.k - 1);
+            if (!near_groups && !soft && listed && (whole || kth - least > 2.f * err)) mine = order_list(g, z, mine, taken);
+            else mine = choose64<T, PER>(g, z);
+        }
         if (lane >= g.r.k) mine = -1;
         const bool live = mine >= 0;
         const float logit = live ? to_f32(z[mine]) : kNone;
