@@ -78,24 +78,6 @@ struct Sums {
     }
 };
 
-// Number, mean and sum of squared differences from it, of two sets together: no cancellation where the mean
-// is far from 0.
-struct Moments {
-    float n, mean, m2;
-    __device__ __forceinline__ void join(float n2, float mean2, float m22) {
-        const float all = n + n2;
-        if (all == 0.f) return;
-        const float d = mean2 - mean, part = __fdividef(n2, all);
-        mean += d * part;
-        m2 += m22 + d * d * n * part;
-        n = all;
-    }
-    __device__ __forceinline__ void join_lanes(int lanes) {   // lane 0's is the one to use: others' last bits differ
-        for (int o = lanes / 2; o > 0; o >>= 1)
-            join(__shfl_xor_sync(0xffffffffu, n, o), __shfl_xor_sync(0xffffffffu, mean, o), __shfl_xor_sync(0xffffffffu, m2, o));
-    }
-};
-
 // Two float32 operations an instruction, over a thread's P values (one at a time where P is 1).
 __device__ __forceinline__ unsigned long long pair(float a, float b) {
     unsigned long long r;
@@ -274,55 +256,64 @@ __device__ __forceinline__ void load_gate(const ResidualArgs& g, const Columns<V
     for (int i = 0; i < V * C; ++i) k[i] *= g.scale;
 }
 
-// Mean and 1 / sqrt of a row, in the same two steps as Sums.
+// Mean and 1 / sqrt of a row, in the same two steps as Sums.  MEAN: each warp's mean first and the squared differences from it,
+// then the warps' means and differences from theirs, so that nothing cancels where the mean is far from 0.
 template <bool MEAN, int V, int C>
 struct NormStats {
     Sums<1> sums;
-    Moments m;
     float* at;
     int turn = 0;
-    __device__ __forceinline__ NormStats(const Worker& w, int place) : sums(w, place), at(w.red + place * w.warps) {}
-    __device__ __forceinline__ void give(const Columns<V, C>& cols, const float (&v)[V * C], const Worker& w) {
+    float mean_w = 0.f, m2_w = 0.f;        // of this warp
+    float values_w = 0.f, each_w = 0.f;    // how many values it has, and one over that
+    __device__ __forceinline__ NormStats(const Worker& w, int place, int width) : sums(w, place), at(w.red + place * w.warps) {
         if constexpr (MEAN) {
-            float sum = 0.f;
             int n = 0;
 #pragma unroll
+            for (int j = 0; j < C; ++j) n += max(0, min(32 * V, width - (j * w.threads + (w.tid & ~31)) * V));
+            values_w = (float)n;
+            each_w = n > 0 ? 1.f / values_w : 0.f;
+        }
+    }
+    __device__ __forceinline__ static float warp_sum(float x, int lanes) {
+        for (int o = lanes / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        return x;
+    }
+    __device__ __forceinline__ void give(const Columns<V, C>& cols, const float (&v)[V * C], const Worker& w) {
+        if constexpr (MEAN) {
+            const float s = dot(Same{1.f}, v);   // (columns past the row's end are 0)
+            mean_w = warp_sum(s, 32) * each_w;
+            float d[V * C];
+            sub(d, v, mean_w);
+#pragma unroll
             for (int j = 0; j < C; ++j)
-                if (cols.in(j)) {
-                    n += V;
+                if (!cols.in(j))
 #pragma unroll
-                    for (int i = 0; i < V; ++i) sum += v[j * V + i];
-                }
-            m = {(float)n, n > 0 ? __fdividef(sum, (float)n) : 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < C; ++j)
-                if (cols.in(j))
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float d = v[j * V + i] - m.mean;
-                        m.m2 += d * d;
-                    }
-            m.join_lanes(32);
-            float* to = at + turn * kRed + (w.tid >> 5) * 3;
-            if (w.warps > 1 && (threadIdx.x & 31) == 0) to[0] = m.n, to[1] = m.mean, to[2] = m.m2;
+                    for (int i = 0; i < V; ++i) d[j * V + i] = 0.f;
+            m2_w = warp_sum(dot(d, d), 32);
+            float* to = at + turn * kRed + (w.tid >> 5) * 4;
+            if (w.warps > 1 && (threadIdx.x & 31) == 0) to[0] = mean_w, to[1] = m2_w, to[2] = values_w;
         } else {
-            const float s[1] = {dot(v, v)};   // (columns past the row's end are 0)
+            const float s[1] = {dot(v, v)};
             sums.give(s, w);
         }
     }
     __device__ __forceinline__ void take(const ResidualArgs& g, int kind, const Worker& w, float& mean, float& rinv) {
         if constexpr (MEAN) {
+            float m = mean_w, m2 = m2_w;
             if (w.warps > 1) {
                 const int lane = threadIdx.x & 31;
-                const float* from = at + turn * kRed + lane * 3;
-                m = {0.f, 0.f, 0.f};
-                if (lane < w.warps) m = {from[0], from[1], from[2]};
-                m.join_lanes(16);
+                const float* from = at + turn * kRed + lane * 4;
+                const bool in = lane < w.warps;
+                const float m_w = in ? from[0] : 0.f, n_w = in ? from[2] : 0.f;
+                m = warp_sum(m_w * n_w, kMaxWarps) * g.each;
+                m = __shfl_sync(0xffffffffu, m, 0);
+                const float d = m_w - m;
+                m2 = warp_sum((in ? from[1] : 0.f) + n_w * d * d, kMaxWarps);
+                m2 = __shfl_sync(0xffffffffu, m2, 0);
                 turn ^= 1;
             }
-            m.mean = __shfl_sync(0xffffffffu, m.mean, 0);
-            const float var = __shfl_sync(0xffffffffu, m.m2, 0) * g.each + (kind == BP_NORM_LAYER ? 0.f : m.mean * m.mean);
-            mean = kind == BP_NORM_LAYER ? m.mean : 0.f;
+            const float var = m2 * g.each + (kind == BP_NORM_LAYER ? 0.f : m * m);
+            mean = kind == BP_NORM_LAYER ? m : 0.f;
             rinv = rsqrtf(var + g.eps);
         } else {
             float s[1];
@@ -372,7 +363,7 @@ __global__ void __maxnreg__(V * C <= 8 && !MEAN ? 64 : 128) k_residual(ResidualA
     float k[P], wi[P], kb[MEAN ? P : 1], bi[MEAN ? P : 1];   // k: scale * gate * w_out, kb: scale * gate * b_out
     load_floats(cols, g.wi, 1.f, wi);
     if constexpr (MEAN) load_floats(cols, g.bi, 0.f, bi);
-    NormStats<MEAN, V, C> of_f(w, 0), of_y(w, 4);
+    NormStats<MEAN, V, C> of_f(w, 0, g.width), of_y(w, 4, g.width);
     Stretch now{0, r0};
     for (int r = r0; r < r1; ++r) {
         if (r >= now.end) {
