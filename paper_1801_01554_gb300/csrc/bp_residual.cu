@@ -169,11 +169,11 @@ __device__ __forceinline__ void round_to(const float (&x)[V * C], Piece<T, V> (&
         p[j].set(y);
     }
 }
-template <class T, int V, int C>
-__device__ __forceinline__ void store_row(const Columns<V, C>& cols, const Piece<T, V> (&p)[C], T* to) {
+template <class T, int V, int C, int M>
+__device__ __forceinline__ void store_row(const Columns<V, C>& cols, const Piece<T, V> (&p)[M], T* to, int j0 = 0) {
 #pragma unroll
-    for (int j = 0; j < C; ++j)
-        if (cols.in(j)) p[j].store(to + j * cols.threads * V);
+    for (int i = 0; i < M; ++i)
+        if (cols.in(j0 + i)) p[i].store(to + (j0 + i) * cols.threads * V);
 }
 
 // Rows on their way: S rows of N arrays, each thread's pieces in places of its own in shared memory, so that a thread
@@ -201,13 +201,15 @@ struct Ring {
     }
     __device__ __forceinline__ static void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
     __device__ __forceinline__ static void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory"); }   // for the first of S rows
-    // The row's pieces; zeros for an array that is not there and past the row's end.
-    __device__ __forceinline__ void take(const Columns<V, C>& cols, bool there, unsigned slot, int n, Piece<T, V> (&out)[C]) const {
+    // The row's pieces from the j0-th on; zeros for an array that is not there and past the row's end.
+    template <int M>
+    __device__ __forceinline__ void take(const Columns<V, C>& cols, bool there, unsigned slot, int n, Piece<T, V> (&out)[M], int j0 = 0) const {
 #pragma unroll
-        for (int j = 0; j < C; ++j) {
-            out[j].u = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < M; ++i) {
+            const int j = j0 + i;
+            out[i].u = make_uint4(0u, 0u, 0u, 0u);
             if (!there || !cols.in(j)) continue;
-            uint4& u = out[j].u;
+            uint4& u = out[i].u;
             if constexpr (kBytes == 16)
                 asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(place(slot, n, j)) : "memory");
             else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u.x) : "r"(place(slot, n, j)) : "memory");
@@ -215,11 +217,16 @@ struct Ring {
     }
 };
 // Stages.  Three rows are enough to keep the memory busy (16,384 rows of 4,096 bfloat16 units, forward: 2 stages 100.0 us,
-// 3 98.5, 6 as 4: what more of them take from the L1 cache is missed).
+// 3 98.5, 6 as 4: what more of them take from the L1 cache is missed); what fits beside wide rows' weights going back.
 template <class T, int V, int C>
 constexpr int stages(bool back) {
     constexpr int bytes = V * C * (int)sizeof(T);
-    return bytes <= 32 ? 3 : back ? 1 : 3;
+    return back && V * C >= 16 ? (bytes <= 32 ? 2 : 1) : 3;
+}
+// Shared memory of a thread: the stages, and going back the weights of 16 values.
+template <class T, int V, int C>
+constexpr int thread_bytes(bool back) {
+    return stages<T, V, C>(back) * (back ? 4 : 2) * C * V * (int)sizeof(T) + (back && V * C >= 16 ? 2 * V * C * 4 : 0);
 }
 
 // Rows that share a row of gates: of row r, the gates' row (-1: none) and the first row from r on that is not of it.
@@ -466,9 +473,32 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
     const bool out_normed = FULL || g.norm_out != BP_NORM_NONE;
     const float layer_in = g.norm_in == BP_NORM_LAYER ? 1.f : 0.f, layer_out = g.norm_out == BP_NORM_LAYER ? 1.f : 0.f;
     const bool by_range = g.n_gates > 0 && g.offsets != nullptr;
-    float k[P], wi[P];
-    load_floats(cols, g.wi, 1.f, wi);
-    float A[P] = {}, B[MEAN ? P : 1] = {}, CI[P] = {}, D[MEAN ? P : 1] = {};
+    // 16 values a thread are taken 8 at a time, twice a row, and their weights lie in shared memory: all at once they
+    // would take more registers than there are.
+    constexpr bool WIDE = P >= 16;
+    constexpr int Q = WIDE ? 8 : P, Z = P / Q, JC = Q / V;   // values of a part, parts, pieces of a part
+    float k_all[WIDE ? 1 : Q], wi_all[WIDE ? 1 : Q];
+    float* const own = reinterpret_cast<float*>(room + (size_t)S * 4 * P * sizeof(T) * blockDim.x) + threadIdx.x;   // (WIDE)
+    const auto keep = [&](const float (&x)[P], float (&to)[WIDE ? 1 : Q], int first) {
+#pragma unroll
+        for (int c = 0; c < P; ++c) {
+            if constexpr (WIDE) own[(first + c) * blockDim.x] = x[c];
+            else to[c] = x[c];
+        }
+    };
+    const auto kept = [&](const float (&from)[WIDE ? 1 : Q], int first, int z, float (&x)[Q]) {
+#pragma unroll
+        for (int c = 0; c < Q; ++c) {
+            if constexpr (WIDE) x[c] = own[(first + z * Q + c) * blockDim.x];
+            else x[c] = from[c];
+        }
+    };
+    {
+        float x[P];
+        load_floats(cols, g.wi, 1.f, x);
+        keep(x, wi_all, P);
+    }
+    float A[Z][Q] = {}, B[MEAN ? Z : 1][MEAN ? Q : 1] = {}, CI[Z][Q] = {}, D[MEAN ? Z : 1][MEAN ? Q : 1] = {};
     bool fresh = true;   // nothing of this worker in W and WB
     // Gates by range: the sums of a stretch to its record, and times scale * gate to this worker's part of the weights'
     // gradients.
@@ -482,13 +512,15 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int c = j * V + i;
-                if (seg >= 0 && g.Ggate != nullptr) g.A[rec + i] = A[c];
-                if (g.Gwo != nullptr) g.W[row + i] = (fresh ? 0.f : g.W[row + i]) + q[c] * A[c];
-                A[c] = 0.f;
+                float& a = A[c / Q][c % Q];
+                if (seg >= 0 && g.Ggate != nullptr) g.A[rec + i] = a;
+                if (g.Gwo != nullptr) g.W[row + i] = (fresh ? 0.f : g.W[row + i]) + q[c] * a;
+                a = 0.f;
                 if constexpr (MEAN) {
-                    if (seg >= 0 && g.Ggate != nullptr) g.B[rec + i] = B[c];
-                    if (g.Gbo != nullptr) g.WB[row + i] = (fresh ? 0.f : g.WB[row + i]) + q[c] * B[c];
-                    B[c] = 0.f;
+                    float& b = B[c / Q][c % Q];
+                    if (seg >= 0 && g.Ggate != nullptr) g.B[rec + i] = b;
+                    if (g.Gbo != nullptr) g.WB[row + i] = (fresh ? 0.f : g.WB[row + i]) + q[c] * b;
+                    b = 0.f;
                 }
             }
         }
@@ -506,32 +538,37 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
         if (r >= now.end) {
             if (r > r0) flush(now.seg);
             now = stretch_of(g, r);
-            load_gate(g, cols, now.seg, k);
-            float wo[P];
+            float x[P], wo[P];
+            load_gate(g, cols, now.seg, x);
             load_floats(cols, g.wo, 1.f, wo);
-            mul(k, k, wo);
+            mul(x, x, wo);
+            keep(x, k_all, 0);
         }
         const float mf = next[0], rf = next[1], my = next[2], ry = next[3];
         if (r + 1 < r1) load_stats(r + 1);
         ring.wait();
-        float yv[P], fv[P], av[P], bv[P], s[N];
-        {
-            Piece<T, V> y[C], f[C], a[C], b[C];
-            ring.take(cols, has_h, slot, 0, y);
-            ring.take(cols, has_f, slot, 1, f);
-            ring.take(cols, has_y, slot, 2, a);
-            ring.take(cols, has_h, slot, 3, b);
-            values<T, V, C>(y, yv), values<T, V, C>(f, fv), values<T, V, C>(a, av), values<T, V, C>(b, bv);
-        }
-        if constexpr (MEAN) sub(yv, yv, my), sub(fv, fv, mf);
-        {
-            float e[P], t[P];
+        float yv[Q], fv[Q], av[Q], bv[Q], k[Q], wi[Q], s[N];
+        const auto load = [&](int z) {
+            Piece<T, V> y[JC], f[JC], a[JC], b[JC];
+            ring.take(cols, has_h, slot, 0, y, z * JC);
+            ring.take(cols, has_f, slot, 1, f, z * JC);
+            ring.take(cols, has_y, slot, 2, a, z * JC);
+            ring.take(cols, has_h, slot, 3, b, z * JC);
+            values<T, V, JC>(y, yv), values<T, V, JC>(f, fv), values<T, V, JC>(a, av), values<T, V, JC>(b, bv);
+            if constexpr (MEAN) sub(yv, yv, my), sub(fv, fv, mf);
+            kept(k_all, 0, z, k), kept(wi_all, P, z, wi);
+        };
+#pragma unroll
+        for (int z = 0; z < Z; ++z) {
+            load(z);
+            float e[Q], t[Q];
             mul(e, bv, wi);
             mul(t, k, fv);
-            s[0] = dot(e, yv), s[1] = dot(t, av), s[2] = dot(t, e), s[3] = dot(t, yv);
+            const auto add = [&](int i, float x) { s[i] = z == 0 ? x : s[i] + x; };
+            add(0, dot(e, yv)), add(1, dot(t, av)), add(2, dot(t, e)), add(3, dot(t, yv));
             if constexpr (MEAN) {
                 const Same one{1.f};
-                s[4] = dot(one, e), s[5] = dot(one, t), s[6] = dot(k, av), s[7] = dot(k, e), s[8] = dot(k, yv), s[9] = dot(one, k);
+                add(4, dot(one, e)), add(5, dot(one, t)), add(6, dot(k, av)), add(7, dot(k, e)), add(8, dot(k, yv)), add(9, dot(one, k));
             }
         }
         sums.give(s, w);
@@ -548,46 +585,50 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
             }
             d1 = rf * (s[1] + ry * x) * g.each;
         }
-        mul(yv, yv, Same{ry});
-        mul(fv, fv, Same{rf});
-        fma(CI, bv, yv, CI);
-        if constexpr (MEAN) fma(D, bv, Same{1.f}, D);
-        mul(bv, bv, wi);
-        fma(av, bv, Same{ry}, av);
-        fma(av, yv, Same{-ry * c1}, av);   // dy
-        if constexpr (MEAN) sub(av, av, ry * c0);
-        fma(A, av, fv, A);
-        if constexpr (MEAN) fma(B, av, Same{1.f}, B);
-        Piece<T, V> p[C];
-        if (gives_x) {
-            round_to<T, V, C>(av, p);
-            store_row<T>(cols, p, dX);
-        }
-        if (gives_f) {
-            mul(av, av, k);
-            mul(av, av, Same{rf});
-            fma(av, fv, Same{-rf * d1}, av);
-            if constexpr (MEAN) sub(av, av, rf * d0);
-            round_to<T, V, C>(av, p);
-            store_row<T>(cols, p, dF);
+#pragma unroll
+        for (int z = 0; z < Z; ++z) {
+            if constexpr (WIDE) load(z);
+            mul(yv, yv, Same{ry});
+            mul(fv, fv, Same{rf});
+            fma(CI[z], bv, yv, CI[z]);
+            if constexpr (MEAN) fma(D[z], bv, Same{1.f}, D[z]);
+            mul(bv, bv, wi);
+            fma(av, bv, Same{ry}, av);
+            fma(av, yv, Same{-ry * c1}, av);   // dy
+            if constexpr (MEAN) sub(av, av, ry * c0);
+            fma(A[z], av, fv, A[z]);
+            if constexpr (MEAN) fma(B[z], av, Same{1.f}, B[z]);
+            Piece<T, V> p[JC];
+            if (gives_x) {
+                round_to<T, V, JC>(av, p);
+                store_row<T>(cols, p, dX, z * JC);
+            }
+            if (gives_f) {
+                mul(av, av, k);
+                mul(av, av, Same{rf});
+                fma(av, fv, Same{-rf * d1}, av);
+                if constexpr (MEAN) sub(av, av, rf * d0);
+                round_to<T, V, JC>(av, p);
+                store_row<T>(cols, p, dF, z * JC);
+            }
         }
         ask();   // (the row's values are in registers)
         dX += g.width, dF += g.width;
     }
     if (by_range && live && (g.Gwo != nullptr || g.Gbo != nullptr || g.Ggate != nullptr)) flush(now.seg);
     // The block's sums over its rows.
-    const auto put = [&](const float* acc, float* to) {
+    const auto put = [&](const auto& acc, float* to) {
         if (g.workers_a_block == 1) {
 #pragma unroll
             for (int c = 0; c < P; ++c)
-                if (cols.in(c / V)) to[(size_t)blockIdx.x * g.width + cols.at(c / V) + c % V] = acc[c];
+                if (cols.in(c / V)) to[(size_t)blockIdx.x * g.width + cols.at(c / V) + c % V] = acc[c / Q][c % Q];
             return;
         }
         float* part = reinterpret_cast<float*>(room);
         __syncthreads();
 #pragma unroll
         for (int c = 0; c < P; ++c)
-            if (cols.in(c / V)) part[w.id * g.width + cols.at(c / V) + c % V] = acc[c];
+            if (cols.in(c / V)) part[w.id * g.width + cols.at(c / V) + c % V] = acc[c / Q][c % Q];
         __syncthreads();
         for (int c = threadIdx.x; c < g.width; c += blockDim.x) {
             float x = part[c];
@@ -707,7 +748,7 @@ struct Launch {
     cudaError_t shape() const {
         const bool mean = a->norm_out == BP_NORM_LAYER || a->norm_in == BP_NORM_LAYER;
         const int threads = a->workers_a_block * a->worker_warps * 32, blocks = (a->workers + a->workers_a_block - 1) / a->workers_a_block;
-        const int bytes = stages<T, V, C>(back) * (back ? 4 : 2) * C * V * (int)sizeof(T) * threads;
+        const int bytes = thread_bytes<T, V, C>(back) * threads;
         const bool norms = a->F != nullptr && a->norm_out != BP_NORM_NONE && a->norm_in != BP_NORM_NONE;
         const bool full = V > 1 && norms && (back ? a->dY != nullptr && a->dH != nullptr && a->dX != nullptr && a->dF != nullptr : a->H != nullptr);
         const auto go = [&](auto k) { k<<<blocks, threads, bytes, s>>>(*a); };
@@ -724,8 +765,7 @@ struct Launch {
 struct Setup {
     template <class T, int V, int C>
     cudaError_t shape() const {
-        const int out = stages<T, V, C>(false) * 2 * C * V * (int)sizeof(T) * kMaxThreads;
-        const int back = stages<T, V, C>(true) * 4 * C * V * (int)sizeof(T) * kMaxThreads;
+        const int out = thread_bytes<T, V, C>(false) * kMaxThreads, back = thread_bytes<T, V, C>(true) * kMaxThreads;
         const auto set = [](auto k, int bytes) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
         cudaError_t e = cudaSuccess;
         const auto both = [&](auto full, auto mean) {
