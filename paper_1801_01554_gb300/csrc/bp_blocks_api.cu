@@ -373,7 +373,9 @@ bp_status bp_clip_create(const void* const* h_in, void* const* h_out, const int6
         if (st == BP_OK) st = cuda_status(cudaDeviceGetAttribute(&l->num_sms, cudaDevAttrMultiProcessorCount, l->device), call);
         if (st == BP_OK) st = cuda_status(clip_setup(l->a.n_chunks, chunk == kClipTile, &l->a.few), call);
         if (st == BP_OK) st = make_array(&l->chunks, chunks.size(), call);
-        if (st == BP_OK) st = make_array(&l->a.partial, (size_t)clip_blocks(l->num_sms), call);
+        if (st == BP_OK) st = make_array(&l->a.partial, (size_t)clip_blocks(l->num_sms) + 1, call);
+        if (st == BP_OK) l->a.total = l->a.partial + clip_blocks(l->num_sms);
+        if (st == BP_OK) st = make_counts(&l->a.arrived, 1, call);
         if (st == BP_OK && !chunks.empty())
             st = cuda_status(cudaMemcpy(l->chunks, chunks.data(), chunks.size() * sizeof(ClipChunk), cudaMemcpyHostToDevice), call);
         if (st == BP_OK) st = layer_ready(call);
@@ -396,6 +398,7 @@ void bp_clip_destroy(bp_clip* l) {
     cudaFree(l->a.flags);
     cudaFree(l->chunks);
     cudaFree(l->a.partial);
+    cudaFree(l->a.arrived);
     delete l;
 }
 

@@ -77,7 +77,9 @@ struct ClipArgs {
     int write;                 // 0: the norm alone
     float max_norm;
     float* norm;               // or NULL
-    double* partial;           // [clip_blocks]
+    double* partial;           // [clip_blocks], and one for their sum
+    double* total;
+    unsigned* arrived;         // a zero, left zero
     int* flags;
 };
 constexpr int kClipTile = 8192;   // values that a block takes at a time

@@ -26,8 +26,9 @@ __device__ __forceinline__ double squares(const float (&v)[N]) {
     return (double)s * (large ? 0x1p140 : 0x1p-200);
 }
 
-// The block's sum, in one order, in every thread.
-__device__ __forceinline__ double block_sum(double x, double* part) {
+// The block's sum, in one order, in every thread: each warp's first where the block has its SM to itself; by one warp
+// where it shares it, as a float64 sum is 16 cycles of the SM's unit for every warp that takes part.
+__device__ __forceinline__ double block_sum_alone(double x, double* part) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
@@ -35,6 +36,19 @@ __device__ __forceinline__ double block_sum(double x, double* part) {
     x = part[0];
     for (int w = 1; w < kWarps; ++w) x += part[w];
     return x;
+}
+__device__ __forceinline__ double block_sum(double x, double* part) {   // part [kThreads]
+    part[threadIdx.x] = x;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) x += part[w * 32 + threadIdx.x];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        if (threadIdx.x == 0) part[0] = x;
+    }
+    __syncthreads();
+    return part[0];
 }
 
 // A chunk's values in 16-byte pieces: `head` values before the first whole piece, `pieces` pieces, `tail` values
@@ -124,9 +138,11 @@ __device__ __forceinline__ void scale_chunk(const ClipChunk& c, float by) {
     }
 }
 
-// Squares of every blocks-th chunk, summed up by block.  Bound by reading the values once.
+// Squares of every blocks-th chunk, summed up by block; the block that comes last adds up the blocks' sums, in their
+// order.  Bound by reading the values once.
 __global__ void __launch_bounds__(kThreads) k_clip_norm(ClipArgs g) {
-    __shared__ double part[kWarps];
+    __shared__ double part[kThreads];
+    __shared__ bool last;
     pdl_launch();
     double sum = 0.0;
     for (int i = blockIdx.x; i < g.n_chunks; i += gridDim.x) {
@@ -134,7 +150,20 @@ __global__ void __launch_bounds__(kThreads) k_clip_norm(ClipArgs g) {
         sum += c.dtype == BP_BF16 ? chunk_squares<__nv_bfloat16>(c) : chunk_squares<float>(c);
     }
     sum = block_sum(sum, part);
-    if (threadIdx.x == 0) g.partial[blockIdx.x] = sum;
+    if (threadIdx.x == 0) {
+        g.partial[blockIdx.x] = sum;
+        __threadfence();
+        last = atomicAdd(g.arrived, 1u) == gridDim.x - 1;
+        if (last) *g.arrived = 0u;   // for the next call
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    sum = 0.0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads) sum += __ldcg(g.partial + i);
+    __syncthreads();
+    sum = block_sum(sum, part);
+    if (threadIdx.x == 0) *g.total = sum;
 }
 
 // What the values are multiplied by, the same in every block: 1 where nothing is clipped.  The root is float32's, of the sum
@@ -161,12 +190,9 @@ __device__ __forceinline__ void scale(const ClipArgs& g, int i, float by) {
 
 // Bound by reading the values again and writing them.  (Of 1 GB that the norm has read L2 keeps nothing to speak of: the same time
 // from the last chunk to the first.)
-__global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs g, int blocks) {
-    __shared__ double part[kWarps];
+__global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs g) {
     pdl_wait();
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < blocks; i += kThreads) sum += __ldcg(g.partial + i);
-    const float by = clip_factor(g, block_sum(sum, part));
+    const float by = clip_factor(g, __ldcg(g.total));
     if (!g.write || (by == 1.f && g.in_place)) return;
     for (int i = blockIdx.x; i < g.n_chunks; i += gridDim.x) scale(g, i, by);
 }
@@ -201,7 +227,7 @@ __device__ __forceinline__ void clip_chunk(const ClipArgs& g, const ClipChunk& c
 #pragma unroll
         for (int i = 0; i < V; ++i) v[j * V + i] = x[i];
     }
-    const double sum = block_sum(squares(v) + squares(e), part);
+    const double sum = block_sum_alone(squares(v) + squares(e), part);
     if (threadIdx.x == 0) *mine = sum;
     cluster_sync();
     double sums[kFewCtas], total = 0.0;
@@ -283,7 +309,7 @@ cudaError_t clip_run(const ClipArgs& a, const ClipFew& few, int num_sms, cudaStr
     const int blocks = max(1, min(a.n_chunks, clip_blocks(num_sms)));
     k_clip_norm<<<blocks, kThreads, 0, s>>>(a);
     const cudaError_t e = cudaGetLastError();
-    return e != cudaSuccess ? e : launch_pdl(k_clip_scale, a.write ? blocks : 1, 1, kThreads, 0, s, a, blocks);
+    return e != cudaSuccess ? e : launch_pdl(k_clip_scale, a.write ? blocks : 1, 1, kThreads, 0, s, a);
 }
 
 }  // namespace bp
