@@ -6,9 +6,11 @@
 
 namespace bp {
 namespace {
-constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
+constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;   // of a worker
 constexpr int kSums = 16;        // of the reductions between two barriers, at most
-constexpr int kRed = kMaxWarps * kSums;
+constexpr int kRed = 32 * kSums;
+// Warps of a block, one block an SM: as many as its registers are enough for (64, 80 or 128 a thread).
+constexpr int block_warps(bool back, bool mean, int v, int c) { return back || v * c > 8 || (mean && c > 1) ? 16 : mean ? 24 : 32; }
 constexpr int kWorkerRows = 4;   // of a worker of the backward pass, at least: its sums by column are added up at the end
 
 // A worker is `warps` warps that take a row at a time, a thread C pieces of V columns; a block has one or more.
@@ -335,7 +337,7 @@ struct NormStats {
 // are on their way in shared memory.  MEAN: a norm takes means off.  FULL: every operand and both norms are there, known
 // to the compiler.  Bound by reading X and F once and writing Y and H once.
 template <class T, int V, int C, bool MEAN, bool FULL>
-__global__ void __maxnreg__(V * C <= 8 && !MEAN ? 64 : 128) k_residual(ResidualArgs g) {
+__global__ void __maxnreg__(65536 / (32 * block_warps(false, MEAN, V, C)) / 8 * 8) k_residual(ResidualArgs g) {
     constexpr int P = V * C, S = stages<T, V, C>(false);
     extern __shared__ __align__(16) unsigned char room[];
     __shared__ float red[2 * kRed];
@@ -715,21 +717,23 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(ResidualArgs 
 }
 
 // How rows of `width` are shared out: pieces of v values, c of them a thread, `warps` a worker, `workers` a block; one block
-// an SM.  Going forward, 16 values a thread where a row has them: what a thread does once a row (its part of
+// an SM.  Going forward, 8 values a thread where a row has them for more than
+// 32 threads (16,000 rows of 600 float32 units, layer norms: 39 us, 50 with 4), 16 from 4,096 bytes on: what a thread does once a row (its part of
 // two reductions, addresses) is a third of its instructions then (16,384 rows of 4,096 bfloat16 units: 88.7 us, 6.05 TB/s;
 // 98.5 us with 8).  Backward that would take more registers than 512 threads have, and half the threads are no faster
 // (143 us, 5.6 TB/s, with 8 values and 512 threads; the same with 16 and 256).
 struct Shape {
     int v, c, warps, workers;
 };
-Shape shape_of(int width, int size, bool pieces, bool back) {
+Shape shape_of(int width, int size, bool pieces, bool back, bool mean) {
     Shape s;
     s.v = pieces ? 16 / size : 1;
     const int nv = (width + s.v - 1) / s.v;
     s.c = 1;
+    while (!back && (nv + s.c - 1) / s.c > 32 && s.c * s.v < 8) s.c *= 2;
     while ((nv + s.c - 1) / s.c > (back ? kMaxThreads : kMaxThreads / 2) && s.c * s.v < 16) s.c *= 2;
     s.warps = ((nv + s.c - 1) / s.c + 31) / 32;
-    s.workers = kMaxWarps / s.warps;
+    s.workers = min(s.warps > 1 ? 15 : 32, block_warps(back, mean, s.v, s.c) / s.warps);   // (15: barriers)
     return s;
 }
 
@@ -739,6 +743,8 @@ bool pieces16(const ResidualArgs& a) {
     return (p & 15) == 0 && a.width % 4 == 0;
 }
 
+bool takes_means(const ResidualArgs& a) { return a.norm_out == BP_NORM_LAYER || a.norm_in == BP_NORM_LAYER; }
+
 // What to do with the kernels of a shape: launch one, or set up both.
 struct Launch {
     const ResidualArgs* a;
@@ -746,7 +752,7 @@ struct Launch {
     cudaStream_t s;
     template <class T, int V, int C>
     cudaError_t shape() const {
-        const bool mean = a->norm_out == BP_NORM_LAYER || a->norm_in == BP_NORM_LAYER;
+        const bool mean = takes_means(*a);
         const int threads = a->workers_a_block * a->worker_warps * 32, blocks = (a->workers + a->workers_a_block - 1) / a->workers_a_block;
         const int bytes = thread_bytes<T, V, C>(back) * threads;
         const bool norms = a->F != nullptr && a->norm_out != BP_NORM_NONE && a->norm_in != BP_NORM_NONE;
@@ -765,12 +771,12 @@ struct Launch {
 struct Setup {
     template <class T, int V, int C>
     cudaError_t shape() const {
-        const int out = thread_bytes<T, V, C>(false) * kMaxThreads, back = thread_bytes<T, V, C>(true) * kMaxThreads;
+        const auto most = [](bool back, bool mean) { return thread_bytes<T, V, C>(back) * block_warps(back, mean, V, C) * 32; };
         const auto set = [](auto k, int bytes) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); };
         cudaError_t e = cudaSuccess;
         const auto both = [&](auto full, auto mean) {
-            if (e == cudaSuccess) e = set(k_residual<T, V, C, decltype(mean)::value, decltype(full)::value>, out);
-            if (e == cudaSuccess) e = set(k_residual_backward<T, V, C, decltype(mean)::value, decltype(full)::value>, back);
+            if (e == cudaSuccess) e = set(k_residual<T, V, C, decltype(mean)::value, decltype(full)::value>, most(false, decltype(mean)::value));
+            if (e == cudaSuccess) e = set(k_residual_backward<T, V, C, decltype(mean)::value, decltype(full)::value>, most(true, decltype(mean)::value));
         };
         both(std::false_type{}, std::false_type{}), both(std::false_type{}, std::true_type{});
         if constexpr (V > 1) both(std::true_type{}, std::false_type{}), both(std::true_type{}, std::true_type{});
@@ -789,21 +795,23 @@ cudaError_t with_shape(const F& f, int dtype, const Shape& h) {
         default: return f.template shape<float, 1, 16>();
     }
 }
-Shape shape_of(const ResidualArgs& a, bool back) { return shape_of(a.width, a.dtype == BP_F32 ? 4 : 2, a.dtype == BP_BF16 || pieces16(a), back); }
+Shape shape_of(const ResidualArgs& a, bool back) {
+    return shape_of(a.width, a.dtype == BP_F32 ? 4 : 2, a.dtype == BP_BF16 || pieces16(a), back, takes_means(a));
+}
 
 }  // namespace
 
 int residual_workers(int num_sms, int width, int dtype) {
-    const Shape s = shape_of(width, dtype == BP_F32 ? 4 : 2, true, true);
+    const Shape s = shape_of(width, dtype == BP_F32 ? 4 : 2, true, true, true);
     if (dtype == BP_BF16) return num_sms * s.workers;
-    return num_sms * max(s.workers, shape_of(width, 4, false, true).workers);   // a call's rows may be whole pieces or not
+    return num_sms * max(s.workers, shape_of(width, 4, false, true, true).workers);   // a call's rows may be whole pieces or not
 }
 
 cudaError_t residual_setup(int width, int dtype) {
     const int size = dtype == BP_F32 ? 4 : 2;
     cudaError_t e = cudaSuccess;
     for (int i = 0; i < 4 && e == cudaSuccess; ++i)   // rows in whole pieces or not, either direction
-        if ((i & 1) == 0 || dtype == BP_F32) e = with_shape(Setup{}, dtype, shape_of(width, size, (i & 1) == 0, i >= 2));
+        if ((i & 1) == 0 || dtype == BP_F32) e = with_shape(Setup{}, dtype, shape_of(width, size, (i & 1) == 0, i >= 2, true));
     return e;
 }
 
