@@ -11,7 +11,8 @@
  * The conventions of bp.h and bp_experts.h hold (row-major contiguous buffers, caller-owned device
  * memory, streams, status codes, bp_last_error; values float32 or bfloat16 as the handle's dtype says;
  * gates, norms' weights, biases, statistics and every change G float32 in both; BP_BF16 rows are
- * multiples of 8 units on 16-byte boundaries, float32 and int buffers lie on 4-byte boundaries).  Values
+ * multiples of 8 units on 16-byte boundaries, and so is d_G of their embeddings; other float32 and int
+ * buffers lie on 4-byte boundaries).  Values
  * are computed and summed in float32 and rounded once, on the way out.  Besides:
  *   - A handle belongs to the device that was current when it was made; calls with another
  *     one current are refused (BP_EINVAL).
