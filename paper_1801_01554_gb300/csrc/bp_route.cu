@@ -113,17 +113,43 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_columns(RouteArgs g, in
     if (threadIdx.x == 0) h[blocks] = carry;
 }
 
-// Rows of every block's choices, from the counts.
+// Rows of every block's choices, from the counts.  FEW: up to kFewBlocks blocks, whose counts each block adds up itself,
+// several threads an expert (no k_route_columns before).
+constexpr int kFewBlocks = 64;
+
+template <bool FEW>
 __global__ void __launch_bounds__(kRouteThreads) k_route_place(RouteArgs g) {
     constexpr int kWords = kRoutePatterns / 32;
     __shared__ unsigned bits[BP_MAX_EXPERTS * kWords];
     __shared__ int base[BP_MAX_EXPERTS];
+    __shared__ int before[FEW ? BP_MAX_EXPERTS : 1];
     __shared__ int warp_tot[32];
     const int p0 = blockIdx.x * kRoutePatterns, np = min(kRoutePatterns, g.n - p0);
     for (int i = threadIdx.x; i < g.E * kWords; i += kRouteThreads) bits[i] = 0u;
     pdl_wait();
     const int* h = g.hist;
-    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] = h[(size_t)e * (gridDim.x + 1) + gridDim.x];
+    if constexpr (FEW) {   // eight threads an expert, each every eighth block
+        const int sub = threadIdx.x & 7, blocks = gridDim.x;
+        for (int e0 = 0; e0 < g.E; e0 += kRouteThreads / 8) {
+            const int e = e0 + (int)(threadIdx.x >> 3);
+            int all = 0, mine = 0;
+#pragma unroll
+            for (int i = 0; i < kFewBlocks / 8; ++i) {
+                const int b = i * 8 + sub;
+                const int x = e < g.E && b < blocks ? __ldg(h + (size_t)e * (blocks + 1) + b) : 0;
+                all += x;
+                if (b < (int)blockIdx.x) mine += x;
+            }
+#pragma unroll
+            for (int o = 4; o > 0; o >>= 1) {
+                all += __shfl_xor_sync(0xffffffffu, all, o);
+                mine += __shfl_xor_sync(0xffffffffu, mine, o);
+            }
+            if (sub == 0 && e < g.E) base[e] = all, before[e] = mine;
+        }
+    } else {
+        for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] = h[(size_t)e * (gridDim.x + 1) + gridDim.x];
+    }
     __syncthreads();
     for (int i = threadIdx.x; i < np * g.k; i += kRouteThreads) {
         const int p = i / g.k, e = g.expert[(size_t)p0 * g.k + i];
@@ -135,7 +161,7 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_place(RouteArgs g) {
         if (threadIdx.x == 0) g.offsets[g.E] = total;
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] += h[(size_t)e * (gridDim.x + 1) + blockIdx.x];
+    for (int e = threadIdx.x; e < g.E; e += kRouteThreads) base[e] += FEW ? before[e] : h[(size_t)e * (gridDim.x + 1) + blockIdx.x];
     __syncthreads();
     for (int i = p0 * g.k + threadIdx.x; i < (p0 + np) * g.k; i += kRouteThreads)
         if (i >= total) g.source[i] = -1;
@@ -342,8 +368,9 @@ int mix_warps(int n, int N, int per_warp) {
 
 cudaError_t route_order(const RouteArgs& a, cudaStream_t s) {
     const int blocks = (a.n + kRoutePatterns - 1) / kRoutePatterns;
+    if (blocks <= kFewBlocks) return launch_pdl(k_route_place<true>, blocks, 1, kRouteThreads, 0, s, a);
     const cudaError_t e = launch_pdl(k_route_columns, a.E, 1, kRouteThreads, 0, s, a, blocks);
-    return e != cudaSuccess ? e : launch_pdl(k_route_place, blocks, 1, kRouteThreads, 0, s, a);
+    return e != cudaSuccess ? e : launch_pdl(k_route_place<false>, blocks, 1, kRouteThreads, 0, s, a);
 }
 
 cudaError_t route_forward(const RouteArgs& a, cudaStream_t s) {

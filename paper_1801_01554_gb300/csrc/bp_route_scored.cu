@@ -325,12 +325,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == kThreads && PER <= 8 ? 4 :
             near = near_groups = left > kNone && !(kept - left > 6.f * err);   // (a worth is off by 2 err, and by its sum's rounding)
             if (!open) m1 = kNone;
         }
-        // The values from the (k + 1)-th largest lane's largest on: as many as are wanted, and few more.  They go to a lane
-        // each, in the experts' order, and from there to the place that they have by size.
+        // The values from the (k + 3)-th largest lane's largest on: as many as are wanted, and some more (so that the last choice
+        // is hardly ever too near to what is not among them).  They go to a lane each, in the experts' order, and from there to the place that they have by size.
         float least = kNone;
         {
             float t = m1;
-            for (int j = 0; j <= g.r.k; ++j) {
+            for (int j = 0; j < g.r.k + 3; ++j) {
                 least = warp_max(t);
                 if (!(least > kNone)) break;
                 t = t == least ? kNone : t;
