@@ -53,7 +53,6 @@ __global__ void __launch_bounds__(kThreads) k_embed(EmbedArgs g, int lanes, int 
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kMaxDigits = 512;
 constexpr int kMostCtas = 16;
-constexpr int kSortAlone = 1024;   // ids that one CTA takes
 constexpr int kHold = 8;
 constexpr int kSortBytes = (kSortWarps + 3) * kMaxDigits * 4 + kSortWarps * kHold * 32 * 8;
 
@@ -429,7 +428,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
 // out their rows to its warps, 32 rows a sum and the sums in order.  One launch, no order of all ids.
 constexpr int kFewThreads = 1024, kFewWarps = kFewThreads / 32;
 constexpr int kFewIds = 4096, kFewChunks = kFewIds / kFewThreads;   // of a call; of a warp, 32 at a time
-constexpr long long kFewBlocks = 256;                               // of a call: as many as run at a time
 
 template <class T, int V>
 __global__ void __launch_bounds__(kFewThreads) k_embed_few(EmbedArgs g) {
@@ -506,8 +504,11 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(EmbedArgs g) {
         *to = g.accumulate ? *to + x : x;
     }
 }
-// Whether a call is for it: measured beside the sort at 3,584 ids of 29 tokens and 15 units, 7 us of 27.
-bool is_few(const EmbedArgs& a, int slabs) { return a.n <= kFewIds && (long long)a.n_tokens * slabs <= kFewBlocks; }
+// Whether a call is for it.  Its time grows with its blocks, by 13 us a thousand, that of the next kernel with the ids, by 5 us a
+// thousand; at the limit they are about as fast (of 256 units, bfloat16: 1,000 ids of 300 tokens take 5.6 us, by the next
+// kernel 7.8; of 500 8.5 and 8.2; 4,000 of 1,000 15 and 21; 100 of 256 4.7 and 3.6).  3,584 ids of 29 tokens and 15 units take
+// 5 us, by the sort 18.
+bool is_few(const EmbedArgs& a, int slabs) { return a.n <= kFewIds && 4 * (long long)a.n_tokens * slabs <= a.n + 256; }
 
 template <class T, int V>
 bool few(const EmbedArgs& a, cudaStream_t s, cudaError_t& e) {
@@ -520,7 +521,8 @@ bool few(const EmbedArgs& a, cudaStream_t s, cudaError_t& e) {
 
 // Few ids of many tokens: zeros everywhere first, then a block an id, which looks all ids through for its token.  The block
 // of every 32nd id of a token (the first one, mostly the only one, among them) adds up the rows of it and the 31 behind it;
-// more than 32 are joined as pieces, as in k_embed_sums, in the slots that the ids' order would give them.
+// more than 32 are joined as pieces, as in k_embed_sums, in the slots that the ids' order would give them.  Its time grows with
+// the ids: 100 of 2,000 tokens and 256 units take 4 us, 1,000 10, 4,000 24; by the sort 21, 23 and 23.
 constexpr int kScanIds = 4096;
 
 __global__ void __launch_bounds__(kThreads) k_zero(float* G, long long n) {
@@ -749,7 +751,7 @@ cudaError_t embed_backward(const EmbedArgs& a, cudaStream_t s) {
     const int bits = sort_bits(a.n_tokens, passes);
     if (a.n > 0) {
         cudaLaunchAttribute at;
-        const cudaLaunchConfig_t c = sort_config(a.n <= kSortAlone ? 1 : a.sort_ctas, &at, s);
+        const cudaLaunchConfig_t c = sort_config(a.sort_ctas, &at, s);
         const cudaError_t e = cudaLaunchKernelEx(&c, k_sort, a, passes, bits);
         if (e != cudaSuccess) return e;
     }

@@ -14,8 +14,7 @@ constexpr int block_warps(bool back, bool mean, int v, int c) { return back || v
 constexpr int kWorkerRows = 4;   // of a worker of the backward pass, at least: its sums by column are added up at the end
 
 // A worker is `warps` warps that take a row at a time, a thread C pieces of V columns; a block has one or more.
-// (Rows of 2,048 bytes and more have a block to themselves; with narrow ones a worker is a warp, whose reductions
-// need no barrier.)
+// (With narrow rows a worker is a warp, whose reductions need no barrier.)
 struct Worker {
     int id, warps, tid, threads;   // id: in the block
     float* red;

@@ -59,6 +59,26 @@ def test_embedding_matches_oracle(kind, n, V, width, dtype):
         check(ids, V, width, dtype, 1.75, Y, G, table, D)
 
 
+@pytest.mark.parametrize("dtype,width", [(bp.BP_F32, 9), (bp.BP_F32, 128), (bp.BP_BF16, 256), (bp.BP_BF16, 264)])
+@pytest.mark.parametrize("kind,n,V", [("any", 4096, 1088), ("holes", 4096, 1089), ("runs", 4095, 544), ("any", 1000, 314),
+                                      ("any", 1000, 315), ("any", 9, 66), ("one", 9, 67)])
+def test_either_side_of_a_block_a_token(kind, n, V, width, dtype):
+    """Calls with as many tokens as a block a token is taken for, and one more; once over what was there."""
+    rng = np.random.default_rng([n, V, width, 5])
+    ids = make(rng, kind, n, V)
+    table, D = rounded(rng.standard_normal((V, width)), dtype), rounded(rng.standard_normal((n, width)), dtype)
+    Y, G, twice = empty((n, width), dtype), empty((V, width), bp.BP_F32), empty((V, width), bp.BP_F32)
+    td, dd, idd = dev(table, dtype), dev(D, dtype), dev(ids)
+    with bp.Embedding(V, width, dtype, max_ids=n) as layer:
+        layer.forward(td, idd, n, Y, scale=1.75)
+        layer.backward(idd, n, dd, G, scale=1.75)
+        layer.backward(idd, n, dd, twice, scale=1.75)
+        layer.backward(idd, n, dd, twice, scale=1.75, accumulate=True)
+        layer.check()
+        check(ids, V, width, dtype, 1.75, Y, G, table, D)
+    assert torch.equal(twice, G * 2)
+
+
 @pytest.mark.parametrize("dtype,width", [(bp.BP_F32, 9), (bp.BP_BF16, 16)])
 @pytest.mark.parametrize("kind,n,V", [("any", 70001, 1 << 18), ("one", 40000, 1 << 24), ("runs", 9000, 400), ("holes", 5000, 1000)])
 def test_long_lists_and_wide_tokens(kind, n, V, width, dtype):
