@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_place(RouteArgs g) {
 #pragma unroll
             for (int i = 0; i < kFewBlocks / 8; ++i) {
                 const int b = i * 8 + sub;
-                const int x = e < g.E && b < blocks ? __ldg(h + (size_t)e * (blocks + 1) + b) : 0;
+                const int x = e < g.E && b < blocks ? __ldcg(h + (size_t)e * (blocks + 1) + b) : 0;   // (just written)
                 all += x;
                 if (b < (int)blockIdx.x) mine += x;
             }
