@@ -32,6 +32,7 @@ bp_status fail(bp_status st, const char* fmt, ...) {
 }
 
 bp_status cuda_fail(cudaError_t e, const char* what) {
+    cudaGetLastError();   // reported here: the check of a later launch must not find it again
     return fail(e == cudaErrorMemoryAllocation ? BP_ENOMEM : BP_ECUDA, "%s: %s (%s)", what,
                 cudaGetErrorName(e), cudaGetErrorString(e));
 }

@@ -29,6 +29,7 @@ inline bp_status fail(bp_status st, const char* fmt, ...) {
 
 inline bp_status cuda_status(cudaError_t e, const char* what) {
     if (e == cudaSuccess) return BP_OK;
+    cudaGetLastError();   // reported here: the check of a later launch must not find it again
     return fail(e == cudaErrorMemoryAllocation ? BP_ENOMEM : BP_ECUDA, "%s: %s (%s)", what, cudaGetErrorName(e),
                 cudaGetErrorString(e));
 }
