@@ -124,9 +124,10 @@ void bp_clip_destroy(bp_clip* clip);   /* NULL-safe; synchronises the device */
 /* d_norm [1] (float32; may be NULL) = sqrt of the sum of the squares of all values; where it is above max_norm
  * every value is multiplied by max_norm / norm on its way to its output, else the outputs are the inputs.
  * Squares and sums neither overflow nor vanish (32 values at a time are float32's,
- * scaled by a power of two where need be; beyond they are float64).  A norm that is not
- * finite (a NaN or an infinity among the values) clips nothing, and is latched for bp_clip_check.  max_norm >= 0; infinity: the norm
- * alone, outputs are not written.  Errors: BP_EINVAL, BP_ECUDA. */
+ * scaled by a power of two where need be; beyond they are float64), nor does max_norm / norm.  The norm of finite values may lie
+ * above float32's largest: *d_norm is then infinity, the values are clipped all the same, and nothing is latched.  A NaN or an
+ * infinity among the values clips nothing, and is latched for bp_clip_check; *d_norm is then that NaN or infinity.
+ * max_norm >= 0; infinity: the norm alone, outputs are not written.  Errors: BP_EINVAL, BP_ECUDA. */
 bp_status bp_clip_run(bp_clip* clip, float max_norm, float* d_norm, void* stream);
 
 /* Wait for `stream`, then report and clear what was latched: BP_ENONFINITE.  Errors: also BP_EINVAL, BP_ECUDA. */

@@ -99,6 +99,19 @@ __device__ __forceinline__ double chunk_squares(const ClipChunk& c) {
     return sum;
 }
 
+// What values are multiplied by: `by`, or `far` where the factor is below float32's normal numbers, which have fewer bits the
+// smaller they are, and then none (a bound of 1e-9 for a norm of 1e38 takes a factor of 1e-47 to values of 1e-9); else 0.
+struct Factor {
+    float by;
+    double far;
+};
+template <class T>
+__device__ __forceinline__ void scale_far(const ClipChunk& c, double far) {
+    const T* in = (const T*)c.in;
+    T* out = (T*)c.out;
+    for (unsigned i = threadIdx.x; i < c.count; i += kThreads) out[i] = from_f32<T>((float)((double)to_f32(in[i]) * far));
+}
+
 template <class T>
 __device__ __forceinline__ void scale_chunk(const ClipChunk& c, float by) {
     constexpr int V = Split<T>::V, J = kValues / V;
@@ -168,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) k_clip_norm(ClipArgs g) {
 
 // What the values are multiplied by, the same in every block: 1 where nothing is clipped.  The root is float32's, of the sum
 // times an even power of two (float64's root and quotient take some 2 us).
-__device__ __forceinline__ float clip_factor(const ClipArgs& g, double total) {
+__device__ __forceinline__ Factor clip_factor(const ClipArgs& g, double total) {
     const bool finite = total <= 1.7e308;   // (not a NaN)
     const int half = total > 0.0 && finite ? (((__double2hiint(total) >> 20) & 0x7ff) - 1023) >> 1 : 0;
     // total * 4^-half lies in [1, 4): a normal number, as sums of squares are none or at least 2^-298
@@ -178,23 +191,34 @@ __device__ __forceinline__ float clip_factor(const ClipArgs& g, double total) {
         if (g.norm != nullptr) *g.norm = norm;
         if (!finite) atomicOr(g.flags, kFlagNonfinite);
     }
-    return finite && norm > g.max_norm ? ldexpf(g.max_norm / root, -half) : 1.f;
+    Factor f{1.f, 0.0};
+    if (finite && norm > g.max_norm) {   // (infinity is above every bound)
+        f.by = ldexpf(g.max_norm / root, -half);
+        if (f.by < 0x1p-126f && g.max_norm > 0.f) f.far = ldexp((double)g.max_norm / (double)root, -half);
+    }
+    return f;
 }
 
-__device__ __forceinline__ void scale(const ClipArgs& g, int i, float by) {
+__device__ __forceinline__ void scale(const ClipArgs& g, int i, const Factor& f) {
     const ClipChunk c = g.chunks[i];
-    if (by == 1.f && c.in == c.out) return;
-    if (c.dtype == BP_BF16) scale_chunk<__nv_bfloat16>(c, by);
-    else scale_chunk<float>(c, by);
+    if (f.by == 1.f && c.in == c.out) return;
+    if (f.far != 0.0) {
+        if (c.dtype == BP_BF16) scale_far<__nv_bfloat16>(c, f.far);
+        else scale_far<float>(c, f.far);
+    } else if (c.dtype == BP_BF16) {
+        scale_chunk<__nv_bfloat16>(c, f.by);
+    } else {
+        scale_chunk<float>(c, f.by);
+    }
 }
 
 // Bound by reading the values again and writing them.  (Of 1 GB that the norm has read L2 keeps nothing to speak of: the same time
 // from the last chunk to the first.)
 __global__ void __launch_bounds__(kThreads) k_clip_scale(ClipArgs g) {
     pdl_wait();
-    const float by = clip_factor(g, __ldcg(g.total));
-    if (!g.write || (by == 1.f && g.in_place)) return;
-    for (int i = blockIdx.x; i < g.n_chunks; i += gridDim.x) scale(g, i, by);
+    const Factor f = clip_factor(g, __ldcg(g.total));
+    if (!g.write || (f.by == 1.f && g.in_place)) return;
+    for (int i = blockIdx.x; i < g.n_chunks; i += gridDim.x) scale(g, i, f);
 }
 
 // Few chunks: one launch of one cluster, a CTA a chunk, whose values stay in registers while the CTAs read one
@@ -240,8 +264,11 @@ __device__ __forceinline__ void clip_chunk(const ClipArgs& g, const ClipChunk& c
 #pragma unroll
     for (int r = 0; r < kFewCtas; ++r) total += sums[r];
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // this CTA has read the sums
-    const float by = clip_factor(g, total);
-    if (g.write && !(by == 1.f && c.in == c.out)) {
+    const Factor f = clip_factor(g, total);
+    const float by = f.by;
+    if (g.write && f.far != 0.0) {
+        scale_far<T>(c, f.far);
+    } else if (g.write && !(by == 1.f && c.in == c.out)) {
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const long long at = j * kThreads + threadIdx.x;
