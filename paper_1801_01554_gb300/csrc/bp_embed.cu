@@ -240,12 +240,15 @@ __device__ __forceinline__ void warp_lower_bounds(const IdPlace* keys, int n, un
 }
 
 constexpr int kZeroTokens = 16;   // tokens of a warp that writes zeros
+// Pieces that are added up one after another.  (A plain sum of all of them is off by more the more there are: 32,768 pieces of equal
+// rows by up to 1.8e-4, as every addition rounds the same way.  By 32 it is 2^-24 times 31 for the piece and for each of log32.)
+constexpr int kChain = 32;
 
 // A warp takes kEmbedTile sorted ids and 32 C pieces of their rows (two a lane for bfloat16: 40,001 rows of 1,024 units in 46 us,
 // 48 with one), and adds up runs of equal tokens in registers.
 // A run of at most kEmbedTile ids is summed by the tile that it starts in, also past that tile's end, and is stored at
 // once.  A longer one is cut at the tiles' ends: its pieces go to scratch, and the warp whose piece comes
-// last adds them in order, so that sums do not depend on which that is.  Further warps write the zeros of
+// last adds them up in an order of their own, so that sums do not depend on which that is.  Further warps write the zeros of
 // tokens without ids.  Bound by reading D once and writing G once.
 template <class T, int V, int C>
 __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const IdPlace* keys, long long sum_warps, int slabs) {
@@ -319,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
             b = 32 + __ffs(~more) - 1;   // (at most 31 more)
         }
     }
-    constexpr int B = C > 1 ? 4 : 16, J = 4;     // rows, and pieces of a run, under way
+    constexpr int B = C > 1 ? 4 : 16, J = V == 1 ? 16 : 64 / (V * C);   // rows, and pieces of a run, under way
     const int c0 = (slab * 32 * C + lane) * V;   // and every 32 V columns on
     bool in[C];
 #pragma unroll
@@ -363,22 +366,34 @@ __global__ void __launch_bounds__(kThreads, 2) k_embed_sums(EmbedArgs g, const I
         mine = __shfl_sync(0xffffffffu, mine, 0);
         if (mine != (unsigned)(to - from)) return;
         __threadfence();
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-            if (in[c]) load_floats_l2<V>(piece_of(2 * from + 1, c), acc[c]);
-        for (int t = from + 1; t <= to; t += J) {
-            float x[J][C][V] = {};
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int c = 0; c < C; ++c)
-                    if (t + j <= to && in[c]) load_floats_l2<V>(piece_of(2 * (t + j), c), x[j][c]);
-#pragma unroll
-            for (int j = 0; j < J; ++j)
+        // kChain at a time, each sum in the place of its first piece, until one is left: a lane reads what it wrote.
+        const int pieces = to - from + 1;
+        const auto place_of_piece = [&](int q) { return q == 0 ? 2 * from + 1 : 2 * (from + q); };
+        for (int step = 1; step < pieces; step *= kChain) {
+            for (int q0 = 0; q0 < pieces; q0 += step * kChain) {
+                const int end = min(pieces, q0 + step * kChain);
 #pragma unroll
                 for (int c = 0; c < C; ++c)
+                    if (in[c]) load_floats_l2<V>(piece_of(place_of_piece(q0), c), acc[c]);
+                for (int q = q0 + step; q < end; q += J * step) {
+                    float x[J][C][V] = {};
 #pragma unroll
-                    for (int i = 0; i < V; ++i) acc[c][i] += x[j][c][i];
+                    for (int j = 0; j < J; ++j)
+#pragma unroll
+                        for (int c = 0; c < C; ++c)
+                            if (q + j * step < end && in[c]) load_floats_l2<V>(piece_of(2 * (from + q + j * step), c), x[j][c]);
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+#pragma unroll
+                        for (int c = 0; c < C; ++c)
+#pragma unroll
+                            for (int i = 0; i < V; ++i) acc[c][i] += x[j][c][i];
+                }
+                if (step * kChain >= pieces) break;   // the last sum
+#pragma unroll
+                for (int c = 0; c < C; ++c)
+                    if (in[c]) store_floats<V>(piece_of(place_of_piece(q0), c), acc[c]);
+            }
         }
         write(token);
     };
