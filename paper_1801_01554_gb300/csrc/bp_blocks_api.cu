@@ -180,10 +180,13 @@ bp_status bp_residual_create(int width, int dtype, int max_rows, int max_gates, 
         const size_t w = width, workers = residual_workers(l->a.num_sms, width, dtype) * w;
         const size_t records = workers + max_gates * w;
         const bool layer = norm_out == BP_NORM_LAYER || norm_in == BP_NORM_LAYER;
-        st = make_array(&l->sums, (layer ? 2 : 1) * (records + 2 * workers), call);
+        st = make_array(&l->sums, (layer ? 2 : 1) * (records + 8 * workers), call);
         float* p = l->sums;
         const auto take = [&](size_t n) { return p += n, p - n; };
+        const auto take64 = [&] { return reinterpret_cast<double*>(take(2 * workers)); };   // (first: 8-byte boundaries)
         if (st == BP_OK) {
+            l->a.A_run = take64(), l->a.W_run = take64(), l->a.C_run = take64();
+            if (layer) l->a.B_run = take64(), l->a.WB_run = take64(), l->a.D_run = take64();
             l->a.A = take(records), l->a.W = take(workers), l->a.C = take(workers);
             if (layer) l->a.B = take(records), l->a.WB = take(workers), l->a.D = take(workers);
         }

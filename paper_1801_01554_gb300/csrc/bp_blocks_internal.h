@@ -51,6 +51,7 @@ struct ResidualArgs {
     // that number), and W, WB [workers, width]: the same times scale * gate, over the worker's rows.  C, D
     // [blocks, width]: of dH y^ and dH.
     float *A, *B, *W, *WB, *C, *D;
+    double *A_run, *B_run, *W_run, *WB_run, *C_run, *D_run;   // [workers, width] each: sums of a worker's rows but for the last run of them
     int worker_warps, workers, workers_a_block;   // (set by the launchers)
     int* flags;
 };

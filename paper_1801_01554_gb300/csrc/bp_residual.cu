@@ -11,7 +11,11 @@ constexpr int kSums = 16;        // of the reductions between two barriers, at m
 constexpr int kRed = 32 * kSums;
 // Warps of a block, one block an SM: as many as its registers are enough for (64, 80 or 128 a thread).
 constexpr int block_warps(bool back, bool mean, int v, int c) { return back || v * c > 8 || (mean && c > 1) ? 16 : mean ? 24 : 32; }
-constexpr int kWorkerRows = 4;   // of a worker of the backward pass, at least: its sums by column are added up at the end
+constexpr int kWorkerRows = 4;   // the backward pass has a worker for every so many rows, up to the device's: their sums by column are joined at the end
+// Rows whose sums by column are added up in registers; then they go on to float64 sums.  (A worker may have millions of rows: 3,290 equal
+// ones in one float32 sum were off by 3e-5, as every addition rounds the same way.  300,000 rows of 1,024 bfloat16 units take 585 us going
+// back, 572 without float64 sums; calls of fewer rows a worker reach none.)
+constexpr int kRunRows = 128;
 
 // A worker is `warps` warps that take a row at a time, a thread C pieces of V columns; a block has one or more.
 // (With narrow rows a worker is a warp, whose reductions need no barrier.)
@@ -435,7 +439,7 @@ __global__ void __maxnreg__(65536 / (32 * block_warps(false, MEAN, V, C)) / 8 * 
 //   dy = dY + r_y (e - mean(e) - y^ mean(e y^)),   dF = r_f (k dy - mean(k dy) - f^ mean(k dy f^))
 // (means of e and k dy for BP_NORM_LAYER only).  dy is linear in the first two means, so those of k dy are
 // sums that need not wait for them: one reduction a row.  The sums by column stay in registers over a
-// worker's rows: of dy f^ and dy (what gates and output weights want, by stretch where gates are by range), of dH y^
+// run of a worker's rows: of dy f^ and dy (what gates and output weights want, by stretch where gates are by range), of dH y^
 // and dH.  Bound by reading Y, F, dY and dH once and writing dX and dF once.
 template <class T, int V, int C, bool MEAN, bool FULL>
 __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs g) {
@@ -500,32 +504,43 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
         keep(x, wi_all, P);
     }
     float A[Z][Q] = {}, B[MEAN ? Z : 1][MEAN ? Q : 1] = {}, CI[Z][Q] = {}, D[MEAN ? Z : 1][MEAN ? Q : 1] = {};
-    bool fresh = true;   // nothing of this worker in W and WB
+    // What there is of earlier rows: sums of A and B, of C and D, and of W and WB; and whether a stretch ends at `stop`.
+    enum : unsigned { kRanOut = 1u, kRanIn = 2u, kWeights = 4u, kEnds = 8u };
+    unsigned state = kEnds;
+    const auto each_column = [&](const auto& f) {   // f(value, its place in a row of sums by worker)
+#pragma unroll
+        for (int c = 0; c < P; ++c)
+            if (cols.in(c / V)) f(c, (size_t)mine * g.width + cols.at(c / V) + c % V);
+    };
+    const auto to_run = [&](auto& acc, double* run, bool ran) {
+        each_column([&](int c, size_t at) {
+            run[at] = (ran ? run[at] : 0.0) + (double)acc[c / Q][c % Q];
+            acc[c / Q][c % Q] = 0.f;
+        });
+    };
+    const auto with_run = [&](auto& acc, const double* run, bool ran) {
+        if (ran) each_column([&](int c, size_t at) { acc[c / Q][c % Q] = (float)(run[at] + (double)acc[c / Q][c % Q]); });
+    };
     // Gates by range: the sums of a stretch to its record, and times scale * gate to this worker's part of the weights'
     // gradients.
-    const auto flush = [&](int seg) {
+    const auto flush = [&](int seg, bool last) {
         float q[P];
         load_gate(g, cols, seg, q);
-#pragma unroll
-        for (int j = 0; j < C; ++j) {
-            if (!cols.in(j)) continue;
-            const size_t row = (size_t)mine * g.width + cols.at(j), rec = row + (size_t)max(seg, 0) * g.width;
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = j * V + i;
-                float& a = A[c / Q][c % Q];
-                if (seg >= 0 && g.Ggate != nullptr) g.A[rec + i] = a;
-                if (g.Gwo != nullptr) g.W[row + i] = (fresh ? 0.f : g.W[row + i]) + q[c] * a;
-                a = 0.f;
-                if constexpr (MEAN) {
-                    float& b = B[c / Q][c % Q];
-                    if (seg >= 0 && g.Ggate != nullptr) g.B[rec + i] = b;
-                    if (g.Gbo != nullptr) g.WB[row + i] = (fresh ? 0.f : g.WB[row + i]) + q[c] * b;
-                    b = 0.f;
-                }
-            }
-        }
-        fresh = false;
+        const auto take = [&](auto& acc, const double* run, const float* gates, float* records, const float* weights, double* weights_run, float* out) {
+            with_run(acc, run, state & kRanOut);
+            each_column([&](int c, size_t at) {
+                const float x = acc[c / Q][c % Q];
+                acc[c / Q][c % Q] = 0.f;
+                if (seg >= 0 && gates != nullptr) records[at + (size_t)seg * g.width] = x;
+                if (weights == nullptr) return;
+                const double sum = (state & kWeights ? weights_run[at] : 0.0) + (double)(q[c] * x);
+                if (last) out[at] = (float)sum;
+                else weights_run[at] = sum;
+            });
+        };
+        take(A, g.A_run, g.Ggate, g.A, g.Gwo, g.W_run, g.W);
+        if constexpr (MEAN) take(B, g.B_run, g.Ggate, g.B, g.Gbo, g.WB_run, g.WB);
+        state = (state & ~kRanOut) | kWeights;
     };
     Sums<N> sums(w);
     float next[4] = {};   // the row's statistics
@@ -534,16 +549,31 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
         for (int i = 0; i < 4; ++i) next[i] = __ldg(g.stats + (size_t)r * 4 + i);
     };
     if (r0 < r1) load_stats(r0);
-    Stretch now{0, r0};
+    int stop = r0, seg = 0;   // stop: the row that begins a stretch or a run
     for (int r = r0; r < r1; ++r) {
-        if (r >= now.end) {
-            if (r > r0) flush(now.seg);
-            now = stretch_of(g, r);
-            float x[P], wo[P];
-            load_gate(g, cols, now.seg, x);
-            load_floats(cols, g.wo, 1.f, wo);
-            mul(x, x, wo);
-            keep(x, k_all, 0);
+        if (r == stop) {
+            const Stretch now = stretch_of(g, r);
+            const int of_run = (r - r0) % kRunRows, run_end = r + kRunRows - of_run;
+            if (state & kEnds) {
+                if (r > r0) flush(seg, false);
+                float x[P], wo[P];
+                load_gate(g, cols, now.seg, x);
+                load_floats(cols, g.wo, 1.f, wo);
+                mul(x, x, wo);
+                keep(x, k_all, 0);
+            } else {
+                to_run(A, g.A_run, state & kRanOut);
+                if constexpr (MEAN) to_run(B, g.B_run, state & kRanOut);
+                state |= kRanOut;
+            }
+            if (r > r0 && of_run == 0) {
+                to_run(CI, g.C_run, state & kRanIn);
+                if constexpr (MEAN) to_run(D, g.D_run, state & kRanIn);
+                state |= kRanIn;
+            }
+            seg = now.seg;
+            stop = min(now.end, run_end);
+            state = now.end <= run_end ? state | kEnds : state & ~kEnds;
         }
         const float mf = next[0], rf = next[1], my = next[2], ry = next[3];
         if (r + 1 < r1) load_stats(r + 1);
@@ -616,7 +646,13 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
         ask();   // (the row's values are in registers)
         dX += g.width, dF += g.width;
     }
-    if (by_range && live && (g.Gwo != nullptr || g.Gbo != nullptr || g.Ggate != nullptr)) flush(now.seg);
+    if (by_range && live && (g.Gwo != nullptr || g.Gbo != nullptr || g.Ggate != nullptr)) flush(seg, true);
+    with_run(A, g.A_run, state & kRanOut);
+    with_run(CI, g.C_run, state & kRanIn);
+    if constexpr (MEAN) {
+        with_run(B, g.B_run, state & kRanOut);
+        with_run(D, g.D_run, state & kRanIn);
+    }
     // The block's sums over its rows.
     const auto put = [&](const auto& acc, float* to) {
         if (g.workers_a_block == 1) {
