@@ -84,7 +84,8 @@ void bp_residual_destroy(bp_residual* stream);   /* NULL-safe; synchronises the 
  * d_wo, d_wi [width]: NULL is 1; d_bo, d_bi [width], BP_NORM_LAYER only: NULL is 0.
  * d_gate [n_gates, width] or NULL (1; n_gates 0): row t has the gates g with d_offsets[g] <= t <
  * d_offsets[g + 1], d_offsets [n_gates + 1] on the device, from 0 to n; d_offsets NULL: one row of gates,
- * for all.  Rows outside every range have gates of 0; offsets that do not ascend or leave [0, n] are
+ * for all.  Rows outside every range have gates of 0 and nothing of f, whatever lies there (a NaN too): their y is x, their d_dF is
+ * zeros, and they have no part in d_Gwo, d_Gbo and d_Ggate.  Offsets that do not ascend or leave [0, n] are
  * latched for bp_residual_check (results then mean nothing, and stay inside their buffers).
  * d_stats [n, 4] or NULL: mean and 1 / sqrt(...) of f, then of y, for the backward pass (0 and 1 where there
  * is no such norm; the mean is 0 for BP_NORM_RMS).

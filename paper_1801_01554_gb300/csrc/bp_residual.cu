@@ -376,10 +376,11 @@ __global__ void __maxnreg__(65536 / (32 * block_warps(false, MEAN, V, C)) / 8 * 
     load_floats(cols, g.wi, 1.f, wi);
     if constexpr (MEAN) load_floats(cols, g.bi, 0.f, bi);
     NormStats<MEAN, V, C> of_f(w, 0, g.width), of_y(w, 4, g.width);
-    Stretch now{0, r0};
+    int end = r0;   // of the stretch, or ~end of one that no range has (which takes no further register)
     for (int r = r0; r < r1; ++r) {
-        if (r >= now.end) {
-            now = stretch_of(g, r);
+        if (r >= (end ^ (end >> 31))) {
+            const Stretch now = stretch_of(g, r);
+            end = now.seg >= 0 ? now.end : ~now.end;
             load_gate(g, cols, now.seg, k);
             if constexpr (MEAN) {
                 load_floats(cols, g.bo, 0.f, kb);
@@ -408,6 +409,7 @@ __global__ void __maxnreg__(65536 / (32 * block_warps(false, MEAN, V, C)) / 8 * 
             fma(y, k, u, y);
             if constexpr (MEAN) fma(y, kb, Same{1.f}, y);
             round_to<T, V, C>(y, p);
+            if (end < 0) ring.take(cols, true, slot, 0, p);   // a row of no range is x, also where f is not a number
             values<T, V, C>(p, y);
         } else {
             round_to<T, V, C>(y, p);
@@ -529,7 +531,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
         const auto take = [&](auto& acc, const double* run, const float* gates, float* records, const float* weights, double* weights_run, float* out) {
             with_run(acc, run, state & kRanOut);
             each_column([&](int c, size_t at) {
-                const float x = acc[c / Q][c % Q];
+                const float x = seg >= 0 ? acc[c / Q][c % Q] : 0.f;
                 acc[c / Q][c % Q] = 0.f;
                 if (seg >= 0 && gates != nullptr) records[at + (size_t)seg * g.width] = x;
                 if (weights == nullptr) return;
@@ -575,6 +577,7 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
             stop = min(now.end, run_end);
             state = now.end <= run_end ? state | kEnds : state & ~kEnds;
         }
+        const bool none = seg < 0;   // a row of no range has no part in f's gradients, also where f is not a number
         const float mf = next[0], rf = next[1], my = next[2], ry = next[3];
         if (r + 1 < r1) load_stats(r + 1);
         ring.wait();
@@ -640,6 +643,9 @@ __global__ void __launch_bounds__(kMaxThreads) k_residual_backward(ResidualArgs 
                 fma(av, fv, Same{-rf * d1}, av);
                 if constexpr (MEAN) sub(av, av, rf * d0);
                 round_to<T, V, JC>(av, p);
+                if (none)
+#pragma unroll
+                    for (int i = 0; i < JC; ++i) p[i].u = make_uint4(0u, 0u, 0u, 0u);
                 store_row<T>(cols, p, dF, z * JC);
             }
         }
