@@ -18,7 +18,8 @@
  *     one current are refused (BP_EINVAL).
  *   - Handles own scratch that each call reuses: calls on one handle, and graphs captured from
  *     them, belong on one stream at a time.  Compute calls allocate nothing and may be captured.
- *   - Results do not depend on the launch: every sum has one order for given sizes.
+ *   - A call has the same bits on every run: the order of its sums depends on its sizes, ids and offsets, on whether
+ *     its float32 buffers lie on 16-byte boundaries, and on the device's number of SMs, and on nothing else.
  */
 #ifndef BP_BLOCKS_H
 #define BP_BLOCKS_H
@@ -35,7 +36,7 @@ typedef struct bp_clip bp_clip;
 
 #define BP_MAX_TOKENS (1 << 24)   /* rows of a table */
 #define BP_MAX_IDS (1 << 26)      /* ids of one call */
-#define BP_MAX_WIDTH 8192         /* units of a residual stream */
+#define BP_MAX_WIDTH 8192         /* units of a residual stream: 16 for each of the 512 threads that keep a row's weights */
 #define BP_MAX_TENSORS 65535      /* changes that are clipped together */
 
 /* A table of n_tokens rows of `width` units, for up to max_ids ids a call.

@@ -759,7 +759,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) k_residual_join(ResidualArgs 
 
 // How rows of `width` are shared out: pieces of v values, c of them a thread, `warps` a worker, `workers` a block; one block
 // an SM.  Going forward, 8 values a thread where a row has them for more than
-// 32 threads (16,000 rows of 600 float32 units, layer norms: 39 us, 50 with 4), 16 from 4,096 bytes on: what a thread does once a row (its part of
+// 32 threads (16,000 rows of 600 float32 units, layer norms: 39 us, 50 with 4), 16 above 2,048 units: what a thread does once a row (its part of
 // two reductions, addresses) is a third of its instructions then (16,384 rows of 4,096 bfloat16 units: 88.7 us, 6.05 TB/s;
 // 98.5 us with 8).  Backward that would take more registers than 512 threads have, and half the threads are no faster
 // (143 us, 5.6 TB/s, with 8 values and 512 threads; the same with 16 and 256).
